@@ -481,6 +481,59 @@ NNT_API int32_t nnt_embedding_bwd(nnt_ctx* ctx, const int32_t* tokens, nnt_tenso
 NNT_API int32_t nnt_cross_entropy(nnt_ctx* ctx, nnt_tensor* X, const int32_t* labels, nnt_tensor* stats,
                           float* losses, float* loss);
 
+/* Log-probabilities of given tokens under logits split into tiles, in one read of the logits, which stay as
+ * they are: logp[s,b] = x[c,s,b] - log(sum_j exp(x[j,s,b])), c = labels[s + N_s * b].
+ * X: [N_v, N_s, N_b] logits, fp32 or bf16; labels: device pointer to N_s * N_b int32; a label outside
+ * [0, N_v) marks a position without one (a prompt, padding): its logits are not read and its logp is 0.
+ * logp: fp32 [N_s, N_b] tensor tiled like X's other axes, overwritten.  It is taken in 64 bits from the
+ * fp32 statistics of the column and rounded once.  At most 2^20 vectors of 16 bytes in a column, counted per vocabulary tile
+ * (4 M fp32 or 8 M bf16 logits), and 2^22 - 1 positions.  One task whatever the context's granularity, as for
+ * the two losses below. */
+NNT_API int32_t nnt_token_logprob(nnt_ctx* ctx, nnt_tensor* X, const int32_t* labels, nnt_tensor* logp);
+
+#define NNT_REDUCE_SUM        0   /* plain sum (as nnt_cross_entropy)                                        */
+#define NNT_REDUCE_TOKENS     1   /* divided by the number of positions with a label                         */
+#define NNT_REDUCE_SEQUENCES  2   /* mean over a sequence's positions with a label, then mean over the
+                                     sequences that have any (pairs: mean over the pairs)                    */
+
+/* Clipped policy loss with a KL term, and its gradient with respect to the logits, in one read of them: with r =
+ * exp(logp - old_logp), k = ref_logp - logp and the position's weight w that `reduction` gives,
+ *   loss(s,b) = w (-min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A) + kl_coef (exp(k) - k - 1)),
+ *   dX[j,s,b] = dloss/dlogp ([j = label] - softmax(x)[j]),
+ *   dloss/dlogp = w (-r A where the unclipped term is the smaller one (or both are alike), else 0, + kl_coef (1 - exp(k))).
+ * X, labels, logp as for nnt_token_logprob; positions without a label have loss and gradient 0, whatever the
+ * other inputs hold there.  old_logp, ref_logp, advantages: fp32 [N_s, N_b] tensors tiled like X's other axes;
+ * old_logp NULL: the present logp, r = 1 (one update per batch of samples); ref_logp may be NULL if kl_coef is 0, with
+ * which it is not read; advantages may be [N_b] (one per sequence, tiled like X's last axis).  dX: the gradient, a tensor of
+ * X's type, shape and tiling, X itself (in place), or NULL (loss only).  losses: device buffer of N_s * N_b
+ * floats (the weighted losses), loss: device float, their sum in a fixed order; the caller owns both and must not
+ * reuse them before nnt_wait or a later operation on logp.  0 <= clip_low <= 1, clip_high >= 0, kl_coef >= 0.
+ * Any reduction but the sum uses the context's per-stream scratch, which must exist before a graph capture (run the call once). */
+typedef struct nnt_policy_cfg {
+    double clip_low, clip_high, kl_coef;
+    int32_t reduction;
+} nnt_policy_cfg;
+NNT_API int32_t nnt_policy_loss(nnt_ctx* ctx, const nnt_policy_cfg* cfg, nnt_tensor* X, const int32_t* labels,
+                        nnt_tensor* old_logp, nnt_tensor* ref_logp, nnt_tensor* advantages, nnt_tensor* dX,
+                        nnt_tensor* logp, float* losses, float* loss);
+
+/* Preference loss of pairs of answers, and its gradient with respect to the logits: sequence p of the first half of the batch
+ * is preferred to sequence p + N_b / 2.  With R_b = beta sum_s (logp - ref_logp) over the positions with a label,
+ * z_p = R_p - R_{p + N_b/2}, sig(z) = 1 / (1 + exp(-z)) and the pair's weight w (1, or 2 / N_b with NNT_REDUCE_SEQUENCES),
+ *   loss(p) = w (-(1 - label_smoothing) log sig(z) - label_smoothing log sig(-z)),
+ *   dX[j,s,b] = +-w beta (sig(z) - (1 - label_smoothing)) ([j = label] - softmax(x)[j])   (+ for the preferred one).
+ * A sequence without any label has R = 0.  X, labels, logp, dX as above; N_b even; ref_logp: fp32 [N_s, N_b] or NULL (0).
+ * rewards: device buffer of N_b floats (R), losses: N_b / 2 floats, loss: one float, their sum in a fixed order; same
+ * rule as above.  beta > 0, 0 <= label_smoothing <= 0.5.  The sums over a sequence are in 64 bits.  Uses the context's per-stream
+ * scratch (4 N_s N_b + 2 N_b floats), which must exist before a graph capture. */
+typedef struct nnt_preference_cfg {
+    double beta, label_smoothing;
+    int32_t reduction;
+} nnt_preference_cfg;
+NNT_API int32_t nnt_preference_loss(nnt_ctx* ctx, const nnt_preference_cfg* cfg, nnt_tensor* X, const int32_t* labels,
+                            nnt_tensor* ref_logp, nnt_tensor* dX, nnt_tensor* logp, float* rewards,
+                            float* losses, float* loss);
+
 /* SGD with momentum (section 3, Optimizers: the update is a weighted sum of the
  * parameter, the gradient and the momentum term):
  *   g' = g + weight_decay * p;  v <- momentum * v + g';

@@ -362,6 +362,79 @@ def cross_entropy(X, labels):
     return losses.sum(), losses, dX
 
 
+def token_logprob(X, labels):
+    """logp[s,b] = x[c] - log sum_j exp(x[j]), c = labels[s,b]; 0 where the label is outside [0, N_v)."""
+    X = np.asarray(X, F64)
+    labels = np.asarray(labels)
+    has = (labels >= 0) & (labels < X.shape[0])
+    logp = np.zeros(labels.shape)
+    for s, b in zip(*np.nonzero(has)):
+        x = X[:, s, b]
+        m = x.max()
+        logp[s, b] = x[labels[s, b]] - m - np.log(np.exp(x - m).sum())
+    return logp
+
+
+def logits_gradient(X, labels, g):
+    """dL/dX for a loss that sees the logits through logp only, g = dL/dlogp: g ([j = label] - softmax(x)[j])."""
+    X = np.asarray(X, F64)
+    labels = np.asarray(labels)
+    has = (labels >= 0) & (labels < X.shape[0])
+    dX = np.zeros(X.shape)
+    for s, b in zip(*np.nonzero(has)):
+        e = np.exp(X[:, s, b] - X[:, s, b].max())
+        dX[:, s, b] = -g[s, b] * e / e.sum()
+        dX[labels[s, b], s, b] += g[s, b]
+    return dX
+
+
+def position_weights(has, reduction):
+    """Weights of the labelled positions: "sum" 1, "tokens" 1 / their number, "sequences" the mean over each sequence's and
+    then over the sequences that have any."""
+    has = np.asarray(has, bool)
+    if reduction == "tokens":
+        return has / max(has.sum(), 1)
+    if reduction == "sequences":
+        n = has.sum(axis=0)
+        return has / np.maximum(n, 1) / max((n > 0).sum(), 1)
+    return has.astype(F64)
+
+
+def policy_loss(X, labels, old, ref, adv, clip_low=0.2, clip_high=0.2, kl_coef=0.0, reduction="sum"):
+    """Clipped policy loss with a KL term on logits [N_v, N_s, N_b]; old, ref (None: the present logp; no KL term): [N_s, N_b],
+    adv: [N_s, N_b] or [N_b].  Returns (loss, weighted losses, logp, dloss/dX)."""
+    labels = np.asarray(labels)
+    has = (labels >= 0) & (labels < X.shape[0])
+    logp = token_logprob(X, labels)
+    w = position_weights(has, reduction)
+    A = np.where(has, np.broadcast_to(np.asarray(adv, F64), labels.shape), 0.0)
+    r = np.where(has, np.exp(logp - old), 0.0) if old is not None else has.astype(F64)
+    free, held = r * A, np.clip(r, 1.0 - clip_low, 1.0 + clip_high) * A
+    losses = -np.minimum(free, held)
+    g = np.where(free <= held, -free, 0.0)
+    if kl_coef:
+        k = np.where(has, np.asarray(ref, F64) - logp, 0.0)
+        losses = losses + kl_coef * (np.exp(k) - k - 1.0)
+        g = g + kl_coef * (1.0 - np.exp(k))
+    losses, g = np.where(has, w * losses, 0.0), np.where(has, w * g, 0.0)
+    return losses.sum(), losses, logp, logits_gradient(X, labels, g)
+
+
+def preference_loss(X, labels, ref, beta=0.1, label_smoothing=0.0, mean=False):
+    """Preference loss of the pairs (p, p + N_b / 2).  Returns (loss, losses, rewards, logp, dloss/dX)."""
+    labels = np.asarray(labels)
+    has = (labels >= 0) & (labels < X.shape[0])
+    logp = token_logprob(X, labels)
+    n = labels.shape[1] // 2
+    R = beta * np.where(has, logp - (0.0 if ref is None else ref), 0.0).sum(axis=0)
+    z = R[:n] - R[n:]
+    w = 1.0 / n if mean else 1.0
+    losses = w * ((1.0 - label_smoothing) * np.logaddexp(0.0, -z) + label_smoothing * np.logaddexp(0.0, z))
+    slope = w * beta * (1.0 / (1.0 + np.exp(-z)) - (1.0 - label_smoothing))
+    g = np.where(has, np.concatenate([slope, -slope])[None, :], 0.0)
+    return losses.sum(), losses, R, logp, logits_gradient(X, labels, g)
+
+
 def sgd_step(p, g, v, lr=1e-2, momentum=0.9, weight_decay=0.0, nesterov=False):
     """SGD with momentum (section 3, Optimizers: a weighted sum of parameter, gradient and momentum
     term): g' = g + weight_decay p, v <- momentum v + g', p <- p - lr v; with `nesterov` the step

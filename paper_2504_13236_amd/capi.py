@@ -18,6 +18,7 @@ NNT_F32, NNT_BF16 = 0, 1
 NNT_OP_N, NNT_OP_T = 0, 1
 NNT_GELU_TANH, NNT_GELU_ERF = 0, 1
 NNT_GRAN_OP, NNT_GRAN_TILE = 0, 1
+NNT_REDUCE_SUM, NNT_REDUCE_TOKENS, NNT_REDUCE_SEQUENCES = 0, 1, 2
 NNT_MAX_DIM = 4
 
 _ERR = {NNT_EINVAL: "NNT_EINVAL", NNT_EDTYPE: "NNT_EDTYPE", NNT_EHIP: "NNT_EHIP",
@@ -69,6 +70,14 @@ class nnt_gpt2_block_cfg(C.Structure):
 
 class nnt_sgd_cfg(C.Structure):
     _fields_ = [("lr", C.c_double), ("momentum", C.c_double), ("weight_decay", C.c_double), ("nesterov", C.c_int32)]
+
+
+class nnt_policy_cfg(C.Structure):
+    _fields_ = [("clip_low", C.c_double), ("clip_high", C.c_double), ("kl_coef", C.c_double), ("reduction", C.c_int32)]
+
+
+class nnt_preference_cfg(C.Structure):
+    _fields_ = [("beta", C.c_double), ("label_smoothing", C.c_double), ("reduction", C.c_int32)]
 
 
 class nnt_slot_info(C.Structure):
@@ -169,6 +178,9 @@ PROTOTYPES = {
     "nnt_embedding_fwd": (_i32, [_p, _p, _p, _p]),
     "nnt_embedding_bwd": (_i32, [_p, _p, _p, _p]),
     "nnt_cross_entropy": (_i32, [_p, _p, _p, _p, _p, _p]),
+    "nnt_token_logprob": (_i32, [_p, _p, _p, _p]),
+    "nnt_policy_loss": (_i32, [_p, C.POINTER(nnt_policy_cfg), _p, _p, _p, _p, _p, _p, _p, _p, _p]),
+    "nnt_preference_loss": (_i32, [_p, C.POINTER(nnt_preference_cfg), _p, _p, _p, _p, _p, _p, _p, _p]),
     "nnt_sgd_step": (_i32, [_p, C.POINTER(nnt_sgd_cfg), _p, _p, _p, _p]),
     "nnt_gpt2_block_slot": (_i32, [C.POINTER(nnt_gpt2_block_cfg), _i32, C.POINTER(nnt_slot_info)]),
     "nnt_gpt2_block_create": (_i32, [_p, C.POINTER(nnt_gpt2_block_cfg), _pp, _pp]),

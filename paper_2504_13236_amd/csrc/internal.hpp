@@ -245,6 +245,29 @@ inline bool null_alike(const nnt_tensor* a, const nnt_tensor* b) {
     return true;
 }
 
+// Makes a context's device the current one of the calling thread for as long as it lives.
+struct DeviceScope {
+    int before = -1;
+    explicit DeviceScope(int device) {
+        int now = device;
+        if (hipGetDevice(&now) == hipSuccess && now != device && hipSetDevice(device) == hipSuccess) before = now;
+    }
+    ~DeviceScope() { if (before >= 0) (void)hipSetDevice(before); }
+    DeviceScope(const DeviceScope&) = delete;
+    DeviceScope& operator=(const DeviceScope&) = delete;
+};
+// Runs the body of a C entry point on the context's device; nothing thrown inside leaves it.
+template <typename F>
+int32_t entry(nnt_ctx* ctx, F&& body) {
+    NNT_CHECK_CTX(ctx);
+    try {
+        DeviceScope on(ctx->device);
+        return body();
+    } catch (...) {
+        return NNT_ENOMEM;      // the library itself throws nothing: the host ran out of memory
+    }
+}
+
 // ---- stream-level launchers used both by the tile API and by the tensor ops
 int32_t launch_status(const char* what);
 
