@@ -547,6 +547,43 @@ typedef struct nnt_sgd_cfg {
 NNT_API int32_t nnt_sgd_step(nnt_ctx* ctx, const nnt_sgd_cfg* cfg, nnt_tensor* G, nnt_tensor* P, nnt_tensor* V,
                      nnt_tensor* P_lowp);
 
+/* Orthogonalisation by Newton-Schulz products: for each of n matrices G (at least as many columns as rows; else
+ * everything holds for its transpose)
+ *   X = G / (|G|_F + eps),  then `steps` times  A = X X^T,  X <- a X + (b A + c A^2) X,   O = X,
+ * which drives every singular value of G towards the polynomial's fixed range around 1 and keeps the singular vectors.
+ * G[k], O[k]: tensors of two axes, fp32 or bf16 each, tiled alike, all tiles present; O[k] may be G[k].  Sums and norms are
+ * in 32 bits or more, the factors of the products in two fp16 halves (22 bits): results are about as far from 64 bits as with
+ * fp32 products.  A zero matrix gives zeros; a matrix that holds an infinity or a NaN gives NaN.  eps > 0, 1 <= steps <= 64.
+ * The coefficients must keep singular values, their squares and b s^2 + c s^4 below 8 from any start in [0, 1] (NNT_EINVAL
+ * otherwise); (3.4445, -4.7750, 2.0315) with 5 steps is the usual choice, (1.5, -0.5, 0) the classical one.
+ * As many matrices as fill the chip go through one set of launches; G and O are arrays of n pointers.  One task per
+ * set, whatever the context's granularity; it uses a workspace of the context, about 16 bytes per element of the set's
+ * matrices and 8 per element of their Gram matrices, which must exist before a graph capture (run the call once). */
+typedef struct nnt_newton_schulz_cfg {
+    double a, b, c, eps;
+    int32_t steps;
+} nnt_newton_schulz_cfg;
+NNT_API int32_t nnt_orthogonalize(nnt_ctx* ctx, const nnt_newton_schulz_cfg* cfg, int32_t n, nnt_tensor* const* G,
+                          nnt_tensor* const* O);
+
+#define NNT_MUON_SCALE_NONE   0   /* s = 1                                          */
+#define NNT_MUON_SCALE_ASPECT 1   /* s = sqrt(max(1, rows / columns))               */
+#define NNT_MUON_SCALE_RMS    2   /* s = 0.2 sqrt(max(rows, columns)): updates of about the size of Adam's */
+
+/* One step of the momentum optimiser with orthogonalised updates on n matrices:
+ *   M <- momentum M + G;  U = M (nesterov != 0: G + momentum M);
+ *   O = U orthogonalised as above;  P <- (1 - lr weight_decay) P - lr s O.
+ * G[k], P[k], M[k]: fp32 tensors of two axes, tiled alike, all tiles present, each in one role only; P_lowp: NULL or n
+ * pointers to bf16 tensors tiled alike (or NULL), which receive a copy of the new parameters.  Matrices only: vectors and embeddings go to
+ * nnt_adam_step or nnt_sgd_step. */
+typedef struct nnt_muon_cfg {
+    double lr, momentum, weight_decay;
+    int32_t nesterov, scale;
+    nnt_newton_schulz_cfg iteration;
+} nnt_muon_cfg;
+NNT_API int32_t nnt_muon_step(nnt_ctx* ctx, const nnt_muon_cfg* cfg, int32_t n, nnt_tensor* const* G, nnt_tensor* const* P,
+                      nnt_tensor* const* M, nnt_tensor* const* P_lowp);
+
 /* ------------------------------------------------------------------------- */
 /* One GPT-2 block (pre-LN, biases on all four linear layers, causal attention, */
 /* no dropout): forward, backward and Adam as a flow of the tasks above.        */

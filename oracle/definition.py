@@ -435,6 +435,30 @@ def preference_loss(X, labels, ref, beta=0.1, label_smoothing=0.0, mean=False):
     return losses.sum(), losses, R, logp, logits_gradient(X, labels, g)
 
 
+NEWTON_SCHULZ = dict(a=3.4445, b=-4.7750, c=2.0315, eps=1e-7, steps=5)
+
+
+def orthogonalize(G, a=3.4445, b=-4.7750, c=2.0315, eps=1e-7, steps=5):
+    """Newton-Schulz iteration X <- a X + b (X X^T) X + c (X X^T)^2 X from X = G / (|G|_F + eps), G a matrix of any shape."""
+    G = np.asarray(G, F64)
+    X = G / (np.sqrt((G * G).sum()) + eps)
+    for _ in range(steps):
+        A = X @ X.T if X.shape[0] <= X.shape[1] else X.T @ X
+        B = b * A + c * (A @ A)
+        X = a * X + (B @ X if X.shape[0] <= X.shape[1] else X @ B)
+    return X
+
+
+def muon_step(p, g, m, lr=0.02, momentum=0.95, weight_decay=0.0, nesterov=True, scale="none", **iteration):
+    """Momentum, orthogonalised: returns (new p, new m)."""
+    p, g, m = (np.asarray(x, F64) for x in (p, g, m))
+    m = momentum * m + g
+    O = orthogonalize(g + momentum * m if nesterov else m, **iteration)
+    rows, cols = p.shape
+    s = {"none": 1.0, "aspect": np.sqrt(max(1.0, rows / cols)), "rms": 0.2 * np.sqrt(max(rows, cols))}[scale]
+    return (1.0 - lr * weight_decay) * p - lr * s * O, m
+
+
 def sgd_step(p, g, v, lr=1e-2, momentum=0.9, weight_decay=0.0, nesterov=False):
     """SGD with momentum (section 3, Optimizers: a weighted sum of parameter, gradient and momentum
     term): g' = g + weight_decay p, v <- momentum v + g', p <- p - lr v; with `nesterov` the step

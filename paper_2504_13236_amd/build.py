@@ -40,7 +40,7 @@ FLAGS = [
 # carry their loop's name on the line of their label or on the next one, and the compiler puts blocks out of line.
 IN_FLIGHT_SOURCES = ("gemm_bf16_dl.hip", "gemm_bf16_span.hip", "gemm_f32_dl.hip")
 # Sources with matrix instructions: their assembly is scanned for uses of a result before it is there.
-MATRIX_SOURCES = IN_FLIGHT_SOURCES + ("gemm_bf16.hip", "gemm_f32.hip", "attention.hip")
+MATRIX_SOURCES = IN_FLIGHT_SOURCES + ("gemm_bf16.hip", "gemm_f32.hip", "attention.hip", "newton_schulz.hip")
 
 
 _VREG = re.compile(r"\bv(\d+)\b|\bv\[(\d+):(\d+)\]")
@@ -59,7 +59,7 @@ def _vregs(text: str) -> set:
 # Wait states (instructions, an `s_nop n` counting as n + 1) that have to lie between a matrix instruction and another
 # kind of instruction that names its result: the hardware does not hold such an instruction back.  The numbers
 # are those that the compiler leaves in straight-line code.
-MATRIX_WAIT_STATES = {"v_mfma_f32_32x32x2_f32": 18, "v_mfma_f32_32x32x16_bf16": 12}
+MATRIX_WAIT_STATES = {"v_mfma_f32_32x32x2_f32": 18, "v_mfma_f32_32x32x16_bf16": 12, "v_mfma_f32_32x32x16_f16": 12}
 _ANYREG = re.compile(r"\b([va])(\d+)\b|\b([va])\[(\d+):(\d+)\]")
 
 

@@ -19,6 +19,7 @@ NNT_OP_N, NNT_OP_T = 0, 1
 NNT_GELU_TANH, NNT_GELU_ERF = 0, 1
 NNT_GRAN_OP, NNT_GRAN_TILE = 0, 1
 NNT_REDUCE_SUM, NNT_REDUCE_TOKENS, NNT_REDUCE_SEQUENCES = 0, 1, 2
+NNT_MUON_SCALE_NONE, NNT_MUON_SCALE_ASPECT, NNT_MUON_SCALE_RMS = 0, 1, 2
 NNT_MAX_DIM = 4
 
 _ERR = {NNT_EINVAL: "NNT_EINVAL", NNT_EDTYPE: "NNT_EDTYPE", NNT_EHIP: "NNT_EHIP",
@@ -78,6 +79,15 @@ class nnt_policy_cfg(C.Structure):
 
 class nnt_preference_cfg(C.Structure):
     _fields_ = [("beta", C.c_double), ("label_smoothing", C.c_double), ("reduction", C.c_int32)]
+
+
+class nnt_newton_schulz_cfg(C.Structure):
+    _fields_ = [("a", C.c_double), ("b", C.c_double), ("c", C.c_double), ("eps", C.c_double), ("steps", C.c_int32)]
+
+
+class nnt_muon_cfg(C.Structure):
+    _fields_ = [("lr", C.c_double), ("momentum", C.c_double), ("weight_decay", C.c_double), ("nesterov", C.c_int32), ("scale", C.c_int32),
+                ("iteration", nnt_newton_schulz_cfg)]
 
 
 class nnt_slot_info(C.Structure):
@@ -181,6 +191,8 @@ PROTOTYPES = {
     "nnt_token_logprob": (_i32, [_p, _p, _p, _p]),
     "nnt_policy_loss": (_i32, [_p, C.POINTER(nnt_policy_cfg), _p, _p, _p, _p, _p, _p, _p, _p, _p]),
     "nnt_preference_loss": (_i32, [_p, C.POINTER(nnt_preference_cfg), _p, _p, _p, _p, _p, _p, _p, _p]),
+    "nnt_orthogonalize": (_i32, [_p, C.POINTER(nnt_newton_schulz_cfg), _i32, _pp, _pp]),
+    "nnt_muon_step": (_i32, [_p, C.POINTER(nnt_muon_cfg), _i32, _pp, _pp, _pp, _pp]),
     "nnt_sgd_step": (_i32, [_p, C.POINTER(nnt_sgd_cfg), _p, _p, _p, _p]),
     "nnt_gpt2_block_slot": (_i32, [C.POINTER(nnt_gpt2_block_cfg), _i32, C.POINTER(nnt_slot_info)]),
     "nnt_gpt2_block_create": (_i32, [_p, C.POINTER(nnt_gpt2_block_cfg), _pp, _pp]),

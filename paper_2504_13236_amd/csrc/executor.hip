@@ -336,6 +336,10 @@ int32_t ensure_stream_scratch(nnt_ctx* ctx, int64_t elems) {
     return grow_scratch(ctx, &ctx->stream_scratch, &ctx->stream_scratch_elems, &ctx->stream_mem, elems, ctx->n_streams);
 }
 
+int32_t ensure_matrix_scratch(nnt_ctx* ctx, int64_t bytes) {
+    return grow_scratch(ctx, &ctx->matrix_scratch, &ctx->matrix_scratch_elems, &ctx->matrix_mem, (bytes + 3) / 4, 1);
+}
+
 }  // namespace nnt
 
 using namespace nnt;
@@ -344,7 +348,7 @@ struct nnt_graph {
     nnt_ctx* ctx;
     hipGraph_t graph;
     hipGraphExec_t exec;
-    std::shared_ptr<Scratch> mem[3];     // what its tasks write partial sums and operands to: kept also where the context takes larger buffers
+    std::shared_ptr<Scratch> mem[4];     // what its tasks write partial sums and operands to: kept also where the context takes larger buffers
 };
 
 extern "C" {
@@ -493,7 +497,8 @@ int32_t nnt_ctx_stats(nnt_ctx* ctx, nnt_exec_stats* out) {
     *out = ctx->stats;
     out->plans = (int64_t)ctx->gemm_plans.size();
     out->device_table_bytes = ctx->table_bytes;
-    out->device_workspace_bytes = (ctx->red_mem ? ctx->red_mem->bytes : 0) + (ctx->stream_mem ? ctx->stream_mem->bytes : 0);
+    out->device_workspace_bytes = (ctx->red_mem ? ctx->red_mem->bytes : 0) + (ctx->stream_mem ? ctx->stream_mem->bytes : 0) +
+                                  (ctx->matrix_mem ? ctx->matrix_mem->bytes : 0);
     if (const std::shared_ptr<PackSpace> pack = ctx->pack_space.lock()) out->device_workspace_bytes += pack->mem->bytes;
     for (const std::weak_ptr<Scratch>& w : ctx->replaced_mem)
         if (const std::shared_ptr<Scratch> m = w.lock()) out->device_workspace_bytes += m->bytes;
@@ -590,7 +595,7 @@ int32_t nnt_capture_end(nnt_ctx* ctx, nnt_graph** out) {
     NNT_HIP(ctx, hipGraphInstantiate(&exec, graph, nullptr, nullptr, 0));
     if (trace) fprintf(stderr, "nnt: capture_end: instantiated\n");
     const std::shared_ptr<PackSpace> pack = ctx->pack_space.lock();
-    nnt_graph* g = new (std::nothrow) nnt_graph{ctx, graph, exec, {ctx->red_mem, ctx->stream_mem, pack ? pack->mem : nullptr}};
+    nnt_graph* g = new (std::nothrow) nnt_graph{ctx, graph, exec, {ctx->red_mem, ctx->stream_mem, pack ? pack->mem : nullptr, ctx->matrix_mem}};
     if (!g) return NNT_ENOMEM;
     *out = g;
     return NNT_OK;

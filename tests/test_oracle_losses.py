@@ -1,5 +1,5 @@
-"""Pins of the oracle's losses on given tokens that do not go through the oracle: CPU torch in float64 with autograd, closed
-forms and finite differences."""
+"""Pins of the oracle's losses on given tokens and of its matrix-wise optimiser that do not go through the oracle: CPU torch in float64 with
+autograd, closed forms, singular values and finite differences."""
 import math
 
 import numpy as np
@@ -92,3 +92,38 @@ def test_preference_loss_against_autograd_and_differences(mean, soft):
         M[at] -= 1e-6
         fd = (D.preference_loss(P, lab, ref, 0.5, soft, mean)[0] - D.preference_loss(M, lab, ref, 0.5, soft, mean)[0]) / 2e-6
         assert abs(fd - dX[at]) < 1e-8
+
+
+# ------------------------------------------------------------------ Newton-Schulz iteration
+@pytest.mark.parametrize("shape", [(1, 1), (1, 9), (7, 7), (5, 12), (12, 5)])
+def test_orthogonalize_acts_on_singular_values_only(shape):
+    """O = U f(S) V^T with the scalar iteration f, whatever the shape; O(G^T) = O(G)^T; scaling of G does not matter."""
+    r = np.random.default_rng(5)
+    G = r.standard_normal(shape)
+    U, S, Vt = np.linalg.svd(G, full_matrices=False)
+    s = S / (np.linalg.norm(S) + 1e-7)
+    for _ in range(5):
+        s = 3.4445 * s - 4.7750 * s ** 3 + 2.0315 * s ** 5
+    O = D.orthogonalize(G)
+    np.testing.assert_allclose(O, (U * s) @ Vt, atol=1e-10)
+    np.testing.assert_allclose(D.orthogonalize(G.T), O.T, atol=1e-10)
+    np.testing.assert_allclose(D.orthogonalize(100.0 * G), O, atol=1e-6)
+    assert not D.orthogonalize(np.zeros(shape)).any()
+
+
+def test_orthogonalize_cubic_iteration_reaches_the_polar_factor():
+    G = np.random.default_rng(6).standard_normal((6, 9))
+    U, _, Vt = np.linalg.svd(G, full_matrices=False)
+    np.testing.assert_allclose(D.orthogonalize(G, 1.5, -0.5, 0.0, 1e-12, 40), U @ Vt, atol=1e-10)
+
+
+def test_muon_step_by_hand():
+    r = np.random.default_rng(7)
+    p, g, m = (r.standard_normal((8, 3)) for _ in range(3))
+    q, n = D.muon_step(p, g, m, 0.1, 0.9, 0.01, True, "aspect")
+    np.testing.assert_allclose(n, 0.9 * m + g)
+    np.testing.assert_allclose(q, 0.999 * p - 0.1 * math.sqrt(8 / 3) * D.orthogonalize(g + 0.9 * n), atol=1e-14)
+    q, _ = D.muon_step(p, g, m, 0.1, 0.9, 0.0, False, "rms")
+    np.testing.assert_allclose(q, p - 0.1 * 0.2 * math.sqrt(8) * D.orthogonalize(n), atol=1e-14)
+    q, _ = D.muon_step(p.T, g.T, m.T, 0.1, 0.0, 0.0, False, "aspect")
+    np.testing.assert_allclose(q, (p - 0.1 * D.orthogonalize(g)).T, atol=1e-14)
