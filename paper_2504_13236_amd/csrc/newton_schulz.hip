@@ -11,13 +11,14 @@
 // results are as far from 64 bits as those of fp32 products to within a small factor.  2^12 keeps both halves of the entries that matter
 // away from fp16's smallest numbers and leaves room up to 16; what the iteration's polynomials can reach is checked by the caller.
 //
-// All operands of the products lie in the workspace as panels: 64 rows x 32 columns of the contraction, hi part and lo part of 4 KB each,
+// All operands of the products lie in the workspace as panels: 64 rows x 16 columns of the contraction, hi part and lo part of 2 KB each,
 // inside them eight columns of a row next to each other (16 bytes), 64 rows of those, then the next eight columns.  That is the
-// image that the products want in LDS, so loads are contiguous, and a matrix instruction's operand is one 16-byte LDS read per lane
-// without bank conflicts.  Every product has the contraction along the columns of both operands: A = X X^T and A^2 = A A^T anyway, and B X
+// image that the products want in LDS, so loads go straight there in runs of 4 KB, and a matrix instruction's operand is one 16-byte LDS
+// read per lane without bank conflicts.  Every product has the contraction along the columns of both operands: A = X X^T and A^2 = A A^T anyway, and B X
 // reads X as its transpose, which the step before (or the set-up) has written beside X itself.  Rows and columns are padded with zeros to whole
 // tiles; zeros stay zeros through the iteration.
 #include "device_util.hpp"
+#include "gemm_dl_common.hpp"
 #include "internal.hpp"
 #include "raw_vec.hpp"
 
@@ -33,7 +34,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kGroupMatrices = 16;        // matrices of one set of launches
 constexpr int kNormBlocks = 512;          // most partial sums of a matrix's norm
 constexpr float kScale = 4096.f;          // 2^12
-constexpr int kPanelBytes = 8192;         // 64 rows x 32 columns, both parts
+constexpr int kPanelBytes = 4096;         // 64 rows x 16 columns, both parts
+constexpr int kPartBytes = 2048;
 
 // A matrix as a tiled tensor of two axes.
 struct MatView {
@@ -44,84 +46,121 @@ struct MatView {
 struct NsMatrix {
     int32_t rows, cols, base0, base1, grid0, grid1;      // the tensors' geometry
     int32_t flip;                                        // X is the transpose (more rows than columns)
-    int32_t mp, np;                                      // X's padded extents, mp <= np up to padding
-    int32_t first_sym, first_full, first_patch;          // workgroups of the matrices before it, per kind of launch
+    int32_t mp, np;                                      // X's extents, mp <= np, padded to whole panels of 64 rows
     int64_t X, XT, A, B, part;                           // bytes from the start of the workspace; X and XT: two buffers each, one behind the other
     MatView G, M, P, LP;                                 // gradient, momentum, parameter (or result), bf16 copy
     float decay, step;                                   // P <- decay P - step X (step < 0: P <- X)
 };
 
+// The matrices' sizes, an argument of every launch.
+struct NsSizes {
+    int32_t n;
+    uint32_t blocks[kGroupMatrices];                     // mp / 64 and np / 64, 16 bits each
+};
+
+// Written to the start of the workspace by the first launch, so that the others have short arguments (a launch with all 2.6 KB of it takes the host
+// 0.6 us longer).
 struct NsGroup {
     char* space;
     int32_t n, norm_blocks, nesterov;
     float mu;                                            // < 0: no momentum, U = G
     float a, b, c, eps;
+    int64_t partial;                                     // parts of A's tiles, bytes from the start of the workspace
     NsMatrix mat[kGroupMatrices];
 };
+
+static_assert(sizeof(NsGroup) <= 4096 && sizeof(NsGroup) % 4 == 0, "copied by one workgroup, a word to a thread");
 
 __device__ __forceinline__ float load_of(const MatView& v, int tile, int64_t off) {
     return v.dtype == NNT_F32 ? global_as<const float>(v.tiles[tile])[off] : bf2f(global_as<const bf16_t>(v.tiles[tile])[off]);
 }
 
 // ---------------------------------------------------------------- momentum and norm
-// Workgroups take chunks of 2048 elements of a tile in turn; each leaves one partial sum of squares in 64 bits (no value of fp32 overflows or
-// vanishes in it).
-__global__ void __launch_bounds__(256) ns_norm_kernel(NsGroup g) {
-    __shared__ double red[4];
+// Workgroups take chunks of 8192 elements of a tile in turn, eight to a thread; each leaves one partial sum of squares in 64 bits (no value of
+// fp32 overflows or vanishes in it).
+constexpr int kNormChunk = 8192;
+__global__ void __launch_bounds__(1024) ns_norm_kernel(NsGroup g) {
+    __shared__ double red[16];
+    // the launches behind this one read the group from the workspace
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < sizeof(NsGroup) / 4)
+        reinterpret_cast<uint32_t*>(g.space)[threadIdx.x] = reinterpret_cast<const uint32_t*>(&g)[threadIdx.x];
     const NsMatrix& q = g.mat[blockIdx.y];
     const int tid = threadIdx.x;
-    constexpr int kChunk = 2048;
     const int64_t full = (int64_t)q.base0 * q.base1;
-    const int per_tile = (int)((full + kChunk - 1) / kChunk);
+    const int per_tile = (int)((full + kNormChunk - 1) / kNormChunk);
     const int64_t chunks = (int64_t)per_tile * q.grid0 * q.grid1;
     double sum = 0.0;
     for (int64_t ch = blockIdx.x; ch < chunks; ch += gridDim.x) {
         const int tile = (int)(ch / per_tile);
         const int t0 = tile % q.grid0, t1 = tile / q.grid0;
         const int64_t numel = (int64_t)min(q.base0, q.rows - t0 * q.base0) * min(q.base1, q.cols - t1 * q.base1);
-        const int64_t at = (ch - (int64_t)tile * per_tile) * kChunk;
+        const int64_t at = (ch - (int64_t)tile * per_tile) * kNormChunk + tid * 4;
+        float u[2][4];
+        RawVec<float> m[2];
+        int cnt[2];
+        float* mp = g.mu >= 0.f ? global_as<float>(q.M.tiles[tile]) : nullptr;
 #pragma unroll
         for (int s = 0; s < 2; s++) {
-            const int64_t e = at + (s * 256 + tid) * 4;
-            if (e >= numel) continue;
-            const int cnt = (int)min((int64_t)4, numel - e);
-            float u[4];
+            const int64_t e = at + s * 4096;
+            cnt[s] = e < numel ? (int)min((int64_t)4, numel - e) : 0;
+            if (cnt[s] == 0) continue;
             if (q.G.dtype == NNT_F32) {
                 RawVec<float> x;
-                x.load(global_as<const float>(q.G.tiles[tile]) + e, cnt);
+                x.load(global_as<const float>(q.G.tiles[tile]) + e, cnt[s]);
 #pragma unroll
-                for (int k = 0; k < 4; k++) u[k] = x.at(k);
+                for (int k = 0; k < 4; k++) u[s][k] = x.at(k);
             } else {
 #pragma unroll
-                for (int k = 0; k < 4; k++) u[k] = k < cnt ? bf2f(global_as<const bf16_t>(q.G.tiles[tile])[e + k]) : 0.f;
+                for (int k = 0; k < 4; k++) u[s][k] = k < cnt[s] ? bf2f(global_as<const bf16_t>(q.G.tiles[tile])[e + k]) : 0.f;
             }
-            if (g.mu >= 0.f) {
-                float* mp = global_as<float>(q.M.tiles[tile]) + e;
-                RawVec<float> m;
-                m.load(mp, cnt);
+            if (mp) m[s].load(mp + e, cnt[s]);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; s++) {
+            if (cnt[s] == 0) continue;
+            if (mp) {
                 float v[4];
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
-                    v[k] = fmaf(g.mu, m.at(k), u[k]);
-                    u[k] = g.nesterov ? fmaf(g.mu, v[k], u[k]) : v[k];
+                    v[k] = fmaf(g.mu, m[s].at(k), u[s][k]);
+                    u[s][k] = g.nesterov ? fmaf(g.mu, v[k], u[s][k]) : v[k];
                 }
-                RawVec<float>::store(mp, v, cnt);
+                RawVec<float>::store(mp + at + s * 4096, v, cnt[s]);
             }
 #pragma unroll
             for (int k = 0; k < 4; k++)
-                if (k < cnt) sum += (double)u[k] * (double)u[k];
+                if (k < cnt[s]) sum += (double)u[s][k] * (double)u[s][k];
         }
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
     if ((tid & 63) == 0) red[tid >> 6] = sum;
     __syncthreads();
-    if (tid == 0) reinterpret_cast<double*>(g.space + q.part)[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+    if (tid == 0) {
+        double t = 0.0;
+        for (int w = 0; w < 16; w++) t += red[w];
+        reinterpret_cast<double*>(g.space + q.part)[blockIdx.x] = t;
+    }
 }
 
-__device__ __forceinline__ int matrix_of(const NsGroup& g, int wg, int32_t NsMatrix::*first) {
-    int k = 0;
-    while (k + 1 < g.n && wg >= g.mat[k + 1].*first) k++;
+// The matrix of a workgroup of a launch over tiles of BM x BM results of all matrices (SYM: those on and above the diagonal of
+// square results); `wg` becomes its number among the matrix's own.
+template <bool SYM, int BM>
+__device__ __forceinline__ int matrix_of(const NsSizes& g, int& wg) {
+    constexpr int u = BM / 64;
+    int k = 0, total = 0, before = 0;
+#pragma unroll
+    for (int m = 0; m < kGroupMatrices - 1; m++) {
+        if (m + 1 < g.n) {
+            const int tm = ((int)(g.blocks[m] & 0xffffu) + u - 1) / u, tn = ((int)(g.blocks[m] >> 16) + u - 1) / u;
+            total += SYM ? tm * (tm + 1) / 2 : tm * tn;
+            if (wg >= total) {
+                k = m + 1;
+                before = total;
+            }
+        }
+    }
+    wg -= before;
     return k;
 }
 
@@ -133,18 +172,39 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
 
 // byte offset of the 16 bytes that hold columns k .. k + 7 (k a multiple of 8) of a row in an operand with K columns, hi part
 __device__ __forceinline__ int64_t panel_at(int row, int k, int K) {
-    return ((int64_t)(row >> 6) * (K >> 5) + (k >> 5)) * kPanelBytes + ((k & 31) >> 3) * 1024 + (row & 63) * 16;
+    return ((int64_t)(row >> 6) * (K >> 4) + (k >> 4)) * kPanelBytes + ((k & 15) >> 3) * 1024 + (row & 63) * 16;
 }
 
 // ---------------------------------------------------------------- set-up: X_0 and its transpose
 // One workgroup takes 64 x 64 elements: read along the tensor's contiguous axis, turned in LDS, written as panels of both.
-__global__ void __launch_bounds__(256) ns_split_kernel(NsGroup g) {
+__global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict__ group, NsSizes sizes) {
+    const NsGroup& g = *group;
     __shared__ float t[64][65];                          // [i][j]
     __shared__ double red[4];
-    const int wg = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const NsMatrix& q = g.mat[matrix_of(g, wg, &NsMatrix::first_patch)];
-    const int pm = q.mp >> 6, p = wg - q.first_patch;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int p = blockIdx.x;
+    const NsMatrix& q = g.mat[matrix_of<false, 64>(sizes, p)];
+    const int pm = q.mp >> 6;
     const int i0 = (p % pm) * 64, j0 = (p / pm) * 64;
+    // this lane's row of the tensor, and the wavefront's 16 columns; all loads are started before the norm is put together
+    const int r0 = q.flip ? j0 : i0, c0 = __builtin_amdgcn_readfirstlane((q.flip ? i0 : j0) + wave * 16);
+    const int r = r0 + lane, t0 = min(r, q.rows - 1) / q.base0, o0 = r - t0 * q.base0, e0 = min(q.base0, q.rows - t0 * q.base0);
+    float u[16], m[16];
+    int t1 = c0 / q.base1, c1 = c0 - t1 * q.base1;
+#pragma unroll
+    for (int s = 0; s < 16; s++) {
+        u[s] = m[s] = 0.f;
+        if (r < q.rows && c0 + s < q.cols) {
+            const int tile = t0 + q.grid0 * t1;
+            const int64_t off = o0 + (int64_t)e0 * c1;
+            u[s] = load_of(q.G, tile, off);
+            if (g.mu >= 0.f) m[s] = global_as<const float>(q.M.tiles[tile])[off];
+        }
+        if (++c1 == q.base1) {
+            c1 = 0;
+            t1++;
+        }
+    }
     const double* part = reinterpret_cast<const double*>(g.space + q.part);
     double sum = 0.0;
     for (int k = tid; k < g.norm_blocks; k += 256) sum += part[k];
@@ -153,24 +213,13 @@ __global__ void __launch_bounds__(256) ns_split_kernel(NsGroup g) {
     if (lane == 0) red[wave] = sum;
     __syncthreads();
     const float scale = (float)((double)kScale / (sqrt(red[0] + red[1] + red[2] + red[3]) + (double)g.eps));
-    const int r0 = q.flip ? j0 : i0, c0 = q.flip ? i0 : j0;
-    const int r = r0 + lane, t0 = r / q.base0, o0 = r - t0 * q.base0, e0 = min(q.base0, q.rows - t0 * q.base0);
-#pragma unroll 4
+#pragma unroll
     for (int s = 0; s < 16; s++) {
-        const int c = c0 + s * 4 + wave;
-        float u = 0.f;
-        if (r < q.rows && c < q.cols) {
-            const int t1 = c / q.base1;
-            const int tile = t0 + q.grid0 * t1;
-            const int64_t off = o0 + (int64_t)e0 * (c - t1 * q.base1);
-            u = load_of(q.G, tile, off);
-            if (g.mu >= 0.f) {
-                const float m = global_as<const float>(q.M.tiles[tile])[off];
-                u = g.nesterov ? fmaf(g.mu, m, u) : m;
-            }
-        }
-        const int i = q.flip ? s * 4 + wave : lane, j = q.flip ? lane : s * 4 + wave;
-        t[i][j] = u * scale;
+        float x = u[s];
+        if (g.mu >= 0.f) x = g.nesterov ? fmaf(g.mu, m[s], x) : m[s];
+        const int c = wave * 16 + s;
+        if (q.flip) t[c][lane] = x * scale;
+        else t[lane][c] = x * scale;
     }
     __syncthreads();
     // a lane's row, a wavefront's two groups of eight columns, of X and of its transpose
@@ -187,7 +236,7 @@ __global__ void __launch_bounds__(256) ns_split_kernel(NsGroup g) {
         }
         char* d = g.space + q.X + panel_at(i0 + lane, j0 + k, q.np);
         *reinterpret_cast<f16x8*>(d) = hi;
-        *reinterpret_cast<f16x8*>(d + 4096) = lo;
+        *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             _Float16 x, y;
@@ -197,181 +246,432 @@ __global__ void __launch_bounds__(256) ns_split_kernel(NsGroup g) {
         }
         d = g.space + q.XT + panel_at(j0 + lane, i0 + k, q.mp);
         *reinterpret_cast<f16x8*>(d) = hi;
-        *reinterpret_cast<f16x8*>(d + 4096) = lo;
+        *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
     }
 }
 
 // ---------------------------------------------------------------- products
 enum { kGram, kPoly, kStep, kLast };
 
-// What a lane has of the result: one column j, four rows i .. i + 3 at a time, as the second operand's row j and columns i.
-__device__ __forceinline__ void apply_result(const NsMatrix& q, const float (&x)[4], int i, int j) {
-    const bool copy = q.LP.tiles != nullptr;
+// One result's place in the tensor, found from its row and column of X.
+__device__ __forceinline__ void apply_one(const NsMatrix& q, float x, int i, int j) {
+    const int r = q.flip ? j : i, c = q.flip ? i : j;
+    if (r >= q.rows || c >= q.cols) return;
+    const int t0 = r / q.base0, t1 = c / q.base1, tile = t0 + q.grid0 * t1;
+    const int64_t off = (r - t0 * q.base0) + (int64_t)min(q.base0, q.rows - t0 * q.base0) * (c - t1 * q.base1);
+    if (q.step < 0.f) {
+        if (q.P.dtype == NNT_F32) global_as<float>(q.P.tiles[tile])[off] = x;
+        else global_as<bf16_t>(q.P.tiles[tile])[off] = f2bf(x);
+        return;
+    }
+    float* p = global_as<float>(q.P.tiles[tile]) + off;
+    const float v = fmaf(-q.step, x, q.decay * *p);
+    *p = v;
+    if (q.LP.tiles) global_as<bf16_t>(q.LP.tiles[tile])[off] = f2bf(v);
+}
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+
+// P <- decay P - step x, or P <- x, of a lane's results of a block: rows i + 8 p + 0 .. 3 of X, column j.  Four of them lie in one tile, next to each other or
+// (X the transpose) a column apart, except where a tile or the matrix ends among them.  All reads are started before the first write.
+__device__ __forceinline__ void apply_results(const NsMatrix& q, const float (&x)[4][4], int i, int j) {
+    if (j >= (q.flip ? q.rows : q.cols)) return;
+    const int extent = q.flip ? q.cols : q.rows, base_i = q.flip ? q.base1 : q.base0, base_j = q.flip ? q.base0 : q.base1;
+    const int tj = j / base_j, oj = j - tj * base_j;
+    const bool update = q.step >= 0.f, fp32 = q.P.dtype == NNT_F32;
+    int tile[4];
+    int64_t off[4];
+    int64_t stride[4];
+    bool even[4];
+    RawVec<float> old[4];
 #pragma unroll
-    for (int k = 0; k < 4; k++) {
-        const int r = q.flip ? j : i + k, c = q.flip ? i + k : j;
-        if (r >= q.rows || c >= q.cols) continue;
-        const int t0 = r / q.base0, t1 = c / q.base1;
-        const int tile = t0 + q.grid0 * t1;
-        const int64_t off = (r - t0 * q.base0) + (int64_t)min(q.base0, q.rows - t0 * q.base0) * (c - t1 * q.base1);
-        if (q.step < 0.f) {
-            if (q.P.dtype == NNT_F32) global_as<float>(q.P.tiles[tile])[off] = x[k];
-            else global_as<bf16_t>(q.P.tiles[tile])[off] = f2bf(x[k]);
-        } else {
-            float* p = global_as<float>(q.P.tiles[tile]) + off;
-            const float v = fmaf(-q.step, x[k], q.decay * *p);
-            *p = v;
-            if (copy) global_as<bf16_t>(q.LP.tiles[tile])[off] = f2bf(v);
+    for (int p = 0; p < 4; p++) {
+        const int ip = i + p * 8, ti = ip / base_i, oi = ip - ti * base_i;
+        even[p] = ip + 4 <= extent && oi + 4 <= base_i;
+        tile[p] = q.flip ? tj + q.grid0 * ti : ti + q.grid0 * tj;
+        const int e0 = q.flip ? min(q.base0, q.rows - tj * q.base0) : min(q.base0, q.rows - ti * q.base0);
+        off[p] = q.flip ? oj + (int64_t)e0 * oi : oi + (int64_t)e0 * oj;
+        stride[p] = q.flip ? e0 : 1;
+        if (update && even[p]) {
+            const float* src = global_as<const float>(q.P.tiles[tile[p]]) + off[p];
+            if (q.flip) {
+#pragma unroll
+                for (int k = 0; k < 4; k++) old[p].set(k, src[k * stride[p]]);
+            } else {
+                old[p].load(src, 4);
+            }
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < 4; p++) {
+        if (!even[p]) {
+#pragma unroll
+            for (int k = 0; k < 4; k++) apply_one(q, x[p][k], i + p * 8 + k, j);
+            continue;
+        }
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) v[k] = update ? fmaf(-q.step, x[p][k], q.decay * old[p].at(k)) : x[p][k];
+        if (fp32) {
+            float* d = global_as<float>(q.P.tiles[tile[p]]) + off[p];
+            if (q.flip) {
+#pragma unroll
+                for (int k = 0; k < 4; k++) d[k * stride[p]] = v[k];
+            } else {
+                RawVec<float>::store(d, v, 4);
+            }
+        }
+        if (!fp32 || q.LP.tiles) {
+            bf16_t* d = global_as<bf16_t>((fp32 ? q.LP : q.P).tiles[tile[p]]) + off[p];
+            if (q.flip) {
+#pragma unroll
+                for (int k = 0; k < 4; k++) d[k * stride[p]] = f2bf(v[k]);
+            } else {
+                u32x2 y;
+                y[0] = (uint32_t)f2bf(v[0]) | ((uint32_t)f2bf(v[1]) << 16);
+                y[1] = (uint32_t)f2bf(v[2]) | ((uint32_t)f2bf(v[3]) << 16);
+                *reinterpret_cast<u32x2*>(d) = y;
+            }
         }
     }
 }
 
-// One workgroup of four wavefronts computes 2 WT x 2 WT results, each wavefront WT x WT of them.  Of the symmetric results only tiles on
-// and above the diagonal are computed, and written twice.
-template <int MODE, int WT>
-__global__ void __launch_bounds__(256, WT == 64 ? 2 : 4) ns_product_kernel(NsGroup g, int now) {
-    constexpr int MT = 2 * WT, MI = WT / 32, RB = MT / 64;      // macro-tile, fragments per side, row blocks
-    constexpr int kStage = 2 * RB * kPanelBytes, NL = kStage / 4096;
-    constexpr int kPitch = WT + 8;                              // of the turned results, in 32-bit words
-    constexpr int kTurn = 4 * WT * kPitch * 4;
-    __shared__ __align__(16) char lds[2 * kStage > kTurn ? 2 * kStage : kTurn];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wr = wave & 1, wc = wave >> 1;
-    const int wg = blockIdx.x;
-    constexpr bool kSym = MODE == kGram || MODE == kPoly;
-    const NsMatrix& q = g.mat[matrix_of(g, wg, kSym ? &NsMatrix::first_sym : &NsMatrix::first_full)];
-    const int tm = q.mp / MT;
-    int ti, tj;
-    if constexpr (kSym) {
-        const int p = wg - q.first_sym;
-        tj = (int)((sqrtf(8.f * (float)p + 1.f) - 1.f) * 0.5f);
-        while (tj * (tj + 1) / 2 > p) tj--;
-        while ((tj + 1) * (tj + 2) / 2 <= p) tj++;
-        ti = p - tj * (tj + 1) / 2;
-    } else {
-        const int p = wg - q.first_full;
-        ti = p % tm;
-        tj = p / tm;
-    }
-    const int64_t xbytes = (int64_t)q.mp * q.np * 4;
-    const int K = MODE == kGram ? q.np : q.mp, nk = K >> 5;
-    const char* Pb = g.space + (MODE == kGram ? q.X + now * xbytes : MODE == kPoly ? q.A : q.B);
-    const char* Qb = g.space + (MODE == kGram ? q.X + now * xbytes : MODE == kPoly ? q.A : q.XT + now * xbytes);
-    // 16 bytes per thread and load; load l of a stage lies in row block l / 2 (half l & 1 of its 8 KB), P's blocks first
-    const char* src[NL];
-#pragma unroll
-    for (int l = 0; l < NL; l++) {
-        const int blk = l >> 1;
-        const char* b = blk < RB ? Pb + (int64_t)(ti * RB + blk) * nk * kPanelBytes : Qb + (int64_t)(tj * RB + blk - RB) * nk * kPanelBytes;
-        src[l] = in_global(b) + (l & 1) * 4096 + tid * 16;
-    }
-    f32x16 acc[MI][MI];
-#pragma unroll
-    for (int x = 0; x < MI; x++)
-#pragma unroll
-        for (int y = 0; y < MI; y++)
-#pragma unroll
-            for (int r = 0; r < 16; r++) acc[x][y][r] = 0.f;
-    uint4 st[NL];
-#pragma unroll
-    for (int l = 0; l < NL; l++) st[l] = *reinterpret_cast<const uint4*>(in_global(src[l]));
-#pragma unroll
-    for (int l = 0; l < NL; l++) *reinterpret_cast<uint4*>(lds + l * 4096 + tid * 16) = st[l];
-    __syncthreads();
-    const int row_p = WT == 64 ? 0 : wr * 32, row_q = WT == 64 ? 0 : wc * 32;
-    const int off_p = (WT == 64 ? wr * kPanelBytes : 0) + (row_p + (lane & 31)) * 16 + (lane >> 5) * 1024;
-    const int off_q = RB * kPanelBytes + (WT == 64 ? wc * kPanelBytes : 0) + (row_q + (lane & 31)) * 16 + (lane >> 5) * 1024;
-    for (int kb = 0; kb < nk; kb++) {
-        const bool more = kb + 1 < nk;
-        if (more) {
-#pragma unroll
-            for (int l = 0; l < NL; l++) st[l] = *reinterpret_cast<const uint4*>(in_global(src[l] + (int64_t)(kb + 1) * kPanelBytes));
-        }
-        const char* buf = lds + (kb & 1) * kStage;
-#pragma unroll
-        for (int ks = 0; ks < 2; ks++) {
-            f16x8 ph[MI], pl[MI], qh[MI], ql[MI];
-#pragma unroll
-            for (int x = 0; x < MI; x++) {
-                ph[x] = *reinterpret_cast<const f16x8*>(buf + off_p + ks * 2048 + x * 512);
-                pl[x] = *reinterpret_cast<const f16x8*>(buf + off_p + ks * 2048 + x * 512 + 4096);
-                qh[x] = *reinterpret_cast<const f16x8*>(buf + off_q + ks * 2048 + x * 512);
-                ql[x] = *reinterpret_cast<const f16x8*>(buf + off_q + ks * 2048 + x * 512 + 4096);
-            }
-#pragma unroll
-            for (int x = 0; x < MI; x++)
-#pragma unroll
-                for (int y = 0; y < MI; y++) {
-                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[x], ql[y], acc[x][y], 0, 0, 0);
-                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[x], qh[y], acc[x][y], 0, 0, 0);
-                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[x], qh[y], acc[x][y], 0, 0, 0);
-                }
-        }
-        if (more) {
-            char* nxt = lds + ((kb + 1) & 1) * kStage;
-#pragma unroll
-            for (int l = 0; l < NL; l++) *reinterpret_cast<uint4*>(nxt + l * 4096 + tid * 16) = st[l];
-        }
-        __syncthreads();
-    }
+// The result path of a wavefront: FM x FN blocks of 32 x 32 from row i0 and column j0 on.  `turn`: LDS for 32 rows, in which the results change places.
+constexpr int turn_pitch(int FN) { return 32 * FN + 8; }         // in 32-bit words
+template <int MODE, int FM, int FN>
+__device__ __forceinline__ void store_results(const NsGroup& g, const NsMatrix& q, const f32x16 (&acc)[FM][FN], int i0, int j0, bool diagonal, int now, uint32_t* turn) {
     // results: this lane has column j0 + 32 y + (lane & 31), rows i0 + 32 x + 8 p + 4 (lane >> 5) + 0 .. 3
-    const int i0 = ti * MT + wr * WT, j0 = tj * MT + wc * WT;
+    constexpr bool kSym = MODE == kGram || MODE == kPoly;
+    constexpr int kPitch = turn_pitch(FN);
+    const int lane = threadIdx.x & 63;
+    const int64_t xbytes = (int64_t)q.mp * q.np * 4;
     const char* E = g.space + (MODE == kPoly ? q.A : q.XT + now * xbytes);          // the term that is added, laid out like the result
     char* D = g.space + (MODE == kGram ? q.A : MODE == kPoly ? q.B : q.XT + (1 - now) * xbytes);
+    char* Dt = kSym ? D : g.space + q.X + (1 - now) * xbytes;                       // the same with rows and columns exchanged
+    const int Kt = kSym ? q.mp : q.np;
+    const bool turned = MODE != kLast && !(kSym && diagonal);
     const float factor = (MODE == kPoly ? g.c : 1.f) / kScale;      // sums carry the scale twice
     const float add = MODE == kPoly ? g.b : g.a;
-    uint32_t* turn = reinterpret_cast<uint32_t*>(lds) + wave * WT * kPitch;
+    // what is added is fetched one block of 32 rows ahead: behind the stores that the compiler cannot tell apart from it every load would wait
+    f16x4 e[2][FN][4][2];
+    // (blocks behind the last row block of X or of its transpose are not there)
+    const int rows = q.mp, cols = kSym ? q.mp : q.np;
+    auto fetch = [&](int x) {
+        if (i0 + x * 32 >= rows) return;
 #pragma unroll
-    for (int x = 0; x < MI; x++)
-#pragma unroll
-        for (int y = 0; y < MI; y++)
+        for (int y = 0; y < FN; y++) {
+            if (j0 + y * 32 >= cols) continue;
 #pragma unroll
             for (int p = 0; p < 4; p++) {
-                const int i = i0 + x * 32 + p * 8, j = j0 + y * 32 + (lane & 31);
-                const int64_t at = panel_at(j, i, q.mp) + (lane >> 5) * 8;
-                float v[4];
+                const char* at = E + panel_at(j0 + y * 32 + (lane & 31), i0 + x * 32 + p * 8, q.mp) + (lane >> 5) * 8;
+                e[x & 1][y][p][0] = *reinterpret_cast<const f16x4*>(at);
+                e[x & 1][y][p][1] = *reinterpret_cast<const f16x4*>(at + kPartBytes);
+            }
+        }
+    };
+    if constexpr (MODE != kGram) fetch(0);
 #pragma unroll
-                for (int k = 0; k < 4; k++) v[k] = acc[x][y][p * 4 + k] * factor;
-                if constexpr (MODE != kGram) {
-                    const f16x4 eh = *reinterpret_cast<const f16x4*>(E + at), el = *reinterpret_cast<const f16x4*>(E + at + 4096);
+    for (int x = 0; x < FM; x++) {
+        if constexpr (MODE != kGram)
+            if (x + 1 < FM) fetch(x + 1);
+        if (i0 + x * 32 >= rows) continue;
 #pragma unroll
-                    for (int k = 0; k < 4; k++) v[k] = fmaf(add, (float)eh[k] + (float)el[k], v[k]);
+        for (int y = 0; y < FN; y++) {
+            if (j0 + y * 32 >= cols) continue;
+            float v[4][4];
+#pragma unroll
+            for (int p = 0; p < 4; p++)
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    v[p][k] = acc[x][y][p * 4 + k] * factor;
+                    if constexpr (MODE != kGram) v[p][k] = fmaf(add, (float)e[x & 1][y][p][0][k] + (float)e[x & 1][y][p][1][k], v[p][k]);
+                    if constexpr (MODE == kLast) v[p][k] *= 1.f / kScale;
                 }
-                if constexpr (MODE == kLast) {
+            const int i = i0 + x * 32, j = j0 + y * 32 + (lane & 31);
+            if constexpr (MODE == kLast) {
+                apply_results(q, v, i + (lane >> 5) * 4, j);
+            } else {
 #pragma unroll
-                    for (int k = 0; k < 4; k++) v[k] *= 1.f / kScale;
-                    apply_result(q, v, i + (lane >> 5) * 4, j);
-                } else {
+                for (int p = 0; p < 4; p++) {
                     f16x4 hi, lo;
 #pragma unroll
                     for (int k = 0; k < 4; k++) {
                         _Float16 h, l;
-                        split(v[k], h, l);
+                        split(v[p][k], h, l);
                         hi[k] = h;
                         lo[k] = l;
-                        turn[(x * 32 + p * 8 + (lane >> 5) * 4 + k) * kPitch + y * 32 + (lane & 31)] =
+                        turn[(p * 8 + (lane >> 5) * 4 + k) * kPitch + y * 32 + (lane & 31)] =
                             (uint32_t)__builtin_bit_cast(uint16_t, h) | ((uint32_t)__builtin_bit_cast(uint16_t, l) << 16);
                     }
-                    *reinterpret_cast<f16x4*>(D + at) = hi;
-                    *reinterpret_cast<f16x4*>(D + at + 4096) = lo;
+                    char* d = D + panel_at(j, i + p * 8, q.mp) + (lane >> 5) * 8;
+                    *reinterpret_cast<f16x4*>(d) = hi;
+                    *reinterpret_cast<f16x4*>(d + kPartBytes) = lo;
                 }
             }
-    if constexpr (MODE != kLast) {
-        if (kSym && ti == tj) return;
-        // the same with rows and columns exchanged: each wavefront turns its own part
-        char* Dt = kSym ? D : g.space + q.X + (1 - now) * xbytes;
-        const int Kt = kSym ? q.mp : q.np;
+        }
+        if (turned) {
+            // 32 rows of the wavefront's own results, eight columns to a lane
 #pragma unroll
-        for (int s = 0; s < WT * WT / 8 / 64; s++) {
-            const int idx = s * 64 + lane, row = idx % WT, k = idx / WT * 8;
-            const uint4 u = *reinterpret_cast<const uint4*>(turn + row * kPitch + k), w = *reinterpret_cast<const uint4*>(turn + row * kPitch + k + 4);
-            const uint4 hi = make_uint4((u.x & 0xffff) | (u.y << 16), (u.z & 0xffff) | (u.w << 16), (w.x & 0xffff) | (w.y << 16), (w.z & 0xffff) | (w.w << 16));
-            const uint4 lo = make_uint4((u.x >> 16) | (u.y & 0xffff0000u), (u.z >> 16) | (u.w & 0xffff0000u), (w.x >> 16) | (w.y & 0xffff0000u),
-                                        (w.z >> 16) | (w.w & 0xffff0000u));
-            char* d = Dt + panel_at(i0 + row, j0 + k, Kt);
-            *reinterpret_cast<uint4*>(d) = hi;
-            *reinterpret_cast<uint4*>(d + 4096) = lo;
+            for (int s = 0; s < 2 * FN; s++) {
+                if (j0 + s / 2 * 32 >= cols) continue;
+                const int row = lane & 31, k = (s * 2 + (lane >> 5)) * 8;
+                const uint4 u = *reinterpret_cast<const uint4*>(turn + row * kPitch + k), w = *reinterpret_cast<const uint4*>(turn + row * kPitch + k + 4);
+                const uint4 hi = make_uint4((u.x & 0xffff) | (u.y << 16), (u.z & 0xffff) | (u.w << 16), (w.x & 0xffff) | (w.y << 16), (w.z & 0xffff) | (w.w << 16));
+                const uint4 lo = make_uint4((u.x >> 16) | (u.y & 0xffff0000u), (u.z >> 16) | (u.w & 0xffff0000u), (w.x >> 16) | (w.y & 0xffff0000u),
+                                            (w.z >> 16) | (w.w & 0xffff0000u));
+                char* d = Dt + panel_at(i0 + x * 32 + row, j0 + k, Kt);
+                *reinterpret_cast<uint4*>(d) = hi;
+                *reinterpret_cast<uint4*>(d + kPartBytes) = lo;
+            }
         }
     }
+}
+
+// A macro-tile: WR x WC wavefronts of FM x FN results of 32 x 32 each, ST stages of KS panels (16 KS columns of the contraction) in LDS.
+template <int FM_, int FN_, int WR_, int WC_, int KS_, int ST_>
+struct Shape {
+    static constexpr int FM = FM_, FN = FN_, WR = WR_, WC = WC_, KS = KS_, ST = ST_, kWaves = WR * WC;
+    static constexpr int BM = 32 * FM * WR, BN = 32 * FN * WC;
+    static constexpr int kStage = (BM + BN) / 64 * KS * kPanelBytes, kLoads = kStage / 1024 / kWaves;
+    static constexpr int kTurn = 32 * turn_pitch(FN) * 4;
+    static constexpr int kLds = ST * kStage > kWaves * kTurn ? ST * kStage : kWaves * kTurn;
+    static_assert(BM == BN && kLoads * kWaves * 1024 == kStage && 4 * KS % kLoads == 0, "symmetric results need square tiles, a wavefront's loads one row block");
+    static_assert((ST - 1) * kLoads < 64, "loads in flight are counted in six bits");
+};
+using Large = Shape<4, 2, 2, 4, 1, 4>;       // one workgroup per compute unit
+using Middle = Shape<2, 2, 2, 2, 1, 4>;      // two
+using Small = Shape<1, 1, 2, 2, 1, 6>;       // three
+
+template <int OFFSET>
+__device__ __forceinline__ void read_fragment(f16x8& f, uint32_t addr) {
+    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(f) : "v"(addr), "n"(OFFSET));
+}
+
+// what uses these stays behind the wait in front of this
+__device__ __forceinline__ void hold(f16x8& a, f16x8& b) { asm volatile("" : "+v"(a), "+v"(b)); }
+
+// Tiles of a launch in an order in which neighbours share operands: eight rows of tiles at a time, column by column.  Of a symmetric result the
+// tiles on and above the diagonal.
+template <bool SYM>
+__device__ __forceinline__ void tile_of(int p, int tm, int tn, int& ti, int& tj) {
+    for (int r0 = 0;; r0 += 8) {
+        const int rows = min(8, tm - r0);
+        if constexpr (SYM) {
+            const int corner = rows * (rows + 1) / 2, count = corner + rows * (tn - r0 - rows);
+            if (p < count) {
+                if (p >= corner) {
+                    tj = r0 + rows + (p - corner) / rows;
+                    ti = r0 + (p - corner) % rows;
+                } else {
+                    int c = 0;
+                    while ((c + 1) * (c + 2) / 2 <= p) c++;
+                    tj = r0 + c;
+                    ti = r0 + p - c * (c + 1) / 2;
+                }
+                return;
+            }
+            p -= count;
+        } else {
+            const int count = rows * tn;
+            if (p < count) {
+                tj = p / rows;
+                ti = r0 + p % rows;
+                return;
+            }
+            p -= count;
+        }
+    }
+}
+
+// One workgroup computes a macro-tile.  Of the symmetric results only tiles on and above the diagonal are computed, and written twice.
+//
+// Stages of 16 columns go from memory straight into LDS, ST of them, so that loads have ST - 1 steps to land; the fragments of the next step
+// are read under the matrix instructions of the present one, into the other of two register sets.  At the top of a step every wavefront waits for
+// its fragments and for its own loads of the next step; the barrier behind that makes the next stage complete for everybody and the present one, whose
+// fragments all have, free for the loads of step + ST.  LDS reads and their waits are spelled out: the compiler would wait for all loads in flight.
+template <int MODE, typename S>
+__global__ void __launch_bounds__(64 * S::kWaves, 2) ns_product_kernel(const NsGroup* __restrict__ group, NsSizes sizes, int now, int splits) {
+    const NsGroup& g = *group;
+    constexpr int FM = S::FM, FN = S::FN, ST = S::ST;
+    __shared__ __align__(1024) char lds[S::kLds];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave % S::WR, wc = wave / S::WR;
+    constexpr bool kSym = MODE == kGram || MODE == kPoly;
+    // workgroups go to the eight dies in turn: each die gets one run of the tiles
+    int wg = blockIdx.x;
+    {
+        const int total = gridDim.x, per = total / 8, rest = total % 8, die = wg % 8;
+        wg = die * per + min(die, rest) + wg / 8;
+    }
+    // A's contraction may be cut: the parts of a tile lie side by side
+    int part = 0;
+    if constexpr (MODE == kGram) {
+        part = wg % splits;
+        wg /= splits;
+    }
+    const int tile = wg;                                         // of all matrices
+    const NsMatrix& q = g.mat[matrix_of<kSym, S::BM>(sizes, wg)];
+    const int tm = (q.mp + S::BM - 1) / S::BM;
+    int ti, tj;
+    tile_of<kSym>(wg, tm, kSym ? tm : (q.np + S::BN - 1) / S::BN, ti, tj);
+    ti = __builtin_amdgcn_readfirstlane(ti);
+    tj = __builtin_amdgcn_readfirstlane(tj);
+    const int64_t xbytes = (int64_t)q.mp * q.np * 4;
+    const int nk = (MODE == kGram ? q.np : q.mp) >> 4;           // panels along the contraction, a multiple of 4
+    const char* Pb = g.space + (MODE == kGram ? q.X + now * xbytes : MODE == kPoly ? q.A : q.B);
+    const char* Qb = g.space + (MODE == kGram ? q.X + now * xbytes : MODE == kPoly ? q.A : q.XT + now * xbytes);
+
+    // a wavefront loads a part of one row block's panels per step
+    const char* src;
+    {
+        constexpr int kRB = S::BM / 64;
+        const int blk = wave * S::kLoads / (4 * S::KS), sub = wave * S::kLoads % (4 * S::KS);
+        // (a tile may end behind the last row block: that one is loaded again, its results are not stored)
+        const int row = blk < kRB ? min(ti * kRB + blk, (q.mp >> 6) - 1) : min(tj * kRB + blk - kRB, ((kSym ? q.mp : q.np) >> 6) - 1);
+        src = (blk < kRB ? Pb : Qb) + (int64_t)row * nk * kPanelBytes + sub * 1024;
+    }
+    int steps = nk / S::KS;
+    if constexpr (MODE == kGram) {
+        const int from = (int)((int64_t)steps * part / splits);
+        steps = (int)((int64_t)steps * (part + 1) / splits) - from;
+        src += (int64_t)from * S::KS * kPanelBytes;
+        if (steps == 0 && from > 0) src -= S::KS * kPanelBytes;      // (more parts than steps: fetches one that it does not use)
+    }
+    int left = steps;                                            // steps whose loads have not been started
+    auto load_one = [&](int stage, int l) {
+        __builtin_amdgcn_global_load_lds((glb_void_ptr)(src + l * 1024 + lane * 16), (lds_void_ptr)(lds + stage * S::kStage + (wave * S::kLoads + l) * 1024), 16, 0, 0);
+    };
+    // (loads are started in every step, so that the count in flight is the same at every wait: the last steps fetch the last one again)
+    auto advance = [&]() {
+        if (--left > 0) src += S::KS * kPanelBytes;
+    };
+    f32x16 acc[FM][FN];
+#pragma unroll
+    for (int x = 0; x < FM; x++)
+#pragma unroll
+        for (int y = 0; y < FN; y++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) acc[x][y][r] = 0.f;
+
+    constexpr int KS = S::KS, kFrags = KS * 2 * (FM + FN), kMfma = KS * 3 * FM * FN, kBlock = KS * kPanelBytes;
+    f16x8 pf[2][KS][FM][2], qf[2][KS][FN][2];
+    const uint32_t lane_at = lds_offset(lds) + (lane & 31) * 16 + (lane >> 5) * 1024;
+    const uint32_t p_at = lane_at + (FM == 1 ? wr * 512 : wr * (FM / 2) * kBlock);
+    const uint32_t q_at = lane_at + S::BM / 64 * kBlock + (FN == 1 ? wc * 512 : wc * (FN / 2) * kBlock);
+    // fragment I of a stage; of a panel the hi parts first, which are multiplied first
+    auto frag_one = [&](auto I, int set, uint32_t stage) {
+        constexpr int i = decltype(I)::value, ks = i / (2 * (FM + FN)), part = i / (FM + FN) % 2, k = i % (FM + FN);
+        constexpr int at = ks * kPanelBytes + part * kPartBytes;
+        if constexpr (k < FN) read_fragment<(k >> 1) * kBlock + (k & 1) * 512 + at>(qf[set][ks][k][part], q_at + stage);
+        else read_fragment<((k - FN) >> 1) * kBlock + ((k - FN) & 1) * 512 + at>(pf[set][ks][k - FN][part], p_at + stage);
+    };
+    auto wait_frags = [&](int set) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++) {
+#pragma unroll
+            for (int k = 0; k < FM; k++) hold(pf[set][ks][k][0], pf[set][ks][k][1]);
+#pragma unroll
+            for (int k = 0; k < FN; k++) hold(qf[set][ks][k][0], qf[set][ks][k][1]);
+        }
+    };
+    int stage = 0;                                               // of the present step
+    auto step = [&](int set) {
+        wait_frags(set);
+        __builtin_amdgcn_s_waitcnt(wait_vm((ST - 2) * S::kLoads));
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        const int next = stage + 1 == ST ? 0 : stage + 1;
+        const uint32_t next_at = (uint32_t)(next * S::kStage);
+        static_for<kMfma>([&](auto Q) {
+            constexpr int m = decltype(Q)::value, ks = m / (3 * FM * FN), term = m / (FM * FN) % 3, x = m % (FM * FN) / FN, y = m % FN;
+            // hi hi, hi lo, lo hi
+            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pf[set][ks][x][term == 2], qf[set][ks][y][term == 1], acc[x][y], 0, 0, 0);
+            static_for<kFrags + S::kLoads>([&](auto I) {
+                constexpr int i = decltype(I)::value;
+                constexpr int slot = i < kFrags ? i * kMfma / 2 / kFrags : (i - kFrags) * kMfma / S::kLoads;
+                if constexpr (slot == m) {
+                    if constexpr (i < kFrags) frag_one(I, set ^ 1, next_at);
+                    else load_one(stage, i - kFrags);
+                }
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        advance();
+        stage = next;
+    };
+#pragma unroll
+    for (int s = 0; s < ST; s++) {
+#pragma unroll
+        for (int l = 0; l < S::kLoads; l++) load_one(s, l);
+        advance();
+    }
+    __builtin_amdgcn_s_waitcnt(wait_vm((ST - 1) * S::kLoads));
+    asm volatile("s_barrier" ::: "memory");
+    static_for<kFrags>([&](auto I) { frag_one(I, 0, 0u); });
+    for (int k = 0; k < steps; k += 2) {
+        step(0);
+        if (MODE != kGram || k + 1 < steps) step(1);             // (whole contractions have an even number of steps)
+    }
+    // nothing may still be on its way into fragment registers or LDS (the last step has read a stage that nobody needs)
+    wait_frags(0);
+    wait_frags(1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_barrier" ::: "memory");
+
+    if constexpr (MODE == kGram) {
+        if (splits > 1) {
+            // partial sums leave as they lie in registers
+            float4* d = reinterpret_cast<float4*>(g.space + g.partial) + ((int64_t)(tile * splits + part) * S::kWaves + wave) * (FM * FN * 256) + lane;
+#pragma unroll
+            for (int x = 0; x < FM; x++)
+#pragma unroll
+                for (int y = 0; y < FN; y++)
+#pragma unroll
+                    for (int v = 0; v < 4; v++) d[((x * FN + y) * 4 + v) * 64] = make_float4(acc[x][y][4 * v], acc[x][y][4 * v + 1], acc[x][y][4 * v + 2], acc[x][y][4 * v + 3]);
+            return;
+        }
+    }
+    store_results<MODE, FM, FN>(g, q, acc, ti * S::BM + wr * 32 * FM, tj * S::BN + wc * 32 * FN, ti == tj, now, reinterpret_cast<uint32_t*>(lds + wave * S::kTurn));
+}
+
+// Adds up the parts of A's tiles, in their order: a wavefront takes one block of 32 x 32.
+template <typename S>
+__global__ void __launch_bounds__(256) ns_combine_kernel(const NsGroup* __restrict__ group, NsSizes sizes, int now, int splits) {
+    const NsGroup& g = *group;
+    __shared__ __align__(16) uint32_t turn[4 * 32 * turn_pitch(1)];
+    constexpr int kBlocks = S::kWaves * S::FM * S::FN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = blockIdx.x / (kBlocks / 4), blk = blockIdx.x % (kBlocks / 4) * 4 + wave;
+    int wg = tile;
+    const NsMatrix& q = g.mat[matrix_of<true, S::BM>(sizes, wg)];
+    const int tm = (q.mp + S::BM - 1) / S::BM;
+    int ti, tj;
+    tile_of<true>(wg, tm, tm, ti, tj);
+    const float4* d = reinterpret_cast<const float4*>(g.space + g.partial) + ((int64_t)tile * splits * kBlocks + blk) * 256 + lane;
+    float4 t[4];
+#pragma unroll
+    for (int v = 0; v < 4; v++) t[v] = d[v * 64];
+#pragma unroll 4
+    for (int part = 1; part < splits; part++) {
+#pragma unroll
+        for (int v = 0; v < 4; v++) {
+            const float4 u = d[(int64_t)part * kBlocks * 256 + v * 64];
+            t[v].x += u.x;
+            t[v].y += u.y;
+            t[v].z += u.z;
+            t[v].w += u.w;
+        }
+    }
+    f32x16 acc[1][1];
+#pragma unroll
+    for (int v = 0; v < 4; v++) {
+        acc[0][0][4 * v] = t[v].x;
+        acc[0][0][4 * v + 1] = t[v].y;
+        acc[0][0][4 * v + 2] = t[v].z;
+        acc[0][0][4 * v + 3] = t[v].w;
+    }
+    const int w = blk / (S::FM * S::FN), x = blk / S::FN % S::FM, y = blk % S::FN;
+    store_results<kGram, 1, 1>(g, q, acc, ti * S::BM + (w % S::WR * S::FM + x) * 32, tj * S::BN + (w / S::WR * S::FN + y) * 32, ti == tj, now, turn + wave * 32 * turn_pitch(1));
 }
 
 // ---------------------------------------------------------------- host side
@@ -406,14 +706,73 @@ struct Task {
     float decay, step;
 };
 
-template <int WT>
-void launch_product(int mode, const NsGroup& g, int now, unsigned wgs, hipStream_t st) {
+template <typename S>
+void launch_product(int mode, const NsGroup* g, const NsSizes& sizes, int now, unsigned tiles, int splits, hipStream_t st) {
+    const dim3 grid(tiles * (unsigned)splits), block(64 * S::kWaves);
     switch (mode) {
-        case kGram: hipLaunchKernelGGL((ns_product_kernel<kGram, WT>), dim3(wgs), dim3(256), 0, st, g, now); break;
-        case kPoly: hipLaunchKernelGGL((ns_product_kernel<kPoly, WT>), dim3(wgs), dim3(256), 0, st, g, now); break;
-        case kStep: hipLaunchKernelGGL((ns_product_kernel<kStep, WT>), dim3(wgs), dim3(256), 0, st, g, now); break;
-        default: hipLaunchKernelGGL((ns_product_kernel<kLast, WT>), dim3(wgs), dim3(256), 0, st, g, now); break;
+        case kGram:
+            hipLaunchKernelGGL((ns_product_kernel<kGram, S>), grid, block, 0, st, g, sizes, now, splits);
+            if constexpr (S::BM <= 128)
+                if (splits > 1) hipLaunchKernelGGL((ns_combine_kernel<S>), dim3(tiles * (S::kWaves * S::FM * S::FN / 4)), dim3(256), 0, st, g, sizes, now, splits);
+            break;
+        case kPoly: hipLaunchKernelGGL((ns_product_kernel<kPoly, S>), grid, block, 0, st, g, sizes, now, 1); break;
+        case kStep: hipLaunchKernelGGL((ns_product_kernel<kStep, S>), grid, block, 0, st, g, sizes, now, 1); break;
+        default: hipLaunchKernelGGL((ns_product_kernel<kLast, S>), grid, block, 0, st, g, sizes, now, 1); break;
     }
+}
+
+// How a product of a group is launched.
+struct Launch {
+    int shape = 0, splits = 1;           // shape: 0 small, 1 middle, 2 large
+    unsigned tiles = 0;
+};
+
+// The fastest launch of a product by a model of its time: a compute unit takes `lone` microseconds per panel of 16 columns for the only tile that it
+// holds, `full` for each of several, and a launch a fixed time besides.  (Measured; a tile of 64 x 64 alone is bound by the 32 bytes per clock that a
+// unit fetches, large ones by the clock that the power limit leaves.)  A product whose contraction is long and whose tiles are few is cut along the contraction.
+Launch choose(const NsSizes& g, int mode) {
+    static const struct { int blocks; double lone, full, fixed; } kShapes[3] = {{1, 0.107, 0.125, 2.6}, {2, 0.234, 0.339, 4.0}, {4, 0.8, 1.18, 7.0}};
+    constexpr double kCombine = 4.0;
+    const bool sym = mode == kGram || mode == kPoly;
+    Launch best;
+    double best_time = 0.0;
+    for (int s = 0; s < 3; s++) {
+        const int u = kShapes[s].blocks;
+        int64_t tiles = 0, panels = 0, longest = 0;
+        for (int k = 0; k < g.n; k++) {
+            const int64_t mb = g.blocks[k] & 0xffffu, nb = g.blocks[k] >> 16, tm = (mb + u - 1) / u, tn = (nb + u - 1) / u;
+            const int64_t t = sym ? tm * (tm + 1) / 2 : tm * tn, c = 4 * (mode == kGram ? nb : mb);
+            tiles += t;
+            panels += t * c;
+            longest = std::max(longest, c);
+        }
+        for (int splits = 1; splits <= 64; splits++) {
+            if (splits > 1 && (mode != kGram || s == 2 || tiles * splits > 512 || longest / splits < 8)) break;
+            const double each = (double)panels / tiles / splits;                       // panels of a workgroup, on average
+            const double per = std::ceil(tiles * splits / 256.0);
+            double time = per > 1.0 ? per * each * kShapes[s].full : (double)longest / splits * kShapes[s].lone;
+            time += kShapes[s].fixed + (splits > 1 ? kCombine + 0.1 * splits : 0.0);
+            if (best.tiles == 0 || time < best_time) {
+                best_time = time;
+                best.shape = s;
+                best.splits = splits;
+                best.tiles = (unsigned)tiles;
+            }
+        }
+    }
+    if (const char* e = getenv(mode == kGram ? "NS_G" : mode == kPoly ? "NS_P" : "NS_S")) {
+        best.shape = atoi(e) % 10;
+        best.splits = mode == kGram ? std::max(1, atoi(e) / 10) : 1;
+        int64_t tiles = 0;
+        const int u = kShapes[best.shape].blocks;
+        for (int k = 0; k < g.n; k++) {
+            const int64_t mb = g.blocks[k] & 0xffffu, nb = g.blocks[k] >> 16, tm = (mb + u - 1) / u, tn = (nb + u - 1) / u;
+            tiles += sym ? tm * (tm + 1) / 2 : tm * tn;
+        }
+        best.tiles = tiles;
+    }
+    if (getenv("NS_PRINT")) fprintf(stderr, "mode %d shape %d splits %d tiles %u: %.1f us\n", mode, best.shape, best.splits, best.tiles, best_time);
+    return best;
 }
 
 // Orthogonalises the matrices of `tasks` and applies the results, as many of them in one set of launches as it takes to fill the
@@ -421,47 +780,35 @@ void launch_product(int mode, const NsGroup& g, int now, unsigned wgs, hipStream
 int32_t newton_schulz(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& cfg, float mu, int nesterov, const std::vector<Task>& tasks) {
     size_t first = 0;
     while (first < tasks.size()) {
-        // macro-tiles of 128 x 128 as soon as they fill the chip
-        const size_t most = std::min(tasks.size() - first, (size_t)kGroupMatrices);
-        auto count = [&](size_t k, int mt) {
-            const nnt_tensor* t = tasks[first + k].G;
-            return (t->shape[0] + mt - 1) / mt * ((t->shape[1] + mt - 1) / mt);
-        };
-        size_t n = 0;
-        int64_t wide = 0;
-        while (n < most && wide < 1024) wide += count(n++, 128);
-        const int wt = wide >= 256 ? 64 : 32, mt = 2 * wt;
         NsGroup g{};
-        g.n = (int32_t)n;
+        NsSizes sizes{};
         g.nesterov = nesterov;
         g.mu = mu;
         g.a = (float)cfg.a;
         g.b = (float)cfg.b;
         g.c = (float)cfg.c;
         g.eps = (float)cfg.eps;
-        int64_t bytes = 0, sym = 0, full = 0, patch = 0, chunks = 0;
+        int64_t bytes = (sizeof(NsGroup) + 255) / 256 * 256, patch = 0, chunks = 0;
         double work = 0.0;
         std::vector<Access> acc;
-        for (size_t k = 0; k < n; k++) {
-            const Task& t = tasks[first + k];
-            NsMatrix& q = g.mat[k];
-            q.rows = (int32_t)t.G->shape[0];
-            q.cols = (int32_t)t.G->shape[1];
+        while (first < tasks.size() && g.n < kGroupMatrices && patch < 4096) {
+            const Task& t = tasks[first++];
+            const int64_t rows = t.G->shape[0], cols = t.G->shape[1], m = std::min(rows, cols), l = std::max(rows, cols);
+            const int64_t mb = (m + 63) / 64, nb = (l + 63) / 64;
+            if (nb > 0xffff || mb * nb > (1 << 24)) return fail(ctx, NNT_EINVAL, std::string(label) + ": matrix too large");
+            sizes.blocks[g.n] = (uint32_t)mb | ((uint32_t)nb << 16);
+            NsMatrix& q = g.mat[g.n++];
+            q.rows = (int32_t)rows;
+            q.cols = (int32_t)cols;
             q.base0 = (int32_t)t.G->base[0];
             q.base1 = (int32_t)t.G->base[1];
             q.grid0 = (int32_t)t.G->grid[0];
             q.grid1 = (int32_t)t.G->grid[1];
-            q.flip = q.rows > q.cols;
-            q.mp = (std::min(q.rows, q.cols) + mt - 1) / mt * mt;
-            q.np = (std::max(q.rows, q.cols) + mt - 1) / mt * mt;
-            q.first_sym = (int32_t)sym;
-            q.first_full = (int32_t)full;
-            q.first_patch = (int32_t)patch;
-            const int64_t tm = q.mp / mt, tn = q.np / mt;
-            sym += tm * (tm + 1) / 2;
-            full += tm * tn;
-            patch += (int64_t)(q.mp / 64) * (q.np / 64);
-            chunks = std::max(chunks, ((int64_t)q.base0 * q.base1 + 2047) / 2048 * q.grid0 * q.grid1);
+            q.flip = rows > cols;
+            q.mp = (int32_t)(mb * 64);
+            q.np = (int32_t)(nb * 64);
+            patch += mb * nb;
+            chunks = std::max(chunks, (t.G->base[0] * t.G->base[1] + kNormChunk - 1) / kNormChunk * t.G->grid[0] * t.G->grid[1]);
             const int64_t x = (int64_t)q.mp * q.np * 4, a = (int64_t)q.mp * q.mp * 4;
             q.X = bytes;
             q.XT = q.X + 2 * x;
@@ -475,35 +822,38 @@ int32_t newton_schulz(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_c
             if (t.LP) q.LP = MatView{t.LP->d_tiles, NNT_BF16};
             q.decay = t.decay;
             q.step = t.step;
-            const double m = std::min(q.rows, q.cols), l = std::max(q.rows, q.cols);
-            work += cfg.steps * (3.0 * m * m * l + m * m * m);
+            work += cfg.steps * (3.0 * m * m * l + (double)m * m * m);
             acc.push_back(t.G->all(kRead));
             acc.push_back(t.P->all(t.step < 0.f ? kWrite : kReadWrite));
             if (t.M) acc.push_back(t.M->all(kReadWrite));
             if (t.LP) acc.push_back(t.LP->all(kWrite));
         }
-        if (full > INT32_MAX || patch > INT32_MAX) return fail(ctx, NNT_EINVAL, std::string(label) + ": matrix too large");
         g.norm_blocks = (int32_t)std::min<int64_t>(chunks, kNormBlocks);
+        sizes.n = g.n;
+        const Launch gram = choose(sizes, kGram), poly = choose(sizes, kPoly), step = choose(sizes, kStep);
+        g.partial = bytes;
+        if (gram.splits > 1) bytes += (int64_t)gram.tiles * gram.splits * (gram.shape == 0 ? Small::BM * Small::BM : Middle::BM * Middle::BM) * 4;
         const int32_t rc = ensure_matrix_scratch(ctx, bytes);
         if (rc != NNT_OK) return rc;
         g.space = reinterpret_cast<char*>(ctx->matrix_scratch);
         acc.push_back(Access{&ctx->matrix_dep, 1, kReadWrite});
         const int steps = cfg.steps;
         OpTag tag(ctx, label, work, false);
+        const NsGroup* there = reinterpret_cast<const NsGroup*>(g.space);
         const int32_t sc = submit(ctx, acc, [=](hipStream_t st) {
-            hipLaunchKernelGGL(ns_norm_kernel, dim3((unsigned)g.norm_blocks, (unsigned)g.n), dim3(256), 0, st, g);
-            hipLaunchKernelGGL(ns_split_kernel, dim3((unsigned)patch), dim3(256), 0, st, g);
+            hipLaunchKernelGGL(ns_norm_kernel, dim3((unsigned)g.norm_blocks, (unsigned)g.n), dim3(1024), 0, st, g);
+            hipLaunchKernelGGL(ns_split_kernel, dim3((unsigned)patch), dim3(256), 0, st, there, sizes);
             for (int s = 0; s < steps; s++) {
                 for (int mode : {(int)kGram, (int)kPoly, s + 1 < steps ? (int)kStep : (int)kLast}) {
-                    const unsigned wgs = (unsigned)(mode == kGram || mode == kPoly ? sym : full);
-                    if (wt == 64) launch_product<64>(mode, g, s & 1, wgs, st);
-                    else launch_product<32>(mode, g, s & 1, wgs, st);
+                    const Launch& l = mode == kGram ? gram : mode == kPoly ? poly : step;
+                    if (l.shape == 2) launch_product<Large>(mode, there, sizes, s & 1, l.tiles, l.splits, st);
+                    else if (l.shape == 1) launch_product<Middle>(mode, there, sizes, s & 1, l.tiles, l.splits, st);
+                    else launch_product<Small>(mode, there, sizes, s & 1, l.tiles, l.splits, st);
                 }
             }
             return launched();
-        }, 2 + 3 * steps);
+        }, 2 + (gram.splits > 1 ? 4 : 3) * steps);
         if (sc != NNT_OK) return sc;
-        first += n;
     }
     return NNT_OK;
 }
