@@ -71,8 +71,29 @@ struct NsGroup {
 
 static_assert(sizeof(NsGroup) <= 4096 && sizeof(NsGroup) % 4 == 0, "copied by one workgroup, a word to a thread");
 
-__device__ __forceinline__ float load_of(const MatView& v, int tile, int64_t off) {
-    return v.dtype == NNT_F32 ? global_as<const float>(v.tiles[tile])[off] : bf2f(global_as<const bf16_t>(v.tiles[tile])[off]);
+// 16 columns, from column c0 on, of a row of a matrix: t0, o0, e0 are its tile, its place in it and the tile's height; 0 where there is none
+template <typename T>
+__device__ __forceinline__ void read_columns_as(const NsMatrix& q, void* const* tiles, bool there, int t0, int o0, int e0, int c0, float (&v)[16]) {
+    int t1 = c0 / q.base1, c1 = c0 - t1 * q.base1;
+    const T* p = there && c0 < q.cols ? global_as<const T>(tiles[t0 + q.grid0 * t1]) + o0 + (int64_t)e0 * c1 : nullptr;
+#pragma unroll
+    for (int s = 0; s < 16; s++) {
+        v[s] = 0.f;
+        if (there && c0 + s < q.cols) {
+            if constexpr (sizeof(T) == 4) v[s] = *p;
+            else v[s] = bf2f(*p);
+        }
+        p += e0;
+        if (++c1 == q.base1) {                           // (the tiles' pointers are looked up once each)
+            c1 = 0;
+            t1++;
+            if (there && c0 + s + 1 < q.cols) p = global_as<const T>(tiles[t0 + q.grid0 * t1]) + o0;
+        }
+    }
+}
+__device__ __forceinline__ void read_columns(const NsMatrix& q, const MatView& w, bool there, int t0, int o0, int e0, int c0, float (&v)[16]) {
+    if (w.dtype == NNT_F32) read_columns_as<float>(q, w.tiles, there, t0, o0, e0, c0, v);
+    else read_columns_as<bf16_t>(q, w.tiles, there, t0, o0, e0, c0, v);
 }
 
 // ---------------------------------------------------------------- momentum and norm
@@ -190,21 +211,8 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict
     const int r0 = q.flip ? j0 : i0, c0 = __builtin_amdgcn_readfirstlane((q.flip ? i0 : j0) + wave * 16);
     const int r = r0 + lane, t0 = min(r, q.rows - 1) / q.base0, o0 = r - t0 * q.base0, e0 = min(q.base0, q.rows - t0 * q.base0);
     float u[16], m[16];
-    int t1 = c0 / q.base1, c1 = c0 - t1 * q.base1;
-#pragma unroll
-    for (int s = 0; s < 16; s++) {
-        u[s] = m[s] = 0.f;
-        if (r < q.rows && c0 + s < q.cols) {
-            const int tile = t0 + q.grid0 * t1;
-            const int64_t off = o0 + (int64_t)e0 * c1;
-            u[s] = load_of(q.G, tile, off);
-            if (g.mu >= 0.f) m[s] = global_as<const float>(q.M.tiles[tile])[off];
-        }
-        if (++c1 == q.base1) {
-            c1 = 0;
-            t1++;
-        }
-    }
+    read_columns(q, q.G, r < q.rows, t0, o0, e0, c0, u);
+    if (g.mu >= 0.f) read_columns(q, q.M, r < q.rows, t0, o0, e0, c0, m);
     const double* part = reinterpret_cast<const double*>(g.space + q.part);
     double sum = 0.0;
     for (int k = tid; k < g.norm_blocks; k += 256) sum += part[k];
@@ -502,11 +510,12 @@ __global__ void __launch_bounds__(64 * S::kWaves, 2) ns_product_kernel(const NsG
         const int total = gridDim.x, per = total / 8, rest = total % 8, die = wg % 8;
         wg = die * per + min(die, rest) + wg / 8;
     }
-    // A's contraction may be cut: the parts of a tile lie side by side
+    // A's contraction may be cut: the tiles of one part lie side by side, so that a die finds most of what they share in its own cache
     int part = 0;
     if constexpr (MODE == kGram) {
-        part = wg % splits;
-        wg /= splits;
+        const int tiles = gridDim.x / splits;
+        part = wg / tiles;
+        wg -= part * tiles;
     }
     const int tile = wg;                                         // of all matrices
     const NsMatrix& q = g.mat[matrix_of<kSym, S::BM>(sizes, wg)];
@@ -674,6 +683,217 @@ __global__ void __launch_bounds__(256) ns_combine_kernel(const NsGroup* __restri
     store_results<kGram, 1, 1>(g, q, acc, ti * S::BM + (w % S::WR * S::FM + x) * 32, tj * S::BN + (w / S::WR * S::FN + y) * 32, ti == tj, now, turn + wave * 32 * turn_pitch(1));
 }
 
+// ---------------------------------------------------------------- matrices with a side of at most 64
+// Here a launch is longer than what it computes, so a whole iteration is one launch.  A workgroup holds some of X's column blocks of 64; it adds up the
+// parts of A that the workgroups have left (its own and the others'), computes B (64 x 64, every workgroup the same), its blocks of X and their
+// part of the next A.  X is kept as its transpose only.  The first launch takes U in place of B X, the last one leaves the results.
+enum { kFirst, kMiddle, kFinal };
+
+// how many workgroups share a matrix of nt column blocks: each adds up as many parts (0.2 us) as there are, and takes nt / parts blocks (1.5 us) in turn
+__host__ __device__ inline int narrow_parts(int nt) { return nt <= 16 ? nt : nt <= 64 ? 16 : 32; }
+constexpr int kNarrowBlocks = 256;                       // longer matrices take the products above
+
+constexpr int kImage = 4 * kPanelBytes;                  // 64 x 64: four panels
+__device__ __forceinline__ int image_at(int row, int k) { return (k >> 4) * kPanelBytes + ((k & 15) >> 3) * 1024 + row * 16 + (k & 7) * 2; }
+
+// A wavefront's block of 32 x 32 of the product of two images: rows r0 of the first, rows c0 of the second, over all 64 columns.
+template <typename LoadQ>
+__device__ __forceinline__ void multiply(const char* image, int r0, LoadQ&& second, f32x16& acc) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int ks = 0; ks < 4; ks++) {
+        const char* p = image + ks * kPanelBytes + (lane >> 5) * 1024 + (r0 + (lane & 31)) * 16;
+        const f16x8 ph = *reinterpret_cast<const f16x8*>(p), pl = *reinterpret_cast<const f16x8*>(p + kPartBytes);
+        f16x8 qh, ql;
+        second(ks, qh, ql);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc, 0, 0, 0);
+    }
+}
+__device__ __forceinline__ void multiply(const char* image, int r0, const char* second, int c0, f32x16& acc) {
+    const int lane = threadIdx.x & 63;
+    multiply(image, r0, [&](int ks, f16x8& qh, f16x8& ql) {
+        const char* p = second + ks * kPanelBytes + (lane >> 5) * 1024 + (c0 + (lane & 31)) * 16;
+        qh = *reinterpret_cast<const f16x8*>(p);
+        ql = *reinterpret_cast<const f16x8*>(p + kPartBytes);
+    }, acc);
+}
+
+template <int PHASE>
+__global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restrict__ group, NsSizes sizes, int now) {
+    const NsGroup& g = *group;
+    __shared__ __align__(16) char image[3][kImage];      // A (set-up: U in fp32), B, X's block with its rows along the contraction
+    __shared__ double red[4];
+    const int nt = sizes.blocks[blockIdx.y] >> 16, parts = narrow_parts(nt), part = blockIdx.x;
+    if (part >= parts) return;
+    const NsMatrix& q = g.mat[blockIdx.y];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave & 1, wc = wave >> 1;
+    float4* sums = reinterpret_cast<float4*>(g.space + q.A);             // two buffers of `parts` images of 64 x 64 in fp32, as they lie in registers
+    auto sum_at = [&](int buffer, int p, int v) { return (((int64_t)buffer * parts + p) * 4 + wave) * 256 + v * 64 + lane; };
+    const int i = wr * 32 + (lane >> 5) * 4, j = wc * 32 + (lane & 31);    // this lane's results: rows i + 8 p + 0 .. 3, column j of a block
+    float scale = 0.f;
+    if constexpr (PHASE == kFirst) {
+        const double* norms = reinterpret_cast<const double*>(g.space + q.part);
+        double sum = 0.0;
+        for (int k = tid; k < g.norm_blocks; k += 256) sum += norms[k];
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        if (lane == 0) red[wave] = sum;
+        __syncthreads();
+        scale = (float)((double)kScale / (sqrt(red[0] + red[1] + red[2] + red[3]) + (double)g.eps));
+    } else {
+        float4 t[4];
+#pragma unroll
+        for (int v = 0; v < 4; v++) t[v] = sums[sum_at(now, 0, v)];
+#pragma unroll 4
+        for (int p = 1; p < parts; p++) {
+#pragma unroll
+            for (int v = 0; v < 4; v++) {
+                const float4 u = sums[sum_at(now, p, v)];
+                t[v].x += u.x;
+                t[v].y += u.y;
+                t[v].z += u.z;
+                t[v].w += u.w;
+            }
+        }
+        // (A and B are symmetric: a lane's four rows of a column are four columns of a row)
+        float a[4][4];
+        auto store = [&](char* dst, const float (&x)[4][4]) {
+#pragma unroll
+            for (int p = 0; p < 4; p++) {
+                f16x4 hi, lo;
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    _Float16 h, l;
+                    split(x[p][k], h, l);
+                    hi[k] = h;
+                    lo[k] = l;
+                }
+                char* d = dst + image_at(j, i + p * 8);
+                *reinterpret_cast<f16x4*>(d) = hi;
+                *reinterpret_cast<f16x4*>(d + kPartBytes) = lo;
+            }
+        };
+#pragma unroll
+        for (int p = 0; p < 4; p++) {
+            a[p][0] = t[p].x / kScale;
+            a[p][1] = t[p].y / kScale;
+            a[p][2] = t[p].z / kScale;
+            a[p][3] = t[p].w / kScale;
+        }
+        store(image[0], a);
+        __syncthreads();
+        f32x16 acc;
+#pragma unroll
+        for (int k = 0; k < 16; k++) acc[k] = 0.f;
+        multiply(image[0], wr * 32, image[0], wc * 32, acc);
+#pragma unroll
+        for (int p = 0; p < 4; p++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) a[p][k] = fmaf(g.b, a[p][k], acc[p * 4 + k] * (g.c / kScale));
+        store(image[1], a);
+        __syncthreads();
+    }
+    f32x16 gram;
+#pragma unroll
+    for (int k = 0; k < 16; k++) gram[k] = 0.f;
+    for (int t = part * nt / parts; t < (part + 1) * nt / parts; t++) {
+        char* X = in_global(g.space + q.XT + (int64_t)t * kImage);
+        if constexpr (PHASE == kFirst) {
+            float (*u)[65] = reinterpret_cast<float (*)[65]>(image[0]);      // [i][j] (16640 bytes: reaches into the second image, which is free)
+            const int r0 = q.flip ? t * 64 : 0, c0 = (q.flip ? 0 : t * 64) + wave * 16;
+            const int r = r0 + lane, t0 = min(r, q.rows - 1) / q.base0, o0 = r - t0 * q.base0, e0 = min(q.base0, q.rows - t0 * q.base0);
+            float x[16], m[16];
+            read_columns(q, q.G, r < q.rows, t0, o0, e0, c0, x);
+            if (g.mu >= 0.f) read_columns(q, q.M, r < q.rows, t0, o0, e0, c0, m);
+#pragma unroll
+            for (int s = 0; s < 16; s++) {
+                if (g.mu >= 0.f) x[s] = g.nesterov ? fmaf(g.mu, m[s], x[s]) : m[s];
+                if (q.flip) u[wave * 16 + s][lane] = x[s] * scale;
+                else u[lane][wave * 16 + s] = x[s] * scale;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int k = (wave * 2 + h) * 8;
+                f16x8 hi, lo;
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    _Float16 y, z;
+                    split(u[lane][k + e], y, z);
+                    hi[e] = y;
+                    lo[e] = z;
+                }
+                char* d = image[2] + image_at(lane, k);
+                *reinterpret_cast<f16x8*>(d) = hi;
+                *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    _Float16 y, z;
+                    split(u[k + e][lane], y, z);
+                    hi[e] = y;
+                    lo[e] = z;
+                }
+                d = X + image_at(lane, k);
+                *reinterpret_cast<f16x8*>(d) = hi;
+                *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
+            }
+        } else {
+            f16x4 eh[4], el[4];
+#pragma unroll
+            for (int p = 0; p < 4; p++) {
+                const char* e = X + image_at(j, i + p * 8);
+                eh[p] = *reinterpret_cast<const f16x4*>(e);
+                el[p] = *reinterpret_cast<const f16x4*>(e + kPartBytes);
+            }
+            f32x16 acc;
+#pragma unroll
+            for (int k = 0; k < 16; k++) acc[k] = 0.f;
+            multiply(image[1], wr * 32, X, wc * 32, acc);
+            float x[4][4];
+#pragma unroll
+            for (int p = 0; p < 4; p++)
+#pragma unroll
+                for (int k = 0; k < 4; k++) x[p][k] = fmaf(g.a, (float)eh[p][k] + (float)el[p][k], acc[p * 4 + k] / kScale);
+            if constexpr (PHASE == kFinal) {
+#pragma unroll
+                for (int p = 0; p < 4; p++)
+#pragma unroll
+                    for (int k = 0; k < 4; k++) x[p][k] *= 1.f / kScale;
+                apply_results(q, x, i, t * 64 + j);
+                continue;
+            }
+            __syncthreads();                             // everybody has read X's block, which is overwritten, and is done with the last one's image
+#pragma unroll
+            for (int p = 0; p < 4; p++) {
+                f16x4 hi, lo;
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    _Float16 h, l;
+                    split(x[p][k], h, l);
+                    hi[k] = h;
+                    lo[k] = l;
+                    char* d = image[2] + image_at(i + p * 8 + k, j);
+                    *reinterpret_cast<_Float16*>(d) = h;
+                    *reinterpret_cast<_Float16*>(d + kPartBytes) = l;
+                }
+                char* d = X + image_at(j, i + p * 8);
+                *reinterpret_cast<f16x4*>(d) = hi;
+                *reinterpret_cast<f16x4*>(d + kPartBytes) = lo;
+            }
+        }
+        __syncthreads();
+        multiply(image[2], wr * 32, image[2], wc * 32, gram);
+        if constexpr (PHASE == kFirst) __syncthreads();  // (before the next block's U and image)
+    }
+    if constexpr (PHASE != kFinal) {
+        const int next = PHASE == kFirst ? now : 1 - now;
+#pragma unroll
+        for (int v = 0; v < 4; v++) sums[sum_at(next, part, v)] = make_float4(gram[4 * v], gram[4 * v + 1], gram[4 * v + 2], gram[4 * v + 3]);
+    }
+}
+
 // ---------------------------------------------------------------- host side
 int32_t launched() { return hipGetLastError() == hipSuccess ? (int32_t)NNT_OK : (int32_t)NNT_EHIP; }
 
@@ -746,7 +966,7 @@ Launch choose(const NsSizes& g, int mode) {
             panels += t * c;
             longest = std::max(longest, c);
         }
-        for (int splits = 1; splits <= 64; splits++) {
+        for (int splits = 1; splits <= 64; splits *= 2) {
             if (splits > 1 && (mode != kGram || s == 2 || tiles * splits > 512 || longest / splits < 8)) break;
             const double each = (double)panels / tiles / splits;                       // panels of a workgroup, on average
             const double per = std::ceil(tiles * splits / 256.0);
@@ -777,7 +997,7 @@ Launch choose(const NsSizes& g, int mode) {
 
 // Orthogonalises the matrices of `tasks` and applies the results, as many of them in one set of launches as it takes to fill the
 // chip.  mu < 0: no momentum.
-int32_t newton_schulz(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& cfg, float mu, int nesterov, const std::vector<Task>& tasks) {
+int32_t run_tasks(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& cfg, float mu, int nesterov, const std::vector<Task>& tasks, bool narrow) {
     size_t first = 0;
     while (first < tasks.size()) {
         NsGroup g{};
@@ -809,9 +1029,11 @@ int32_t newton_schulz(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_c
             q.np = (int32_t)(nb * 64);
             patch += mb * nb;
             chunks = std::max(chunks, (t.G->base[0] * t.G->base[1] + kNormChunk - 1) / kNormChunk * t.G->grid[0] * t.G->grid[1]);
-            const int64_t x = (int64_t)q.mp * q.np * 4, a = (int64_t)q.mp * q.mp * 4;
+            // (narrow ones: the transpose once, and A in parts)
+            const int64_t x = narrow ? (int64_t)q.mp * q.np * 2 : (int64_t)q.mp * q.np * 4;
+            const int64_t a = narrow ? (int64_t)narrow_parts((int)nb) * 64 * 64 * 4 : (int64_t)q.mp * q.mp * 4;
             q.X = bytes;
-            q.XT = q.X + 2 * x;
+            q.XT = narrow ? bytes : q.X + 2 * x;
             q.A = q.XT + 2 * x;
             q.B = q.A + a;
             q.part = q.B + a;
@@ -830,9 +1052,11 @@ int32_t newton_schulz(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_c
         }
         g.norm_blocks = (int32_t)std::min<int64_t>(chunks, kNormBlocks);
         sizes.n = g.n;
+        int parts = 0;
+        for (int k = 0; k < g.n; k++) parts = std::max(parts, narrow_parts((int)(sizes.blocks[k] >> 16)));
         const Launch gram = choose(sizes, kGram), poly = choose(sizes, kPoly), step = choose(sizes, kStep);
         g.partial = bytes;
-        if (gram.splits > 1) bytes += (int64_t)gram.tiles * gram.splits * (gram.shape == 0 ? Small::BM * Small::BM : Middle::BM * Middle::BM) * 4;
+        if (!narrow && gram.splits > 1) bytes += (int64_t)gram.tiles * gram.splits * (gram.shape == 0 ? Small::BM * Small::BM : Middle::BM * Middle::BM) * 4;
         const int32_t rc = ensure_matrix_scratch(ctx, bytes);
         if (rc != NNT_OK) return rc;
         g.space = reinterpret_cast<char*>(ctx->matrix_scratch);
@@ -842,6 +1066,13 @@ int32_t newton_schulz(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_c
         const NsGroup* there = reinterpret_cast<const NsGroup*>(g.space);
         const int32_t sc = submit(ctx, acc, [=](hipStream_t st) {
             hipLaunchKernelGGL(ns_norm_kernel, dim3((unsigned)g.norm_blocks, (unsigned)g.n), dim3(1024), 0, st, g);
+            if (narrow) {
+                const dim3 grid((unsigned)parts, (unsigned)g.n), block(256);
+                hipLaunchKernelGGL((ns_narrow_kernel<kFirst>), grid, block, 0, st, there, sizes, 0);
+                for (int s = 0; s + 1 < steps; s++) hipLaunchKernelGGL((ns_narrow_kernel<kMiddle>), grid, block, 0, st, there, sizes, s & 1);
+                hipLaunchKernelGGL((ns_narrow_kernel<kFinal>), grid, block, 0, st, there, sizes, (steps - 1) & 1);
+                return launched();
+            }
             hipLaunchKernelGGL(ns_split_kernel, dim3((unsigned)patch), dim3(256), 0, st, there, sizes);
             for (int s = 0; s < steps; s++) {
                 for (int mode : {(int)kGram, (int)kPoly, s + 1 < steps ? (int)kStep : (int)kLast}) {
@@ -852,8 +1083,21 @@ int32_t newton_schulz(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_c
                 }
             }
             return launched();
-        }, 2 + (gram.splits > 1 ? 4 : 3) * steps);
+        }, narrow ? 2 + steps : 2 + (gram.splits > 1 ? 4 : 3) * steps);
         if (sc != NNT_OK) return sc;
+    }
+    return NNT_OK;
+}
+
+int32_t newton_schulz(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& cfg, float mu, int nesterov, const std::vector<Task>& tasks) {
+    std::vector<Task> kind[2];
+    for (const Task& t : tasks) {
+        const int64_t m = std::min(t.G->shape[0], t.G->shape[1]), l = std::max(t.G->shape[0], t.G->shape[1]);
+        kind[m <= 64 && l <= 64 * kNarrowBlocks].push_back(t);
+    }
+    for (int narrow = 0; narrow < 2; narrow++) {
+        const int32_t rc = run_tasks(ctx, label, cfg, mu, nesterov, kind[narrow], narrow != 0);
+        if (rc != NNT_OK) return rc;
     }
     return NNT_OK;
 }

@@ -44,7 +44,7 @@ def handles(mods, ts):
 
 
 SHAPES = [((1, 1), (1, 1)), ((1, 40), (1, 40)), ((40, 1), (7, 1)), ((3, 5), (2, 2)), ((64, 64), (64, 64)), ((64, 256), (32, 32)), ((65, 63), (65, 63)), ((129, 400), (100, 128)),
-          ((400, 129), (128, 100)), ((192, 192), (37, 64)), ((777, 1111), (300, 300)), ((1111, 777), (300, 300)), ((30, 2500), (30, 1000)), ((1536, 2100), (512, 512)), ((2100, 1536), (2100, 1536))]
+          ((400, 129), (128, 100)), ((192, 192), (37, 64)), ((777, 1111), (300, 300)), ((1111, 777), (300, 300)), ((30, 2500), (30, 1000)), ((64, 5000), (64, 900)), ((4100, 33), (1000, 33)), ((20, 17000), (20, 17000)), ((64, 1024), (64, 1024)), ((64, 1089), (30, 500)), ((1536, 2100), (512, 512)), ((2100, 1536), (2100, 1536))]
 
 
 @pytest.mark.parametrize("types", ["f32 f32", "bf16 bf16", "f32 bf16", "bf16 f32"])
