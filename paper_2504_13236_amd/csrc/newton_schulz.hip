@@ -897,19 +897,35 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
 // ---------------------------------------------------------------- host side
 int32_t launched() { return hipGetLastError() == hipSuccess ? (int32_t)NNT_OK : (int32_t)NNT_EHIP; }
 
-// Whether the iteration stays where the workspace's numbers can hold it: singular values start in [0, 1]; followed on a grid, they, their squares' polynomial
-// and its parts have to stay below 8 (2^12 times 16 is fp16's largest number).
+// The largest |c1 x + c2 x^2| between 0 and x = top.
+double most_of_square(double c1, double c2, double top) {
+    double most = std::fabs(c1 * top + c2 * top * top);
+    if (c2 != 0.0) {
+        const double x = -c1 / (2.0 * c2);
+        if (x > 0.0 && x < top) most = std::max(most, std::fabs(c1 * x + c2 * x * x));
+    }
+    return most;
+}
+// Whether the iteration stays where the workspace's numbers can hold it (2^12 times 16 is fp16's largest number): singular values start in [0, 1]; with their
+// bound followed from step to step, they, their squares and b s^2 + c s^4 have to stay below 8.
 bool in_range(const nnt_newton_schulz_cfg& c) {
     if (!std::isfinite(c.a) || !std::isfinite(c.b) || !std::isfinite(c.c) || !(c.eps > 0.0) || !std::isfinite(c.eps) || c.steps < 1 || c.steps > 64) return false;
-    constexpr int n = 4096;
-    for (int k = 0; k <= n; k++) {
-        double s = (double)k / n;
-        for (int t = 0; t < c.steps; t++) {
-            const double l = s * s, p = c.b * l + c.c * l * l;
-            if (!(l <= 8.0) || !(std::fabs(p) <= 8.0)) return false;
-            s = std::fabs(s * (c.a + p));
-            if (!(s <= 8.0)) return false;
+    double top = 1.0;
+    for (int t = 0; t < c.steps; t++) {
+        const double l = top * top;
+        if (!(most_of_square(c.b, c.c, l) <= 8.0)) return false;
+        // f(s) = a s + b s^3 + c s^5 is largest at the end or where a + 3 b s^2 + 5 c s^4 = 0
+        auto f = [&](double x) { return std::fabs(std::sqrt(x) * (c.a + c.b * x + c.c * x * x)); };
+        double most = f(l);
+        const double p = 3.0 * c.b, q = 5.0 * c.c, d = p * p - 4.0 * q * c.a;
+        if (q == 0.0) {
+            if (p != 0.0 && -c.a / p > 0.0 && -c.a / p < l) most = std::max(most, f(-c.a / p));
+        } else if (d >= 0.0) {
+            for (double x : {(-p + std::sqrt(d)) / (2.0 * q), (-p - std::sqrt(d)) / (2.0 * q)})
+                if (x > 0.0 && x < l) most = std::max(most, f(x));
         }
+        if (!(most <= 8.0) || !(most * most <= 8.0)) return false;
+        top = most;
     }
     return true;
 }
