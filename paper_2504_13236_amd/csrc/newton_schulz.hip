@@ -47,7 +47,7 @@ struct NsMatrix {
     int32_t rows, cols, base0, base1, grid0, grid1;      // the tensors' geometry
     int32_t flip;                                        // X is the transpose (more rows than columns)
     int32_t mp, np;                                      // X's extents, mp <= np, padded to whole panels of 64 rows
-    int64_t X, XT, A, B, part;                           // bytes from the start of the workspace; X and XT: two buffers each, one behind the other
+    int64_t X, XT, A, part;                              // bytes from the start of the workspace; X and XT: two buffers each, one behind the other; A: see NsOp
     MatView G, M, P, LP;                                 // gradient, momentum, parameter (or result), bf16 copy
     float decay, step;                                   // P <- decay P - step X (step < 0: P <- X)
 };
@@ -261,6 +261,14 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict
 // ---------------------------------------------------------------- products
 enum { kGram, kPoly, kStep, kLast };
 
+// What a product of square symmetric matrices, or one with X, is made of.  The group's matrices have up to four square buffers each (0: A).
+//   kPoly  buffer d = mul (buffer p)(buffer q) + add (buffer e) + diag I
+//   kStep  X = (buffer p) X + add X;  kLast  the same, applied
+struct NsOp {
+    int32_t p, q, e, d;
+    float mul, add, diag;
+};
+
 // One result's place in the tensor, found from its row and column of X.
 __device__ __forceinline__ void apply_one(const NsMatrix& q, float x, int i, int j) {
     const int r = q.flip ? j : i, c = q.flip ? i : j;
@@ -347,19 +355,21 @@ __device__ __forceinline__ void apply_results(const NsMatrix& q, const float (&x
 // The result path of a wavefront: FM x FN blocks of 32 x 32 from row i0 and column j0 on.  `turn`: LDS for 32 rows, in which the results change places.
 constexpr int turn_pitch(int FN) { return 32 * FN + 8; }         // in 32-bit words
 template <int MODE, int FM, int FN>
-__device__ __forceinline__ void store_results(const NsGroup& g, const NsMatrix& q, const f32x16 (&acc)[FM][FN], int i0, int j0, bool diagonal, int now, uint32_t* turn) {
+__device__ __forceinline__ void store_results(const NsGroup& g, const NsMatrix& q, const f32x16 (&acc)[FM][FN], int i0, int j0, bool diagonal, int now, const NsOp& op, uint32_t* turn) {
     // results: this lane has column j0 + 32 y + (lane & 31), rows i0 + 32 x + 8 p + 4 (lane >> 5) + 0 .. 3
     constexpr bool kSym = MODE == kGram || MODE == kPoly;
     constexpr int kPitch = turn_pitch(FN);
     const int lane = threadIdx.x & 63;
     const int64_t xbytes = (int64_t)q.mp * q.np * 4;
-    const char* E = g.space + (MODE == kPoly ? q.A : q.XT + now * xbytes);          // the term that is added, laid out like the result
-    char* D = g.space + (MODE == kGram ? q.A : MODE == kPoly ? q.B : q.XT + (1 - now) * xbytes);
+    const int64_t square = (int64_t)q.mp * q.mp * 4;
+    const char* E = g.space + (MODE == kPoly ? q.A + op.e * square : q.XT + now * xbytes);          // the term that is added, laid out like the result
+    char* D = g.space + (MODE == kGram ? q.A : MODE == kPoly ? q.A + op.d * square : q.XT + (1 - now) * xbytes);
     char* Dt = kSym ? D : g.space + q.X + (1 - now) * xbytes;                       // the same with rows and columns exchanged
     const int Kt = kSym ? q.mp : q.np;
     const bool turned = MODE != kLast && !(kSym && diagonal);
-    const float factor = (MODE == kPoly ? g.c : 1.f) / kScale;      // sums carry the scale twice
-    const float add = MODE == kPoly ? g.b : g.a;
+    const float factor = (MODE == kPoly ? op.mul : 1.f) / kScale;      // sums carry the scale twice
+    const float add = op.add, diag = op.diag * kScale;
+    const bool fetches = MODE != kGram && add != 0.f;
     // what is added is fetched one block of 32 rows ahead: behind the stores that the compiler cannot tell apart from it every load would wait
     f16x4 e[2][FN][4][2];
     // (blocks behind the last row block of X or of its transpose are not there)
@@ -377,11 +387,10 @@ __device__ __forceinline__ void store_results(const NsGroup& g, const NsMatrix& 
             }
         }
     };
-    if constexpr (MODE != kGram) fetch(0);
+    if (fetches) fetch(0);
 #pragma unroll
     for (int x = 0; x < FM; x++) {
-        if constexpr (MODE != kGram)
-            if (x + 1 < FM) fetch(x + 1);
+        if (fetches && x + 1 < FM) fetch(x + 1);
         if (i0 + x * 32 >= rows) continue;
 #pragma unroll
         for (int y = 0; y < FN; y++) {
@@ -392,7 +401,9 @@ __device__ __forceinline__ void store_results(const NsGroup& g, const NsMatrix& 
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
                     v[p][k] = acc[x][y][p * 4 + k] * factor;
-                    if constexpr (MODE != kGram) v[p][k] = fmaf(add, (float)e[x & 1][y][p][0][k] + (float)e[x & 1][y][p][1][k], v[p][k]);
+                    if (fetches) v[p][k] = fmaf(add, (float)e[x & 1][y][p][0][k] + (float)e[x & 1][y][p][1][k], v[p][k]);
+                    if constexpr (MODE == kPoly)
+                        if (diagonal && i0 + x * 32 + p * 8 + (lane >> 5) * 4 + k == j0 + y * 32 + (lane & 31)) v[p][k] += diag;
                     if constexpr (MODE == kLast) v[p][k] *= 1.f / kScale;
                 }
             const int i = i0 + x * 32, j = j0 + y * 32 + (lane & 31);
@@ -498,7 +509,7 @@ __device__ __forceinline__ void tile_of(int p, int tm, int tn, int& ti, int& tj)
 // its fragments and for its own loads of the next step; the barrier behind that makes the next stage complete for everybody and the present one, whose
 // fragments all have, free for the loads of step + ST.  LDS reads and their waits are spelled out: the compiler would wait for all loads in flight.
 template <int MODE, typename S>
-__global__ void __launch_bounds__(64 * S::kWaves, 2) ns_product_kernel(const NsGroup* __restrict__ group, NsSizes sizes, int now, int splits) {
+__global__ void __launch_bounds__(64 * S::kWaves, 2) ns_product_kernel(const NsGroup* __restrict__ group, NsSizes sizes, NsOp op, int now, int splits) {
     const NsGroup& g = *group;
     constexpr int FM = S::FM, FN = S::FN, ST = S::ST;
     __shared__ __align__(1024) char lds[S::kLds];
@@ -526,8 +537,9 @@ __global__ void __launch_bounds__(64 * S::kWaves, 2) ns_product_kernel(const NsG
     tj = __builtin_amdgcn_readfirstlane(tj);
     const int64_t xbytes = (int64_t)q.mp * q.np * 4;
     const int nk = (MODE == kGram ? q.np : q.mp) >> 4;           // panels along the contraction, a multiple of 4
-    const char* Pb = g.space + (MODE == kGram ? q.X + now * xbytes : MODE == kPoly ? q.A : q.B);
-    const char* Qb = g.space + (MODE == kGram ? q.X + now * xbytes : MODE == kPoly ? q.A : q.XT + now * xbytes);
+    const int64_t square = (int64_t)q.mp * q.mp * 4;
+    const char* Pb = g.space + (MODE == kGram ? q.X + now * xbytes : q.A + op.p * square);
+    const char* Qb = g.space + (MODE == kGram ? q.X + now * xbytes : MODE == kPoly ? q.A + op.q * square : q.XT + now * xbytes);
 
     // a wavefront loads a part of one row block's panels per step
     const char* src;
@@ -640,12 +652,12 @@ __global__ void __launch_bounds__(64 * S::kWaves, 2) ns_product_kernel(const NsG
             return;
         }
     }
-    store_results<MODE, FM, FN>(g, q, acc, ti * S::BM + wr * 32 * FM, tj * S::BN + wc * 32 * FN, ti == tj, now, reinterpret_cast<uint32_t*>(lds + wave * S::kTurn));
+    store_results<MODE, FM, FN>(g, q, acc, ti * S::BM + wr * 32 * FM, tj * S::BN + wc * 32 * FN, ti == tj, now, op, reinterpret_cast<uint32_t*>(lds + wave * S::kTurn));
 }
 
 // Adds up the parts of A's tiles, in their order: a wavefront takes one block of 32 x 32.
 template <typename S>
-__global__ void __launch_bounds__(256) ns_combine_kernel(const NsGroup* __restrict__ group, NsSizes sizes, int now, int splits) {
+__global__ void __launch_bounds__(256) ns_combine_kernel(const NsGroup* __restrict__ group, NsSizes sizes, int splits) {
     const NsGroup& g = *group;
     __shared__ __align__(16) uint32_t turn[4 * 32 * turn_pitch(1)];
     constexpr int kBlocks = S::kWaves * S::FM * S::FN;
@@ -680,7 +692,7 @@ __global__ void __launch_bounds__(256) ns_combine_kernel(const NsGroup* __restri
         acc[0][0][4 * v + 3] = t[v].w;
     }
     const int w = blk / (S::FM * S::FN), x = blk / S::FN % S::FM, y = blk % S::FN;
-    store_results<kGram, 1, 1>(g, q, acc, ti * S::BM + (w % S::WR * S::FM + x) * 32, tj * S::BN + (w / S::WR * S::FN + y) * 32, ti == tj, now, turn + wave * 32 * turn_pitch(1));
+    store_results<kGram, 1, 1>(g, q, acc, ti * S::BM + (w % S::WR * S::FM + x) * 32, tj * S::BN + (w / S::WR * S::FN + y) * 32, ti == tj, 0, NsOp{}, turn + wave * 32 * turn_pitch(1));
 }
 
 // ---------------------------------------------------------------- matrices with a side of at most 64
@@ -943,17 +955,20 @@ struct Task {
 };
 
 template <typename S>
-void launch_product(int mode, const NsGroup* g, const NsSizes& sizes, int now, unsigned tiles, int splits, hipStream_t st) {
+void launch_product(int mode, const NsGroup* g, const NsSizes& sizes, const NsOp& op, int now, unsigned tiles, int splits, hipStream_t st) {
     const dim3 grid(tiles * (unsigned)splits), block(64 * S::kWaves);
     switch (mode) {
         case kGram:
-            hipLaunchKernelGGL((ns_product_kernel<kGram, S>), grid, block, 0, st, g, sizes, now, splits);
+            hipLaunchKernelGGL((ns_product_kernel<kGram, S>), grid, block, 0, st, g, sizes, op, now, splits);
             if constexpr (S::BM <= 128)
-                if (splits > 1) hipLaunchKernelGGL((ns_combine_kernel<S>), dim3(tiles * (S::kWaves * S::FM * S::FN / 4)), dim3(256), 0, st, g, sizes, now, splits);
+                if (splits > 1) hipLaunchKernelGGL((ns_combine_kernel<S>), dim3(tiles * (S::kWaves * S::FM * S::FN / 4)), dim3(256), 0, st, g, sizes, splits);
             break;
-        case kPoly: hipLaunchKernelGGL((ns_product_kernel<kPoly, S>), grid, block, 0, st, g, sizes, now, 1); break;
-        case kStep: hipLaunchKernelGGL((ns_product_kernel<kStep, S>), grid, block, 0, st, g, sizes, now, 1); break;
-        default: hipLaunchKernelGGL((ns_product_kernel<kLast, S>), grid, block, 0, st, g, sizes, now, 1); break;
+        case kPoly: hipLaunchKernelGGL((ns_product_kernel<kPoly, S>), grid, block, 0, st, g, sizes, op, now, 1); break;
+        case kStep: hipLaunchKernelGGL((ns_product_kernel<kStep, S>), grid, block, 0, st, g, sizes, op, now, 1); break;
+        default:
+            // (the results' way into the tensors' tiles does not fit the registers of the large shape)
+            if constexpr (S::BM <= 128) hipLaunchKernelGGL((ns_product_kernel<kLast, S>), grid, block, 0, st, g, sizes, op, now, 1);
+            break;
     }
 }
 
@@ -961,7 +976,42 @@ void launch_product(int mode, const NsGroup* g, const NsSizes& sizes, int now, u
 struct Launch {
     int shape = 0, splits = 1;           // shape: 0 small, 1 middle, 2 large
     unsigned tiles = 0;
+    double time = 0.0;                   // of the model below, in microseconds
 };
+struct Item {
+    int mode;
+    NsOp op;
+    int now;
+};
+
+// The products of an iteration of `steps` steps.  Two steps can be taken at once: with A_1 = P_0 A_0 P_0, P = a I + b A + c A^2, the second one's polynomial comes
+// from square products alone, and X <- (P_1 P_0) X once: one product of X with itself and one with X (3 m^2 n flops) less for three square ones
+// (3 m^3) more.  A is recomputed from X after that, so what A_1 loses of the small singular values is not handed on.
+std::vector<Item> plan(const nnt_newton_schulz_cfg& c, bool pairs) {
+    const float A = (float)c.a, B = (float)c.b, C = (float)c.c;
+    std::vector<Item> out;
+    int now = 0;
+    for (int left = c.steps; left > 0;) {
+        const bool two = pairs && left >= 2;
+        out.push_back(Item{kGram, NsOp{}, now});
+        if (two) {
+            // (the multiples of the identity are kept out of the factors where they can be: rounded among their entries they would cost as much as the rest)
+            out.push_back(Item{kPoly, NsOp{0, 0, 0, 1, C, B, 0.f}, now});        // B_0 = P_0 - a I
+            out.push_back(Item{kPoly, NsOp{1, 0, 0, 2, 1.f, A, 0.f}, now});      // P_0 A_0
+            out.push_back(Item{kPoly, NsOp{1, 2, 2, 3, 1.f, A, 0.f}, now});      // A_1 = P_0 (P_0 A_0)
+            out.push_back(Item{kPoly, NsOp{3, 3, 3, 2, C, B, A}, now});          // P_1
+            out.push_back(Item{kPoly, NsOp{2, 1, 2, 0, 1.f, A, -A * A}, now});   // P_1 P_0 - a^2 I
+            left -= 2;
+            out.push_back(Item{left ? kStep : kLast, NsOp{0, 0, 0, 0, 1.f, A * A, 0.f}, now});
+        } else {
+            out.push_back(Item{kPoly, NsOp{0, 0, 0, 1, C, B, 0.f}, now});
+            left--;
+            out.push_back(Item{left ? kStep : kLast, NsOp{1, 0, 0, 0, 1.f, A, 0.f}, now});
+        }
+        now = 1 - now;
+    }
+    return out;
+}
 
 // The fastest launch of a product by a model of its time: a compute unit takes `lone` microseconds per panel of 16 columns for the only tile that it
 // holds, `full` for each of several, and a launch a fixed time besides.  (Measured; a tile of 64 x 64 alone is bound by the 32 bytes per clock that a
@@ -972,7 +1022,7 @@ Launch choose(const NsSizes& g, int mode) {
     const bool sym = mode == kGram || mode == kPoly;
     Launch best;
     double best_time = 0.0;
-    for (int s = 0; s < 3; s++) {
+    for (int s = 0; s < (mode == kLast ? 2 : 3); s++) {
         const int u = kShapes[s].blocks;
         int64_t tiles = 0, panels = 0, longest = 0;
         for (int k = 0; k < g.n; k++) {
@@ -989,14 +1039,14 @@ Launch choose(const NsSizes& g, int mode) {
             double time = per > 1.0 ? per * each * kShapes[s].full : (double)longest / splits * kShapes[s].lone;
             time += kShapes[s].fixed + (splits > 1 ? kCombine + 0.1 * splits : 0.0);
             if (best.tiles == 0 || time < best_time) {
-                best_time = time;
+                best_time = best.time = time;
                 best.shape = s;
                 best.splits = splits;
                 best.tiles = (unsigned)tiles;
             }
         }
     }
-    if (const char* e = getenv(mode == kGram ? "NS_G" : mode == kPoly ? "NS_P" : "NS_S")) {
+    if (const char* e = getenv(mode == kGram ? "NS_G" : mode == kPoly ? "NS_P" : mode == kStep ? "NS_S" : "NS_L")) {
         best.shape = atoi(e) % 10;
         best.splits = mode == kGram ? std::max(1, atoi(e) / 10) : 1;
         int64_t tiles = 0;
@@ -1047,12 +1097,11 @@ int32_t run_tasks(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& 
             chunks = std::max(chunks, (t.G->base[0] * t.G->base[1] + kNormChunk - 1) / kNormChunk * t.G->grid[0] * t.G->grid[1]);
             // (narrow ones: the transpose once, and A in parts)
             const int64_t x = narrow ? (int64_t)q.mp * q.np * 2 : (int64_t)q.mp * q.np * 4;
-            const int64_t a = narrow ? (int64_t)narrow_parts((int)nb) * 64 * 64 * 4 : (int64_t)q.mp * q.mp * 4;
+            const int64_t a = narrow ? (int64_t)narrow_parts((int)nb) * 64 * 64 * 2 : (int64_t)q.mp * q.mp * 4;
             q.X = bytes;
             q.XT = narrow ? bytes : q.X + 2 * x;
             q.A = q.XT + 2 * x;
-            q.B = q.A + a;
-            q.part = q.B + a;
+            q.part = q.A + 4 * a;
             bytes = q.part + kNormBlocks * 8;
             q.G = MatView{t.G->d_tiles, t.G->dtype};
             q.P = MatView{t.P->d_tiles, t.P->dtype};
@@ -1070,7 +1119,7 @@ int32_t run_tasks(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& 
         sizes.n = g.n;
         int parts = 0;
         for (int k = 0; k < g.n; k++) parts = std::max(parts, narrow_parts((int)(sizes.blocks[k] >> 16)));
-        const Launch gram = choose(sizes, kGram), poly = choose(sizes, kPoly), step = choose(sizes, kStep);
+        const Launch gram = choose(sizes, kGram), poly = choose(sizes, kPoly), step = choose(sizes, kStep), last = choose(sizes, kLast);
         g.partial = bytes;
         if (!narrow && gram.splits > 1) bytes += (int64_t)gram.tiles * gram.splits * (gram.shape == 0 ? Small::BM * Small::BM : Middle::BM * Middle::BM) * 4;
         const int32_t rc = ensure_matrix_scratch(ctx, bytes);
@@ -1078,6 +1127,9 @@ int32_t run_tasks(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& 
         g.space = reinterpret_cast<char*>(ctx->matrix_scratch);
         acc.push_back(Access{&ctx->matrix_dep, 1, kReadWrite});
         const int steps = cfg.steps;
+        bool pairs = 3.0 * poly.time < gram.time + step.time;
+        if (const char* e = getenv("NS_PAIRS")) pairs = atoi(e);
+        const std::vector<Item> items = narrow ? std::vector<Item>() : plan(cfg, pairs);
         OpTag tag(ctx, label, work, false);
         const NsGroup* there = reinterpret_cast<const NsGroup*>(g.space);
         const int32_t sc = submit(ctx, acc, [=](hipStream_t st) {
@@ -1090,16 +1142,14 @@ int32_t run_tasks(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& 
                 return launched();
             }
             hipLaunchKernelGGL(ns_split_kernel, dim3((unsigned)patch), dim3(256), 0, st, there, sizes);
-            for (int s = 0; s < steps; s++) {
-                for (int mode : {(int)kGram, (int)kPoly, s + 1 < steps ? (int)kStep : (int)kLast}) {
-                    const Launch& l = mode == kGram ? gram : mode == kPoly ? poly : step;
-                    if (l.shape == 2) launch_product<Large>(mode, there, sizes, s & 1, l.tiles, l.splits, st);
-                    else if (l.shape == 1) launch_product<Middle>(mode, there, sizes, s & 1, l.tiles, l.splits, st);
-                    else launch_product<Small>(mode, there, sizes, s & 1, l.tiles, l.splits, st);
-                }
+            for (const Item& t : items) {
+                const Launch& l = t.mode == kGram ? gram : t.mode == kPoly ? poly : t.mode == kStep ? step : last;
+                if (l.shape == 2) launch_product<Large>(t.mode, there, sizes, t.op, t.now, l.tiles, l.splits, st);
+                else if (l.shape == 1) launch_product<Middle>(t.mode, there, sizes, t.op, t.now, l.tiles, l.splits, st);
+                else launch_product<Small>(t.mode, there, sizes, t.op, t.now, l.tiles, l.splits, st);
             }
             return launched();
-        }, narrow ? 2 + steps : 2 + (gram.splits > 1 ? 4 : 3) * steps);
+        }, narrow ? 2 + steps : 2 + (int)items.size() + (gram.splits > 1 ? steps : 0));
         if (sc != NNT_OK) return sc;
     }
     return NNT_OK;
