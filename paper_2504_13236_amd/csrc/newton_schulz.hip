@@ -1014,10 +1014,10 @@ std::vector<Item> plan(const nnt_newton_schulz_cfg& c, bool pairs) {
 }
 
 // The fastest launch of a product by a model of its time: a compute unit takes `lone` microseconds per panel of 16 columns for the only tile that it
-// holds, `full` for each of several, and a launch a fixed time besides.  (Measured; a tile of 64 x 64 alone is bound by the 32 bytes per clock that a
+// holds, `full` for each of several, and a launch a fixed time besides and the time of its results' way to memory (5 TB/s).  (Measured; a tile of 64 x 64 alone is bound by the 32 bytes per clock that a
 // unit fetches, large ones by the clock that the power limit leaves.)  A product whose contraction is long and whose tiles are few is cut along the contraction.
 Launch choose(const NsSizes& g, int mode) {
-    static const struct { int blocks; double lone, full, fixed; } kShapes[3] = {{1, 0.107, 0.125, 2.6}, {2, 0.234, 0.339, 4.0}, {4, 0.8, 1.18, 7.0}};
+    static const struct { int blocks; double lone, full, fixed; } kShapes[3] = {{1, 0.107, 0.12, 2.6}, {2, 0.25, 0.339, 4.0}, {4, 0.8, 1.18, 7.0}};
     constexpr double kCombine = 4.0;
     const bool sym = mode == kGram || mode == kPoly;
     Launch best;
@@ -1025,19 +1025,21 @@ Launch choose(const NsSizes& g, int mode) {
     for (int s = 0; s < (mode == kLast ? 2 : 3); s++) {
         const int u = kShapes[s].blocks;
         int64_t tiles = 0, panels = 0, longest = 0;
+        double bytes = 0.0;                                                            // of the result path
         for (int k = 0; k < g.n; k++) {
             const int64_t mb = g.blocks[k] & 0xffffu, nb = g.blocks[k] >> 16, tm = (mb + u - 1) / u, tn = (nb + u - 1) / u;
             const int64_t t = sym ? tm * (tm + 1) / 2 : tm * tn, c = 4 * (mode == kGram ? nb : mb);
             tiles += t;
             panels += t * c;
             longest = std::max(longest, c);
+            bytes += 4096.0 * mb * (mode == kGram ? 4 * mb : mode == kPoly ? 6 * mb : mode == kStep ? 12 * nb : 16 * nb);
         }
         for (int splits = 1; splits <= 64; splits *= 2) {
             if (splits > 1 && (mode != kGram || s == 2 || tiles * splits > 512 || longest / splits < 8)) break;
             const double each = (double)panels / tiles / splits;                       // panels of a workgroup, on average
             const double per = std::ceil(tiles * splits / 256.0);
             double time = per > 1.0 ? per * each * kShapes[s].full : (double)longest / splits * kShapes[s].lone;
-            time += kShapes[s].fixed + (splits > 1 ? kCombine + 0.1 * splits : 0.0);
+            time += kShapes[s].fixed + bytes / 5e6 + (splits > 1 ? kCombine + 0.1 * splits : 0.0);
             if (best.tiles == 0 || time < best_time) {
                 best_time = best.time = time;
                 best.shape = s;
@@ -1046,18 +1048,6 @@ Launch choose(const NsSizes& g, int mode) {
             }
         }
     }
-    if (const char* e = getenv(mode == kGram ? "NS_G" : mode == kPoly ? "NS_P" : mode == kStep ? "NS_S" : "NS_L")) {
-        best.shape = atoi(e) % 10;
-        best.splits = mode == kGram ? std::max(1, atoi(e) / 10) : 1;
-        int64_t tiles = 0;
-        const int u = kShapes[best.shape].blocks;
-        for (int k = 0; k < g.n; k++) {
-            const int64_t mb = g.blocks[k] & 0xffffu, nb = g.blocks[k] >> 16, tm = (mb + u - 1) / u, tn = (nb + u - 1) / u;
-            tiles += sym ? tm * (tm + 1) / 2 : tm * tn;
-        }
-        best.tiles = tiles;
-    }
-    if (getenv("NS_PRINT")) fprintf(stderr, "mode %d shape %d splits %d tiles %u: %.1f us\n", mode, best.shape, best.splits, best.tiles, best_time);
     return best;
 }
 
@@ -1127,8 +1117,7 @@ int32_t run_tasks(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& 
         g.space = reinterpret_cast<char*>(ctx->matrix_scratch);
         acc.push_back(Access{&ctx->matrix_dep, 1, kReadWrite});
         const int steps = cfg.steps;
-        bool pairs = 3.0 * poly.time < gram.time + step.time;
-        if (const char* e = getenv("NS_PAIRS")) pairs = atoi(e);
+        const bool pairs = 1.15 * 3.0 * poly.time < gram.time + step.time;
         const std::vector<Item> items = narrow ? std::vector<Item>() : plan(cfg, pairs);
         OpTag tag(ctx, label, work, false);
         const NsGroup* there = reinterpret_cast<const NsGroup*>(g.space);
