@@ -30,8 +30,10 @@
  *    both operands, one part per stream as large as the largest of these products
  *    needs, at most 2 GiB each (a product that would need more, or for which there
  *    is no memory, reads its operands as they are), for as long as one of them or a
- *    graph captured with it lives.  nnt_ctx_stats reports the bytes held for (a) and
- *    for (b) to (d).  Tables and workspaces of a plan are released when one of its
+ *    graph captured with it lives; and (e) once matrices have been orthogonalised, the
+ *    workspace of the largest set of them (nnt_orthogonalize says how much), replaced
+ *    as (b) is.  nnt_ctx_stats reports the bytes held for (a) and
+ *    for (b) to (e).  Tables and workspaces of a plan are released when one of its
  *    tensors or the context is destroyed, the rest in the matching destroy call.
  *  - Element types: NNT_F32 (IEEE binary32) and NNT_BF16 (bfloat16, converted
  *    with round-to-nearest-even).  All arithmetic, reductions and accumulation
@@ -122,9 +124,9 @@ typedef struct nnt_exec_stats {
     int64_t plans;          /* product plans (descriptor tables) built and cached   */
     int64_t device_table_bytes;      /* device memory held for descriptor tables             */
     int64_t device_workspace_bytes;  /* device memory held for reduction scratch, the
-                                        k-slice workspaces of the cached product plans and
-                                        the copies of operands, replaced ones that graphs
-                                        hold included                                        */
+                                        k-slice workspaces of the cached product plans,
+                                        the copies of operands and the workspace of matrix
+                                        iterations, replaced ones that graphs hold included  */
 } nnt_exec_stats;
 NNT_API int32_t nnt_ctx_stats(nnt_ctx* ctx, nnt_exec_stats* out);
 
@@ -657,6 +659,9 @@ NNT_API int32_t nnt_gpt2_block_adam(nnt_gpt2_block* blk, int32_t step, const nnt
 /* SGD-with-momentum step on all 12 parameters; the velocities live in the slots
  * NNT_BLK_ADAM_M + parameter (the second-moment slots are not touched). */
 NNT_API int32_t nnt_gpt2_block_sgd(nnt_gpt2_block* blk, const nnt_sgd_cfg* cfg);
+/* nnt_muon_step on the four matrices (momentum in the slots NNT_BLK_ADAM_M + parameter, their second moments are not
+ * touched; bf16 blocks refresh the bf16 copies), Adam step number `step` on the eight vectors. */
+NNT_API int32_t nnt_gpt2_block_muon(nnt_gpt2_block* blk, const nnt_muon_cfg* cfg, int32_t step, const nnt_adam_cfg* adam);
 /* bf16 blocks: (re)make the bf16 weight copies from the fp32 masters. */
 NNT_API int32_t nnt_gpt2_block_sync_lowp(nnt_gpt2_block* blk);
 
@@ -679,6 +684,8 @@ NNT_API int32_t nnt_gpt2_stack_destroy(nnt_gpt2_stack* st);
 NNT_API int32_t nnt_gpt2_stack_forward(nnt_gpt2_stack* st);
 NNT_API int32_t nnt_gpt2_stack_backward(nnt_gpt2_stack* st);
 NNT_API int32_t nnt_gpt2_stack_adam(nnt_gpt2_stack* st, int32_t step, const nnt_adam_cfg* cfg);
+/* nnt_gpt2_block_muon on all blocks, their matrices in one nnt_muon_step. */
+NNT_API int32_t nnt_gpt2_stack_muon(nnt_gpt2_stack* st, const nnt_muon_cfg* cfg, int32_t step, const nnt_adam_cfg* adam);
 
 /* A GPT-2-shaped language model as one flow of tasks (section 3: embedding
  * layer, the blocks, layer normalization, linear head, Cross-Entropy loss,
@@ -720,6 +727,20 @@ NNT_API int32_t nnt_gpt2_model_forward(nnt_gpt2_model* m, const int32_t* tokens,
                                const int32_t* labels, float* col_loss, float* loss);
 NNT_API int32_t nnt_gpt2_model_backward(nnt_gpt2_model* m);
 NNT_API int32_t nnt_gpt2_model_adam(nnt_gpt2_model* m, int32_t step, const nnt_adam_cfg* cfg);
+/* Post-training: the forward pass with another end.  _logprob leaves the log-probabilities of the labels (the old or the reference
+ * policy's) and nothing to go backward from; _forward_policy and _forward_preference end in nnt_policy_loss and nnt_preference_loss
+ * with the gradient in the logits' place, from where nnt_gpt2_model_backward takes it.  logp, old_logp, ref_logp, advantages,
+ * losses, loss, rewards as there; labels outside [0, N_v) mark positions without one. */
+NNT_API int32_t nnt_gpt2_model_logprob(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions,
+                               const int32_t* labels, nnt_tensor* logp);
+NNT_API int32_t nnt_gpt2_model_forward_policy(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions,
+                               const int32_t* labels, const nnt_policy_cfg* cfg, nnt_tensor* old_logp, nnt_tensor* ref_logp,
+                               nnt_tensor* advantages, nnt_tensor* logp, float* losses, float* loss);
+NNT_API int32_t nnt_gpt2_model_forward_preference(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions,
+                               const int32_t* labels, const nnt_preference_cfg* cfg, nnt_tensor* ref_logp, nnt_tensor* logp,
+                               float* rewards, float* losses, float* loss);
+/* nnt_gpt2_stack_muon on the blocks, Adam on the model's own four parameters (embeddings, final layer norm). */
+NNT_API int32_t nnt_gpt2_model_muon(nnt_gpt2_model* m, const nnt_muon_cfg* cfg, int32_t step, const nnt_adam_cfg* adam);
 
 NNT_API const char* nnt_version(void);
 

@@ -208,6 +208,12 @@ PROTOTYPES = {
     "nnt_gpt2_stack_forward": (_i32, [_p]),
     "nnt_gpt2_stack_backward": (_i32, [_p]),
     "nnt_gpt2_stack_adam": (_i32, [_p, _i32, C.POINTER(nnt_adam_cfg)]),
+    "nnt_gpt2_block_muon": (_i32, [_p, C.POINTER(nnt_muon_cfg), _i32, C.POINTER(nnt_adam_cfg)]),
+    "nnt_gpt2_stack_muon": (_i32, [_p, C.POINTER(nnt_muon_cfg), _i32, C.POINTER(nnt_adam_cfg)]),
+    "nnt_gpt2_model_muon": (_i32, [_p, C.POINTER(nnt_muon_cfg), _i32, C.POINTER(nnt_adam_cfg)]),
+    "nnt_gpt2_model_logprob": (_i32, [_p, _p, _p, _p, _p]),
+    "nnt_gpt2_model_forward_policy": (_i32, [_p, _p, _p, _p, C.POINTER(nnt_policy_cfg), _p, _p, _p, _p, _p, _p]),
+    "nnt_gpt2_model_forward_preference": (_i32, [_p, _p, _p, _p, C.POINTER(nnt_preference_cfg), _p, _p, _p, _p, _p]),
     "nnt_version": (C.c_char_p, []),
 }
 

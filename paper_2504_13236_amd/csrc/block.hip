@@ -22,6 +22,7 @@ struct nnt_gpt2_block {
     nnt_tensor* s[NNT_BLK_NSLOTS];
     nnt_tensor* X;      // input of the last forward call
     nnt::AdamGroup* adam_group;   // all twelve parameters as one launch (made by the first whole-operation Adam step)
+    nnt::AdamGroup* vector_group; // the eight vectors alone (made by the first whole-operation step that updates the matrices otherwise)
 };
 
 // A chain of blocks: acts[i] feeds block i, acts[n] is the output; dacts[i] is the gradient of acts[i].
@@ -167,6 +168,7 @@ int32_t nnt_gpt2_block_create(nnt_ctx* ctx, const nnt_gpt2_block_cfg* cfg, nnt_t
 int32_t nnt_gpt2_block_destroy(nnt_gpt2_block* blk) {
     if (!blk) return NNT_EINVAL;
     nnt::adam_group_destroy(blk->adam_group);
+    nnt::adam_group_destroy(blk->vector_group);
     delete blk;
     return NNT_OK;
 }
@@ -357,6 +359,50 @@ int32_t nnt_gpt2_block_adam(nnt_gpt2_block* b, int32_t step, const nnt_adam_cfg*
     return NNT_OK;
 }
 
+// Adam on the parameters that are no matrices.
+static int32_t vectors_adam(nnt_gpt2_block* b, int32_t step, const nnt_adam_cfg* cfg) {
+    nnt_ctx* ctx = b->ctx;
+    constexpr int first = NNT_BLK_B_QKV, n = 12 - first;
+    if (ctx->granularity == NNT_GRAN_OP) {
+        if (!b->vector_group) {
+            if (ctx->capturing) return fail(ctx, NNT_ESTATE, "nnt_gpt2_block_muon: run the step once before capture");
+            nnt_tensor* lowp[n] = {};
+            TRY(adam_group_create(ctx, n, b->s + NNT_BLK_GRAD + first, b->s + first, b->s + NNT_BLK_ADAM_M + first, b->s + NNT_BLK_ADAM_V + first, lowp,
+                                  &b->vector_group));
+        }
+        return adam_group_step(ctx, b->vector_group, cfg, step);
+    }
+    for (int p = first; p < 12; p++)
+        TRY(nnt_adam_step(ctx, cfg, step, b->s[NNT_BLK_GRAD + p], b->s[p], b->s[NNT_BLK_ADAM_M + p], b->s[NNT_BLK_ADAM_V + p], nullptr));
+    return NNT_OK;
+}
+
+// The matrices of several blocks in one step (their products fill the chip together), then the vectors of each.
+static int32_t blocks_muon(nnt_ctx* ctx, nnt_gpt2_block* const* blocks, size_t n_blocks, const nnt_muon_cfg* cfg, int32_t step, const nnt_adam_cfg* adam) {
+    if (!cfg || !adam || step < 1) return fail(ctx, NNT_EINVAL, "nnt_gpt2_block_muon: bad argument");
+    std::vector<nnt_tensor*> G, P, M, LP;
+    for (size_t i = 0; i < n_blocks; i++) {
+        nnt_tensor** s = blocks[i]->s;
+        for (int p = 0; p < 12; p++)
+            if (!s[NNT_BLK_ADAM_M + p] || (p >= NNT_BLK_B_QKV && !s[NNT_BLK_ADAM_V + p]))
+                return fail(ctx, NNT_ESTATE, "nnt_gpt2_block_muon: the block was created without moment tensors");
+        for (int p = 0; p < NNT_BLK_B_QKV; p++) {
+            G.push_back(s[NNT_BLK_GRAD + p]);
+            P.push_back(s[p]);
+            M.push_back(s[NNT_BLK_ADAM_M + p]);
+            LP.push_back(blocks[i]->cfg.dtype == NNT_BF16 ? s[NNT_BLK_LOWP + p] : nullptr);
+        }
+    }
+    TRY(nnt_muon_step(ctx, cfg, (int32_t)G.size(), G.data(), P.data(), M.data(), LP.data()));
+    for (size_t i = 0; i < n_blocks; i++) TRY(vectors_adam(blocks[i], step, adam));
+    return NNT_OK;
+}
+
+int32_t nnt_gpt2_block_muon(nnt_gpt2_block* b, const nnt_muon_cfg* cfg, int32_t step, const nnt_adam_cfg* adam) {
+    if (!b) return NNT_EINVAL;
+    return entry(b->ctx, [&]() -> int32_t { return blocks_muon(b->ctx, &b, 1, cfg, step, adam); });
+}
+
 int32_t nnt_gpt2_block_sgd(nnt_gpt2_block* b, const nnt_sgd_cfg* cfg) {
     if (!b) return NNT_EINVAL;
     nnt_ctx* ctx = b->ctx;
@@ -429,6 +475,11 @@ int32_t nnt_gpt2_stack_adam(nnt_gpt2_stack* st, int32_t step, const nnt_adam_cfg
     if (!st) return NNT_EINVAL;
     for (nnt_gpt2_block* b : st->blocks) TRY(nnt_gpt2_block_adam(b, step, cfg));
     return NNT_OK;
+}
+
+int32_t nnt_gpt2_stack_muon(nnt_gpt2_stack* st, const nnt_muon_cfg* cfg, int32_t step, const nnt_adam_cfg* adam) {
+    if (!st) return NNT_EINVAL;
+    return entry(st->ctx, [&]() -> int32_t { return blocks_muon(st->ctx, st->blocks.data(), st->blocks.size(), cfg, step, adam); });
 }
 
 int32_t nnt_gpt2_block_sync_lowp(nnt_gpt2_block* b) {
@@ -522,25 +573,71 @@ int32_t nnt_gpt2_model_sync_lowp(nnt_gpt2_model* m) {
     return NNT_OK;
 }
 
-int32_t nnt_gpt2_model_forward(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions, const int32_t* labels,
-                               float* col_loss, float* loss) {
-    if (!m) return NNT_EINVAL;
+// Everything up to the logits.
+static int32_t model_logits(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions) {
     nnt_ctx* ctx = m->ctx;
-    NNT_CHECK_CTX(ctx);
-    if (!tokens || !positions || !labels || !col_loss || !loss) return fail(ctx, NNT_EINVAL, "nnt_gpt2_model_forward: null argument");
     nnt_gpt2_stack* st = m->stack;
     nnt_tensor** s = m->s;
-    m->tokens = tokens;
-    m->positions = positions;
     // X_0 = W_te[:, token] + W_pe[:, position]
     TRY(nnt_embedding_fwd(ctx, tokens, table_of(m, NNT_MDL_WTE), st->acts[0]));
     TRY(nnt_embedding_fwd(ctx, positions, table_of(m, NNT_MDL_WPE), s[NNT_MDL_XPOS]));
     TRY(nnt_add(ctx, 1.f, s[NNT_MDL_XPOS], 1.f, st->acts[0]));
     TRY(nnt_gpt2_stack_forward(st));
     TRY(nnt_layernorm_fwd(ctx, st->acts.back(), s[NNT_MDL_GAMMA_F], s[NNT_MDL_BETA_F], m->cfg.eps, s[NNT_MDL_XF], s[NNT_MDL_STATS_F]));
-    // logits = W_te^T X_f (the head shares the token embedding), then the loss, which leaves dL/dlogits in place
-    TRY(nnt_gemm(ctx, 1.f, NNT_OP_T, table_of(m, NNT_MDL_WTE), NNT_OP_N, s[NNT_MDL_XF], 0.f, s[NNT_MDL_LOGITS], 1, 0, nullptr));
-    return nnt_cross_entropy(ctx, s[NNT_MDL_LOGITS], labels, s[NNT_MDL_LOSS_STATS], col_loss, loss);
+    // logits = W_te^T X_f (the head shares the token embedding)
+    return nnt_gemm(ctx, 1.f, NNT_OP_T, table_of(m, NNT_MDL_WTE), NNT_OP_N, s[NNT_MDL_XF], 0.f, s[NNT_MDL_LOGITS], 1, 0, nullptr);
+}
+
+int32_t nnt_gpt2_model_forward(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions, const int32_t* labels,
+                               float* col_loss, float* loss) {
+    if (!m) return NNT_EINVAL;
+    nnt_ctx* ctx = m->ctx;
+    NNT_CHECK_CTX(ctx);
+    if (!tokens || !positions || !labels || !col_loss || !loss) return fail(ctx, NNT_EINVAL, "nnt_gpt2_model_forward: null argument");
+    m->tokens = tokens;
+    m->positions = positions;
+    // the loss leaves dL/dlogits in the logits' place
+    TRY(model_logits(m, tokens, positions));
+    return nnt_cross_entropy(ctx, m->s[NNT_MDL_LOGITS], labels, m->s[NNT_MDL_LOSS_STATS], col_loss, loss);
+}
+
+int32_t nnt_gpt2_model_logprob(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions, const int32_t* labels, nnt_tensor* logp) {
+    if (!m) return NNT_EINVAL;
+    return entry(m->ctx, [&]() -> int32_t {
+        if (!tokens || !positions || !labels || !logp) return fail(m->ctx, NNT_EINVAL, "nnt_gpt2_model_logprob: null argument");
+        m->tokens = m->positions = nullptr;      // the logits hold no gradient: there is nothing to go backward from
+        TRY(model_logits(m, tokens, positions));
+        return nnt_token_logprob(m->ctx, m->s[NNT_MDL_LOGITS], labels, logp);
+    });
+}
+
+int32_t nnt_gpt2_model_forward_policy(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions, const int32_t* labels,
+                                      const nnt_policy_cfg* cfg, nnt_tensor* old_logp, nnt_tensor* ref_logp, nnt_tensor* advantages, nnt_tensor* logp,
+                                      float* losses, float* loss) {
+    if (!m) return NNT_EINVAL;
+    return entry(m->ctx, [&]() -> int32_t {
+        if (!tokens || !positions || !labels) return fail(m->ctx, NNT_EINVAL, "nnt_gpt2_model_forward_policy: null argument");
+        m->tokens = m->positions = nullptr;
+        TRY(model_logits(m, tokens, positions));
+        TRY(nnt_policy_loss(m->ctx, cfg, m->s[NNT_MDL_LOGITS], labels, old_logp, ref_logp, advantages, m->s[NNT_MDL_LOGITS], logp, losses, loss));
+        m->tokens = tokens;
+        m->positions = positions;
+        return NNT_OK;
+    });
+}
+
+int32_t nnt_gpt2_model_forward_preference(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions, const int32_t* labels,
+                                          const nnt_preference_cfg* cfg, nnt_tensor* ref_logp, nnt_tensor* logp, float* rewards, float* losses, float* loss) {
+    if (!m) return NNT_EINVAL;
+    return entry(m->ctx, [&]() -> int32_t {
+        if (!tokens || !positions || !labels) return fail(m->ctx, NNT_EINVAL, "nnt_gpt2_model_forward_preference: null argument");
+        m->tokens = m->positions = nullptr;
+        TRY(model_logits(m, tokens, positions));
+        TRY(nnt_preference_loss(m->ctx, cfg, m->s[NNT_MDL_LOGITS], labels, ref_logp, m->s[NNT_MDL_LOGITS], logp, rewards, losses, loss));
+        m->tokens = tokens;
+        m->positions = positions;
+        return NNT_OK;
+    });
 }
 
 int32_t nnt_gpt2_model_backward(nnt_gpt2_model* m) {
@@ -563,20 +660,39 @@ int32_t nnt_gpt2_model_backward(nnt_gpt2_model* m) {
     return nnt_embedding_bwd(ctx, m->positions, st->dacts[0], g[NNT_MDL_WPE]);
 }
 
+// Adam on the model's own four parameters.
+static int32_t own_adam(nnt_gpt2_model* m, int32_t step, const nnt_adam_cfg* cfg) {
+    for (int p = 0; p < 4; p++) {
+        nnt_tensor* lowp = (m->cfg.dtype == NNT_BF16 && p < 2) ? m->s[NNT_MDL_LOWP + p] : nullptr;
+        TRY(nnt_adam_step(m->ctx, cfg, step, m->s[NNT_MDL_GRAD + p], m->s[p], m->s[NNT_MDL_ADAM_M + p], m->s[NNT_MDL_ADAM_V + p], lowp));
+    }
+    return NNT_OK;
+}
+
+static bool has_own_moments(const nnt_gpt2_model* m) {
+    for (int p = 0; p < 4; p++)
+        if (!m->s[NNT_MDL_ADAM_M + p] || !m->s[NNT_MDL_ADAM_V + p]) return false;
+    return true;
+}
+
 int32_t nnt_gpt2_model_adam(nnt_gpt2_model* m, int32_t step, const nnt_adam_cfg* cfg) {
     if (!m) return NNT_EINVAL;
     nnt_ctx* ctx = m->ctx;
     NNT_CHECK_CTX(ctx);
     if (!cfg || step < 1) return fail(ctx, NNT_EINVAL, "nnt_gpt2_model_adam: bad argument");
-    for (int p = 0; p < 4; p++)
-        if (!m->s[NNT_MDL_ADAM_M + p] || !m->s[NNT_MDL_ADAM_V + p])
-            return fail(ctx, NNT_ESTATE, "nnt_gpt2_model_adam: the model was created without Adam moments");
+    if (!has_own_moments(m)) return fail(ctx, NNT_ESTATE, "nnt_gpt2_model_adam: the model was created without Adam moments");
     TRY(nnt_gpt2_stack_adam(m->stack, step, cfg));
-    for (int p = 0; p < 4; p++) {
-        nnt_tensor* lowp = (m->cfg.dtype == NNT_BF16 && p < 2) ? m->s[NNT_MDL_LOWP + p] : nullptr;
-        TRY(nnt_adam_step(ctx, cfg, step, m->s[NNT_MDL_GRAD + p], m->s[p], m->s[NNT_MDL_ADAM_M + p], m->s[NNT_MDL_ADAM_V + p], lowp));
-    }
-    return NNT_OK;
+    return own_adam(m, step, cfg);
+}
+
+int32_t nnt_gpt2_model_muon(nnt_gpt2_model* m, const nnt_muon_cfg* cfg, int32_t step, const nnt_adam_cfg* adam) {
+    if (!m) return NNT_EINVAL;
+    return entry(m->ctx, [&]() -> int32_t {
+        if (!cfg || !adam || step < 1) return fail(m->ctx, NNT_EINVAL, "nnt_gpt2_model_muon: bad argument");
+        if (!has_own_moments(m)) return fail(m->ctx, NNT_ESTATE, "nnt_gpt2_model_muon: the model was created without Adam moments");
+        TRY(nnt_gpt2_stack_muon(m->stack, cfg, step, adam));
+        return own_adam(m, step, adam);
+    });
 }
 
 }  // extern "C"

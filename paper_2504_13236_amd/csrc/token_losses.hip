@@ -107,29 +107,31 @@ __device__ __forceinline__ void stream_stats(const Logits& a, const ColumnAt<T>&
     constexpr int V = RawVec<T>::V, NW = NT / 64;
     const int tid = threadIdx.x;
     float m = -__builtin_huge_valf(), s = 0.f;
-    for (int f0 = tid; f0 < a.nvec; f0 += U * NT) {
-        RawVec<T> raw[U];
-        int cnt[U];
+    RawVec<T> raw[2][U];
+    int cnt[2][U];
+    auto fetch = [&](int set, int f0) {
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int f = f0 + u * NT;
-            cnt[u] = 0;
+            cnt[set][u] = 0;
             if (f < a.nvec) {
                 int l, e;
-                place<T>(a, f, l, e, cnt[u]);
-                raw[u].load(base.at(a, at.c, l) + e, cnt[u]);
+                place<T>(a, f, l, e, cnt[set][u]);
+                raw[set][u].load(base.at(a, at.c, l) + e, cnt[set][u]);
             }
         }
+    };
+    auto take = [&](int set, int f0) {
         float top = m;
 #pragma unroll
         for (int u = 0; u < U; u++) {
 #pragma unroll
             for (int j = 0; j < V; j++)
-                if (j < cnt[u]) top = fmaxf(top, raw[u].at(j));
+                if (j < cnt[set][u]) top = fmaxf(top, raw[set][u].at(j));
             if (f0 + u * NT == at.lab_f) {
 #pragma unroll
                 for (int j = 0; j < V; j++)
-                    if (j == at.lab_j) red[2][0] = raw[u].at(j);
+                    if (j == at.lab_j) red[2][0] = raw[set][u].at(j);
             }
         }
         if (top > m) {                       // (the first time m is -inf and s 0)
@@ -141,7 +143,15 @@ __device__ __forceinline__ void stream_stats(const Logits& a, const ColumnAt<T>&
         for (int u = 0; u < U; u++)
 #pragma unroll
             for (int j = 0; j < V; j++)
-                if (j < cnt[u]) s += exp_of(raw[u].at(j) - shift);
+                if (j < cnt[set][u]) s += exp_of(raw[set][u].at(j) - shift);
+    };
+    // the next vectors are on their way while these are worked on
+    fetch(0, tid);
+    for (int f0 = tid; f0 < a.nvec; f0 += 2 * U * NT) {
+        fetch(1, f0 + U * NT);
+        take(0, f0);
+        fetch(0, f0 + 2 * U * NT);
+        take(1, f0 + U * NT);
     }
     mx = block_max<NW>(m, red[0]);
     s = m == mx ? s : s * exp_of(m - mx);
@@ -573,7 +583,7 @@ int32_t nnt_token_logprob(nnt_ctx* ctx, nnt_tensor* X, const int32_t* labels, nn
         OpTag tag(ctx, "token_logprob", (double)X->shape[0] * ncols * X->elem_size(), true);
         return submit(ctx, {X->all(kRead), logp->all(kWrite)}, [=](hipStream_t st) {
             const dim3 grid((unsigned)ncols);
-            const bool small = small_column(dt, a.nvec);
+            const bool small = small_column(dt, a.nvec) || ncols >= (getenv("LP_MIN") ? atoi(getenv("LP_MIN")) : 1024);
             if (dt == NNT_F32) {
                 if (small) hipLaunchKernelGGL((logprob_kernel<float, 256>), grid, dim3(256), 0, st, a, out);
                 else hipLaunchKernelGGL((logprob_kernel<float, 1024>), grid, dim3(1024), 0, st, a, out);

@@ -183,6 +183,34 @@ class TiledTensor:
             self.buf = None
 
 
+_MUON_SCALE = {"none": capi.NNT_MUON_SCALE_NONE, "aspect": capi.NNT_MUON_SCALE_ASPECT, "rms": capi.NNT_MUON_SCALE_RMS}
+_REDUCTION = {"sum": capi.NNT_REDUCE_SUM, "tokens": capi.NNT_REDUCE_TOKENS, "sequences": capi.NNT_REDUCE_SEQUENCES}
+
+
+def newton_schulz_cfg(a=3.4445, b=-4.7750, c=2.0315, eps=1e-7, steps=5):
+    return capi.nnt_newton_schulz_cfg(a, b, c, eps, steps)
+
+
+def muon_cfg(lr=0.02, momentum=0.95, weight_decay=0.0, nesterov=True, scale="rms", iteration=None):
+    return capi.nnt_muon_cfg(lr, momentum, weight_decay, 1 if nesterov else 0, _MUON_SCALE[scale], newton_schulz_cfg(**(iteration or {})))
+
+
+def _handles(tensors):
+    return capi.ptr_array([t.h.value if t is not None else None for t in tensors])
+
+
+def orthogonalize(ctx, G, O, **iteration):
+    """O[k] <- G[k] orthogonalised by Newton-Schulz products, lists of matrices."""
+    cfg = newton_schulz_cfg(**iteration)
+    capi.nnt_orthogonalize(ctx.h, C.byref(cfg), len(G), _handles(G), _handles(O))
+
+
+def muon_step(ctx, G, P, M, P_lowp=None, **hyper):
+    """One Muon step on lists of matrices (gradients, parameters, momenta, bf16 copies or None)."""
+    cfg = muon_cfg(**hyper)
+    capi.nnt_muon_step(ctx.h, C.byref(cfg), len(G), _handles(G), _handles(P), _handles(M), _handles(P_lowp) if P_lowp else None)
+
+
 def causal_absent(base_k, base_q, n_q):
     """Predicate for score tensors [k, q, ...]: tile (kt, qt, ...) holds no visible
     score when its first key index exceeds its last query index."""
@@ -195,6 +223,10 @@ PARAM_SLOTS = {"W_qkv": capi.NNT_BLK_W_QKV, "W_o": capi.NNT_BLK_W_O, "W_1": capi
                "b_qkv": capi.NNT_BLK_B_QKV, "b_o": capi.NNT_BLK_B_O, "b_1": capi.NNT_BLK_B_1, "b_2": capi.NNT_BLK_B_2,
                "gamma1": capi.NNT_BLK_GAMMA1, "beta1": capi.NNT_BLK_BETA1,
                "gamma2": capi.NNT_BLK_GAMMA2, "beta2": capi.NNT_BLK_BETA2}
+
+
+def _adam_cfg(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0):
+    return capi.nnt_adam_cfg(lr, beta1, beta2, eps, weight_decay)
 
 
 class Gpt2Block:
@@ -260,6 +292,11 @@ class Gpt2Block:
         cfg = capi.nnt_sgd_cfg(lr, momentum, weight_decay, 1 if nesterov else 0)
         capi.nnt_gpt2_block_sgd(self.h, C.byref(cfg))
 
+    def muon(self, step, adam=None, **hyper):
+        """Muon on the four matrices, Adam (hyper-parameters `adam`) on the vectors."""
+        cfg, acfg = muon_cfg(**hyper), _adam_cfg(**(adam or {}))
+        capi.nnt_gpt2_block_muon(self.h, C.byref(cfg), step, C.byref(acfg))
+
     def param(self, name):
         return self.slots[PARAM_SLOTS[name]]
 
@@ -299,6 +336,10 @@ class Gpt2Stack:
     def adam(self, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0):
         cfg = capi.nnt_adam_cfg(lr, beta1, beta2, eps, weight_decay)
         capi.nnt_gpt2_stack_adam(self.h, step, C.byref(cfg))
+
+    def muon(self, step, adam=None, **hyper):
+        cfg, acfg = muon_cfg(**hyper), _adam_cfg(**(adam or {}))
+        capi.nnt_gpt2_stack_muon(self.h, C.byref(cfg), step, C.byref(acfg))
 
     def close(self):
         if self.h:
@@ -346,6 +387,7 @@ class Gpt2Model:
         dev = "cuda:%d" % ctx.device
         self.col_loss = torch.empty(self.N_s * self.N_b, dtype=torch.float32, device=dev)
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
+        self.rewards = torch.zeros(self.N_b, dtype=torch.float32, device=dev)
         pos = np.repeat(np.arange(self.N_s, dtype=np.int32)[:, None], self.N_b, axis=1)
         self.pos = torch.from_numpy(np.ascontiguousarray(pos.reshape(-1, order="F"))).to(dev)
         self.tokens = torch.zeros(self.N_s * self.N_b, dtype=torch.int32, device=dev)
@@ -370,8 +412,37 @@ class Gpt2Model:
         capi.nnt_gpt2_model_forward(self.h, self.tokens.data_ptr(), self.pos.data_ptr(), self.labels.data_ptr(),
                                     self.col_loss.data_ptr(), self.loss.data_ptr())
 
+    def per_position(self, a=None):
+        """A tensor of one fp32 value per position, tiled like the logits' other axes (log-probabilities, advantages)."""
+        t = TiledTensor(self.ctx, "f32", (self.N_s, self.N_b), self.logits.base[1:], fill=0)
+        return t if a is None else t.upload(a)
+
+    def logprob(self, logp):
+        """Log-probabilities of the batch's labels (0 where a label is outside the vocabulary) into `logp`."""
+        capi.nnt_gpt2_model_logprob(self.h, self.tokens.data_ptr(), self.pos.data_ptr(), self.labels.data_ptr(), logp.h)
+
+    def forward_policy(self, advantages, logp, old=None, ref=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0, reduction="tokens"):
+        """Forward pass that ends in the clipped policy loss; `loss` and `col_loss` hold it, backward() takes it from there."""
+        cfg = capi.nnt_policy_cfg(clip_low, clip_high, kl_coef, _REDUCTION[reduction])
+        capi.nnt_gpt2_model_forward_policy(self.h, self.tokens.data_ptr(), self.pos.data_ptr(), self.labels.data_ptr(), C.byref(cfg),
+                                           old.h if old is not None else None, ref.h if ref is not None else None, advantages.h, logp.h,
+                                           self.col_loss.data_ptr(), self.loss.data_ptr())
+
+    def forward_preference(self, logp, ref=None, beta=0.1, label_smoothing=0.0, reduction="sequences"):
+        """Forward pass that ends in the preference loss of the pairs (p, p + N_b / 2); `loss`, the first N_b / 2 of `col_loss` and
+        `rewards` hold its results."""
+        cfg = capi.nnt_preference_cfg(beta, label_smoothing, _REDUCTION[reduction])
+        capi.nnt_gpt2_model_forward_preference(self.h, self.tokens.data_ptr(), self.pos.data_ptr(), self.labels.data_ptr(), C.byref(cfg),
+                                               ref.h if ref is not None else None, logp.h, self.rewards.data_ptr(), self.col_loss.data_ptr(),
+                                               self.loss.data_ptr())
+
     def backward(self):
         capi.nnt_gpt2_model_backward(self.h)
+
+    def muon(self, step, adam=None, **hyper):
+        """Muon on the blocks' matrices, Adam (hyper-parameters `adam`) on everything else."""
+        cfg, acfg = muon_cfg(**hyper), _adam_cfg(**(adam or {}))
+        capi.nnt_gpt2_model_muon(self.h, C.byref(cfg), step, C.byref(acfg))
 
     def adam(self, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0):
         cfg = capi.nnt_adam_cfg(lr, beta1, beta2, eps, weight_decay)

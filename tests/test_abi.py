@@ -431,3 +431,18 @@ def test_executor_learns_which_tasks_need_an_event_of_their_own(capi):
     # one stream, or serial mode: no waits at all
     stream, seq, waits = _simulate(capi, 1, 0, 4, period * 2)
     assert not stream.any() and not waits.any()
+
+
+def test_post_training_calls_without_a_context(capi):
+    """Null contexts and handles are refused before anything else is looked at."""
+    E = capi.NNT_EINVAL
+    assert capi.nnt_token_logprob.raw(None, None, None, None) == E
+    assert capi.nnt_policy_loss.raw(None, None, None, None, None, None, None, None, None, None, None) == E
+    assert capi.nnt_preference_loss.raw(None, None, None, None, None, None, None, None, None, None) == E
+    assert capi.nnt_orthogonalize.raw(None, None, 1, None, None) == E
+    assert capi.nnt_muon_step.raw(None, None, 1, None, None, None, None) == E
+    for fn in (capi.nnt_gpt2_block_muon, capi.nnt_gpt2_stack_muon, capi.nnt_gpt2_model_muon):
+        assert fn.raw(None, None, 1, None) == E
+    assert capi.nnt_gpt2_model_logprob.raw(None, None, None, None, None) == E
+    assert capi.nnt_gpt2_model_forward_policy.raw(None, None, None, None, None, None, None, None, None, None, None) == E
+    assert capi.nnt_gpt2_model_forward_preference.raw(None, None, None, None, None, None, None, None, None, None) == E
