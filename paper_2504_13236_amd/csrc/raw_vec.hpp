@@ -20,6 +20,19 @@ template <> struct RawVec<float> {
             for (int j = 0; j < V; j++) x[j] = j < cnt ? p[j] : 0.f;
         }
     }
+    // the same with -inf in the place of what is not there
+    __device__ __forceinline__ void load_or_none(const float* p, int cnt) {
+        if (cnt >= V) {
+            x = *reinterpret_cast<const vec*>(p);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; j++) x[j] = j < cnt ? p[j] : -__builtin_huge_valf();
+        }
+    }
+    __device__ __forceinline__ void none() {
+#pragma unroll
+        for (int j = 0; j < V; j++) x[j] = -__builtin_huge_valf();
+    }
     static constexpr bool kKeeps = true;          // holds fp32 values: the shifted exponentials can take the logits' place
     __device__ __forceinline__ float at(int j) const { return x[j]; }
     __device__ __forceinline__ void set(int j, float f) { x[j] = f; }
@@ -47,6 +60,17 @@ template <> struct RawVec<bf16_t> {
                 if (j < cnt) x[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
         }
     }
+    __device__ __forceinline__ void load_or_none(const bf16_t* p, int cnt) {
+        if (cnt >= V) {
+            x = *reinterpret_cast<const vec*>(p);
+        } else {
+            none();
+#pragma unroll
+            for (int j = 0; j < V; j++)
+                if (j < cnt) x[j >> 1] = (j & 1) ? (x[j >> 1] & 0xffffu) | ((uint32_t)p[j] << 16) : (x[j >> 1] & 0xffff0000u) | (uint32_t)p[j];
+        }
+    }
+    __device__ __forceinline__ void none() { x = vec{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }
     static constexpr bool kKeeps = false;
     __device__ __forceinline__ void set(int, float) {}
     __device__ __forceinline__ float at(int j) const { return __uint_as_float((j & 1) ? (x[j >> 1] & 0xffff0000u) : (x[j >> 1] << 16)); }

@@ -107,17 +107,18 @@ __device__ __forceinline__ void stream_stats(const Logits& a, const ColumnAt<T>&
     constexpr int V = RawVec<T>::V, NW = NT / 64;
     const int tid = threadIdx.x;
     float m = -__builtin_huge_valf(), s = 0.f;
+    // (what is not there counts as -inf: its exponential is 0, and no element needs a test)
     RawVec<T> raw[2][U];
-    int cnt[2][U];
     auto fetch = [&](int set, int f0) {
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int f = f0 + u * NT;
-            cnt[set][u] = 0;
             if (f < a.nvec) {
-                int l, e;
-                place<T>(a, f, l, e, cnt[set][u]);
-                raw[set][u].load(base.at(a, at.c, l) + e, cnt[set][u]);
+                int l, e, cnt;
+                place<T>(a, f, l, e, cnt);
+                raw[set][u].load_or_none(base.at(a, at.c, l) + e, cnt);
+            } else {
+                raw[set][u].none();
             }
         }
     };
@@ -126,8 +127,7 @@ __device__ __forceinline__ void stream_stats(const Logits& a, const ColumnAt<T>&
 #pragma unroll
         for (int u = 0; u < U; u++) {
 #pragma unroll
-            for (int j = 0; j < V; j++)
-                if (j < cnt[set][u]) top = fmaxf(top, raw[set][u].at(j));
+            for (int j = 0; j < V; j++) top = fmaxf(top, raw[set][u].at(j));
             if (f0 + u * NT == at.lab_f) {
 #pragma unroll
                 for (int j = 0; j < V; j++)
@@ -142,8 +142,7 @@ __device__ __forceinline__ void stream_stats(const Logits& a, const ColumnAt<T>&
 #pragma unroll
         for (int u = 0; u < U; u++)
 #pragma unroll
-            for (int j = 0; j < V; j++)
-                if (j < cnt[set][u]) s += exp_of(raw[set][u].at(j) - shift);
+            for (int j = 0; j < V; j++) s += exp_of(raw[set][u].at(j) - shift);
     };
     // the next vectors are on their way while these are worked on
     fetch(0, tid);
@@ -226,8 +225,11 @@ __device__ __forceinline__ void policy_of(const Logits& a, const PolicyArgs& p, 
 // One workgroup takes one column.  SLOTS > 0: the column is read once into registers, SLOTS vectors per thread, and the gradient leaves from
 // there.  SLOTS = 0: a column too long for that is read twice.
 template <typename T, int SLOTS, int NT>
-__global__ void __launch_bounds__(NT, (sizeof(T) == 2 && NT == 1024) ? 8 : 1) policy_kernel(Logits a, PolicyArgs p) {
+__global__ void __launch_bounds__(NT, (sizeof(T) == 2 && NT == 1024 && SLOTS > 0) ? 8 : 1) policy_kernel(Logits a, PolicyArgs p) {
     constexpr int V = RawVec<T>::V, NW = NT / 64;
+    // Vectors that are not there count as -inf, which needs no test; with 64 registers for two workgroups of 1024 per unit the test per vector is what keeps
+    // the compiler from unpacking them all at once (6 vectors of bf16: 39 registers spilled, 462 instead of 291 us for 8192 columns of 50304).
+    constexpr bool kTests = sizeof(T) == 2 && NT == 1024;
     __shared__ uint64_t table[2][kTableTiles];
     __shared__ float red[3][NW];
     __shared__ float g_s;
@@ -261,40 +263,34 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 && NT == 1024) ? 8 : 1) po
             if (f < a.nvec) {
                 int l, e, cnt;
                 place<T>(a, f, l, e, cnt);
-                raw[it].load(base.at(a, at.c, l) + e, cnt);
+                raw[it].load_or_none(base.at(a, at.c, l) + e, cnt);
+            } else if (!kTests) {
+                raw[it].none();
             }
         }
         mx = -__builtin_huge_valf();
 #pragma unroll
         for (int it = 0; it < SLOTS; it++) {
             const int f = it * NT + tid;
-            if (f < a.nvec) {
-                int l, e, cnt;
-                place<T>(a, f, l, e, cnt);
+            if (kTests && f >= a.nvec) continue;
+#pragma unroll
+            for (int j = 0; j < V; j++) mx = fmaxf(mx, raw[it].at(j));
+            if (f == at.lab_f) {
 #pragma unroll
                 for (int j = 0; j < V; j++)
-                    if (j < cnt) mx = fmaxf(mx, raw[it].at(j));
-                if (f == at.lab_f) {
-#pragma unroll
-                    for (int j = 0; j < V; j++)
-                        if (j == at.lab_j) red[2][0] = raw[it].at(j);
-                }
+                    if (j == at.lab_j) red[2][0] = raw[it].at(j);
             }
         }
         mx = block_max<NW>(mx, red[0]);
         sum = 0.f;
 #pragma unroll
         for (int it = 0; it < SLOTS; it++) {
-            const int f = it * NT + tid;
-            if (f < a.nvec) {
-                int l, e, cnt;
-                place<T>(a, f, l, e, cnt);
+            if (kTests && it * NT + tid >= a.nvec) continue;
 #pragma unroll
-                for (int j = 0; j < V; j++) {
-                    const float x = exp_of(raw[it].at(j) - mx);
-                    if (RawVec<T>::kKeeps) raw[it].set(j, x);
-                    if (j < cnt) sum += x;
-                }
+            for (int j = 0; j < V; j++) {
+                const float x = exp_of(raw[it].at(j) - mx);
+                if (RawVec<T>::kKeeps) raw[it].set(j, x);
+                sum += x;
             }
         }
         sum = block_sum<NW>(sum, red[1]);
@@ -506,21 +502,45 @@ __global__ void __launch_bounds__(NT) preference_gradient_kernel(Logits a, Prefe
 }
 
 // ---------------------------------------------------------------- host side
-// Workgroup size of a column: 256 threads where its vectors fit their registers, 1024 for longer ones.
-bool small_column(int dtype, int64_t nvec) { return nvec <= (dtype == NNT_F32 ? 4096 : 2048); }
+// Workgroup size of a column.  One wavefront where there are many short columns: what a column costs besides its logits counts then, and 32 of them share
+// a compute unit (log-probabilities of 16384 columns of 2000 in bf16 64 -> 22 us, of 8192 of 6513 35 -> 22).  256 threads where a column's vectors fit their
+// registers, or where there are so many that several of them share a unit anyway (8192 columns of 50304 in bf16 192 -> 123 us); 1024 for few long ones
+// (64 columns of 50304 10 us, 14 with 256).  `streams`: the kernel does not hold the column in registers.
+int threads_of(int dtype, int64_t nvec, int64_t ncols, bool streams) {
+    if (ncols >= 512 && nvec <= (streams || dtype == NNT_F32 ? 1024 : 512)) return 64;
+    if (nvec <= (dtype == NNT_F32 ? 4096 : 2048) || (streams && ncols >= 1024)) return 256;
+    return 1024;
+}
 
 using PolicyFn = void (*)(Logits, PolicyArgs);
 // the instance that holds a column of `nvec` vectors with the fewest registers, and its workgroup size
-PolicyFn policy_of(int dtype, int64_t nvec, int* nt) {
-    *nt = small_column(dtype, nvec) ? 256 : 1024;
+PolicyFn policy_of(int dtype, int64_t nvec, int64_t ncols, int* nt) {
+    *nt = threads_of(dtype, nvec, ncols, false);
     const int64_t per = (nvec + *nt - 1) / *nt;
     if (dtype == NNT_F32) {
+        if (*nt == 64) return per <= 4 ? policy_kernel<float, 4, 64> : policy_kernel<float, 16, 64>;
         if (*nt == 256) return per <= 4 ? policy_kernel<float, 4, 256> : policy_kernel<float, 16, 256>;
         return per <= 8 ? policy_kernel<float, 8, 1024> : per <= 13 ? policy_kernel<float, 13, 1024> : per <= 16 ? policy_kernel<float, 16, 1024> : policy_kernel<float, 0, 1024>;
     }
+    if (*nt == 64) return per <= 2 ? policy_kernel<bf16_t, 2, 64> : policy_kernel<bf16_t, 8, 64>;
     if (*nt == 256) return per <= 2 ? policy_kernel<bf16_t, 2, 256> : policy_kernel<bf16_t, 8, 256>;
     return per <= 4 ? policy_kernel<bf16_t, 4, 1024> : per <= 7 ? policy_kernel<bf16_t, 7, 1024> : per <= 8 ? policy_kernel<bf16_t, 8, 1024> : policy_kernel<bf16_t, 0, 1024>;
 }
+
+#define NNT_PER_COLUMN(KERNEL, NT, ...)                                                                                      \
+    do {                                                                                                                     \
+        const dim3 grid((unsigned)ncols);                                                                                    \
+        if (dt == NNT_F32) {                                                                                                 \
+            if ((NT) == 64) hipLaunchKernelGGL((KERNEL<float, 64>), grid, dim3(64), 0, st, __VA_ARGS__);                     \
+            else if ((NT) == 256) hipLaunchKernelGGL((KERNEL<float, 256>), grid, dim3(256), 0, st, __VA_ARGS__);             \
+            else hipLaunchKernelGGL((KERNEL<float, 1024>), grid, dim3(1024), 0, st, __VA_ARGS__);                            \
+        } else {                                                                                                             \
+            if ((NT) == 64) hipLaunchKernelGGL((KERNEL<bf16_t, 64>), grid, dim3(64), 0, st, __VA_ARGS__);                    \
+            else if ((NT) == 256) hipLaunchKernelGGL((KERNEL<bf16_t, 256>), grid, dim3(256), 0, st, __VA_ARGS__);            \
+            else hipLaunchKernelGGL((KERNEL<bf16_t, 1024>), grid, dim3(1024), 0, st, __VA_ARGS__);                           \
+        }                                                                                                                    \
+        TRY(launched());                                                                                                     \
+    } while (0)
 
 bool all_there(const nnt_tensor* t) {
     for (void* p : t->tiles)
@@ -582,16 +602,8 @@ int32_t nnt_token_logprob(nnt_ctx* ctx, nnt_tensor* X, const int32_t* labels, nn
         float* const* out = out_tiles(logp);
         OpTag tag(ctx, "token_logprob", (double)X->shape[0] * ncols * X->elem_size(), true);
         return submit(ctx, {X->all(kRead), logp->all(kWrite)}, [=](hipStream_t st) {
-            const dim3 grid((unsigned)ncols);
-            const bool small = small_column(dt, a.nvec) || ncols >= (getenv("LP_MIN") ? atoi(getenv("LP_MIN")) : 1024);
-            if (dt == NNT_F32) {
-                if (small) hipLaunchKernelGGL((logprob_kernel<float, 256>), grid, dim3(256), 0, st, a, out);
-                else hipLaunchKernelGGL((logprob_kernel<float, 1024>), grid, dim3(1024), 0, st, a, out);
-            } else {
-                if (small) hipLaunchKernelGGL((logprob_kernel<bf16_t, 256>), grid, dim3(256), 0, st, a, out);
-                else hipLaunchKernelGGL((logprob_kernel<bf16_t, 1024>), grid, dim3(1024), 0, st, a, out);
-            }
-            return launched();
+            NNT_PER_COLUMN(logprob_kernel, threads_of(dt, a.nvec, ncols, true), a, out);
+            return (int32_t)NNT_OK;
         });
     });
 }
@@ -623,7 +635,7 @@ int32_t nnt_policy_loss(nnt_ctx* ctx, const nnt_policy_cfg* cfg, nnt_tensor* X, 
         const int reduction = cfg->reduction;
         if (reduction != NNT_REDUCE_SUM) TRY(ensure_stream_scratch(ctx, X->shape[2]));
         int nt;
-        const PolicyFn fn = policy_of(X->dtype, a.nvec, &nt);
+        const PolicyFn fn = policy_of(X->dtype, a.nvec, ncols, &nt);
         PolicyArgs p{};
         p.old_logp = in_tiles(old_logp);
         p.ref_logp = cfg->kl_coef > 0.0 ? in_tiles(ref_logp) : nullptr;
@@ -692,21 +704,12 @@ int32_t nnt_preference_loss(nnt_ctx* ctx, const nnt_preference_cfg* cfg, nnt_ten
             w.diff = reinterpret_cast<double*>(stream_scratch_of(ctx));
             w.reward = w.diff + ncols;
             w.stats = reinterpret_cast<float*>(w.reward + N_b);
-            const dim3 grid((unsigned)ncols);
-            const bool small = small_column(dt, a.nvec);
-#define NNT_PREFERENCE(KERNEL, ...)                                                                                          \
-    do {                                                                                                                     \
-        if (dt == NNT_F32 && small) hipLaunchKernelGGL((KERNEL<float, 256>), grid, dim3(256), 0, st, __VA_ARGS__);           \
-        else if (dt == NNT_F32) hipLaunchKernelGGL((KERNEL<float, 1024>), grid, dim3(1024), 0, st, __VA_ARGS__);             \
-        else if (small) hipLaunchKernelGGL((KERNEL<bf16_t, 256>), grid, dim3(256), 0, st, __VA_ARGS__);                      \
-        else hipLaunchKernelGGL((KERNEL<bf16_t, 1024>), grid, dim3(1024), 0, st, __VA_ARGS__);                               \
-        TRY(launched());                                                                                                     \
-    } while (0)
-            NNT_PREFERENCE(preference_stats_kernel, a, ref, out, w);
+            const int nt = threads_of(dt, a.nvec, ncols, true);
+            NNT_PER_COLUMN(preference_stats_kernel, nt, a, ref, out, w);
             hipLaunchKernelGGL(reward_kernel, dim3((unsigned)N_b), dim3(256), 0, st, w, N_s, p.beta, rewards);
             TRY(launched());
-            if (grad) NNT_PREFERENCE(preference_gradient_kernel, a, w, p, grad);
-#undef NNT_PREFERENCE
+            // (a column's gradient has no end to wait for: here many threads keep more of it on its way)
+            if (grad) NNT_PER_COLUMN(preference_gradient_kernel, threads_of(dt, a.nvec, ncols, false), a, w, p, grad);
             hipLaunchKernelGGL(preference_total_kernel, dim3(1), dim3(256), 0, st, w, p, losses, loss);
             return launched();
         }, grad ? 4 : 3);
