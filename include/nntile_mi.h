@@ -558,9 +558,11 @@ NNT_API int32_t nnt_sgd_step(nnt_ctx* ctx, const nnt_sgd_cfg* cfg, nnt_tensor* G
  * fp32 products.  A zero matrix gives zeros; a matrix that holds an infinity or a NaN gives NaN.  eps > 0, 1 <= steps <= 64.
  * The coefficients must keep singular values, their squares and b s^2 + c s^4 below 8 from any start in [0, 1] (NNT_EINVAL
  * otherwise); (3.4445, -4.7750, 2.0315) with 5 steps is the usual choice, (1.5, -0.5, 0) the classical one.
- * As many matrices as fill the chip go through one set of launches; G and O are arrays of n pointers.  One task per
- * set, whatever the context's granularity; it uses a workspace of the context, about 16 bytes per element of the set's
- * matrices and 8 per element of their Gram matrices, which must exist before a graph capture (run the call once). */
+ * As many matrices as fill the chip (at most 16) go through one set of launches; G and O are arrays of n pointers.  One
+ * task per set, whatever the context's granularity; it uses a workspace of the context, about 16 bytes per element
+ * of the set's matrices and 16 per element of their Gram matrices, which must exist before a graph capture (run the
+ * call once).  NNT_ENOMEM (nothing has been launched, the context stays usable): no memory for it.  At most 2^22 rows
+ * or columns and 2^36 elements a matrix. */
 typedef struct nnt_newton_schulz_cfg {
     double a, b, c, eps;
     int32_t steps;

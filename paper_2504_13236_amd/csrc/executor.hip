@@ -336,8 +336,25 @@ int32_t ensure_stream_scratch(nnt_ctx* ctx, int64_t elems) {
     return grow_scratch(ctx, &ctx->stream_scratch, &ctx->stream_scratch_elems, &ctx->stream_mem, elems, ctx->n_streams);
 }
 
+// (Several GB for the largest matrices: a lack of memory is the caller's to deal with, not the end of the context.)
 int32_t ensure_matrix_scratch(nnt_ctx* ctx, int64_t bytes) {
-    return grow_scratch(ctx, &ctx->matrix_scratch, &ctx->matrix_scratch_elems, &ctx->matrix_mem, (bytes + 3) / 4, 1);
+    const int64_t have = ctx->matrix_mem ? ctx->matrix_mem->bytes : 0;
+    if (bytes <= have) return NNT_OK;
+    if (ctx->capturing) return fail(ctx, NNT_ESTATE, "the workspace of matrix iterations must exist before capture: run the operation once first");
+    const int32_t rc = sync_all(ctx);
+    if (rc != NNT_OK) return rc;
+    ctx->matrix_scratch = nullptr;
+    replace_mem(ctx, &ctx->matrix_mem);
+    std::shared_ptr<Scratch> fresh(new Scratch());
+    fresh->bytes = (bytes + 0xfffff) / 0x100000 * 0x100000;
+    if (hipMalloc((void**)&fresh->p, (size_t)fresh->bytes) != hipSuccess) {
+        fresh->p = nullptr;
+        (void)hipGetLastError();
+        return fail(ctx, NNT_ENOMEM, "no memory for the workspace of matrix iterations: " + std::to_string(fresh->bytes) + " bytes");
+    }
+    ctx->matrix_scratch = fresh->p;
+    ctx->matrix_mem = std::move(fresh);
+    return NNT_OK;
 }
 
 }  // namespace nnt

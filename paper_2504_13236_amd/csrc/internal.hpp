@@ -166,7 +166,6 @@ struct nnt_ctx {
     std::shared_ptr<nnt::Scratch> stream_mem;
     // what the Newton-Schulz iterations of matrices work in; one task at a time
     float* matrix_scratch = nullptr;
-    int64_t matrix_scratch_elems = 0;
     std::shared_ptr<nnt::Scratch> matrix_mem;
     nnt::TileDep matrix_dep;
     std::weak_ptr<nnt::PackSpace> pack_space;

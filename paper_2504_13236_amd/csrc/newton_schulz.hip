@@ -919,10 +919,10 @@ double most_of_square(double c1, double c2, double top) {
     return most;
 }
 // Whether the iteration stays where the workspace's numbers can hold it (2^12 times 16 is fp16's largest number): singular values start in [0, 1]; with their
-// bound followed from step to step, they, their squares and b s^2 + c s^4 have to stay below 8.
-bool in_range(const nnt_newton_schulz_cfg& c) {
+// bound followed from step to step, they, their squares and b s^2 + c s^4 have to stay below 8.  *reach: the largest of the bounds.
+bool in_range(const nnt_newton_schulz_cfg& c, double* reach = nullptr) {
     if (!std::isfinite(c.a) || !std::isfinite(c.b) || !std::isfinite(c.c) || !(c.eps > 0.0) || !std::isfinite(c.eps) || c.steps < 1 || c.steps > 64) return false;
-    double top = 1.0;
+    double top = 1.0, far = 1.0;
     for (int t = 0; t < c.steps; t++) {
         const double l = top * top;
         if (!(most_of_square(c.b, c.c, l) <= 8.0)) return false;
@@ -938,8 +938,26 @@ bool in_range(const nnt_newton_schulz_cfg& c) {
         }
         if (!(most <= 8.0) || !(most * most <= 8.0)) return false;
         top = most;
+        far = std::max(far, top);
     }
+    if (reach) *reach = far;
     return true;
+}
+
+// Whether two steps can be taken at once: the workspace also has to hold P = a I + b A + c A^2 and P_1 P_0 - a^2 I then.
+bool pairs_in_range(const nnt_newton_schulz_cfg& c) {
+    double low = c.a, high = c.a, reach = 1.0;
+    if (!in_range(c, &reach)) return false;
+    const double l = reach * reach;
+    for (double x : {l, c.c != 0.0 ? -c.b / (2.0 * c.c) : 0.0})
+        if (x > 0.0 && x <= l) {
+            const double p = c.a + c.b * x + c.c * x * x;
+            low = std::min(low, p);
+            high = std::max(high, p);
+        }
+    double most = std::max(std::fabs(low), std::fabs(high));
+    for (double p : {low * low, low * high, high * high}) most = std::max(most, std::fabs(p - c.a * c.a));
+    return most < 15.0;
 }
 
 bool whole_matrix(const nnt_ctx* ctx, const nnt_tensor* t) {
@@ -1051,110 +1069,128 @@ Launch choose(const NsSizes& g, int mode) {
     return best;
 }
 
-// Orthogonalises the matrices of `tasks` and applies the results, as many of them in one set of launches as it takes to fill the
-// chip.  mu < 0: no momentum.
-int32_t run_tasks(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& cfg, float mu, int nesterov, const std::vector<Task>& tasks, bool narrow) {
-    size_t first = 0;
-    while (first < tasks.size()) {
-        NsGroup g{};
-        NsSizes sizes{};
-        g.nesterov = nesterov;
-        g.mu = mu;
-        g.a = (float)cfg.a;
-        g.b = (float)cfg.b;
-        g.c = (float)cfg.c;
-        g.eps = (float)cfg.eps;
-        int64_t bytes = (sizeof(NsGroup) + 255) / 256 * 256, patch = 0, chunks = 0;
-        double work = 0.0;
-        std::vector<Access> acc;
-        while (first < tasks.size() && g.n < kGroupMatrices && patch < 4096) {
-            const Task& t = tasks[first++];
-            const int64_t rows = t.G->shape[0], cols = t.G->shape[1], m = std::min(rows, cols), l = std::max(rows, cols);
-            const int64_t mb = (m + 63) / 64, nb = (l + 63) / 64;
-            if (nb > 0xffff || mb * nb > (1 << 24)) return fail(ctx, NNT_EINVAL, std::string(label) + ": matrix too large");
-            sizes.blocks[g.n] = (uint32_t)mb | ((uint32_t)nb << 16);
-            NsMatrix& q = g.mat[g.n++];
-            q.rows = (int32_t)rows;
-            q.cols = (int32_t)cols;
-            q.base0 = (int32_t)t.G->base[0];
-            q.base1 = (int32_t)t.G->base[1];
-            q.grid0 = (int32_t)t.G->grid[0];
-            q.grid1 = (int32_t)t.G->grid[1];
-            q.flip = rows > cols;
-            q.mp = (int32_t)(mb * 64);
-            q.np = (int32_t)(nb * 64);
-            patch += mb * nb;
-            chunks = std::max(chunks, (t.G->base[0] * t.G->base[1] + kNormChunk - 1) / kNormChunk * t.G->grid[0] * t.G->grid[1]);
-            // (narrow ones: the transpose once, and A in parts)
-            const int64_t x = narrow ? (int64_t)q.mp * q.np * 2 : (int64_t)q.mp * q.np * 4;
-            const int64_t a = narrow ? (int64_t)narrow_parts((int)nb) * 64 * 64 * 2 : (int64_t)q.mp * q.mp * 4;
-            q.X = bytes;
-            q.XT = narrow ? bytes : q.X + 2 * x;
-            q.A = q.XT + 2 * x;
-            q.part = q.A + 4 * a;
-            bytes = q.part + kNormBlocks * 8;
-            q.G = MatView{t.G->d_tiles, t.G->dtype};
-            q.P = MatView{t.P->d_tiles, t.P->dtype};
-            if (t.M) q.M = MatView{t.M->d_tiles, NNT_F32};
-            if (t.LP) q.LP = MatView{t.LP->d_tiles, NNT_BF16};
-            q.decay = t.decay;
-            q.step = t.step;
-            work += cfg.steps * (3.0 * m * m * l + (double)m * m * m);
-            acc.push_back(t.G->all(kRead));
-            acc.push_back(t.P->all(t.step < 0.f ? kWrite : kReadWrite));
-            if (t.M) acc.push_back(t.M->all(kReadWrite));
-            if (t.LP) acc.push_back(t.LP->all(kWrite));
-        }
-        g.norm_blocks = (int32_t)std::min<int64_t>(chunks, kNormBlocks);
-        sizes.n = g.n;
-        int parts = 0;
-        for (int k = 0; k < g.n; k++) parts = std::max(parts, narrow_parts((int)(sizes.blocks[k] >> 16)));
-        const Launch gram = choose(sizes, kGram), poly = choose(sizes, kPoly), step = choose(sizes, kStep), last = choose(sizes, kLast);
-        g.partial = bytes;
-        if (!narrow && gram.splits > 1) bytes += (int64_t)gram.tiles * gram.splits * (gram.shape == 0 ? Small::BM * Small::BM : Middle::BM * Middle::BM) * 4;
-        const int32_t rc = ensure_matrix_scratch(ctx, bytes);
-        if (rc != NNT_OK) return rc;
-        g.space = reinterpret_cast<char*>(ctx->matrix_scratch);
-        acc.push_back(Access{&ctx->matrix_dep, 1, kReadWrite});
-        const int steps = cfg.steps;
-        const bool pairs = 1.15 * 3.0 * poly.time < gram.time + step.time;
-        const std::vector<Item> items = narrow ? std::vector<Item>() : plan(cfg, pairs);
-        OpTag tag(ctx, label, work, false);
-        const NsGroup* there = reinterpret_cast<const NsGroup*>(g.space);
-        const int32_t sc = submit(ctx, acc, [=](hipStream_t st) {
-            hipLaunchKernelGGL(ns_norm_kernel, dim3((unsigned)g.norm_blocks, (unsigned)g.n), dim3(1024), 0, st, g);
-            if (narrow) {
-                const dim3 grid((unsigned)parts, (unsigned)g.n), block(256);
-                hipLaunchKernelGGL((ns_narrow_kernel<kFirst>), grid, block, 0, st, there, sizes, 0);
-                for (int s = 0; s + 1 < steps; s++) hipLaunchKernelGGL((ns_narrow_kernel<kMiddle>), grid, block, 0, st, there, sizes, s & 1);
-                hipLaunchKernelGGL((ns_narrow_kernel<kFinal>), grid, block, 0, st, there, sizes, (steps - 1) & 1);
-                return launched();
-            }
-            hipLaunchKernelGGL(ns_split_kernel, dim3((unsigned)patch), dim3(256), 0, st, there, sizes);
-            for (const Item& t : items) {
-                const Launch& l = t.mode == kGram ? gram : t.mode == kPoly ? poly : t.mode == kStep ? step : last;
-                if (l.shape == 2) launch_product<Large>(t.mode, there, sizes, t.op, t.now, l.tiles, l.splits, st);
-                else if (l.shape == 1) launch_product<Middle>(t.mode, there, sizes, t.op, t.now, l.tiles, l.splits, st);
-                else launch_product<Small>(t.mode, there, sizes, t.op, t.now, l.tiles, l.splits, st);
-            }
-            return launched();
-        }, narrow ? 2 + steps : 2 + (int)items.size() + (gram.splits > 1 ? steps : 0));
-        if (sc != NNT_OK) return sc;
+// One set of launches: as many matrices as it takes to fill the chip.
+struct Set {
+    NsGroup g{};
+    NsSizes sizes{};
+    bool narrow = false;
+    Launch launch[4];                    // by mode
+    std::vector<Item> items;
+    int parts = 0;
+    int64_t patch = 0, bytes = 0;        // 64 x 64 blocks of all matrices; workspace
+    double work = 0.0;
+    std::vector<Access> acc;
+};
+
+// Puts tasks from number *first on into a set.
+int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& cfg, float mu, int nesterov, const std::vector<Task>& tasks, bool narrow, size_t* first, Set* out) {
+    Set& w = *out;
+    NsGroup& g = w.g;
+    g.nesterov = nesterov;
+    g.mu = mu;
+    g.a = (float)cfg.a;
+    g.b = (float)cfg.b;
+    g.c = (float)cfg.c;
+    g.eps = (float)cfg.eps;
+    w.narrow = narrow;
+    int64_t bytes = (sizeof(NsGroup) + 255) / 256 * 256, chunks = 0;
+    while (*first < tasks.size() && g.n < kGroupMatrices && w.patch < 4096) {
+        const Task& t = tasks[(*first)++];
+        const int64_t rows = t.G->shape[0], cols = t.G->shape[1], m = std::min(rows, cols), l = std::max(rows, cols);
+        const int64_t mb = (m + 63) / 64, nb = (l + 63) / 64;
+        if (nb > 0xffff || mb * nb > (1 << 24)) return fail(ctx, NNT_EINVAL, std::string(label) + ": matrix too large");
+        w.sizes.blocks[g.n] = (uint32_t)mb | ((uint32_t)nb << 16);
+        NsMatrix& q = g.mat[g.n++];
+        q.rows = (int32_t)rows;
+        q.cols = (int32_t)cols;
+        q.base0 = (int32_t)t.G->base[0];
+        q.base1 = (int32_t)t.G->base[1];
+        q.grid0 = (int32_t)t.G->grid[0];
+        q.grid1 = (int32_t)t.G->grid[1];
+        q.flip = rows > cols;
+        q.mp = (int32_t)(mb * 64);
+        q.np = (int32_t)(nb * 64);
+        w.patch += mb * nb;
+        if (narrow) w.parts = std::max(w.parts, narrow_parts((int)nb));
+        chunks = std::max(chunks, (t.G->base[0] * t.G->base[1] + kNormChunk - 1) / kNormChunk * t.G->grid[0] * t.G->grid[1]);
+        // X and its transpose, two buffers each, and four square ones; narrow matrices: the transpose once, and two times A in parts
+        const int64_t x = (int64_t)q.mp * q.np * 4, a = (int64_t)q.mp * q.mp * 4;
+        q.X = bytes;
+        q.XT = narrow ? bytes : q.X + 2 * x;
+        q.A = narrow ? q.XT + x : q.XT + 2 * x;
+        q.part = q.A + (narrow ? (int64_t)narrow_parts((int)nb) * 64 * 64 * 4 * 2 : 4 * a);
+        bytes = q.part + kNormBlocks * 8;
+        q.G = MatView{t.G->d_tiles, t.G->dtype};
+        q.P = MatView{t.P->d_tiles, t.P->dtype};
+        if (t.M) q.M = MatView{t.M->d_tiles, NNT_F32};
+        if (t.LP) q.LP = MatView{t.LP->d_tiles, NNT_BF16};
+        q.decay = t.decay;
+        q.step = t.step;
+        w.work += cfg.steps * (3.0 * m * m * l + (double)m * m * m);
+        w.acc.push_back(t.G->all(kRead));
+        w.acc.push_back(t.P->all(t.step < 0.f ? kWrite : kReadWrite));
+        if (t.M) w.acc.push_back(t.M->all(kReadWrite));
+        if (t.LP) w.acc.push_back(t.LP->all(kWrite));
     }
+    w.acc.push_back(Access{&ctx->matrix_dep, 1, kReadWrite});
+    g.norm_blocks = (int32_t)std::min<int64_t>(chunks, kNormBlocks);
+    w.sizes.n = g.n;
+    g.partial = bytes;
+    if (!narrow) {
+        for (int mode : {(int)kGram, (int)kPoly, (int)kStep, (int)kLast}) w.launch[mode] = choose(w.sizes, mode);
+        const Launch& gram = w.launch[kGram];
+        if (gram.splits > 1) bytes += (int64_t)gram.tiles * gram.splits * (gram.shape == 0 ? Small::BM * Small::BM : Middle::BM * Middle::BM) * 4;
+        // (the model is a tenth and more off either way: two steps at once have to promise that much)
+        w.items = plan(cfg, pairs_in_range(cfg) && 1.15 * 3.0 * w.launch[kPoly].time < gram.time + w.launch[kStep].time);
+    }
+    w.bytes = bytes;
     return NNT_OK;
 }
 
+int32_t submit_set(nnt_ctx* ctx, const char* label, int steps, const Set& w) {
+    NsGroup g = w.g;
+    g.space = reinterpret_cast<char*>(ctx->matrix_scratch);
+    const NsGroup* there = reinterpret_cast<const NsGroup*>(g.space);
+    OpTag tag(ctx, label, w.work, false);
+    return submit(ctx, w.acc, [&](hipStream_t st) {
+        hipLaunchKernelGGL(ns_norm_kernel, dim3((unsigned)g.norm_blocks, (unsigned)g.n), dim3(1024), 0, st, g);
+        if (w.narrow) {
+            const dim3 grid((unsigned)w.parts, (unsigned)g.n), block(256);
+            hipLaunchKernelGGL((ns_narrow_kernel<kFirst>), grid, block, 0, st, there, w.sizes, 0);
+            for (int s = 0; s + 1 < steps; s++) hipLaunchKernelGGL((ns_narrow_kernel<kMiddle>), grid, block, 0, st, there, w.sizes, s & 1);
+            hipLaunchKernelGGL((ns_narrow_kernel<kFinal>), grid, block, 0, st, there, w.sizes, (steps - 1) & 1);
+            return launched();
+        }
+        hipLaunchKernelGGL(ns_split_kernel, dim3((unsigned)w.patch), dim3(256), 0, st, there, w.sizes);
+        for (const Item& t : w.items) {
+            const Launch& l = w.launch[t.mode];
+            if (l.shape == 2) launch_product<Large>(t.mode, there, w.sizes, t.op, t.now, l.tiles, l.splits, st);
+            else if (l.shape == 1) launch_product<Middle>(t.mode, there, w.sizes, t.op, t.now, l.tiles, l.splits, st);
+            else launch_product<Small>(t.mode, there, w.sizes, t.op, t.now, l.tiles, l.splits, st);
+        }
+        return launched();
+    }, w.narrow ? 2 + steps : 2 + (int)w.items.size() + (w.launch[kGram].splits > 1 ? steps : 0));
+}
+
+// Orthogonalises the matrices of `tasks` and applies the results.  mu < 0: no momentum.  Nothing is launched before all sets are known to fit.
 int32_t newton_schulz(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& cfg, float mu, int nesterov, const std::vector<Task>& tasks) {
     std::vector<Task> kind[2];
     for (const Task& t : tasks) {
         const int64_t m = std::min(t.G->shape[0], t.G->shape[1]), l = std::max(t.G->shape[0], t.G->shape[1]);
         kind[m <= 64 && l <= 64 * kNarrowBlocks].push_back(t);
     }
-    for (int narrow = 0; narrow < 2; narrow++) {
-        const int32_t rc = run_tasks(ctx, label, cfg, mu, nesterov, kind[narrow], narrow != 0);
-        if (rc != NNT_OK) return rc;
-    }
-    return NNT_OK;
+    std::vector<Set> sets;
+    int64_t bytes = 0;
+    for (int narrow = 0; narrow < 2; narrow++)
+        for (size_t first = 0; first < kind[narrow].size();) {
+            sets.emplace_back();
+            const int32_t rc = make_set(ctx, label, cfg, mu, nesterov, kind[narrow], narrow != 0, &first, &sets.back());
+            if (rc != NNT_OK) return rc;
+            bytes = std::max(bytes, sets.back().bytes);
+        }
+    int32_t rc = ensure_matrix_scratch(ctx, bytes);
+    for (size_t k = 0; rc == NNT_OK && k < sets.size(); k++) rc = submit_set(ctx, label, cfg.steps, sets[k]);
+    return rc;
 }
 
 }  // namespace

@@ -88,6 +88,74 @@ def test_iterations(mods, steps, a, b, c):
         assert np.linalg.norm(tO.download() - want) <= bound(want, steps, a)
 
 
+@pytest.mark.parametrize("shape", [(50, 70), (768, 2304), (700, 3000)])
+@pytest.mark.parametrize("steps,a,b,c", [(1, A, B, CC), (2, A, B, CC), (3, A, B, CC), (4, 2.0, -1.5, 0.5), (7, 1.5, -0.5, 0.0)])
+def test_iterations_of_narrow_and_of_long_matrices(mods, shape, steps, a, b, c):
+    """One launch per step, and two steps at once with one left over or none."""
+    capi, tiled = mods
+    G = np.random.default_rng(2).standard_normal(shape).astype(np.float32)
+    want = D.orthogonalize(G, a, b, c, 1e-7, steps)
+    with tiled.Context(n_streams=1) as ctx:
+        tG, tO = tiled.TiledTensor.from_numpy(ctx, G, (64, 1000)), tiled.TiledTensor(ctx, "f32", G.shape, (64, 1000))
+        capi.nnt_orthogonalize(ctx.h, C.byref(ns(capi, steps, a, b, c)), 1, handles(mods, [tG]), handles(mods, [tO]))
+        assert np.linalg.norm(tO.download() - want) <= bound(want, steps, a)
+
+
+def test_pairs_of_steps_stay_in_range(mods):
+    """Coefficients that the iteration itself can take, but not the polynomial of two steps: those go one by one."""
+    capi, tiled = mods
+    a, b, c = 3.9, -5.2, 2.1
+    G = gradient(np.random.default_rng(8), 512, 2560)
+    want = D.orthogonalize(G, a, b, c, 1e-7, 2)
+    with tiled.Context(n_streams=1) as ctx:
+        tG, tO = tiled.TiledTensor.from_numpy(ctx, G, (512, 2560)), tiled.TiledTensor(ctx, "f32", G.shape, (512, 2560))
+        capi.nnt_orthogonalize(ctx.h, C.byref(ns(capi, 2, a, b, c)), 1, handles(mods, [tG]), handles(mods, [tO]))
+        assert np.linalg.norm(tO.download() - want) <= bound(want, 2, a)
+
+
+@pytest.mark.parametrize("shape", [(4096, 4096), (2500, 8300), (6000, 3000)])
+def test_large_matrices(mods, shape):
+    """The largest macro-tiles, ends inside them, tall and wide; against plain products in 64 bits on the device."""
+    capi, tiled = mods
+    g = torch.Generator(device="cuda").manual_seed(5)
+    G = torch.randn(*shape, generator=g, device="cuda", dtype=torch.float32)
+    X = G.double() / torch.linalg.vector_norm(G.double())
+    flip = shape[0] > shape[1]
+    X = X.t().contiguous() if flip else X
+    for _ in range(5):
+        S = torch.mm(X, X.t())
+        X = A * X + torch.mm(B * S + CC * torch.mm(S, S), X)
+    want = X.t() if flip else X
+    with tiled.Context(n_streams=2) as ctx:
+        base = (3000, 3000)
+        tG, tO = tiled.TiledTensor(ctx, "f32", shape, base), tiled.TiledTensor(ctx, "f32", shape, base)
+        for k, idx in enumerate(tG.tile_index):
+            tG.tile_view(k).copy_(G[tG.slices(idx)].t().reshape(-1))
+        torch.cuda.synchronize()
+        capi.nnt_orthogonalize(ctx.h, C.byref(ns(capi)), 1, handles(mods, [tG]), handles(mods, [tO]))
+        ctx.wait()
+        err = 0.0
+        for k, idx in enumerate(tO.tile_index):
+            w = want[tO.slices(idx)]
+            err += (tO.tile_view(k).view(w.shape[1], w.shape[0]).t().double() - w).square().sum().item()
+        norm = torch.linalg.vector_norm(want).item()
+        assert err ** 0.5 <= 2.0 ** -22 * (8 * A ** 5 + 64 * norm)
+
+
+def test_contractions_of_very_different_lengths_in_one_group(mods):
+    """The long contraction is cut into more parts than the short one has steps."""
+    capi, tiled = mods
+    r = np.random.default_rng(9)
+    Gs = [gradient(r, 100, 6000), gradient(r, 70, 66), gradient(r, 130, 90)]
+    with tiled.Context(n_streams=1) as ctx:
+        G = [tiled.TiledTensor.from_numpy(ctx, x, (64, 1000)) for x in Gs]
+        O = [tiled.TiledTensor(ctx, "f32", x.shape, (64, 1000)) for x in Gs]
+        capi.nnt_orthogonalize(ctx.h, C.byref(ns(capi)), 3, handles(mods, G), handles(mods, O))
+        for x, o in zip(Gs, O):
+            want = D.orthogonalize(x)
+            assert np.linalg.norm(o.download() - want) <= bound(want)
+
+
 def test_scales_zeros_and_values_that_are_no_numbers(mods):
     """Gradients of any size (squares that overflow or vanish in fp32), single entries, zeros; NaN and infinity."""
     capi, tiled = mods
@@ -219,6 +287,15 @@ def test_captured_and_replayed(mods):
             go()
             np.testing.assert_array_equal(P.download(), replayed[0])
             np.testing.assert_array_equal(M.download(), replayed[1])
+        # narrow and other matrices in one call inside a capture: nothing is recorded if the workspace is too small
+        narrow, wide = T(gradient(r, 40, 300)), T(gradient(r, 1500, 2000))
+        capi.nnt_capture_begin(ctx.h)
+        before = ctx.stats()["launches"]
+        assert capi.nnt_orthogonalize.raw(ctx.h, C.byref(ns(capi)), 2, handles(mods, [narrow, wide]), handles(mods, [narrow, wide])) == capi.NNT_ESTATE
+        assert ctx.stats()["launches"] == before
+        empty = C.c_void_p()
+        capi.nnt_capture_end(ctx.h, C.byref(empty))
+        capi.nnt_graph_destroy(empty)
         held = ctx.stats()["device_workspace_bytes"]
         capi.nnt_graph_destroy(g)
         assert ctx.stats()["device_workspace_bytes"] < held
