@@ -64,7 +64,8 @@ struct NsGroup {
     char* space;
     int32_t n, norm_blocks, nesterov;
     float mu;                                            // < 0: no momentum, U = G
-    float a, b, c, eps;
+    float a, b, c;
+    double eps;
     int64_t partial;                                     // parts of A's tiles, bytes from the start of the workspace
     NsMatrix mat[kGroupMatrices];
 };
@@ -196,6 +197,18 @@ __device__ __forceinline__ int64_t panel_at(int row, int k, int K) {
     return ((int64_t)(row >> 6) * (K >> 4) + (k >> 4)) * kPanelBytes + ((k & 15) >> 3) * 1024 + (row & 63) * 16;
 }
 
+// 2^12 x / length, for any length above 0 (in 64 bits: the sum of the partial sums' root and eps): a factor between 1 and 2 and a power of two, since the
+// quotient alone can lie outside of fp32.
+struct Scale {
+    float factor;
+    int exponent;
+    __device__ __forceinline__ explicit Scale(double length) {
+        factor = (float)(1.0 / frexp(length, &exponent));
+        exponent = 12 - exponent;
+    }
+    __device__ __forceinline__ float operator()(float x) const { return ldexpf(x, exponent) * factor; }
+};
+
 // ---------------------------------------------------------------- set-up: X_0 and its transpose
 // One workgroup takes 64 x 64 elements: read along the tensor's contiguous axis, turned in LDS, written as panels of both.
 __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict__ group, NsSizes sizes) {
@@ -220,14 +233,14 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
     if (lane == 0) red[wave] = sum;
     __syncthreads();
-    const float scale = (float)((double)kScale / (sqrt(red[0] + red[1] + red[2] + red[3]) + (double)g.eps));
+    const Scale scaled(sqrt(red[0] + red[1] + red[2] + red[3]) + g.eps);
 #pragma unroll
     for (int s = 0; s < 16; s++) {
         float x = u[s];
         if (g.mu >= 0.f) x = g.nesterov ? fmaf(g.mu, m[s], x) : m[s];
         const int c = wave * 16 + s;
-        if (q.flip) t[c][lane] = x * scale;
-        else t[lane][c] = x * scale;
+        if (q.flip) t[c][lane] = scaled(x);
+        else t[lane][c] = scaled(x);
     }
     __syncthreads();
     // a lane's row, a wavefront's two groups of eight columns, of X and of its transpose
@@ -744,7 +757,7 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
     float4* sums = reinterpret_cast<float4*>(g.space + q.A);             // two buffers of `parts` images of 64 x 64 in fp32, as they lie in registers
     auto sum_at = [&](int buffer, int p, int v) { return (((int64_t)buffer * parts + p) * 4 + wave) * 256 + v * 64 + lane; };
     const int i = wr * 32 + (lane >> 5) * 4, j = wc * 32 + (lane & 31);    // this lane's results: rows i + 8 p + 0 .. 3, column j of a block
-    float scale = 0.f;
+    Scale scaled(1.0);
     if constexpr (PHASE == kFirst) {
         const double* norms = reinterpret_cast<const double*>(g.space + q.part);
         double sum = 0.0;
@@ -753,7 +766,7 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
         for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
         if (lane == 0) red[wave] = sum;
         __syncthreads();
-        scale = (float)((double)kScale / (sqrt(red[0] + red[1] + red[2] + red[3]) + (double)g.eps));
+        scaled = Scale(sqrt(red[0] + red[1] + red[2] + red[3]) + g.eps);
     } else {
         float4 t[4];
 #pragma unroll
@@ -822,8 +835,8 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
 #pragma unroll
             for (int s = 0; s < 16; s++) {
                 if (g.mu >= 0.f) x[s] = g.nesterov ? fmaf(g.mu, m[s], x[s]) : m[s];
-                if (q.flip) u[wave * 16 + s][lane] = x[s] * scale;
-                else u[lane][wave * 16 + s] = x[s] * scale;
+                if (q.flip) u[wave * 16 + s][lane] = scaled(x[s]);
+                else u[lane][wave * 16 + s] = scaled(x[s]);
             }
             __syncthreads();
 #pragma unroll
@@ -1091,7 +1104,7 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
     g.a = (float)cfg.a;
     g.b = (float)cfg.b;
     g.c = (float)cfg.c;
-    g.eps = (float)cfg.eps;
+    g.eps = cfg.eps;
     w.narrow = narrow;
     int64_t bytes = (sizeof(NsGroup) + 255) / 256 * 256, chunks = 0;
     while (*first < tasks.size() && g.n < kGroupMatrices && w.patch < 4096) {

@@ -179,6 +179,23 @@ def test_scales_zeros_and_values_that_are_no_numbers(mods):
             assert np.isnan(run(bad, 1e-7)).all()
 
 
+@pytest.mark.parametrize("shape", [(20, 30), (100, 130)])
+def test_lengths_near_the_ends_of_32_bits(mods, shape):
+    """Matrices whose length, or 2^12 over it, fp32 does not hold, and an eps that it does not hold either."""
+    capi, tiled = mods
+    G = gradient(np.random.default_rng(3), *shape)
+    with tiled.Context(n_streams=2) as ctx:
+        for largest in (2.0 ** -123, 2.0 ** 127):
+            x = np.float32(G / np.abs(G).max() * largest)
+            want = D.orthogonalize(x, eps=1e-300)
+            tG, tO = tiled.TiledTensor.from_numpy(ctx, x, (64, 64)), tiled.TiledTensor(ctx, "f32", G.shape, (64, 64))
+            capi.nnt_orthogonalize(ctx.h, C.byref(ns(capi, eps=1e-300)), 1, handles(mods, [tG]), handles(mods, [tO]))
+            assert np.linalg.norm(tO.download() - want) <= bound(want)
+        zero = tiled.TiledTensor.from_numpy(ctx, np.zeros(shape, np.float32), (64, 64))
+        capi.nnt_orthogonalize(ctx.h, C.byref(ns(capi, eps=1e-300)), 1, handles(mods, [zero]), handles(mods, [tO]))
+        assert not tO.download().any()
+
+
 @pytest.mark.parametrize("nesterov", [0, 1])
 @pytest.mark.parametrize("scale", ["none", "aspect", "rms"])
 @pytest.mark.parametrize("low", [False, True])

@@ -286,6 +286,61 @@ def test_nan_in_a_column_stays_in_it(mods):
         assert np.isfinite(logp[ok]).all() and np.isfinite(dX[:, ok]).all()
 
 
+@pytest.mark.parametrize("reduction", [1, 2])
+@pytest.mark.parametrize("N_s,N_b", [(40, 1030), (33, 1023), (32, 70), (1, 2050), (3000, 2), (5, 1)])
+def test_weights_of_many_and_of_few_sequences(mods, N_s, N_b, reduction):
+    """Logits that are all alike: every position's loss is its weight times -A."""
+    capi, tiled = mods
+    r = np.random.default_rng(N_s + N_b)
+    lab = labels_for(r, 3, N_s, N_b, 0.4)
+    if N_b > 1:
+        lab[:, N_b // 2] = -1                                     # a sequence without any label
+    w = D.position_weights(has_label(lab, 3), ("sum", "tokens", "sequences")[reduction])
+    with tiled.Context(n_streams=1) as ctx:
+        c = Call(mods, ctx, np.zeros((3, N_s, N_b), np.float32), lab, (3, N_s, N_b), "f32", gradient=False, adv=np.ones(N_b))
+        c.policy(reduction=reduction)
+        ctx.wait()
+        got = c.losses[:N_s * N_b].cpu().numpy().reshape(N_s, N_b, order="F")
+        # 1 / n, 1 / count and their product: a rounding each, and half of one for the count's own quotient
+        c.close_to(got, -w, 4 * 2.0 ** -24, 0.0, "weights")
+
+
+def test_ratio_beyond_32_bits(mods):
+    """exp(90) is more than fp32 holds: without an advantage the position still has no loss and no gradient."""
+    capi, tiled = mods
+    X = np.zeros((40, 4, 1), np.float32)
+    X[3] = 5.0
+    lab = np.full((4, 1), 3)
+    logp = D.token_logprob(X, lab)
+    old = np.float32(logp - np.array([[90.0], [0.1], [500.0], [0.0]]))
+    adv = np.float32([[0.0], [1.5], [0.0], [0.0]])
+    with tiled.Context(n_streams=1) as ctx:
+        c = Call(mods, ctx, X, lab, (16, 4, 1), "f32", old=old, adv=adv)
+        c.policy()
+        ctx.wait()
+        loss, losses, _, want = D.policy_loss(X, lab, old, None, adv)
+        c.close_to(c.check_sum(4, loss), losses.reshape(-1, order="F"), 3e-5, 0.0, "losses")
+        c.check_gradient(want, np.ones((4, 1), bool))
+        assert not c.dX.download()[:, [0, 2, 3]].any()
+
+
+def test_answer_that_cannot_be_given(mods):
+    """A rejected answer with a token of probability 0: the margin is infinite, the loss and the gradients are 0; the other way round the loss is infinite."""
+    capi, tiled = mods
+    X = np.random.default_rng(4).standard_normal((40, 2, 4)).astype(np.float32)
+    lab = np.random.default_rng(5).integers(0, 40, (2, 4))
+    X[lab[1, 2], 1, 2] = -np.inf
+    X[lab[0, 1], 0, 1] = -np.inf
+    with tiled.Context(n_streams=1) as ctx:
+        c = Call(mods, ctx, X, lab, (16, 2, 4), "f32")
+        c.preference()
+        ctx.wait()
+        got = c.losses[:2].cpu().numpy()
+        assert got[0] == 0.0 and got[1] == np.inf and c.loss[0].item() == np.inf
+        assert not c.dX.download()[:, :, [0, 2]].any()
+        assert c.rewards[2].item() == -np.inf
+
+
 def test_losses_from_four_streams_and_repeated(mods):
     """Independent calls on one context at once, each with its own tensors, twice over: the same results bit for bit; and a
     loss that reads the log-probabilities which an earlier call wrote."""
