@@ -23,9 +23,17 @@ constexpr int kTableTiles = 64;               // vocabulary tiles whose addresse
 constexpr int64_t kMaxPositions = 1 << 22;    // a workgroup of 1024 threads each: 2^32 threads are more than a launch takes
 constexpr int64_t kMaxVectors = 1 << 20;      // of a column: up to there `place` finds a vector's tile exactly
 
-// exp(t): both factors of the exponent's product with 1/ln 2 are kept, since the rounded constant alone makes every
-// log-probability 6e-8 too small, and hundreds of them add up in a reward
-__device__ __forceinline__ float exp_of(float t) { return __builtin_amdgcn_exp2f(fmaf(t, 1.4426950216293335f, t * 1.9259629911e-8f)); }
+// exp(t), t <= 0, for logits of type T.  Both factors of the exponent's product with 1/ln 2 are kept, since the rounded constant alone makes
+// every log-probability 6e-8 too small, and hundreds of them add up in a reward.  What is left is the rounding of y = t / ln 2, 6e-8 |t| at most: enough in front
+// of bf16.  In front of fp32 it is put right: exp(t) = 2^y (1 + d), d = t - y ln 2.  There the factor in y is 2.4e-7 too large, so that d lies between 0 and
+// 3e-7 |t| (its square is nothing) and the limits that keep the infinity of t = -inf out of it cost no instruction of their own: one more than the other form,
+// and gradients off by 4e-8 instead of 2e-7 of their value.
+template <typename T>
+__device__ __forceinline__ float exp_of(float t) {
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(fmaf(t, 1.4426950216293335f, t * 1.9259629911e-8f));
+    const float y = t * 1.44269538f, r = __builtin_amdgcn_exp2f(y);
+    return fmaf(r, __builtin_amdgcn_fmed3f(fmaf(y, -0.693147182f, t), 0.f, 1.f), r);
+}
 
 // What the kernels know of the logits.  The vectors of all vocabulary tiles are numbered through, `vt` to a tile and `nvec` in all.
 struct Logits {
@@ -151,16 +159,16 @@ __device__ __forceinline__ void stream_stats(const Logits& a, const ColumnAt<T>&
             }
         }
         if (top > m) {                       // (the first time m is -inf and s 0)
-            s *= exp_of(m - top);
+            s *= exp_of<T>(m - top);
             m = top;
         }
         float part[U];
         const float shift = m == -__builtin_huge_valf() ? 0.f : m;       // nothing but -inf so far: their exponentials are 0, not NaN
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            part[u] = exp_of(raw[set][u].at(0) - shift);
+            part[u] = exp_of<T>(raw[set][u].at(0) - shift);
 #pragma unroll
-            for (int j = 1; j < V; j++) part[u] += exp_of(raw[set][u].at(j) - shift);
+            for (int j = 1; j < V; j++) part[u] += exp_of<T>(raw[set][u].at(j) - shift);
         }
         static_assert(U == 4, "added up in pairs");
         s += (part[0] + part[1]) + (part[2] + part[3]);
@@ -174,7 +182,7 @@ __device__ __forceinline__ void stream_stats(const Logits& a, const ColumnAt<T>&
         take(1, f0 + U * NT);
     }
     mx = block_max<NW>(m, red.mx);
-    sum = block_sum64<NW>(m == mx ? s : s * exp_of(m - mx), red.sum);
+    sum = block_sum64<NW>(m == mx ? s : s * exp_of<T>(m - mx), red.sum);
     x_label = red.x_label;
 }
 
@@ -313,7 +321,7 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 && NT == 1024 && SLOTS > 0
             float part = 0.f;
 #pragma unroll
             for (int j = 0; j < V; j++) {
-                const float x = exp_of(raw[it].at(j) - mx);
+                const float x = exp_of<T>(raw[it].at(j) - mx);
                 if (RawVec<T>::kKeeps) raw[it].set(j, x);
                 part += x;
             }
@@ -343,8 +351,8 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 && NT == 1024 && SLOTS > 0
         float y[V];
 #pragma unroll
         for (int j = 0; j < V; j++) {
-            if constexpr (SLOTS > 0) y[j] = (RawVec<T>::kKeeps ? raw[it].at(j) : exp_of(raw[it].at(j) - mx)) * scale;
-            else y[j] = exp_of(x.at(j) - mx) * scale;
+            if constexpr (SLOTS > 0) y[j] = (RawVec<T>::kKeeps ? raw[it].at(j) : exp_of<T>(raw[it].at(j) - mx)) * scale;
+            else y[j] = exp_of<T>(x.at(j) - mx) * scale;
         }
         if (f == at.lab_f) {
 #pragma unroll
@@ -535,7 +543,7 @@ __global__ void __launch_bounds__(NT) preference_gradient_kernel(Logits a, Prefe
             RawVec<T> x;
             x.load(base.at(a, at.c, l) + e, cnt);
 #pragma unroll
-            for (int j = 0; j < V; j++) y[j] = exp_of(x.at(j) - mx) * scale;
+            for (int j = 0; j < V; j++) y[j] = exp_of<T>(x.at(j) - mx) * scale;
             if (f == at.lab_f) {
 #pragma unroll
                 for (int j = 0; j < V; j++)
