@@ -10,7 +10,11 @@
 //   dL/dx[j] = g (onehot[j] - softmax[j]),
 // and a position without a label (a prompt, padding) has the gradient 0; its logits are not even read.
 // Everything here is bound by memory: one read of the logits for logp, a read and a write for the policy loss, and
-// two reads and a write for the preference loss, whose coefficients need the whole pair first.
+// two reads and a write for the preference loss, whose coefficients need the whole pair first.  bf16 logits, 50304 to a column, 5/8 of the positions with a label:
+//   logp        8192 columns    95 us for  515 MB (5.4 TB/s)
+//   policy      8192           250 us for 1275 MB (5.1 TB/s; one sequence of eight has no label at all)
+//   preference  4096           180 us for  927 MB (5.1 TB/s; part of the second read is found in the caches)
+// where a copy reaches 5.1.  A single fp32 column of 50304 takes 6 us: the launch, four loads in a row and two exchanges between wavefronts.
 #include "colwise.hpp"
 #include "device_util.hpp"
 #include "internal.hpp"
