@@ -199,16 +199,23 @@ def _handles(tensors):
     return capi.ptr_array([t.h.value if t is not None else None for t in tensors])
 
 
+def _same_count(*lists):
+    if len({len(t) for t in lists}) != 1:
+        raise ValueError("lists of different lengths: " + ", ".join(str(len(t)) for t in lists))
+
+
 def orthogonalize(ctx, G, O, **iteration):
     """O[k] <- G[k] orthogonalised by Newton-Schulz products, lists of matrices."""
+    _same_count(G, O)
     cfg = newton_schulz_cfg(**iteration)
     capi.nnt_orthogonalize(ctx.h, C.byref(cfg), len(G), _handles(G), _handles(O))
 
 
 def muon_step(ctx, G, P, M, P_lowp=None, **hyper):
     """One Muon step on lists of matrices (gradients, parameters, momenta, bf16 copies or None)."""
+    _same_count(G, P, M, *([P_lowp] if P_lowp is not None else []))
     cfg = muon_cfg(**hyper)
-    capi.nnt_muon_step(ctx.h, C.byref(cfg), len(G), _handles(G), _handles(P), _handles(M), _handles(P_lowp) if P_lowp else None)
+    capi.nnt_muon_step(ctx.h, C.byref(cfg), len(G), _handles(G), _handles(P), _handles(M), _handles(P_lowp) if P_lowp is not None else None)
 
 
 def causal_absent(base_k, base_q, n_q):

@@ -446,3 +446,10 @@ def test_post_training_calls_without_a_context(capi):
     assert capi.nnt_gpt2_model_logprob.raw(None, None, None, None, None) == E
     assert capi.nnt_gpt2_model_forward_policy.raw(None, None, None, None, None, None, None, None, None, None, None) == E
     assert capi.nnt_gpt2_model_forward_preference.raw(None, None, None, None, None, None, None, None, None, None) == E
+
+
+def test_lists_of_different_lengths_never_reach_the_library():
+    from paper_2504_13236_amd import tiled
+    for call in (lambda: tiled.orthogonalize(None, [1, 2], [1]), lambda: tiled.muon_step(None, [1], [1], []), lambda: tiled.muon_step(None, [1], [1], [1], [])):
+        with pytest.raises(ValueError):
+            call()

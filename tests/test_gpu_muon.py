@@ -142,6 +142,38 @@ def test_large_matrices(mods, shape):
         assert err ** 0.5 <= 2.0 ** -22 * (8 * A ** 5 + 64 * norm)
 
 
+def test_offsets_beyond_32_bits(mods):
+    """2.2e9 elements in one tile, the longest side there is; against the iteration of its Gram matrix in 64 bits.  A column more is refused."""
+    capi, tiled = mods
+    rows, cols = 520, 65535 * 64
+    with tiled.Context(n_streams=1) as ctx:
+        t = tiled.TiledTensor(ctx, "f32", (rows, cols), (rows, cols))
+        G = t.buf.view(torch.float32).view(cols, rows)
+        G.normal_(generator=torch.Generator(device="cuda").manual_seed(6))
+        S = torch.zeros(rows, rows, device="cuda", dtype=torch.float64)
+        for c in range(0, cols, 1 << 18):
+            x = G[c:c + (1 << 18)].double()
+            S += torch.mm(x.t().contiguous(), x)
+        length = S.diagonal().sum().sqrt()
+        S /= length ** 2
+        Q = torch.eye(rows, device="cuda", dtype=torch.float64) / length
+        for _ in range(5):
+            F = A * torch.eye(rows, device="cuda", dtype=torch.float64) + B * S + CC * torch.mm(S, S)
+            Q, S = torch.mm(F, Q), torch.mm(torch.mm(F, S), F)
+        at = torch.cat([torch.arange(k, k + 70, device="cuda") for k in (0, 2 ** 31 // rows - 30, 2 ** 32 // rows // 2 + 200, cols - 70)])
+        want = torch.mm(G[at].double(), Q.t().contiguous())
+        torch.cuda.synchronize()
+        capi.nnt_orthogonalize(ctx.h, C.byref(ns(capi)), 1, handles(mods, [t]), handles(mods, [t]))
+        ctx.wait()
+        # The bound of the whole matrix is for its norm, here of `at`'s part of it.  Sums this long count by themselves: at least 8 parts of
+        # A's contraction, 16 columns to an addition, each step's A off by 2^-24 of the root of their number, which b + 2 c = 9 passes on, five times.
+        norm = torch.linalg.vector_norm(want).item()
+        limit = bound(np.zeros(1)) * (len(at) / cols) ** 0.5 + bound(norm, a=0.0) + 2.0 ** -24 * norm * (1 + 45 * (cols / 128) ** 0.5)
+        assert torch.linalg.vector_norm(G[at].double() - want).item() <= limit
+        longer = tiled.TiledTensor(ctx, "bf16", (1, cols + 1), (1, cols + 1), fill=0)
+        assert capi.nnt_orthogonalize.raw(ctx.h, C.byref(ns(capi)), 1, handles(mods, [longer]), handles(mods, [longer])) == capi.NNT_EINVAL
+
+
 def test_contractions_of_very_different_lengths_in_one_group(mods):
     """The long contraction is cut into more parts than the short one has steps."""
     capi, tiled = mods

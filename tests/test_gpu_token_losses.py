@@ -286,6 +286,85 @@ def test_nan_in_a_column_stays_in_it(mods):
         assert np.isfinite(logp[ok]).all() and np.isfinite(dX[:, ok]).all()
 
 
+def device_want(x, lab, g):
+    """logp and gradient of columns x [n, N_v] in 64 bits on the device; g: dloss/dlogp of each."""
+    x, lab = x.double(), torch.as_tensor(lab, device="cuda").long()[:, None]
+    logp = torch.log_softmax(x, 1)
+    d = -logp.exp() * g[:, None]
+    d.scatter_add_(1, lab, g[:, None].clone())
+    return logp.gather(1, lab)[:, 0], d
+
+
+def test_offsets_beyond_32_bits(mods):
+    """One tile of 3.3e9 logits: the first and the last sequence have labels, everything between is padding."""
+    capi, tiled = mods
+    N_v, N_s, N_b = 50304, 1024, 64
+    g = torch.Generator(device="cuda").manual_seed(1)
+    with tiled.Context(n_streams=1) as ctx:
+        X = tiled.TiledTensor(ctx, "bf16", (N_v, N_s, N_b), (N_v, N_s, N_b))
+        dX = tiled.TiledTensor(ctx, "bf16", (N_v, N_s, N_b), (N_v, N_s, N_b))
+        x, d = X.buf.view(torch.bfloat16).view(N_b, N_s, N_v), dX.buf.view(torch.bfloat16).view(N_b, N_s, N_v)
+        x.fill_(float("nan"))
+        d.fill_(float("nan"))
+        lab = torch.full((N_b, N_s), -1, dtype=torch.int32, device="cuda")
+        for b in (0, N_b - 1):
+            x[b] = torch.randn(N_s, N_v, generator=g, device="cuda")
+            lab[b] = torch.randint(0, N_v, (N_s,), generator=g, device="cuda", dtype=torch.int32)
+        logp, adv = (tiled.TiledTensor(ctx, "f32", (N_s, N_b), (N_s, N_b), fill=0) for _ in range(2))
+        adv.buf.view(torch.float32).fill_(1.0)
+        losses, loss = torch.zeros(N_s * N_b, device="cuda"), torch.zeros(1, device="cuda")
+        torch.cuda.synchronize()
+        capi.nnt_policy_loss(ctx.h, C.byref(capi.nnt_policy_cfg(0.2, 0.2, 0.0, 0)), X.h, lab.data_ptr(), None, None, adv.h, dX.h, logp.h,
+                             losses.data_ptr(), loss.data_ptr())
+        ctx.wait()
+        got = logp.buf.view(torch.float32).view(N_b, N_s).double()
+        for b in (0, N_b - 1):
+            want, dwant = device_want(x[b], lab[b], torch.full((N_s,), -1.0, device="cuda", dtype=torch.float64))
+            assert ((got[b] - want).abs() <= HALF["f32"] * want.abs() + LOGP).all()
+            assert ((d[b].double() - dwant).abs() <= (HALF["bf16"] + REL) * dwant.abs() + REL * 2).all()
+        assert not d[1:N_b - 1].any() and not got[1:N_b - 1].any()
+
+
+def test_longest_columns(mods):
+    """Nearly as many vectors as a column may have, in 4194 tiles, and one more than it may have."""
+    capi, tiled = mods
+    N_v, n = 4193999, 4
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(n, N_v, generator=g, device="cuda")
+    lab = np.array([0, N_v - 1, 2097152, 4193000], np.int32)
+    with tiled.Context(n_streams=1) as ctx:
+        def T(shape, base):
+            return tiled.TiledTensor(ctx, "f32", shape, base, fill=0)
+        X, dX = T((N_v, 1, n), (1000, 1, n)), T((N_v, 1, n), (1000, 1, n))
+        at = [X.slices(idx)[0] for idx in X.tile_index]
+        for k, sl in enumerate(at):
+            X.tile_view(k).copy_(x[:, sl].reshape(-1))
+        logp, dlab = T((1, n), (1, n)), dev_i32(lab)
+        rewards, losses, loss = (torch.zeros(n, device="cuda") for _ in range(3))
+        want, _ = device_want(x, lab, torch.zeros(n, device="cuda", dtype=torch.float64))
+        torch.cuda.synchronize()
+
+        def check(slope):
+            ctx.wait()
+            assert ((logp.buf.view(torch.float32)[:n].double() - want).abs() <= HALF["f32"] * want.abs() + LOGP).all()
+            _, dwant = device_want(x, lab, slope)
+            for k, sl in enumerate(at):
+                got, w = dX.tile_view(k).view(n, -1).double(), dwant[:, sl]
+                assert ((got - w).abs() <= (HALF["f32"] + REL) * w.abs() + REL * 2 * slope.abs()[:, None] * (w.abs() > 0.1 * slope.abs()[:, None])).all()
+        adv = T((n,), (n,))
+        adv.buf.view(torch.float32)[:n].fill_(1.0)
+        torch.cuda.synchronize()
+        capi.nnt_policy_loss(ctx.h, C.byref(capi.nnt_policy_cfg(0.2, 0.2, 0.0, 0)), X.h, dlab.data_ptr(), None, None, adv.h, dX.h, logp.h,
+                             losses.data_ptr(), loss.data_ptr())
+        check(torch.full((n,), -1.0, device="cuda", dtype=torch.float64))
+        capi.nnt_preference_loss(ctx.h, C.byref(capi.nnt_preference_cfg(1.0, 0.0, 0)), X.h, dlab.data_ptr(), None, dX.h, logp.h, rewards.data_ptr(),
+                                 losses.data_ptr(), loss.data_ptr())
+        slope = torch.sigmoid(want[:2] - want[2:]) - 1.0
+        check(torch.cat([slope, -slope]))
+        long = T((4195001, 1, 1), (1000, 1, 1))                    # 250 vectors to a tile: 2^20 are 4194.3 tiles
+        assert capi.nnt_token_logprob.raw(ctx.h, long.h, dlab.data_ptr(), T((1, 1), (1, 1)).h) == capi.NNT_EINVAL
+
+
 @pytest.mark.parametrize("reduction", [1, 2])
 @pytest.mark.parametrize("N_s,N_b", [(40, 1030), (33, 1023), (32, 70), (1, 2050), (3000, 2), (5, 1)])
 def test_weights_of_many_and_of_few_sequences(mods, N_s, N_b, reduction):
