@@ -22,6 +22,7 @@
 #include "internal.hpp"
 #include "raw_vec.hpp"
 
+#include <algorithm>
 #include <cmath>
 
 namespace nnt {
@@ -186,8 +187,10 @@ __device__ __forceinline__ int matrix_of(const NsSizes& g, int& wg) {
     return k;
 }
 
-// hi and lo part of a value of the workspace's scale
+// hi and lo part of a value of the workspace's scale.  The value is made definite first: as the result of a product the compiler rounds it straight
+// to fp16 in one place and by way of fp32 in another, and where the two differ, one value in some ten thousand, hi + lo is off by 2^-11.
 __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
+    asm("" : "+v"(v));
     hi = (_Float16)v;
     lo = (_Float16)(v - (float)hi);
 }
@@ -752,6 +755,63 @@ __device__ __forceinline__ void multiply(const char* image, int r0, const char* 
     }, acc);
 }
 
+// A lane's results of a block of 64 x 64: rows i + 8 p + 0 .. 3, column j.
+// A symmetric block as an image: four rows of a column are four columns of a row.
+__device__ __forceinline__ void store_symmetric(char* dst, const float (&x)[4][4], int i, int j) {
+#pragma unroll
+    for (int p = 0; p < 4; p++) {
+        f16x4 hi, lo;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            _Float16 h, l;
+            split(x[p][k], h, l);
+            hi[k] = h;
+            lo[k] = l;
+        }
+        char* d = dst + image_at(j, i + p * 8);
+        *reinterpret_cast<f16x4*>(d) = hi;
+        *reinterpret_cast<f16x4*>(d + kPartBytes) = lo;
+    }
+}
+// X's block as its transpose, and as it is.
+__device__ __forceinline__ void store_both(char* XT, char* X, const float (&x)[4][4], int i, int j) {
+#pragma unroll
+    for (int p = 0; p < 4; p++) {
+        f16x4 hi, lo;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            _Float16 h, l;
+            split(x[p][k], h, l);
+            hi[k] = h;
+            lo[k] = l;
+            char* d = X + image_at(i + p * 8 + k, j);
+            *reinterpret_cast<_Float16*>(d) = h;
+            *reinterpret_cast<_Float16*>(d + kPartBytes) = l;
+        }
+        char* d = XT + image_at(j, i + p * 8);
+        *reinterpret_cast<f16x4*>(d) = hi;
+        *reinterpret_cast<f16x4*>(d + kPartBytes) = lo;
+    }
+}
+// a X + B X of X's block, X as its transpose
+__device__ __forceinline__ void step_block(const char* B, const char* XT, int wr, int wc, int i, int j, float a, float (&x)[4][4]) {
+    f16x4 eh[4], el[4];
+#pragma unroll
+    for (int p = 0; p < 4; p++) {
+        const char* e = XT + image_at(j, i + p * 8);
+        eh[p] = *reinterpret_cast<const f16x4*>(e);
+        el[p] = *reinterpret_cast<const f16x4*>(e + kPartBytes);
+    }
+    f32x16 acc;
+#pragma unroll
+    for (int k = 0; k < 16; k++) acc[k] = 0.f;
+    multiply(B, wr * 32, XT, wc * 32, acc);
+#pragma unroll
+    for (int p = 0; p < 4; p++)
+#pragma unroll
+        for (int k = 0; k < 4; k++) x[p][k] = fmaf(a, (float)eh[p][k] + (float)el[p][k], acc[p * 4 + k] / kScale);
+}
+
 template <int PHASE>
 __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restrict__ group, NsSizes sizes, int now) {
     const NsGroup& g = *group;
@@ -789,24 +849,7 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
                 t[v].w += u.w;
             }
         }
-        // (A and B are symmetric: a lane's four rows of a column are four columns of a row)
         float a[4][4];
-        auto store = [&](char* dst, const float (&x)[4][4]) {
-#pragma unroll
-            for (int p = 0; p < 4; p++) {
-                f16x4 hi, lo;
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    _Float16 h, l;
-                    split(x[p][k], h, l);
-                    hi[k] = h;
-                    lo[k] = l;
-                }
-                char* d = dst + image_at(j, i + p * 8);
-                *reinterpret_cast<f16x4*>(d) = hi;
-                *reinterpret_cast<f16x4*>(d + kPartBytes) = lo;
-            }
-        };
 #pragma unroll
         for (int p = 0; p < 4; p++) {
             a[p][0] = t[p].x / kScale;
@@ -814,7 +857,7 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
             a[p][2] = t[p].z / kScale;
             a[p][3] = t[p].w / kScale;
         }
-        store(image[0], a);
+        store_symmetric(image[0], a, i, j);
         __syncthreads();
         f32x16 acc;
 #pragma unroll
@@ -824,7 +867,7 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
         for (int p = 0; p < 4; p++)
 #pragma unroll
             for (int k = 0; k < 4; k++) a[p][k] = fmaf(g.b, a[p][k], acc[p * 4 + k] * (g.c / kScale));
-        store(image[1], a);
+        store_symmetric(image[1], a, i, j);
         __syncthreads();
     }
     f32x16 gram;
@@ -872,22 +915,8 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
                 *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
             }
         } else {
-            f16x4 eh[4], el[4];
-#pragma unroll
-            for (int p = 0; p < 4; p++) {
-                const char* e = X + image_at(j, i + p * 8);
-                eh[p] = *reinterpret_cast<const f16x4*>(e);
-                el[p] = *reinterpret_cast<const f16x4*>(e + kPartBytes);
-            }
-            f32x16 acc;
-#pragma unroll
-            for (int k = 0; k < 16; k++) acc[k] = 0.f;
-            multiply(image[1], wr * 32, X, wc * 32, acc);
             float x[4][4];
-#pragma unroll
-            for (int p = 0; p < 4; p++)
-#pragma unroll
-                for (int k = 0; k < 4; k++) x[p][k] = fmaf(g.a, (float)eh[p][k] + (float)el[p][k], acc[p * 4 + k] / kScale);
+            step_block(image[1], X, wr, wc, i, j, g.a, x);
             if constexpr (PHASE == kFinal) {
 #pragma unroll
                 for (int p = 0; p < 4; p++)
@@ -897,23 +926,7 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
                 continue;
             }
             __syncthreads();                             // everybody has read X's block, which is overwritten, and is done with the last one's image
-#pragma unroll
-            for (int p = 0; p < 4; p++) {
-                f16x4 hi, lo;
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    _Float16 h, l;
-                    split(x[p][k], h, l);
-                    hi[k] = h;
-                    lo[k] = l;
-                    char* d = image[2] + image_at(i + p * 8 + k, j);
-                    *reinterpret_cast<_Float16*>(d) = h;
-                    *reinterpret_cast<_Float16*>(d + kPartBytes) = l;
-                }
-                char* d = X + image_at(j, i + p * 8);
-                *reinterpret_cast<f16x4*>(d) = hi;
-                *reinterpret_cast<f16x4*>(d + kPartBytes) = lo;
-            }
+            store_both(X, image[2], x, i, j);
         }
         __syncthreads();
         multiply(image[2], wr * 32, image[2], wc * 32, gram);
@@ -923,6 +936,138 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
         const int next = PHASE == kFirst ? now : 1 - now;
 #pragma unroll
         for (int v = 0; v < 4; v++) sums[sum_at(next, part, v)] = make_float4(gram[4 * v], gram[4 * v + 1], gram[4 * v + 2], gram[4 * v + 3]);
+    }
+}
+
+// ---------------------------------------------------------------- matrices of at most 64 x 256
+// One workgroup holds all of X in LDS and does everything in one launch: momentum, norm, the steps, the results.  Four wavefronts to a column block of 64; the first four
+// put A together and compute B for all.  A step takes MEASURE us.
+constexpr int kHeldBlocks = 4;
+
+// the momentum's way back to where read_columns found it
+__device__ __forceinline__ void write_columns(const NsMatrix& q, void* const* tiles, bool there, int t0, int o0, int e0, int c0, const float (&v)[16]) {
+    int t1 = c0 / q.base1, c1 = c0 - t1 * q.base1;
+#pragma unroll
+    for (int s = 0; s < 16; s++) {
+        if (there && c0 + s < q.cols) global_as<float>(tiles[t0 + q.grid0 * t1])[o0 + (int64_t)e0 * c1] = v[s];
+        if (++c1 == q.base1) {
+            c1 = 0;
+            t1++;
+        }
+    }
+}
+
+__global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, int steps) {
+    __shared__ __align__(16) char images[2 * kHeldBlocks + 1][kImage];       // X's transpose and X by block; A, then B
+    __shared__ double red[4 * kHeldBlocks];
+    const NsMatrix& q = g.mat[blockIdx.x];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane((tid >> 6) & 3), t = __builtin_amdgcn_readfirstlane(tid >> 8);
+    const int wr = wave & 1, wc = wave >> 1, nt = q.np >> 6;
+    const int i = wr * 32 + (lane >> 5) * 4, j = wc * 32 + (lane & 31);
+    const bool mine = t < nt;                            // (the launch has as many wavefronts as its longest matrix wants)
+    char *XT = images[t], *X = images[kHeldBlocks + t], *S = images[2 * kHeldBlocks];
+    {
+        const int r0 = q.flip ? t * 64 : 0, c0 = (q.flip ? 0 : t * 64) + wave * 16;
+        const int r = r0 + lane, t0 = min(r, q.rows - 1) / q.base0, o0 = r - t0 * q.base0, e0 = min(q.base0, q.rows - t0 * q.base0);
+        const bool there = mine && r < q.rows;
+        float u[16];
+        read_columns(q, q.G, there, t0, o0, e0, c0, u);
+        if (g.mu >= 0.f) {
+            float m[16];
+            read_columns(q, q.M, there, t0, o0, e0, c0, m);
+#pragma unroll
+            for (int s = 0; s < 16; s++) {
+                m[s] = fmaf(g.mu, m[s], u[s]);
+                u[s] = g.nesterov ? fmaf(g.mu, m[s], u[s]) : m[s];
+            }
+            write_columns(q, q.M.tiles, there, t0, o0, e0, c0, m);
+        }
+        double sum = 0.0;
+#pragma unroll
+        for (int s = 0; s < 16; s++) sum += (double)u[s] * (double)u[s];
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        if (lane == 0) red[tid >> 6] = sum;
+        __syncthreads();
+        sum = 0.0;
+        for (int w = 0; w < 4 * nt; w++) sum += red[w];
+        const Scale scaled(sqrt(sum) + g.eps);
+        if (mine) {
+            // a lane has a row of X and 16 columns of it, or (X the transpose) a column and 16 rows
+            char *along = q.flip ? XT : X, *across = q.flip ? X : XT;
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                f16x8 hi, lo;
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    _Float16 y, z;
+                    split(scaled(u[h * 8 + e]), y, z);
+                    hi[e] = y;
+                    lo[e] = z;
+                    char* d = across + image_at(wave * 16 + h * 8 + e, lane);
+                    *reinterpret_cast<_Float16*>(d) = y;
+                    *reinterpret_cast<_Float16*>(d + kPartBytes) = z;
+                }
+                char* d = along + image_at(lane, wave * 16 + h * 8);
+                *reinterpret_cast<f16x8*>(d) = hi;
+                *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
+            }
+        }
+    }
+    for (int step = 0;; step++) {
+        __syncthreads();
+        f32x16 acc;
+#pragma unroll
+        for (int k = 0; k < 16; k++) acc[k] = 0.f;
+        if (mine) multiply(X, wr * 32, X, wc * 32, acc);
+        __syncthreads();                                 // X's image has been read: the blocks' parts of A take its place
+        auto part_at = [&](int block, int v) { return reinterpret_cast<float4*>(images[kHeldBlocks + block]) + (wave * 4 + v) * 64 + lane; };
+        if (mine && t > 0)
+#pragma unroll
+            for (int v = 0; v < 4; v++) *part_at(t, v) = make_float4(acc[4 * v], acc[4 * v + 1], acc[4 * v + 2], acc[4 * v + 3]);
+        __syncthreads();
+        float a[4][4];
+        if (t == 0) {
+            for (int b = 1; b < nt; b++)
+#pragma unroll
+                for (int v = 0; v < 4; v++) {
+                    const float4 y = *part_at(b, v);
+                    acc[4 * v] += y.x;
+                    acc[4 * v + 1] += y.y;
+                    acc[4 * v + 2] += y.z;
+                    acc[4 * v + 3] += y.w;
+                }
+#pragma unroll
+            for (int p = 0; p < 4; p++)
+#pragma unroll
+                for (int k = 0; k < 4; k++) a[p][k] = acc[p * 4 + k] / kScale;
+            store_symmetric(S, a, i, j);
+        }
+        __syncthreads();
+        if (t == 0) {
+#pragma unroll
+            for (int k = 0; k < 16; k++) acc[k] = 0.f;
+            multiply(S, wr * 32, S, wc * 32, acc);
+#pragma unroll
+            for (int p = 0; p < 4; p++)
+#pragma unroll
+                for (int k = 0; k < 4; k++) a[p][k] = fmaf(g.b, a[p][k], acc[p * 4 + k] * (g.c / kScale));
+        }
+        __syncthreads();                                 // A has been read
+        if (t == 0) store_symmetric(S, a, i, j);
+        __syncthreads();
+        float x[4][4];
+        if (mine) step_block(S, XT, wr, wc, i, j, g.a, x);
+        if (step + 1 == steps) {
+#pragma unroll
+            for (int p = 0; p < 4; p++)
+#pragma unroll
+                for (int k = 0; k < 4; k++) x[p][k] *= 1.f / kScale;
+            if (mine) apply_results(q, x, i, t * 64 + j);
+            return;
+        }
+        __syncthreads();                                 // X's transpose has been read
+        if (mine) store_both(XT, X, x, i, j);
     }
 }
 
@@ -1089,11 +1234,15 @@ Launch choose(const NsSizes& g, int mode) {
     return best;
 }
 
+// How a matrix is worked on.
+enum { kProducts, kNarrow, kHeld };
+int kind_of(int64_t m, int64_t l) { return m > 64 || l > 64 * kNarrowBlocks ? kProducts : l > 64 * kHeldBlocks ? kNarrow : kHeld; }
+
 // One set of launches: as many matrices as it takes to fill the chip.
 struct Set {
     NsGroup g{};
     NsSizes sizes{};
-    bool narrow = false;
+    int kind = 0;                        // kProducts, kNarrow, kHeld
     Launch launch[4];                    // by mode
     std::vector<Item> items;
     int parts = 0;
@@ -1103,7 +1252,7 @@ struct Set {
 };
 
 // Puts tasks from number *first on into a set.
-int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& cfg, float mu, int nesterov, const std::vector<Task>& tasks, bool narrow, size_t* first, Set* out) {
+int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& cfg, float mu, int nesterov, const std::vector<Task>& tasks, int kind, size_t* first, Set* out) {
     Set& w = *out;
     NsGroup& g = w.g;
     g.nesterov = nesterov;
@@ -1112,10 +1261,16 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
     g.b = (float)cfg.b;
     g.c = (float)cfg.c;
     g.eps = cfg.eps;
-    w.narrow = narrow;
+    const bool narrow = kind == kNarrow;
+    w.kind = kind;
     int64_t bytes = (sizeof(NsGroup) + 255) / 256 * 256, chunks = 0;
+    std::vector<const nnt_tensor*> taken;                // inputs of this set
     while (*first < tasks.size() && g.n < kGroupMatrices && w.patch < 4096) {
-        const Task& t = tasks[(*first)++];
+        const Task& t = tasks[*first];
+        // (a workgroup that holds its matrix does not wait for the others to have read theirs)
+        if (kind == kHeld && std::any_of(taken.begin(), taken.end(), [&](const nnt_tensor* G) { return G == t.P; })) break;
+        taken.push_back(t.G);
+        ++*first;
         const int64_t rows = t.G->shape[0], cols = t.G->shape[1], m = std::min(rows, cols), l = std::max(rows, cols);
         const int64_t mb = (m + 63) / 64, nb = (l + 63) / 64;
         if (nb > 0xffff || mb * nb > (1 << 24)) return fail(ctx, NNT_EINVAL, std::string(label) + ": matrix too large");
@@ -1131,7 +1286,7 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
         q.mp = (int32_t)(mb * 64);
         q.np = (int32_t)(nb * 64);
         w.patch += mb * nb;
-        if (narrow) w.parts = std::max(w.parts, narrow_parts((int)nb));
+        if (kind != kProducts) w.parts = std::max(w.parts, narrow ? narrow_parts((int)nb) : (int)nb);
         chunks = std::max(chunks, (t.G->base[0] * t.G->base[1] + kNormChunk - 1) / kNormChunk * t.G->grid[0] * t.G->grid[1]);
         // X and its transpose, two buffers each, and four square ones; narrow matrices: the transpose once, and two times A in parts
         const int64_t x = (int64_t)q.mp * q.np * 4, a = (int64_t)q.mp * q.mp * 4;
@@ -1152,11 +1307,12 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
         if (t.M) w.acc.push_back(t.M->all(kReadWrite));
         if (t.LP) w.acc.push_back(t.LP->all(kWrite));
     }
+    w.sizes.n = g.n;
+    if (kind == kHeld) return NNT_OK;                    // (needs no workspace)
     w.acc.push_back(Access{&ctx->matrix_dep, 1, kReadWrite});
     g.norm_blocks = (int32_t)std::min<int64_t>(chunks, kNormBlocks);
-    w.sizes.n = g.n;
     g.partial = bytes;
-    if (!narrow) {
+    if (kind == kProducts) {
         for (int mode : {(int)kGram, (int)kPoly, (int)kStep, (int)kLast}) w.launch[mode] = choose(w.sizes, mode);
         const Launch& gram = w.launch[kGram];
         if (gram.splits > 1) bytes += (int64_t)gram.tiles * gram.splits * (gram.shape == 0 ? Small::BM * Small::BM : Middle::BM * Middle::BM) * 4;
@@ -1172,9 +1328,14 @@ int32_t submit_set(nnt_ctx* ctx, const char* label, int steps, const Set& w) {
     g.space = reinterpret_cast<char*>(ctx->matrix_scratch);
     const NsGroup* there = reinterpret_cast<const NsGroup*>(g.space);
     OpTag tag(ctx, label, w.work, false);
+    if (w.kind == kHeld)
+        return submit(ctx, w.acc, [&](hipStream_t st) {
+            hipLaunchKernelGGL(ns_held_kernel, dim3((unsigned)g.n), dim3(256u * w.parts), 0, st, g, steps);
+            return launched();
+        });
     return submit(ctx, w.acc, [&](hipStream_t st) {
         hipLaunchKernelGGL(ns_norm_kernel, dim3((unsigned)g.norm_blocks, (unsigned)g.n), dim3(1024), 0, st, g);
-        if (w.narrow) {
+        if (w.kind == kNarrow) {
             const dim3 grid((unsigned)w.parts, (unsigned)g.n), block(256);
             hipLaunchKernelGGL((ns_narrow_kernel<kFirst>), grid, block, 0, st, there, w.sizes, 0);
             for (int s = 0; s + 1 < steps; s++) hipLaunchKernelGGL((ns_narrow_kernel<kMiddle>), grid, block, 0, st, there, w.sizes, s & 1);
@@ -1189,22 +1350,22 @@ int32_t submit_set(nnt_ctx* ctx, const char* label, int steps, const Set& w) {
             else launch_product<Small>(t.mode, there, w.sizes, t.op, t.now, l.tiles, l.splits, st);
         }
         return launched();
-    }, w.narrow ? 2 + steps : 2 + (int)w.items.size() + (w.launch[kGram].splits > 1 ? steps : 0));
+    }, w.kind == kNarrow ? 2 + steps : 2 + (int)w.items.size() + (w.launch[kGram].splits > 1 ? steps : 0));
 }
 
 // Orthogonalises the matrices of `tasks` and applies the results.  mu < 0: no momentum.  Nothing is launched before all sets are known to fit.
 int32_t newton_schulz(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& cfg, float mu, int nesterov, const std::vector<Task>& tasks) {
-    std::vector<Task> kind[2];
+    std::vector<Task> kind[3];
     for (const Task& t : tasks) {
         const int64_t m = std::min(t.G->shape[0], t.G->shape[1]), l = std::max(t.G->shape[0], t.G->shape[1]);
-        kind[m <= 64 && l <= 64 * kNarrowBlocks].push_back(t);
+        kind[kind_of(m, l)].push_back(t);
     }
     std::vector<Set> sets;
     int64_t bytes = 0;
-    for (int narrow = 0; narrow < 2; narrow++)
-        for (size_t first = 0; first < kind[narrow].size();) {
+    for (int k = 0; k < 3; k++)
+        for (size_t first = 0; first < kind[k].size();) {
             sets.emplace_back();
-            const int32_t rc = make_set(ctx, label, cfg, mu, nesterov, kind[narrow], narrow != 0, &first, &sets.back());
+            const int32_t rc = make_set(ctx, label, cfg, mu, nesterov, kind[k], k, &first, &sets.back());
             if (rc != NNT_OK) return rc;
             bytes = std::max(bytes, sets.back().bytes);
         }

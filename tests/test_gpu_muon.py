@@ -280,6 +280,22 @@ def test_many_matrices(mods, shape, count):
             np.testing.assert_array_equal(o.download(), first)
 
 
+@pytest.mark.parametrize("shape", [(64, 256), (60, 500), (200, 300)])
+def test_results_in_the_place_of_earlier_inputs(mods, shape):
+    """O[k] = G[k - 1], eleven in a row: every input is read before its place is taken."""
+    capi, tiled = mods
+    n = 12
+    G = [gradient(np.random.default_rng(k), *shape) for k in range(n)]
+    with tiled.Context(n_streams=4) as ctx:
+        t = [tiled.TiledTensor.from_numpy(ctx, g, (33, 256)) for g in G]
+        t.append(tiled.TiledTensor(ctx, "f32", shape, (33, 256)))
+        # G: 0 .. n-1; O: n, 0, 1, ...
+        capi.nnt_orthogonalize(ctx.h, C.byref(ns(capi)), n, handles(mods, t[:n]), handles(mods, [t[n]] + t[:n - 1]))
+        for k in range(n):
+            want = D.orthogonalize(G[k])
+            assert np.linalg.norm((t[n] if k == 0 else t[k - 1]).download() - want) <= bound(want) + 2.0 ** -24 * np.linalg.norm(want)
+
+
 def test_matrices_after_tasks_that_make_them(mods):
     """The step waits for the product that writes the gradient, and what reads the parameter waits for the step, on any streams."""
     capi, tiled = mods
