@@ -720,8 +720,8 @@ __global__ void __launch_bounds__(256) ns_combine_kernel(const NsGroup* __restri
 // ---------------------------------------------------------------- matrices with a side of at most 64
 // Here a launch is longer than what it computes, so a whole iteration is one launch.  A workgroup holds some of X's column blocks of 64; it adds up the
 // parts of A that the workgroups have left (its own and the others'), computes B (64 x 64, every workgroup the same), its blocks of X and their
-// part of the next A.  X is kept as its transpose only.  The first launch takes U in place of B X, the last one leaves the results.  Four matrices of
-// 64 to 256 x 64: 6 us a launch, 42 in all (30 more with the products above); it is the launches that bound it, and within one the parts' way through memory.
+// part of the next A.  X is kept as its transpose only.  The first launch takes U in place of B X, the last one leaves the results.  64 x 320: 6 us a
+// launch, 43 in all (some 75 with the products above); it is the launches that bound it, and within one the parts' way through memory.
 enum { kFirst, kMiddle, kFinal };
 
 // how many workgroups share a matrix of nt column blocks: each adds up as many parts (0.2 us) as there are, and takes nt / parts blocks (1.5 us) in turn
@@ -941,7 +941,9 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
 
 // ---------------------------------------------------------------- matrices of at most 64 x 256
 // One workgroup holds all of X in LDS and does everything in one launch: momentum, norm, the steps, the results.  Four wavefronts to a column block of 64; the first four
-// put A together and compute B for all.  A step takes MEASURE us.
+// put A together and compute B for all.  64 x 64 22 us (33 with a launch per step), 64 x 256 43 (43), and the rest of the chip is free meanwhile: passes over the four
+// matrices of a block of 64 that need not wait for one another take 25 us each (42).  What bounds it is LDS, 3 us a step and 1.2 for each further block.  (X computed
+// twice, as its transpose too, in place of the two-byte writes: 40 us, but the two drift apart, errors a quarter larger.)
 constexpr int kHeldBlocks = 4;
 
 // the momentum's way back to where read_columns found it
