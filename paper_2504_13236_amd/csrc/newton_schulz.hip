@@ -1111,7 +1111,12 @@ bool in_range(const nnt_newton_schulz_cfg& c, double* reach = nullptr) {
     return true;
 }
 
-// Whether two steps can be taken at once: the workspace also has to hold P = a I + b A + c A^2 and P_1 P_0 - a^2 I then.
+// What is kept out of the factor P_1 P_0 of two steps at once, as a multiple of the identity: rounded among the factor's entries it would cost as much as the rest.  The first
+// steps find small singular values and a factor near a^2, the later ones values around 1 and a factor between 0.4 and some 10.  (a^2 for all of them: errors of
+// 1024 x 4096 4.5e-6 instead of 3.5e-6; nothing after the first: 3.9e-6.)
+double kept_out(const nnt_newton_schulz_cfg& c, bool first) { return first ? c.a * c.a : c.a * c.a / 4.0; }
+
+// Whether two steps can be taken at once: the workspace also has to hold P = a I + b A + c A^2 and what is left of P_1 P_0 then.
 bool pairs_in_range(const nnt_newton_schulz_cfg& c) {
     double low = c.a, high = c.a, reach = 1.0;
     if (!in_range(c, &reach)) return false;
@@ -1123,7 +1128,8 @@ bool pairs_in_range(const nnt_newton_schulz_cfg& c) {
             high = std::max(high, p);
         }
     double most = std::max(std::fabs(low), std::fabs(high));
-    for (double p : {low * low, low * high, high * high}) most = std::max(most, std::fabs(p - c.a * c.a));
+    for (double p : {low * low, low * high, high * high})
+        for (bool first : {true, false}) most = std::max(most, std::fabs(p - kept_out(c, first)));
     return most < 15.0;
 }
 
@@ -1180,14 +1186,14 @@ std::vector<Item> plan(const nnt_newton_schulz_cfg& c, bool pairs) {
         const bool two = pairs && left >= 2;
         out.push_back(Item{kGram, NsOp{}, now});
         if (two) {
-            // (the multiples of the identity are kept out of the factors where they can be: rounded among their entries they would cost as much as the rest)
+            const float out_of = (float)kept_out(c, left == c.steps);
             out.push_back(Item{kPoly, NsOp{0, 0, 0, 1, C, B, 0.f}, now});        // B_0 = P_0 - a I
             out.push_back(Item{kPoly, NsOp{1, 0, 0, 2, 1.f, A, 0.f}, now});      // P_0 A_0
             out.push_back(Item{kPoly, NsOp{1, 2, 2, 3, 1.f, A, 0.f}, now});      // A_1 = P_0 (P_0 A_0)
             out.push_back(Item{kPoly, NsOp{3, 3, 3, 2, C, B, A}, now});          // P_1
-            out.push_back(Item{kPoly, NsOp{2, 1, 2, 0, 1.f, A, -A * A}, now});   // P_1 P_0 - a^2 I
+            out.push_back(Item{kPoly, NsOp{2, 1, 2, 0, 1.f, A, -out_of}, now});  // P_1 P_0 without what is kept out
             left -= 2;
-            out.push_back(Item{left ? kStep : kLast, NsOp{0, 0, 0, 0, 1.f, A * A, 0.f}, now});
+            out.push_back(Item{left ? kStep : kLast, NsOp{0, 0, 0, 0, 1.f, out_of, 0.f}, now});
         } else {
             out.push_back(Item{kPoly, NsOp{0, 0, 0, 1, C, B, 0.f}, now});
             left--;
@@ -1265,7 +1271,7 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
     g.eps = cfg.eps;
     const bool narrow = kind == kNarrow;
     w.kind = kind;
-    int64_t bytes = (sizeof(NsGroup) + 255) / 256 * 256, chunks = 0;
+    int64_t bytes = (sizeof(NsGroup) + 255) / 256 * 256, chunks = 0, shortest = INT64_MAX;
     std::vector<const nnt_tensor*> taken;                // inputs of this set
     while (*first < tasks.size() && g.n < kGroupMatrices && w.patch < 4096) {
         const Task& t = tasks[*first];
@@ -1288,6 +1294,7 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
         q.mp = (int32_t)(mb * 64);
         q.np = (int32_t)(nb * 64);
         w.patch += mb * nb;
+        shortest = std::min(shortest, m);
         if (kind != kProducts) w.parts = std::max(w.parts, narrow ? narrow_parts((int)nb) : (int)nb);
         chunks = std::max(chunks, (t.G->base[0] * t.G->base[1] + kNormChunk - 1) / kNormChunk * t.G->grid[0] * t.G->grid[1]);
         // X and its transpose, two buffers each, and four square ones; narrow matrices: the transpose once, and two times A in parts
@@ -1318,8 +1325,9 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
         for (int mode : {(int)kGram, (int)kPoly, (int)kStep, (int)kLast}) w.launch[mode] = choose(w.sizes, mode);
         const Launch& gram = w.launch[kGram];
         if (gram.splits > 1) bytes += (int64_t)gram.tiles * gram.splits * (gram.shape == 0 ? Small::BM * Small::BM : Middle::BM * Middle::BM) * 4;
-        // (the model is a tenth and more off either way: two steps at once have to promise that much)
-        w.items = plan(cfg, pairs_in_range(cfg) && 1.15 * 3.0 * w.launch[kPoly].time < gram.time + w.launch[kStep].time);
+        // (The model is a tenth and more off either way: two steps at once have to promise that much.  Below 256 rows they gain less, 128 x 6272 120 us instead of 128, and
+        // their errors are larger than those of fp32 products, 128 x 1000 2.9e-6 after five steps instead of 1.7e-6.)
+        w.items = plan(cfg, shortest >= 256 && pairs_in_range(cfg) && 1.15 * 3.0 * w.launch[kPoly].time < gram.time + w.launch[kStep].time);
     }
     w.bytes = bytes;
     return NNT_OK;
