@@ -101,6 +101,25 @@ def test_iterations_of_narrow_and_of_long_matrices(mods, shape, steps, a, b, c):
         assert np.linalg.norm(tO.download() - want) <= bound(want, steps, a)
 
 
+@pytest.mark.parametrize("shape", [(64, 256), (256, 64), (64, 64), (60, 900), (200, 300), (300, 2000)])
+def test_every_entry_of_one_step(mods, shape):
+    """No entry is off by more than its own factors: 2^-20 (four times 2^-22) of a X and of the norms that B X is made of."""
+    capi, tiled = mods
+    for seed in range(3):
+        G = gradient(np.random.default_rng(seed), *shape)
+        want = D.orthogonalize(G, steps=1)
+        X = G.astype(np.float64) / np.linalg.norm(G.astype(np.float64))
+        X = X if shape[0] <= shape[1] else X.T
+        S = X @ X.T
+        limit = 2.0 ** -20 * (A * np.abs(X) + (abs(B) + CC) * np.linalg.norm(S, axis=1)[:, None] * np.linalg.norm(X, axis=0)[None, :])
+        limit = limit if shape[0] <= shape[1] else limit.T
+        with tiled.Context(n_streams=1) as ctx:
+            tG, tO = tiled.TiledTensor.from_numpy(ctx, G, (100, 256)), tiled.TiledTensor(ctx, "f32", shape, (100, 256))
+            capi.nnt_orthogonalize(ctx.h, C.byref(ns(capi, 1)), 1, handles(mods, [tG]), handles(mods, [tO]))
+            d = np.abs(tO.download() - want)
+            assert (d <= limit + 2.0 ** -24 * np.abs(want)).all(), (seed, (d / limit).max())
+
+
 def test_pairs_of_steps_stay_in_range(mods):
     """Coefficients that the iteration itself can take, but not the polynomial of two steps: those go one by one."""
     capi, tiled = mods
@@ -364,6 +383,45 @@ def test_captured_and_replayed(mods):
         held = ctx.stats()["device_workspace_bytes"]
         capi.nnt_graph_destroy(g)
         assert ctx.stats()["device_workspace_bytes"] < held
+
+
+def test_two_graphs_with_one_workspace(mods):
+    """Matrices of every kind in two graphs that share the workspace, replayed in turn with an eager call between."""
+    capi, tiled = mods
+    r = np.random.default_rng(9)
+    with tiled.Context(n_streams=4) as ctx:
+        def group():
+            G = [gradient(r, *s) for s in ((64, 64), (250, 60), (40, 300), (200, 300), (300, 1500))]
+            t = [tiled.TiledTensor.from_numpy(ctx, g, (100, 128)) for g in G]
+            o = [tiled.TiledTensor(ctx, "f32", g.shape, (100, 128)) for g in G]
+            return G, t, o
+
+        def go(t, o):
+            capi.nnt_orthogonalize(ctx.h, C.byref(ns(capi)), len(t), handles(mods, t), handles(mods, o))
+        groups, graphs, want = [group() for _ in range(3)], [], []
+        for G, t, o in groups:
+            go(t, o)
+            want.append([x.download() for x in o])
+            assert all(np.linalg.norm(w - D.orthogonalize(g)) <= bound(w) for w, g in zip(want[-1], G))
+        for _, t, o in groups[:2]:
+            g = C.c_void_p()
+            capi.nnt_capture_begin(ctx.h)
+            go(t, o)
+            capi.nnt_capture_end(ctx.h, C.byref(g))
+            graphs.append(g)
+        for _ in range(4):
+            for _, _, o in groups:
+                for x in o:
+                    x.buf.fill_(0x5a)
+            torch.cuda.synchronize()
+            capi.nnt_graph_launch(graphs[0])
+            go(*groups[2][1:])
+            capi.nnt_graph_launch(graphs[1])
+            for (_, _, o), ws in zip(groups, want):
+                for x, w in zip(o, ws):
+                    np.testing.assert_array_equal(x.download(), w)
+        for g in graphs:
+            capi.nnt_graph_destroy(g)
 
 
 def test_refusals(mods):
