@@ -337,13 +337,16 @@ int32_t ensure_stream_scratch(nnt_ctx* ctx, int64_t elems) {
 }
 
 // (Several GB for the largest matrices: a lack of memory is the caller's to deal with, not the end of the context.)
-int32_t ensure_matrix_scratch(nnt_ctx* ctx, int64_t bytes) {
+int32_t ensure_matrix_scratch(nnt_ctx* ctx, int64_t half, int64_t whole) {
     const int64_t have = ctx->matrix_mem ? ctx->matrix_mem->bytes : 0;
-    if (bytes <= have) return NNT_OK;
+    if (half <= ctx->matrix_half && whole <= have) return NNT_OK;
+    half = std::max((half + 0xfff) / 0x1000 * 0x1000, ctx->matrix_half);
+    const int64_t bytes = std::max({whole, half * std::min(ctx->n_streams, 2), have});
     if (ctx->capturing) return fail(ctx, NNT_ESTATE, "the workspace of matrix iterations must exist before capture: run the operation once first");
     const int32_t rc = sync_all(ctx);
     if (rc != NNT_OK) return rc;
     ctx->matrix_scratch = nullptr;
+    ctx->matrix_half = 0;
     replace_mem(ctx, &ctx->matrix_mem);
     std::shared_ptr<Scratch> fresh(new Scratch());
     fresh->bytes = (bytes + 0xfffff) / 0x100000 * 0x100000;
@@ -352,7 +355,8 @@ int32_t ensure_matrix_scratch(nnt_ctx* ctx, int64_t bytes) {
         (void)hipGetLastError();
         return fail(ctx, NNT_ENOMEM, "no memory for the workspace of matrix iterations: " + std::to_string(fresh->bytes) + " bytes");
     }
-    ctx->matrix_scratch = fresh->p;
+    ctx->matrix_scratch = reinterpret_cast<char*>(fresh->p);
+    ctx->matrix_half = half;
     ctx->matrix_mem = std::move(fresh);
     return NNT_OK;
 }

@@ -164,10 +164,12 @@ struct nnt_ctx {
     float* stream_scratch = nullptr;
     int64_t stream_scratch_elems = 0;        // per stream
     std::shared_ptr<nnt::Scratch> stream_mem;
-    // what the Newton-Schulz iterations of matrices work in; one task at a time
-    float* matrix_scratch = nullptr;
+    // what the Newton-Schulz iterations of matrices work in: two halves for tasks that run side by side, or all of it for one
+    char* matrix_scratch = nullptr;
+    int64_t matrix_half = 0;                 // bytes
+    unsigned matrix_turn = 0;
     std::shared_ptr<nnt::Scratch> matrix_mem;
-    nnt::TileDep matrix_dep;
+    nnt::TileDep matrix_dep[2];
     std::weak_ptr<nnt::PackSpace> pack_space;
     std::vector<std::weak_ptr<nnt::Scratch>> replaced_mem;      // some of it may still be held by graphs
     int cur_stream = 0;                      // stream of the task whose launches are being issued
@@ -222,7 +224,8 @@ int32_t submit(nnt_ctx* ctx, const std::vector<Access>& acc,
                const std::function<int32_t(hipStream_t)>& launch, int n_launches = 1);
 int32_t ensure_scratch(nnt_ctx* ctx, int64_t elems);
 int32_t ensure_stream_scratch(nnt_ctx* ctx, int64_t elems);
-int32_t ensure_matrix_scratch(nnt_ctx* ctx, int64_t bytes);
+// halves of at least `half` bytes (of one stream: one), and at least `whole` bytes in all
+int32_t ensure_matrix_scratch(nnt_ctx* ctx, int64_t half, int64_t whole);
 // inside a task's launch function: the part of the stream it has been given (as large as every ensure_stream_scratch so far)
 inline float* stream_scratch_of(const nnt_ctx* ctx) { return ctx->stream_scratch + ctx->cur_stream * ctx->stream_scratch_elems; }
 // Space of at least `bytes` per stream for operands laid out afresh; an empty pointer where there is no memory for it.

@@ -1246,6 +1246,11 @@ Launch choose(const NsSizes& g, int mode) {
 enum { kProducts, kNarrow, kHeld };
 int kind_of(int64_t m, int64_t l) { return m > 64 || l > 64 * kNarrowBlocks ? kProducts : l > 64 * kHeldBlocks ? kNarrow : kHeld; }
 
+// Sets of up to this size take the two halves of the workspace in turn, so that two of them run side by side: a launch's beginning and end, and the units that
+// it leaves idle, are the other's (sets of a step on 12 blocks of 768 wide 4.23 -> 3.61 ms, 777 x 1111 165 -> 104 us each; more than two at a time, four sets of a
+// block of 1600 10.0 -> 10.7 ms).  Larger ones fill the chip (two of 4096 x 4096 7.97 ms either way) and take all of it.
+constexpr int64_t kHalfBytes = (int64_t)512 << 20;
+
 // One set of launches: as many matrices as it takes to fill the chip.
 struct Set {
     NsGroup g{};
@@ -1257,6 +1262,7 @@ struct Set {
     int64_t patch = 0, bytes = 0;        // 64 x 64 blocks of all matrices; workspace
     double work = 0.0;
     std::vector<Access> acc;
+    bool whole() const { return bytes > kHalfBytes; }
 };
 
 // Puts tasks from number *first on into a set.
@@ -1318,7 +1324,6 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
     }
     w.sizes.n = g.n;
     if (kind == kHeld) return NNT_OK;                    // (needs no workspace)
-    w.acc.push_back(Access{&ctx->matrix_dep, 1, kReadWrite});
     g.norm_blocks = (int32_t)std::min<int64_t>(chunks, kNormBlocks);
     g.partial = bytes;
     if (kind == kProducts) {
@@ -1333,9 +1338,14 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
     return NNT_OK;
 }
 
-int32_t submit_set(nnt_ctx* ctx, const char* label, int steps, const Set& w) {
+int32_t submit_set(nnt_ctx* ctx, const char* label, int steps, Set& w) {
     NsGroup g = w.g;
-    g.space = reinterpret_cast<char*>(ctx->matrix_scratch);
+    if (w.kind != kHeld) {
+        const int half = w.whole() || ctx->n_streams == 1 ? 0 : ctx->matrix_turn++ & 1;
+        for (int k = 0; k < 2; k++)
+            if (k == half || w.whole()) w.acc.push_back(Access{&ctx->matrix_dep[k], 1, kReadWrite});
+        g.space = ctx->matrix_scratch + half * ctx->matrix_half;
+    }
     const NsGroup* there = reinterpret_cast<const NsGroup*>(g.space);
     OpTag tag(ctx, label, w.work, false);
     if (w.kind == kHeld)
@@ -1371,15 +1381,16 @@ int32_t newton_schulz(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_c
         kind[kind_of(m, l)].push_back(t);
     }
     std::vector<Set> sets;
-    int64_t bytes = 0;
+    int64_t half = 0, whole = 0;
     for (int k = 0; k < 3; k++)
         for (size_t first = 0; first < kind[k].size();) {
             sets.emplace_back();
             const int32_t rc = make_set(ctx, label, cfg, mu, nesterov, kind[k], k, &first, &sets.back());
             if (rc != NNT_OK) return rc;
-            bytes = std::max(bytes, sets.back().bytes);
+            int64_t& most = sets.back().whole() ? whole : half;
+            most = std::max(most, sets.back().bytes);
         }
-    int32_t rc = ensure_matrix_scratch(ctx, bytes);
+    int32_t rc = ensure_matrix_scratch(ctx, half, whole);
     for (size_t k = 0; rc == NNT_OK && k < sets.size(); k++) rc = submit_set(ctx, label, cfg.steps, sets[k]);
     return rc;
 }

@@ -385,6 +385,31 @@ def test_captured_and_replayed(mods):
         assert ctx.stats()["device_workspace_bytes"] < held
 
 
+def test_calls_side_by_side(mods):
+    """Calls that share the workspace by halves, between them one that takes all of it: on four streams the same bits as on one."""
+    capi, tiled = mods
+    shapes = [(300, 500), (200, 300), (65, 70), (40, 900), (64, 64), (4096, 4100), (300, 500), (900, 200), (30, 4000), (128, 900)]
+    G = [torch.randn(*s, generator=torch.Generator(device="cuda").manual_seed(k), device="cuda") for k, s in enumerate(shapes)]
+    results = []
+    for streams in (1, 2, 4):
+        with tiled.Context(n_streams=streams) as ctx:
+            t, o = [[tiled.TiledTensor(ctx, "f32", s, s, fill=0) for s in shapes] for _ in range(2)]
+            for x, g in zip(t, G):
+                x.tile_view(0).copy_(g.t().reshape(-1))
+            torch.cuda.synchronize()
+            for _ in range(3):
+                for x, y in zip(t, o):
+                    capi.nnt_orthogonalize(ctx.h, C.byref(ns(capi)), 1, handles(mods, [x]), handles(mods, [y]))
+            ctx.wait()
+            results.append([y.tile_view(0).clone() for y in o])
+            torch.cuda.synchronize()
+    for other in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], other))
+    for g, a in zip(G[:5], results[0]):
+        want = D.orthogonalize(g.cpu().numpy())
+        assert np.linalg.norm(a.view(g.shape[1], g.shape[0]).t().cpu().numpy() - want) <= bound(want) + 2.0 ** -24 * np.linalg.norm(want)
+
+
 def test_two_graphs_with_one_workspace(mods):
     """Matrices of every kind in two graphs that share the workspace, replayed in turn with an eager call between."""
     capi, tiled = mods
