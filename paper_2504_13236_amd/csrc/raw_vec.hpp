@@ -36,9 +36,17 @@ template <> struct RawVec<float> {
     static constexpr bool kKeeps = true;          // holds fp32 values: the shifted exponentials can take the logits' place
     __device__ __forceinline__ float at(int j) const { return x[j]; }
     __device__ __forceinline__ void set(int j, float f) { x[j] = f; }
-    static __device__ __forceinline__ void store(float* p, const float (&f)[V], int cnt) {
+    // away: past the caches
+    static __device__ __forceinline__ void store(float* p, const float (&f)[V], int cnt, bool away = false) {
         if (cnt >= V) {
-            *reinterpret_cast<vec*>(p) = vec{f[0], f[1], f[2], f[3]};
+            const vec y{f[0], f[1], f[2], f[3]};
+            if (away) {
+                asm volatile("");                        // (else the two stores become one, of the other kind)
+                __builtin_nontemporal_store(y, reinterpret_cast<vec*>(p));
+                asm volatile("");
+            } else {
+                *reinterpret_cast<vec*>(p) = y;
+            }
         } else {
 #pragma unroll
             for (int j = 0; j < V; j++)
@@ -74,12 +82,18 @@ template <> struct RawVec<bf16_t> {
     static constexpr bool kKeeps = false;
     __device__ __forceinline__ void set(int, float) {}
     __device__ __forceinline__ float at(int j) const { return __uint_as_float((j & 1) ? (x[j >> 1] & 0xffff0000u) : (x[j >> 1] << 16)); }
-    static __device__ __forceinline__ void store(bf16_t* p, const float (&f)[V], int cnt) {
+    static __device__ __forceinline__ void store(bf16_t* p, const float (&f)[V], int cnt, bool away = false) {
         if (cnt >= V) {
             vec y;
 #pragma unroll
             for (int j = 0; j < 4; j++) y[j] = (uint32_t)f2bf(f[2 * j]) | ((uint32_t)f2bf(f[2 * j + 1]) << 16);
-            *reinterpret_cast<vec*>(p) = y;
+            if (away) {
+                asm volatile("");                        // (else the two stores become one, of the other kind)
+                __builtin_nontemporal_store(y, reinterpret_cast<vec*>(p));
+                asm volatile("");
+            } else {
+                *reinterpret_cast<vec*>(p) = y;
+            }
         } else {
 #pragma unroll
             for (int j = 0; j < V; j++)

@@ -12,8 +12,8 @@
 // Everything here is bound by memory: one read of the logits for logp, a read and a write for the policy loss, and
 // two reads and a write for the preference loss, whose coefficients need the whole pair first.  bf16 logits, 50304 to a column, 5/8 of the positions with a label:
 //   logp        8192 columns    95 us for  515 MB (5.4 TB/s)
-//   policy      8192           250 us for 1275 MB (5.1 TB/s; one sequence of eight has no label at all)
-//   preference  4096           180 us for  927 MB (5.1 TB/s; part of the second read is found in the caches)
+//   policy      8192           241 us for 1275 MB (5.3 TB/s; one sequence of eight has no label at all)
+//   preference  4096           175 us for  927 MB (5.3 TB/s; part of the second read is found in the caches)
 // where a copy reaches 5.1.  A single fp32 column of 50304 takes 6 us: the launch, four loads in a row and two exchanges between wavefronts.
 #include "colwise.hpp"
 #include "device_util.hpp"
@@ -26,6 +26,11 @@ namespace {
 constexpr int kTableTiles = 64;               // vocabulary tiles whose addresses a workgroup keeps in LDS
 constexpr int64_t kMaxPositions = 1 << 22;    // a workgroup of 1024 threads each: 2^32 threads are more than a launch takes
 constexpr int64_t kMaxVectors = 1 << 20;      // of a column: up to there `place` finds a vector's tile exactly
+
+// Gradients of more than this leave past the caches: they would drive out logits that are still to be read a second time, and nobody finds so much of them there
+// later (preference loss of 1998 fp32 columns of 32003, 256 MB: 114 -> 98 us; policy loss of 8192 of 50304 in bf16 255 -> 241).  Smaller ones are
+// read from the caches by the head's products (a model's step with 103 MB of logits 886 us, 893 with this).
+constexpr int64_t kCached = (int64_t)128 << 20;
 
 // exp(t), t <= 0, for logits of type T.  Both factors of the exponent's product with 1/ln 2 are kept, since the rounded constant alone makes
 // every log-probability 6e-8 too small, and hundreds of them add up in a reward.  What is left is the rounding of y = t / ln 2, 6e-8 |t| at most: enough in front
@@ -45,6 +50,7 @@ struct Logits {
     TiledView X;
     int32_t vt, nvec;
     float inv_vt;
+    bool away;                                    // gradients leave past the caches
 };
 
 // A workgroup's column: where it lies, its label, and the vector that holds the label's logit.
@@ -284,7 +290,7 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 && NT == 1024 && SLOTS > 0
             for (int f = tid; f < a.nvec; f += NT) {
                 int l, e, cnt;
                 place<T>(a, f, l, e, cnt);
-                RawVec<T>::store(out.at(a, at.c, l) + e, z, cnt);
+                RawVec<T>::store(out.at(a, at.c, l) + e, z, cnt, a.away);
             }
         }
         return;
@@ -363,7 +369,7 @@ __global__ void __launch_bounds__(NT, (sizeof(T) == 2 && NT == 1024 && SLOTS > 0
             for (int j = 0; j < V; j++)
                 if (j == at.lab_j) y[j] += g;
         }
-        RawVec<T>::store(out.at(a, at.c, l) + e, y, cnt);
+        RawVec<T>::store(out.at(a, at.c, l) + e, y, cnt, a.away);
     };
     if constexpr (SLOTS > 0) {
 #pragma unroll
@@ -554,7 +560,7 @@ __global__ void __launch_bounds__(NT) preference_gradient_kernel(Logits a, Prefe
                     if (j == at.lab_j) y[j] += g;
             }
         }
-        RawVec<T>::store(out.at(a, at.c, l) + e, y, cnt);
+        RawVec<T>::store(out.at(a, at.c, l) + e, y, cnt, a.away);
     }
 }
 
@@ -614,7 +620,7 @@ int32_t take_logits(nnt_ctx* ctx, const std::string& who, nnt_tensor* X, const i
     const int64_t nvec = vt * (X->grid[0] - 1) + (X->tile_extent(0, X->grid[0] - 1) + V - 1) / V;
     if (nvec > kMaxVectors) return fail(ctx, NNT_EINVAL, who + ": vocabulary too long");
     if (X->shape[1] >= kMaxPositions || X->shape[2] >= kMaxPositions || X->shape[1] * X->shape[2] >= kMaxPositions) return fail(ctx, NNT_EINVAL, who + ": too many positions");
-    *out = Logits{labels, X->view(), (int32_t)vt, (int32_t)nvec, 1.f / (float)vt};
+    *out = Logits{labels, X->view(), (int32_t)vt, (int32_t)nvec, 1.f / (float)vt, X->elem_size() * X->shape[0] * X->shape[1] * X->shape[2] > kCached};
     return NNT_OK;
 }
 
