@@ -5,18 +5,26 @@
 //
 // A step costs m^2 n (A is symmetric: half of it) + m^3 (A^2: half) + 2 m^2 n flops, so it is bound by the matrix cores
 // for all but the smallest matrices.  The fp32 matrix instructions reach 150 TFLOP/s; the fp16 ones eight times that
-// and more.  A value x is therefore kept as two halves, hi = fp16(2^12 x) and lo = fp16(2^12 x - hi), and a product is
+// and more.  A value x is therefore kept as two halves, hi = fp16(2^14 x) and lo = fp16(2^14 x - hi), and a product is
 // hi hi + hi lo + lo hi with sums in fp32: three instructions of the fast kind in place of one of the slow.  hi + lo hold 22 bits of
-// x (the last one that an fp16 number of this scale can have is 2^-36), the term lo lo that is left out is below 2^-22 of the product, so
-// results are as far from 64 bits as those of fp32 products to within a small factor.  2^12 keeps both halves of the entries that matter
-// away from fp16's smallest numbers and leaves room up to 16; what the iteration's polynomials can reach is checked by the caller.
+// x, but none below 2^-38, the last one that an fp16 number of this scale can have; the term lo lo that is left out is below 2^-22 of the product.  X stays below
+// 2.83; polynomials in A are kept at a scale of 2^12, which leaves room up to 16: what the iteration can reach is checked by the caller.
+//
+// fp32 products keep every row of X to 24 bits of its own size, however small it is beside the others, and the iteration brings such a row up to them, by a factor
+// of `a` a step.  So here each row has a power of two of its own: what is stored is D X, D = diag(2^e_i), with rows of at most length 1 wherever e_i > 0.  e_i comes from
+// the row's length in X_0 and falls by what a step can make a row grow, max |a + b s^2 + c s^4|, until it is 0 (x_i <- x_i (a I + b X^T X + c (X^T X)^2): a row
+// grows by no more than its singular directions do).  Products keep to it without a factor inside the sums:
+//   (D X)(D X)^T = D A D;  stored as  D A = (D A D) D^-1, so that  (D A)(D A)^T = D A^2 D  and so on for all polynomials in A, which commute;
+//   B is stored as  D B D^-1,  so that  (D B D^-1)(D X) = D B X.
+// The values that are stored stay below 16: |x_i (.) X^T| <= max s |.| for rows of length 1, and |b + c s^2| s <= 13.6 where |b s^2 + c s^4| <= 8 on [0, 1].
+// Gradients with rows of 1e-8 of the others, 128 x 300, 20 steps: 3e-6 of the result off, fp32 products 3e-6, one scale for all 5e-2.
 //
 // All operands of the products lie in the workspace as panels: 64 rows x 16 columns of the contraction, hi part and lo part of 2 KB each,
 // inside them eight columns of a row next to each other (16 bytes), 64 rows of those, then the next eight columns.  That is the
 // image that the products want in LDS, so loads go straight there in runs of 4 KB, and a matrix instruction's operand is one 16-byte LDS
 // read per lane without bank conflicts.  Every product has the contraction along the columns of both operands: A = X X^T and A^2 = A A^T anyway, and B X
-// reads X as its transpose, which the step before (or the set-up) has written beside X itself.  Rows and columns are padded with zeros to whole
-// tiles; zeros stay zeros through the iteration.
+// reads X as its transpose, which the step before (or the set-up) has written beside X itself.  D A and D B D^-1 are not symmetric, but their sums are: tiles on and above
+// the diagonal are computed, and scaled twice.  Rows and columns are padded with zeros to whole tiles; zeros stay zeros through the iteration.
 #include "device_util.hpp"
 #include "gemm_dl_common.hpp"
 #include "internal.hpp"
@@ -33,8 +41,9 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kGroupMatrices = 16;        // matrices of one set of launches
-constexpr int kNormBlocks = 512;          // most partial sums of a matrix's norm
-constexpr float kScale = 4096.f;          // 2^12
+constexpr float kScale = 4096.f;          // of square matrices, 2^12
+constexpr float kScaleX = 16384.f;        // of X, whose entries stay below 2.83: 2^14
+constexpr float kGramFactor = kScale / kScaleX / kScaleX;
 constexpr int kPanelBytes = 4096;         // 64 rows x 16 columns, both parts
 constexpr int kPartBytes = 2048;
 
@@ -48,7 +57,9 @@ struct NsMatrix {
     int32_t rows, cols, base0, base1, grid0, grid1;      // the tensors' geometry
     int32_t flip;                                        // X is the transpose (more rows than columns)
     int32_t mp, np;                                      // X's extents, mp <= np, padded to whole panels of 64 rows
-    int64_t X, XT, A, part;                              // bytes from the start of the workspace; X and XT: two buffers each, one behind the other; A: see NsOp
+    int32_t splits;                                      // of the long side by the workgroups that add up squares
+    int64_t X, XT, A;                                    // bytes from the start of the workspace; X and XT: two buffers each, one behind the other; A: see NsOp
+    int64_t squares, part, exponents;                    // sums of squares by split and row of X, the same of 64 rows at a time; e_i of the first step
     MatView G, M, P, LP;                                 // gradient, momentum, parameter (or result), bf16 copy
     float decay, step;                                   // P <- decay P - step X (step < 0: P <- X)
 };
@@ -63,7 +74,7 @@ struct NsSizes {
 // 0.6 us longer).
 struct NsGroup {
     char* space;
-    int32_t n, norm_blocks, nesterov;
+    int32_t n, nesterov, growth;                         // growth: log2 of what a step can make a row grow by, in 1/256
     float mu;                                            // < 0: no momentum, U = G
     float a, b, c;
     double eps;
@@ -98,73 +109,132 @@ __device__ __forceinline__ void read_columns(const NsMatrix& q, const MatView& w
     else read_columns_as<bf16_t>(q, w.tiles, there, t0, o0, e0, c0, v);
 }
 
-// ---------------------------------------------------------------- momentum and norm
-// Workgroups take chunks of 8192 elements of a tile in turn, eight to a thread; each leaves one partial sum of squares in 64 bits (no value of
-// fp32 overflows or vanishes in it).  Bound by memory: 8192 x 8192 with momentum, 139 us for 805 MB.
-constexpr int kNormChunk = 8192;
+// ... to where read_columns finds them
+__device__ __forceinline__ void write_columns(const NsMatrix& q, void* const* tiles, bool there, int t0, int o0, int e0, int c0, const float (&v)[16]) {
+    int t1 = c0 / q.base1, c1 = c0 - t1 * q.base1;
+    float* p = there && c0 < q.cols ? global_as<float>(tiles[t0 + q.grid0 * t1]) + o0 + (int64_t)e0 * c1 : nullptr;
+#pragma unroll
+    for (int s = 0; s < 16; s++) {
+        if (there && c0 + s < q.cols) *p = v[s];
+        p += e0;
+        if (++c1 == q.base1) {
+            c1 = 0;
+            t1++;
+            if (there && c0 + s + 1 < q.cols) p = global_as<float>(tiles[t0 + q.grid0 * t1]) + o0;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- momentum and norms
+// Sums over the wavefront of 16 values each: the lane's own of the sums, number sum16_index(lane).  Halves are exchanged while there is more than one value left,
+// 17 exchanges for all of them.
+__device__ __forceinline__ int sum16_index(int lane) { return lane >> 2; }
+__device__ __forceinline__ double sum16(double (&v)[16], int lane) {
+#pragma unroll
+    for (int half = 8; half > 0; half >>= 1) {
+        const bool up = lane & (half * 4);
+#pragma unroll
+        for (int k = 0; k < half; k++) {
+            const double keep = up ? v[k + half] : v[k], give = up ? v[k] : v[k + half];
+            v[k] = keep + __shfl_xor(give, half * 4, 64);
+        }
+    }
+    v[0] += __shfl_xor(v[0], 2, 64);
+    return v[0] + __shfl_xor(v[0], 1, 64);
+}
+
+// A workgroup takes 64 rows of X and a part of its columns, 256 at a time: a lane a row of the tensor and a wavefront 16 columns of it.  Squares are added up in 64
+// bits (no value of fp32 overflows or vanishes in it), by row of X and over the 64 rows.  Bound by memory.
 __global__ void __launch_bounds__(1024) ns_norm_kernel(NsGroup g) {
-    __shared__ double red[16];
+    __shared__ double red[16][64];
     // the launches behind this one read the group from the workspace
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < sizeof(NsGroup) / 4)
         reinterpret_cast<uint32_t*>(g.space)[threadIdx.x] = reinterpret_cast<const uint32_t*>(&g)[threadIdx.x];
     const NsMatrix& q = g.mat[blockIdx.y];
-    const int tid = threadIdx.x;
-    const int64_t full = (int64_t)q.base0 * q.base1;
-    const int per_tile = (int)((full + kNormChunk - 1) / kNormChunk);
-    const int64_t chunks = (int64_t)per_tile * q.grid0 * q.grid1;
-    double sum = 0.0;
-    for (int64_t ch = blockIdx.x; ch < chunks; ch += gridDim.x) {
-        const int tile = (int)(ch / per_tile);
-        const int t0 = tile % q.grid0, t1 = tile / q.grid0;
-        const int64_t numel = (int64_t)min(q.base0, q.rows - t0 * q.base0) * min(q.base1, q.cols - t1 * q.base1);
-        const int64_t at = (ch - (int64_t)tile * per_tile) * kNormChunk + tid * 4;
-        float u[2][4];
-        RawVec<float> m[2];
-        int cnt[2];
-        float* mp = g.mu >= 0.f ? global_as<float>(q.M.tiles[tile]) : nullptr;
+    const int row_blocks = q.mp >> 6, splits = q.splits;
+    if ((int)blockIdx.x >= row_blocks * splits) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rb = blockIdx.x % row_blocks, part = blockIdx.x / row_blocks;
+    double sum[16];
 #pragma unroll
-        for (int s = 0; s < 2; s++) {
-            const int64_t e = at + s * 4096;
-            cnt[s] = e < numel ? (int)min((int64_t)4, numel - e) : 0;
-            if (cnt[s] == 0) continue;
-            if (q.G.dtype == NNT_F32) {
-                RawVec<float> x;
-                x.load(global_as<const float>(q.G.tiles[tile]) + e, cnt[s]);
+    for (int s = 0; s < 16; s++) sum[s] = 0.0;
+    for (int l0 = part * 256; l0 < q.np; l0 += splits * 256) {
+        const int r = (q.flip ? l0 + (wave >> 2) * 64 : rb * 64) + lane, c0 = q.flip ? rb * 64 + (wave & 3) * 16 : l0 + wave * 16;
+        const int t0 = min(r, q.rows - 1) / q.base0, o0 = r - t0 * q.base0, e0 = min(q.base0, q.rows - t0 * q.base0);
+        const bool there = r < q.rows;
+        float u[16];
+        read_columns(q, q.G, there, t0, o0, e0, c0, u);
+        if (g.mu >= 0.f) {
+            float m[16];
+            read_columns(q, q.M, there, t0, o0, e0, c0, m);
 #pragma unroll
-                for (int k = 0; k < 4; k++) u[s][k] = x.at(k);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 4; k++) u[s][k] = k < cnt[s] ? bf2f(global_as<const bf16_t>(q.G.tiles[tile])[e + k]) : 0.f;
+            for (int s = 0; s < 16; s++) {
+                m[s] = fmaf(g.mu, m[s], u[s]);
+                u[s] = g.nesterov ? fmaf(g.mu, m[s], u[s]) : m[s];
             }
-            if (mp) m[s].load(mp + e, cnt[s]);
+            write_columns(q, q.M.tiles, there, t0, o0, e0, c0, m);
         }
 #pragma unroll
-        for (int s = 0; s < 2; s++) {
-            if (cnt[s] == 0) continue;
-            if (mp) {
-                float v[4];
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    v[k] = fmaf(g.mu, m[s].at(k), u[s][k]);
-                    u[s][k] = g.nesterov ? fmaf(g.mu, v[k], u[s][k]) : v[k];
-                }
-                RawVec<float>::store(mp + at + s * 4096, v, cnt[s]);
-            }
-#pragma unroll
-            for (int k = 0; k < 4; k++)
-                if (k < cnt[s]) sum += (double)u[s][k] * (double)u[s][k];
-        }
+        for (int s = 0; s < 16; s++) sum[s] += (double)u[s] * (double)u[s];
     }
+    if (q.flip) {
+        const double x = sum16(sum, lane);
+        if ((lane & 3) == 0) red[wave >> 2][(wave & 3) * 16 + sum16_index(lane)] = x;
+    } else {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    if ((tid & 63) == 0) red[tid >> 6] = sum;
+        for (int s = 1; s < 16; s++) sum[0] += sum[s];
+        red[wave][lane] = sum[0];
+    }
     __syncthreads();
-    if (tid == 0) {
+    if (tid < 64) {
         double t = 0.0;
-        for (int w = 0; w < 16; w++) t += red[w];
-        reinterpret_cast<double*>(g.space + q.part)[blockIdx.x] = t;
+        for (int w = 0; w < (q.flip ? 4 : 16); w++) t += red[w][tid];
+        reinterpret_cast<double*>(g.space + q.squares)[(int64_t)part * q.mp + rb * 64 + tid] = t;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
+        if (tid == 0) reinterpret_cast<double*>(g.space + q.part)[blockIdx.x] = t;
     }
 }
+
+// e of a row of the given sum of squares in a matrix of the given length: the row of X_0 times 2^e is between 1/2 and 1 long.  0 for rows without one (zeros, no numbers).
+__device__ __forceinline__ int row_exponent(double squares, double length) {
+    const double x = sqrt(squares) / length;
+    if (!(x > 0.0) || x > 1.0) return 0;
+    int k;
+    (void)frexp(x, &k);
+    return max(0, -k);
+}
+
+// Set-up of a workgroup of four wavefronts: the matrix's length, and the exponents of the 64 rows of X from row i0 on.
+struct SetUp {
+    double total[4], squares[4][64];
+    int exponent[64];
+};
+__device__ __forceinline__ double length_and_exponents(const NsGroup& g, const NsMatrix& q, int i0, bool keep, SetUp& w) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const double *part = reinterpret_cast<const double*>(g.space + q.part), *squares = reinterpret_cast<const double*>(g.space + q.squares);
+    double sum = 0.0, row = 0.0;
+    for (int k = tid; k < (q.mp >> 6) * q.splits; k += 256) sum += part[k];
+#pragma unroll 8
+    for (int k = wave; k < q.splits; k += 4) row += squares[(int64_t)k * q.mp + i0 + lane];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if (lane == 0) w.total[wave] = sum;
+    w.squares[wave][lane] = row;
+    __syncthreads();
+    const double length = sqrt(w.total[0] + w.total[1] + w.total[2] + w.total[3]) + g.eps;
+    if (wave == 0) {
+        const int e = row_exponent(w.squares[0][lane] + w.squares[1][lane] + w.squares[2][lane] + w.squares[3][lane], length);
+        w.exponent[lane] = e;
+        if (keep) reinterpret_cast<int*>(g.space + q.exponents)[i0 + lane] = e;
+    }
+    __syncthreads();
+    return length;
+}
+
+// What `steps` steps can make a row grow by, as a power of two; e of a row behind that.
+__host__ __device__ inline int grown_by(int growth, int steps) { return (growth * steps + 255) >> 8; }
+__device__ __forceinline__ int exponent_at(int first, int grown) { return max(first - grown, 0); }
 
 // The matrix of a workgroup of a launch over tiles of BM x BM results of all matrices (SYM: those on and above the diagonal of
 // square results); `wg` becomes its number among the matrix's own.
@@ -200,16 +270,16 @@ __device__ __forceinline__ int64_t panel_at(int row, int k, int K) {
     return ((int64_t)(row >> 6) * (K >> 4) + (k >> 4)) * kPanelBytes + ((k & 15) >> 3) * 1024 + (row & 63) * 16;
 }
 
-// 2^12 x / length, for any length above 0 (in 64 bits: the sum of the partial sums' root and eps): a factor between 1 and 2 and a power of two, since the
+// 2^14 x / length times another power of two, for any length above 0 (in 64 bits: the sum of the partial sums' root and eps): a factor between 1 and 2 and a power of two, since the
 // quotient alone can lie outside of fp32.
 struct Scale {
     float factor;
     int exponent;
     __device__ __forceinline__ explicit Scale(double length) {
         factor = (float)(1.0 / frexp(length, &exponent));
-        exponent = 12 - exponent;
+        exponent = 14 - exponent;
     }
-    __device__ __forceinline__ float operator()(float x) const { return ldexpf(x, exponent) * factor; }
+    __device__ __forceinline__ float operator()(float x, int more) const { return ldexpf(x, exponent + more) * factor; }
 };
 
 // ---------------------------------------------------------------- set-up: X_0 and its transpose
@@ -218,7 +288,7 @@ struct Scale {
 __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict__ group, NsSizes sizes) {
     const NsGroup& g = *group;
     __shared__ float t[64][65];                          // [i][j]
-    __shared__ double red[4];
+    __shared__ SetUp setup;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int p = blockIdx.x;
     const NsMatrix& q = g.mat[matrix_of<false, 64>(sizes, p)];
@@ -230,21 +300,14 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict
     float u[16], m[16];
     read_columns(q, q.G, r < q.rows, t0, o0, e0, c0, u);
     if (g.mu >= 0.f) read_columns(q, q.M, r < q.rows, t0, o0, e0, c0, m);
-    const double* part = reinterpret_cast<const double*>(g.space + q.part);
-    double sum = 0.0;
-    for (int k = tid; k < g.norm_blocks; k += 256) sum += part[k];
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    if (lane == 0) red[wave] = sum;
-    __syncthreads();
-    const Scale scaled(sqrt(red[0] + red[1] + red[2] + red[3]) + g.eps);
+    const Scale scaled(length_and_exponents(g, q, i0, j0 == 0, setup));
 #pragma unroll
     for (int s = 0; s < 16; s++) {
         float x = u[s];
         if (g.mu >= 0.f) x = g.nesterov ? fmaf(g.mu, m[s], x) : m[s];
         const int c = wave * 16 + s;
-        if (q.flip) t[c][lane] = scaled(x);
-        else t[lane][c] = scaled(x);
+        if (q.flip) t[c][lane] = scaled(x, setup.exponent[c]);
+        else t[lane][c] = scaled(x, setup.exponent[lane]);
     }
     __syncthreads();
     // a lane's row, a wavefront's two groups of eight columns, of X and of its transpose
@@ -276,15 +339,19 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict
 }
 
 // ---------------------------------------------------------------- products
-enum { kGram, kPoly, kStep, kLast };
+enum { kGram, kPoly, kPair, kStep, kLast };
 
-// What a product of square symmetric matrices, or one with X, is made of.  The group's matrices have up to four square buffers each (0: A).
-//   kPoly  buffer d = mul (buffer p)(buffer q) + add (buffer e) + diag I
-//   kStep  X = (buffer p) X + add X;  kLast  the same, applied
+// What a product of square matrices, or one with X, is made of.  The group's matrices have up to four square buffers each (0: A), that hold D p of a polynomial
+// p in A without a constant term, or (`apart`) D p D^-1 for the product with X, with such a term.
+//   kPoly  buffer d = mul (buffer p)(buffer q) + add (buffer e)
+//   kPair  the same + add (buffer p) + diag I, at a scale of 2^10 (it reaches some 50)
+//   kStep  X = mul (buffer p) X + add X;  kLast  the same, applied
+// Rows of X have grown by up to 2^from before, and by 2^to behind it.
 struct NsOp {
-    int32_t p, q, e, d;
+    int32_t p, q, e, d, apart, from, to;
     float mul, add, diag;
 };
+constexpr int kPairShift = 2;             // 2^12 / 2^10
 
 // One result's place in the tensor, found from its row and column of X.
 __device__ __forceinline__ void apply_one(const NsMatrix& q, float x, int i, int j) {
@@ -369,60 +436,96 @@ __device__ __forceinline__ void apply_results(const NsMatrix& q, const float (&x
     }
 }
 
-// The result path of a wavefront: FM x FN blocks of 32 x 32 from row i0 and column j0 on.  `turn`: LDS for 32 rows, in which the results change places.
+// The result path of a wavefront: FM x FN blocks of 32 x 32 from row i0 and column j0 on.  er, ec: what the powers of two of its rows and columns go by, from LDS (of square
+// results e_i; of X what it changes by).  `turn`: LDS for 32 rows, in which the results change places.
 constexpr int turn_pitch(int FN) { return 32 * FN + 8; }         // in 32-bit words
 template <int MODE, int FM, int FN>
-__device__ __forceinline__ void store_results(const NsGroup& g, const NsMatrix& q, const f32x16 (&acc)[FM][FN], int i0, int j0, bool diagonal, int now, const NsOp& op, uint32_t* turn) {
+__device__ __forceinline__ void store_results(const NsGroup& g, const NsMatrix& q, const f32x16 (&acc)[FM][FN], int i0, int j0, bool diagonal, int now, const NsOp& op,
+                                              const int* er, const int* ec, uint32_t* turn) {
     // results: this lane has column j0 + 32 y + (lane & 31), rows i0 + 32 x + 8 p + 4 (lane >> 5) + 0 .. 3
-    constexpr bool kSym = MODE == kGram || MODE == kPoly;
-    constexpr int kPitch = turn_pitch(FN);
+    constexpr bool kSym = MODE == kGram || MODE == kPoly || MODE == kPair;
+    constexpr int kPitch = turn_pitch(FN), kTerms = MODE == kGram ? 0 : MODE == kPair ? 2 : 1;
     const int lane = threadIdx.x & 63;
     const int64_t xbytes = (int64_t)q.mp * q.np * 4;
     const int64_t square = (int64_t)q.mp * q.mp * 4;
-    const char* E = g.space + (MODE == kPoly ? q.A + op.e * square : q.XT + now * xbytes);          // the term that is added, laid out like the result
-    char* D = g.space + (MODE == kGram ? q.A : MODE == kPoly ? q.A + op.d * square : q.XT + (1 - now) * xbytes);
+    // the terms that are added, laid out like the result
+    const char* E[2] = {g.space + (MODE == kPoly ? q.A + op.e * square : MODE == kPair ? q.A + op.p * square : q.XT + now * xbytes), g.space + q.A + op.q * square};
+    char* D = g.space + (MODE == kGram ? q.A : kSym ? q.A + op.d * square : q.XT + (1 - now) * xbytes);
     char* Dt = kSym ? D : g.space + q.X + (1 - now) * xbytes;                       // the same with rows and columns exchanged
     const int Kt = kSym ? q.mp : q.np;
     const bool turned = MODE != kLast && !(kSym && diagonal);
-    const float factor = (MODE == kPoly ? op.mul : 1.f) / kScale;      // sums carry the scale twice
-    const float add = op.add, diag = op.diag * kScale;
-    const bool fetches = MODE != kGram && add != 0.f;
-    // what is added is fetched one block of 32 rows ahead: behind the stores that the compiler cannot tell apart from it every load would wait
-    f16x4 e[2][FN][4][2];
+    const float factor = MODE == kGram ? kGramFactor : op.mul / kScale;      // sums carry both factors' scales
+    const float add = op.add;
+    const bool fetches = kTerms > 0 && add != 0.f, apart = MODE == kPair || (MODE == kPoly && op.apart);
+    constexpr int kShift = MODE == kPair ? kPairShift : 0;
+    // what is added is fetched one block of 32 rows ahead: behind the stores that the compiler cannot tell apart from it every load would wait (two terms: no registers for that)
+    constexpr int kAhead = kTerms == 1;
+    f16x4 e[1 + kAhead][kTerms ? kTerms : 1][FN][4][2];
+    f16x8 et[kTerms ? kTerms : 1][2 * FN][2];                          // the same of symmetric results with rows and columns exchanged
     // (blocks behind the last row block of X or of its transpose are not there)
     const int rows = q.mp, cols = kSym ? q.mp : q.np;
     auto fetch = [&](int x) {
         if (i0 + x * 32 >= rows) return;
 #pragma unroll
-        for (int y = 0; y < FN; y++) {
-            if (j0 + y * 32 >= cols) continue;
+        for (int t = 0; t < kTerms; t++)
 #pragma unroll
-            for (int p = 0; p < 4; p++) {
-                const char* at = E + panel_at(j0 + y * 32 + (lane & 31), i0 + x * 32 + p * 8, q.mp) + (lane >> 5) * 8;
-                e[x & 1][y][p][0] = *reinterpret_cast<const f16x4*>(at);
-                e[x & 1][y][p][1] = *reinterpret_cast<const f16x4*>(at + kPartBytes);
+            for (int y = 0; y < FN; y++) {
+                if (j0 + y * 32 >= cols) continue;
+#pragma unroll
+                for (int p = 0; p < 4; p++) {
+                    const char* at = E[t] + panel_at(j0 + y * 32 + (lane & 31), i0 + x * 32 + p * 8, q.mp) + (lane >> 5) * 8;
+                    e[x & kAhead][t][y][p][0] = *reinterpret_cast<const f16x4*>(at);
+                    e[x & kAhead][t][y][p][1] = *reinterpret_cast<const f16x4*>(at + kPartBytes);
+                }
             }
+    };
+    // (a lane's eight columns of `turn`, see below)
+    const int turned_row = lane & 31, turned_col = (lane >> 5) * 8;
+    auto fetch_turned = [&](int x) {
+        if constexpr (kSym) {
+#pragma unroll
+            for (int t = 0; t < kTerms; t++)
+#pragma unroll
+                for (int s = 0; s < 2 * FN; s++) {
+                    if (j0 + s / 2 * 32 >= cols) continue;
+                    const char* at = E[t] + panel_at(i0 + x * 32 + turned_row, j0 + s * 16 + turned_col, q.mp);
+                    et[t][s][0] = *reinterpret_cast<const f16x8*>(at);
+                    et[t][s][1] = *reinterpret_cast<const f16x8*>(at + kPartBytes);
+                }
         }
     };
-    if (fetches) fetch(0);
+    if (fetches && kAhead) fetch(0);
 #pragma unroll
     for (int x = 0; x < FM; x++) {
-        if (fetches && x + 1 < FM) fetch(x + 1);
+        if (fetches && x + kAhead < FM) fetch(x + kAhead);
         if (i0 + x * 32 >= rows) continue;
+        if (fetches && turned) fetch_turned(x);
 #pragma unroll
         for (int y = 0; y < FN; y++) {
             if (j0 + y * 32 >= cols) continue;
             float v[4][4];
 #pragma unroll
-            for (int p = 0; p < 4; p++)
+            for (int p = 0; p < 4; p++) {
+                const int4 ei = *reinterpret_cast<const int4*>(er + x * 32 + p * 8 + (lane >> 5) * 4);
+                const int ek[4] = {ei.x, ei.y, ei.z, ei.w};
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
-                    v[p][k] = acc[x][y][p * 4 + k] * factor;
-                    if (fetches) v[p][k] = fmaf(add, (float)e[x & 1][y][p][0][k] + (float)e[x & 1][y][p][1][k], v[p][k]);
-                    if constexpr (MODE == kPoly)
-                        if (diagonal && i0 + x * 32 + p * 8 + (lane >> 5) * 4 + k == j0 + y * 32 + (lane & 31)) v[p][k] += diag;
-                    if constexpr (MODE == kLast) v[p][k] *= 1.f / kScale;
+                    float w = acc[x][y][p * 4 + k] * factor;
+                    if constexpr (kSym) {
+                        if (turned) turn[(p * 8 + (lane >> 5) * 4 + k) * kPitch + y * 32 + (lane & 31)] = __float_as_uint(w);
+                        w = ldexpf(w, -ek[k]);
+                    }
+                    if (fetches)
+#pragma unroll
+                        for (int t = 0; t < kTerms; t++) w = fmaf(add, (float)e[x & kAhead][t][y][p][0][k] + (float)e[x & kAhead][t][y][p][1][k], w);
+                    if constexpr (!kSym) w = ldexpf(w, ek[k]);
+                    else if (apart) w = ldexpf(w, -ek[k] - kShift);
+                    if constexpr (MODE == kPair)
+                        if (diagonal && i0 + x * 32 + p * 8 + (lane >> 5) * 4 + k == j0 + y * 32 + (lane & 31)) w = fmaf(op.diag, kScale / (1 << kShift), w);
+                    if constexpr (MODE == kLast) w *= 1.f / kScaleX;
+                    v[p][k] = w;
                 }
+            }
             const int i = i0 + x * 32, j = j0 + y * 32 + (lane & 31);
             if constexpr (MODE == kLast) {
                 apply_results(q, v, i + (lane >> 5) * 4, j);
@@ -436,8 +539,9 @@ __device__ __forceinline__ void store_results(const NsGroup& g, const NsMatrix& 
                         split(v[p][k], h, l);
                         hi[k] = h;
                         lo[k] = l;
-                        turn[(p * 8 + (lane >> 5) * 4 + k) * kPitch + y * 32 + (lane & 31)] =
-                            (uint32_t)__builtin_bit_cast(uint16_t, h) | ((uint32_t)__builtin_bit_cast(uint16_t, l) << 16);
+                        if constexpr (!kSym)
+                            turn[(p * 8 + (lane >> 5) * 4 + k) * kPitch + y * 32 + (lane & 31)] =
+                                (uint32_t)__builtin_bit_cast(uint16_t, h) | ((uint32_t)__builtin_bit_cast(uint16_t, l) << 16);
                     }
                     char* d = D + panel_at(j, i + p * 8, q.mp) + (lane >> 5) * 8;
                     *reinterpret_cast<f16x4*>(d) = hi;
@@ -450,17 +554,44 @@ __device__ __forceinline__ void store_results(const NsGroup& g, const NsMatrix& 
 #pragma unroll
             for (int s = 0; s < 2 * FN; s++) {
                 if (j0 + s / 2 * 32 >= cols) continue;
-                const int row = lane & 31, k = (s * 2 + (lane >> 5)) * 8;
-                const uint4 u = *reinterpret_cast<const uint4*>(turn + row * kPitch + k), w = *reinterpret_cast<const uint4*>(turn + row * kPitch + k + 4);
-                const uint4 hi = make_uint4((u.x & 0xffff) | (u.y << 16), (u.z & 0xffff) | (u.w << 16), (w.x & 0xffff) | (w.y << 16), (w.z & 0xffff) | (w.w << 16));
-                const uint4 lo = make_uint4((u.x >> 16) | (u.y & 0xffff0000u), (u.z >> 16) | (u.w & 0xffff0000u), (w.x >> 16) | (w.y & 0xffff0000u),
-                                            (w.z >> 16) | (w.w & 0xffff0000u));
-                char* d = Dt + panel_at(i0 + x * 32 + row, j0 + k, Kt);
-                *reinterpret_cast<uint4*>(d) = hi;
-                *reinterpret_cast<uint4*>(d + kPartBytes) = lo;
+                const int k = s * 16 + turned_col;
+                const uint4 u = *reinterpret_cast<const uint4*>(turn + turned_row * kPitch + k), w = *reinterpret_cast<const uint4*>(turn + turned_row * kPitch + k + 4);
+                char* d = Dt + panel_at(i0 + x * 32 + turned_row, j0 + k, Kt);
+                if constexpr (kSym) {
+                    const uint32_t sums[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
+                    const int4 ea = *reinterpret_cast<const int4*>(ec + k), eb = *reinterpret_cast<const int4*>(ec + k + 4);
+                    const int ek[8] = {ea.x, ea.y, ea.z, ea.w, eb.x, eb.y, eb.z, eb.w};
+                    f16x8 hi, lo;
+#pragma unroll
+                    for (int m = 0; m < 8; m++) {
+                        float r = ldexpf(__uint_as_float(sums[m]), -ek[m]);
+                        if (fetches)
+#pragma unroll
+                            for (int t = 0; t < kTerms; t++) r = fmaf(add, (float)et[t][s][0][m] + (float)et[t][s][1][m], r);
+                        if (apart) r = ldexpf(r, -ek[m] - kShift);
+                        _Float16 h, l;
+                        split(r, h, l);
+                        hi[m] = h;
+                        lo[m] = l;
+                    }
+                    *reinterpret_cast<f16x8*>(d) = hi;
+                    *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
+                } else {
+                    const uint4 hi = make_uint4((u.x & 0xffff) | (u.y << 16), (u.z & 0xffff) | (u.w << 16), (w.x & 0xffff) | (w.y << 16), (w.z & 0xffff) | (w.w << 16));
+                    const uint4 lo = make_uint4((u.x >> 16) | (u.y & 0xffff0000u), (u.z >> 16) | (u.w & 0xffff0000u), (w.x >> 16) | (w.y & 0xffff0000u),
+                                                (w.z >> 16) | (w.w & 0xffff0000u));
+                    *reinterpret_cast<uint4*>(d) = hi;
+                    *reinterpret_cast<uint4*>(d + kPartBytes) = lo;
+                }
             }
         }
     }
+}
+// What a row's exponent does to the results of a product.
+template <int MODE>
+__device__ __forceinline__ int result_exponent(int first, const NsOp& op) {
+    const int e = exponent_at(first, op.from);
+    return MODE == kStep ? exponent_at(first, op.to) - e : MODE == kLast ? -e : e;
 }
 
 // A macro-tile: WR x WC wavefronts of FM x FN results of 32 x 32 each, ST stages of KS panels (16 KS columns of the contraction) in LDS.
@@ -535,8 +666,10 @@ __global__ void __launch_bounds__(64 * S::kWaves, 2) ns_product_kernel(const NsG
     const NsGroup& g = *group;
     constexpr int FM = S::FM, FN = S::FN, ST = S::ST;
     __shared__ __align__(1024) char lds[S::kLds];
+    __shared__ __align__(16) int ex[S::BM + S::BN];
+    static_assert(S::BM + S::BN <= 64 * S::kWaves, "a thread fetches one exponent");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave % S::WR, wc = wave / S::WR;
-    constexpr bool kSym = MODE == kGram || MODE == kPoly;
+    constexpr bool kSym = MODE == kGram || MODE == kPoly || MODE == kPair;
     // workgroups go to the eight dies in turn: each die gets one run of the tiles
     int wg = blockIdx.x;
     {
@@ -561,7 +694,10 @@ __global__ void __launch_bounds__(64 * S::kWaves, 2) ns_product_kernel(const NsG
     const int nk = (MODE == kGram ? q.np : q.mp) >> 4;           // panels along the contraction, a multiple of 4
     const int64_t square = (int64_t)q.mp * q.mp * 4;
     const char* Pb = g.space + (MODE == kGram ? q.X + now * xbytes : q.A + op.p * square);
-    const char* Qb = g.space + (MODE == kGram ? q.X + now * xbytes : MODE == kPoly ? q.A + op.q * square : q.XT + now * xbytes);
+    const char* Qb = g.space + (MODE == kGram ? q.X + now * xbytes : kSym ? q.A + op.q * square : q.XT + now * xbytes);
+
+    // (older than the loads that are counted below, which it can only make wait longer)
+    const int exponent = reinterpret_cast<const int*>(g.space + q.exponents)[min(tid < S::BM ? ti * S::BM + tid : tj * S::BN + tid - S::BM, q.mp - 1)];
 
     // a wavefront loads a part of one row block's panels per step
     const char* src;
@@ -674,14 +810,18 @@ __global__ void __launch_bounds__(64 * S::kWaves, 2) ns_product_kernel(const NsG
             return;
         }
     }
-    store_results<MODE, FM, FN>(g, q, acc, ti * S::BM + wr * 32 * FM, tj * S::BN + wc * 32 * FN, ti == tj, now, op, reinterpret_cast<uint32_t*>(lds + wave * S::kTurn));
+    if (tid < S::BM + S::BN) ex[tid] = result_exponent<MODE>(exponent, op);
+    __syncthreads();
+    store_results<MODE, FM, FN>(g, q, acc, ti * S::BM + wr * 32 * FM, tj * S::BN + wc * 32 * FN, ti == tj, now, op, ex + wr * 32 * FM, ex + S::BM + wc * 32 * FN,
+                                reinterpret_cast<uint32_t*>(lds + wave * S::kTurn));
 }
 
 // Adds up the parts of A's tiles, in their order: a wavefront takes one block of 32 x 32.
 template <typename S>
-__global__ void __launch_bounds__(256) ns_combine_kernel(const NsGroup* __restrict__ group, NsSizes sizes, int splits) {
+__global__ void __launch_bounds__(256) ns_combine_kernel(const NsGroup* __restrict__ group, NsSizes sizes, NsOp op, int splits) {
     const NsGroup& g = *group;
     __shared__ __align__(16) uint32_t turn[4 * 32 * turn_pitch(1)];
+    __shared__ __align__(16) int ex[4][64];                 // of a wavefront's 32 rows and 32 columns
     constexpr int kBlocks = S::kWaves * S::FM * S::FN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tile = blockIdx.x / (kBlocks / 4), blk = blockIdx.x % (kBlocks / 4) * 4 + wave;
@@ -714,7 +854,10 @@ __global__ void __launch_bounds__(256) ns_combine_kernel(const NsGroup* __restri
         acc[0][0][4 * v + 3] = t[v].w;
     }
     const int w = blk / (S::FM * S::FN), x = blk / S::FN % S::FM, y = blk % S::FN;
-    store_results<kGram, 1, 1>(g, q, acc, ti * S::BM + (w % S::WR * S::FM + x) * 32, tj * S::BN + (w / S::WR * S::FN + y) * 32, ti == tj, 0, NsOp{}, turn + wave * 32 * turn_pitch(1));
+    const int i0 = ti * S::BM + (w % S::WR * S::FM + x) * 32, j0 = tj * S::BN + (w / S::WR * S::FN + y) * 32;
+    ex[wave][lane] = result_exponent<kGram>(reinterpret_cast<const int*>(g.space + q.exponents)[min((lane < 32 ? i0 : j0 - 32) + lane, q.mp - 1)], op);
+    __syncthreads();
+    store_results<kGram, 1, 1>(g, q, acc, i0, j0, ti == tj, 0, op, ex[wave], ex[wave] + 32, turn + wave * 32 * turn_pitch(1));
 }
 
 // ---------------------------------------------------------------- matrices with a side of at most 64
@@ -756,15 +899,15 @@ __device__ __forceinline__ void multiply(const char* image, int r0, const char* 
 }
 
 // A lane's results of a block of 64 x 64: rows i + 8 p + 0 .. 3, column j.
-// A symmetric block as an image: four rows of a column are four columns of a row.
-__device__ __forceinline__ void store_symmetric(char* dst, const float (&x)[4][4], int i, int j) {
+// A symmetric block D p D as the image of D p (`times` 1) or D p D^-1 (2): four rows of a column are four columns of a row.
+__device__ __forceinline__ void store_symmetric(char* dst, const float (&x)[4][4], const int (&e)[4][4], int times, int i, int j) {
 #pragma unroll
     for (int p = 0; p < 4; p++) {
         f16x4 hi, lo;
 #pragma unroll
         for (int k = 0; k < 4; k++) {
             _Float16 h, l;
-            split(x[p][k], h, l);
+            split(ldexpf(x[p][k], -times * e[p][k]), h, l);
             hi[k] = h;
             lo[k] = l;
         }
@@ -793,6 +936,18 @@ __device__ __forceinline__ void store_both(char* XT, char* X, const float (&x)[4
         *reinterpret_cast<f16x4*>(d + kPartBytes) = lo;
     }
 }
+// The exponents of a lane's rows behind `steps` steps.
+__device__ __forceinline__ void exponents_of(const int* first, int growth, int steps, int i, int (&e)[4][4]) {
+    const int grown = grown_by(growth, steps);
+#pragma unroll
+    for (int p = 0; p < 4; p++) {
+        const int4 f = *reinterpret_cast<const int4*>(first + i + p * 8);
+        e[p][0] = exponent_at(f.x, grown);
+        e[p][1] = exponent_at(f.y, grown);
+        e[p][2] = exponent_at(f.z, grown);
+        e[p][3] = exponent_at(f.w, grown);
+    }
+}
 // a X + B X of X's block, X as its transpose
 __device__ __forceinline__ void step_block(const char* B, const char* XT, int wr, int wc, int i, int j, float a, float (&x)[4][4]) {
     f16x4 eh[4], el[4];
@@ -813,10 +968,11 @@ __device__ __forceinline__ void step_block(const char* B, const char* XT, int wr
 }
 
 template <int PHASE>
-__global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restrict__ group, NsSizes sizes, int now) {
+__global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restrict__ group, NsSizes sizes, int step) {
     const NsGroup& g = *group;
     __shared__ __align__(16) char image[3][kImage];      // A (set-up: U in fp32), B, X's block with its rows along the contraction
-    __shared__ double red[4];
+    __shared__ __align__(16) SetUp setup;
+    const int now = step & 1;                            // the sums' buffer of this step
     const int nt = sizes.blocks[blockIdx.y] >> 16, parts = narrow_parts(nt), part = blockIdx.x;
     if (part >= parts) return;
     const NsMatrix& q = g.mat[blockIdx.y];
@@ -825,16 +981,11 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
     auto sum_at = [&](int buffer, int p, int v) { return (((int64_t)buffer * parts + p) * 4 + wave) * 256 + v * 64 + lane; };
     const int i = wr * 32 + (lane >> 5) * 4, j = wc * 32 + (lane & 31);    // this lane's results: rows i + 8 p + 0 .. 3, column j of a block
     Scale scaled(1.0);
+    int e[4][4] = {};                                    // exponents of this lane's rows
     if constexpr (PHASE == kFirst) {
-        const double* norms = reinterpret_cast<const double*>(g.space + q.part);
-        double sum = 0.0;
-        for (int k = tid; k < g.norm_blocks; k += 256) sum += norms[k];
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        if (lane == 0) red[wave] = sum;
-        __syncthreads();
-        scaled = Scale(sqrt(red[0] + red[1] + red[2] + red[3]) + g.eps);
+        scaled = Scale(length_and_exponents(g, q, 0, part == 0, setup));
     } else {
+        if (tid < 64) setup.exponent[tid] = reinterpret_cast<const int*>(g.space + q.exponents)[tid];
         float4 t[4];
 #pragma unroll
         for (int v = 0; v < 4; v++) t[v] = sums[sum_at(now, 0, v)];
@@ -852,12 +1003,14 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
         float a[4][4];
 #pragma unroll
         for (int p = 0; p < 4; p++) {
-            a[p][0] = t[p].x / kScale;
-            a[p][1] = t[p].y / kScale;
-            a[p][2] = t[p].z / kScale;
-            a[p][3] = t[p].w / kScale;
+            a[p][0] = t[p].x * kGramFactor;
+            a[p][1] = t[p].y * kGramFactor;
+            a[p][2] = t[p].z * kGramFactor;
+            a[p][3] = t[p].w * kGramFactor;
         }
-        store_symmetric(image[0], a, i, j);
+        __syncthreads();
+        exponents_of(setup.exponent, g.growth, step, i, e);
+        store_symmetric(image[0], a, e, 1, i, j);
         __syncthreads();
         f32x16 acc;
 #pragma unroll
@@ -867,9 +1020,11 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
         for (int p = 0; p < 4; p++)
 #pragma unroll
             for (int k = 0; k < 4; k++) a[p][k] = fmaf(g.b, a[p][k], acc[p * 4 + k] * (g.c / kScale));
-        store_symmetric(image[1], a, i, j);
+        store_symmetric(image[1], a, e, 2, i, j);
         __syncthreads();
     }
+    int next_e[4][4];
+    if constexpr (PHASE == kMiddle) exponents_of(setup.exponent, g.growth, step + 1, i, next_e);
     f32x16 gram;
 #pragma unroll
     for (int k = 0; k < 16; k++) gram[k] = 0.f;
@@ -885,8 +1040,8 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
 #pragma unroll
             for (int s = 0; s < 16; s++) {
                 if (g.mu >= 0.f) x[s] = g.nesterov ? fmaf(g.mu, m[s], x[s]) : m[s];
-                if (q.flip) u[wave * 16 + s][lane] = scaled(x[s]);
-                else u[lane][wave * 16 + s] = scaled(x[s]);
+                if (q.flip) u[wave * 16 + s][lane] = scaled(x[s], setup.exponent[wave * 16 + s]);
+                else u[lane][wave * 16 + s] = scaled(x[s], setup.exponent[lane]);
             }
             __syncthreads();
 #pragma unroll
@@ -921,10 +1076,14 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
 #pragma unroll
                 for (int p = 0; p < 4; p++)
 #pragma unroll
-                    for (int k = 0; k < 4; k++) x[p][k] *= 1.f / kScale;
+                    for (int k = 0; k < 4; k++) x[p][k] = ldexpf(x[p][k], -e[p][k]) * (1.f / kScaleX);
                 apply_results(q, x, i, t * 64 + j);
                 continue;
             }
+#pragma unroll
+            for (int p = 0; p < 4; p++)
+#pragma unroll
+                for (int k = 0; k < 4; k++) x[p][k] = ldexpf(x[p][k], next_e[p][k] - e[p][k]);
             __syncthreads();                             // everybody has read X's block, which is overwritten, and is done with the last one's image
             store_both(X, image[2], x, i, j);
         }
@@ -946,22 +1105,10 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
 // twice, as its transpose too, in place of the two-byte writes: 40 us, but the two drift apart, errors a quarter larger.)
 constexpr int kHeldBlocks = 4;
 
-// the momentum's way back to where read_columns found it
-__device__ __forceinline__ void write_columns(const NsMatrix& q, void* const* tiles, bool there, int t0, int o0, int e0, int c0, const float (&v)[16]) {
-    int t1 = c0 / q.base1, c1 = c0 - t1 * q.base1;
-#pragma unroll
-    for (int s = 0; s < 16; s++) {
-        if (there && c0 + s < q.cols) global_as<float>(tiles[t0 + q.grid0 * t1])[o0 + (int64_t)e0 * c1] = v[s];
-        if (++c1 == q.base1) {
-            c1 = 0;
-            t1++;
-        }
-    }
-}
-
 __global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, int steps) {
     __shared__ __align__(16) char images[2 * kHeldBlocks + 1][kImage];       // X's transpose and X by block; A, then B
-    __shared__ double red[4 * kHeldBlocks];
+    __shared__ double red[4 * kHeldBlocks][64];          // sums of squares of X's rows
+    __shared__ __align__(16) int exponent[64];
     const NsMatrix& q = g.mat[blockIdx.x];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane((tid >> 6) & 3), t = __builtin_amdgcn_readfirstlane(tid >> 8);
     const int wr = wave & 1, wc = wave >> 1, nt = q.np >> 6;
@@ -984,18 +1131,30 @@ __global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, i
             }
             write_columns(q, q.M.tiles, there, t0, o0, e0, c0, m);
         }
-        double sum = 0.0;
+        // a lane has a row of X and 16 columns of it, or (X the transpose) a column and 16 rows
+        double square[16];
 #pragma unroll
-        for (int s = 0; s < 16; s++) sum += (double)u[s] * (double)u[s];
+        for (int s = 0; s < 16; s++) square[s] = (double)u[s] * (double)u[s];
+        if (q.flip) {
+            const double x = sum16(square, lane);
+            if ((lane & 3) == 0) red[t][wave * 16 + sum16_index(lane)] = x;
+        } else {
+#pragma unroll
+            for (int s = 1; s < 16; s++) square[0] += square[s];
+            red[tid >> 6][lane] = square[0];
+        }
+        __syncthreads();
+        double row = 0.0;
+        for (int w = 0; w < (q.flip ? nt : 4 * nt); w++) row += red[w][lane];
+        double sum = row;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        if (lane == 0) red[tid >> 6] = sum;
+        const double length = sqrt(sum) + g.eps;         // (every wavefront by itself, in the same order)
+        const int mine_e = row_exponent(row, length);
+        if (tid < 64) exponent[lane] = mine_e;
         __syncthreads();
-        sum = 0.0;
-        for (int w = 0; w < 4 * nt; w++) sum += red[w];
-        const Scale scaled(sqrt(sum) + g.eps);
+        const Scale scaled(length);
         if (mine) {
-            // a lane has a row of X and 16 columns of it, or (X the transpose) a column and 16 rows
             char *along = q.flip ? XT : X, *across = q.flip ? X : XT;
 #pragma unroll
             for (int h = 0; h < 2; h++) {
@@ -1003,7 +1162,7 @@ __global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, i
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
                     _Float16 y, z;
-                    split(scaled(u[h * 8 + e]), y, z);
+                    split(scaled(u[h * 8 + e], q.flip ? exponent[wave * 16 + h * 8 + e] : mine_e), y, z);
                     hi[e] = y;
                     lo[e] = z;
                     char* d = across + image_at(wave * 16 + h * 8 + e, lane);
@@ -1016,6 +1175,8 @@ __global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, i
             }
         }
     }
+    int e[4][4], next_e[4][4];                           // exponents of this lane's rows
+    exponents_of(exponent, g.growth, 0, i, e);
     for (int step = 0;; step++) {
         __syncthreads();
         f32x16 acc;
@@ -1042,8 +1203,8 @@ __global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, i
 #pragma unroll
             for (int p = 0; p < 4; p++)
 #pragma unroll
-                for (int k = 0; k < 4; k++) a[p][k] = acc[p * 4 + k] / kScale;
-            store_symmetric(S, a, i, j);
+                for (int k = 0; k < 4; k++) a[p][k] = acc[p * 4 + k] * kGramFactor;
+            store_symmetric(S, a, e, 1, i, j);
         }
         __syncthreads();
         if (t == 0) {
@@ -1056,7 +1217,7 @@ __global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, i
                 for (int k = 0; k < 4; k++) a[p][k] = fmaf(g.b, a[p][k], acc[p * 4 + k] * (g.c / kScale));
         }
         __syncthreads();                                 // A has been read
-        if (t == 0) store_symmetric(S, a, i, j);
+        if (t == 0) store_symmetric(S, a, e, 2, i, j);
         __syncthreads();
         float x[4][4];
         if (mine) step_block(S, XT, wr, wc, i, j, g.a, x);
@@ -1064,10 +1225,18 @@ __global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, i
 #pragma unroll
             for (int p = 0; p < 4; p++)
 #pragma unroll
-                for (int k = 0; k < 4; k++) x[p][k] *= 1.f / kScale;
+                for (int k = 0; k < 4; k++) x[p][k] = ldexpf(x[p][k], -e[p][k]) * (1.f / kScaleX);
             if (mine) apply_results(q, x, i, t * 64 + j);
             return;
         }
+        exponents_of(exponent, g.growth, step + 1, i, next_e);
+#pragma unroll
+        for (int p = 0; p < 4; p++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                x[p][k] = ldexpf(x[p][k], next_e[p][k] - e[p][k]);
+                e[p][k] = next_e[p][k];
+            }
         __syncthreads();                                 // X's transpose has been read
         if (mine) store_both(XT, X, x, i, j);
     }
@@ -1086,12 +1255,13 @@ double most_of_square(double c1, double c2, double top) {
     return most;
 }
 // Whether the iteration stays where the workspace's numbers can hold it (2^12 times 16 is fp16's largest number): singular values start in [0, 1]; with their
-// bound followed from step to step, they, their squares and b s^2 + c s^4 have to stay below 8.  *reach: the largest of the bounds.
-bool in_range(const nnt_newton_schulz_cfg& c, double* reach = nullptr) {
+// bound followed from step to step, they, their squares and b s^2 + c s^4 have to stay below 8.  *reach: the largest of the bounds; *before: the largest that a step starts from.
+bool in_range(const nnt_newton_schulz_cfg& c, double* reach = nullptr, double* before = nullptr) {
     if (!std::isfinite(c.a) || !std::isfinite(c.b) || !std::isfinite(c.c) || !(c.eps > 0.0) || !std::isfinite(c.eps) || c.steps < 1 || c.steps > 64) return false;
-    double top = 1.0, far = 1.0;
+    double top = 1.0, far = 1.0, start = 1.0;
     for (int t = 0; t < c.steps; t++) {
         const double l = top * top;
+        start = std::max(start, top);
         if (!(most_of_square(c.b, c.c, l) <= 8.0)) return false;
         // f(s) = a s + b s^3 + c s^5 is largest at the end or where a + 3 b s^2 + 5 c s^4 = 0
         auto f = [&](double x) { return std::fabs(std::sqrt(x) * (c.a + c.b * x + c.c * x * x)); };
@@ -1108,6 +1278,7 @@ bool in_range(const nnt_newton_schulz_cfg& c, double* reach = nullptr) {
         far = std::max(far, top);
     }
     if (reach) *reach = far;
+    if (before) *before = start;
     return true;
 }
 
@@ -1116,21 +1287,30 @@ bool in_range(const nnt_newton_schulz_cfg& c, double* reach = nullptr) {
 // 1024 x 4096 4.5e-6 instead of 3.5e-6; nothing after the first: 3.9e-6.)
 double kept_out(const nnt_newton_schulz_cfg& c, bool first) { return first ? c.a * c.a : c.a * c.a / 4.0; }
 
-// Whether two steps can be taken at once: the workspace also has to hold P = a I + b A + c A^2 and what is left of P_1 P_0 then.
+// What a step can make a row grow by, the largest |a + b s^2 + c s^4|, as its logarithm in 1/256 (rounded up; rows that shrink are followed for 16 binary places a step).
+int growth_of(const nnt_newton_schulz_cfg& c) {
+    double before = 1.0;
+    (void)in_range(c, nullptr, &before);
+    const double l = before * before, x = c.c != 0.0 ? -c.b / (2.0 * c.c) : 0.0;
+    double most = std::max(std::fabs(c.a), std::fabs(c.a + c.b * l + c.c * l * l));
+    if (x > 0.0 && x < l) most = std::max(most, std::fabs(c.a + c.b * x + c.c * x * x));
+    return (int)std::ceil(256.0 * std::max(std::log2(most), -16.0) + 0.01);
+}
+
+// Whether two steps can be taken at once.  The buffers hold polynomials in A = X X^T without a constant term, p(s^2) = s^2 r(s^2), as D p, whose entries reach |r| s in a row
+// of length 1 and |p| in one that keeps its length; the last one, P_1 P_0, the same at a quarter of the scale and with a multiple of the identity.  4097 places of polynomials
+// of degree 9 in s^2, and a margin.
 bool pairs_in_range(const nnt_newton_schulz_cfg& c) {
-    double low = c.a, high = c.a, reach = 1.0;
+    double reach = 1.0;
     if (!in_range(c, &reach)) return false;
-    const double l = reach * reach;
-    for (double x : {l, c.c != 0.0 ? -c.b / (2.0 * c.c) : 0.0})
-        if (x > 0.0 && x <= l) {
-            const double p = c.a + c.b * x + c.c * x * x;
-            low = std::min(low, p);
-            high = std::max(high, p);
-        }
-    double most = std::max(std::fabs(low), std::fabs(high));
-    for (double p : {low * low, low * high, high * high})
-        for (bool first : {true, false}) most = std::max(most, std::fabs(p - kept_out(c, first)));
-    return most < 15.0;
+    double most = 0.0, last = 0.0;
+    for (int i = 0; i <= 4096; i++) {
+        const double l = reach * reach * i / 4096.0, at = std::max(std::sqrt(l), l);
+        const double p0 = c.a + c.b * l + c.c * l * l, r0 = c.b + c.c * l, r1 = p0 * p0 * (c.b + c.c * l * p0 * p0);
+        for (double r : {r0, p0, p0 * p0, r1}) most = std::max(most, at * std::fabs(r));
+        last = std::max(last, at * std::fabs(r1 * l * r0 + c.a * (r0 + r1)));
+    }
+    return most < 15.0 && last + c.a * c.a < 60.0;
 }
 
 bool whole_matrix(const nnt_ctx* ctx, const nnt_tensor* t) {
@@ -1152,13 +1332,16 @@ void launch_product(int mode, const NsGroup* g, const NsSizes& sizes, const NsOp
         case kGram:
             hipLaunchKernelGGL((ns_product_kernel<kGram, S>), grid, block, 0, st, g, sizes, op, now, splits);
             if constexpr (S::BM <= 128)
-                if (splits > 1) hipLaunchKernelGGL((ns_combine_kernel<S>), dim3(tiles * (S::kWaves * S::FM * S::FN / 4)), dim3(256), 0, st, g, sizes, splits);
+                if (splits > 1) hipLaunchKernelGGL((ns_combine_kernel<S>), dim3(tiles * (S::kWaves * S::FM * S::FN / 4)), dim3(256), 0, st, g, sizes, op, splits);
             break;
         case kPoly: hipLaunchKernelGGL((ns_product_kernel<kPoly, S>), grid, block, 0, st, g, sizes, op, now, 1); break;
         case kStep: hipLaunchKernelGGL((ns_product_kernel<kStep, S>), grid, block, 0, st, g, sizes, op, now, 1); break;
         default:
-            // (the results' way into the tensors' tiles does not fit the registers of the large shape)
-            if constexpr (S::BM <= 128) hipLaunchKernelGGL((ns_product_kernel<kLast, S>), grid, block, 0, st, g, sizes, op, now, 1);
+            // (two terms to add, or the results' way into the tensors' tiles, do not fit the registers of the large shape)
+            if constexpr (S::BM <= 128) {
+                if (mode == kPair) hipLaunchKernelGGL((ns_product_kernel<kPair, S>), grid, block, 0, st, g, sizes, op, now, 1);
+                else hipLaunchKernelGGL((ns_product_kernel<kLast, S>), grid, block, 0, st, g, sizes, op, now, 1);
+            }
             break;
     }
 }
@@ -1178,27 +1361,31 @@ struct Item {
 // The products of an iteration of `steps` steps.  Two steps can be taken at once: with A_1 = P_0 A_0 P_0, P = a I + b A + c A^2, the second one's polynomial comes
 // from square products alone, and X <- (P_1 P_0) X once: one product of X with itself and one with X (3 m^2 n flops) less for three square ones
 // (3 m^3) more.  A is recomputed from X after that, so what A_1 loses of the small singular values is not handed on.
-std::vector<Item> plan(const nnt_newton_schulz_cfg& c, bool pairs) {
+std::vector<Item> plan(const nnt_newton_schulz_cfg& c, int growth, bool pairs) {
     const float A = (float)c.a, B = (float)c.b, C = (float)c.c;
     std::vector<Item> out;
     int now = 0;
     for (int left = c.steps; left > 0;) {
         const bool two = pairs && left >= 2;
-        out.push_back(Item{kGram, NsOp{}, now});
+        const int from = grown_by(growth, c.steps - left);
+        auto poly = [&](int mode, int p, int q, int e, int d, int apart, float mul, float add, float diag) {
+            out.push_back(Item{mode, NsOp{p, q, e, d, apart, from, from, mul, add, diag}, now});
+        };
+        out.push_back(Item{kGram, NsOp{0, 0, 0, 0, 0, from, from, 1.f, 0.f, 0.f}, now});
+        const int factor = two ? 0 : 1;                      // the buffer of what X is multiplied by
+        float kept = A;
         if (two) {
-            const float out_of = (float)kept_out(c, left == c.steps);
-            out.push_back(Item{kPoly, NsOp{0, 0, 0, 1, C, B, 0.f}, now});        // B_0 = P_0 - a I
-            out.push_back(Item{kPoly, NsOp{1, 0, 0, 2, 1.f, A, 0.f}, now});      // P_0 A_0
-            out.push_back(Item{kPoly, NsOp{1, 2, 2, 3, 1.f, A, 0.f}, now});      // A_1 = P_0 (P_0 A_0)
-            out.push_back(Item{kPoly, NsOp{3, 3, 3, 2, C, B, A}, now});          // P_1
-            out.push_back(Item{kPoly, NsOp{2, 1, 2, 0, 1.f, A, -out_of}, now});  // P_1 P_0 without what is kept out
-            left -= 2;
-            out.push_back(Item{left ? kStep : kLast, NsOp{0, 0, 0, 0, 1.f, out_of, 0.f}, now});
+            kept = (float)kept_out(c, left == c.steps);
+            poly(kPoly, 0, 0, 0, 1, 0, C, B, 0.f);           // B_0 = P_0 - a I
+            poly(kPoly, 1, 0, 0, 2, 0, 1.f, A, 0.f);         // P_0 A_0
+            poly(kPoly, 1, 2, 2, 3, 0, 1.f, A, 0.f);         // A_1 = P_0 (P_0 A_0)
+            poly(kPoly, 3, 3, 3, 2, 0, C, B, 0.f);           // B_1 = P_1 - a I
+            poly(kPair, 2, 1, 0, 0, 1, 1.f, A, A * A - kept);    // P_1 P_0 = B_1 B_0 + a B_1 + a B_0 + a^2 I without what is kept out
         } else {
-            out.push_back(Item{kPoly, NsOp{0, 0, 0, 1, C, B, 0.f}, now});
-            left--;
-            out.push_back(Item{left ? kStep : kLast, NsOp{1, 0, 0, 0, 1.f, A, 0.f}, now});
+            poly(kPoly, 0, 0, 0, 1, 1, C, B, 0.f);
         }
+        left -= two ? 2 : 1;
+        out.push_back(Item{left ? kStep : kLast, NsOp{factor, 0, 0, 0, 0, from, grown_by(growth, c.steps - left), two ? (float)(1 << kPairShift) : 1.f, kept, 0.f}, now});
         now = 1 - now;
     }
     return out;
@@ -1210,10 +1397,10 @@ std::vector<Item> plan(const nnt_newton_schulz_cfg& c, bool pairs) {
 Launch choose(const NsSizes& g, int mode) {
     static const struct { int blocks; double lone, full, fixed; } kShapes[3] = {{1, 0.107, 0.12, 2.6}, {2, 0.25, 0.339, 4.0}, {4, 0.8, 1.18, 7.0}};
     constexpr double kCombine = 4.0;
-    const bool sym = mode == kGram || mode == kPoly;
+    const bool sym = mode == kGram || mode == kPoly || mode == kPair;
     Launch best;
     double best_time = 0.0;
-    for (int s = 0; s < (mode == kLast ? 2 : 3); s++) {
+    for (int s = 0; s < (mode == kLast || mode == kPair ? 2 : 3); s++) {
         const int u = kShapes[s].blocks;
         int64_t tiles = 0, panels = 0, longest = 0;
         double bytes = 0.0;                                                            // of the result path
@@ -1223,7 +1410,7 @@ Launch choose(const NsSizes& g, int mode) {
             tiles += t;
             panels += t * c;
             longest = std::max(longest, c);
-            bytes += 4096.0 * mb * (mode == kGram ? 4 * mb : mode == kPoly ? 6 * mb : mode == kStep ? 12 * nb : 16 * nb);
+            bytes += 4096.0 * mb * (mode == kGram ? 4 * mb : mode == kPoly ? 6 * mb : mode == kPair ? 8 * mb : mode == kStep ? 12 * nb : 16 * nb);
         }
         for (int splits = 1; splits <= 64; splits *= 2) {
             if (splits > 1 && (mode != kGram || s == 2 || tiles * splits > 512 || longest / splits < 8)) break;
@@ -1256,9 +1443,10 @@ struct Set {
     NsGroup g{};
     NsSizes sizes{};
     int kind = 0;                        // kProducts, kNarrow, kHeld
-    Launch launch[4];                    // by mode
+    Launch launch[5];                    // by mode
     std::vector<Item> items;
     int parts = 0;
+    unsigned norm_blocks = 0;
     int64_t patch = 0, bytes = 0;        // 64 x 64 blocks of all matrices; workspace
     double work = 0.0;
     std::vector<Access> acc;
@@ -1275,9 +1463,10 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
     g.b = (float)cfg.b;
     g.c = (float)cfg.c;
     g.eps = cfg.eps;
+    g.growth = growth_of(cfg);
     const bool narrow = kind == kNarrow;
     w.kind = kind;
-    int64_t bytes = (sizeof(NsGroup) + 255) / 256 * 256, chunks = 0, shortest = INT64_MAX;
+    int64_t bytes = (sizeof(NsGroup) + 255) / 256 * 256, shortest = INT64_MAX;
     std::vector<const nnt_tensor*> taken;                // inputs of this set
     while (*first < tasks.size() && g.n < kGroupMatrices && w.patch < 4096) {
         const Task& t = tasks[*first];
@@ -1302,14 +1491,19 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
         w.patch += mb * nb;
         shortest = std::min(shortest, m);
         if (kind != kProducts) w.parts = std::max(w.parts, narrow ? narrow_parts((int)nb) : (int)nb);
-        chunks = std::max(chunks, (t.G->base[0] * t.G->base[1] + kNormChunk - 1) / kNormChunk * t.G->grid[0] * t.G->grid[1]);
+        // squares are added up by as many workgroups as fill the chip; the set-up reads one sum per row and part
+        const int64_t rounds = (q.np + 255) / 256;
+        q.splits = (int32_t)std::min({rounds, std::max<int64_t>(1, 512 / mb), std::max<int64_t>(32, std::min<int64_t>(rounds / 16, 128))});
+        w.norm_blocks = std::max(w.norm_blocks, (unsigned)(mb * q.splits));
         // X and its transpose, two buffers each, and four square ones; narrow matrices: the transpose once, and two times A in parts
         const int64_t x = (int64_t)q.mp * q.np * 4, a = (int64_t)q.mp * q.mp * 4;
         q.X = bytes;
         q.XT = narrow ? bytes : q.X + 2 * x;
         q.A = narrow ? q.XT + x : q.XT + 2 * x;
-        q.part = q.A + (narrow ? (int64_t)narrow_parts((int)nb) * 64 * 64 * 4 * 2 : 4 * a);
-        bytes = q.part + kNormBlocks * 8;
+        q.squares = q.A + (narrow ? (int64_t)narrow_parts((int)nb) * 64 * 64 * 4 * 2 : 4 * a);
+        q.part = q.squares + (int64_t)q.splits * q.mp * 8;
+        q.exponents = q.part + mb * q.splits * 8;
+        bytes = (q.exponents + q.mp * 4 + 255) / 256 * 256;
         q.G = MatView{t.G->d_tiles, t.G->dtype};
         q.P = MatView{t.P->d_tiles, t.P->dtype};
         if (t.M) q.M = MatView{t.M->d_tiles, NNT_F32};
@@ -1324,15 +1518,14 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
     }
     w.sizes.n = g.n;
     if (kind == kHeld) return NNT_OK;                    // (needs no workspace)
-    g.norm_blocks = (int32_t)std::min<int64_t>(chunks, kNormBlocks);
     g.partial = bytes;
     if (kind == kProducts) {
-        for (int mode : {(int)kGram, (int)kPoly, (int)kStep, (int)kLast}) w.launch[mode] = choose(w.sizes, mode);
+        for (int mode : {(int)kGram, (int)kPoly, (int)kPair, (int)kStep, (int)kLast}) w.launch[mode] = choose(w.sizes, mode);
         const Launch& gram = w.launch[kGram];
         if (gram.splits > 1) bytes += (int64_t)gram.tiles * gram.splits * (gram.shape == 0 ? Small::BM * Small::BM : Middle::BM * Middle::BM) * 4;
         // (The model is a tenth and more off either way: two steps at once have to promise that much.  Below 256 rows they gain less, 128 x 6272 120 us instead of 128, and
         // their errors are larger than those of fp32 products, 128 x 1000 2.9e-6 after five steps instead of 1.7e-6.)
-        w.items = plan(cfg, shortest >= 256 && pairs_in_range(cfg) && 1.15 * 3.0 * w.launch[kPoly].time < gram.time + w.launch[kStep].time);
+        w.items = plan(cfg, g.growth, shortest >= 256 && pairs_in_range(cfg) && 1.15 * 3.0 * w.launch[kPoly].time < gram.time + w.launch[kStep].time);
     }
     w.bytes = bytes;
     return NNT_OK;
@@ -1354,12 +1547,12 @@ int32_t submit_set(nnt_ctx* ctx, const char* label, int steps, Set& w) {
             return launched();
         });
     return submit(ctx, w.acc, [&](hipStream_t st) {
-        hipLaunchKernelGGL(ns_norm_kernel, dim3((unsigned)g.norm_blocks, (unsigned)g.n), dim3(1024), 0, st, g);
+        hipLaunchKernelGGL(ns_norm_kernel, dim3(w.norm_blocks, (unsigned)g.n), dim3(1024), 0, st, g);
         if (w.kind == kNarrow) {
             const dim3 grid((unsigned)w.parts, (unsigned)g.n), block(256);
             hipLaunchKernelGGL((ns_narrow_kernel<kFirst>), grid, block, 0, st, there, w.sizes, 0);
-            for (int s = 0; s + 1 < steps; s++) hipLaunchKernelGGL((ns_narrow_kernel<kMiddle>), grid, block, 0, st, there, w.sizes, s & 1);
-            hipLaunchKernelGGL((ns_narrow_kernel<kFinal>), grid, block, 0, st, there, w.sizes, (steps - 1) & 1);
+            for (int s = 0; s + 1 < steps; s++) hipLaunchKernelGGL((ns_narrow_kernel<kMiddle>), grid, block, 0, st, there, w.sizes, s);
+            hipLaunchKernelGGL((ns_narrow_kernel<kFinal>), grid, block, 0, st, there, w.sizes, steps - 1);
             return launched();
         }
         hipLaunchKernelGGL(ns_split_kernel, dim3((unsigned)w.patch), dim3(256), 0, st, there, w.sizes);
