@@ -359,21 +359,24 @@ int32_t nnt_gpt2_block_adam(nnt_gpt2_block* b, int32_t step, const nnt_adam_cfg*
     return NNT_OK;
 }
 
-// Adam on the parameters that are no matrices.
-static int32_t vectors_adam(nnt_gpt2_block* b, int32_t step, const nnt_adam_cfg* cfg) {
+// What Adam on the parameters that are no matrices needs: nothing may stop it once the matrices have been updated.
+static int32_t vectors_prepare(nnt_gpt2_block* b) {
     nnt_ctx* ctx = b->ctx;
     constexpr int first = NNT_BLK_B_QKV, n = 12 - first;
+    nnt_tensor **G = b->s + NNT_BLK_GRAD + first, **P = b->s + first, **M = b->s + NNT_BLK_ADAM_M + first, **V = b->s + NNT_BLK_ADAM_V + first;
     if (ctx->granularity == NNT_GRAN_OP) {
-        if (!b->vector_group) {
-            if (ctx->capturing) return fail(ctx, NNT_ESTATE, "nnt_gpt2_block_muon: run the step once before capture");
-            nnt_tensor* lowp[n] = {};
-            TRY(adam_group_create(ctx, n, b->s + NNT_BLK_GRAD + first, b->s + first, b->s + NNT_BLK_ADAM_M + first, b->s + NNT_BLK_ADAM_V + first, lowp,
-                                  &b->vector_group));
-        }
-        return adam_group_step(ctx, b->vector_group, cfg, step);
+        if (b->vector_group) return NNT_OK;
+        if (ctx->capturing) return fail(ctx, NNT_ESTATE, "nnt_gpt2_block_muon: run the step once before capture");
+        nnt_tensor* lowp[n] = {};
+        return adam_group_create(ctx, n, G, P, M, V, lowp, &b->vector_group);
     }
-    for (int p = first; p < 12; p++)
-        TRY(nnt_adam_step(ctx, cfg, step, b->s[NNT_BLK_GRAD + p], b->s[p], b->s[NNT_BLK_ADAM_M + p], b->s[NNT_BLK_ADAM_V + p], nullptr));
+    for (int p = 0; p < n; p++) TRY(adam_check(ctx, G[p], P[p], M[p], V[p], nullptr));
+    return NNT_OK;
+}
+static int32_t vectors_adam(nnt_gpt2_block* b, int32_t step, const nnt_adam_cfg* cfg) {
+    if (b->ctx->granularity == NNT_GRAN_OP) return adam_group_step(b->ctx, b->vector_group, cfg, step);
+    for (int p = NNT_BLK_B_QKV; p < 12; p++)
+        TRY(nnt_adam_step(b->ctx, cfg, step, b->s[NNT_BLK_GRAD + p], b->s[p], b->s[NNT_BLK_ADAM_M + p], b->s[NNT_BLK_ADAM_V + p], nullptr));
     return NNT_OK;
 }
 
@@ -393,6 +396,7 @@ static int32_t blocks_muon(nnt_ctx* ctx, nnt_gpt2_block* const* blocks, size_t n
             LP.push_back(blocks[i]->cfg.dtype == NNT_BF16 ? s[NNT_BLK_LOWP + p] : nullptr);
         }
     }
+    for (size_t i = 0; i < n_blocks; i++) TRY(vectors_prepare(blocks[i]));
     TRY(nnt_muon_step(ctx, cfg, (int32_t)G.size(), G.data(), P.data(), M.data(), LP.data()));
     for (size_t i = 0; i < n_blocks; i++) TRY(vectors_adam(blocks[i], step, adam));
     return NNT_OK;
@@ -661,11 +665,14 @@ int32_t nnt_gpt2_model_backward(nnt_gpt2_model* m) {
 }
 
 // Adam on the model's own four parameters.
+static nnt_tensor* own_lowp(const nnt_gpt2_model* m, int p) { return (m->cfg.dtype == NNT_BF16 && p < 2) ? m->s[NNT_MDL_LOWP + p] : nullptr; }
+static int32_t own_check(nnt_gpt2_model* m) {
+    for (int p = 0; p < 4; p++) TRY(adam_check(m->ctx, m->s[NNT_MDL_GRAD + p], m->s[p], m->s[NNT_MDL_ADAM_M + p], m->s[NNT_MDL_ADAM_V + p], own_lowp(m, p)));
+    return NNT_OK;
+}
 static int32_t own_adam(nnt_gpt2_model* m, int32_t step, const nnt_adam_cfg* cfg) {
-    for (int p = 0; p < 4; p++) {
-        nnt_tensor* lowp = (m->cfg.dtype == NNT_BF16 && p < 2) ? m->s[NNT_MDL_LOWP + p] : nullptr;
-        TRY(nnt_adam_step(m->ctx, cfg, step, m->s[NNT_MDL_GRAD + p], m->s[p], m->s[NNT_MDL_ADAM_M + p], m->s[NNT_MDL_ADAM_V + p], lowp));
-    }
+    for (int p = 0; p < 4; p++)
+        TRY(nnt_adam_step(m->ctx, cfg, step, m->s[NNT_MDL_GRAD + p], m->s[p], m->s[NNT_MDL_ADAM_M + p], m->s[NNT_MDL_ADAM_V + p], own_lowp(m, p)));
     return NNT_OK;
 }
 
@@ -690,6 +697,7 @@ int32_t nnt_gpt2_model_muon(nnt_gpt2_model* m, const nnt_muon_cfg* cfg, int32_t 
     return entry(m->ctx, [&]() -> int32_t {
         if (!cfg || !adam || step < 1) return fail(m->ctx, NNT_EINVAL, "nnt_gpt2_model_muon: bad argument");
         if (!has_own_moments(m)) return fail(m->ctx, NNT_ESTATE, "nnt_gpt2_model_muon: the model was created without Adam moments");
+        TRY(own_check(m));
         TRY(nnt_gpt2_stack_muon(m->stack, cfg, step, adam));
         return own_adam(m, step, adam);
     });

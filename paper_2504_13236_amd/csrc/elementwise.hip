@@ -390,14 +390,28 @@ int32_t nnt_bias_add(nnt_ctx* ctx, nnt_tensor* b, nnt_tensor* Y) {
     return NNT_OK;
 }
 
-int32_t nnt_adam_step(nnt_ctx* ctx, const nnt_adam_cfg* cfg, int32_t step, nnt_tensor* G, nnt_tensor* P,
-                      nnt_tensor* M, nnt_tensor* V, nnt_tensor* LP) {
-    NNT_CHECK_CTX(ctx);
-    if (!cfg || !G || !P || !M || !V || step < 1) return fail(ctx, NNT_EINVAL, "nnt_adam_step: bad argument");
+}  // extern "C"
+
+namespace nnt {
+int32_t adam_check(nnt_ctx* ctx, nnt_tensor* G, nnt_tensor* P, nnt_tensor* M, nnt_tensor* V, nnt_tensor* LP) {
+    if (!G || !P || !M || !V) return fail(ctx, NNT_EINVAL, "nnt_adam_step: bad argument");
     if (!same_tiling(G, P) || !same_tiling(G, M) || !same_tiling(G, V) || (LP && !same_tiling(G, LP)))
         return fail(ctx, NNT_EINVAL, "nnt_adam_step: operands tiled differently");
     if (G->dtype != NNT_F32 || P->dtype != NNT_F32 || M->dtype != NNT_F32 || V->dtype != NNT_F32 || (LP && LP->dtype != NNT_BF16))
         return fail(ctx, NNT_EDTYPE, "nnt_adam_step: g, p, m, v must be fp32 and the low-precision copy bf16");
+    if (P->ntiles > 65535) return fail(ctx, NNT_EINVAL, "too many tiles for one launch");
+    return NNT_OK;
+}
+}  // namespace nnt
+
+extern "C" {
+
+int32_t nnt_adam_step(nnt_ctx* ctx, const nnt_adam_cfg* cfg, int32_t step, nnt_tensor* G, nnt_tensor* P,
+                      nnt_tensor* M, nnt_tensor* V, nnt_tensor* LP) {
+    NNT_CHECK_CTX(ctx);
+    if (!cfg || step < 1) return fail(ctx, NNT_EINVAL, "nnt_adam_step: bad argument");
+    const int32_t rc = adam_check(ctx, G, P, M, V, LP);
+    if (rc != NNT_OK) return rc;
     const bool vec = all_aligned(G) && all_aligned(P) && all_aligned(M) && all_aligned(V) && (!LP || all_aligned(LP));
     OpTag tag(ctx, "adam", present_numel(P) * (28 + (LP ? 2 : 0)), true);
     AdamF base = make_adam(step, cfg->lr, cfg->beta1, cfg->beta2, cfg->eps, cfg->weight_decay, present_numel(P) * 30.0);

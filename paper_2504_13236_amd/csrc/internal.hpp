@@ -234,6 +234,8 @@ int32_t static_scratch_setup();      // looks up the current device's address of
 
 // Adam on several parameter tensors in one launch (elementwise.hip); the group owns small device tables.
 struct AdamGroup;
+// whether nnt_adam_step takes these operands
+int32_t adam_check(nnt_ctx* ctx, nnt_tensor* G, nnt_tensor* P, nnt_tensor* M, nnt_tensor* V, nnt_tensor* LP);
 int32_t adam_group_create(nnt_ctx* ctx, int n, nnt_tensor* const* G, nnt_tensor* const* P, nnt_tensor* const* M,
                           nnt_tensor* const* V, nnt_tensor* const* LP, AdamGroup** out);
 int32_t adam_group_step(nnt_ctx* ctx, AdamGroup* a, const nnt_adam_cfg* cfg, int32_t step);

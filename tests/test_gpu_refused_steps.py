@@ -1,0 +1,62 @@
+"""What a refused optimiser step or forward pass of the language model leaves as it was."""
+import ctypes as C
+from types import SimpleNamespace
+
+import numpy as np
+import pytest
+
+from test_gpu_post_training import MATRICES, Problem, check_muon, close, snapshot
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mods():
+    from paper_2504_13236_amd import capi, tiled
+    return capi, tiled
+
+
+def with_gradients(q, tiled, ctx):
+    m = q.model(tiled, ctx)
+    logp = m.per_position()
+    m.forward_preference(logp)
+    m.backward()
+    ctx.wait()
+    return m
+
+
+@pytest.mark.parametrize("whose", ["block", "stack", "model"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_muon_refused_inside_a_capture_records_nothing(mods, whose, dtype):
+    """The vectors' table of pointers does not exist yet and cannot be made there: neither may the matrices be updated."""
+    capi, tiled = mods
+    q = Problem(dtype)
+    with tiled.Context(n_streams=2) as ctx:
+        m = with_gradients(q, tiled, ctx)
+        cfg, acfg = tiled.muon_cfg(lr=0.02, momentum=0.9), capi.nnt_adam_cfg(1e-3, 0.9, 0.999, 1e-8, 0.0)
+        call, h = {"block": (capi.nnt_gpt2_block_muon, m.blocks[1].h), "stack": (capi.nnt_gpt2_stack_muon, m.stack.h), "model": (capi.nnt_gpt2_model_muon, m.h)}[whose]
+        if whose != "block":
+            m.blocks[0].muon(1, lr=0.0)                       # the first block is prepared, the second is not
+        # the matrices' workspace is there
+        tiled.muon_step(ctx, *[[f(b, k) for b in m.blocks for k in MATRICES] for f in (lambda b, k: b.grad(k), lambda b, k: b.param(k), lambda b, k: b.moment(k, "m"))], lr=0.0)
+        ctx.wait()
+        before = snapshot(m)
+        g = C.c_void_p()
+        capi.nnt_capture_begin(ctx.h)
+        launches = ctx.stats()["launches"]
+        assert call.raw(h, C.byref(cfg), 1, C.byref(acfg)) == capi.NNT_ESTATE
+        assert ctx.stats()["launches"] == launches
+        capi.nnt_capture_end(ctx.h, C.byref(g))
+        capi.nnt_graph_launch(g)
+        ctx.wait()
+        capi.nnt_graph_destroy(g)
+        for (p0, m0), (p1, m1) in zip(before, snapshot(m)):
+            for k in MATRICES:
+                np.testing.assert_array_equal(p0[k], p1[k])
+                np.testing.assert_array_equal(m0[k], m1[k])
+        # the same call outside of a capture is one whole step
+        if whose == "block":
+            assert call.raw(h, C.byref(cfg), 1, C.byref(acfg)) == capi.NNT_OK
+            check_muon(SimpleNamespace(blocks=m.blocks[1:], capi=capi), before[1:], 0.02, dict(lr=0.02, momentum=0.9, nesterov=True, scale="rms"))
+        ctx.wait()
+        close(m)
