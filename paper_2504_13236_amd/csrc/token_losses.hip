@@ -243,8 +243,8 @@ __device__ __forceinline__ void policy_of(const Logits& a, const PolicyArgs& p, 
     } else {
         adv = global_as<const float>(p.adv[c.stat_tile])[c.colidx];
     }
-    // (against itself: 1, but NaN for a column that holds one)
-    const double d = logp - (p.old_logp ? (double)global_as<const float>(p.old_logp[c.stat_tile])[c.colidx] : logp);
+    // (against itself: 1, also for a banned token, whose logp is -inf, but NaN for a column that holds one)
+    const double d = p.old_logp ? logp - (double)global_as<const float>(p.old_logp[c.stat_tile])[c.colidx] : logp == logp ? 0.0 : logp;
     const float r = expf((float)d);
     // (no advantage is no loss, also where the ratio is beyond 32 bits: up to exp(709) it is a number)
     const float free = adv == 0.f && d < 709.0 ? 0.f : r * adv, held = fminf(fmaxf(r, p.lo), p.hi) * adv;
