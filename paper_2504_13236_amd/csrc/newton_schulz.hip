@@ -1546,6 +1546,7 @@ int32_t submit_set(nnt_ctx* ctx, const char* label, int steps, Set& w) {
             hipLaunchKernelGGL(ns_held_kernel, dim3((unsigned)g.n), dim3(256u * w.parts), 0, st, g, steps);
             return launched();
         });
+    const int grams = (int)std::count_if(w.items.begin(), w.items.end(), [](const Item& t) { return t.mode == kGram; });      // each with a launch that adds up its parts, if it is cut
     return submit(ctx, w.acc, [&](hipStream_t st) {
         hipLaunchKernelGGL(ns_norm_kernel, dim3(w.norm_blocks, (unsigned)g.n), dim3(1024), 0, st, g);
         if (w.kind == kNarrow) {
@@ -1563,7 +1564,7 @@ int32_t submit_set(nnt_ctx* ctx, const char* label, int steps, Set& w) {
             else launch_product<Small>(t.mode, there, w.sizes, t.op, t.now, l.tiles, l.splits, st);
         }
         return launched();
-    }, w.kind == kNarrow ? 2 + steps : 2 + (int)w.items.size() + (w.launch[kGram].splits > 1 ? steps : 0));
+    }, w.kind == kNarrow ? 2 + steps : 2 + (int)w.items.size() + (w.launch[kGram].splits > 1 ? grams : 0));
 }
 
 // Orthogonalises the matrices of `tasks` and applies the results.  mu < 0: no momentum.  Nothing is launched before all sets are known to fit.

@@ -144,3 +144,17 @@ def test_other_coefficients(mods, shape, steps, a, b, c):
     want = D.orthogonalize(G, a, b, c, 1e-7, steps)
     plain, got = (rows_off(f, want) for f in (fp32_products(G, steps, 1e-7, a, b, c), orthogonalize(mods, G, steps, 1e-7, (256, 1024), a, b, c)))
     assert got <= ROW * max(plain, 2.0 ** -24 * steps), "%.2e of a row, fp32 products %.2e" % (got, plain)
+
+
+@pytest.mark.parametrize("shape,steps,launches", [((64, 256), 5, 1), ((40, 900), 5, 2 + 5), ((512, 512), 1, 2 + 3), ((777, 1111), 5, 2 + 3 * 5),
+                                                  # two steps at once: 7 products in place of 6, and X X^T once, whose parts are added up by a launch of their own
+                                                  ((512, 2560), 1, 2 + 4), ((512, 2560), 2, 2 + 8), ((512, 2560), 4, 2 + 16), ((512, 2560), 5, 2 + 16 + 4), ((2560, 512), 5, 2 + 16 + 4)])
+def test_launches_are_counted(mods, shape, steps, launches):
+    capi, tiled = mods
+    with tiled.Context(n_streams=1) as ctx:
+        tG, tO = (tiled.TiledTensor(ctx, "f32", shape, (256, 1024), fill=0) for _ in range(2))
+        cfg = capi.nnt_newton_schulz_cfg(A, B, CC, 1e-7, steps)
+        before = ctx.stats()["launches"]
+        capi.nnt_orthogonalize(ctx.h, C.byref(cfg), 1, handles(mods, [tG]), handles(mods, [tO]))
+        assert ctx.stats()["launches"] - before == launches
+        ctx.wait()
