@@ -562,7 +562,8 @@ NNT_API int32_t nnt_sgd_step(nnt_ctx* ctx, const nnt_sgd_cfg* cfg, nnt_tensor* G
  * As many matrices as fill the chip (at most 16) go through one set of launches; G and O are arrays of n pointers.  One
  * task per set, whatever the context's granularity; it uses a workspace of the context, about 16 bytes per element
  * of the set's matrices and 16 per element of their Gram matrices, twice that (two sets side by side) for sets of up to 512 MiB
- * on several streams; matrices of at most 64 x 256 use none.  It must exist before a graph capture (run the call once).  NNT_ENOMEM (nothing has been launched, the context stays usable): no memory for it.  At most 65535 x 64
+ * on several streams, where there is memory for that; matrices of at most 64 x 256 use none.  It must exist before a graph capture (run the call once).  NNT_ENOMEM: no memory
+ * for it; nothing has been launched, and the workspace that was there before is there again.  At most 65535 x 64
  * rows or columns and 2^36 elements a matrix. */
 typedef struct nnt_newton_schulz_cfg {
     double a, b, c, eps;

@@ -336,27 +336,55 @@ int32_t ensure_stream_scratch(nnt_ctx* ctx, int64_t elems) {
     return grow_scratch(ctx, &ctx->stream_scratch, &ctx->stream_scratch_elems, &ctx->stream_mem, elems, ctx->n_streams);
 }
 
-// (Several GB for the largest matrices: a lack of memory is the caller's to deal with, not the end of the context.)
-int32_t ensure_matrix_scratch(nnt_ctx* ctx, int64_t half, int64_t whole) {
-    const int64_t have = ctx->matrix_mem ? ctx->matrix_mem->bytes : 0;
-    if (half <= ctx->matrix_half && whole <= have) return NNT_OK;
-    half = std::max((half + 0xfff) / 0x1000 * 0x1000, ctx->matrix_half);
-    const int64_t bytes = std::max({whole, half * std::min(ctx->n_streams, 2), have});
-    if (ctx->capturing) return fail(ctx, NNT_ESTATE, "the workspace of matrix iterations must exist before capture: run the operation once first");
-    const int32_t rc = sync_all(ctx);
-    if (rc != NNT_OK) return rc;
-    ctx->matrix_scratch = nullptr;
-    ctx->matrix_half = 0;
-    replace_mem(ctx, &ctx->matrix_mem);
+static std::shared_ptr<Scratch> scratch_if_possible(int64_t bytes) {
     std::shared_ptr<Scratch> fresh(new Scratch());
     fresh->bytes = (bytes + 0xfffff) / 0x100000 * 0x100000;
     if (hipMalloc((void**)&fresh->p, (size_t)fresh->bytes) != hipSuccess) {
         fresh->p = nullptr;
         (void)hipGetLastError();
-        return fail(ctx, NNT_ENOMEM, "no memory for the workspace of matrix iterations: " + std::to_string(fresh->bytes) + " bytes");
+        return nullptr;
+    }
+    return fresh;
+}
+
+// (Several GB for the largest matrices: a lack of memory is the caller's to deal with, not the end of the context.)
+int32_t ensure_matrix_scratch(nnt_ctx* ctx, int64_t half, int64_t whole) {
+    const int64_t have = ctx->matrix_mem ? ctx->matrix_mem->bytes : 0;
+    if (half <= ctx->matrix_half && whole <= have) return NNT_OK;
+    half = std::max((half + 0xfff) / 0x1000 * 0x1000, ctx->matrix_half);
+    if (ctx->capturing) return fail(ctx, NNT_ESTATE, "the workspace of matrix iterations must exist before capture: run the operation once first");
+    const int32_t rc = sync_all(ctx);
+    if (rc != NNT_OK) return rc;
+    // What is there goes first (a graph may keep it).  Two halves let sets run side by side; where there is no memory for the second, they take turns in one.
+    std::shared_ptr<Scratch> old = ctx->matrix_mem;
+    const bool kept = old.use_count() > 2;
+    if (!kept) {
+        ctx->matrix_mem.reset();
+        old.reset();
+    }
+    int halves = std::min(ctx->n_streams, 2);
+    std::shared_ptr<Scratch> fresh = scratch_if_possible(std::max({whole, half * halves, have}));
+    if (!fresh) {
+        halves = 1;
+        fresh = scratch_if_possible(std::max(whole, half));
+    }
+    if (!fresh) {
+        // what was there stays there: smaller sets go on, inside a capture too
+        const int64_t wanted = std::max(whole, half);
+        if (!kept && have) {
+            ctx->matrix_mem = scratch_if_possible(have);
+            ctx->matrix_scratch = ctx->matrix_mem ? reinterpret_cast<char*>(ctx->matrix_mem->p) : nullptr;
+            if (!ctx->matrix_mem) ctx->matrix_half = 0;
+        }
+        return fail(ctx, NNT_ENOMEM, "no memory for the workspace of matrix iterations: " + std::to_string(wanted) + " bytes");
+    }
+    if (kept) {
+        old.reset();
+        replace_mem(ctx, &ctx->matrix_mem);
     }
     ctx->matrix_scratch = reinterpret_cast<char*>(fresh->p);
     ctx->matrix_half = half;
+    ctx->matrix_halves = halves;
     ctx->matrix_mem = std::move(fresh);
     return NNT_OK;
 }

@@ -167,6 +167,7 @@ struct nnt_ctx {
     // what the Newton-Schulz iterations of matrices work in: two halves for tasks that run side by side, or all of it for one
     char* matrix_scratch = nullptr;
     int64_t matrix_half = 0;                 // bytes
+    int matrix_halves = 1;                   // two, or one where memory was short
     unsigned matrix_turn = 0;
     std::shared_ptr<nnt::Scratch> matrix_mem;
     nnt::TileDep matrix_dep[2];
@@ -224,7 +225,7 @@ int32_t submit(nnt_ctx* ctx, const std::vector<Access>& acc,
                const std::function<int32_t(hipStream_t)>& launch, int n_launches = 1);
 int32_t ensure_scratch(nnt_ctx* ctx, int64_t elems);
 int32_t ensure_stream_scratch(nnt_ctx* ctx, int64_t elems);
-// halves of at least `half` bytes (of one stream: one), and at least `whole` bytes in all
+// halves of at least `half` bytes (of one stream, or without memory for two: one), and at least `whole` bytes in all
 int32_t ensure_matrix_scratch(nnt_ctx* ctx, int64_t half, int64_t whole);
 // inside a task's launch function: the part of the stream it has been given (as large as every ensure_stream_scratch so far)
 inline float* stream_scratch_of(const nnt_ctx* ctx) { return ctx->stream_scratch + ctx->cur_stream * ctx->stream_scratch_elems; }

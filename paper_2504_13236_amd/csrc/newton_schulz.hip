@@ -1534,9 +1534,10 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
 int32_t submit_set(nnt_ctx* ctx, const char* label, int steps, Set& w) {
     NsGroup g = w.g;
     if (w.kind != kHeld) {
-        const int half = w.whole() || ctx->n_streams == 1 ? 0 : ctx->matrix_turn++ & 1;
+        const bool alone = w.whole() || ctx->matrix_halves == 1;
+        const int half = alone ? 0 : ctx->matrix_turn++ & 1;
         for (int k = 0; k < 2; k++)
-            if (k == half || w.whole()) w.acc.push_back(Access{&ctx->matrix_dep[k], 1, kReadWrite});
+            if (k == half || alone) w.acc.push_back(Access{&ctx->matrix_dep[k], 1, kReadWrite});
         g.space = ctx->matrix_scratch + half * ctx->matrix_half;
     }
     const NsGroup* there = reinterpret_cast<const NsGroup*>(g.space);

@@ -1,0 +1,104 @@
+"""The workspace of the matrix iterations where memory is short."""
+import ctypes as C
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mods():
+    from paper_2504_13236_amd import capi, tiled
+    return capi, tiled
+
+
+MB = 1 << 20
+
+
+def all_but(free):
+    """Blocks that leave about `free` bytes of the device's memory (what it reports as free is less than what it gives)."""
+    torch.cuda.empty_cache()
+    blocks = [torch.empty(max(0, torch.cuda.mem_get_info()[0] - 1024 * MB), dtype=torch.uint8, device="cuda")]
+    try:
+        for _ in range(1000):
+            blocks.append(torch.empty(30 * MB, dtype=torch.uint8, device="cuda"))
+    except torch.cuda.OutOfMemoryError:
+        pass
+    for _ in range(free // (30 * MB)):
+        blocks.pop()
+    torch.cuda.empty_cache()
+    return blocks
+
+
+def test_workspace_where_memory_is_short(mods):
+    """Room for one half but not for two: the call goes through, with the same results.  Room for neither: it is refused, and smaller calls go on as before."""
+    capi, tiled = mods
+    cfg = capi.nnt_newton_schulz_cfg(3.4445, -4.7750, 2.0315, 1e-7, 2)
+    shapes = dict(small=(300, 500), middle=(2048, 6000), large=(4096, 12000))      # about 5, 270 and 1100 MB of workspace
+
+    def tensors(ctx):
+        t = {}
+        for k, s in shapes.items():
+            G, O = (tiled.TiledTensor(ctx, "f32", s, s) for _ in range(2))
+            G.buf.view(torch.float32).normal_(generator=torch.Generator(device="cuda").manual_seed(len(k)))
+            t[k] = (G, O)
+        torch.cuda.synchronize()
+        return t
+
+    def go(ctx, t, *which):
+        a = [capi.ptr_array([t[k][i].h.value for k in which]) for i in (0, 1)]
+        rc = capi.nnt_orthogonalize.raw(ctx.h, C.byref(cfg), len(which), *a)
+        ctx.wait()
+        return rc
+    with tiled.Context(n_streams=1) as ctx:
+        t = tensors(ctx)
+        want = {}
+        for k in ("small", "middle"):
+            assert go(ctx, t, k) == capi.NNT_OK
+            want[k] = t[k][1].buf.clone()
+    with tiled.Context(n_streams=2) as ctx:
+        t = tensors(ctx)
+        assert go(ctx, t, "small") == capi.NNT_OK
+        fill = None
+        try:
+            fill = all_but(420 * MB)
+            t["small"][1].buf.zero_()
+            assert go(ctx, t, "middle") == capi.NNT_OK
+            assert torch.equal(t["middle"][1].buf, want["middle"])
+            assert ctx.stats()["device_workspace_bytes"] < 420 * MB
+            # two sets of that size, one after the other in the one half
+            for k in ("middle", "small"):
+                t[k][1].buf.zero_()
+            torch.cuda.synchronize()
+            a = [[capi.ptr_array([t[k][i].h.value]) for i in (0, 1)] for k in ("middle", "small", "middle", "small")]
+            for x in a:
+                assert capi.nnt_orthogonalize.raw(ctx.h, C.byref(cfg), 1, *x) == capi.NNT_OK
+            ctx.wait()
+            assert all(torch.equal(t[k][1].buf, want[k]) for k in want)
+            # no room: nothing is launched, what was there is there again, and may be captured
+            held, launches = ctx.stats()["device_workspace_bytes"], ctx.stats()["launches"]
+            for _ in range(2):
+                assert go(ctx, t, "large") == capi.NNT_ENOMEM
+            assert ctx.stats()["device_workspace_bytes"] == held and ctx.stats()["launches"] == launches
+            g = C.c_void_p()
+            capi.nnt_capture_begin(ctx.h)
+            rc = capi.nnt_orthogonalize.raw(ctx.h, C.byref(cfg), 1, *a[0])
+            capi.nnt_capture_end(ctx.h, C.byref(g))
+            assert rc == capi.NNT_OK
+            # a graph keeps its own
+            assert go(ctx, t, "large") == capi.NNT_ENOMEM
+            for _ in range(3):
+                t["middle"][1].buf.zero_()
+                torch.cuda.synchronize()
+                capi.nnt_graph_launch(g)
+                ctx.wait()
+                assert torch.equal(t["middle"][1].buf, want["middle"])
+            capi.nnt_graph_destroy(g)
+            assert go(ctx, t, "small") == capi.NNT_OK and torch.equal(t["small"][1].buf, want["small"])
+        finally:
+            del fill
+            torch.cuda.empty_cache()
+        # with memory again
+        assert go(ctx, t, "large") == capi.NNT_OK
+        assert go(ctx, t, "middle") == capi.NNT_OK and torch.equal(t["middle"][1].buf, want["middle"])
