@@ -608,7 +608,8 @@ int32_t nnt_gpt2_model_forward(nnt_gpt2_model* m, const int32_t* tokens, const i
 int32_t nnt_gpt2_model_logprob(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions, const int32_t* labels, nnt_tensor* logp) {
     if (!m) return NNT_EINVAL;
     return entry(m->ctx, [&]() -> int32_t {
-        if (!tokens || !positions || !labels || !logp) return fail(m->ctx, NNT_EINVAL, "nnt_gpt2_model_logprob: null argument");
+        if (!tokens || !positions) return fail(m->ctx, NNT_EINVAL, "nnt_gpt2_model_logprob: null argument");
+        TRY(token_logprob_check(m->ctx, m->s[NNT_MDL_LOGITS], labels, logp));
         m->tokens = m->positions = nullptr;      // the logits hold no gradient: there is nothing to go backward from
         TRY(model_logits(m, tokens, positions));
         return nnt_token_logprob(m->ctx, m->s[NNT_MDL_LOGITS], labels, logp);
@@ -620,7 +621,8 @@ int32_t nnt_gpt2_model_forward_policy(nnt_gpt2_model* m, const int32_t* tokens, 
                                       float* losses, float* loss) {
     if (!m) return NNT_EINVAL;
     return entry(m->ctx, [&]() -> int32_t {
-        if (!tokens || !positions || !labels) return fail(m->ctx, NNT_EINVAL, "nnt_gpt2_model_forward_policy: null argument");
+        if (!tokens || !positions) return fail(m->ctx, NNT_EINVAL, "nnt_gpt2_model_forward_policy: null argument");
+        TRY(policy_loss_check(m->ctx, cfg, m->s[NNT_MDL_LOGITS], labels, old_logp, ref_logp, advantages, m->s[NNT_MDL_LOGITS], logp, losses, loss));
         m->tokens = m->positions = nullptr;
         TRY(model_logits(m, tokens, positions));
         TRY(nnt_policy_loss(m->ctx, cfg, m->s[NNT_MDL_LOGITS], labels, old_logp, ref_logp, advantages, m->s[NNT_MDL_LOGITS], logp, losses, loss));
@@ -634,7 +636,8 @@ int32_t nnt_gpt2_model_forward_preference(nnt_gpt2_model* m, const int32_t* toke
                                           const nnt_preference_cfg* cfg, nnt_tensor* ref_logp, nnt_tensor* logp, float* rewards, float* losses, float* loss) {
     if (!m) return NNT_EINVAL;
     return entry(m->ctx, [&]() -> int32_t {
-        if (!tokens || !positions || !labels) return fail(m->ctx, NNT_EINVAL, "nnt_gpt2_model_forward_preference: null argument");
+        if (!tokens || !positions) return fail(m->ctx, NNT_EINVAL, "nnt_gpt2_model_forward_preference: null argument");
+        TRY(preference_loss_check(m->ctx, cfg, m->s[NNT_MDL_LOGITS], labels, ref_logp, m->s[NNT_MDL_LOGITS], logp, rewards, losses, loss));
         m->tokens = m->positions = nullptr;
         TRY(model_logits(m, tokens, positions));
         TRY(nnt_preference_loss(m->ctx, cfg, m->s[NNT_MDL_LOGITS], labels, ref_logp, m->s[NNT_MDL_LOGITS], logp, rewards, losses, loss));

@@ -256,6 +256,13 @@ inline bool null_alike(const nnt_tensor* a, const nnt_tensor* b) {
     return true;
 }
 
+// whether the losses on given tokens take these operands; their scratch is there afterwards (token_losses.hip)
+int32_t token_logprob_check(nnt_ctx* ctx, nnt_tensor* X, const int32_t* labels, nnt_tensor* logp);
+int32_t policy_loss_check(nnt_ctx* ctx, const nnt_policy_cfg* cfg, nnt_tensor* X, const int32_t* labels, nnt_tensor* old_logp, nnt_tensor* ref_logp,
+                          nnt_tensor* advantages, nnt_tensor* dX, nnt_tensor* logp, float* losses, float* loss);
+int32_t preference_loss_check(nnt_ctx* ctx, const nnt_preference_cfg* cfg, nnt_tensor* X, const int32_t* labels, nnt_tensor* ref_logp, nnt_tensor* dX,
+                              nnt_tensor* logp, float* rewards, float* losses, float* loss);
+
 // Makes a context's device the current one of the calling thread for as long as it lives.
 struct DeviceScope {
     int before = -1;

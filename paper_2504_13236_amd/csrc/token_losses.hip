@@ -577,7 +577,7 @@ int threads_of(int dtype, int64_t nvec, int64_t ncols, bool streams) {
 
 using PolicyFn = void (*)(Logits, PolicyArgs);
 // the instance that holds a column of `nvec` vectors with the fewest registers, and its workgroup size
-PolicyFn policy_of(int dtype, int64_t nvec, int64_t ncols, int* nt) {
+PolicyFn policy_instance(int dtype, int64_t nvec, int64_t ncols, int* nt) {
     *nt = threads_of(dtype, nvec, ncols, false);
     const int64_t per = (nvec + *nt - 1) / *nt;
     if (dtype == NNT_F32) {
@@ -649,17 +649,66 @@ const float* const* in_tiles(nnt_tensor* t) { return t ? reinterpret_cast<const 
     } while (0)
 
 }  // namespace
+
+// What the entry points ask of their arguments, and the scratch that they need: the language model asks before its forward pass.
+int32_t token_logprob_check(nnt_ctx* ctx, nnt_tensor* X, const int32_t* labels, nnt_tensor* logp) {
+    const std::string who = "nnt_token_logprob";
+    if (!X || !labels || !logp) return fail(ctx, NNT_EINVAL, who + ": null argument");
+    Logits a;
+    TRY(take_logits(ctx, who, X, labels, &a));
+    return check_positions(ctx, who, "logp", X, logp);
+}
+
+int32_t policy_loss_check(nnt_ctx* ctx, const nnt_policy_cfg* cfg, nnt_tensor* X, const int32_t* labels, nnt_tensor* old_logp, nnt_tensor* ref_logp,
+                          nnt_tensor* advantages, nnt_tensor* dX, nnt_tensor* logp, float* losses, float* loss) {
+    const std::string who = "nnt_policy_loss";
+    if (!cfg || !X || !labels || !advantages || !logp || !losses || !loss) return fail(ctx, NNT_EINVAL, who + ": null argument");
+    if (!(cfg->clip_low >= 0.0 && cfg->clip_low <= 1.0) || !(cfg->clip_high >= 0.0 && cfg->clip_high < 1e30) || !(cfg->kl_coef >= 0.0 && cfg->kl_coef < 1e30) ||
+        cfg->reduction < NNT_REDUCE_SUM || cfg->reduction > NNT_REDUCE_SEQUENCES)
+        return fail(ctx, NNT_EINVAL, who + ": bad configuration");
+    if (cfg->kl_coef > 0.0 && !ref_logp) return fail(ctx, NNT_EINVAL, who + ": a KL term needs the reference's log-probabilities");
+    Logits a;
+    TRY(take_logits(ctx, who, X, labels, &a));
+    TRY(check_positions(ctx, who, "logp", X, logp));
+    if (old_logp) TRY(check_positions(ctx, who, "old_logp", X, old_logp));
+    if (ref_logp) TRY(check_positions(ctx, who, "ref_logp", X, ref_logp));
+    if (advantages->ndim == 1) {
+        if (advantages->ctx != ctx || advantages->dtype != NNT_F32 || advantages->shape[0] != X->shape[2] || advantages->base[0] != X->base[2] || !all_there(advantages))
+            return fail(ctx, NNT_EINVAL, who + ": advantages per sequence must be fp32 [N_b], tiled like the logits' last axis, all tiles present");
+    } else {
+        TRY(check_positions(ctx, who, "advantages", X, advantages));
+    }
+    TRY(check_gradient(ctx, who, X, dX));
+    if (logp == old_logp || logp == ref_logp || logp == advantages) return fail(ctx, NNT_EINVAL, who + ": logp must not be one of the inputs");
+    return cfg->reduction == NNT_REDUCE_SUM ? (int32_t)NNT_OK : ensure_stream_scratch(ctx, X->shape[2]);
+}
+
+int32_t preference_loss_check(nnt_ctx* ctx, const nnt_preference_cfg* cfg, nnt_tensor* X, const int32_t* labels, nnt_tensor* ref_logp, nnt_tensor* dX,
+                              nnt_tensor* logp, float* rewards, float* losses, float* loss) {
+    const std::string who = "nnt_preference_loss";
+    if (!cfg || !X || !labels || !logp || !rewards || !losses || !loss) return fail(ctx, NNT_EINVAL, who + ": null argument");
+    if (!(cfg->beta > 0.0 && cfg->beta < 1e30) || !(cfg->label_smoothing >= 0.0 && cfg->label_smoothing <= 0.5) ||
+        (cfg->reduction != NNT_REDUCE_SUM && cfg->reduction != NNT_REDUCE_SEQUENCES))
+        return fail(ctx, NNT_EINVAL, who + ": bad configuration");
+    Logits a;
+    TRY(take_logits(ctx, who, X, labels, &a));
+    if (X->shape[2] % 2) return fail(ctx, NNT_EINVAL, who + ": pairs need an even batch");
+    TRY(check_positions(ctx, who, "logp", X, logp));
+    if (ref_logp) TRY(check_positions(ctx, who, "ref_logp", X, ref_logp));
+    TRY(check_gradient(ctx, who, X, dX));
+    if (logp == ref_logp) return fail(ctx, NNT_EINVAL, who + ": logp must not be one of the inputs");
+    return ensure_stream_scratch(ctx, 4 * X->shape[1] * X->shape[2] + 2 * X->shape[2]);
+}
+
 }  // namespace nnt
 
 using namespace nnt;
 
 int32_t nnt_token_logprob(nnt_ctx* ctx, nnt_tensor* X, const int32_t* labels, nnt_tensor* logp) {
     return entry(ctx, [&]() -> int32_t {
-        const std::string who = "nnt_token_logprob";
-        if (!X || !labels || !logp) return fail(ctx, NNT_EINVAL, who + ": null argument");
+        TRY(token_logprob_check(ctx, X, labels, logp));
         Logits a;
-        TRY(take_logits(ctx, who, X, labels, &a));
-        TRY(check_positions(ctx, who, "logp", X, logp));
+        TRY(take_logits(ctx, "nnt_token_logprob", X, labels, &a));
         const int64_t ncols = X->shape[1] * X->shape[2];
         const int dt = X->dtype;
         float* const* out = out_tiles(logp);
@@ -674,36 +723,18 @@ int32_t nnt_token_logprob(nnt_ctx* ctx, nnt_tensor* X, const int32_t* labels, nn
 int32_t nnt_policy_loss(nnt_ctx* ctx, const nnt_policy_cfg* cfg, nnt_tensor* X, const int32_t* labels, nnt_tensor* old_logp, nnt_tensor* ref_logp,
                         nnt_tensor* advantages, nnt_tensor* dX, nnt_tensor* logp, float* losses, float* loss) {
     return entry(ctx, [&]() -> int32_t {
-        const std::string who = "nnt_policy_loss";
-        if (!cfg || !X || !labels || !advantages || !logp || !losses || !loss) return fail(ctx, NNT_EINVAL, who + ": null argument");
-        if (!(cfg->clip_low >= 0.0 && cfg->clip_low <= 1.0) || !(cfg->clip_high >= 0.0 && cfg->clip_high < 1e30) || !(cfg->kl_coef >= 0.0 && cfg->kl_coef < 1e30) ||
-            cfg->reduction < NNT_REDUCE_SUM || cfg->reduction > NNT_REDUCE_SEQUENCES)
-            return fail(ctx, NNT_EINVAL, who + ": bad configuration");
-        if (cfg->kl_coef > 0.0 && !ref_logp) return fail(ctx, NNT_EINVAL, who + ": a KL term needs the reference's log-probabilities");
+        TRY(policy_loss_check(ctx, cfg, X, labels, old_logp, ref_logp, advantages, dX, logp, losses, loss));
         Logits a;
-        TRY(take_logits(ctx, who, X, labels, &a));
-        TRY(check_positions(ctx, who, "logp", X, logp));
-        if (old_logp) TRY(check_positions(ctx, who, "old_logp", X, old_logp));
-        if (ref_logp) TRY(check_positions(ctx, who, "ref_logp", X, ref_logp));
-        const bool per_sequence = advantages->ndim == 1;
-        if (per_sequence) {
-            if (advantages->ctx != ctx || advantages->dtype != NNT_F32 || advantages->shape[0] != X->shape[2] || advantages->base[0] != X->base[2] || !all_there(advantages))
-                return fail(ctx, NNT_EINVAL, who + ": advantages per sequence must be fp32 [N_b], tiled like the logits' last axis, all tiles present");
-        } else {
-            TRY(check_positions(ctx, who, "advantages", X, advantages));
-        }
-        TRY(check_gradient(ctx, who, X, dX));
-        if (logp == old_logp || logp == ref_logp || logp == advantages) return fail(ctx, NNT_EINVAL, who + ": logp must not be one of the inputs");
+        TRY(take_logits(ctx, "nnt_policy_loss", X, labels, &a));
         const int64_t ncols = X->shape[1] * X->shape[2];
         const int reduction = cfg->reduction;
-        if (reduction != NNT_REDUCE_SUM) TRY(ensure_stream_scratch(ctx, X->shape[2]));
         int nt;
-        const PolicyFn fn = policy_of(X->dtype, a.nvec, ncols, &nt);
+        const PolicyFn fn = policy_instance(X->dtype, a.nvec, ncols, &nt);
         PolicyArgs p{};
         p.old_logp = in_tiles(old_logp);
         p.ref_logp = cfg->kl_coef > 0.0 ? in_tiles(ref_logp) : nullptr;
         p.adv = in_tiles(advantages);
-        p.adv_per_sequence = per_sequence;
+        p.adv_per_sequence = advantages->ndim == 1;
         p.lo = (float)(1.0 - cfg->clip_low);
         p.hi = (float)(1.0 + cfg->clip_high);
         p.kl = (float)cfg->kl_coef;
@@ -737,21 +768,11 @@ int32_t nnt_policy_loss(nnt_ctx* ctx, const nnt_policy_cfg* cfg, nnt_tensor* X, 
 int32_t nnt_preference_loss(nnt_ctx* ctx, const nnt_preference_cfg* cfg, nnt_tensor* X, const int32_t* labels, nnt_tensor* ref_logp, nnt_tensor* dX,
                             nnt_tensor* logp, float* rewards, float* losses, float* loss) {
     return entry(ctx, [&]() -> int32_t {
-        const std::string who = "nnt_preference_loss";
-        if (!cfg || !X || !labels || !logp || !rewards || !losses || !loss) return fail(ctx, NNT_EINVAL, who + ": null argument");
-        if (!(cfg->beta > 0.0 && cfg->beta < 1e30) || !(cfg->label_smoothing >= 0.0 && cfg->label_smoothing <= 0.5) ||
-            (cfg->reduction != NNT_REDUCE_SUM && cfg->reduction != NNT_REDUCE_SEQUENCES))
-            return fail(ctx, NNT_EINVAL, who + ": bad configuration");
+        TRY(preference_loss_check(ctx, cfg, X, labels, ref_logp, dX, logp, rewards, losses, loss));
         Logits a;
-        TRY(take_logits(ctx, who, X, labels, &a));
-        if (X->shape[2] % 2) return fail(ctx, NNT_EINVAL, who + ": pairs need an even batch");
-        TRY(check_positions(ctx, who, "logp", X, logp));
-        if (ref_logp) TRY(check_positions(ctx, who, "ref_logp", X, ref_logp));
-        TRY(check_gradient(ctx, who, X, dX));
-        if (logp == ref_logp) return fail(ctx, NNT_EINVAL, who + ": logp must not be one of the inputs");
+        TRY(take_logits(ctx, "nnt_preference_loss", X, labels, &a));
         const int64_t ncols = X->shape[1] * X->shape[2];
         const int N_s = (int)X->shape[1], N_b = (int)X->shape[2], dt = X->dtype;
-        TRY(ensure_stream_scratch(ctx, 4 * ncols + 2 * N_b));
         const PreferenceArgs p{cfg->beta, cfg->label_smoothing, cfg->reduction == NNT_REDUCE_SUM ? 1.0 : 2.0 / N_b, N_b / 2};
         const float* const* ref = in_tiles(ref_logp);
         float* const* out = out_tiles(logp);

@@ -60,3 +60,36 @@ def test_muon_refused_inside_a_capture_records_nothing(mods, whose, dtype):
             check_muon(SimpleNamespace(blocks=m.blocks[1:], capi=capi), before[1:], 0.02, dict(lr=0.02, momentum=0.9, nesterov=True, scale="rms"))
         ctx.wait()
         close(m)
+
+
+@pytest.mark.parametrize("which", ["logprob", "policy", "preference"])
+def test_refused_ends_of_the_forward_pass_leave_the_last_one(mods, which):
+    """A call that is refused launches nothing, and the pass before it can still go backward."""
+    capi, tiled = mods
+    q = Problem("f32")
+    with tiled.Context(n_streams=2) as ctx:
+        m = q.model(tiled, ctx)
+        logp, wrong = m.per_position(), tiled.TiledTensor(ctx, "f32", (q.cfg.N_s + 1, q.cfg.N_b), m.logits.base[1:], fill=0)
+        adv = tiled.TiledTensor.from_numpy(ctx, q.adv, m.logits.base[2:])
+        T, P, L, f = m.tokens.data_ptr(), m.pos.data_ptr(), m.labels.data_ptr(), m.col_loss.data_ptr()
+        pcfg, dcfg = capi.nnt_policy_cfg(0.2, 0.2, 0.1, 0), capi.nnt_preference_cfg(-1.0, 0.0, 0)
+
+        def backward():
+            m.backward()
+            ctx.wait()
+            return [b.grad(k).download() for b in m.blocks for k in MATRICES] + [m.gamma["g"].download()]
+        m.forward_policy(adv, logp)
+        first = backward()
+        m.forward_policy(adv, logp)
+        ctx.wait()
+        launches = ctx.stats()["launches"]
+        if which == "logprob":
+            assert capi.nnt_gpt2_model_logprob.raw(m.h, T, P, L, wrong.h) == capi.NNT_EINVAL
+        elif which == "policy":                               # a KL term without a reference
+            assert capi.nnt_gpt2_model_forward_policy.raw(m.h, T, P, L, C.byref(pcfg), None, None, adv.h, logp.h, f, f) == capi.NNT_EINVAL
+        else:                                                 # a negative strength
+            assert capi.nnt_gpt2_model_forward_preference.raw(m.h, T, P, L, C.byref(dcfg), None, logp.h, f, f, f) == capi.NNT_EINVAL
+        assert ctx.stats()["launches"] == launches
+        for a, b in zip(first, backward()):
+            np.testing.assert_array_equal(a, b)
+        close(m)
