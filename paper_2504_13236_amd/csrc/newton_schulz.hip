@@ -1298,14 +1298,14 @@ int growth_of(const nnt_newton_schulz_cfg& c) {
 }
 
 // Whether two steps can be taken at once.  The buffers hold polynomials in A = X X^T without a constant term, p(s^2) = s^2 r(s^2), as D p, whose entries reach |r| s in a row
-// of length 1 and |p| in one that keeps its length; the last one, P_1 P_0, the same at a quarter of the scale and with a multiple of the identity.  4097 places of polynomials
-// of degree 9 in s^2, and a margin.
+// of length 1 and |p| in one that keeps its length; the last one, P_1 P_0, the same at a quarter of the scale and with a multiple of the identity.  r has degree 11 in s^2 at most:
+// between two of 257 places it rises by less than 4 % of its largest value (|r''| <= 11^2 (11^2 - 1) / 3 (2 / l)^2 of it), s by what the next place has; the margin is 6 %.
 bool pairs_in_range(const nnt_newton_schulz_cfg& c) {
     double reach = 1.0;
     if (!in_range(c, &reach)) return false;
     double most = 0.0, last = 0.0;
-    for (int i = 0; i <= 4096; i++) {
-        const double l = reach * reach * i / 4096.0, at = std::max(std::sqrt(l), l);
+    for (int i = 0; i <= 256; i++) {
+        const double l = reach * reach * i / 256.0, next = reach * reach * (i + 1) / 256.0, at = std::max(std::sqrt(next), next);
         const double p0 = c.a + c.b * l + c.c * l * l, r0 = c.b + c.c * l, r1 = p0 * p0 * (c.b + c.c * l * p0 * p0);
         for (double r : {r0, p0, p0 * p0, r1}) most = std::max(most, at * std::fabs(r));
         last = std::max(last, at * std::fabs(r1 * l * r0 + c.a * (r0 + r1)));
@@ -1525,7 +1525,7 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
         if (gram.splits > 1) bytes += (int64_t)gram.tiles * gram.splits * (gram.shape == 0 ? Small::BM * Small::BM : Middle::BM * Middle::BM) * 4;
         // (The model is a tenth and more off either way: two steps at once have to promise that much.  Below 256 rows they gain less, 128 x 6272 120 us instead of 128, and
         // their errors are larger than those of fp32 products, 128 x 1000 2.9e-6 after five steps instead of 1.7e-6.)
-        w.items = plan(cfg, g.growth, shortest >= 256 && pairs_in_range(cfg) && 1.15 * 3.0 * w.launch[kPoly].time < gram.time + w.launch[kStep].time);
+        w.items = plan(cfg, g.growth, shortest >= 256 && 1.15 * 3.0 * w.launch[kPoly].time < gram.time + w.launch[kStep].time && pairs_in_range(cfg));
     }
     w.bytes = bytes;
     return NNT_OK;

@@ -93,3 +93,23 @@ def test_refused_ends_of_the_forward_pass_leave_the_last_one(mods, which):
         for a, b in zip(first, backward()):
             np.testing.assert_array_equal(a, b)
         close(m)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_muon_in_tile_granularity(mods, dtype):
+    """One task per tile for the vectors: the same step."""
+    capi, tiled = mods
+    q = Problem(dtype)
+    results = []
+    for granularity in (capi.NNT_GRAN_OP, capi.NNT_GRAN_TILE):
+        with tiled.Context(n_streams=3) as ctx:
+            m = with_gradients(q, tiled, ctx)
+            capi.nnt_ctx_set_granularity(ctx.h, granularity)
+            m.muon(1, lr=0.02, momentum=0.9)
+            ctx.wait()
+            results.append([b.param(k).download() for b in m.blocks for k in MATRICES + ("b_qkv", "gamma2")] + [m.wte["p"].download(), m.gamma["p"].download()])
+            close(m)
+    # (the embeddings' gradients are sums over positions in any order: Adam's first step is lr times their sign, and moves by it where they are 0)
+    for a, b in zip(results[0][:-2] + results[0][-1:], results[1][:-2] + results[1][-1:]):
+        assert np.abs(a - b).max() <= 1e-6 * np.abs(a).max() + 1e-7
+    assert np.abs(results[0][-2] - results[1][-2]).max() <= 2.1e-3
