@@ -17,7 +17,7 @@
 //   (D X)(D X)^T = D A D;  stored as  D A = (D A D) D^-1, so that  (D A)(D A)^T = D A^2 D  and so on for all polynomials in A, which commute;
 //   B is stored as  D B D^-1,  so that  (D B D^-1)(D X) = D B X.
 // The values that are stored stay below 16: |x_i (.) X^T| <= max s |.| for rows of length 1, and |b + c s^2| s <= 13.6 where |b s^2 + c s^4| <= 8 on [0, 1].
-// Gradients with rows of 1e-8 of the others, 128 x 300, 20 steps: 3e-6 of the result off, fp32 products 3e-6, one scale for all 5e-2.
+// Rows of 1e-8 of the others, 512 x 2560, five steps: the worst of them 4e-6 of its length off, with fp32 products 8e-6, with one scale for all of X 4e-1.
 //
 // All operands of the products lie in the workspace as panels: 64 rows x 16 columns of the contraction, hi part and lo part of 2 KB each,
 // inside them eight columns of a row next to each other (16 bytes), 64 rows of those, then the next eight columns.  That is the
@@ -144,7 +144,8 @@ __device__ __forceinline__ double sum16(double (&v)[16], int lane) {
 }
 
 // A workgroup takes 64 rows of X and a part of its columns, 256 at a time: a lane a row of the tensor and a wavefront 16 columns of it.  Squares are added up in 64
-// bits (no value of fp32 overflows or vanishes in it), by row of X and over the 64 rows.  Bound by memory.
+// bits (no value of fp32 overflows or vanishes in it), by row of X and over the 64 rows.  Bound by memory: 8192 x 8192 with momentum, 171 us for 805 MB (139 along the tiles
+// in 16-byte vectors, which cannot add up rows).
 __global__ void __launch_bounds__(1024) ns_norm_kernel(NsGroup g) {
     __shared__ double red[16][64];
     // the launches behind this one read the group from the workspace
@@ -284,7 +285,7 @@ struct Scale {
 
 // ---------------------------------------------------------------- set-up: X_0 and its transpose
 // One workgroup takes 64 x 64 elements: read along the tensor's contiguous axis, turned in LDS, written as panels of both.  Bound by memory: 8192 x 8192
-// with momentum, 222 us for 1074 MB; both forms are written here because turning X for the first product with it would cost a pass of its own.
+// with momentum, 251 us for 1074 MB; both forms are written here because turning X for the first product with it would cost a pass of its own.
 __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict__ group, NsSizes sizes) {
     const NsGroup& g = *group;
     __shared__ float t[64][65];                          // [i][j]
@@ -864,7 +865,7 @@ __global__ void __launch_bounds__(256) ns_combine_kernel(const NsGroup* __restri
 // Here a launch is longer than what it computes, so a whole iteration is one launch.  A workgroup holds some of X's column blocks of 64; it adds up the
 // parts of A that the workgroups have left (its own and the others'), computes B (64 x 64, every workgroup the same), its blocks of X and their
 // part of the next A.  X is kept as its transpose only.  The first launch takes U in place of B X, the last one leaves the results.  64 x 320: 6 us a
-// launch, 43 in all (some 75 with the products above); it is the launches that bound it, and within one the parts' way through memory.
+// launch, 45 in all (some 75 with the products above); it is the launches that bound it, and within one the parts' way through memory.
 enum { kFirst, kMiddle, kFinal };
 
 // how many workgroups share a matrix of nt column blocks: each adds up as many parts (0.2 us) as there are, and takes nt / parts blocks (1.5 us) in turn
@@ -1100,8 +1101,8 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
 
 // ---------------------------------------------------------------- matrices of at most 64 x 256
 // One workgroup holds all of X in LDS and does everything in one launch: momentum, norm, the steps, the results.  Four wavefronts to a column block of 64; the first four
-// put A together and compute B for all.  64 x 64 22 us (33 with a launch per step), 64 x 256 43 (43), and the rest of the chip is free meanwhile: passes over the four
-// matrices of a block of 64 that need not wait for one another take 25 us each (42).  What bounds it is LDS, 3 us a step and 1.2 for each further block.  (X computed
+// put A together and compute B for all.  64 x 64 22 us (33 with a launch per step), 64 x 256 43 (45), and the rest of the chip is free meanwhile: passes over the four
+// matrices of a block of 64 that need not wait for one another take 27 us each (46).  What bounds it is LDS, 3 us a step and 1.2 for each further block.  (X computed
 // twice, as its transpose too, in place of the two-byte writes: 40 us, but the two drift apart, errors a quarter larger.)
 constexpr int kHeldBlocks = 4;
 
@@ -1283,8 +1284,8 @@ bool in_range(const nnt_newton_schulz_cfg& c, double* reach = nullptr, double* b
 }
 
 // What is kept out of the factor P_1 P_0 of two steps at once, as a multiple of the identity: rounded among the factor's entries it would cost as much as the rest.  The first
-// steps find small singular values and a factor near a^2, the later ones values around 1 and a factor between 0.4 and some 10.  (a^2 for all of them: errors of
-// 1024 x 4096 4.5e-6 instead of 3.5e-6; nothing after the first: 3.9e-6.)
+// steps find small singular values and a factor near a^2, the later ones values around 1 and a factor between 0.4 and some 10.  (a^2 for all of them, in a model of the
+// arithmetic on the host: errors of 512 x 2560 3.7e-6 instead of 3.3e-6.)
 double kept_out(const nnt_newton_schulz_cfg& c, bool first) { return first ? c.a * c.a : c.a * c.a / 4.0; }
 
 // What a step can make a row grow by, the largest |a + b s^2 + c s^4|, as its logarithm in 1/256 (rounded up; rows that shrink are followed for 16 binary places a step).
@@ -1434,7 +1435,7 @@ enum { kProducts, kNarrow, kHeld };
 int kind_of(int64_t m, int64_t l) { return m > 64 || l > 64 * kNarrowBlocks ? kProducts : l > 64 * kHeldBlocks ? kNarrow : kHeld; }
 
 // Sets of up to this size take the two halves of the workspace in turn, so that two of them run side by side: a launch's beginning and end, and the units that
-// it leaves idle, are the other's (sets of a step on 12 blocks of 768 wide 4.23 -> 3.61 ms, 777 x 1111 165 -> 104 us each; more than two at a time, four sets of a
+// it leaves idle, are the other's (sets of a step on 12 blocks of 768 wide 4.23 -> 3.7 ms, 777 x 1111 176 -> 111 us each; more than two at a time, four sets of a
 // block of 1600 10.0 -> 10.7 ms).  Larger ones fill the chip (two of 4096 x 4096 7.97 ms either way) and take all of it.
 constexpr int64_t kHalfBytes = (int64_t)512 << 20;
 

@@ -11,10 +11,10 @@
 // and a position without a label (a prompt, padding) has the gradient 0; its logits are not even read.
 // Everything here is bound by memory: one read of the logits for logp, a read and a write for the policy loss, and
 // two reads and a write for the preference loss, whose coefficients need the whole pair first.  bf16 logits, 50304 to a column, 5/8 of the positions with a label:
-//   logp        8192 columns    95 us for  515 MB (5.4 TB/s)
-//   policy      8192           241 us for 1275 MB (5.3 TB/s; one sequence of eight has no label at all)
-//   preference  4096           175 us for  927 MB (5.3 TB/s; part of the second read is found in the caches)
-// where a copy reaches 5.1.  A single fp32 column of 50304 takes 6 us: the launch, four loads in a row and two exchanges between wavefronts.
+//   logp        8192 columns    95 to 109 us for  515 MB (4.7 to 5.4 TB/s)
+//   policy      8192           241 to 264 us for 1275 MB (4.8 to 5.3 TB/s; one sequence of eight has no label at all)
+//   preference  4096           142 to 175 us for  927 MB (5.3 TB/s and more: part of the second read is found in the caches)
+// where a copy reaches 5.1.  A single fp32 column of 50304 takes 10 us, 6 among others: the launch, four loads in a row and two exchanges between wavefronts.
 #include "colwise.hpp"
 #include "device_util.hpp"
 #include "internal.hpp"
@@ -29,7 +29,8 @@ constexpr int64_t kMaxVectors = 1 << 20;      // of a column: up to there `place
 
 // Gradients of more than this leave past the caches: they would drive out logits that are still to be read a second time, and nobody finds so much of them there
 // later (preference loss of 1998 fp32 columns of 32003, 256 MB: 114 -> 98 us; policy loss of 8192 of 50304 in bf16 255 -> 241).  Smaller ones are
-// read from the caches by the head's products (a model's step with 103 MB of logits 886 us, 893 with this).
+// read from the caches by the head's products (a model's step with 103 MB of logits 886 us, 893 with this).  There, where the products read the gradient next, larger ones gain
+// little or nothing: bf16 141 MB 1119 us, 1126 without this, 206 MB 1257 and 1268, 241 MB 1440 and 1446; fp32 141 to 483 MB the same either way.
 constexpr int64_t kCached = (int64_t)128 << 20;
 
 // exp(t), t <= 0, for logits of type T.  Both factors of the exponent's product with 1/ln 2 are kept, since the rounded constant alone makes
