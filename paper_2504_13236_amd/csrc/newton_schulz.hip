@@ -10,21 +10,25 @@
 // x, but none below 2^-38, the last one that an fp16 number of this scale can have; the term lo lo that is left out is below 2^-22 of the product.  X stays below
 // 2.83; polynomials in A are kept at a scale of 2^12, which leaves room up to 16: what the iteration can reach is checked by the caller.
 //
-// fp32 products keep every row of X to 24 bits of its own size, however small it is beside the others, and the iteration brings such a row up to them, by a factor
-// of `a` a step.  So here each row has a power of two of its own: what is stored is D X, D = diag(2^e_i), with rows of at most length 1 wherever e_i > 0.  e_i comes from
-// the row's length in X_0 and falls by what a step can make a row grow, max |a + b s^2 + c s^4|, until it is 0 (x_i <- x_i (a I + b X^T X + c (X^T X)^2): a row
-// grows by no more than its singular directions do).  Products keep to it without a factor inside the sums:
+// fp32 products keep every entry of X to 24 bits of its own size, and what is small beside its row's or column's neighbours counts: the iteration brings it up to them, by a
+// factor of `a` a step.  So here rows and columns have powers of two of their own.  X is there three times: in fp32 (E), which the next X is made of; with rows as 2^e_i x_ij for
+// A = X X^T, to which a column much smaller than the others contributes nothing that counts; and as its transpose with columns as 2^f_j x_ij for B X, to which a small row contributes
+// nothing that counts.  Rows and columns are at most of length 1 then wherever e_i or f_j > 0.  Both come from the lengths in X_0 and fall by what a step can make a row or
+// column grow, max |a + b s^2 + c s^4|, until they are 0 (X <- p(X X^T) X: a row or column grows by no more than its singular directions do).  With D = diag(2^e_i) the square products
+// keep to it without a factor inside the sums:
 //   (D X)(D X)^T = D A D;  stored as  D A = (D A D) D^-1, so that  (D A)(D A)^T = D A^2 D  and so on for all polynomials in A, which commute;
-//   B is stored as  D B D^-1,  so that  (D B D^-1)(D X) = D B X.
-// The values that are stored stay below 16: |x_i (.) X^T| <= max s |.| for rows of length 1, and |b + c s^2| s <= 13.6 where |b s^2 + c s^4| <= 8 on [0, 1].
+//   (D B)(X diag(2^f_j)) = D (B X) diag(2^f_j).
+// What is stored stays below 16: |x_i (.) X^T| <= max s |.| for rows of length 1, and |b + c s^2| s <= 13.6 where |b s^2 + c s^4| <= 8 on [0, 1].  B's diagonal is kept out of it: a + B_ii, in
+// fp32, is what X's row i is multiplied by (most of the step once X has arrived, where B is near a multiple of the identity).
 // Rows of 1e-8 of the others, 512 x 2560, five steps: the worst of them 4e-6 of its length off, with fp32 products 8e-6, with one scale for all of X 4e-1.
 //
 // All operands of the products lie in the workspace as panels: 64 rows x 16 columns of the contraction, hi part and lo part of 2 KB each,
 // inside them eight columns of a row next to each other (16 bytes), 64 rows of those, then the next eight columns.  That is the
 // image that the products want in LDS, so loads go straight there in runs of 4 KB, and a matrix instruction's operand is one 16-byte LDS
 // read per lane without bank conflicts.  Every product has the contraction along the columns of both operands: A = X X^T and A^2 = A A^T anyway, and B X
-// reads X as its transpose, which the step before (or the set-up) has written beside X itself.  D A and D B D^-1 are not symmetric, but their sums are: tiles on and above
-// the diagonal are computed, and scaled twice.  Rows and columns are padded with zeros to whole tiles; zeros stay zeros through the iteration.
+// reads X as its transpose.  D A and D B are not symmetric, but their sums are: tiles on and above
+// the diagonal are computed, and scaled twice.  E lies as the results do in registers, by blocks of 32 x 32.  Rows and columns are padded with zeros to whole tiles; zeros stay zeros
+// through the iteration.
 #include "device_util.hpp"
 #include "gemm_dl_common.hpp"
 #include "internal.hpp"
@@ -44,6 +48,7 @@ constexpr int kGroupMatrices = 16;        // matrices of one set of launches
 constexpr float kScale = 4096.f;          // of square matrices, 2^12
 constexpr float kScaleX = 16384.f;        // of X, whose entries stay below 2.83: 2^14
 constexpr float kGramFactor = kScale / kScaleX / kScaleX;
+constexpr int kShift = 12, kShiftX = 14;  // the same as powers of two
 constexpr int kPanelBytes = 4096;         // 64 rows x 16 columns, both parts
 constexpr int kPartBytes = 2048;
 
@@ -58,8 +63,9 @@ struct NsMatrix {
     int32_t flip;                                        // X is the transpose (more rows than columns)
     int32_t mp, np;                                      // X's extents, mp <= np, padded to whole panels of 64 rows
     int32_t splits;                                      // of the long side by the workgroups that add up squares
-    int64_t X, XT, A;                                    // bytes from the start of the workspace; X and XT: two buffers each, one behind the other; A: see NsOp
-    int64_t squares, part, exponents;                    // sums of squares by split and row of X, the same of 64 rows at a time; e_i of the first step
+    int64_t X, XT, E, A;                                 // bytes from the start of the workspace; XT: two buffers, one behind the other; A: see NsOp
+    int64_t squares, part, largest;                      // sums of squares by split and row of X, the same of 64 rows at a time; largest entries by 64 (X the transpose: 16) rows and column
+    int64_t exponents, columns, coefficients;            // e_i and f_j of the first step; a + B_ii
     MatView G, M, P, LP;                                 // gradient, momentum, parameter (or result), bf16 copy
     float decay, step;                                   // P <- decay P - step X (step < 0: P <- X)
 };
@@ -82,7 +88,7 @@ struct NsGroup {
     NsMatrix mat[kGroupMatrices];
 };
 
-static_assert(sizeof(NsGroup) <= 4096 && sizeof(NsGroup) % 4 == 0, "copied by one workgroup, a word to a thread");
+static_assert(sizeof(NsGroup) <= 4096 && sizeof(NsGroup) % 4 == 0, "an argument, copied by words");
 
 // 16 columns, from column c0 on, of a row of a matrix: t0, o0, e0 are its tile, its place in it and the tile's height; 0 where there is none
 template <typename T>
@@ -129,38 +135,71 @@ __device__ __forceinline__ void write_columns(const NsMatrix& q, void* const* ti
 // Sums over the wavefront of 16 values each: the lane's own of the sums, number sum16_index(lane).  Halves are exchanged while there is more than one value left,
 // 17 exchanges for all of them.
 __device__ __forceinline__ int sum16_index(int lane) { return lane >> 2; }
-__device__ __forceinline__ double sum16(double (&v)[16], int lane) {
+template <int HALF>
+__device__ __forceinline__ void sum_halves(double (&v)[16], int lane) {
+    const bool up = lane & (HALF * 4);
 #pragma unroll
-    for (int half = 8; half > 0; half >>= 1) {
-        const bool up = lane & (half * 4);
-#pragma unroll
-        for (int k = 0; k < half; k++) {
-            const double keep = up ? v[k + half] : v[k], give = up ? v[k] : v[k + half];
-            v[k] = keep + __shfl_xor(give, half * 4, 64);
-        }
+    for (int k = 0; k < HALF; k++) {
+        const double keep = up ? v[k + HALF] : v[k], give = up ? v[k] : v[k + HALF];
+        v[k] = keep + __shfl_xor(give, HALF * 4, 64);
     }
+}
+__device__ __forceinline__ double sum16(double (&v)[16], int lane) {
+    sum_halves<8>(v, lane);
+    sum_halves<4>(v, lane);
+    sum_halves<2>(v, lane);
+    sum_halves<1>(v, lane);
     v[0] += __shfl_xor(v[0], 2, 64);
     return v[0] + __shfl_xor(v[0], 1, 64);
 }
 
-// A workgroup takes 64 rows of X and a part of its columns, 256 at a time: a lane a row of the tensor and a wavefront 16 columns of it.  Squares are added up in 64
-// bits (no value of fp32 overflows or vanishes in it), by row of X and over the 64 rows.  Bound by memory: 8192 x 8192 with momentum, 171 us for 805 MB (139 along the tiles
-// in 16-byte vectors, which cannot add up rows).
-__global__ void __launch_bounds__(1024) ns_norm_kernel(NsGroup g) {
-    __shared__ double red[16][64];
-    // the launches behind this one read the group from the workspace
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < sizeof(NsGroup) / 4)
-        reinterpret_cast<uint32_t*>(g.space)[threadIdx.x] = reinterpret_cast<const uint32_t*>(&g)[threadIdx.x];
-    const NsMatrix& q = g.mat[blockIdx.y];
-    const int row_blocks = q.mp >> 6, splits = q.splits;
-    if ((int)blockIdx.x >= row_blocks * splits) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int rb = blockIdx.x % row_blocks, part = blockIdx.x / row_blocks;
-    double sum[16];
+// The upper half of an absolute value's bits, rounded up.
+__device__ __forceinline__ uint32_t upper_half(float v) { return (__float_as_uint(fabsf(v)) + 0xffffu) >> 16; }
+__device__ __forceinline__ float from_upper_half(uint32_t h) { return __uint_as_float(h << 16); }
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t larger_halves(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+// The same as sum16 for the upper halves of the largest absolute values, two at a time: lane 8 k has number k in its lower half and number k + 8 in its upper half.
+__device__ __forceinline__ uint32_t largest16(const float (&u)[16], int lane) {
+    uint32_t v[8];
 #pragma unroll
-    for (int s = 0; s < 16; s++) sum[s] = 0.0;
-    for (int l0 = part * 256; l0 < q.np; l0 += splits * 256) {
-        const int r = (q.flip ? l0 + (wave >> 2) * 64 : rb * 64) + lane, c0 = q.flip ? rb * 64 + (wave & 3) * 16 : l0 + wave * 16;
+    for (int k = 0; k < 8; k++) v[k] = upper_half(u[k]) | (upper_half(u[k + 8]) << 16);
+#pragma unroll
+    for (int half = 4; half > 0; half >>= 1) {
+        const bool up = lane & (half * 8);
+#pragma unroll
+        for (int k = 0; k < half; k++) {
+            const uint32_t keep = up ? v[k + half] : v[k], give = up ? v[k] : v[k + half];
+            v[k] = larger_halves(keep, __shfl_xor(give, half * 8, 64));
+        }
+    }
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) v[0] = larger_halves(v[0], __shfl_xor(v[0], o, 64));
+    return v[0];
+}
+// and within a lane
+__device__ __forceinline__ float largest_of(const float (&u)[16]) {
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; k++) v = fmaxf(v, fabsf(u[k]));
+    return v;
+}
+
+// A workgroup takes 64 rows of X and a part of its columns, 128 at a time: a lane a row of the tensor and a wavefront 16 columns of it.  Squares are added up in 64
+// bits (no value of fp32 overflows or vanishes in it), by row of X and over the 64 rows; of X's columns the largest entries are left.  Bound by memory: 8192 x 8192 with momentum, 171 us for 805 MB (139 along the tiles
+// in 16-byte vectors, which cannot add up rows).
+constexpr int kNormWaves = 8, kNormSpan = 16 * kNormWaves;
+template <bool FLIP>
+__device__ __forceinline__ void norm_part(const NsGroup& g, const NsMatrix& q, int rb, int part, double (*red)[64]) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint16_t* largest = reinterpret_cast<uint16_t*>(g.space + q.largest);
+    double sum[FLIP ? 16 : 1];
+#pragma unroll
+    for (int s = 0; s < (FLIP ? 16 : 1); s++) sum[s] = 0.0;
+#pragma unroll 1
+    for (int l0 = part * kNormSpan; l0 < q.np; l0 += q.splits * kNormSpan) {
+        const int r = (FLIP ? l0 + (wave >> 2) * 64 : rb * 64) + lane, c0 = FLIP ? rb * 64 + (wave & 3) * 16 : l0 + wave * 16;
         const int t0 = min(r, q.rows - 1) / q.base0, o0 = r - t0 * q.base0, e0 = min(q.base0, q.rows - t0 * q.base0);
         const bool there = r < q.rows;
         float u[16];
@@ -176,20 +215,41 @@ __global__ void __launch_bounds__(1024) ns_norm_kernel(NsGroup g) {
             write_columns(q, q.M.tiles, there, t0, o0, e0, c0, m);
         }
 #pragma unroll
-        for (int s = 0; s < 16; s++) sum[s] += (double)u[s] * (double)u[s];
+        for (int s = 0; s < 16; s++) sum[FLIP ? s : 0] += (double)u[s] * (double)u[s];
+        if constexpr (FLIP) {
+            if (r < q.np) largest[(int64_t)(rb * 4 + (wave & 3)) * q.np + r] = (uint16_t)upper_half(largest_of(u));
+        } else {
+            const uint32_t x = largest16(u, lane);
+            if (c0 < q.np && (lane & 7) == 0) {
+                uint16_t* d = largest + (int64_t)rb * q.np + c0 + (lane >> 3);
+                d[0] = (uint16_t)x;
+                d[8] = (uint16_t)(x >> 16);
+            }
+        }
     }
-    if (q.flip) {
+    if constexpr (FLIP) {
         const double x = sum16(sum, lane);
         if ((lane & 3) == 0) red[wave >> 2][(wave & 3) * 16 + sum16_index(lane)] = x;
     } else {
-#pragma unroll
-        for (int s = 1; s < 16; s++) sum[0] += sum[s];
         red[wave][lane] = sum[0];
     }
+}
+
+__global__ void __launch_bounds__(64 * kNormWaves, 6) ns_norm_kernel(NsGroup g) {
+    __shared__ double red[kNormWaves][64];
+    // the launches behind this one read the group from the workspace
+    if (blockIdx.x == 0 && blockIdx.y == 0)
+        for (unsigned k = threadIdx.x; k < sizeof(NsGroup) / 4; k += 64 * kNormWaves) reinterpret_cast<uint32_t*>(g.space)[k] = reinterpret_cast<const uint32_t*>(&g)[k];
+    const NsMatrix& q = g.mat[blockIdx.y];
+    const int row_blocks = q.mp >> 6, tid = threadIdx.x;
+    if ((int)blockIdx.x >= row_blocks * q.splits) return;
+    const int rb = blockIdx.x % row_blocks, part = blockIdx.x / row_blocks;
+    if (q.flip) norm_part<true>(g, q, rb, part, red);
+    else norm_part<false>(g, q, rb, part, red);
     __syncthreads();
     if (tid < 64) {
         double t = 0.0;
-        for (int w = 0; w < (q.flip ? 4 : 16); w++) t += red[w][tid];
+        for (int w = 0; w < (q.flip ? kNormWaves / 4 : kNormWaves); w++) t += red[w][tid];
         reinterpret_cast<double*>(g.space + q.squares)[(int64_t)part * q.mp + rb * 64 + tid] = t;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
@@ -197,27 +257,45 @@ __global__ void __launch_bounds__(1024) ns_norm_kernel(NsGroup g) {
     }
 }
 
-// e of a row of the given sum of squares in a matrix of the given length: the row of X_0 times 2^e is between 1/2 and 1 long.  0 for rows without one (zeros, no numbers).
-__device__ __forceinline__ int row_exponent(double squares, double length) {
-    const double x = sqrt(squares) / length;
+// e of a row or column of at most the given length in a matrix of the given length: that of X_0 times 2^e is at most 1 long.  0 for those without a length (zeros, no numbers).
+__device__ __forceinline__ int exponent_of(double length, double of) {
+    const double x = length / of;
     if (!(x > 0.0) || x > 1.0) return 0;
     int k;
     (void)frexp(x, &k);
     return max(0, -k);
 }
 
-// Set-up of a workgroup of four wavefronts: the matrix's length, and the exponents of the 64 rows of X from row i0 on.
+// Set-up of a workgroup of four wavefronts: the matrix's length, and the exponents of the 64 rows of X from row i0 on and of the 64 columns from column j0 on.
 struct SetUp {
     double total[4], squares[4][64];
-    int exponent[64];
+    int largest[4][64];
+    int row[64], column[64];
 };
-__device__ __forceinline__ double length_and_exponents(const NsGroup& g, const NsMatrix& q, int i0, bool keep, SetUp& w) {
+__device__ __forceinline__ void largest_of_columns(const NsGroup& g, const NsMatrix& q, int j0, SetUp& w) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint16_t* largest = reinterpret_cast<const uint16_t*>(g.space + q.largest) + j0 + lane;
+    int most = 0;
+#pragma unroll 8
+    for (int k = wave; k < (q.flip ? q.mp >> 4 : q.mp >> 6); k += 4) most = max(most, (int)largest[(int64_t)k * q.np]);
+    w.largest[wave][lane] = most;
+}
+__device__ __forceinline__ void column_exponents(const NsGroup& g, const NsMatrix& q, int j0, bool keep, double length, SetUp& w) {
+    const int lane = threadIdx.x & 63;
+    const int most = max(max(w.largest[0][lane], w.largest[1][lane]), max(w.largest[2][lane], w.largest[3][lane]));
+    const int f = exponent_of((double)from_upper_half((uint32_t)most) * sqrt((double)q.mp), length);
+    w.column[lane] = f;
+    if (keep) reinterpret_cast<int*>(g.space + q.columns)[j0 + lane] = f;
+}
+// j0 < 0: rows only
+__device__ __forceinline__ double length_and_exponents(const NsGroup& g, const NsMatrix& q, int i0, int j0, bool keep_rows, bool keep_columns, SetUp& w) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const double *part = reinterpret_cast<const double*>(g.space + q.part), *squares = reinterpret_cast<const double*>(g.space + q.squares);
     double sum = 0.0, row = 0.0;
     for (int k = tid; k < (q.mp >> 6) * q.splits; k += 256) sum += part[k];
 #pragma unroll 8
     for (int k = wave; k < q.splits; k += 4) row += squares[(int64_t)k * q.mp + i0 + lane];
+    if (j0 >= 0) largest_of_columns(g, q, j0, w);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
     if (lane == 0) w.total[wave] = sum;
@@ -225,15 +303,15 @@ __device__ __forceinline__ double length_and_exponents(const NsGroup& g, const N
     __syncthreads();
     const double length = sqrt(w.total[0] + w.total[1] + w.total[2] + w.total[3]) + g.eps;
     if (wave == 0) {
-        const int e = row_exponent(w.squares[0][lane] + w.squares[1][lane] + w.squares[2][lane] + w.squares[3][lane], length);
-        w.exponent[lane] = e;
-        if (keep) reinterpret_cast<int*>(g.space + q.exponents)[i0 + lane] = e;
+        const int e = exponent_of(sqrt(w.squares[0][lane] + w.squares[1][lane] + w.squares[2][lane] + w.squares[3][lane]), length);
+        w.row[lane] = e;
+        if (keep_rows) reinterpret_cast<int*>(g.space + q.exponents)[i0 + lane] = e;
     }
-    __syncthreads();
-    return length;
+    if (wave == 1 && j0 >= 0) column_exponents(g, q, j0, keep_columns, length, w);
+    return length;                                       // (w.row and w.column are there behind the next barrier)
 }
 
-// What `steps` steps can make a row grow by, as a power of two; e of a row behind that.
+// What `steps` steps can make a row or column grow by, as a power of two; its exponent behind that.
 __host__ __device__ inline int grown_by(int growth, int steps) { return (growth * steps + 255) >> 8; }
 __device__ __forceinline__ int exponent_at(int first, int grown) { return max(first - grown, 0); }
 
@@ -266,26 +344,29 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
     lo = (_Float16)(v - (float)hi);
 }
 
+// byte offset in E of a lane's results p .. of the block of 32 x 32 at row i and column j: rows i + 8 p + 4 (lane >> 5) + 0 .. 3, column j + (lane & 31)
+__device__ __forceinline__ int64_t block_at(int i, int j, int mp) { return ((int64_t)(j >> 5) * (mp >> 5) + (i >> 5)) * 4096 + (threadIdx.x & 63) * 16; }
+
 // byte offset of the 16 bytes that hold columns k .. k + 7 (k a multiple of 8) of a row in an operand with K columns, hi part
 __device__ __forceinline__ int64_t panel_at(int row, int k, int K) {
     return ((int64_t)(row >> 6) * (K >> 4) + (k >> 4)) * kPanelBytes + ((k & 15) >> 3) * 1024 + (row & 63) * 16;
 }
 
-// 2^14 x / length times another power of two, for any length above 0 (in 64 bits: the sum of the partial sums' root and eps): a factor between 1 and 2 and a power of two, since the
+// x / length times a power of two, for any length above 0 (in 64 bits: the sum of the partial sums' root and eps): a factor between 1 and 2 and a power of two, since the
 // quotient alone can lie outside of fp32.
 struct Scale {
     float factor;
     int exponent;
     __device__ __forceinline__ explicit Scale(double length) {
         factor = (float)(1.0 / frexp(length, &exponent));
-        exponent = 14 - exponent;
+        exponent = -exponent;
     }
     __device__ __forceinline__ float operator()(float x, int more) const { return ldexpf(x, exponent + more) * factor; }
 };
 
-// ---------------------------------------------------------------- set-up: X_0 and its transpose
-// One workgroup takes 64 x 64 elements: read along the tensor's contiguous axis, turned in LDS, written as panels of both.  Bound by memory: 8192 x 8192
-// with momentum, 251 us for 1074 MB; both forms are written here because turning X for the first product with it would cost a pass of its own.
+// ---------------------------------------------------------------- set-up: X_0 in its three forms
+// One workgroup takes 64 x 64 elements: read along the tensor's contiguous axis, turned in LDS, written as panels of X and of its transpose and in fp32.  Bound by memory: all
+// forms are written here because turning X for the first product with it would cost a pass of its own.
 __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict__ group, NsSizes sizes) {
     const NsGroup& g = *group;
     __shared__ float t[64][65];                          // [i][j]
@@ -301,14 +382,14 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict
     float u[16], m[16];
     read_columns(q, q.G, r < q.rows, t0, o0, e0, c0, u);
     if (g.mu >= 0.f) read_columns(q, q.M, r < q.rows, t0, o0, e0, c0, m);
-    const Scale scaled(length_and_exponents(g, q, i0, j0 == 0, setup));
+    const Scale scaled(length_and_exponents(g, q, i0, j0, j0 == 0, i0 == 0, setup));
 #pragma unroll
     for (int s = 0; s < 16; s++) {
         float x = u[s];
         if (g.mu >= 0.f) x = g.nesterov ? fmaf(g.mu, m[s], x) : m[s];
         const int c = wave * 16 + s;
-        if (q.flip) t[c][lane] = scaled(x, setup.exponent[c]);
-        else t[lane][c] = scaled(x, setup.exponent[lane]);
+        if (q.flip) t[c][lane] = x;
+        else t[lane][c] = x;
     }
     __syncthreads();
     // a lane's row, a wavefront's two groups of eight columns, of X and of its transpose
@@ -319,7 +400,7 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             _Float16 x, y;
-            split(t[lane][k + e], x, y);
+            split(scaled(t[lane][k + e], kShiftX + setup.row[lane]), x, y);
             hi[e] = x;
             lo[e] = y;
         }
@@ -329,7 +410,7 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             _Float16 x, y;
-            split(t[k + e][lane], x, y);
+            split(scaled(t[k + e][lane], kShiftX + setup.column[lane]), x, y);
             hi[e] = x;
             lo[e] = y;
         }
@@ -337,20 +418,28 @@ __global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict
         *reinterpret_cast<f16x8*>(d) = hi;
         *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
     }
+    // a wavefront's block of 32 x 32
+    const int wi = (wave & 1) * 32, wj = (wave >> 1) * 32;
+    float4* E = reinterpret_cast<float4*>(g.space + q.E + block_at(i0 + wi, j0 + wj, q.mp));
+#pragma unroll
+    for (int b = 0; b < 4; b++) {
+        const int i = wi + b * 8 + (lane >> 5) * 4, j = wj + (lane & 31);
+        E[b * 64] = make_float4(scaled(t[i][j], 0), scaled(t[i + 1][j], 0), scaled(t[i + 2][j], 0), scaled(t[i + 3][j], 0));
+    }
 }
 
 // ---------------------------------------------------------------- products
 enum { kGram, kPoly, kPair, kStep, kLast };
 
 // What a product of square matrices, or one with X, is made of.  The group's matrices have up to four square buffers each (0: A), that hold D p of a polynomial
-// p in A without a constant term, or (`apart`) D p D^-1 for the product with X, with such a term.
+// p in A without a constant term.  The `last` one of a step is what X is multiplied by: its diagonal goes into the coefficients, with `base` added.
 //   kPoly  buffer d = mul (buffer p)(buffer q) + add (buffer e)
-//   kPair  the same + add (buffer p) + diag I, at a scale of 2^10 (it reaches some 50)
-//   kStep  X = mul (buffer p) X + add X;  kLast  the same, applied
-// Rows of X have grown by up to 2^from before, and by 2^to behind it.
+//   kPair  the same with two terms, add (buffer p) + add (buffer q), at a scale of 2^10 (it reaches some 32)
+//   kStep  X = (buffer p) X + coefficients X;  kLast  the same, applied.  2^shift: the sums' scales
+// Rows and columns of X have grown by up to 2^from before, and by 2^to behind it.
 struct NsOp {
-    int32_t p, q, e, d, apart, from, to;
-    float mul, add, diag;
+    int32_t p, q, e, d, last, from, to, shift;
+    float mul, add, base;
 };
 constexpr int kPairShift = 2;             // 2^12 / 2^10
 
@@ -437,41 +526,37 @@ __device__ __forceinline__ void apply_results(const NsMatrix& q, const float (&x
     }
 }
 
-// The result path of a wavefront: FM x FN blocks of 32 x 32 from row i0 and column j0 on.  er, ec: what the powers of two of its rows and columns go by, from LDS (of square
-// results e_i; of X what it changes by).  `turn`: LDS for 32 rows, in which the results change places.
 constexpr int turn_pitch(int FN) { return 32 * FN + 8; }         // in 32-bit words
+
+// The result path of a wavefront for square matrices: FM x FN blocks of 32 x 32 from row i0 and column j0 on.  er, ec: the exponents of its rows and columns, from LDS.  `turn`: LDS
+// for 32 rows, in which the sums change places.
 template <int MODE, int FM, int FN>
-__device__ __forceinline__ void store_results(const NsGroup& g, const NsMatrix& q, const f32x16 (&acc)[FM][FN], int i0, int j0, bool diagonal, int now, const NsOp& op,
-                                              const int* er, const int* ec, uint32_t* turn) {
+__device__ __forceinline__ void store_square(const NsGroup& g, const NsMatrix& q, const f32x16 (&acc)[FM][FN], int i0, int j0, bool diagonal, const NsOp& op,
+                                             const int* er, const int* ec, uint32_t* turn) {
     // results: this lane has column j0 + 32 y + (lane & 31), rows i0 + 32 x + 8 p + 4 (lane >> 5) + 0 .. 3
-    constexpr bool kSym = MODE == kGram || MODE == kPoly || MODE == kPair;
     constexpr int kPitch = turn_pitch(FN), kTerms = MODE == kGram ? 0 : MODE == kPair ? 2 : 1;
     const int lane = threadIdx.x & 63;
-    const int64_t xbytes = (int64_t)q.mp * q.np * 4;
     const int64_t square = (int64_t)q.mp * q.mp * 4;
     // the terms that are added, laid out like the result
-    const char* E[2] = {g.space + (MODE == kPoly ? q.A + op.e * square : MODE == kPair ? q.A + op.p * square : q.XT + now * xbytes), g.space + q.A + op.q * square};
-    char* D = g.space + (MODE == kGram ? q.A : kSym ? q.A + op.d * square : q.XT + (1 - now) * xbytes);
-    char* Dt = kSym ? D : g.space + q.X + (1 - now) * xbytes;                       // the same with rows and columns exchanged
-    const int Kt = kSym ? q.mp : q.np;
-    const bool turned = MODE != kLast && !(kSym && diagonal);
+    const char* E[2] = {g.space + q.A + (MODE == kPoly ? op.e : op.p) * square, g.space + q.A + op.q * square};
+    char* D = g.space + q.A + (MODE == kGram ? 0 : op.d * square);
     const float factor = MODE == kGram ? kGramFactor : op.mul / kScale;      // sums carry both factors' scales
     const float add = op.add;
-    const bool fetches = kTerms > 0 && add != 0.f, apart = MODE == kPair || (MODE == kPoly && op.apart);
-    constexpr int kShift = MODE == kPair ? kPairShift : 0;
+    const bool fetches = kTerms > 0 && add != 0.f, last = MODE == kPair || (MODE == kPoly && op.last);
+    constexpr int kDown = MODE == kPair ? kPairShift : 0;
     // what is added is fetched one block of 32 rows ahead: behind the stores that the compiler cannot tell apart from it every load would wait (two terms: no registers for that)
     constexpr int kAhead = kTerms == 1;
     f16x4 e[1 + kAhead][kTerms ? kTerms : 1][FN][4][2];
-    f16x8 et[kTerms ? kTerms : 1][2 * FN][2];                          // the same of symmetric results with rows and columns exchanged
-    // (blocks behind the last row block of X or of its transpose are not there)
-    const int rows = q.mp, cols = kSym ? q.mp : q.np;
+    f16x8 et[kTerms ? kTerms : 1][2 * FN][2];                          // the same with rows and columns exchanged
+    // (blocks behind the last row block are not there)
+    const int rows = q.mp;
     auto fetch = [&](int x) {
         if (i0 + x * 32 >= rows) return;
 #pragma unroll
         for (int t = 0; t < kTerms; t++)
 #pragma unroll
             for (int y = 0; y < FN; y++) {
-                if (j0 + y * 32 >= cols) continue;
+                if (j0 + y * 32 >= rows) continue;
 #pragma unroll
                 for (int p = 0; p < 4; p++) {
                     const char* at = E[t] + panel_at(j0 + y * 32 + (lane & 31), i0 + x * 32 + p * 8, q.mp) + (lane >> 5) * 8;
@@ -483,27 +568,26 @@ __device__ __forceinline__ void store_results(const NsGroup& g, const NsMatrix& 
     // (a lane's eight columns of `turn`, see below)
     const int turned_row = lane & 31, turned_col = (lane >> 5) * 8;
     auto fetch_turned = [&](int x) {
-        if constexpr (kSym) {
 #pragma unroll
-            for (int t = 0; t < kTerms; t++)
+        for (int t = 0; t < kTerms; t++)
 #pragma unroll
-                for (int s = 0; s < 2 * FN; s++) {
-                    if (j0 + s / 2 * 32 >= cols) continue;
-                    const char* at = E[t] + panel_at(i0 + x * 32 + turned_row, j0 + s * 16 + turned_col, q.mp);
-                    et[t][s][0] = *reinterpret_cast<const f16x8*>(at);
-                    et[t][s][1] = *reinterpret_cast<const f16x8*>(at + kPartBytes);
-                }
-        }
+            for (int s = 0; s < 2 * FN; s++) {
+                if (j0 + s / 2 * 32 >= rows) continue;
+                const char* at = E[t] + panel_at(i0 + x * 32 + turned_row, j0 + s * 16 + turned_col, q.mp);
+                et[t][s][0] = *reinterpret_cast<const f16x8*>(at);
+                et[t][s][1] = *reinterpret_cast<const f16x8*>(at + kPartBytes);
+            }
     };
     if (fetches && kAhead) fetch(0);
 #pragma unroll
     for (int x = 0; x < FM; x++) {
         if (fetches && x + kAhead < FM) fetch(x + kAhead);
         if (i0 + x * 32 >= rows) continue;
-        if (fetches && turned) fetch_turned(x);
+        if (fetches && !diagonal) fetch_turned(x);
 #pragma unroll
         for (int y = 0; y < FN; y++) {
-            if (j0 + y * 32 >= cols) continue;
+            if (j0 + y * 32 >= rows) continue;
+            const int i = i0 + x * 32 + (lane >> 5) * 4, j = j0 + y * 32 + (lane & 31);
             float v[4][4];
 #pragma unroll
             for (int p = 0; p < 4; p++) {
@@ -511,88 +595,156 @@ __device__ __forceinline__ void store_results(const NsGroup& g, const NsMatrix& 
                 const int ek[4] = {ei.x, ei.y, ei.z, ei.w};
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
-                    float w = acc[x][y][p * 4 + k] * factor;
-                    if constexpr (kSym) {
-                        if (turned) turn[(p * 8 + (lane >> 5) * 4 + k) * kPitch + y * 32 + (lane & 31)] = __float_as_uint(w);
-                        w = ldexpf(w, -ek[k]);
-                    }
+                    const float w = acc[x][y][p * 4 + k] * factor;
+                    if (!diagonal) turn[(p * 8 + (lane >> 5) * 4 + k) * kPitch + y * 32 + (lane & 31)] = __float_as_uint(w);
+                    v[p][k] = ldexpf(w, -ek[k]);
                     if (fetches)
 #pragma unroll
-                        for (int t = 0; t < kTerms; t++) w = fmaf(add, (float)e[x & kAhead][t][y][p][0][k] + (float)e[x & kAhead][t][y][p][1][k], w);
-                    if constexpr (!kSym) w = ldexpf(w, ek[k]);
-                    else if (apart) w = ldexpf(w, -ek[k] - kShift);
-                    if constexpr (MODE == kPair)
-                        if (diagonal && i0 + x * 32 + p * 8 + (lane >> 5) * 4 + k == j0 + y * 32 + (lane & 31)) w = fmaf(op.diag, kScale / (1 << kShift), w);
-                    if constexpr (MODE == kLast) w *= 1.f / kScaleX;
-                    v[p][k] = w;
+                        for (int t = 0; t < kTerms; t++) v[p][k] = fmaf(add, (float)e[x & kAhead][t][y][p][0][k] + (float)e[x & kAhead][t][y][p][1][k], v[p][k]);
                 }
             }
-            const int i = i0 + x * 32, j = j0 + y * 32 + (lane & 31);
+            if (MODE != kGram && last && diagonal) {
+#pragma unroll
+                for (int p = 0; p < 4; p++)
+#pragma unroll
+                    for (int k = 0; k < 4; k++)
+                        if (i + p * 8 + k == j) {
+                            reinterpret_cast<float*>(g.space + q.coefficients)[j] = op.base + ldexpf(v[p][k], -er[x * 32 + p * 8 + (lane >> 5) * 4 + k] - kShift);
+                            v[p][k] = 0.f;
+                        }
+            }
+#pragma unroll
+            for (int p = 0; p < 4; p++) {
+                f16x4 hi, lo;
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    _Float16 h, l;
+                    split(kDown ? v[p][k] * (1.f / (1 << kDown)) : v[p][k], h, l);
+                    hi[k] = h;
+                    lo[k] = l;
+                }
+                char* d = D + panel_at(j, i0 + x * 32 + p * 8, q.mp) + (lane >> 5) * 8;
+                *reinterpret_cast<f16x4*>(d) = hi;
+                *reinterpret_cast<f16x4*>(d + kPartBytes) = lo;
+            }
+        }
+        if (!diagonal) {
+            // 32 rows of the wavefront's own sums, eight columns to a lane
+#pragma unroll
+            for (int s = 0; s < 2 * FN; s++) {
+                if (j0 + s / 2 * 32 >= rows) continue;
+                const int k = s * 16 + turned_col;
+                const uint4 u = *reinterpret_cast<const uint4*>(turn + turned_row * kPitch + k), w = *reinterpret_cast<const uint4*>(turn + turned_row * kPitch + k + 4);
+                const uint32_t sums[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
+                const int4 ea = *reinterpret_cast<const int4*>(ec + k), eb = *reinterpret_cast<const int4*>(ec + k + 4);
+                const int ek[8] = {ea.x, ea.y, ea.z, ea.w, eb.x, eb.y, eb.z, eb.w};
+                f16x8 hi, lo;
+#pragma unroll
+                for (int m = 0; m < 8; m++) {
+                    float r = ldexpf(__uint_as_float(sums[m]), -ek[m]);
+                    if (fetches)
+#pragma unroll
+                        for (int t = 0; t < kTerms; t++) r = fmaf(add, (float)et[t][s][0][m] + (float)et[t][s][1][m], r);
+                    _Float16 h, l;
+                    split(kDown ? r * (1.f / (1 << kDown)) : r, h, l);
+                    hi[m] = h;
+                    lo[m] = l;
+                }
+                char* d = D + panel_at(i0 + x * 32 + turned_row, j0 + k, q.mp);
+                *reinterpret_cast<f16x8*>(d) = hi;
+                *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
+            }
+        }
+    }
+}
+
+// The same for X: fp32 results from X's form in fp32, from which the two others are made.  er, ec: the first exponents of X's rows and columns; cf: the rows' coefficients.
+template <int MODE, int FM, int FN>
+__device__ __forceinline__ void store_step(const NsGroup& g, const NsMatrix& q, const f32x16 (&acc)[FM][FN], int i0, int j0, int now, const NsOp& op,
+                                           const int* er, const int* ec, const float* cf, uint32_t* turn) {
+    constexpr int kPitch = turn_pitch(FN);
+    const int lane = threadIdx.x & 63;
+    char *XT = g.space + q.XT + (1 - now) * ((int64_t)q.mp * q.np * 4), *X = g.space + q.X;
+    char* E = g.space + q.E;
+    float4 e[2][FN][4];
+    const int rows = q.mp, cols = q.np;
+    auto fetch = [&](int x) {
+        if (i0 + x * 32 >= rows) return;
+#pragma unroll
+        for (int y = 0; y < FN; y++) {
+            if (j0 + y * 32 >= cols) continue;
+            const float4* at = reinterpret_cast<const float4*>(E + block_at(i0 + x * 32, j0 + y * 32, q.mp));
+#pragma unroll
+            for (int p = 0; p < 4; p++) e[x & 1][y][p] = at[p * 64];
+        }
+    };
+    fetch(0);
+#pragma unroll
+    for (int x = 0; x < FM; x++) {
+        if (x + 1 < FM) fetch(x + 1);
+        if (i0 + x * 32 >= rows) continue;
+#pragma unroll
+        for (int y = 0; y < FN; y++) {
+            if (j0 + y * 32 >= cols) continue;
+            const int i = i0 + x * 32, j = j0 + y * 32 + (lane & 31), column = ec[y * 32 + (lane & 31)], f = exponent_at(column, op.from);
+            float v[4][4];
+#pragma unroll
+            for (int p = 0; p < 4; p++) {
+                const int at = x * 32 + p * 8 + (lane >> 5) * 4;
+                const int4 first = *reinterpret_cast<const int4*>(er + at);
+                const float4 c = *reinterpret_cast<const float4*>(cf + at), old = e[x & 1][y][p];
+                const int down = op.shift - f;
+                v[p][0] = fmaf(c.x, old.x, ldexpf(acc[x][y][p * 4], down - exponent_at(first.x, op.from)));
+                v[p][1] = fmaf(c.y, old.y, ldexpf(acc[x][y][p * 4 + 1], down - exponent_at(first.y, op.from)));
+                v[p][2] = fmaf(c.z, old.z, ldexpf(acc[x][y][p * 4 + 2], down - exponent_at(first.z, op.from)));
+                v[p][3] = fmaf(c.w, old.w, ldexpf(acc[x][y][p * 4 + 3], down - exponent_at(first.w, op.from)));
+            }
             if constexpr (MODE == kLast) {
                 apply_results(q, v, i + (lane >> 5) * 4, j);
             } else {
+                const int up = kShiftX + exponent_at(column, op.to);
+                float4* to = reinterpret_cast<float4*>(E + block_at(i, j0 + y * 32, q.mp));
 #pragma unroll
                 for (int p = 0; p < 4; p++) {
                     f16x4 hi, lo;
 #pragma unroll
                     for (int k = 0; k < 4; k++) {
                         _Float16 h, l;
-                        split(v[p][k], h, l);
+                        split(ldexpf(v[p][k], up), h, l);
                         hi[k] = h;
                         lo[k] = l;
-                        if constexpr (!kSym)
-                            turn[(p * 8 + (lane >> 5) * 4 + k) * kPitch + y * 32 + (lane & 31)] =
-                                (uint32_t)__builtin_bit_cast(uint16_t, h) | ((uint32_t)__builtin_bit_cast(uint16_t, l) << 16);
+                        turn[(p * 8 + (lane >> 5) * 4 + k) * kPitch + y * 32 + (lane & 31)] = __float_as_uint(v[p][k]);
                     }
-                    char* d = D + panel_at(j, i + p * 8, q.mp) + (lane >> 5) * 8;
+                    to[p * 64] = make_float4(v[p][0], v[p][1], v[p][2], v[p][3]);
+                    char* d = XT + panel_at(j, i + p * 8, q.mp) + (lane >> 5) * 8;
                     *reinterpret_cast<f16x4*>(d) = hi;
                     *reinterpret_cast<f16x4*>(d + kPartBytes) = lo;
                 }
             }
         }
-        if (turned) {
+        if constexpr (MODE == kStep) {
             // 32 rows of the wavefront's own results, eight columns to a lane
+            const int row = lane & 31, up = kShiftX + exponent_at(er[x * 32 + row], op.to);
 #pragma unroll
             for (int s = 0; s < 2 * FN; s++) {
                 if (j0 + s / 2 * 32 >= cols) continue;
-                const int k = s * 16 + turned_col;
-                const uint4 u = *reinterpret_cast<const uint4*>(turn + turned_row * kPitch + k), w = *reinterpret_cast<const uint4*>(turn + turned_row * kPitch + k + 4);
-                char* d = Dt + panel_at(i0 + x * 32 + turned_row, j0 + k, Kt);
-                if constexpr (kSym) {
-                    const uint32_t sums[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
-                    const int4 ea = *reinterpret_cast<const int4*>(ec + k), eb = *reinterpret_cast<const int4*>(ec + k + 4);
-                    const int ek[8] = {ea.x, ea.y, ea.z, ea.w, eb.x, eb.y, eb.z, eb.w};
-                    f16x8 hi, lo;
+                const int k = (s * 2 + (lane >> 5)) * 8;
+                const uint4 u = *reinterpret_cast<const uint4*>(turn + row * kPitch + k), w = *reinterpret_cast<const uint4*>(turn + row * kPitch + k + 4);
+                const uint32_t x8[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
+                f16x8 hi, lo;
 #pragma unroll
-                    for (int m = 0; m < 8; m++) {
-                        float r = ldexpf(__uint_as_float(sums[m]), -ek[m]);
-                        if (fetches)
-#pragma unroll
-                            for (int t = 0; t < kTerms; t++) r = fmaf(add, (float)et[t][s][0][m] + (float)et[t][s][1][m], r);
-                        if (apart) r = ldexpf(r, -ek[m] - kShift);
-                        _Float16 h, l;
-                        split(r, h, l);
-                        hi[m] = h;
-                        lo[m] = l;
-                    }
-                    *reinterpret_cast<f16x8*>(d) = hi;
-                    *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
-                } else {
-                    const uint4 hi = make_uint4((u.x & 0xffff) | (u.y << 16), (u.z & 0xffff) | (u.w << 16), (w.x & 0xffff) | (w.y << 16), (w.z & 0xffff) | (w.w << 16));
-                    const uint4 lo = make_uint4((u.x >> 16) | (u.y & 0xffff0000u), (u.z >> 16) | (u.w & 0xffff0000u), (w.x >> 16) | (w.y & 0xffff0000u),
-                                                (w.z >> 16) | (w.w & 0xffff0000u));
-                    *reinterpret_cast<uint4*>(d) = hi;
-                    *reinterpret_cast<uint4*>(d + kPartBytes) = lo;
+                for (int m = 0; m < 8; m++) {
+                    _Float16 h, l;
+                    split(ldexpf(__uint_as_float(x8[m]), up), h, l);
+                    hi[m] = h;
+                    lo[m] = l;
                 }
+                char* d = X + panel_at(i0 + x * 32 + row, j0 + k, q.np);
+                *reinterpret_cast<f16x8*>(d) = hi;
+                *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
             }
         }
     }
-}
-// What a row's exponent does to the results of a product.
-template <int MODE>
-__device__ __forceinline__ int result_exponent(int first, const NsOp& op) {
-    const int e = exponent_at(first, op.from);
-    return MODE == kStep ? exponent_at(first, op.to) - e : MODE == kLast ? -e : e;
 }
 
 // A macro-tile: WR x WC wavefronts of FM x FN results of 32 x 32 each, ST stages of KS panels (16 KS columns of the contraction) in LDS.
@@ -666,11 +818,12 @@ template <int MODE, typename S>
 __global__ void __launch_bounds__(64 * S::kWaves, 2) ns_product_kernel(const NsGroup* __restrict__ group, NsSizes sizes, NsOp op, int now, int splits) {
     const NsGroup& g = *group;
     constexpr int FM = S::FM, FN = S::FN, ST = S::ST;
+    constexpr bool kSym = MODE == kGram || MODE == kPoly || MODE == kPair;
     __shared__ __align__(1024) char lds[S::kLds];
     __shared__ __align__(16) int ex[S::BM + S::BN];
+    __shared__ __align__(16) float cf[kSym ? 4 : S::BM];
     static_assert(S::BM + S::BN <= 64 * S::kWaves, "a thread fetches one exponent");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave % S::WR, wc = wave / S::WR;
-    constexpr bool kSym = MODE == kGram || MODE == kPoly || MODE == kPair;
     // workgroups go to the eight dies in turn: each die gets one run of the tiles
     int wg = blockIdx.x;
     {
@@ -694,11 +847,14 @@ __global__ void __launch_bounds__(64 * S::kWaves, 2) ns_product_kernel(const NsG
     const int64_t xbytes = (int64_t)q.mp * q.np * 4;
     const int nk = (MODE == kGram ? q.np : q.mp) >> 4;           // panels along the contraction, a multiple of 4
     const int64_t square = (int64_t)q.mp * q.mp * 4;
-    const char* Pb = g.space + (MODE == kGram ? q.X + now * xbytes : q.A + op.p * square);
-    const char* Qb = g.space + (MODE == kGram ? q.X + now * xbytes : kSym ? q.A + op.q * square : q.XT + now * xbytes);
+    const char* Pb = g.space + (MODE == kGram ? q.X : q.A + op.p * square);
+    const char* Qb = g.space + (MODE == kGram ? q.X : kSym ? q.A + op.q * square : q.XT + now * xbytes);
 
-    // (older than the loads that are counted below, which it can only make wait longer)
-    const int exponent = reinterpret_cast<const int*>(g.space + q.exponents)[min(tid < S::BM ? ti * S::BM + tid : tj * S::BN + tid - S::BM, q.mp - 1)];
+    // a thread's row or column (older than the loads that are counted below, which they can only make wait longer)
+    const int mine = tid < S::BM ? min(ti * S::BM + tid, q.mp - 1) : min(tj * S::BN + tid - S::BM, (kSym ? q.mp : q.np) - 1);
+    const int exponent = reinterpret_cast<const int*>(g.space + (kSym || tid < S::BM ? q.exponents : q.columns))[mine];
+    float coefficient = 0.f;
+    if constexpr (!kSym) coefficient = reinterpret_cast<const float*>(g.space + q.coefficients)[min(mine, q.mp - 1)];
 
     // a wavefront loads a part of one row block's panels per step
     const char* src;
@@ -811,10 +967,13 @@ __global__ void __launch_bounds__(64 * S::kWaves, 2) ns_product_kernel(const NsG
             return;
         }
     }
-    if (tid < S::BM + S::BN) ex[tid] = result_exponent<MODE>(exponent, op);
+    if (tid < S::BM + S::BN) ex[tid] = kSym ? exponent_at(exponent, op.from) : exponent;
+    if (!kSym && tid < S::BM) cf[tid] = coefficient;
     __syncthreads();
-    store_results<MODE, FM, FN>(g, q, acc, ti * S::BM + wr * 32 * FM, tj * S::BN + wc * 32 * FN, ti == tj, now, op, ex + wr * 32 * FM, ex + S::BM + wc * 32 * FN,
-                                reinterpret_cast<uint32_t*>(lds + wave * S::kTurn));
+    const int ri = wr * 32 * FM, cj = wc * 32 * FN;
+    uint32_t* turn = reinterpret_cast<uint32_t*>(lds + wave * S::kTurn);
+    if constexpr (kSym) store_square<MODE, FM, FN>(g, q, acc, ti * S::BM + ri, tj * S::BN + cj, ti == tj, op, ex + ri, ex + S::BM + cj, turn);
+    else store_step<MODE, FM, FN>(g, q, acc, ti * S::BM + ri, tj * S::BN + cj, now, op, ex + ri, ex + S::BM + cj, cf + ri, turn);
 }
 
 // Adds up the parts of A's tiles, in their order: a wavefront takes one block of 32 x 32.
@@ -856,15 +1015,15 @@ __global__ void __launch_bounds__(256) ns_combine_kernel(const NsGroup* __restri
     }
     const int w = blk / (S::FM * S::FN), x = blk / S::FN % S::FM, y = blk % S::FN;
     const int i0 = ti * S::BM + (w % S::WR * S::FM + x) * 32, j0 = tj * S::BN + (w / S::WR * S::FN + y) * 32;
-    ex[wave][lane] = result_exponent<kGram>(reinterpret_cast<const int*>(g.space + q.exponents)[min((lane < 32 ? i0 : j0 - 32) + lane, q.mp - 1)], op);
+    ex[wave][lane] = exponent_at(reinterpret_cast<const int*>(g.space + q.exponents)[min((lane < 32 ? i0 : j0 - 32) + lane, q.mp - 1)], op.from);
     __syncthreads();
-    store_results<kGram, 1, 1>(g, q, acc, i0, j0, ti == tj, 0, op, ex[wave], ex[wave] + 32, turn + wave * 32 * turn_pitch(1));
+    store_square<kGram, 1, 1>(g, q, acc, i0, j0, ti == tj, op, ex[wave], ex[wave] + 32, turn + wave * 32 * turn_pitch(1));
 }
 
 // ---------------------------------------------------------------- matrices with a side of at most 64
 // Here a launch is longer than what it computes, so a whole iteration is one launch.  A workgroup holds some of X's column blocks of 64; it adds up the
 // parts of A that the workgroups have left (its own and the others'), computes B (64 x 64, every workgroup the same), its blocks of X and their
-// part of the next A.  X is kept as its transpose only.  The first launch takes U in place of B X, the last one leaves the results.  64 x 320: 6 us a
+// part of the next A.  X is kept as its transpose and in fp32.  The first launch takes U in place of B X, the last one leaves the results.  64 x 320: 6 us a
 // launch, 45 in all (some 75 with the products above); it is the launches that bound it, and within one the parts' way through memory.
 enum { kFirst, kMiddle, kFinal };
 
@@ -900,15 +1059,34 @@ __device__ __forceinline__ void multiply(const char* image, int r0, const char* 
 }
 
 // A lane's results of a block of 64 x 64: rows i + 8 p + 0 .. 3, column j.
-// A symmetric block D p D as the image of D p (`times` 1) or D p D^-1 (2): four rows of a column are four columns of a row.
-__device__ __forceinline__ void store_symmetric(char* dst, const float (&x)[4][4], const int (&e)[4][4], int times, int i, int j) {
+// The exponents of a lane's rows i .. i + 3, from LDS, where rows have grown by 2^grown.
+struct RowExponents {
+    const int* first;
+    int grown;
+    __device__ __forceinline__ void at(int i, int (&e)[4]) const {
+        const int4 f = *reinterpret_cast<const int4*>(first + i);
+        e[0] = exponent_at(f.x, grown);
+        e[1] = exponent_at(f.y, grown);
+        e[2] = exponent_at(f.z, grown);
+        e[3] = exponent_at(f.w, grown);
+    }
+};
+// A symmetric block D p D as the image of D p: four rows of a column are four columns of a row.  `coefficients`: where the diagonal goes, with `base` added (B).
+__device__ __forceinline__ void store_symmetric(char* dst, const float (&x)[4][4], const RowExponents& rows, int i, int j, float* coefficients = nullptr, float base = 0.f) {
 #pragma unroll
     for (int p = 0; p < 4; p++) {
+        int e[4];
+        rows.at(i + p * 8, e);
         f16x4 hi, lo;
 #pragma unroll
         for (int k = 0; k < 4; k++) {
+            float w = ldexpf(x[p][k], -e[k]);
+            if (coefficients && i + p * 8 + k == j) {
+                coefficients[j] = base + ldexpf(w, -e[k] - kShift);
+                w = 0.f;
+            }
             _Float16 h, l;
-            split(ldexpf(x[p][k], -times * e[p][k]), h, l);
+            split(w, h, l);
             hi[k] = h;
             lo[k] = l;
         }
@@ -917,55 +1095,45 @@ __device__ __forceinline__ void store_symmetric(char* dst, const float (&x)[4][4
         *reinterpret_cast<f16x4*>(d + kPartBytes) = lo;
     }
 }
-// X's block as its transpose, and as it is.
-__device__ __forceinline__ void store_both(char* XT, char* X, const float (&x)[4][4], int i, int j) {
+// X's block as its transpose, with its column's exponent f, and as it is, with its rows' exponents.
+__device__ __forceinline__ void store_both(char* XT, char* X, const float (&x)[4][4], const RowExponents& rows, int f, int i, int j) {
 #pragma unroll
     for (int p = 0; p < 4; p++) {
+        int e[4];
+        rows.at(i + p * 8, e);
         f16x4 hi, lo;
 #pragma unroll
         for (int k = 0; k < 4; k++) {
             _Float16 h, l;
-            split(x[p][k], h, l);
-            hi[k] = h;
-            lo[k] = l;
+            split(ldexpf(x[p][k], kShiftX + e[k]), h, l);
             char* d = X + image_at(i + p * 8 + k, j);
             *reinterpret_cast<_Float16*>(d) = h;
             *reinterpret_cast<_Float16*>(d + kPartBytes) = l;
+            split(ldexpf(x[p][k], kShiftX + f), h, l);
+            hi[k] = h;
+            lo[k] = l;
         }
         char* d = XT + image_at(j, i + p * 8);
         *reinterpret_cast<f16x4*>(d) = hi;
         *reinterpret_cast<f16x4*>(d + kPartBytes) = lo;
     }
 }
-// The exponents of a lane's rows behind `steps` steps.
-__device__ __forceinline__ void exponents_of(const int* first, int growth, int steps, int i, int (&e)[4][4]) {
-    const int grown = grown_by(growth, steps);
-#pragma unroll
-    for (int p = 0; p < 4; p++) {
-        const int4 f = *reinterpret_cast<const int4*>(first + i + p * 8);
-        e[p][0] = exponent_at(f.x, grown);
-        e[p][1] = exponent_at(f.y, grown);
-        e[p][2] = exponent_at(f.z, grown);
-        e[p][3] = exponent_at(f.w, grown);
-    }
-}
-// a X + B X of X's block, X as its transpose
-__device__ __forceinline__ void step_block(const char* B, const char* XT, int wr, int wc, int i, int j, float a, float (&x)[4][4]) {
-    f16x4 eh[4], el[4];
-#pragma unroll
-    for (int p = 0; p < 4; p++) {
-        const char* e = XT + image_at(j, i + p * 8);
-        eh[p] = *reinterpret_cast<const f16x4*>(e);
-        el[p] = *reinterpret_cast<const f16x4*>(e + kPartBytes);
-    }
+// x <- coefficients x + B X of X's block, f: the exponent of this lane's column
+__device__ __forceinline__ void step_block(const char* B, const char* XT, int wr, int wc, int i, const float* coefficients, const RowExponents& rows, int f, float (&x)[4][4]) {
     f32x16 acc;
 #pragma unroll
     for (int k = 0; k < 16; k++) acc[k] = 0.f;
     multiply(B, wr * 32, XT, wc * 32, acc);
 #pragma unroll
-    for (int p = 0; p < 4; p++)
-#pragma unroll
-        for (int k = 0; k < 4; k++) x[p][k] = fmaf(a, (float)eh[p][k] + (float)el[p][k], acc[p * 4 + k] / kScale);
+    for (int p = 0; p < 4; p++) {
+        const float4 c = *reinterpret_cast<const float4*>(coefficients + i + p * 8);
+        int e[4];
+        rows.at(i + p * 8, e);
+        x[p][0] = fmaf(c.x, x[p][0], ldexpf(acc[p * 4], -kShift - kShiftX - f - e[0]));
+        x[p][1] = fmaf(c.y, x[p][1], ldexpf(acc[p * 4 + 1], -kShift - kShiftX - f - e[1]));
+        x[p][2] = fmaf(c.z, x[p][2], ldexpf(acc[p * 4 + 2], -kShift - kShiftX - f - e[2]));
+        x[p][3] = fmaf(c.w, x[p][3], ldexpf(acc[p * 4 + 3], -kShift - kShiftX - f - e[3]));
+    }
 }
 
 template <int PHASE>
@@ -973,6 +1141,7 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
     const NsGroup& g = *group;
     __shared__ __align__(16) char image[3][kImage];      // A (set-up: U in fp32), B, X's block with its rows along the contraction
     __shared__ __align__(16) SetUp setup;
+    __shared__ __align__(16) float coefficients[64];
     const int now = step & 1;                            // the sums' buffer of this step
     const int nt = sizes.blocks[blockIdx.y] >> 16, parts = narrow_parts(nt), part = blockIdx.x;
     if (part >= parts) return;
@@ -981,12 +1150,12 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
     float4* sums = reinterpret_cast<float4*>(g.space + q.A);             // two buffers of `parts` images of 64 x 64 in fp32, as they lie in registers
     auto sum_at = [&](int buffer, int p, int v) { return (((int64_t)buffer * parts + p) * 4 + wave) * 256 + v * 64 + lane; };
     const int i = wr * 32 + (lane >> 5) * 4, j = wc * 32 + (lane & 31);    // this lane's results: rows i + 8 p + 0 .. 3, column j of a block
-    Scale scaled(1.0);
-    int e[4][4] = {};                                    // exponents of this lane's rows
+    double length = 1.0;
+    const RowExponents rows{setup.row, grown_by(g.growth, step)};
     if constexpr (PHASE == kFirst) {
-        scaled = Scale(length_and_exponents(g, q, 0, part == 0, setup));
+        length = length_and_exponents(g, q, 0, -1, part == 0, false, setup);
     } else {
-        if (tid < 64) setup.exponent[tid] = reinterpret_cast<const int*>(g.space + q.exponents)[tid];
+        if (tid < 64) setup.row[tid] = reinterpret_cast<const int*>(g.space + q.exponents)[tid];
         float4 t[4];
 #pragma unroll
         for (int v = 0; v < 4; v++) t[v] = sums[sum_at(now, 0, v)];
@@ -1010,8 +1179,7 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
             a[p][3] = t[p].w * kGramFactor;
         }
         __syncthreads();
-        exponents_of(setup.exponent, g.growth, step, i, e);
-        store_symmetric(image[0], a, e, 1, i, j);
+        store_symmetric(image[0], a, rows, i, j);
         __syncthreads();
         f32x16 acc;
 #pragma unroll
@@ -1021,72 +1189,61 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
         for (int p = 0; p < 4; p++)
 #pragma unroll
             for (int k = 0; k < 4; k++) a[p][k] = fmaf(g.b, a[p][k], acc[p * 4 + k] * (g.c / kScale));
-        store_symmetric(image[1], a, e, 2, i, j);
+        store_symmetric(image[1], a, rows, i, j, coefficients, g.a);
         __syncthreads();
     }
-    int next_e[4][4];
-    if constexpr (PHASE == kMiddle) exponents_of(setup.exponent, g.growth, step + 1, i, next_e);
     f32x16 gram;
 #pragma unroll
     for (int k = 0; k < 16; k++) gram[k] = 0.f;
     for (int t = part * nt / parts; t < (part + 1) * nt / parts; t++) {
-        char* X = in_global(g.space + q.XT + (int64_t)t * kImage);
+        char* XT = in_global(g.space + q.XT + (int64_t)t * kImage);
+        float4* E = reinterpret_cast<float4*>(in_global(g.space + q.E + block_at(wr * 32, t * 64 + wc * 32, 64)));
+        float x[4][4];
         if constexpr (PHASE == kFirst) {
             float (*u)[65] = reinterpret_cast<float (*)[65]>(image[0]);      // [i][j] (16640 bytes: reaches into the second image, which is free)
             const int r0 = q.flip ? t * 64 : 0, c0 = (q.flip ? 0 : t * 64) + wave * 16;
             const int r = r0 + lane, t0 = min(r, q.rows - 1) / q.base0, o0 = r - t0 * q.base0, e0 = min(q.base0, q.rows - t0 * q.base0);
-            float x[16], m[16];
-            read_columns(q, q.G, r < q.rows, t0, o0, e0, c0, x);
+            float y[16], m[16];
+            read_columns(q, q.G, r < q.rows, t0, o0, e0, c0, y);
             if (g.mu >= 0.f) read_columns(q, q.M, r < q.rows, t0, o0, e0, c0, m);
+            largest_of_columns(g, q, t * 64, setup);
+            const Scale scaled(length);
 #pragma unroll
             for (int s = 0; s < 16; s++) {
-                if (g.mu >= 0.f) x[s] = g.nesterov ? fmaf(g.mu, m[s], x[s]) : m[s];
-                if (q.flip) u[wave * 16 + s][lane] = scaled(x[s], setup.exponent[wave * 16 + s]);
-                else u[lane][wave * 16 + s] = scaled(x[s], setup.exponent[lane]);
+                if (g.mu >= 0.f) y[s] = g.nesterov ? fmaf(g.mu, m[s], y[s]) : m[s];
+                if (q.flip) u[wave * 16 + s][lane] = scaled(y[s], 0);
+                else u[lane][wave * 16 + s] = scaled(y[s], 0);
             }
             __syncthreads();
+            if (wave == 0) column_exponents(g, q, t * 64, true, length, setup);
+            __syncthreads();
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const int k = (wave * 2 + h) * 8;
-                f16x8 hi, lo;
+            for (int p = 0; p < 4; p++) {
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    _Float16 y, z;
-                    split(u[lane][k + e], y, z);
-                    hi[e] = y;
-                    lo[e] = z;
-                }
-                char* d = image[2] + image_at(lane, k);
-                *reinterpret_cast<f16x8*>(d) = hi;
-                *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
-#pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    _Float16 y, z;
-                    split(u[k + e][lane], y, z);
-                    hi[e] = y;
-                    lo[e] = z;
-                }
-                d = X + image_at(lane, k);
-                *reinterpret_cast<f16x8*>(d) = hi;
-                *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
+                for (int k = 0; k < 4; k++) x[p][k] = u[i + p * 8 + k][j];
+                E[p * 64] = make_float4(x[p][0], x[p][1], x[p][2], x[p][3]);
             }
+            store_both(XT, image[2], x, rows, setup.column[j], i, j);
         } else {
-            float x[4][4];
-            step_block(image[1], X, wr, wc, i, j, g.a, x);
+            const int column = reinterpret_cast<const int*>(g.space + q.columns)[t * 64 + j];
+#pragma unroll
+            for (int p = 0; p < 4; p++) {
+                const float4 y = E[p * 64];
+                x[p][0] = y.x;
+                x[p][1] = y.y;
+                x[p][2] = y.z;
+                x[p][3] = y.w;
+            }
+            step_block(image[1], XT, wr, wc, i, coefficients, rows, exponent_at(column, rows.grown), x);
             if constexpr (PHASE == kFinal) {
-#pragma unroll
-                for (int p = 0; p < 4; p++)
-#pragma unroll
-                    for (int k = 0; k < 4; k++) x[p][k] = ldexpf(x[p][k], -e[p][k]) * (1.f / kScaleX);
                 apply_results(q, x, i, t * 64 + j);
                 continue;
             }
 #pragma unroll
-            for (int p = 0; p < 4; p++)
-#pragma unroll
-                for (int k = 0; k < 4; k++) x[p][k] = ldexpf(x[p][k], next_e[p][k] - e[p][k]);
+            for (int p = 0; p < 4; p++) E[p * 64] = make_float4(x[p][0], x[p][1], x[p][2], x[p][3]);
             __syncthreads();                             // everybody has read X's block, which is overwritten, and is done with the last one's image
-            store_both(X, image[2], x, i, j);
+            const RowExponents next{setup.row, grown_by(g.growth, step + 1)};
+            store_both(XT, image[2], x, next, exponent_at(column, next.grown), i, j);
         }
         __syncthreads();
         multiply(image[2], wr * 32, image[2], wc * 32, gram);
@@ -1110,12 +1267,16 @@ __global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, i
     __shared__ __align__(16) char images[2 * kHeldBlocks + 1][kImage];       // X's transpose and X by block; A, then B
     __shared__ double red[4 * kHeldBlocks][64];          // sums of squares of X's rows
     __shared__ __align__(16) int exponent[64];
+    __shared__ __align__(16) float coefficients[64];
+    __shared__ float largest[kHeldBlocks][4][64];        // of X's columns
     const NsMatrix& q = g.mat[blockIdx.x];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane((tid >> 6) & 3), t = __builtin_amdgcn_readfirstlane(tid >> 8);
     const int wr = wave & 1, wc = wave >> 1, nt = q.np >> 6;
     const int i = wr * 32 + (lane >> 5) * 4, j = wc * 32 + (lane & 31);
     const bool mine = t < nt;                            // (the launch has as many wavefronts as its longest matrix wants)
     char *XT = images[t], *X = images[kHeldBlocks + t], *S = images[2 * kHeldBlocks];
+    float x[4][4];                                       // X in fp32, from step to step
+    int column;                                          // the first exponent of this lane's column
     {
         const int r0 = q.flip ? t * 64 : 0, c0 = (q.flip ? 0 : t * 64) + wave * 16;
         const int r = r0 + lane, t0 = min(r, q.rows - 1) / q.base0, o0 = r - t0 * q.base0, e0 = min(q.base0, q.rows - t0 * q.base0);
@@ -1139,10 +1300,16 @@ __global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, i
         if (q.flip) {
             const double x = sum16(square, lane);
             if ((lane & 3) == 0) red[t][wave * 16 + sum16_index(lane)] = x;
+            largest[t][wave][lane] = largest_of(u);
         } else {
 #pragma unroll
             for (int s = 1; s < 16; s++) square[0] += square[s];
             red[tid >> 6][lane] = square[0];
+            const uint32_t x = largest16(u, lane);
+            if ((lane & 7) == 0) {
+                largest[t][0][wave * 16 + (lane >> 3)] = from_upper_half(x & 0xffffu);
+                largest[t][0][wave * 16 + 8 + (lane >> 3)] = from_upper_half(x >> 16);
+            }
         }
         __syncthreads();
         double row = 0.0;
@@ -1151,33 +1318,28 @@ __global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, i
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
         const double length = sqrt(sum) + g.eps;         // (every wavefront by itself, in the same order)
-        const int mine_e = row_exponent(row, length);
-        if (tid < 64) exponent[lane] = mine_e;
-        __syncthreads();
+        if (tid < 64) exponent[lane] = exponent_of(sqrt(row), length);
+        const float most = q.flip ? fmaxf(fmaxf(largest[t][0][j], largest[t][1][j]), fmaxf(largest[t][2][j], largest[t][3][j])) : largest[t][0][j];
+        column = exponent_of((double)most * 8.0, length);
+        // through LDS to this lane's results: column c of X's block is 64 floats, in an order in which neither way has many conflicts
         const Scale scaled(length);
-        if (mine) {
-            char *along = q.flip ? XT : X, *across = q.flip ? X : XT;
+        float* turn = reinterpret_cast<float*>(X);
+        auto at = [](int row, int c) { return c * 64 + (row ^ ((c & 15) << 2)); };
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                f16x8 hi, lo;
+        for (int s = 0; s < 16; s++) turn[q.flip ? at(wave * 16 + s, lane) : at(lane, wave * 16 + s)] = scaled(u[s], 0);
+        __syncthreads();
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    _Float16 y, z;
-                    split(scaled(u[h * 8 + e], q.flip ? exponent[wave * 16 + h * 8 + e] : mine_e), y, z);
-                    hi[e] = y;
-                    lo[e] = z;
-                    char* d = across + image_at(wave * 16 + h * 8 + e, lane);
-                    *reinterpret_cast<_Float16*>(d) = y;
-                    *reinterpret_cast<_Float16*>(d + kPartBytes) = z;
-                }
-                char* d = along + image_at(lane, wave * 16 + h * 8);
-                *reinterpret_cast<f16x8*>(d) = hi;
-                *reinterpret_cast<f16x8*>(d + kPartBytes) = lo;
-            }
+        for (int p = 0; p < 4; p++) {
+            const float4 y = *reinterpret_cast<const float4*>(turn + at(i + p * 8, j));
+            x[p][0] = y.x;
+            x[p][1] = y.y;
+            x[p][2] = y.z;
+            x[p][3] = y.w;
         }
     }
-    int e[4][4], next_e[4][4];                           // exponents of this lane's rows
-    exponents_of(exponent, g.growth, 0, i, e);
+    RowExponents rows{exponent, 0};
+    __syncthreads();
+    if (mine) store_both(XT, X, x, rows, column, i, j);
     for (int step = 0;; step++) {
         __syncthreads();
         f32x16 acc;
@@ -1205,7 +1367,7 @@ __global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, i
             for (int p = 0; p < 4; p++)
 #pragma unroll
                 for (int k = 0; k < 4; k++) a[p][k] = acc[p * 4 + k] * kGramFactor;
-            store_symmetric(S, a, e, 1, i, j);
+            store_symmetric(S, a, rows, i, j);
         }
         __syncthreads();
         if (t == 0) {
@@ -1218,28 +1380,16 @@ __global__ void __launch_bounds__(256 * kHeldBlocks) ns_held_kernel(NsGroup g, i
                 for (int k = 0; k < 4; k++) a[p][k] = fmaf(g.b, a[p][k], acc[p * 4 + k] * (g.c / kScale));
         }
         __syncthreads();                                 // A has been read
-        if (t == 0) store_symmetric(S, a, e, 2, i, j);
+        if (t == 0) store_symmetric(S, a, rows, i, j, coefficients, g.a);
         __syncthreads();
-        float x[4][4];
-        if (mine) step_block(S, XT, wr, wc, i, j, g.a, x);
+        if (mine) step_block(S, XT, wr, wc, i, coefficients, rows, exponent_at(column, rows.grown), x);
         if (step + 1 == steps) {
-#pragma unroll
-            for (int p = 0; p < 4; p++)
-#pragma unroll
-                for (int k = 0; k < 4; k++) x[p][k] = ldexpf(x[p][k], -e[p][k]) * (1.f / kScaleX);
             if (mine) apply_results(q, x, i, t * 64 + j);
             return;
         }
-        exponents_of(exponent, g.growth, step + 1, i, next_e);
-#pragma unroll
-        for (int p = 0; p < 4; p++)
-#pragma unroll
-            for (int k = 0; k < 4; k++) {
-                x[p][k] = ldexpf(x[p][k], next_e[p][k] - e[p][k]);
-                e[p][k] = next_e[p][k];
-            }
+        rows.grown = grown_by(g.growth, step + 1);
         __syncthreads();                                 // X's transpose has been read
-        if (mine) store_both(XT, X, x, i, j);
+        if (mine) store_both(XT, X, x, rows, exponent_at(column, rows.grown), i, j);
     }
 }
 
@@ -1283,11 +1433,6 @@ bool in_range(const nnt_newton_schulz_cfg& c, double* reach = nullptr, double* b
     return true;
 }
 
-// What is kept out of the factor P_1 P_0 of two steps at once, as a multiple of the identity: rounded among the factor's entries it would cost as much as the rest.  The first
-// steps find small singular values and a factor near a^2, the later ones values around 1 and a factor between 0.4 and some 10.  (a^2 for all of them, in a model of the
-// arithmetic on the host: errors of 512 x 2560 3.7e-6 instead of 3.3e-6.)
-double kept_out(const nnt_newton_schulz_cfg& c, bool first) { return first ? c.a * c.a : c.a * c.a / 4.0; }
-
 // What a step can make a row grow by, the largest |a + b s^2 + c s^4|, as its logarithm in 1/256 (rounded up; rows that shrink are followed for 16 binary places a step).
 int growth_of(const nnt_newton_schulz_cfg& c) {
     double before = 1.0;
@@ -1299,7 +1444,7 @@ int growth_of(const nnt_newton_schulz_cfg& c) {
 }
 
 // Whether two steps can be taken at once.  The buffers hold polynomials in A = X X^T without a constant term, p(s^2) = s^2 r(s^2), as D p, whose entries reach |r| s in a row
-// of length 1 and |p| in one that keeps its length; the last one, P_1 P_0, the same at a quarter of the scale and with a multiple of the identity.  r has degree 11 in s^2 at most:
+// of length 1 and |p| in one that keeps its length; the last one, P_1 P_0 without its constant term, the same at a quarter of the scale.  r has degree 11 in s^2 at most:
 // between two of 257 places it rises by less than 4 % of its largest value (|r''| <= 11^2 (11^2 - 1) / 3 (2 / l)^2 of it), s by what the next place has; the margin is 6 %.
 bool pairs_in_range(const nnt_newton_schulz_cfg& c) {
     double reach = 1.0;
@@ -1311,7 +1456,7 @@ bool pairs_in_range(const nnt_newton_schulz_cfg& c) {
         for (double r : {r0, p0, p0 * p0, r1}) most = std::max(most, at * std::fabs(r));
         last = std::max(last, at * std::fabs(r1 * l * r0 + c.a * (r0 + r1)));
     }
-    return most < 15.0 && last + c.a * c.a < 60.0;
+    return most < 15.0 && last < 60.0;
 }
 
 bool whole_matrix(const nnt_ctx* ctx, const nnt_tensor* t) {
@@ -1369,24 +1514,21 @@ std::vector<Item> plan(const nnt_newton_schulz_cfg& c, int growth, bool pairs) {
     for (int left = c.steps; left > 0;) {
         const bool two = pairs && left >= 2;
         const int from = grown_by(growth, c.steps - left);
-        auto poly = [&](int mode, int p, int q, int e, int d, int apart, float mul, float add, float diag) {
-            out.push_back(Item{mode, NsOp{p, q, e, d, apart, from, from, mul, add, diag}, now});
+        auto poly = [&](int mode, int p, int q, int e, int d, int last, float mul, float add, float base) {
+            out.push_back(Item{mode, NsOp{p, q, e, d, last, from, from, 0, mul, add, base}, now});
         };
-        out.push_back(Item{kGram, NsOp{0, 0, 0, 0, 0, from, from, 1.f, 0.f, 0.f}, now});
-        const int factor = two ? 0 : 1;                      // the buffer of what X is multiplied by
-        float kept = A;
+        out.push_back(Item{kGram, NsOp{0, 0, 0, 0, 0, from, from, 0, 1.f, 0.f, 0.f}, now});
         if (two) {
-            kept = (float)kept_out(c, left == c.steps);
             poly(kPoly, 0, 0, 0, 1, 0, C, B, 0.f);           // B_0 = P_0 - a I
             poly(kPoly, 1, 0, 0, 2, 0, 1.f, A, 0.f);         // P_0 A_0
             poly(kPoly, 1, 2, 2, 3, 0, 1.f, A, 0.f);         // A_1 = P_0 (P_0 A_0)
             poly(kPoly, 3, 3, 3, 2, 0, C, B, 0.f);           // B_1 = P_1 - a I
-            poly(kPair, 2, 1, 0, 0, 1, 1.f, A, A * A - kept);    // P_1 P_0 = B_1 B_0 + a B_1 + a B_0 + a^2 I without what is kept out
+            poly(kPair, 2, 1, 0, 0, 1, 1.f, A, A * A);       // P_1 P_0 = B_1 B_0 + a B_1 + a B_0 + a^2 I
         } else {
-            poly(kPoly, 0, 0, 0, 1, 1, C, B, 0.f);
+            poly(kPoly, 0, 0, 0, 1, 1, C, B, A);
         }
         left -= two ? 2 : 1;
-        out.push_back(Item{left ? kStep : kLast, NsOp{factor, 0, 0, 0, 0, from, grown_by(growth, c.steps - left), two ? (float)(1 << kPairShift) : 1.f, kept, 0.f}, now});
+        out.push_back(Item{left ? kStep : kLast, NsOp{two ? 0 : 1, 0, 0, 0, 0, from, grown_by(growth, c.steps - left), -kShift - kShiftX + (two ? kPairShift : 0), 1.f, 0.f, 0.f}, now});
         now = 1 - now;
     }
     return out;
@@ -1411,7 +1553,7 @@ Launch choose(const NsSizes& g, int mode) {
             tiles += t;
             panels += t * c;
             longest = std::max(longest, c);
-            bytes += 4096.0 * mb * (mode == kGram ? 4 * mb : mode == kPoly ? 6 * mb : mode == kPair ? 8 * mb : mode == kStep ? 12 * nb : 16 * nb);
+            bytes += 4096.0 * mb * (mode == kGram ? 4 * mb : mode == kPoly ? 6 * mb : mode == kPair ? 8 * mb : mode == kStep ? 16 * nb : 16 * nb);
         }
         for (int splits = 1; splits <= 64; splits *= 2) {
             if (splits > 1 && (mode != kGram || s == 2 || tiles * splits > 512 || longest / splits < 8)) break;
@@ -1493,18 +1635,22 @@ int32_t make_set(nnt_ctx* ctx, const char* label, const nnt_newton_schulz_cfg& c
         shortest = std::min(shortest, m);
         if (kind != kProducts) w.parts = std::max(w.parts, narrow ? narrow_parts((int)nb) : (int)nb);
         // squares are added up by as many workgroups as fill the chip; the set-up reads one sum per row and part
-        const int64_t rounds = (q.np + 255) / 256;
-        q.splits = (int32_t)std::min({rounds, std::max<int64_t>(1, 512 / mb), std::max<int64_t>(32, std::min<int64_t>(rounds / 16, 128))});
+        const int64_t rounds = (q.np + kNormSpan - 1) / kNormSpan;
+        q.splits = (int32_t)std::min({rounds, std::max<int64_t>(1, 1024 / mb), std::max<int64_t>(32, std::min<int64_t>(rounds / 32, 128))});
         w.norm_blocks = std::max(w.norm_blocks, (unsigned)(mb * q.splits));
-        // X and its transpose, two buffers each, and four square ones; narrow matrices: the transpose once, and two times A in parts
+        // X once, its transpose twice, X in fp32, and four square buffers; narrow matrices: the transpose and fp32, and two times A in parts
         const int64_t x = (int64_t)q.mp * q.np * 4, a = (int64_t)q.mp * q.mp * 4;
         q.X = bytes;
-        q.XT = narrow ? bytes : q.X + 2 * x;
-        q.A = narrow ? q.XT + x : q.XT + 2 * x;
+        q.XT = narrow ? bytes : q.X + x;
+        q.E = narrow ? q.XT + x : q.XT + 2 * x;
+        q.A = q.E + x;
         q.squares = q.A + (narrow ? (int64_t)narrow_parts((int)nb) * 64 * 64 * 4 * 2 : 4 * a);
         q.part = q.squares + (int64_t)q.splits * q.mp * 8;
         q.exponents = q.part + mb * q.splits * 8;
-        bytes = (q.exponents + q.mp * 4 + 255) / 256 * 256;
+        q.columns = q.exponents + q.mp * 4;
+        q.coefficients = q.columns + (int64_t)q.np * 4;
+        q.largest = q.coefficients + q.mp * 4;
+        bytes = (q.largest + mb * (q.flip ? 4 : 1) * q.np * 2 + 255) / 256 * 256;
         q.G = MatView{t.G->d_tiles, t.G->dtype};
         q.P = MatView{t.P->d_tiles, t.P->dtype};
         if (t.M) q.M = MatView{t.M->d_tiles, NNT_F32};
@@ -1550,7 +1696,7 @@ int32_t submit_set(nnt_ctx* ctx, const char* label, int steps, Set& w) {
         });
     const int grams = (int)std::count_if(w.items.begin(), w.items.end(), [](const Item& t) { return t.mode == kGram; });      // each with a launch that adds up its parts, if it is cut
     return submit(ctx, w.acc, [&](hipStream_t st) {
-        hipLaunchKernelGGL(ns_norm_kernel, dim3(w.norm_blocks, (unsigned)g.n), dim3(1024), 0, st, g);
+        hipLaunchKernelGGL(ns_norm_kernel, dim3(w.norm_blocks, (unsigned)g.n), dim3(64 * kNormWaves), 0, st, g);
         if (w.kind == kNarrow) {
             const dim3 grid((unsigned)w.parts, (unsigned)g.n), block(256);
             hipLaunchKernelGGL((ns_narrow_kernel<kFirst>), grid, block, 0, st, there, w.sizes, 0);

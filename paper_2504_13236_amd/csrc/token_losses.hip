@@ -134,8 +134,8 @@ struct Exchange {
 // Maximum, sum of shifted exponentials and the label's logit of a column that is read once, U vectors per thread at a time:
 // a running maximum per thread, the sum rescaled where it moves.  Hundreds of logp add up in a reward, so log(sum) is kept free of an error that all of them
 // share: bf16 logits have few different values, each rounded the same way whenever it is added to a large sum, so a thread's sum is put together from
-// those of U vectors, and the threads' sums meet in 64 bits.  (One chain of additions: 3.3e-8 off on average, with bf16 logits of 50304.  Now 1.3e-8
-// at most, and 5e-9 to 2e-8 around that.)
+// those of U vectors, and the threads' sums meet in 64 bits.  (One chain of additions: 3.3e-8 off on average, with bf16 logits of 50304.  Now 4e-9
+// at most, and 5e-9 to 4e-8 around that.)
 template <typename T, int NT, int U>
 __device__ __forceinline__ void stream_stats(const Logits& a, const ColumnAt<T>& at, const TileBases<T>& base, Exchange<NT / 64>& red,
                                              float& mx, double& sum, float& x_label) {

@@ -83,9 +83,9 @@ def test_as_near_to_64_bits_as_fp32_products(mods, shape, iteration, kind):
 ROW = 4.0
 
 
-def rows_off(got, want):
-    """Largest error of a row of X in that row's length."""
-    d, w = (got - want, want) if got.shape[0] <= got.shape[1] else ((got - want).T, want.T)
+def rows_off(got, want, columns=False):
+    """Largest error of a row of X (or of a column) in its length."""
+    d, w = (got - want, want) if (got.shape[0] <= got.shape[1]) != columns else ((got - want).T, want.T)
     return (np.linalg.norm(d, axis=1) / np.linalg.norm(w, axis=1)).max()
 
 
@@ -158,3 +158,65 @@ def test_launches_are_counted(mods, shape, steps, launches):
         capi.nnt_orthogonalize(ctx.h, C.byref(cfg), 1, handles(mods, [tG]), handles(mods, [tO]))
         assert ctx.stats()["launches"] - before == launches
         ctx.wait()
+
+
+@pytest.mark.parametrize("shape", [(4096, 4096), (4096, 16384), (9000, 2500)])
+def test_small_rows_of_large_matrices(mods, shape):
+    """The largest macro-tiles, alone and with two steps at once; the references on the device."""
+    capi, tiled = mods
+    rows, cols = shape
+    G = torch.randn(cols, rows, generator=torch.Generator(device="cuda").manual_seed(7), device="cuda")      # axes reversed: columns of the matrix first
+    X = G.t() if rows <= cols else G
+    X[1::2] *= 1e-6                                           # every other row of X (a view of G)
+
+    def iterate(dtype):
+        Y = X.to(dtype)
+        Y = (Y.double() / (torch.linalg.vector_norm(Y.double()) + 1e-7)).to(dtype)
+        for _ in range(5):
+            S = torch.mm(Y, Y.t())
+            Y = A * Y + torch.mm(B * S + CC * torch.mm(S, S), Y)
+        return Y.double()
+    want = iterate(torch.float64)
+    length = torch.linalg.vector_norm(want, dim=1)
+    plain = (torch.linalg.vector_norm(iterate(torch.float32) - want, dim=1) / length).max().item()
+    with tiled.Context(n_streams=1) as ctx:
+        t = tiled.TiledTensor(ctx, "f32", shape, (3000, 5000))
+        for k, idx in enumerate(t.tile_index):
+            t.tile_view(k).copy_(G[tuple(reversed(t.slices(idx)))].reshape(-1))
+        torch.cuda.synchronize()
+        cfg = capi.nnt_newton_schulz_cfg(A, B, CC, 1e-7, 5)
+        capi.nnt_orthogonalize(ctx.h, C.byref(cfg), 1, handles(mods, [t]), handles(mods, [t]))
+        ctx.wait()
+        for k, idx in enumerate(t.tile_index):
+            part = G[tuple(reversed(t.slices(idx)))]
+            part.copy_(t.tile_view(k).view(part.shape))
+    got = (torch.linalg.vector_norm((G.t() if rows <= cols else G).double() - want, dim=1) / length).max().item()
+    assert got <= ROW * plain, "%.2e of a row, fp32 products %.2e" % (got, plain)
+
+
+@pytest.mark.parametrize("kind", ["columns", "both", "one entry a row"])
+@pytest.mark.parametrize("scale", [1e-4, 1e-8])
+@pytest.mark.parametrize("shape", [(64, 64), (50, 200), (64, 1000), (300, 300), (700, 700), (512, 2560), (2560, 512)])
+@pytest.mark.parametrize("iteration", [USUAL, LONG])
+def test_columns_much_smaller_than_the_others(mods, shape, iteration, scale, kind):
+    """Half of X's columns scaled down, or its rows too, or a matrix of one entry to a row, of any size: a column, too, keeps the precision it started with.  (fp32 products of single
+    entries are exact at 1, so the last rounding of the halves counts there: 2^-24 of the result.)"""
+    steps, a, b, c = iteration
+    r = np.random.default_rng(sum(shape))
+    m, n = min(shape), max(shape)
+    if kind == "one entry a row":
+        G = np.zeros((m, n))
+        G[np.arange(m), r.permutation(n)[:m]] = scale ** r.uniform(0, 1, m)
+    else:
+        G = r.standard_normal((m, n))
+        G[:, n // 2:] *= scale
+        if kind == "both":
+            G[m // 2:] *= scale
+    G = np.float32(G if shape[0] <= shape[1] else G.T)
+    want = D.orthogonalize(G, a, b, c, 1e-7, steps)
+    plain, got = fp32_products(G, steps, 1e-7, a, b, c), orthogonalize(mods, G, steps, 1e-7, (256, 1024), a, b, c)
+    off, own = np.linalg.norm(plain - want), np.linalg.norm(got - want)
+    assert own <= ROW * max(off, 2.0 ** -24 * np.linalg.norm(want)), "%.2e of the result, fp32 products %.2e" % (own / np.linalg.norm(want), off / np.linalg.norm(want))
+    if steps == 5 and kind != "one entry a row":
+        plain, got = rows_off(plain, want, True), rows_off(got, want, True)
+        assert got <= ROW * plain, "%.2e of a column, fp32 products %.2e" % (got, plain)

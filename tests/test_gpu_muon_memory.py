@@ -40,7 +40,7 @@ def test_workspace_where_memory_is_short(mods):
     def tensors(ctx):
         t = {}
         for k, s in shapes.items():
-            G, O = (tiled.TiledTensor(ctx, "f32", s, s) for _ in range(2))
+            G, O = (tiled.TiledTensor(ctx, "f32", s, s, fill=0) for _ in range(2))           # (whole buffers are compared below)
             G.buf.view(torch.float32).normal_(generator=torch.Generator(device="cuda").manual_seed(len(k)))
             t[k] = (G, O)
         torch.cuda.synchronize()
