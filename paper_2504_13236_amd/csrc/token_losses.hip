@@ -227,41 +227,38 @@ struct PolicyArgs {
     const float* const* ref_logp;       // NULL: no KL term
     const float* const* adv;
     int32_t adv_per_sequence;           // tiles of [N_b]
-    float lo, hi, kl;                   // the clip range's ends, weight of the KL term
+    double lo, hi, kl;                  // the clip range's ends, weight of the KL term
     const float* weight;                // per sequence; NULL: 1
     float* const* logp;
     float* losses;
     void* const* dX;                    // NULL: no gradient
 };
 
-// loss and dL/dlogp of one position
+// loss and dL/dlogp of one position, in 64 bits (one thread of a column): what is rounded to 32 is what is written
 __device__ __forceinline__ void policy_of(const Logits& a, const PolicyArgs& p, const Column& c, double logp, float& loss, float& g) {
-    const float w = p.weight ? p.weight[c.c2] : 1.f;
-    float adv;
+    const double w = p.weight ? (double)p.weight[c.c2] : 1.0;
+    double adv;
     if (p.adv_per_sequence) {
         const int t2 = c.c2 / a.X.base[2];
-        adv = global_as<const float>(p.adv[t2])[c.c2 - t2 * a.X.base[2]];
+        adv = (double)global_as<const float>(p.adv[t2])[c.c2 - t2 * a.X.base[2]];
     } else {
-        adv = global_as<const float>(p.adv[c.stat_tile])[c.colidx];
+        adv = (double)global_as<const float>(p.adv[c.stat_tile])[c.colidx];
     }
     // (against itself: 1, also for a banned token, whose logp is -inf, but NaN for a column that holds one)
     const double d = p.old_logp ? logp - (double)global_as<const float>(p.old_logp[c.stat_tile])[c.colidx] : logp == logp ? 0.0 : logp;
-    const float r = expf((float)d);
-    // (no advantage is no loss, also where the ratio is beyond 32 bits: up to exp(709) it is a number)
-    const float free = adv == 0.f && d < 709.0 ? 0.f : r * adv, held = fminf(fmaxf(r, p.lo), p.hi) * adv;
+    const double r = exp(d);
+    const double free = r * adv, held = fmin(fmax(r, p.lo), p.hi) * adv;
     // (written so that a NaN comes through)
-    loss = free > held ? -held : -free;
-    g = free > held ? 0.f : -free;
+    double l = free > held ? -held : -free, s = free > held ? 0.0 : -free;
     if (p.ref_logp) {
-        const float k = (float)((double)global_as<const float>(p.ref_logp[c.stat_tile])[c.colidx] - logp);
-        const float ek = expm1f(k);
+        const double k = (double)global_as<const float>(p.ref_logp[c.stat_tile])[c.colidx] - logp;
+        const double ek = expm1(k);
         // e^k - k - 1: the difference of nearly equal numbers around 0 is summed up as k^2/2 + k^3/6 + ...
-        const float d = fabsf(k) < 0.0625f ? k * k * (0.5f + k * (1.f / 6 + k * (1.f / 24 + k * (1.f / 120)))) : ek - k;
-        loss += p.kl * d;
-        g -= p.kl * ek;
+        l += p.kl * (fabs(k) < 1e-3 ? k * k * (0.5 + k * (1.0 / 6 + k * (1.0 / 24))) : ek - k);
+        s -= p.kl * ek;
     }
-    loss *= w;
-    g *= w;
+    loss = (float)(l * w);
+    g = (float)(s * w);
 }
 
 // One workgroup takes one column.  SLOTS > 0: the column is read once into registers, SLOTS vectors per thread, and the gradient leaves from
@@ -736,9 +733,9 @@ int32_t nnt_policy_loss(nnt_ctx* ctx, const nnt_policy_cfg* cfg, nnt_tensor* X, 
         p.ref_logp = cfg->kl_coef > 0.0 ? in_tiles(ref_logp) : nullptr;
         p.adv = in_tiles(advantages);
         p.adv_per_sequence = advantages->ndim == 1;
-        p.lo = (float)(1.0 - cfg->clip_low);
-        p.hi = (float)(1.0 + cfg->clip_high);
-        p.kl = (float)cfg->kl_coef;
+        p.lo = 1.0 - cfg->clip_low;
+        p.hi = 1.0 + cfg->clip_high;
+        p.kl = cfg->kl_coef;
         p.logp = out_tiles(logp);
         p.losses = losses;
         p.dX = dX ? dX->d_tiles : nullptr;

@@ -159,3 +159,33 @@ def test_preference_loss_entry_by_entry(mods, dtype, shape, base):
         slope = (torch.sigmoid(z) - (1.0 - soft)) * beta / n
         slack = (HALF["f32"] * (R[:n].abs() + R[n:].abs()) / 4 * beta / n / slope.abs()).max().item()
         c.check_gradient(torch.cat([slope, -slope]).unsqueeze(-1) * c.has, slack)
+
+
+@pytest.mark.parametrize("term", ["ratio", "kl"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ratios_beyond_32_bits(mods, dtype, term):
+    """exp(89.5) is no number of fp32, but a two-thousandth of it is: loss and gradient are weighted before they are rounded."""
+    r = np.random.default_rng(12)
+    N_v, N_s, N_b = 50, 1000, 2
+    lab = r.integers(0, N_v, (N_s, N_b))
+    X = quant(r.standard_normal((N_v, N_s, N_b)), dtype)
+    logp = D.token_logprob(X, lab)
+    old, ref = logp.copy(), logp.copy()
+    if term == "ratio":
+        old[::50] -= 89.5                                     # a negative advantage is not clipped from above
+    else:
+        ref[::50] += 89.5
+    old, ref = np.float32(old), np.float32(ref)
+    adv = -np.ones((N_s, N_b))
+    L, losses, logp, dX = D.policy_loss(X, lab, old, ref, adv, 0.2, 0.2, 0.5, "tokens")
+    assert np.abs(losses).max() > 1e35
+    with mods[1].Context(n_streams=2) as ctx:
+        c = Call(mods, ctx, X, lab, (N_v, 128, 2), dtype, old=old, ref=ref, adv=adv)
+        c.policy(0.2, 0.2, 0.5, 1)
+        # e^d moves by the 8e-6 of itself that a log-probability may be off; around d = 0 the loss does by as much of the weight
+        w = 1.0 / lab.size
+        got = c.losses[:lab.size].double().cpu().numpy()
+        assert np.isfinite(got).all()
+        c.close_to(got, losses.reshape(-1, order="F"), LOGP + 2.0 ** -22, 2 * LOGP * w, "losses")
+        g = np.abs(dX).sum(axis=0)
+        c.close_to(c.dX.download(), dX, HALF[dtype] + REL + LOGP, (REL + LOGP) * g[None] + 2 * LOGP * w, "gradient")
