@@ -554,9 +554,10 @@ NNT_API int32_t nnt_sgd_step(nnt_ctx* ctx, const nnt_sgd_cfg* cfg, nnt_tensor* G
  *   X = G / (|G|_F + eps),  then `steps` times  A = X X^T,  X <- a X + (b A + c A^2) X,   O = X,
  * which drives every singular value of G towards the polynomial's fixed range around 1 and keeps the singular vectors.
  * G[k], O[k]: tensors of two axes, fp32 or bf16 each, tiled alike, all tiles present; O[k] may be G[k].  Sums and norms are
- * in 32 bits or more, the factors of the products in two fp16 halves (22 bits) with a power of two of its own for each row of X (the
- * short side): errors, also those of a row much smaller than the others, are those of fp32 products to within a factor of 2.5
- * (bound of the halves against fp32's 24 bits; five steps on gradients 0.4 to 1.4 times theirs).  A zero matrix gives zeros; a matrix that holds an infinity or a NaN gives NaN.  eps > 0, 1 <= steps <= 64.
+ * in 32 bits or more, and so is X; the factors of the products are in two fp16 halves (22 bits) with a power of two of its own for each row and
+ * column of X: errors, also those of rows and columns much smaller than the others, are those of fp32 products to within a small factor
+ * (five steps: 0.5 to 1.4 times theirs; single entries of products that fp32 holds exactly, as of a permuted diagonal matrix, up to 3).  Many steps of
+ * the usual coefficients make roundings grow, in any arithmetic.  A zero matrix gives zeros; a matrix that holds an infinity or a NaN gives NaN.  eps > 0, 1 <= steps <= 64.
  * The coefficients must keep singular values, their squares and b s^2 + c s^4 below 8 from any start in [0, 1] (NNT_EINVAL
  * otherwise); (3.4445, -4.7750, 2.0315) with 5 steps is the usual choice, (1.5, -0.5, 0) the classical one.
  * As many matrices as fill the chip (at most 16) go through one set of launches; G and O are arrays of n pointers.  One

@@ -20,7 +20,7 @@
 //   (D B)(X diag(2^f_j)) = D (B X) diag(2^f_j).
 // What is stored stays below 16: |x_i (.) X^T| <= max s |.| for rows of length 1, and |b + c s^2| s <= 13.6 where |b s^2 + c s^4| <= 8 on [0, 1].  B's diagonal is kept out of it: a + B_ii, in
 // fp32, is what X's row i is multiplied by (most of the step once X has arrived, where B is near a multiple of the identity).
-// Rows of 1e-8 of the others, 512 x 2560, five steps: the worst of them 4e-6 of its length off, with fp32 products 8e-6, with one scale for all of X 4e-1.
+// Rows of 1e-8 of the others, 512 x 2560, five steps: the worst of them 5e-6 of its length off, with fp32 products 8e-6, with one scale for all of X 4e-1.
 //
 // All operands of the products lie in the workspace as panels: 64 rows x 16 columns of the contraction, hi part and lo part of 2 KB each,
 // inside them eight columns of a row next to each other (16 bytes), 64 rows of those, then the next eight columns.  That is the
@@ -187,7 +187,7 @@ __device__ __forceinline__ float largest_of(const float (&u)[16]) {
 }
 
 // A workgroup takes 64 rows of X and a part of its columns, 128 at a time: a lane a row of the tensor and a wavefront 16 columns of it.  Squares are added up in 64
-// bits (no value of fp32 overflows or vanishes in it), by row of X and over the 64 rows; of X's columns the largest entries are left.  Bound by memory: 8192 x 8192 with momentum, 171 us for 805 MB (139 along the tiles
+// bits (no value of fp32 overflows or vanishes in it), by row of X and over the 64 rows; of X's columns the largest entries are left.  Bound by memory: 8192 x 8192 with momentum, 180 us for 805 MB (139 along the tiles
 // in 16-byte vectors, which cannot add up rows).
 constexpr int kNormWaves = 8, kNormSpan = 16 * kNormWaves;
 template <bool FLIP>
@@ -365,9 +365,9 @@ struct Scale {
 };
 
 // ---------------------------------------------------------------- set-up: X_0 in its three forms
-// One workgroup takes 64 x 64 elements: read along the tensor's contiguous axis, turned in LDS, written as panels of X and of its transpose and in fp32.  Bound by memory: all
-// forms are written here because turning X for the first product with it would cost a pass of its own.
-__global__ void __launch_bounds__(256) ns_split_kernel(const NsGroup* __restrict__ group, NsSizes sizes) {
+// One workgroup takes 64 x 64 elements: read along the tensor's contiguous axis, turned in LDS, written as panels of X and of its transpose and in fp32.  Bound by memory: 8192 x 8192
+// with momentum, 310 us for 1342 MB; all forms are written here because turning X for the first product with it would cost a pass of its own.
+__global__ void __launch_bounds__(256, 8) ns_split_kernel(const NsGroup* __restrict__ group, NsSizes sizes) {
     const NsGroup& g = *group;
     __shared__ float t[64][65];                          // [i][j]
     __shared__ SetUp setup;
@@ -811,7 +811,7 @@ __device__ __forceinline__ void tile_of(int p, int tm, int tn, int& ti, int& tj)
 // fragments all have, free for the loads of step + ST.  LDS reads and their waits are spelled out: the compiler would wait for all loads in flight.
 //
 // What bounds it: 8192 x 8192, B X on 256 x 256: 2.44 ms, 1350 TFLOP/s of fp16 (a plain fp16 product of the installed library: 1180), by the clock that the power limit
-// leaves (1.55 GHz, the matrix cores busy for 81 % of the cycles).  Twelve of 768 x 768 on 128 x 128: 45 us, 720 TFLOP/s of fp16, half of it in the loop and half in
+// leaves (1.55 GHz, the matrix cores busy for 81 % of the cycles).  Twelve of 768 x 768 on 128 x 128: 48 us, 680 TFLOP/s of fp16, half of it in the loop and half in
 // the launch, the filling of the stages and the results' way out.  777 x 1111 on 64 x 64: 11 us, of which the loop takes 7, as long as it takes to
 // fetch 8 KB a step at 32 bytes per clock.
 template <int MODE, typename S>
@@ -1023,8 +1023,8 @@ __global__ void __launch_bounds__(256) ns_combine_kernel(const NsGroup* __restri
 // ---------------------------------------------------------------- matrices with a side of at most 64
 // Here a launch is longer than what it computes, so a whole iteration is one launch.  A workgroup holds some of X's column blocks of 64; it adds up the
 // parts of A that the workgroups have left (its own and the others'), computes B (64 x 64, every workgroup the same), its blocks of X and their
-// part of the next A.  X is kept as its transpose and in fp32.  The first launch takes U in place of B X, the last one leaves the results.  64 x 320: 6 us a
-// launch, 45 in all (some 75 with the products above); it is the launches that bound it, and within one the parts' way through memory.
+// part of the next A.  X is kept as its transpose and in fp32.  The first launch takes U in place of B X, the last one leaves the results.  64 x 320: 7 us a
+// launch, 49 in all (some 75 with the products above); it is the launches that bound it, and within one the parts' way through memory.
 enum { kFirst, kMiddle, kFinal };
 
 // how many workgroups share a matrix of nt column blocks: each adds up as many parts (0.2 us) as there are, and takes nt / parts blocks (1.5 us) in turn
@@ -1258,8 +1258,8 @@ __global__ void __launch_bounds__(256) ns_narrow_kernel(const NsGroup* __restric
 
 // ---------------------------------------------------------------- matrices of at most 64 x 256
 // One workgroup holds all of X in LDS and does everything in one launch: momentum, norm, the steps, the results.  Four wavefronts to a column block of 64; the first four
-// put A together and compute B for all.  64 x 64 22 us (33 with a launch per step), 64 x 256 43 (45), and the rest of the chip is free meanwhile: passes over the four
-// matrices of a block of 64 that need not wait for one another take 27 us each (46).  What bounds it is LDS, 3 us a step and 1.2 for each further block.  (X computed
+// put A together and compute B for all.  64 x 64 25 us (33 with a launch per step), 64 x 256 44 (49), and the rest of the chip is free meanwhile: passes over the four
+// matrices of a block of 64 that need not wait for one another take 28 us each (47).  What bounds it is LDS, 3 us a step and 1.2 for each further block.  (X computed
 // twice, as its transpose too, in place of the two-byte writes: 40 us, but the two drift apart, errors a quarter larger.)
 constexpr int kHeldBlocks = 4;
 
@@ -1577,7 +1577,7 @@ enum { kProducts, kNarrow, kHeld };
 int kind_of(int64_t m, int64_t l) { return m > 64 || l > 64 * kNarrowBlocks ? kProducts : l > 64 * kHeldBlocks ? kNarrow : kHeld; }
 
 // Sets of up to this size take the two halves of the workspace in turn, so that two of them run side by side: a launch's beginning and end, and the units that
-// it leaves idle, are the other's (sets of a step on 12 blocks of 768 wide 4.23 -> 3.7 ms, 777 x 1111 176 -> 111 us each; more than two at a time, four sets of a
+// it leaves idle, are the other's (sets of a step on 12 blocks of 768 wide 4.8 -> 4.0 ms, 777 x 1111 185 -> 115 us each; more than two at a time, four sets of a
 // block of 1600 10.0 -> 10.7 ms).  Larger ones fill the chip (two of 4096 x 4096 7.97 ms either way) and take all of it.
 constexpr int64_t kHalfBytes = (int64_t)512 << 20;
 
