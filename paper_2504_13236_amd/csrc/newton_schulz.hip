@@ -258,12 +258,14 @@ __global__ void __launch_bounds__(64 * kNormWaves, 6) ns_norm_kernel(NsGroup g) 
 }
 
 // e of a row or column of at most the given length in a matrix of the given length: that of X_0 times 2^e is at most 1 long.  0 for those without a length (zeros, no numbers).
+// No more than 120: fp32 rounds at 2^-149, and what has shrunk as far as that need not shrink any further (0.6 times the last bit is the last bit).
+constexpr int kMostExponent = 120;
 __device__ __forceinline__ int exponent_of(double length, double of) {
     const double x = length / of;
     if (!(x > 0.0) || x > 1.0) return 0;
     int k;
     (void)frexp(x, &k);
-    return max(0, -k);
+    return min(max(0, -k), kMostExponent);
 }
 
 // Set-up of a workgroup of four wavefronts: the matrix's length, and the exponents of the 64 rows of X from row i0 on and of the 64 columns from column j0 on.
@@ -313,7 +315,7 @@ __device__ __forceinline__ double length_and_exponents(const NsGroup& g, const N
 
 // What `steps` steps can make a row or column grow by, as a power of two; its exponent behind that.
 __host__ __device__ inline int grown_by(int growth, int steps) { return (growth * steps + 255) >> 8; }
-__device__ __forceinline__ int exponent_at(int first, int grown) { return max(first - grown, 0); }
+__device__ __forceinline__ int exponent_at(int first, int grown) { return min(max(first - grown, 0), kMostExponent); }
 
 // The matrix of a workgroup of a launch over tiles of BM x BM results of all matrices (SYM: those on and above the diagonal of
 // square results); `wg` becomes its number among the matrix's own.

@@ -220,3 +220,20 @@ def test_columns_much_smaller_than_the_others(mods, shape, iteration, scale, kin
     if steps == 5 and kind != "one entry a row":
         plain, got = rows_off(plain, want, True), rows_off(got, want, True)
         assert got <= ROW * plain, "%.2e of a column, fp32 products %.2e" % (got, plain)
+
+
+# Coefficients that shrink: 0.6^64 is 2^-47, and a row or column of 2^-112 of the others ends below fp32's last bit, 2^-149, where 0.6 times it is rounded up to itself.  A step is a
+# product with `a` alone, so that a result is off by 2^-24 of itself a step for each of the roundings (of `a`, of the product, X_0 three times), and by the last bit.
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("columns", [False, True])
+@pytest.mark.parametrize("scale,eps", [(2.0**-112, 1e-7), (1.0, 1e36)])
+def test_what_shrinks_into_the_last_bit_stays_a_number(mods, shape, columns, scale, eps):
+    r = np.random.default_rng(1 + sum(shape))
+    G = r.standard_normal(shape).astype(np.float32)
+    (G.T if columns else G)[3] *= np.float32(scale)
+    X = G.astype(np.float64) / (np.linalg.norm(G.astype(np.float64)) + eps)
+    got = orthogonalize(mods, G, 64, eps, (256, 1024), 0.6, 0.0, 0.0)
+    assert np.all(np.isfinite(got))
+    want = 0.6**64 * X
+    off = np.abs(got - want) - (2 * 64 + 4) * 2.0**-24 * np.abs(want)
+    assert off.max() <= 4 * 2.0**-149
