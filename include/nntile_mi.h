@@ -536,6 +536,78 @@ NNT_API int32_t nnt_preference_loss(nnt_ctx* ctx, const nnt_preference_cfg* cfg,
                             nnt_tensor* ref_logp, nnt_tensor* dX, nnt_tensor* logp, float* rewards,
                             float* losses, float* loss);
 
+/* ---- Rollouts: a paged cache of keys and values, attention over it, drawn tokens ---- */
+
+#define NNT_ROTATE_HALVES 0   /* pairs (x[i], x[i + r/2]), i < r/2 */
+#define NNT_ROTATE_PAIRS  1   /* pairs (x[2i], x[2i + 1])          */
+
+/* What the calls on a cache share.  The cache is a pair of tensors K, V [h, n_pages * P, N_kv] of the activations' type, tiled
+ * (h, P, N_kv): a tile is a page of P positions with all N_kv heads.  N_h query heads share N_kv cached ones: head j reads the cached
+ * head j / (N_h / N_kv).  Position p of sequence b lies in slot p % P of page pages[p / P + max_pages * b]; an entry outside
+ * [0, n_pages) is a page that is not there.  start[b] positions of sequence b are in the cache before the call, and the first
+ * count[b] of the call's N_s tokens are new ones, at the positions start[b], start[b] + 1, ... (count NULL: all N_s).  A count
+ * outside [0, N_s] is taken as its nearer end; a position below 0 or from max_pages * P on is one whose page is not there.
+ * pages, start, count: device pointers, which the caller must not reuse before nnt_wait or a later operation that waits for this one.
+ * rotation: NULL, or an fp32 tensor [r, N_pos], r even, r <= h, base tile r along its first axis: column p holds the r/2 cosines, then the
+ * r/2 sines of position p.  The first r components of every key (as it is written) and query (as it is read) are turned by it:
+ * (x, y) <- (x cos - y sin, x sin + y cos) on the pairs that `rotate` names.  Positions from N_pos on have no rotation: such a
+ * key is not written, such a query gives zeros.  window: 0, or how many keys a query sees at most, itself included. */
+typedef struct nnt_cache_cfg {
+    const int32_t* pages;
+    const int32_t* start;
+    const int32_t* count;
+    nnt_tensor* rotation;
+    int32_t N_h, N_kv, max_pages, window, rotate;
+} nnt_cache_cfg;
+/* Writes keys and values of the new tokens to their pages, keys rotated.  QKV: [(N_h + 2 N_kv) * h, N_s, N_b], rows of the
+ * queries, then of the keys, then of the values, head after head (as a block's projection with N_kv = N_h); its row tiles hold whole heads.  h is a
+ * multiple of 8, at most 256; all tiles present and 16-byte aligned.  Tokens whose page is not there are not written, nothing else of the pages is
+ * touched.  Two tokens of one call must not share a slot.  One task, as the next call. */
+NNT_API int32_t nnt_cache_append(nnt_ctx* ctx, const nnt_cache_cfg* cfg, nnt_tensor* QKV, nnt_tensor* K, nnt_tensor* V);
+/* Attention of the new tokens over the cache (which holds their own keys and values, see nnt_cache_append):
+ *   B[i,s,b,j] = sum_k V[i,k] P[k],  P = softmax over k of scale * sum_i K[i,k] rot(Q)[i,s,b,j],
+ * over the positions k <= start[b] + s (and > start[b] + s - window) whose page is there; a query that sees none gives zeros.  Columns of
+ * tokens that are not new (s >= count[b]) are left as they are.  QKV as above (only the queries are read), B: [N_h * h, N_s, N_b],
+ * row tiles of whole heads.  What is masked does not enter, infinities and NaN there included.  scale > 0.  The keys of long sequences are split over workgroups, whose
+ * partial results meet in the context's per-stream scratch (at most N_s * N_b * N_h * (h + 2) * 64 floats), which must exist before a graph
+ * capture (run the call once). */
+NNT_API int32_t nnt_cache_attention(nnt_ctx* ctx, const nnt_cache_cfg* cfg, float scale, nnt_tensor* QKV, nnt_tensor* K,
+                            nnt_tensor* V, nnt_tensor* B);
+
+/* Draws a token from each of n columns of the logits.  With the column's tokens ordered by logit (the largest first, among
+ * equals the lowest number first), m its largest logit and the weights e_j = exp((x_j - m) / temperature):
+ *   top_k > 0 keeps the first top_k;  top_p < 1 keeps of these the fewest first ones whose weights reach top_p of their sum;
+ *   min_p > 0 keeps of these the ones with e_j >= min_p;
+ *   the token is the first kept one, now in the order of their numbers, up to which the kept weights sum up to more than u times all of them.
+ * temperature = 0: the largest logit, among equals the lowest number (the filters and u do not matter).
+ * X: [N_v, N_s, N_b] logits, fp32 or bf16, only read; columns: device pointer to n int32, the columns s + N_s * b to draw from, or
+ * NULL: 0, 1, ... n - 1.  uniforms: device pointer to n floats u in [0, 1) (outside: the nearer end, NaN: 0).  tokens: n int32.  logp: NULL, or n floats: the tokens'
+ * log-probabilities under the unfiltered logits at temperature 1, as nnt_token_logprob gives them.
+ * A NaN counts as -infinity; where logits are +infinity they share the whole mass.  A column without any logit above -infinity, or a column
+ * number outside [0, N_s N_b), gives token -1 and logp 0.  Weights are taken in 64 bits and summed as whole numbers, so that
+ * the same logits and u always give the same token.  temperature >= 0, 0 < top_p <= 1, 0 <= min_p <= 1, top_k >= 0.
+ * The vocabulary's limits are nnt_token_logprob's.  One task; the caller must not reuse columns, uniforms, tokens and logp before
+ * nnt_wait or a later operation that writes X. */
+typedef struct nnt_sample_cfg {
+    double temperature, top_p, min_p;
+    int32_t top_k;
+} nnt_sample_cfg;
+NNT_API int32_t nnt_sample_tokens(nnt_ctx* ctx, const nnt_sample_cfg* cfg, nnt_tensor* X, const int32_t* columns, int32_t n,
+                          const float* uniforms, int32_t* tokens, float* logp);
+
+/* The norm of all gradients, and the gradients clipped by it:
+ *   norm = sqrt(sum over k and all elements of G[k]^2),   O[k] = min(1, max_norm / (norm + eps)) G[k].
+ * G: n tensors, fp32 or bf16 each, of any shapes, each given once; tiles that are not there count as zeros.  O: n tensors with
+ * the types, shapes and tilings of G, O[k] may be G[k]; or NULL: the norm alone.  norm: device float, which the caller must not reuse before nnt_wait or a later
+ * operation on one of O (or G).  Sums are in 64 bits, in a fixed order; each result is rounded once.  An infinite or NaN norm
+ * leaves the gradients as they are.  max_norm > 0 (infinity: not clipped), eps >= 0.  One task; it uses the context's
+ * per-stream scratch, which must exist before a graph capture (run the call once). */
+typedef struct nnt_clip_cfg {
+    double max_norm, eps;
+} nnt_clip_cfg;
+NNT_API int32_t nnt_clip_grad_norm(nnt_ctx* ctx, const nnt_clip_cfg* cfg, int32_t n, nnt_tensor* const* G, nnt_tensor* const* O,
+                           float* norm);
+
 /* SGD with momentum (section 3, Optimizers: the update is a weighted sum of the
  * parameter, the gradient and the momentum term):
  *   g' = g + weight_decay * p;  v <- momentum * v + g';
@@ -667,6 +739,13 @@ NNT_API int32_t nnt_gpt2_block_sgd(nnt_gpt2_block* blk, const nnt_sgd_cfg* cfg);
 /* nnt_muon_step on the four matrices (momentum in the slots NNT_BLK_ADAM_M + parameter, their second moments are not
  * touched; bf16 blocks refresh the bf16 copies), Adam step number `step` on the eight vectors. */
 NNT_API int32_t nnt_gpt2_block_muon(nnt_gpt2_block* blk, const nnt_muon_cfg* cfg, int32_t step, const nnt_adam_cfg* adam);
+/* nnt_clip_grad_norm on the block's twelve gradients, in place: between backward (or what collects gradients) and the optimiser. */
+NNT_API int32_t nnt_gpt2_block_clip(nnt_gpt2_block* blk, const nnt_clip_cfg* cfg, float* norm);
+/* The forward pass of new tokens over a cache: the attention is nnt_cache_append and nnt_cache_attention on NNT_BLK_QKV and
+ * NNT_BLK_BM, with cfg->N_h = cfg->N_kv = the block's N_h.  For causal blocks whose row tiles hold whole heads of a multiple of 8, at most 256,
+ * components.  Nothing is kept to go backward from.  A block of N_s = 1 whose weight slots are those of the trained one generates token by token. */
+NNT_API int32_t nnt_gpt2_block_forward_cached(nnt_gpt2_block* blk, const nnt_cache_cfg* cfg, nnt_tensor* K, nnt_tensor* V,
+                                      nnt_tensor* X, nnt_tensor* Out);
 /* bf16 blocks: (re)make the bf16 weight copies from the fp32 masters. */
 NNT_API int32_t nnt_gpt2_block_sync_lowp(nnt_gpt2_block* blk);
 
@@ -692,6 +771,10 @@ NNT_API int32_t nnt_gpt2_stack_adam(nnt_gpt2_stack* st, int32_t step, const nnt_
 /* nnt_gpt2_block_muon on all blocks, their matrices in one nnt_muon_step. */
 NNT_API int32_t nnt_gpt2_stack_muon(nnt_gpt2_stack* st, const nnt_muon_cfg* cfg, int32_t step, const nnt_adam_cfg* adam);
 
+/* All gradients of the blocks under one norm; the forward pass over a cache, K and V one tensor per block. */
+NNT_API int32_t nnt_gpt2_stack_clip(nnt_gpt2_stack* st, const nnt_clip_cfg* cfg, float* norm);
+NNT_API int32_t nnt_gpt2_stack_forward_cached(nnt_gpt2_stack* st, const nnt_cache_cfg* cfg, nnt_tensor* const* K, nnt_tensor* const* V);
+
 /* A GPT-2-shaped language model as one flow of tasks (section 3: embedding
  * layer, the blocks, layer normalization, linear head, Cross-Entropy loss,
  * optimizer): token and position embedding lookup and their sum, a chain of
@@ -702,8 +785,9 @@ NNT_API int32_t nnt_gpt2_stack_muon(nnt_gpt2_stack* st, const nnt_muon_cfg* cfg,
  * tiling of each of the model's own tensors, allocates them and hands them over;
  * the model keeps pointers, not ownership.
  *   parameters (fp32 masters): W_te [N_e, N_v] (one column per vocabulary item,
- *   tiled tile_e x tile_v), W_pe [N_e, N_s] (one column per position), gain and
- *   bias of the final layer norm [N_e]; + NNT_MDL_GRAD their gradients, +
+ *   tiled tile_e x tile_v), W_pe [N_e, N_s] (one column per position; a tensor of more
+ *   columns, with any tiling of them, is taken too, so that a model of short N_s generates with the embeddings of
+ *   the trained one), gain and bias of the final layer norm [N_e]; + NNT_MDL_GRAD their gradients, +
  *   NNT_MDL_ADAM_M / _V their Adam moments; NNT_MDL_LOWP + {0, 1}: bf16 copies of
  *   W_te, W_pe (bf16 models only).
  *   activations: X_pos (position embeddings of the batch), X_f (final layer norm),
@@ -746,6 +830,14 @@ NNT_API int32_t nnt_gpt2_model_forward_preference(nnt_gpt2_model* m, const int32
                                float* rewards, float* losses, float* loss);
 /* nnt_gpt2_stack_muon on the blocks, Adam on the model's own four parameters (embeddings, final layer norm). */
 NNT_API int32_t nnt_gpt2_model_muon(nnt_gpt2_model* m, const nnt_muon_cfg* cfg, int32_t step, const nnt_adam_cfg* adam);
+/* nnt_clip_grad_norm on all gradients of the model, in place. */
+NNT_API int32_t nnt_gpt2_model_clip(nnt_gpt2_model* m, const nnt_clip_cfg* cfg, float* norm);
+/* One step of generation: the forward pass of the N_s x N_b tokens over the cache (K, V: one tensor per block), then nnt_sample_tokens
+ * on n columns of the logits (columns, uniforms, next, logp as there).  What it draws may be the tokens of the next such call over the
+ * same cache (of this model or another one), which waits for it.  Leaves the logits and nothing to go backward from. */
+NNT_API int32_t nnt_gpt2_model_sample(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions, const nnt_cache_cfg* cache,
+                              nnt_tensor* const* K, nnt_tensor* const* V, const nnt_sample_cfg* cfg, const int32_t* columns, int32_t n,
+                              const float* uniforms, int32_t* next, float* logp);
 
 NNT_API const char* nnt_version(void);
 

@@ -20,6 +20,7 @@ NNT_GELU_TANH, NNT_GELU_ERF = 0, 1
 NNT_GRAN_OP, NNT_GRAN_TILE = 0, 1
 NNT_REDUCE_SUM, NNT_REDUCE_TOKENS, NNT_REDUCE_SEQUENCES = 0, 1, 2
 NNT_MUON_SCALE_NONE, NNT_MUON_SCALE_ASPECT, NNT_MUON_SCALE_RMS = 0, 1, 2
+NNT_ROTATE_HALVES, NNT_ROTATE_PAIRS = 0, 1
 NNT_MAX_DIM = 4
 
 _ERR = {NNT_EINVAL: "NNT_EINVAL", NNT_EDTYPE: "NNT_EDTYPE", NNT_EHIP: "NNT_EHIP",
@@ -88,6 +89,19 @@ class nnt_newton_schulz_cfg(C.Structure):
 class nnt_muon_cfg(C.Structure):
     _fields_ = [("lr", C.c_double), ("momentum", C.c_double), ("weight_decay", C.c_double), ("nesterov", C.c_int32), ("scale", C.c_int32),
                 ("iteration", nnt_newton_schulz_cfg)]
+
+
+class nnt_cache_cfg(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("start", C.c_void_p), ("count", C.c_void_p), ("rotation", C.c_void_p), ("N_h", C.c_int32),
+                ("N_kv", C.c_int32), ("max_pages", C.c_int32), ("window", C.c_int32), ("rotate", C.c_int32)]
+
+
+class nnt_sample_cfg(C.Structure):
+    _fields_ = [("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int32)]
+
+
+class nnt_clip_cfg(C.Structure):
+    _fields_ = [("max_norm", C.c_double), ("eps", C.c_double)]
 
 
 class nnt_slot_info(C.Structure):
@@ -193,6 +207,10 @@ PROTOTYPES = {
     "nnt_preference_loss": (_i32, [_p, C.POINTER(nnt_preference_cfg), _p, _p, _p, _p, _p, _p, _p, _p]),
     "nnt_orthogonalize": (_i32, [_p, C.POINTER(nnt_newton_schulz_cfg), _i32, _pp, _pp]),
     "nnt_muon_step": (_i32, [_p, C.POINTER(nnt_muon_cfg), _i32, _pp, _pp, _pp, _pp]),
+    "nnt_cache_append": (_i32, [_p, C.POINTER(nnt_cache_cfg), _p, _p, _p]),
+    "nnt_cache_attention": (_i32, [_p, C.POINTER(nnt_cache_cfg), _f, _p, _p, _p, _p]),
+    "nnt_sample_tokens": (_i32, [_p, C.POINTER(nnt_sample_cfg), _p, _p, _i32, _p, _p, _p]),
+    "nnt_clip_grad_norm": (_i32, [_p, C.POINTER(nnt_clip_cfg), _i32, _pp, _pp, _p]),
     "nnt_sgd_step": (_i32, [_p, C.POINTER(nnt_sgd_cfg), _p, _p, _p, _p]),
     "nnt_gpt2_block_slot": (_i32, [C.POINTER(nnt_gpt2_block_cfg), _i32, C.POINTER(nnt_slot_info)]),
     "nnt_gpt2_block_create": (_i32, [_p, C.POINTER(nnt_gpt2_block_cfg), _pp, _pp]),
@@ -214,6 +232,12 @@ PROTOTYPES = {
     "nnt_gpt2_model_logprob": (_i32, [_p, _p, _p, _p, _p]),
     "nnt_gpt2_model_forward_policy": (_i32, [_p, _p, _p, _p, C.POINTER(nnt_policy_cfg), _p, _p, _p, _p, _p, _p]),
     "nnt_gpt2_model_forward_preference": (_i32, [_p, _p, _p, _p, C.POINTER(nnt_preference_cfg), _p, _p, _p, _p, _p]),
+    "nnt_gpt2_block_clip": (_i32, [_p, C.POINTER(nnt_clip_cfg), _p]),
+    "nnt_gpt2_block_forward_cached": (_i32, [_p, C.POINTER(nnt_cache_cfg), _p, _p, _p, _p]),
+    "nnt_gpt2_stack_clip": (_i32, [_p, C.POINTER(nnt_clip_cfg), _p]),
+    "nnt_gpt2_stack_forward_cached": (_i32, [_p, C.POINTER(nnt_cache_cfg), _pp, _pp]),
+    "nnt_gpt2_model_clip": (_i32, [_p, C.POINTER(nnt_clip_cfg), _p]),
+    "nnt_gpt2_model_sample": (_i32, [_p, _p, _p, C.POINTER(nnt_cache_cfg), _pp, _pp, C.POINTER(nnt_sample_cfg), _p, _i32, _p, _p, _p]),
     "nnt_version": (C.c_char_p, []),
 }
 

@@ -223,20 +223,21 @@ static bool head_windows(const nnt_gpt2_block* b) {
            b->s[NNT_BLK_DQKV]->base[0] == t0;
 }
 
-int32_t nnt_gpt2_block_forward(nnt_gpt2_block* b, nnt_tensor* X, nnt_tensor* Out) {
-    if (!b) return NNT_EINVAL;
+// The layers of a block; with a cache the attention is that of new tokens over it.
+static int32_t block_layers(nnt_gpt2_block* b, const nnt_cache_cfg* cache, nnt_tensor* K, nnt_tensor* V, nnt_tensor* X, nnt_tensor* Out) {
     nnt_ctx* ctx = b->ctx;
-    NNT_CHECK_CTX(ctx);
-    if (!X || !Out) return fail(ctx, NNT_EINVAL, "nnt_gpt2_block_forward: null tensor");
     nnt_tensor** s = b->s;
     const nnt_gpt2_block_cfg& c = b->cfg;
     const float sc = 1.f / std::sqrt((float)(c.N_e / c.N_h));
     if (!same_tiling(X, s[NNT_BLK_X1]) || !same_tiling(Out, s[NNT_BLK_X1]) || X->dtype != c.dtype || Out->dtype != c.dtype)
         return fail(ctx, NNT_EINVAL, "nnt_gpt2_block_forward: X / Out do not match the block's activations");
-    b->X = X;
+    b->X = cache ? nullptr : X;      // (the cached form leaves nothing to go backward from)
     TRY(nnt_layernorm_fwd(ctx, X, s[NNT_BLK_GAMMA1], s[NNT_BLK_BETA1], c.eps, s[NNT_BLK_X1], s[NNT_BLK_STATS1]));
     TRY(linear(b, weight(b, NNT_BLK_W_QKV), s[NNT_BLK_X1], s[NNT_BLK_B_QKV], s[NNT_BLK_QKV]));
-    if (head_windows(b)) {
+    if (cache) {
+        TRY(nnt_cache_append(ctx, cache, s[NNT_BLK_QKV], K, V));
+        TRY(nnt_cache_attention(ctx, cache, sc, s[NNT_BLK_QKV], K, V, s[NNT_BLK_BM]));
+    } else if (head_windows(b)) {
         // parts 0, 1, 2 of the QKV rows are Q, K, V; the heads' results go straight into Bm
         const int32_t h = (int32_t)(c.N_e / c.N_h), N_h = (int32_t)c.N_h;
         if (c.fused_attention) {
@@ -269,6 +270,28 @@ int32_t nnt_gpt2_block_forward(nnt_gpt2_block* b, nnt_tensor* X, nnt_tensor* Out
         TRY(nnt_gelu(ctx, c.gelu_variant, s[NNT_BLK_H1], s[NNT_BLK_G]));
     }
     return linear(b, weight(b, NNT_BLK_W_2), s[NNT_BLK_G], s[NNT_BLK_B_2], Out, s[NNT_BLK_X2]);   // Out = X2 + W_2 G +. b_2
+}
+
+int32_t nnt_gpt2_block_forward(nnt_gpt2_block* b, nnt_tensor* X, nnt_tensor* Out) {
+    if (!b) return NNT_EINVAL;
+    NNT_CHECK_CTX(b->ctx);
+    if (!X || !Out) return fail(b->ctx, NNT_EINVAL, "nnt_gpt2_block_forward: null tensor");
+    return block_layers(b, nullptr, nullptr, nullptr, X, Out);
+}
+
+static int32_t cached_check(nnt_gpt2_block* b, const nnt_cache_cfg* cfg, nnt_tensor* K, nnt_tensor* V) {
+    if (!cfg) return fail(b->ctx, NNT_EINVAL, "nnt_gpt2_block_forward_cached: null argument");
+    if (!b->cfg.causal || cfg->N_h != b->cfg.N_h || cfg->N_kv != b->cfg.N_h) return fail(b->ctx, NNT_EINVAL, "nnt_gpt2_block_forward_cached: a causal block with a cached head for each of its heads");
+    return cache_check(b->ctx, cfg, b->s[NNT_BLK_QKV], K, V, b->s[NNT_BLK_BM]);
+}
+
+int32_t nnt_gpt2_block_forward_cached(nnt_gpt2_block* b, const nnt_cache_cfg* cfg, nnt_tensor* K, nnt_tensor* V, nnt_tensor* X, nnt_tensor* Out) {
+    if (!b) return NNT_EINVAL;
+    return entry(b->ctx, [&]() -> int32_t {
+        if (!X || !Out) return fail(b->ctx, NNT_EINVAL, "nnt_gpt2_block_forward_cached: null tensor");
+        TRY(cached_check(b, cfg, K, V));
+        return block_layers(b, cfg, K, V, X, Out);
+    });
 }
 
 int32_t nnt_gpt2_block_backward(nnt_gpt2_block* b, nnt_tensor* dOut, nnt_tensor* dX) {
@@ -407,6 +430,21 @@ int32_t nnt_gpt2_block_muon(nnt_gpt2_block* b, const nnt_muon_cfg* cfg, int32_t 
     return entry(b->ctx, [&]() -> int32_t { return blocks_muon(b->ctx, &b, 1, cfg, step, adam); });
 }
 
+// the gradients of several blocks (and others) under one norm
+static int32_t clip_in_place(nnt_ctx* ctx, const nnt_clip_cfg* cfg, const std::vector<nnt_tensor*>& G, float* norm) {
+    return nnt_clip_grad_norm(ctx, cfg, (int32_t)G.size(), G.data(), G.data(), norm);
+}
+static void add_gradients(const nnt_gpt2_block* b, std::vector<nnt_tensor*>* G) { G->insert(G->end(), b->s + NNT_BLK_GRAD, b->s + NNT_BLK_GRAD + 12); }
+
+int32_t nnt_gpt2_block_clip(nnt_gpt2_block* b, const nnt_clip_cfg* cfg, float* norm) {
+    if (!b) return NNT_EINVAL;
+    return entry(b->ctx, [&]() -> int32_t {
+        std::vector<nnt_tensor*> G;
+        add_gradients(b, &G);
+        return clip_in_place(b->ctx, cfg, G, norm);
+    });
+}
+
 int32_t nnt_gpt2_block_sgd(nnt_gpt2_block* b, const nnt_sgd_cfg* cfg) {
     if (!b) return NNT_EINVAL;
     nnt_ctx* ctx = b->ctx;
@@ -467,6 +505,25 @@ int32_t nnt_gpt2_stack_forward(nnt_gpt2_stack* st) {
     if (!st) return NNT_EINVAL;
     for (size_t i = 0; i < st->blocks.size(); i++) TRY(nnt_gpt2_block_forward(st->blocks[i], st->acts[i], st->acts[i + 1]));
     return NNT_OK;
+}
+
+int32_t nnt_gpt2_stack_forward_cached(nnt_gpt2_stack* st, const nnt_cache_cfg* cfg, nnt_tensor* const* K, nnt_tensor* const* V) {
+    if (!st) return NNT_EINVAL;
+    return entry(st->ctx, [&]() -> int32_t {
+        if (!K || !V) return fail(st->ctx, NNT_EINVAL, "nnt_gpt2_stack_forward_cached: null argument");
+        for (size_t i = 0; i < st->blocks.size(); i++) TRY(cached_check(st->blocks[i], cfg, K[i], V[i]));
+        for (size_t i = 0; i < st->blocks.size(); i++) TRY(nnt_gpt2_block_forward_cached(st->blocks[i], cfg, K[i], V[i], st->acts[i], st->acts[i + 1]));
+        return NNT_OK;
+    });
+}
+
+int32_t nnt_gpt2_stack_clip(nnt_gpt2_stack* st, const nnt_clip_cfg* cfg, float* norm) {
+    if (!st) return NNT_EINVAL;
+    return entry(st->ctx, [&]() -> int32_t {
+        std::vector<nnt_tensor*> G;
+        for (nnt_gpt2_block* b : st->blocks) add_gradients(b, &G);
+        return clip_in_place(st->ctx, cfg, G, norm);
+    });
 }
 
 int32_t nnt_gpt2_stack_backward(nnt_gpt2_stack* st) {
@@ -551,7 +608,9 @@ int32_t nnt_gpt2_model_create(nnt_ctx* ctx, const nnt_gpt2_block_cfg* cfg, int64
             return fail(ctx, NNT_EINVAL, "nnt_gpt2_model_create: missing tensor for slot " + std::to_string(i));
         }
         bool ok = t->ctx == ctx && t->dtype == info.dtype && t->ndim == info.ndim;
-        for (int a = 0; ok && a < info.ndim; a++) ok = t->shape[a] == info.shape[a] && t->base[a] == info.basetile[a];
+        // (position embeddings may go on behind the batch's N_s positions)
+        const bool longer = (i < NNT_MDL_LOWP ? i % 4 : i - NNT_MDL_LOWP) == NNT_MDL_WPE && i < NNT_MDL_XPOS && ok && t->shape[1] > info.shape[1];
+        for (int a = 0; ok && a < info.ndim - (longer ? 1 : 0); a++) ok = t->shape[a] == info.shape[a] && t->base[a] == info.basetile[a];
         if (!ok) {
             delete m;
             return fail(ctx, NNT_EINVAL, "nnt_gpt2_model_create: tensor of slot " + std::to_string(i) + " has the wrong type, shape or tiling");
@@ -577,16 +636,17 @@ int32_t nnt_gpt2_model_sync_lowp(nnt_gpt2_model* m) {
     return NNT_OK;
 }
 
-// Everything up to the logits.
-static int32_t model_logits(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions) {
+// Everything up to the logits; with a cache (and its tensors, one pair per block) over that.
+static int32_t model_logits(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions, const nnt_cache_cfg* cache = nullptr,
+                            nnt_tensor* const* K = nullptr, nnt_tensor* const* V = nullptr) {
     nnt_ctx* ctx = m->ctx;
     nnt_gpt2_stack* st = m->stack;
     nnt_tensor** s = m->s;
     // X_0 = W_te[:, token] + W_pe[:, position]
-    TRY(nnt_embedding_fwd(ctx, tokens, table_of(m, NNT_MDL_WTE), st->acts[0]));
+    TRY(embedding_after(ctx, tokens, table_of(m, NNT_MDL_WTE), st->acts[0], cache ? K[0] : nullptr));
     TRY(nnt_embedding_fwd(ctx, positions, table_of(m, NNT_MDL_WPE), s[NNT_MDL_XPOS]));
     TRY(nnt_add(ctx, 1.f, s[NNT_MDL_XPOS], 1.f, st->acts[0]));
-    TRY(nnt_gpt2_stack_forward(st));
+    TRY(cache ? nnt_gpt2_stack_forward_cached(st, cache, K, V) : nnt_gpt2_stack_forward(st));
     TRY(nnt_layernorm_fwd(ctx, st->acts.back(), s[NNT_MDL_GAMMA_F], s[NNT_MDL_BETA_F], m->cfg.eps, s[NNT_MDL_XF], s[NNT_MDL_STATS_F]));
     // logits = W_te^T X_f (the head shares the token embedding)
     return nnt_gemm(ctx, 1.f, NNT_OP_T, table_of(m, NNT_MDL_WTE), NNT_OP_N, s[NNT_MDL_XF], 0.f, s[NNT_MDL_LOGITS], 1, 0, nullptr);
@@ -644,6 +704,30 @@ int32_t nnt_gpt2_model_forward_preference(nnt_gpt2_model* m, const int32_t* toke
         m->tokens = tokens;
         m->positions = positions;
         return NNT_OK;
+    });
+}
+
+int32_t nnt_gpt2_model_sample(nnt_gpt2_model* m, const int32_t* tokens, const int32_t* positions, const nnt_cache_cfg* cache, nnt_tensor* const* K,
+                              nnt_tensor* const* V, const nnt_sample_cfg* cfg, const int32_t* columns, int32_t n, const float* uniforms, int32_t* next,
+                              float* logp) {
+    if (!m) return NNT_EINVAL;
+    return entry(m->ctx, [&]() -> int32_t {
+        if (!tokens || !positions || !cache || !K || !V) return fail(m->ctx, NNT_EINVAL, "nnt_gpt2_model_sample: null argument");
+        for (size_t i = 0; i < m->stack->blocks.size(); i++) TRY(cached_check(m->stack->blocks[i], cache, K[i], V[i]));
+        TRY(sample_check(m->ctx, cfg, m->s[NNT_MDL_LOGITS], columns, n, uniforms, next));
+        m->tokens = m->positions = nullptr;
+        TRY(model_logits(m, tokens, positions, cache, K, V));
+        return sample_ordered(m->ctx, cfg, m->s[NNT_MDL_LOGITS], columns, n, uniforms, next, logp, K[0]);
+    });
+}
+
+int32_t nnt_gpt2_model_clip(nnt_gpt2_model* m, const nnt_clip_cfg* cfg, float* norm) {
+    if (!m) return NNT_EINVAL;
+    return entry(m->ctx, [&]() -> int32_t {
+        std::vector<nnt_tensor*> G;
+        for (nnt_gpt2_block* b : m->stack->blocks) add_gradients(b, &G);
+        G.insert(G.end(), m->s + NNT_MDL_GRAD, m->s + NNT_MDL_GRAD + 4);
+        return clip_in_place(m->ctx, cfg, G, norm);
     });
 }
 

@@ -185,7 +185,9 @@ int32_t check_act(nnt_ctx* ctx, const char* who, const nnt_tensor* Y) {
 
 using namespace nnt;
 
-int32_t nnt_embedding_fwd(nnt_ctx* ctx, const int32_t* tokens, nnt_tensor* W, nnt_tensor* Y) {
+int32_t nnt_embedding_fwd(nnt_ctx* ctx, const int32_t* tokens, nnt_tensor* W, nnt_tensor* Y) { return nnt::embedding_after(ctx, tokens, W, Y, nullptr); }
+
+int32_t nnt::embedding_after(nnt_ctx* ctx, const int32_t* tokens, nnt_tensor* W, nnt_tensor* Y, nnt_tensor* after) {
     NNT_CHECK_CTX(ctx);
     if (!tokens || !W || !Y) return fail(ctx, NNT_EINVAL, "nnt_embedding_fwd: null argument");
     int32_t rc = check_act(ctx, "nnt_embedding_fwd", Y);
@@ -202,7 +204,9 @@ int32_t nnt_embedding_fwd(nnt_ctx* ctx, const int32_t* tokens, nnt_tensor* W, nn
     const TiledView vw = W->view(), vy = Y->view();
     const int dw = W->dtype, dy = Y->dtype;
     OpTag tag(ctx, "embedding_fwd", (double)Y->shape[0] * Y->shape[1] * Y->shape[2] * (W->elem_size() + Y->elem_size()), true);
-    return submit(ctx, {W->all(kRead), Y->all(kWrite)}, [=](hipStream_t st) {
+    std::vector<Access> acc{Y->all(kWrite), W->all(kRead)};
+    if (after) after->whole_access(kRead, &acc);
+    rc = submit(ctx, acc, [=](hipStream_t st) {
         const dim3 grid((unsigned)((total + 255) / 256)), block(256);
 #define NNT_EMB_FWD(TW, TY)                                                                                              \
     do {                                                                                                                 \
@@ -216,6 +220,8 @@ int32_t nnt_embedding_fwd(nnt_ctx* ctx, const int32_t* tokens, nnt_tensor* W, nn
 #undef NNT_EMB_FWD
         return hipGetLastError() == hipSuccess ? (int32_t)NNT_OK : (int32_t)NNT_EHIP;
     });
+    if (rc == NNT_OK && after) after->whole_submitted();
+    return rc;
 }
 
 int32_t nnt_embedding_bwd(nnt_ctx* ctx, const int32_t* tokens, nnt_tensor* dY, nnt_tensor* dW) {

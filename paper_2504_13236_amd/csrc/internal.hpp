@@ -68,6 +68,12 @@ struct nnt_tensor {
     std::vector<void*> tiles;        // host copy of the tile pointers
     void** d_tiles;                  // device copy
     std::vector<nnt::TileDep> deps;  // one per tile
+    // A cache has thousands of pages, and the calls on it name them all, token after token: such calls keep one record for the
+    // whole tensor (whole_access) instead of one per tile.  Each side of the two kinds of users takes over what the other has left.
+    nnt::TileDep whole;
+    bool whole_used = false;         // `whole` is ahead of the tiles' records
+    bool tiles_used = false;         // the tiles' records are ahead of `whole`
+    bool whole_tiles = false;        // every tile is there and 16-byte aligned
     uint64_t id;
 
     int64_t elem_size() const { return dtype == NNT_F32 ? 4 : 2; }
@@ -102,8 +108,36 @@ struct nnt_tensor {
         }
         return v;
     }
-    nnt::Access all(int mode) { return nnt::Access{deps.data(), ntiles, mode}; }
-    nnt::Access one(int64_t idx, int mode) { return nnt::Access{&deps[idx], 1, mode}; }
+    nnt::Access all(int mode) {
+        use_tiles();
+        return nnt::Access{deps.data(), ntiles, mode};
+    }
+    nnt::Access one(int64_t idx, int mode) {
+        use_tiles();
+        return nnt::Access{&deps[idx], 1, mode};
+    }
+    // the accesses of a task that names the tensor as a whole; whole_submitted() once it has been submitted
+    void whole_access(int mode, std::vector<nnt::Access>* acc) {
+        acc->push_back(nnt::Access{&whole, 1, mode});
+        if (tiles_used) acc->push_back(nnt::Access{deps.data(), ntiles, mode});
+    }
+    void whole_submitted() {
+        tiles_used = false;
+        whole_used = true;
+    }
+    void use_tiles() {
+        tiles_used = true;
+        if (!whole_used) return;
+        whole_used = false;
+        for (nnt::TileDep& d : deps) {
+            if (whole.w_stream >= 0) {
+                d = whole;           // that writer came after all that the tile's record knew of
+            } else {
+                for (int s = 0; s < nnt::kMaxStreams; s++) d.r_seq[s] = d.r_seq[s] > whole.r_seq[s] ? d.r_seq[s] : whole.r_seq[s];
+            }
+        }
+        whole = nnt::TileDep();      // (the next such task finds all of it in the tiles' records)
+    }
 };
 
 namespace nnt {
@@ -262,6 +296,17 @@ int32_t policy_loss_check(nnt_ctx* ctx, const nnt_policy_cfg* cfg, nnt_tensor* X
                           nnt_tensor* advantages, nnt_tensor* dX, nnt_tensor* logp, float* losses, float* loss);
 int32_t preference_loss_check(nnt_ctx* ctx, const nnt_preference_cfg* cfg, nnt_tensor* X, const int32_t* labels, nnt_tensor* ref_logp, nnt_tensor* dX,
                               nnt_tensor* logp, float* rewards, float* losses, float* loss);
+
+int32_t sample_check(nnt_ctx* ctx, const nnt_sample_cfg* cfg, nnt_tensor* X, const int32_t* columns, int32_t n, const float* uniforms,
+                     const int32_t* tokens);
+// nnt_sample_tokens and nnt_embedding_fwd whose tasks are ordered against each other by a cache's tensor, as if the one wrote and the other
+// read it (sample.hip, embedding.hip): what is drawn are the tokens that the next step looks up
+int32_t embedding_after(nnt_ctx* ctx, const int32_t* tokens, nnt_tensor* W, nnt_tensor* Y, nnt_tensor* after);
+int32_t sample_ordered(nnt_ctx* ctx, const nnt_sample_cfg* cfg, nnt_tensor* X, const int32_t* columns, int32_t n, const float* uniforms, int32_t* tokens,
+                       float* logp, nnt_tensor* after);
+// whether the calls on a cache take these operands; their scratch is there afterwards (cache.hip)
+int32_t cache_check(nnt_ctx* ctx, const nnt_cache_cfg* cfg, nnt_tensor* QKV, nnt_tensor* K, nnt_tensor* V, nnt_tensor* B);
+int32_t clip_check(nnt_ctx* ctx, const nnt_clip_cfg* cfg, int32_t n, nnt_tensor* const* G, nnt_tensor* const* O, const float* norm);
 
 // Makes a context's device the current one of the calling thread for as long as it lives.
 struct DeviceScope {

@@ -57,6 +57,8 @@ int32_t nnt_tensor_create(nnt_ctx* ctx, int32_t dtype, int32_t ndim, const int64
     }
     t->tiles.assign(tile_ptrs, tile_ptrs + t->ntiles);
     t->deps.resize(t->ntiles);
+    t->whole_tiles = true;
+    for (void* p : t->tiles) t->whole_tiles = t->whole_tiles && p && ((uintptr_t)p & 15) == 0;
     t->d_tiles = nullptr;
     t->id = ctx->next_tensor_id++;
     hipError_t e = hipMalloc((void**)&t->d_tiles, t->ntiles * sizeof(void*));

@@ -218,6 +218,81 @@ def muon_step(ctx, G, P, M, P_lowp=None, **hyper):
     capi.nnt_muon_step(ctx.h, C.byref(cfg), len(G), _handles(G), _handles(P), _handles(M), _handles(P_lowp) if P_lowp is not None else None)
 
 
+def clip_grad_norm(ctx, G, norm, O=None, max_norm=1.0, eps=1e-6):
+    """Norm of all gradients (a list of tensors) into `norm` (device float), the clipped gradients into O (G itself: in place; None: norm only)."""
+    if O is not None:
+        _same_count(G, O)
+    cfg = capi.nnt_clip_cfg(max_norm, eps)
+    capi.nnt_clip_grad_norm(ctx.h, C.byref(cfg), len(G), _handles(G), _handles(O) if O is not None else None, norm.data_ptr())
+
+
+def sample_cfg(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    return capi.nnt_sample_cfg(temperature, top_p, min_p, top_k)
+
+
+def sample_tokens(ctx, X, uniforms, tokens, logp=None, columns=None, **filters):
+    """Draws a token from each column of the logits X that `columns` names (all of them), see sample_cfg for the filters."""
+    if len(tokens) != len(uniforms) or (logp is not None and len(logp) != len(tokens)) or (columns is not None and len(columns) != len(tokens)):
+        raise ValueError("columns, uniforms, tokens and logp must be of one length")
+    cfg = sample_cfg(**filters)
+    capi.nnt_sample_tokens(ctx.h, C.byref(cfg), X.h, columns.data_ptr() if columns is not None else None, len(tokens), uniforms.data_ptr(),
+                           tokens.data_ptr(), logp.data_ptr() if logp is not None else None)
+
+
+def rotation_table(ctx, r, n_positions, base=10000.0):
+    """Cosines and sines of position / base^(2 i / r), from angles in 64 bits, as a tensor that the calls on a cache take."""
+    angle = np.arange(n_positions)[None, :] * base ** (-2.0 * np.arange(r // 2) / r)[:, None]
+    return TiledTensor.from_numpy(ctx, np.concatenate([np.cos(angle), np.sin(angle)]), (r, n_positions))
+
+
+class PagedCache:
+    """Keys and values of `n_layers` blocks in pages of `page` positions, all layers with one table of pages; the host hands the
+    pages out (reserve, release), the calls on the device fill and read them."""
+
+    def __init__(self, ctx: Context, n_layers, h, N_h, N_kv, page, n_pages, N_b, max_pages, dtype="f32", rotation=None, rotate="halves", window=0):
+        self.ctx, self.page, self.N_b, self.max_pages = ctx, int(page), int(N_b), int(max_pages)
+        self.K, self.V = ([TiledTensor(ctx, dtype, (h, n_pages * page, N_kv), (h, page, N_kv)) for _ in range(n_layers)] for _ in range(2))
+        self.N_h, self.N_kv, self.rotation, self.window = N_h, N_kv, rotation, window
+        self.rotate = {"halves": capi.NNT_ROTATE_HALVES, "pairs": capi.NNT_ROTATE_PAIRS}[rotate]
+        self.free = list(range(n_pages - 1, -1, -1))
+        self.of = [[] for _ in range(self.N_b)]
+        self.pages = torch.full((self.N_b, self.max_pages), -1, dtype=torch.int32, device="cuda:%d" % ctx.device)
+
+    def reserve(self, lengths):
+        """Pages for `lengths[b]` positions of every sequence (those it has stay).  Call while nothing that reads the table is under way."""
+        need = [-(-int(n) // self.page) for n in lengths]
+        more = sum(max(0, n - len(p)) for n, p in zip(need, self.of))
+        if len(need) != self.N_b or max(need) > self.max_pages or more > len(self.free):
+            raise ValueError("%d more pages wanted, %d of at most %d a sequence are free" % (more, len(self.free), self.max_pages))
+        for n, p in zip(need, self.of):
+            while len(p) < n:
+                p.append(self.free.pop())
+        self._upload()
+
+    def release(self, b):
+        self.free += reversed(self.of[b])
+        self.of[b] = []
+        self._upload()
+
+    def _upload(self):
+        self.pages.copy_(torch.tensor([p + [-1] * (self.max_pages - len(p)) for p in self.of], dtype=torch.int32))
+        torch.cuda.synchronize()      # the context's streams do not order after torch's current stream
+
+    def cfg(self, start, count=None):
+        """The calls' view of the cache: start, count are int32 device tensors of one entry per sequence (positions cached, new tokens)."""
+        return capi.nnt_cache_cfg(self.pages.data_ptr(), start.data_ptr(), count.data_ptr() if count is not None else None,
+                                  self.rotation.h.value if self.rotation is not None else None, self.N_h, self.N_kv, self.max_pages, self.window, self.rotate)
+
+    def append(self, QKV, start, count=None, layer=0):
+        cfg = self.cfg(start, count)
+        capi.nnt_cache_append(self.ctx.h, C.byref(cfg), QKV.h, self.K[layer].h, self.V[layer].h)
+
+    def attention(self, QKV, B, start, count=None, scale=None, layer=0):
+        cfg = self.cfg(start, count)
+        h = self.K[layer].shape[0]
+        capi.nnt_cache_attention(self.ctx.h, C.byref(cfg), h ** -0.5 if scale is None else scale, QKV.h, self.K[layer].h, self.V[layer].h, B.h)
+
+
 def causal_absent(base_k, base_q, n_q):
     """Predicate for score tensors [k, q, ...]: tile (kt, qt, ...) holds no visible
     score when its first key index exceeds its last query index."""
@@ -241,7 +316,8 @@ class Gpt2Block:
     slot) and exposes forward / backward / adam."""
 
     def __init__(self, ctx: Context, N_e, N_h, N_m, N_s, N_b, tiles, dtype="f32", eps=1e-5, gelu="tanh",
-                 causal=True, adam=True, fused_attention=False):
+                 causal=True, adam=True, fused_attention=False, share=None):
+        """share: a block whose parameters (gradients, moments, bf16 copies) this one uses, for another sequence length or batch."""
         self.ctx = ctx
         cfg = capi.nnt_gpt2_block_cfg()
         cfg.N_e, cfg.N_h, cfg.N_m, cfg.N_s, cfg.N_b = N_e, N_h, N_m, N_s, N_b
@@ -259,6 +335,9 @@ class Gpt2Block:
             info = capi.nnt_slot_info()
             capi.nnt_gpt2_block_slot(C.byref(cfg), s, C.byref(info))
             if not info.used:
+                continue
+            if share is not None and s < capi.NNT_BLK_STATS1:
+                self.slots[s] = share.slots[s]
                 continue
             if capi.NNT_BLK_ADAM_M <= s < capi.NNT_BLK_LOWP and not adam:
                 continue
@@ -288,8 +367,17 @@ class Gpt2Block:
     def forward(self, X, Out):
         capi.nnt_gpt2_block_forward(self.h, X.h, Out.h)
 
+    def forward_cached(self, cache, X, Out, start, count=None, layer=0):
+        cfg = cache.cfg(start, count)
+        capi.nnt_gpt2_block_forward_cached(self.h, C.byref(cfg), cache.K[layer].h, cache.V[layer].h, X.h, Out.h)
+
     def backward(self, dOut, dX):
         capi.nnt_gpt2_block_backward(self.h, dOut.h, dX.h)
+
+    def clip(self, norm, max_norm=1.0, eps=1e-6):
+        """The gradients clipped by their norm, which `norm` (device float) receives."""
+        cfg = capi.nnt_clip_cfg(max_norm, eps)
+        capi.nnt_gpt2_block_clip(self.h, C.byref(cfg), norm.data_ptr())
 
     def adam(self, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0):
         cfg = capi.nnt_adam_cfg(lr, beta1, beta2, eps, weight_decay)
@@ -337,8 +425,16 @@ class Gpt2Stack:
     def forward(self):
         capi.nnt_gpt2_stack_forward(self.h)
 
+    def forward_cached(self, cache, start, count=None):
+        cfg = cache.cfg(start, count)
+        capi.nnt_gpt2_stack_forward_cached(self.h, C.byref(cfg), _handles(cache.K), _handles(cache.V))
+
     def backward(self):
         capi.nnt_gpt2_stack_backward(self.h)
+
+    def clip(self, norm, max_norm=1.0, eps=1e-6):
+        cfg = capi.nnt_clip_cfg(max_norm, eps)
+        capi.nnt_gpt2_stack_clip(self.h, C.byref(cfg), norm.data_ptr())
 
     def adam(self, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0):
         cfg = capi.nnt_adam_cfg(lr, beta1, beta2, eps, weight_decay)
@@ -364,7 +460,9 @@ class Gpt2Model:
     Tensors (paper's axis order): `wte` [N_e, N_v] and `wpe` [N_e, N_s] fp32 masters (one column per
     vocabulary item / position), their gradients and Adam moments, bf16 copies for bf16 models."""
 
-    def __init__(self, ctx: Context, blocks, N_v, tile_v):
+    def __init__(self, ctx: Context, blocks, N_v, tile_v, share=None):
+        """share: a model whose parameters (gradients, moments, bf16 copies) this one uses, for a sequence length up to its own or another
+        batch; `blocks` share those of its blocks."""
         self.ctx, self.blocks = ctx, list(blocks)
         b0 = self.blocks[0]
         self.N_e, self.N_s, self.N_b = b0.act_shape
@@ -375,7 +473,9 @@ class Gpt2Model:
         for s in range(capi.NNT_MDL_NSLOTS):
             info = capi.nnt_slot_info()
             capi.nnt_gpt2_model_slot(C.byref(b0.cfg), self.N_v, int(tile_v), s, C.byref(info))
-            if info.used:
+            if info.used and share is not None and s < capi.NNT_MDL_XPOS:
+                self.slots[s] = share.slots[s]
+            elif info.used:
                 zero = s < capi.NNT_MDL_LOWP            # parameters, gradients and moments start at zero
                 self.slots[s] = TiledTensor(ctx, info.dtype, tuple(info.shape[:info.ndim]), tuple(info.basetile[:info.ndim]),
                                             fill=0 if zero else None)
@@ -442,6 +542,23 @@ class Gpt2Model:
         capi.nnt_gpt2_model_forward_preference(self.h, self.tokens.data_ptr(), self.pos.data_ptr(), self.labels.data_ptr(), C.byref(cfg),
                                                ref.h if ref is not None else None, logp.h, self.rewards.data_ptr(), self.col_loss.data_ptr(),
                                                self.loss.data_ptr())
+
+    def sample(self, cache, start, uniforms, next, count=None, columns=None, logp=None, positions=None, tokens=None, **filters):
+        """One step of generation over a PagedCache: forward pass of the batch's tokens (or `tokens`) at `positions` (those of the last batch of
+        positions), then a token drawn from each of the logits' columns that `columns` names (all of them) into `next`."""
+        if len(next) != len(uniforms) or (logp is not None and len(logp) != len(next)) or (columns is not None and len(columns) != len(next)):
+            raise ValueError("columns, uniforms, next and logp must be of one length")
+        if len(cache.K) != len(self.blocks) or cache.N_b != self.N_b:
+            raise ValueError("the cache is of another number of blocks or sequences")
+        ccfg, scfg = cache.cfg(start, count), sample_cfg(**filters)
+        capi.nnt_gpt2_model_sample(self.h, (self.tokens if tokens is None else tokens).data_ptr(), (self.pos if positions is None else positions).data_ptr(),
+                                   C.byref(ccfg), _handles(cache.K), _handles(cache.V), C.byref(scfg),
+                                   columns.data_ptr() if columns is not None else None, len(next), uniforms.data_ptr(), next.data_ptr(),
+                                   logp.data_ptr() if logp is not None else None)
+
+    def clip(self, norm, max_norm=1.0, eps=1e-6):
+        cfg = capi.nnt_clip_cfg(max_norm, eps)
+        capi.nnt_gpt2_model_clip(self.h, C.byref(cfg), norm.data_ptr())
 
     def backward(self):
         capi.nnt_gpt2_model_backward(self.h)

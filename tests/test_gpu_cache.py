@@ -1,0 +1,471 @@
+"""Paged cache and the attention over it against the oracle: element types, head layouts, page and tile sizes that do not divide anything,
+sequences of different lengths, pages that are not there, what lies in masked places, captured graphs, refusals."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import workload
+from oracle import rollout as R
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+EPS32 = 2.0 ** -24
+HALF = {"f32": EPS32, "bf16": 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2504_13236_amd import tiled
+    c = tiled.Context(n_streams=2)
+    yield c
+    c.close()
+
+
+def quant(a, dtype):
+    a = np.asarray(a, np.float32)
+    return workload.round_through_bf16(a.reshape(-1)).reshape(a.shape).astype(np.float64) if dtype == "bf16" else a.astype(np.float64)
+
+
+def ints(a):
+    return torch.from_numpy(np.ascontiguousarray(np.asarray(a, np.int32))).cuda()
+
+
+class Problem:
+    """A cache, sequences in it and new tokens of them, in numpy and on the device."""
+
+    def __init__(self, ctx, dtype, N_h, N_kv, h, P, start, N_s, count=None, rotation=None, window=0, tiles=(3, 4, 2), seed=0, spare=2, seen_std=1.0):
+        from paper_2504_13236_amd import capi, tiled
+        r = np.random.default_rng(seed)
+        self.ctx, self.dtype, self.N_h, self.N_kv, self.h, self.P, self.window = ctx, dtype, N_h, N_kv, h, P, window
+        N_b = len(start)
+        self.start, self.count = np.array(start, np.int64), None if count is None else np.array(count)
+        need = [-(-(s + (N_s if count is None else max(0, min(N_s, c)))) // P) for s, c in zip(start, count or [0] * N_b)]
+        max_pages = max(need) + 1
+        n_pages = sum(need) + spare
+        order = list(r.permutation(n_pages))
+        self.pages = np.full((max_pages, N_b), -1, np.int64)
+        for b, n in enumerate(need):
+            for i in range(n):
+                self.pages[i, b] = order.pop()
+        self.QKV = quant(r.standard_normal(((N_h + 2 * N_kv) * h, N_s, N_b)), dtype)
+        self.K, self.V = (quant(seen_std * r.standard_normal((h, n_pages * P, N_kv)), dtype) for _ in range(2))
+        self.B = quant(r.standard_normal((N_h * h, N_s, N_b)), dtype)
+        th, ts, tb = tiles
+        T = tiled.TiledTensor
+        self.tQKV = T.from_numpy(ctx, self.QKV, (th * h, ts, tb), dtype)
+        self.tK, self.tV = (T.from_numpy(ctx, a, (h, P, N_kv), dtype) for a in (self.K, self.V))
+        self.tB = T.from_numpy(ctx, self.B, (min(th, N_h) * h, ts + 1, tb), dtype)
+        self.table, self.pairs, self.ttable = None, False, None
+        cfg = capi.nnt_cache_cfg()
+        if rotation:
+            kind, r_dim, n_pos = rotation
+            angle = np.arange(n_pos)[None, :] * 100.0 ** (-2.0 * np.arange(r_dim // 2) / r_dim)[:, None]
+            self.table = np.concatenate([np.cos(angle), np.sin(angle)]).astype(np.float32).astype(np.float64)
+            self.pairs = kind == "pairs"
+            self.ttable = T.from_numpy(ctx, self.table, (r_dim, 5))
+            cfg.rotation, cfg.rotate = self.ttable.h.value, capi.NNT_ROTATE_PAIRS if self.pairs else capi.NNT_ROTATE_HALVES
+        self.dpages, self.dstart = ints(self.pages.T), ints(self.start)
+        self.dcount = None if count is None else ints(count)
+        cfg.pages, cfg.start, cfg.count = self.dpages.data_ptr(), self.dstart.data_ptr(), None if count is None else self.dcount.data_ptr()
+        cfg.N_h, cfg.N_kv, cfg.max_pages, cfg.window = N_h, N_kv, max_pages, window
+        self.cfg, self.scale = cfg, 0.7 * h ** -0.5
+        torch.cuda.synchronize()
+
+    def append(self):
+        from paper_2504_13236_amd import capi
+        capi.nnt_cache_append(self.ctx.h, C.byref(self.cfg), self.tQKV.h, self.tK.h, self.tV.h)
+
+    def attention(self):
+        from paper_2504_13236_amd import capi
+        capi.nnt_cache_attention(self.ctx.h, C.byref(self.cfg), self.scale, self.tQKV.h, self.tK.h, self.tV.h, self.tB.h)
+
+    def expected_cache(self):
+        return R.cache_append(self.QKV, self.K, self.V, self.P, self.N_h, self.pages, self.start, self.count, self.table, self.pairs)
+
+    def check_append(self):
+        K, V = self.expected_cache()
+        gk, gv = self.tK.download(), self.tV.download()
+        assert np.array_equal(gv, V.astype(np.float32))
+        # a turned component: two products and their sum in fp32, rounded to the type once
+        written = K != self.K
+        bound = HALF[self.dtype] * np.abs(K) + 3 * EPS32 * np.abs(self.QKV).max() * 2
+        assert (np.abs(gk - K) <= np.where(written, bound, 0.0)).all(), np.abs(gk - K).max()
+        return gk.astype(np.float64), gv.astype(np.float64)
+
+    def check_attention(self, K, V):
+        """Bounds: a score is a sum of h products in fp32, off by (h + 4) 2^-24 of sum |K||Q| (the rotated query included), in an exponent of
+        base 2 that adds a rounding of its own size; exponentials 2^-22 of their value; n weights and products added in fp32.  Weights may be rounded to
+        the tensors' type before the product with the values: half a step of each.  The result is rounded once."""
+        got = self.tB.download()
+        B, (mass, reach, largest) = R.cache_attention(self.QKV, K, V, self.B, self.P, self.N_h, self.scale, self.pages, self.start, self.count, self.table,
+                                                      self.pairs, self.window)
+        n = int((self.start + self.QKV.shape[1]).max())
+        weight = 2 * (self.h + 8) * EPS32 * reach + (4 + 2 * min(n, 4096)) * EPS32
+        if self.dtype == "bf16":
+            weight = weight + HALF["bf16"]
+        bound = HALF[self.dtype] * np.abs(B) + weight * (mass + np.abs(B)) * 1.01
+        new = np.zeros(B.shape, bool)
+        for b in range(B.shape[2]):
+            new[:, :R.new_tokens(self.count, b, B.shape[1]), b] = True
+        assert np.array_equal(got[~new], self.B.astype(np.float32)[~new])
+        assert np.isfinite(got).all()
+        worst = (np.abs(got - B) - np.where(new, bound, 0.0)).max()
+        assert worst <= 0.0, worst
+        return got
+
+    def close(self):
+        for t in (self.tQKV, self.tK, self.tV, self.tB, self.ttable):
+            if t is not None:
+                t.close()
+
+
+def run(ctx, *args, **kw):
+    p = Problem(ctx, *args, **kw)
+    p.append()
+    K, V = p.check_append()
+    p.attention()
+    p.check_attention(K, V)
+    p.close()
+
+
+CASES = [
+    # N_h, N_kv, h, P, start, N_s, count
+    (1, 1, 8, 1, [0], 1, None),
+    (2, 2, 64, 16, [0, 5, 16, 31], 1, None),
+    (12, 12, 64, 16, [100], 1, None),
+    (4, 2, 128, 7, [50, 0, 6], 1, [1, 1, 1]),
+    (8, 1, 32, 5, [33, 17], 1, None),
+    (6, 2, 96, 24, [200, 3, 77], 3, [3, 1, 2]),
+    (3, 3, 80, 9, [40, 0], 5, [5, 0]),
+    (5, 5, 64, 33, [129, 60, 1], 17, [17, 9, 16]),
+    (2, 1, 256, 3, [10, 20], 4, [4, 4]),
+    (4, 4, 24, 8, [1000], 2, None),
+    (4, 4, 128, 64, [700, 0], 40, [40, 33]),
+    (2, 2, 64, 32, [300, 64], 130, [130, 64]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "h%dx%d_%d_p%d_s%d" % (c[0], c[1], c[2], c[3], c[5]))
+def test_append_and_attention(ctx, dtype, case):
+    N_h, N_kv, h, P, start, N_s, count = case
+    run(ctx, dtype, N_h, N_kv, h, P, start, N_s, count)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rotation", [("halves", 64, 60), ("pairs", 64, 60), ("halves", 20, 60), ("pairs", 6, 60), ("halves", 2, 60)])
+@pytest.mark.parametrize("N_s", [1, 7])
+def test_rotation(ctx, dtype, rotation, N_s):
+    run(ctx, dtype, 4, 2, 64, 8, [21, 0, 40], N_s, rotation=rotation)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N_s", [1, 40])
+def test_positions_behind_the_rotation_are_neither_written_nor_answered(ctx, dtype, N_s):
+    p = Problem(ctx, dtype, 2, 2, 64, 8, [15, 60, 30], N_s, rotation=("halves", 64, 30))
+    p.append()
+    K, V = p.expected_cache()
+    gk, gv = p.tK.download(), p.tV.download()
+    assert np.array_equal(gv, V.astype(np.float32))
+    p.attention()
+    got = p.check_attention(gk.astype(np.float64), gv.astype(np.float64))
+    assert not got[:, :, 1].any() and not got[:, :, 2].any() and got[:, 0, 0].any()
+    p.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("window", [1, 2, 16, 50, 10000])
+@pytest.mark.parametrize("N_s", [1, 3, 70])
+def test_window(ctx, dtype, window, N_s):
+    run(ctx, dtype, 4, 2, 64, 8, [100, 0, 37], N_s, window=window)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N_s", [1, 20, 65])
+def test_pages_that_are_not_there(ctx, dtype, N_s):
+    p = Problem(ctx, dtype, 2, 2, 64, 8, [40, 90, 3], N_s)
+    n_pages = p.K.shape[1] // 8
+    p.pages[1, 0], p.pages[2:9, 1], p.pages[:, 2] = -1, n_pages, 2 ** 31 - 1
+    p.pages[3, 0] = -2 ** 31
+    p.dpages.copy_(torch.from_numpy(p.pages.T.astype(np.int32)))
+    torch.cuda.synchronize()
+    p.append()
+    K, V = p.check_append()
+    p.attention()
+    got = p.check_attention(K, V)
+    assert not got[:, :, 2].any()             # nothing to see
+    p.close()
+
+
+@pytest.mark.parametrize("start", [[-3, -1], [2 ** 31 - 1, 10 ** 6], [-2 ** 31, 2 ** 31 - 3]])
+def test_positions_outside_the_table(ctx, start):
+    p = Problem(ctx, "f32", 2, 2, 64, 8, [40, 9], 5)
+    p.start[:] = start
+    p.dstart.copy_(ints(p.start))
+    torch.cuda.synchronize()
+    p.append()
+    K, V = p.check_append()
+    p.attention()
+    p.QKV_all = p.QKV
+    # (the oracle walks every position of a row: the longest are beyond the table, whose end is where the walk can stop)
+    end = p.pages.shape[0] * p.P
+    from_table = np.array([min(s, end) for s in start])
+    B = p.tB.download()
+    for b, s in enumerate(start):
+        for i in range(5):
+            want, (mass, reach, _) = R.cache_attention(p.QKV[:, i:i + 1, b:b + 1], K, V, p.B[:, i:i + 1, b:b + 1], p.P, 2, p.scale, p.pages[:, b:b + 1],
+                                                       np.array([max(-1, min(s + i, end))]))
+            bound = EPS32 * np.abs(want) + (2 * 72 * EPS32 * reach + 300 * EPS32) * (mass + np.abs(want))
+            assert (np.abs(B[:, i:i + 1, b:b + 1] - want) <= bound).all(), (b, i)
+    assert from_table.shape == (2,)
+    p.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("what", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("N_s", [1, 3, 40])
+def test_what_is_masked_does_not_enter(ctx, dtype, what, N_s):
+    """Slots behind the sequences, keys before a window, pages of nobody and tokens behind a sequence's new ones hold anything."""
+    p = Problem(ctx, dtype, 4, 2, 64, 8, [41, 10], N_s, count=[N_s, (N_s + 1) // 2], window=24)
+    clean = p.expected_cache()
+    K, V = np.full_like(p.K, what), np.full_like(p.V, what)
+    for b in range(2):
+        for pos in range(max(0, p.start[b] - 23), p.start[b]):
+            at = R.slot_of(pos, b, p.pages, 8, K.shape[1] // 8)
+            K[:, at], V[:, at] = p.K[:, at], p.V[:, at]
+    p.tK.upload(K)
+    p.tV.upload(V)
+    Z = p.QKV.copy()
+    Z[:, (N_s + 1) // 2:, 1] = what
+    p.tQKV.upload(Z)
+    p.append()
+    p.attention()
+    ck, cv = clean
+    if p.dtype == "bf16":
+        ck = quant(ck, dtype)
+    p.check_attention(ck, cv)
+    p.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N_s", [2, 40, 70])
+def test_a_token_does_not_see_what_comes_after_it(ctx, dtype, N_s):
+    """Later tokens of the same call with infinities in keys and values: the ones before them do not change."""
+    p = Problem(ctx, dtype, 2, 2, 64, 8, [41, 10], N_s)
+    p.append()
+    K, V = p.check_append()
+    p.attention()
+    before = p.tB.download()
+    half = N_s // 2
+    Z = p.QKV.copy()
+    Z[2 * 64:4 * 64, half:] = np.inf
+    Z[4 * 64:, half:] = np.nan
+    p.tQKV.upload(Z)
+    p.append()
+    p.attention()
+    after = p.tB.download()
+    assert np.array_equal(after[:, :half], before[:, :half])
+    p.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_infinite_and_absent_scores(ctx, dtype):
+    """A NaN that is seen is passed on; -infinity in a key leaves the others."""
+    p = Problem(ctx, dtype, 1, 1, 64, 8, [20, 20], 1)
+    V = p.V.copy()
+    V[5, R.slot_of(7, 0, p.pages, 8, 99), 0] = np.nan
+    p.tV.upload(V)
+    p.append()
+    p.attention()
+    got = p.tB.download()
+    assert np.isnan(got[5, 0, 0]) and np.isfinite(np.delete(got[:, 0, 0], 5)).all() and np.isfinite(got[:, 0, 1]).all()
+    p.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_long_sequence_and_many_short_ones(ctx, dtype):
+    run(ctx, dtype, 2, 1, 64, 64, [9000], 1)
+    run(ctx, dtype, 2, 2, 64, 16, [int(s) for s in np.random.default_rng(5).integers(0, 200, 40)], 1, tiles=(2, 1, 7))
+
+
+def test_counts_outside_the_call(ctx):
+    run(ctx, "f32", 2, 2, 32, 8, [9, 0, 30], 4, count=[-5, 100, 2])
+
+
+@pytest.mark.parametrize("dtype,N_s", [("f32", 1), ("bf16", 1), ("bf16", 33)])
+def test_captured_and_replayed(ctx, dtype, N_s):
+    """A graph of both calls, replayed with other lengths and other inputs, eager work of the same context between the replays."""
+    from paper_2504_13236_amd import capi
+    p = Problem(ctx, dtype, 4, 2, 64, 8, [300, 20], N_s, spare=60)
+    p.append()
+    p.attention()                                  # scratch exists from here on
+    ctx.wait()
+    g = C.c_void_p()
+    capi.nnt_capture_begin(ctx.h)
+    p.append()
+    p.attention()
+    capi.nnt_capture_end(ctx.h, C.byref(g))
+    K, V = p.tK.download().astype(np.float64), p.tV.download().astype(np.float64)
+    for k, start in enumerate(([300, 20], [250, 7], [0, 24 - N_s if N_s < 24 else 0])):
+        p.start[:] = start
+        p.dstart.copy_(ints(start))
+        p.QKV = quant(np.random.default_rng(50 + k).standard_normal(p.QKV.shape), dtype)
+        p.tQKV.upload(p.QKV)
+        p.tB.upload(p.B)
+        p.K, p.V = K, V
+        capi.nnt_graph_launch(g)
+        K, V = p.check_append()
+        got = p.check_attention(K, V)
+        p.tB.upload(p.B)
+        p.attention()
+        assert np.array_equal(p.tB.download(), got)
+    capi.nnt_graph_destroy(g)
+    p.close()
+
+
+def test_two_graphs_share_the_scratch(ctx):
+    from paper_2504_13236_amd import capi
+    a = Problem(ctx, "f32", 2, 2, 64, 8, [700], 1, seed=1)
+    b = Problem(ctx, "f32", 4, 2, 64, 8, [500, 300], 1, seed=2)
+    graphs, want = [], []
+    for p in (a, b):
+        p.append()
+        p.attention()
+        ctx.wait()
+    for p in (a, b):
+        g = C.c_void_p()
+        capi.nnt_capture_begin(ctx.h)
+        p.attention()
+        capi.nnt_capture_end(ctx.h, C.byref(g))
+        graphs.append(g)
+        want.append(p.tB.download())
+    big = Problem(ctx, "f32", 8, 8, 64, 8, [900] * 3, 2, seed=3)     # larger scratch: the graphs keep the one they were captured with
+    big.append()
+    big.attention()
+    for _ in range(3):
+        for p in (a, b):
+            p.tB.upload(p.B)
+        for g in graphs:
+            capi.nnt_graph_launch(g)
+        big.attention()
+        for p, w in zip((a, b), want):
+            assert np.array_equal(p.tB.download(), w)
+    for g in graphs:
+        capi.nnt_graph_destroy(g)
+    for p in (a, b, big):
+        p.close()
+
+
+@pytest.mark.parametrize("granularity", [0, 1])
+def test_ordinary_operations_on_a_cache_are_ordered_with_its_calls(granularity):
+    """Fills and copies of the cache's tensors (tile by tile) before and after the calls that name it as a whole, on four streams."""
+    from paper_2504_13236_amd import capi, tiled
+    with tiled.Context(n_streams=4, granularity=granularity) as ctx:
+        p = Problem(ctx, "f32", 4, 4, 64, 4, [200, 100], 1)
+        copy = tiled.TiledTensor.zeros(ctx, p.V.shape, (64, 4, 4))
+        for k in range(20):
+            capi.nnt_fill(ctx.h, float(k), p.tV.h)
+            p.append()
+            p.attention()
+            capi.nnt_add(ctx.h, 1.0, p.tV.h, 0.0, copy.h)
+            capi.nnt_fill(ctx.h, -1.0, p.tV.h)
+            capi.nnt_fill(ctx.h, 0.0, p.tK.h)
+        ctx.wait()
+        got, kept, v = p.tB.download(), copy.download(), p.tV.download()
+        assert (v == -1.0).all()
+        own = np.zeros(p.V.shape[1], bool)
+        for b in range(2):
+            own[R.slot_of(int(p.start[b]), b, p.pages, 4, p.V.shape[1] // 4)] = True
+        assert (kept[:, ~own] == 19.0).all()
+        values = p.QKV[8 * 64:].reshape(4, 64, 1, 2)
+        assert (np.abs(kept[:, own]).max() > 0) and not (kept[:, own] == 19.0).all()
+        # keys of zeros but the new one: between the fill's value and the new token's
+        lo, hi = np.minimum(values, 19.0), np.maximum(values, 19.0)
+        g = got.reshape(4, 64, 1, 2)
+        assert ((g >= lo - 1e-3) & (g <= hi + 1e-3)).all()
+        p.close()
+        copy.close()
+
+
+def test_results_do_not_hang_on_the_run(ctx):
+    p = Problem(ctx, "bf16", 4, 2, 128, 16, [3000, 100], 1)
+    p.append()
+    p.attention()
+    first = p.tB.download()
+    for _ in range(5):
+        p.attention()
+        assert np.array_equal(p.tB.download(), first)
+    p.close()
+
+
+def test_refusals(ctx):
+    from paper_2504_13236_amd import capi, tiled
+    T = tiled.TiledTensor
+    p = Problem(ctx, "f32", 4, 2, 64, 8, [20, 3], 2, rotation=("halves", 32, 40))
+    keep = [p]
+
+    def refused(code=capi.NNT_EINVAL, scale=0.1, Z=p.tQKV, K=p.tK, V=p.tV, B=p.tB, append=True, **cfg):
+        c = capi.nnt_cache_cfg.from_buffer_copy(p.cfg)
+        for k, v in cfg.items():
+            setattr(c, k, v)
+        h = lambda t: t.h if t is not None else None
+        assert capi.nnt_cache_attention.raw(ctx.h, C.byref(c), scale, h(Z), h(K), h(V), h(B)) == code
+        if append:
+            assert capi.nnt_cache_append.raw(ctx.h, C.byref(c), h(Z), h(K), h(V)) == code
+
+    def t(shape, base, dtype="f32", **kw):
+        x = T.zeros(ctx, shape, base, dtype, **kw)
+        keep.append(x)
+        return x
+    N, n = p.K.shape[1], 2
+    refused(pages=None)
+    refused(start=None)
+    refused(N_h=0)
+    refused(N_h=3)
+    refused(N_kv=3)
+    refused(max_pages=0)
+    refused(max_pages=2 ** 31 - 1)
+    refused(window=-1)
+    refused(rotate=2)
+    refused(Z=None)
+    refused(K=None)
+    refused(K=p.tV)
+    refused(B=None, append=False)
+    refused(B=p.tQKV, append=False)
+    for s in (0.0, -1.0, float("nan"), float("inf")):
+        refused(scale=s, append=False)
+    refused(Z=t((8 * 64, 2, 2), (96, 4, 2)))                              # a row tile that cuts a head
+    refused(Z=t((7 * 64, 2, 2), (64, 4, 2)))
+    refused(code=capi.NNT_EDTYPE, Z=t((8 * 64, 2, 2), (64, 4, 2), "bf16"))
+    refused(B=t((4 * 64, 2, 3), (64, 2, 3)), append=False)
+    refused(B=t((4 * 64, 2, 2), (32, 2, 3)), append=False)
+    refused(code=capi.NNT_EDTYPE, B=t((4 * 64, 2, 2), (64, 2, 3), "bf16"), append=False)
+    refused(K=t((64, N, n), (64, 4, n)))                                   # not V's pages
+    refused(K=t((64, N, n), (32, 8, n)), V=t((64, N, n), (32, 8, n)))      # a page that holds half a head
+    refused(K=t((64, N, n), (64, 8, 1)), V=t((64, N, n), (64, 8, 1)))      # ... or not all heads
+    refused(K=t((64, N - 1, n), (64, 8, n)), V=t((64, N - 1, n), (64, 8, n)))
+    refused(K=t((64, N, n), (64, 8, n), absent=lambda i: i[1] == 1), V=t((64, N, n), (64, 8, n), absent=lambda i: i[1] == 1))
+    refused(rotation=t((33, 40), (33, 40)).h.value)
+    refused(rotation=t((66, 40), (66, 40)).h.value)
+    refused(rotation=t((32, 40), (16, 40)).h.value)
+    refused(rotation=t((32, 40), (32, 40), "bf16").h.value)
+    odd = t((8 * 64, 2, 2), (4 * 64, 4, 2))
+    # a tile that is not 16-byte aligned
+    h = C.c_void_p()
+    capi.nnt_tensor_create(ctx.h, 0, 3, capi.i64_array((8 * 64, 2, 2)), capi.i64_array((8 * 64, 2, 2)), capi.ptr_array([odd.buf.data_ptr() + 4]), C.byref(h))
+    c = capi.nnt_cache_cfg.from_buffer_copy(p.cfg)
+    assert capi.nnt_cache_append.raw(ctx.h, C.byref(c), h, p.tK.h, p.tV.h) == capi.NNT_EINVAL
+    capi.nnt_tensor_destroy(h)
+    with tiled.Context(n_streams=1) as other:
+        x = T.zeros(other, (8 * 64, 2, 2), (64, 2, 2))
+        assert capi.nnt_cache_append.raw(ctx.h, C.byref(p.cfg), x.h, p.tK.h, p.tV.h) == capi.NNT_EINVAL
+        x.close()
+    # nothing of all that was launched, and the context goes on
+    assert np.array_equal(p.tK.download(), p.K.astype(np.float32))
+    p.append()
+    p.check_append()
+    for x in keep[::-1]:
+        x.close()
