@@ -7,10 +7,14 @@
 // whole multiples of 2^-shift: sums do not depend on their order, and where a prefix ends is the same question for every
 // workgroup size and tiling.
 //
-// One workgroup per column; each wavefront owns a run of consecutive vectors of it, in registers where they fit.  No column is sorted:
-// the place where a prefix ends is found by a histogram over 2048 equal parts of the column's range (which a monotone function of the logit picks,
-// so a part is a run of the order), and only the part that holds the border is looked at more closely: sorted in LDS, or, while it
-// holds more than a list of 2048, divided again by the bits of its keys.
+// One workgroup per column.  No column is sorted; all filters come to one border (a logit, and the last number among equal ones), and the draw is one
+// pass over the column in the order of the numbers.  Where the border lies:
+//   bf16 columns of up to 65535: the column is counted by its 16 bits in LDS.  There are few different values, so weights,
+//     sums and borders are those of some thousand (value, count) pairs.
+//   top-k of up to 512, fp32: the k-th largest of the threads' largest logits is at most the k-th largest of all, and little more than k logits
+//     are at least as large: they are sorted in LDS.
+//   else: a histogram over 2048 equal parts of the column's range (which a monotone function of the logit picks, so a part is a run
+//     of the order); the part that holds the border is sorted in LDS, or, while it holds more than a list of 2048, divided again by the bits of its keys.
 #include "colwise.hpp"
 #include "device_util.hpp"
 #include "internal.hpp"
@@ -24,8 +28,11 @@ namespace {
 
 constexpr int kBins = 2048;
 constexpr int kList = 2048;
+constexpr int kTableTiles = 64;               // vocabulary tiles whose addresses a workgroup keeps in LDS
 constexpr int64_t kMaxVectors = 1 << 20;      // of a column: up to there `place` finds a vector's tile exactly
 constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kPosInf = __builtin_huge_valf();
+constexpr double kLog2e = 1.4426950408889634;
 
 struct Sample {
     TiledView X;
@@ -36,7 +43,9 @@ struct Sample {
     int32_t vt, nvec, ncols;          // vectors of a whole tile, of the column; columns of X
     float inv_vt;
     int32_t top_k, greedy, shift;
-    double inv_t, top_p, min_p;
+    double c;                         // 1 / (T ln 2)
+    double top_p;
+    double min_fall;                  // T log(min_p): how far below the largest logit a kept one may lie
 };
 
 __device__ __forceinline__ double wave_sum64(double v) {
@@ -44,20 +53,24 @@ __device__ __forceinline__ double wave_sum64(double v) {
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     return v;
 }
-__device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor((unsigned long long)v, o, 64);
+// Inclusive sums over a wavefront's lanes: rows of 16 lanes by shifts, then the rows' last lanes into the rows behind them (data-parallel moves: a few cycles a step,
+// where a lane exchange through LDS takes a hundred).
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, kRows, 0xf, false); }
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint64_t moved(uint64_t v) { return (uint64_t)moved<kCtrl, kRows>((uint32_t)(v >> 32)) << 32 | moved<kCtrl, kRows>((uint32_t)v); }
+template <typename U>
+__device__ __forceinline__ U wave_scan(U v) {
+    v += moved<0x111, 0xf>(v);
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);
+    v += moved<0x143, 0xc>(v);
     return v;
 }
-__device__ __forceinline__ uint64_t wave_scan_u64(uint64_t v) {      // inclusive
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint64_t y = __shfl_up((unsigned long long)v, o, 64);
-        if (lane >= o) v += y;
-    }
-    return v;
-}
+__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
+__device__ __forceinline__ uint64_t last_lane(uint64_t v) { return (uint64_t)last_lane((uint32_t)(v >> 32)) << 32 | last_lane((uint32_t)v); }
 __device__ __forceinline__ float wave_min(float v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = fminf(v, __shfl_xor(v, o, 64));
@@ -71,46 +84,77 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu)); }
 
-// exp(y), y <= 0: 2^n times the series of e^r, |r| <= ln 2 / 2, up to r^12 / 12!; what is left out is below 2e-16 of the value.
-__device__ __forceinline__ double exp64(double y) {
-    const double n = rint(y * 1.4426950408889634);
-    const double r = fma(n, -1.9082149292705877e-10, fma(n, -0.6931471803691238, y));
-    double p = 1.0 / 479001600.0;
-    p = fma(p, r, 1.0 / 39916800.0);
-    p = fma(p, r, 1.0 / 3628800.0);
-    p = fma(p, r, 1.0 / 362880.0);
-    p = fma(p, r, 1.0 / 40320.0);
-    p = fma(p, r, 1.0 / 5040.0);
-    p = fma(p, r, 1.0 / 720.0);
-    p = fma(p, r, 1.0 / 120.0);
-    p = fma(p, r, 1.0 / 24.0);
-    p = fma(p, r, 1.0 / 6.0);
-    p = fma(p, r, 0.5);
+// 2^(y + shift) as a whole number, -60 <= y <= 0, 0 <= shift <= 51: 2^n (n next to y) is an exponent, 2^(y - n) the polynomial of degree 10 that agrees with it
+// at the eleven Chebyshev points of [-1/2, 1/2] (off by at most 4e-16; fitted in extended precision).
+__device__ __forceinline__ double exp2_scaled(double y, int shift) {
+    const double magic = 6755399441055744.0;              // 3 * 2^51: the sum's low word is the whole number next to y
+    const double t = y + magic;
+    const double r = y - (t - magic);
+    double p = 7.072582572548229e-09;
+    p = fma(p, r, 1.0208690372639245e-07);
+    p = fma(p, r, 1.3215442609276775e-06);
+    p = fma(p, r, 1.525265725977902e-05);
+    p = fma(p, r, 0.0001540353044168443);
+    p = fma(p, r, 0.0013333558230165855);
+    p = fma(p, r, 0.009618129107606949);
+    p = fma(p, r, 0.05550410866444771);
+    p = fma(p, r, 0.24022650695910097);
+    p = fma(p, r, 0.69314718055995);
     p = fma(p, r, 1.0);
-    p = fma(p, r, 1.0);
-    return ldexp(p, (int)n);
+    return __hiloint2double(__double2hiint(p) + ((__double2loint(t) + shift) << 20), __double2loint(p));
+}
+// exp((x - m) / T) in multiples of 2^-shift; below 2^-60 it is 0 anyhow
+__device__ __forceinline__ uint64_t weight_of(const Sample& a, float x, double m) {
+    const double y = fmax(((double)x - m) * a.c, -60.0);
+    return (uint64_t)__double_as_longlong(exp2_scaled(y, a.shift) + 4503599627370496.0) & 0xfffffffffffffull;
 }
 
-// A column as one workgroup sees it: wavefront w owns the vectors [first, end), row i of them is one vector per lane.  NV rows are held in
-// registers; NV = 0: read again whenever they are needed.
-template <typename T, int NT, int NV>
-struct Held {
+// Where the kept logits end: kept are the ones above, and of equal ones the first `ties`, which have numbers up to `number`.
+struct Cut {
+    float x;
+    uint32_t ties;
+    int32_t number;
+};
+
+template <int NT>
+struct Shared {
+    unsigned long long wave[NT / 64];
+    uint32_t ties[NT / 64];
+    uint64_t table[kTableTiles];
+    double sum[NT / 64];
+    float mx[NT / 64], mn[NT / 64];
+    unsigned long long before, total;
+    uint32_t lo, hi;
+    int32_t pos, n;
+    float x;
+};
+
+// A column as one workgroup sees it.
+template <typename T, int NT>
+struct Column_ {
     static constexpr int V = RawVec<T>::V;
     static constexpr int NW = NT / 64;
     const Sample& a;
+    Shared<NT>& sh;
     Column c;
-    int first, end;
+    bool in_lds;
     float top;              // the column's largest logit (0 where that is +infinity)
     bool top_inf;
-    RawVec<T> x[NV > 0 ? NV : 1];
+    double top64;
 
-    __device__ __forceinline__ Held(const Sample& s, int64_t col) : a(s) {
+    __device__ __forceinline__ Column_(const Sample& s, Shared<NT>& shared, int64_t col) : a(s), sh(shared) {
         c = column_of(s.X, col);
-        const int per = ((s.nvec + NW - 1) / NW + 63) / 64 * 64;
-        first = (int)(threadIdx.x >> 6) * per;
-        end = min(s.nvec, first + per);
+        in_lds = s.X.grid[0] <= kTableTiles;
+        if (in_lds && threadIdx.x < (unsigned)s.X.grid[0])
+            sh.table[threadIdx.x] = reinterpret_cast<uint64_t>(global_as<const T>(s.X.tiles[c.tile0 + threadIdx.x]) + (int64_t)c.colidx * ext0_of(s.X, threadIdx.x));
         top = 0.f;
         top_inf = false;
+        top64 = 0.0;
+    }
+    __device__ __forceinline__ void set_top(float m) {
+        top_inf = m == kPosInf;
+        top = top_inf ? 0.f : m;
+        top64 = (double)top;
     }
     // vector f: its tile (the half keeps the product away from an integer), first element, elements that exist
     __device__ __forceinline__ void place(int f, int& l, int& e, int& cnt) const {
@@ -118,38 +162,50 @@ struct Held {
         e = (f - l * a.vt) * V;
         cnt = ext0_of(a.X, l) - e;
     }
-    __device__ __forceinline__ RawVec<T> read(int f) const {
+    __device__ __forceinline__ RawVec<T> read(int f, int end) const {
         RawVec<T> v;
         v.none();
         if (f < end) {
             int l, e, cnt;
             place(f, l, e, cnt);
-            v.load_or_none(global_as<const T>(a.X.tiles[c.tile0 + l]) + (int64_t)c.colidx * ext0_of(a.X, l) + e, cnt);
+            const T* p = in_lds ? in_global(reinterpret_cast<const T*>(sh.table[l])) : global_as<const T>(a.X.tiles[c.tile0 + l]) + (int64_t)c.colidx * ext0_of(a.X, l);
+            v.load_or_none(p + e, cnt);
         }
         return v;
     }
-    __device__ __forceinline__ void load() {
-        if constexpr (NV > 0) {
-#pragma unroll
-            for (int i = 0; i < NV; i++) x[i] = read(first + 64 * i + (int)(threadIdx.x & 63));
-        }
-    }
-    // fn(vector number, vector) for all rows, in order, by whole wavefronts (the lanes beyond the end hold -inf)
-    template <typename F>
-    __device__ __forceinline__ void rows(F&& fn) const {
+    // fn(vector number, vector) for the vectors [lo, hi), row after row of 64, D rows on their way (the lanes beyond the end hold -inf)
+    template <int D, typename F>
+    __device__ __forceinline__ void rows(int lo, int hi, F&& fn) const {
         const int lane = threadIdx.x & 63;
-        if constexpr (NV > 0) {
+        for (int f = lo; f < hi; f += 64 * D) {
+            RawVec<T> v[D];
 #pragma unroll
-            for (int i = 0; i < NV; i++)
-                if (first + 64 * i < end) fn(first + 64 * i + lane, x[i]);
-        } else {
-            for (int f = first; f < end; f += 64) fn(f + lane, read(f + lane));
+            for (int d = 0; d < D; d++) v[d] = read(f + 64 * d + lane, hi);
+#pragma unroll
+            for (int d = 0; d < D; d++)
+                if (f + 64 * d < hi) fn(f + 64 * d + lane, v[d]);
         }
     }
-    // the logit as it counts: no NaN, no -0, and where there are infinite ones these alone
+    // this wavefront's share of [lo, hi): whole 128-byte lines, consecutive ones
+    __device__ __forceinline__ void share(int lo, int hi, int& first, int& end) const {
+        const int per = ((hi - lo + NW - 1) / NW + 7) / 8 * 8;
+        first = lo + (int)(threadIdx.x >> 6) * per;
+        end = min(hi, first + per);
+    }
+    template <int D, typename F>
+    __device__ __forceinline__ void all_rows(F&& fn) const {
+        int first, end;
+        share(0, a.nvec, first, end);
+        rows<D>(first, end, fn);
+    }
+    // the logit as it counts: where there are infinite ones these alone
     __device__ __forceinline__ float value(const RawVec<T>& v, int j) const {
-        float y = v.at(j) + 0.f;
-        if (top_inf) return y == __builtin_huge_valf() ? 0.f : kNegInf;
+        const float y = v.at(j);
+        return top_inf ? (y == kPosInf ? 0.f : kNegInf) : y;
+    }
+    // ... and as a key: no NaN, no -0
+    __device__ __forceinline__ float clean(const RawVec<T>& v, int j) const {
+        const float y = value(v, j) + 0.f;
         return y != y ? kNegInf : y;
     }
     __device__ __forceinline__ int number(int f, int j) const {
@@ -157,49 +213,18 @@ struct Held {
         place(f, l, e, cnt);
         return l * a.X.base[0] + e + j;
     }
-    __device__ __forceinline__ double weight64(float y) const { return exp64(((double)y - (double)top) * a.inv_t); }
-    // the weight in multiples of 2^-shift
-    __device__ __forceinline__ uint64_t weight(float y) const {
-        const double t = ((double)y - (double)top) * a.inv_t;
-        if (!(t > -40.0)) return 0;
-        return (uint64_t)__double_as_longlong(ldexp(exp64(t), a.shift) + 4503599627370496.0) & 0xfffffffffffffull;
-    }
-};
-
-// Where a prefix of the order ends: kept are the keys above, and of equal ones those with numbers up to `number`.
-struct Cut {
-    uint32_t key;
-    int32_t number;
-    __device__ __forceinline__ bool keeps(uint32_t k, int32_t n) const { return k > key || (k == key && n <= number); }
-};
-
-template <int NW>
-struct Shared {
-    union {
-        struct {
-            unsigned long long mass[kBins];
-            uint32_t count[kBins];
-        } h;
-        unsigned long long list[kList];
-    };
-    unsigned long long wave[NW];
-    double sum[NW];
-    float mx[NW], mn[NW];
-    unsigned long long before, total;
-    uint32_t key, lo, hi;
-    int32_t pos, n;
-    float x;
+    __device__ __forceinline__ uint64_t weight(float y) const { return weight_of(a, y, top64); }
 };
 
 // Over the NT * PER numbers of a workgroup, PER consecutive ones per thread: where their running sum first passes `ends`, and the sum before
 // that place (sh.pos, -1 if nowhere; sh.before).  The sum of all is left in sh.total.
 template <int NT, int PER, typename F>
-__device__ __forceinline__ void find_end(Shared<NT / 64>& sh, const uint64_t (&v)[PER], uint64_t base, F&& ends) {
+__device__ __forceinline__ void find_end(Shared<NT>& sh, const uint64_t (&v)[PER], uint64_t base, F&& ends) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     uint64_t s = 0;
 #pragma unroll
     for (int i = 0; i < PER; i++) s += v[i];
-    const uint64_t scan = wave_scan_u64(s);
+    const uint64_t scan = wave_scan(s);
     __syncthreads();
     if (lane == 63) sh.wave[w] = scan;
     if (threadIdx.x == 0) sh.pos = -1;
@@ -211,7 +236,7 @@ __device__ __forceinline__ void find_end(Shared<NT / 64>& sh, const uint64_t (&v
         all += sh.wave[k];
     }
     if (threadIdx.x == 0) sh.total = all;
-    if (!ends(at, all)) {
+    if (!ends(at, all) && ends(at + s, all)) {
         bool found = false;
 #pragma unroll
         for (int i = 0; i < PER; i++) {
@@ -227,69 +252,248 @@ __device__ __forceinline__ void find_end(Shared<NT / 64>& sh, const uint64_t (&v
     __syncthreads();
 }
 
-// The first number, in the order of the numbers, up to which the weights sum up to more than goal(their total): sh.n (-1: all weights are 0), sh.x its logit.
-template <typename T, int NT, int NV, typename W, typename G>
-__device__ __forceinline__ void locate(const Held<T, NT, NV>& h, Shared<NT / 64>& sh, W&& weight, G&& goal) {
-    constexpr int V = Held<T, NT, NV>::V;
+// The first number, in the order of the numbers, up to which the weights sum up to more than goal(their total): sh.n, sh.x its logit.
+// weigh(vector number, vector, weights) gives the weights of a vector's logits above the border and says (by bits) which are equal to it: of these the first
+// `limit` of the column have the weight `tie`.  Each wavefront sums an equal share of the vectors, the share that holds the place is divided
+// again, until there is one vector per thread.
+template <typename T, int NT, typename W, typename G>
+__device__ __forceinline__ void locate(const Column_<T, NT>& h, uint64_t tie, uint32_t limit, W&& weigh, G&& goal) {
+    constexpr int V = Column_<T, NT>::V, NW = NT / 64;
+    Shared<NT>& sh = h.sh;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    uint64_t s = 0;
-    h.rows([&](int f, const RawVec<T>& v) {
+    int lo = 0, hi = h.a.nvec;
+    uint64_t at = 0, to = 0;
+    uint32_t ties_at = 0;
+    bool first = true;
+    auto kept = [&](uint32_t before, uint32_t n) { return (uint64_t)(before >= limit ? 0u : min(limit - before, n)); };
+    while (hi - lo > NT) {
+        int begin, end;
+        h.share(lo, hi, begin, end);
+        uint64_t s = 0;
+        uint32_t ties = 0;
+        h.template rows<2>(begin, end, [&](int f, const RawVec<T>& v) {
+            uint64_t p[V];
+            ties += __popc(weigh(f, v, p));
 #pragma unroll
-        for (int j = 0; j < V; j++) s += weight(f, j, h.value(v, j));
-    });
-    s = wave_sum_u64(s);
-    __syncthreads();
-    if (lane == 0) sh.wave[w] = s;
-    if (threadIdx.x == 0) sh.n = -1;
-    __syncthreads();
-    uint64_t all = 0;
-#pragma unroll
-    for (int k = 0; k < NT / 64; k++) all += sh.wave[k];
-    const uint64_t to = goal(all);
-    uint64_t at = 0;
-    int winner = -1;
-#pragma unroll
-    for (int k = 0; k < NT / 64; k++)
-        if (winner < 0) {
-            if (at + sh.wave[k] > to) winner = k;
-            else at += sh.wave[k];
+            for (int j = 0; j < V; j++) s += p[j];
+        });
+        s = wave_scan(s);
+        ties = wave_scan(ties);
+        __syncthreads();
+        if (lane == 63) {
+            sh.wave[w] = s;
+            sh.ties[w] = ties;
         }
-    if (w == winner) {
-        bool done = false;
-        h.rows([&](int f, const RawVec<T>& v) {
-            if (done) return;
-            uint64_t p = 0;
+        __syncthreads();
+        if (first) {
+            uint64_t all = 0;
+            uint32_t t = 0;
 #pragma unroll
-            for (int j = 0; j < V; j++) p += weight(f, j, h.value(v, j));
-            const uint64_t scan = wave_scan_u64(p);
-            const uint64_t row = __shfl((unsigned long long)scan, 63, 64);
-            if (at + row > to) {
-                done = true;
-                uint64_t mine = at + scan - p;
-                if (mine <= to && mine + p > to) {
-                    bool found = false;
+            for (int k = 0; k < NW; k++) {
+                all += sh.wave[k] + kept(t, sh.ties[k]) * tie;
+                t += sh.ties[k];
+            }
+            to = goal(all);
+            first = false;
+        }
+        const int per = ((hi - lo + NW - 1) / NW + 7) / 8 * 8;
+        int winner = NW - 1;
 #pragma unroll
-                    for (int j = 0; j < V; j++) {
-                        const float y = h.value(v, j);
-                        mine += weight(f, j, y);
-                        if (!found && mine > to) {
-                            found = true;
-                            sh.n = h.number(f, j);
-                            sh.x = y;
-                        }
-                    }
+        for (int k = 0; k < NW - 1; k++)
+            if (winner == NW - 1) {
+                const uint64_t next = at + sh.wave[k] + kept(ties_at, sh.ties[k]) * tie;
+                if (next > to) {
+                    winner = k;
+                } else {
+                    at = next;
+                    ties_at += sh.ties[k];
                 }
             }
-            at += row;
-        });
+        lo += winner * per;
+        hi = min(hi, lo + per);
+    }
+    uint64_t p[V], s = 0;
+    const int f = lo + (int)threadIdx.x;
+    const RawVec<T> v = h.read(f, hi);
+    const uint32_t equal = weigh(f, v, p);
+#pragma unroll
+    for (int j = 0; j < V; j++) s += p[j];
+    const uint64_t scan = wave_scan(s);
+    const uint32_t ties = wave_scan((uint32_t)__popc(equal));
+    __syncthreads();
+    if (lane == 63) {
+        sh.wave[w] = scan;
+        sh.ties[w] = ties;
+    }
+    if (threadIdx.x == 0) sh.n = -1;
+    __syncthreads();
+    // the sum in front of this thread's vector, its equals counted first
+    uint64_t mine = at + scan - s, all = at;
+    uint32_t t_mine = ties_at + ties - __popc(equal), t_all = ties_at;
+#pragma unroll
+    for (int k = 0; k < NW; k++) {
+        if (k < w) {
+            mine += sh.wave[k];
+            t_mine += sh.ties[k];
+        }
+        all += sh.wave[k];
+        t_all += sh.ties[k];
+    }
+    mine += kept(ties_at, t_mine - ties_at) * tie;
+    if (first) to = goal(all + kept(0, t_all) * tie);
+    const uint64_t end_mine = mine + s + kept(t_mine, __popc(equal)) * tie;
+    if (mine <= to && end_mine > to) {
+        int found = -1;
+        uint32_t t = t_mine;
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+            const bool is_tie = (equal >> j) & 1u;
+            mine += is_tie ? kept(t, 1) * tie : p[j];
+            t += is_tie ? 1 : 0;
+            if (found < 0 && mine > to) {
+                found = j;
+                sh.x = h.value(v, j);
+            }
+        }
+        sh.n = h.number(f, found);
     }
     __syncthreads();
 }
 
+// The c-th (from 0) number whose logit is `x`.
+template <typename T, int NT>
+__device__ __forceinline__ int32_t number_of_equal(const Column_<T, NT>& h, float x, uint64_t c) {
+    locate(h, 1, 0xffffffffu,
+           [&](int, const RawVec<T>& v, uint64_t (&p)[Column_<T, NT>::V]) {
+               uint32_t equal = 0;
+#pragma unroll
+               for (int j = 0; j < Column_<T, NT>::V; j++) {
+                   p[j] = 0;
+                   equal |= h.value(v, j) == x ? 1u << j : 0u;
+               }
+               return equal;
+           },
+           [&](uint64_t) { return c; });
+    return h.sh.n;
+}
+
+// how many of n equal weights w it takes to end a prefix that the sum `before` does not end and all of them do
+template <typename F>
+__device__ __forceinline__ uint64_t how_many(uint64_t before, uint64_t w, uint64_t n, uint64_t all, F&& ends) {
+    uint64_t few = 1, many = n;
+    while (few < many) {
+        const uint64_t c = (few + many) / 2;
+        if (ends(before + c * w, all)) many = c;
+        else few = c + 1;
+    }
+    return few;
+}
+
+// The border with the third filter: nothing too far below the largest logit.
+__device__ __forceinline__ Cut with_least(const Sample& a, float top, Cut cut) {
+    if (a.min_fall < -1e300) return cut;
+    // the largest logit that is too far below
+    const double least = (double)top + a.min_fall;
+    float y = (float)least;
+    if ((double)y >= least) y = nextafterf(y, kNegInf);
+    return y >= cut.x ? Cut{y, 0u, -1} : cut;
+}
+__device__ __forceinline__ uint64_t share_of(float u, uint64_t all) { return (uint64_t)((double)u * (double)all); }
+
+// The draw, once the border is known.
+template <typename T, int NT>
+__device__ __forceinline__ void draw(const Column_<T, NT>& h, Cut cut, float u) {
+    constexpr int V = Column_<T, NT>::V;
+    locate(h, cut.ties ? h.weight(cut.x) : 0, cut.ties,
+           [&](int, const RawVec<T>& v, uint64_t (&p)[V]) {
+               bool any = false;
+               uint32_t equal = 0;
+#pragma unroll
+               for (int j = 0; j < V; j++) {
+                   any = any || h.value(v, j) > cut.x;
+                   equal |= h.value(v, j) == cut.x ? 1u << j : 0u;
+                   p[j] = 0;
+               }
+               if (__any(any)) {
+#pragma unroll
+                   for (int j = 0; j < V; j++) {
+                       const uint64_t w = h.weight(h.value(v, j));
+                       p[j] = h.value(v, j) > cut.x ? w : 0;
+                   }
+               }
+               return equal;
+           },
+           [&](uint64_t all) { return share_of(u, all); });
+}
+
+__device__ __forceinline__ float random_of(const Sample& a) { return fminf(fmaxf(a.uniforms[blockIdx.x], 0.f), 0.99999994f); }
+
+__device__ __forceinline__ void no_token(const Sample& a) {
+    if (threadIdx.x == 0) {
+        a.tokens[blockIdx.x] = -1;
+        if (a.logp) a.logp[blockIdx.x] = 0.f;
+    }
+}
+template <int NT>
+__device__ __forceinline__ void answer(const Sample& a, const Shared<NT>& sh, float top, double sum) {
+    if (threadIdx.x == 0) {
+        a.tokens[blockIdx.x] = sh.n;
+        if (a.logp) a.logp[blockIdx.x] = (float)((double)sh.x - (double)top - log(sum));
+    }
+}
+
+// ---------------------------------------------------------------- any column
+struct Parts {
+    union {
+        struct {
+            unsigned long long mass[kBins];
+            uint32_t count[kBins];
+        } h;
+        unsigned long long list[kList];
+    };
+};
+
+// sorts list[0 .. n) (n <= kList) by rising values
+template <int NT>
+__device__ __forceinline__ void sort_list(unsigned long long* list, int n) {
+    int padded = 64;
+    while (padded < n) padded *= 2;
+    for (int i = n + (int)threadIdx.x; i < padded; i += NT) list[i] = ~0ull;
+    __syncthreads();
+    for (int size = 2; size <= padded; size *= 2)
+        for (int step = size / 2; step > 0; step /= 2) {
+            for (int i = threadIdx.x; i < padded / 2; i += NT) {
+                const int p = 2 * i - (i & (step - 1)), q = p + step;
+                const unsigned long long x = list[p], y = list[q];
+                if ((x > y) == ((p & size) == 0)) {
+                    list[p] = y;
+                    list[q] = x;
+                }
+            }
+            __syncthreads();
+        }
+}
+// the order as a whole number: falling logits, rising numbers
+__device__ __forceinline__ unsigned long long entry_of(uint32_t key, int number) { return ((unsigned long long)~key << 32) | (uint32_t)number; }
+__device__ __forceinline__ float logit_of(unsigned long long entry) { return of_key(~(uint32_t)(entry >> 32)); }
+
+// the border at a place of a sorted list that holds all its equals
+template <int NT>
+__device__ __forceinline__ Cut cut_at(const unsigned long long* list, int pos) {
+    const unsigned long long last = list[pos];
+    uint32_t ties = 0;
+    for (int i = 0; i < kList; i += NT) {
+        const int k = i + (int)threadIdx.x;
+        ties += (uint32_t)__syncthreads_count(k <= pos && (uint32_t)(list[k] >> 32) == (uint32_t)(last >> 32));
+    }
+    return Cut{logit_of(last), ties, (int32_t)(uint32_t)last};
+}
+
 // Moves `cut` to where the prefix ends that `ends(running sum, sum of all kept)` says; `kMass`: sums of weights, else of tokens.
-template <bool kMass, typename T, int NT, int NV, typename F>
-__device__ __forceinline__ void select(const Held<T, NT, NV>& h, Shared<NT / 64>& sh, float range, Cut& cut, F&& ends) {
-    constexpr int V = Held<T, NT, NV>::V, PER = kBins / NT;
+template <bool kMass, typename T, int NT, typename F>
+__device__ __forceinline__ void select(const Column_<T, NT>& h, Parts& sp, float range, Cut& cut, F&& ends) {
+    constexpr int V = Column_<T, NT>::V, PER = kBins / NT;
+    Shared<NT>& sh = h.sh;
     const int tid = threadIdx.x;
     const float scale = range > 0.f ? (float)kBins / range : 0.f;      // (0 too for a range beyond fp32: one part)
     uint32_t lo = 0, hi = 0;                                            // the keys that are looked at, and how they are divided
@@ -299,30 +503,37 @@ __device__ __forceinline__ void select(const Held<T, NT, NV>& h, Shared<NT / 64>
         if (bits < 0) return min(kBins - 1, (int)((h.top - y) * scale));
         return (int)((hi - key) >> bits);
     };
+    // fn(logit, key, number) for what is looked at
+    auto members = [&](auto&& fn) {
+        h.template all_rows<1>([&](int f, const RawVec<T>& v) {
+            const int n0 = h.number(f, 0);
+#pragma unroll
+            for (int j = 0; j < V; j++) {
+                const float y = h.clean(v, j);
+                const uint32_t key = key_of(y);
+                const bool kept = y > old.x || (y == old.x && n0 + j <= old.number);
+                if (y > kNegInf && kept && (bits < 0 || (key >= lo && key <= hi))) fn(y, key, n0 + j);
+            }
+        });
+    };
     uint64_t before = 0, all = 0;
     int n = 0, part = 0;
     for (int level = 0;; level++) {
         __syncthreads();
         for (int i = tid; i < kBins; i += NT) {
-            sh.h.count[i] = 0;
-            sh.h.mass[i] = 0;
+            sp.h.count[i] = 0;
+            sp.h.mass[i] = 0;
         }
         __syncthreads();
-        h.rows([&](int f, const RawVec<T>& v) {
-#pragma unroll
-            for (int j = 0; j < V; j++) {
-                const float y = h.value(v, j);
-                const uint32_t key = key_of(y);
-                if (y == kNegInf || !old.keeps(key, h.number(f, j)) || (bits >= 0 && (key < lo || key > hi))) continue;
-                const int b = part_of(y, key);
-                atomicAdd(&sh.h.count[b], 1u);
-                if (kMass) atomicAdd(&sh.h.mass[b], (unsigned long long)h.weight(y));
-            }
+        members([&](float y, uint32_t key, int) {
+            const int b = part_of(y, key);
+            atomicAdd(&sp.h.count[b], 1u);
+            if (kMass) atomicAdd(&sp.h.mass[b], (unsigned long long)h.weight(y));
         });
         __syncthreads();
         uint64_t v[PER];
 #pragma unroll
-        for (int i = 0; i < PER; i++) v[i] = kMass ? sh.h.mass[tid * PER + i] : sh.h.count[tid * PER + i];
+        for (int i = 0; i < PER; i++) v[i] = kMass ? sp.h.mass[tid * PER + i] : sp.h.count[tid * PER + i];
         if (level == 0) {
             find_end<NT, PER>(sh, v, 0, ends);
             all = sh.total;
@@ -332,7 +543,7 @@ __device__ __forceinline__ void select(const Held<T, NT, NV>& h, Shared<NT / 64>
         part = sh.pos;
         if (part < 0) return;                                           // the prefix is everything
         before = sh.before;
-        n = (int)sh.h.count[part];
+        n = (int)sp.h.count[part];
         if (n <= kList) break;
         // divide again: the keys of this part are a run of all keys
         __syncthreads();
@@ -342,15 +553,10 @@ __device__ __forceinline__ void select(const Held<T, NT, NV>& h, Shared<NT / 64>
         }
         __syncthreads();
         uint32_t kl = 0xffffffffu, kh = 0;
-        h.rows([&](int f, const RawVec<T>& v) {
-#pragma unroll
-            for (int j = 0; j < V; j++) {
-                const float y = h.value(v, j);
-                const uint32_t key = key_of(y);
-                if (y == kNegInf || !old.keeps(key, h.number(f, j)) || (bits >= 0 && (key < lo || key > hi)) || part_of(y, key) != part) continue;
-                kl = min(kl, key);
-                kh = max(kh, key);
-            }
+        members([&](float y, uint32_t key, int) {
+            if (part_of(y, key) != part) return;
+            kl = min(kl, key);
+            kh = max(kh, key);
         });
         if (kl <= kh) {
             atomicMin(&sh.lo, kl);
@@ -360,90 +566,90 @@ __device__ __forceinline__ void select(const Held<T, NT, NV>& h, Shared<NT / 64>
         lo = sh.lo;
         hi = sh.hi;
         if (lo == hi) {
-            // equal logits: the first `c` of them
-            uint64_t c = 1;
-            const uint64_t w = kMass ? h.weight(of_key(lo)) : 1;
-            uint64_t few = 1, many = (uint64_t)n;                       // (the last of them ends the prefix)
-            while (few < many) {
-                c = (few + many) / 2;
-                if (ends(before + c * w, all)) many = c;
-                else few = c + 1;
-            }
-            c = few;
-            locate(h, sh, [&](int f, int j, float y) -> uint64_t { return key_of(y) == lo && old.keeps(lo, h.number(f, j)) ? 1 : 0; },
-                   [&](uint64_t) { return c - 1; });
-            cut = Cut{lo, sh.n};
+            // equal logits: the first `c` of them (none of them has been cut off before, or those that were have the last numbers)
+            const float x = of_key(lo);
+            const uint64_t c = how_many(before, kMass ? h.weight(x) : 1, (uint64_t)n, all, ends);
+            cut = Cut{x, (uint32_t)c, number_of_equal(h, x, c - 1)};
             return;
         }
         bits = max(0, 32 - __clz((int)(hi - lo)) - 11);                  // (2^11 parts)
     }
     // the part fits the list: sort it
     __syncthreads();
-    int padded = 64;
-    while (padded < n) padded *= 2;
-    for (int i = tid; i < padded; i += NT) sh.list[i] = ~0ull;
     if (tid == 0) sh.n = 0;
     __syncthreads();
-    h.rows([&](int f, const RawVec<T>& v) {
-#pragma unroll
-        for (int j = 0; j < V; j++) {
-            const float y = h.value(v, j);
-            const uint32_t key = key_of(y);
-            const int number = h.number(f, j);
-            if (y == kNegInf || !old.keeps(key, number) || (bits >= 0 && (key < lo || key > hi)) || part_of(y, key) != part) continue;
-            sh.list[atomicAdd(&sh.n, 1)] = ((uint64_t)~key << 32) | (uint32_t)number;
-        }
+    members([&](float y, uint32_t key, int number) {
+        if (part_of(y, key) == part) sp.list[atomicAdd(&sh.n, 1)] = entry_of(key, number);
     });
     __syncthreads();
-    for (int size = 2; size <= padded; size *= 2)
-        for (int step = size / 2; step > 0; step /= 2) {
-            for (int i = tid; i < padded / 2; i += NT) {
-                const int p = 2 * i - (i & (step - 1)), q = p + step;
-                const unsigned long long x = sh.list[p], y = sh.list[q];
-                if ((x > y) == ((p & size) == 0)) {
-                    sh.list[p] = y;
-                    sh.list[q] = x;
-                }
-            }
-            __syncthreads();
-        }
+    sort_list<NT>(sp.list, n);
     uint64_t v[kList / NT];
 #pragma unroll
     for (int i = 0; i < kList / NT; i++) {
         const int k = tid * (kList / NT) + i;
-        v[i] = k >= n ? 0 : kMass ? h.weight(of_key(~(uint32_t)(sh.list[k] >> 32))) : 1;
+        v[i] = k >= n ? 0 : kMass ? h.weight(logit_of(sp.list[k])) : 1;
     }
     find_end<NT, kList / NT>(sh, v, before, [&](uint64_t s, uint64_t) { return ends(s, all); });
-    const unsigned long long last = sh.list[max(0, sh.pos)];
-    cut = Cut{~(uint32_t)(last >> 32), (int32_t)(uint32_t)last};
-    __syncthreads();
+    cut = cut_at<NT>(sp.list, max(0, sh.pos));
 }
 
-template <typename T, int NT, int NV>
-__global__ void __launch_bounds__(NT) sample_kernel(Sample a) {
-    constexpr int V = RawVec<T>::V, NW = NT / 64;
-    __shared__ Shared<NW> sh;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int64_t col = a.columns ? a.columns[blockIdx.x] : (int)blockIdx.x;
-    if (col < 0 || col >= a.ncols) {
-        if (tid == 0) {
-            a.tokens[blockIdx.x] = -1;
-            if (a.logp) a.logp[blockIdx.x] = 0.f;
-        }
-        return;
+// top-k by the threads' largest logits (`mine`); the k largest are left sorted in the list.  false: more than a list of candidates.
+template <typename T, int NT>
+__device__ __forceinline__ bool list_top_k(const Column_<T, NT>& h, Parts& sp, float mine, int k, Cut& cut) {
+    constexpr int V = Column_<T, NT>::V;
+    Shared<NT>& sh = h.sh;
+    // the k-th largest of NT numbers, to 20 of its key's bits (a lower one does as well)
+    const uint32_t key = key_of(mine + 0.f);
+    uint32_t least = 0;
+    for (int bit = 31; bit >= 12; bit--) {
+        const uint32_t t = least | (1u << bit);
+        if (__syncthreads_count(key >= t) >= k) least = t;
     }
-    Held<T, NT, NV> h(a, col);
-    h.load();
-    float mx = kNegInf, mn = __builtin_huge_valf();
-    h.rows([&](int, const RawVec<T>& v) {
+    const float bound = fmaxf(of_key(max(least, key_of(kNegInf))), -3.402823466e38f);
+    if (threadIdx.x == 0) sh.n = 0;
+    __syncthreads();
+    h.template all_rows<2>([&](int f, const RawVec<T>& v) {
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < V; j++) any = any || h.value(v, j) >= bound;
+        if (!any) return;
+        const int n0 = h.number(f, 0);
 #pragma unroll
         for (int j = 0; j < V; j++) {
-            const float y = h.value(v, j);
-            mx = fmaxf(mx, y);
+            const float y = h.value(v, j) + 0.f;
+            if (y >= bound) {
+                const int at = atomicAdd(&sh.n, 1);
+                if (at < kList) sp.list[at] = entry_of(key_of(y), n0 + j);
+            }
+        }
+    });
+    __syncthreads();
+    const int n = sh.n;
+    if (n > kList) return false;
+    __syncthreads();
+    sort_list<NT>(sp.list, n);
+    if (n >= k) cut = cut_at<NT>(sp.list, k - 1);
+    sh.n = min(n, k);
+    __syncthreads();
+    return true;
+}
+
+template <typename T, int NT>
+__device__ __forceinline__ void any_column(const Sample& a, Column_<T, NT>& h, Parts& sp) {
+    constexpr int V = RawVec<T>::V, NW = NT / 64;
+    Shared<NT>& sh = h.sh;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    __syncthreads();                                  // the tiles' addresses
+    float mine = kNegInf, mn = kPosInf;
+    h.template all_rows<4>([&](int, const RawVec<T>& v) {
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+            const float y = v.at(j);
+            mine = fmaxf(mine, y);
             if (y > kNegInf) mn = fminf(mn, y);
         }
     });
-    mx = wave_max(mx);
+    float mx = wave_max(mine);
     mn = wave_min(mn);
     if (lane == 0) {
         sh.mx[w] = mx;
@@ -456,50 +662,334 @@ __global__ void __launch_bounds__(NT) sample_kernel(Sample a) {
         mn = fminf(mn, sh.mn[k]);
     }
     if (mx == kNegInf) {
-        if (tid == 0) {
-            a.tokens[blockIdx.x] = -1;
-            if (a.logp) a.logp[blockIdx.x] = 0.f;
-        }
+        no_token(a);
         return;
     }
-    h.top_inf = mx == __builtin_huge_valf();
-    h.top = h.top_inf ? 0.f : mx;
-    if (h.top_inf) mn = 0.f;
+    h.set_top(mx);
+    if (h.top_inf) {
+        mn = 0.f;
+        mine = mine == kPosInf ? 0.f : kNegInf;
+    }
     double sum = 0.0;
     if (a.logp) {
-        h.rows([&](int, const RawVec<T>& v) {
+        const float top = h.top;
+        h.template all_rows<2>([&](int, const RawVec<T>& v) {
             float s = 0.f;
 #pragma unroll
-            for (int j = 0; j < V; j++) s += expf(h.value(v, j) - h.top);
+            for (int j = 0; j < V; j++) s += expf(fmaxf(h.value(v, j), kNegInf) - top);      // (fmaxf: no NaN)
             sum += (double)s;
         });
         sum = wave_sum64(sum);
         if (lane == 0) sh.sum[w] = sum;
     }
+    Cut cut{kNegInf, 0u, -1};
     if (a.greedy) {
-        locate(h, sh, [&](int, int, float y) -> uint64_t { return y == h.top ? 1 : 0; }, [](uint64_t) -> uint64_t { return 0; });
+        cut = Cut{h.top, 1u, INT32_MAX};
     } else {
-        Cut cut{0, INT32_MAX};
         const float range = h.top - mn;
-        if (a.top_k > 0 && a.top_k < a.X.shape[0]) select<false>(h, sh, range, cut, [&](uint64_t s, uint64_t) { return s >= (uint64_t)a.top_k; });
-        if (a.top_p < 1.0) select<true>(h, sh, range, cut, [&](uint64_t s, uint64_t all) { return (double)s >= a.top_p * (double)all; });
-        const float u = fminf(fmaxf(a.uniforms[blockIdx.x], 0.f), 0.99999994f);
-        locate(h, sh,
-               [&](int f, int j, float y) -> uint64_t {
-                   if (y == kNegInf || !cut.keeps(key_of(y), h.number(f, j))) return 0;
-                   if (a.min_p > 0.0 && !(h.weight64(y) >= a.min_p)) return 0;
-                   return h.weight(y);
-               },
-               [&](uint64_t all) -> uint64_t { return (uint64_t)((double)u * (double)all); });
-    }
-    if (tid == 0) {
-        a.tokens[blockIdx.x] = sh.n;
-        if (a.logp) {
-            sum = 0.0;
-            for (int k = 0; k < NW; k++) sum += sh.sum[k];
-            a.logp[blockIdx.x] = (float)((double)sh.x - (double)h.top - log(sum));
+        bool listed = false;
+        if (a.top_k > 0 && a.top_k < a.X.shape[0]) {
+            listed = a.top_k <= NT / 2 && list_top_k(h, sp, mine, a.top_k, cut);
+            if (!listed) select<false>(h, sp, range, cut, [&](uint64_t s, uint64_t) { return s >= (uint64_t)a.top_k; });
+        }
+        if (a.top_p < 1.0) {
+            auto ends = [&](uint64_t s, uint64_t all) { return (double)s >= a.top_p * (double)all; };
+            if (listed) {
+                const int n = sh.n;
+                uint64_t v[1];
+                v[0] = tid < n ? h.weight(logit_of(sp.list[tid])) : 0;
+                find_end<NT, 1>(sh, v, 0, ends);
+                if (sh.pos >= 0) cut = cut_at<NT>(sp.list, sh.pos);
+            } else {
+                select<true>(h, sp, range, cut, ends);
+            }
         }
     }
+    draw(h, a.greedy ? cut : with_least(a, h.top, cut), a.greedy ? 0.f : random_of(a));
+    sum = 0.0;
+    if (a.logp && tid == 0)
+        for (int k = 0; k < NW; k++) sum += sh.sum[k];
+    answer(a, sh, h.top, sum);
+}
+
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT) sample_kernel(Sample a) {
+    __shared__ Shared<NT> sh;
+    __shared__ Parts parts;
+    const int64_t col = a.columns ? a.columns[blockIdx.x] : (int)blockIdx.x;
+    if (col < 0 || col >= a.ncols) {
+        no_token(a);
+        return;
+    }
+    Column_<T, NT> h(a, sh, col);
+    any_column(a, h, parts);
+}
+
+// ---------------------------------------------------------------- bf16 columns, counted
+// A bf16 logit with 2^-8 <= |x| < 2^8 is one of 4096: its exponent and mantissa make a code of 11 bits, the sign the twelfth.  The column is counted by code in
+// LDS, so that weights, sums and borders are those of 4096 (value, count) pairs, in their order (positive codes falling, then negative ones
+// rising), eight to a thread, and the draw looks weights up.  What has no code:
+//   0 is counted by itself; smaller ones, few in logits of any spread, are kept in a list (more than it holds, or a border among them: any_column);
+//   larger negative ones, -infinity and NaN weigh nothing next to a largest logit that has a code (unless T is large: any_column);
+//   larger positive ones: any_column.
+// Two workgroups of 512 share a unit, so that one counts while the other looks for borders.
+constexpr int kCodes = 4096;
+constexpr uint32_t kFirst = 0x3b80u, kSide = 2048u;      // bits of 2^-8, codes of one sign
+constexpr int kSmall = 1024;
+constexpr float kLeastCoded = 0.00390625f, kEndCoded = 256.f;
+struct Codes {
+    uint32_t count[kCodes];
+    unsigned long long weight[kCodes + 1];               // the last: of what has no code
+    uint32_t small[kSmall];                              // bits
+};
+__device__ __forceinline__ float of_bits(uint32_t b) { return __uint_as_float(b << 16); }
+// code of the bits b; without one: some number from kCodes on
+__device__ __forceinline__ uint32_t code_of(uint32_t b, bool& has) {
+    const uint32_t u = (b & 0x7fffu) - kFirst;
+    has = u < kSide;
+    return u + ((b >> 15) << 11);
+}
+__device__ __forceinline__ float of_code(uint32_t k) { return of_bits((k & (kSide - 1)) + kFirst + ((k >> 11) << 15)); }
+
+__global__ void __launch_bounds__(512, 4) sample_codes_kernel(Sample a) {
+    constexpr int NT = 512, V = 8, PER = kCodes / NT, SLOTS = PER + 3;
+    __shared__ Shared<NT> sh;
+    __shared__ union {
+        Codes c;
+        Parts parts;
+    } m;
+    __shared__ uint32_t n_zero, n_small, n_large;
+    __shared__ int least_large;                           // (as an order of whole numbers: the largest of the large negative ones)
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int64_t col = a.columns ? a.columns[blockIdx.x] : (int)blockIdx.x;
+    if (col < 0 || col >= a.ncols) {
+        no_token(a);
+        return;
+    }
+    Column_<bf16_t, NT> h(a, sh, col);
+    for (int i = tid; i < kCodes / 4; i += NT) reinterpret_cast<uint4*>(m.c.count)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (tid == 0) n_zero = n_small = n_large = 0;
+    if (tid == 0) least_large = 0;
+    __syncthreads();
+    h.all_rows<4>([&](int, const RawVec<bf16_t>& v) {
+        uint32_t odd = 0;
+#pragma unroll
+        for (int j = 0; j < V; j++) {
+            const uint32_t b = (j & 1) ? v.x[j >> 1] >> 16 : v.x[j >> 1] & 0xffffu;
+            bool has;
+            const uint32_t k = code_of(b, has);
+            if (has) atomicAdd(&m.c.count[k], 1u);
+            else odd |= 1u << j;
+        }
+        while (odd) {
+            const int j = __ffs((int)odd) - 1;
+            odd &= odd - 1;
+            uint32_t word = v.x[0];
+            if ((j >> 1) == 1) word = v.x[1];
+            if ((j >> 1) == 2) word = v.x[2];
+            if ((j >> 1) == 3) word = v.x[3];
+            const uint32_t b = (word >> (16 * (j & 1))) & 0xffffu, mag = b & 0x7fffu;
+            if (mag == 0) {
+                atomicAdd(&n_zero, 1u);
+            } else if (mag < kFirst) {
+                const uint32_t at = atomicAdd(&n_small, 1u);
+                if (at < (uint32_t)kSmall) m.c.small[at] = b;
+            } else if (mag <= 0x7f80u && b < 0x8000u) {
+                n_large = 1u;
+            } else if (mag < 0x7f80u) {
+                atomicMin(&least_large, -(int)(0x8000u - mag));        // the smallest magnitude
+            }
+        }
+    });
+    __syncthreads();
+    const uint32_t zeros = n_zero, smalls = n_small;
+    // a thread's slots, falling: its codes, and behind the smallest positive ones (thread NT / 2 - 1) the small positive ones, 0 and the small negative ones
+    const bool neg = tid >= NT / 2, middle = tid == NT / 2 - 1;
+    uint32_t cnt[SLOTS];
+    float x[PER];
+    float mine = kNegInf;
+#pragma unroll
+    for (int i = PER - 1; i >= 0; i--) {
+        const uint32_t k = neg ? kSide + (uint32_t)((tid - NT / 2) * PER + i) : kSide - 1 - (uint32_t)(tid * PER + i);
+        cnt[i] = m.c.count[k];
+        x[i] = of_code(k);
+        if (cnt[i]) mine = x[i];
+    }
+    cnt[PER] = cnt[PER + 1] = cnt[PER + 2] = 0;
+    if (zeros && tid == 0) mine = fmaxf(mine, 0.f);
+    uint32_t small_up = 0, small_down = 0;                 // of this thread's entries of the list
+    bool plain = n_large == 0 && smalls <= (uint32_t)kSmall;
+    if (plain && smalls) {
+        for (uint32_t i = tid; i < smalls; i += NT) {
+            const uint32_t b = m.c.small[i];
+            mine = fmaxf(mine, of_bits(b));
+            if (b < 0x8000u) small_up++;
+            else small_down++;
+        }
+    }
+    float top = wave_max(mine);
+    if (lane == 0) sh.mx[w] = top;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NT / 64; k++) top = fmaxf(top, sh.mx[k]);
+    // the large negative ones: at least 256 below 0, and weighing less than 2^-60 of the largest
+    if (least_large != 0) {
+        const double fall = (double)of_bits(0x8000u | (uint32_t)(0x8000 + least_large)) - (double)top;
+        plain = plain && fall * a.c < -60.0 && fall * kLog2e < -60.0;
+    }
+    if (!plain || top == kNegInf) {                        // (nothing but -infinity and NaN: said there)
+        any_column(a, h, m.parts);
+        return;
+    }
+    h.set_top(top);
+    // weights; sums of the small ones, which meet in the middle thread's slots
+    uint64_t wt[SLOTS];
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < PER; i++) {
+        wt[i] = cnt[i] ? h.weight(x[i]) : 0;
+        if (a.logp && cnt[i]) sum += (double)cnt[i] * exp2_scaled(fmax(((double)x[i] - h.top64) * kLog2e, -1000.0), 0);
+    }
+    wt[PER] = wt[PER + 1] = wt[PER + 2] = 0;
+    if (middle && zeros) {
+        cnt[PER + 1] = zeros;
+        wt[PER + 1] = h.weight(0.f);
+        if (a.logp) sum += (double)zeros * exp2_scaled(fmax(-h.top64 * kLog2e, -1000.0), 0);
+    }
+    uint64_t mass_up = 0, mass_down = 0;                   // of all small ones (in the middle thread)
+    if (smalls) {
+        uint64_t up = 0, down = 0;
+        for (uint32_t i = tid; i < smalls; i += NT) {
+            const uint32_t b = m.c.small[i];
+            const float y = of_bits(b);
+            if (b < 0x8000u) up += h.weight(y);
+            else down += h.weight(y);
+            if (a.logp) sum += exp2_scaled(fmax(((double)y - h.top64) * kLog2e, -1000.0), 0);
+        }
+        up = wave_scan(up);
+        down = wave_scan(down);
+        const uint64_t both = wave_scan((uint64_t)small_up | (uint64_t)small_down << 32);
+        __syncthreads();
+        if (tid == 0) sh.before = sh.total = 0;
+        if (tid == 0) sh.wave[0] = 0;
+        __syncthreads();
+        if (lane == 63) {
+            atomicAdd(&sh.before, (unsigned long long)up);
+            atomicAdd(&sh.total, (unsigned long long)down);
+            atomicAdd(&sh.wave[0], (unsigned long long)both);
+        }
+        __syncthreads();
+        if (middle) {
+            cnt[PER] = (uint32_t)sh.wave[0];
+            cnt[PER + 2] = (uint32_t)(sh.wave[0] >> 32);
+            mass_up = sh.before;
+            mass_down = sh.total;
+        }
+        __syncthreads();
+    }
+    if (a.logp) {
+        sum = wave_sum64(sum);
+        if (lane == 0) sh.sum[w] = sum;
+    }
+    Cut cut{kNegInf, 0u, -1};
+    if (a.greedy) {
+        cut = Cut{top, 1u, INT32_MAX};
+    } else {
+        // the border at the place `pos` of the order, of which `c` stay; what is behind it counts no more.  false: among the small ones
+        auto end_at = [&](int pos, uint64_t c) {
+#pragma unroll
+            for (int i = 0; i < SLOTS; i++) {
+                if (tid * SLOTS + i == pos) {
+                    cnt[i] = (uint32_t)c;
+                    sh.x = i < PER ? x[i < PER ? i : 0] : i == PER + 1 ? 0.f : 1e30f;
+                }
+                if (tid * SLOTS + i > pos) cnt[i] = 0;
+            }
+            __syncthreads();
+            cut = Cut{sh.x, (uint32_t)c, -1};
+            return cut.x != 1e30f;
+        };
+        uint64_t v[SLOTS];
+        bool coded = true;
+        if (a.top_k > 0 && a.top_k < a.X.shape[0]) {
+#pragma unroll
+            for (int i = 0; i < SLOTS; i++) v[i] = cnt[i];
+            find_end<NT, SLOTS>(sh, v, 0, [&](uint64_t s, uint64_t) { return s >= (uint64_t)a.top_k; });
+            if (sh.pos >= 0) coded = end_at(sh.pos, (uint64_t)a.top_k - sh.before);
+            __syncthreads();
+        }
+        if (coded && a.top_p < 1.0) {
+            auto ends = [&](uint64_t s, uint64_t all) { return (double)s >= a.top_p * (double)all; };
+#pragma unroll
+            for (int i = 0; i < SLOTS; i++) v[i] = (uint64_t)cnt[i] * wt[i];
+            if (middle) {
+                v[PER] = cnt[PER] ? mass_up : 0;
+                v[PER + 2] = cnt[PER + 2] ? mass_down : 0;
+            }
+            find_end<NT, SLOTS>(sh, v, 0, ends);
+            const int pos = sh.pos;
+            if (pos >= 0) {
+                const uint64_t before = sh.before, all = sh.total;
+#pragma unroll
+                for (int i = 0; i < SLOTS; i++)
+                    if (tid * SLOTS + i == pos) {
+                        // (how many are left of what top-k may have cut)
+                        sh.lo = cnt[i];
+                        sh.wave[0] = wt[i];
+                    }
+                __syncthreads();
+                const uint64_t left = sh.lo, one = sh.wave[0];
+                __syncthreads();
+                coded = end_at(pos, how_many(before, one, left, all, ends));
+            }
+            __syncthreads();
+        }
+        if (!coded) {
+            any_column(a, h, m.parts);
+            return;
+        }
+        cut = with_least(a, top, cut);
+    }
+    // the table: what lies above the border
+#pragma unroll
+    for (int i = 0; i < PER; i++) {
+        const uint32_t k = neg ? kSide + (uint32_t)((tid - NT / 2) * PER + i) : kSide - 1 - (uint32_t)(tid * PER + i);
+        m.c.weight[k] = x[i] > cut.x ? wt[i] : 0;
+    }
+    if (tid == 0) m.c.weight[kCodes] = 0;
+    __syncthreads();
+    const bool tied = cut.ties != 0, small_too = cut.x < kLeastCoded && (smalls || zeros);
+    bool has;
+    const uint32_t border = tied ? code_of(__float_as_uint(cut.x) >> 16, has) : 0xffffffffu;
+    locate(h, tied ? h.weight(cut.x) : 0, cut.ties,
+           [&](int, const RawVec<bf16_t>& v, uint64_t (&p)[V]) {
+               uint32_t equal = 0;
+               bool odd = false;
+#pragma unroll
+               for (int j = 0; j < V; j++) {
+                   const uint32_t b = (j & 1) ? v.x[j >> 1] >> 16 : v.x[j >> 1] & 0xffffu;
+                   bool coded;
+                   const uint32_t k = code_of(b, coded);
+                   p[j] = m.c.weight[coded ? k : kCodes];
+                   equal |= k == border ? 1u << j : 0u;
+                   odd = odd || !coded;
+               }
+               if (small_too && __any(odd)) {
+                   equal = 0;
+#pragma unroll
+                   for (int j = 0; j < V; j++) {
+                       const float y = v.at(j);
+                       if (fabsf(y) < kLeastCoded) p[j] = y > cut.x ? h.weight(y) : 0;
+                       equal |= tied && y == cut.x ? 1u << j : 0u;
+                   }
+               }
+               return equal;
+           },
+           [&](uint64_t all) { return share_of(a.greedy ? 0.f : random_of(a), all); });
+    sum = 0.0;
+    if (a.logp && tid == 0)
+        for (int k = 0; k < NT / 64; k++) sum += sh.sum[k];
+    answer(a, sh, top, sum);
 }
 
 int32_t launched() { return hipGetLastError() == hipSuccess ? (int32_t)NNT_OK : (int32_t)NNT_EHIP; }
@@ -512,9 +1002,9 @@ int32_t launched() { return hipGetLastError() == hipSuccess ? (int32_t)NNT_OK : 
 
 using SampleFn = void (*)(Sample);
 SampleFn sample_instance(int dtype, int64_t nvec, int* nt) {
-    *nt = nvec <= 1024 ? 256 : 1024;
-    if (dtype == NNT_F32) return *nt == 256 ? sample_kernel<float, 256, 0> : sample_kernel<float, 1024, 0>;
-    return *nt == 256 ? sample_kernel<bf16_t, 256, 0> : sample_kernel<bf16_t, 1024, 0>;
+    *nt = nvec <= 1024 ? 256 : dtype == NNT_F32 ? 1024 : 512;
+    if (dtype == NNT_F32) return *nt == 256 ? sample_kernel<float, 256> : sample_kernel<float, 1024>;
+    return *nt == 256 ? sample_kernel<bf16_t, 256> : sample_codes_kernel;
 }
 
 int64_t vectors_of(const nnt_tensor* X, int64_t* vt) {
@@ -558,9 +1048,9 @@ int32_t sample_ordered(nnt_ctx* ctx, const nnt_sample_cfg* cfg, nnt_tensor* X, c
     a.inv_vt = 1.f / (float)vt;
     a.top_k = cfg->top_k;
     a.greedy = cfg->temperature == 0.0;
-    a.inv_t = a.greedy ? 1.0 : std::min(1.0 / cfg->temperature, 1e300);
+    a.c = a.greedy ? kLog2e : std::min(kLog2e / cfg->temperature, 1e200);
     a.top_p = cfg->top_p;
-    a.min_p = cfg->min_p;
+    a.min_fall = a.greedy || cfg->min_p == 0.0 ? -__builtin_huge_val() : cfg->temperature * std::log(cfg->min_p);
     // the sum of a column's weights, 1 at most each, stays below 2^62
     int log_n = 0;
     while (((int64_t)1 << log_n) < X->shape[0]) log_n++;
