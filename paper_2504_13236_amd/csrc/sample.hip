@@ -109,6 +109,9 @@ __device__ __forceinline__ uint64_t weight_of(const Sample& a, float x, double m
     return (uint64_t)__double_as_longlong(exp2_scaled(y, a.shift) + 4503599627370496.0) & 0xfffffffffffffull;
 }
 
+// exp(t), t <= 0, for log-probabilities: both factors of t / ln 2 are kept, else all of them would be too small by the rounding of the first.
+__device__ __forceinline__ float exp_of(float t) { return __builtin_amdgcn_exp2f(fmaf(t, 1.4426950216293335f, t * 1.9259629911e-8f)); }
+
 // Where the kept logits end: kept are the ones above, and of equal ones the first `ties`, which have numbers up to `number`.
 struct Cut {
     float x;
@@ -168,22 +171,41 @@ struct Column_ {
         if (f < end) {
             int l, e, cnt;
             place(f, l, e, cnt);
-            const T* p = in_lds ? in_global(reinterpret_cast<const T*>(sh.table[l])) : global_as<const T>(a.X.tiles[c.tile0 + l]) + (int64_t)c.colidx * ext0_of(a.X, l);
-            v.load_or_none(p + e, cnt);
+            v.load_or_none(tile_of(l) + e, cnt);
         }
         return v;
     }
-    // fn(vector number, vector) for the vectors [lo, hi), row after row of 64, D rows on their way (the lanes beyond the end hold -inf)
+    __device__ __forceinline__ const T* tile_of(int l) const {
+        return in_lds ? in_global(reinterpret_cast<const T*>(sh.table[l])) : global_as<const T>(a.X.tiles[c.tile0 + l]) + (int64_t)c.colidx * ext0_of(a.X, l);
+    }
+    // fn(vector number, vector) for the vectors [lo, hi), tile by tile, row after row of 64, D rows on their way (the lanes beyond the end hold -inf)
     template <int D, typename F>
     __device__ __forceinline__ void rows(int lo, int hi, F&& fn) const {
         const int lane = threadIdx.x & 63;
-        for (int f = lo; f < hi; f += 64 * D) {
-            RawVec<T> v[D];
+        for (int f = lo; f < hi;) {
+            const int l = __builtin_amdgcn_readfirstlane((int)(((float)f + 0.5f) * a.inv_vt));
+            const int first = l * a.vt, end = min(hi, first + a.vt), ext = ext0_of(a.X, l);
+            const int whole = min(end, first + ext / V);               // (a tile's last vector may be short)
+            const T* p = tile_of(l);
+            for (; f < whole; f += 64 * D) {
+                const T* at = p + (f - first + lane) * V;
+                RawVec<T> v[D];
 #pragma unroll
-            for (int d = 0; d < D; d++) v[d] = read(f + 64 * d + lane, hi);
+                for (int d = 0; d < D; d++) {
+                    v[d].none();
+                    if (f + 64 * d + lane < whole) v[d].load(at + 64 * d * V, V);
+                }
 #pragma unroll
-            for (int d = 0; d < D; d++)
-                if (f + 64 * d < hi) fn(f + 64 * d + lane, v[d]);
+                for (int d = 0; d < D; d++)
+                    if (f + 64 * d < whole) fn(f + 64 * d + lane, v[d]);
+            }
+            if (whole < end) {
+                RawVec<T> v;
+                v.none();
+                if (lane == 0) v.load_or_none(p + (whole - first) * V, ext - (whole - first) * V);
+                fn(whole + lane, v);
+            }
+            f = end;
         }
     }
     // this wavefront's share of [lo, hi): whole 128-byte lines, consecutive ones
@@ -216,14 +238,14 @@ struct Column_ {
     __device__ __forceinline__ uint64_t weight(float y) const { return weight_of(a, y, top64); }
 };
 
-// Over the NT * PER numbers of a workgroup, PER consecutive ones per thread: where their running sum first passes `ends`, and the sum before
+// Over the NT * PER numbers of a workgroup, v(0) .. v(PER - 1) of each thread, consecutive ones: where their running sum first passes `ends`, and the sum before
 // that place (sh.pos, -1 if nowhere; sh.before).  The sum of all is left in sh.total.
-template <int NT, int PER, typename F>
-__device__ __forceinline__ void find_end(Shared<NT>& sh, const uint64_t (&v)[PER], uint64_t base, F&& ends) {
+template <int NT, int PER, typename W, typename F>
+__device__ __forceinline__ void find_end(Shared<NT>& sh, uint64_t base, W&& v, F&& ends) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     uint64_t s = 0;
 #pragma unroll
-    for (int i = 0; i < PER; i++) s += v[i];
+    for (int i = 0; i < PER; i++) s += v(i);
     const uint64_t scan = wave_scan(s);
     __syncthreads();
     if (lane == 63) sh.wave[w] = scan;
@@ -240,7 +262,7 @@ __device__ __forceinline__ void find_end(Shared<NT>& sh, const uint64_t (&v)[PER
         bool found = false;
 #pragma unroll
         for (int i = 0; i < PER; i++) {
-            const uint64_t next = at + v[i];
+            const uint64_t next = at + v(i);
             if (!found && ends(next, all)) {
                 found = true;
                 sh.pos = (int)threadIdx.x * PER + i;
@@ -255,9 +277,9 @@ __device__ __forceinline__ void find_end(Shared<NT>& sh, const uint64_t (&v)[PER
 // The first number, in the order of the numbers, up to which the weights sum up to more than goal(their total): sh.n, sh.x its logit.
 // weigh(vector number, vector, weights) gives the weights of a vector's logits above the border and says (by bits) which are equal to it: of these the first
 // `limit` of the column have the weight `tie`.  Each wavefront sums an equal share of the vectors, the share that holds the place is divided
-// again, until there is one vector per thread.
-template <typename T, int NT, typename W, typename G>
-__device__ __forceinline__ void locate(const Column_<T, NT>& h, uint64_t tie, uint32_t limit, W&& weigh, G&& goal) {
+// again, until there is one vector per thread.  add(vector, sum, equals) does what the sums of a share need of it.
+template <int D, typename T, int NT, typename A, typename W, typename G>
+__device__ __forceinline__ void locate_by(const Column_<T, NT>& h, uint64_t tie, uint32_t limit, A&& add, W&& weigh, G&& goal) {
     constexpr int V = Column_<T, NT>::V, NW = NT / 64;
     Shared<NT>& sh = h.sh;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -271,12 +293,7 @@ __device__ __forceinline__ void locate(const Column_<T, NT>& h, uint64_t tie, ui
         h.share(lo, hi, begin, end);
         uint64_t s = 0;
         uint32_t ties = 0;
-        h.template rows<2>(begin, end, [&](int f, const RawVec<T>& v) {
-            uint64_t p[V];
-            ties += __popc(weigh(f, v, p));
-#pragma unroll
-            for (int j = 0; j < V; j++) s += p[j];
-        });
+        h.template rows<D>(begin, end, [&](int, const RawVec<T>& v) { add(v, s, ties); });
         s = wave_scan(s);
         ties = wave_scan(ties);
         __syncthreads();
@@ -315,7 +332,7 @@ __device__ __forceinline__ void locate(const Column_<T, NT>& h, uint64_t tie, ui
     uint64_t p[V], s = 0;
     const int f = lo + (int)threadIdx.x;
     const RawVec<T> v = h.read(f, hi);
-    const uint32_t equal = weigh(f, v, p);
+    const uint32_t equal = weigh(v, p);
 #pragma unroll
     for (int j = 0; j < V; j++) s += p[j];
     const uint64_t scan = wave_scan(s);
@@ -360,14 +377,33 @@ __device__ __forceinline__ void locate(const Column_<T, NT>& h, uint64_t tie, ui
     __syncthreads();
 }
 
+// ... by what `weigh` says
+template <typename T, int NT, typename W, typename G>
+__device__ __forceinline__ void locate(const Column_<T, NT>& h, uint64_t tie, uint32_t limit, W&& weigh, G&& goal) {
+    constexpr int V = Column_<T, NT>::V;
+    locate_by<2>(h, tie, limit,
+           [&](const RawVec<T>& v, uint64_t& s, uint32_t& ties) {
+               uint64_t p[V];
+               ties += __popc(weigh(v, p));
+#pragma unroll
+               for (int j = 0; j < V; j++) s += p[j];
+           },
+           weigh, goal);
+}
+
 // The c-th (from 0) number whose logit is `x`.
 template <typename T, int NT>
 __device__ __forceinline__ int32_t number_of_equal(const Column_<T, NT>& h, float x, uint64_t c) {
-    locate(h, 1, 0xffffffffu,
-           [&](int, const RawVec<T>& v, uint64_t (&p)[Column_<T, NT>::V]) {
+    constexpr int V = Column_<T, NT>::V;
+    locate_by<4>(h, 1, 0xffffffffu,
+           [&](const RawVec<T>& v, uint64_t&, uint32_t& ties) {
+#pragma unroll
+               for (int j = 0; j < V; j++) ties += h.value(v, j) == x ? 1 : 0;
+           },
+           [&](const RawVec<T>& v, uint64_t (&p)[V]) {
                uint32_t equal = 0;
 #pragma unroll
-               for (int j = 0; j < Column_<T, NT>::V; j++) {
+               for (int j = 0; j < V; j++) {
                    p[j] = 0;
                    equal |= h.value(v, j) == x ? 1u << j : 0u;
                }
@@ -405,7 +441,7 @@ template <typename T, int NT>
 __device__ __forceinline__ void draw(const Column_<T, NT>& h, Cut cut, float u) {
     constexpr int V = Column_<T, NT>::V;
     locate(h, cut.ties ? h.weight(cut.x) : 0, cut.ties,
-           [&](int, const RawVec<T>& v, uint64_t (&p)[V]) {
+           [&](const RawVec<T>& v, uint64_t (&p)[V]) {
                bool any = false;
                uint32_t equal = 0;
 #pragma unroll
@@ -507,8 +543,8 @@ __device__ __forceinline__ void select(const Column_<T, NT>& h, Parts& sp, float
     auto members = [&](auto&& fn) {
         h.template all_rows<1>([&](int f, const RawVec<T>& v) {
             const int n0 = h.number(f, 0);
-#pragma unroll
-            for (int j = 0; j < V; j++) {
+#pragma unroll 1
+            for (int j = 0; j < V; j++) {            // (rolled: the calls' bodies are long, and this is the rare way)
                 const float y = h.clean(v, j);
                 const uint32_t key = key_of(y);
                 const bool kept = y > old.x || (y == old.x && n0 + j <= old.number);
@@ -531,14 +567,12 @@ __device__ __forceinline__ void select(const Column_<T, NT>& h, Parts& sp, float
             if (kMass) atomicAdd(&sp.h.mass[b], (unsigned long long)h.weight(y));
         });
         __syncthreads();
-        uint64_t v[PER];
-#pragma unroll
-        for (int i = 0; i < PER; i++) v[i] = kMass ? sp.h.mass[tid * PER + i] : sp.h.count[tid * PER + i];
+        auto v = [&](int i) -> uint64_t { return kMass ? sp.h.mass[tid * PER + i] : sp.h.count[tid * PER + i]; };
         if (level == 0) {
-            find_end<NT, PER>(sh, v, 0, ends);
+            find_end<NT, PER>(sh, 0, v, ends);
             all = sh.total;
         } else {
-            find_end<NT, PER>(sh, v, before, [&](uint64_t s, uint64_t) { return ends(s, all); });
+            find_end<NT, PER>(sh, before, v, [&](uint64_t s, uint64_t) { return ends(s, all); });
         }
         part = sh.pos;
         if (part < 0) return;                                           // the prefix is everything
@@ -583,13 +617,11 @@ __device__ __forceinline__ void select(const Column_<T, NT>& h, Parts& sp, float
     });
     __syncthreads();
     sort_list<NT>(sp.list, n);
-    uint64_t v[kList / NT];
-#pragma unroll
-    for (int i = 0; i < kList / NT; i++) {
+    auto v = [&](int i) -> uint64_t {
         const int k = tid * (kList / NT) + i;
-        v[i] = k >= n ? 0 : kMass ? h.weight(logit_of(sp.list[k])) : 1;
-    }
-    find_end<NT, kList / NT>(sh, v, before, [&](uint64_t s, uint64_t) { return ends(s, all); });
+        return k >= n ? 0 : kMass ? h.weight(logit_of(sp.list[k])) : 1;
+    };
+    find_end<NT, kList / NT>(sh, before, v, [&](uint64_t s, uint64_t) { return ends(s, all); });
     cut = cut_at<NT>(sp.list, max(0, sh.pos));
 }
 
@@ -676,7 +708,7 @@ __device__ __forceinline__ void any_column(const Sample& a, Column_<T, NT>& h, P
         h.template all_rows<2>([&](int, const RawVec<T>& v) {
             float s = 0.f;
 #pragma unroll
-            for (int j = 0; j < V; j++) s += expf(fmaxf(h.value(v, j), kNegInf) - top);      // (fmaxf: no NaN)
+            for (int j = 0; j < V; j++) s += exp_of(fmaxf(h.value(v, j), -3.402823466e38f) - top);      // (no NaN, and no -infinity in two terms)
             sum += (double)s;
         });
         sum = wave_sum64(sum);
@@ -696,9 +728,8 @@ __device__ __forceinline__ void any_column(const Sample& a, Column_<T, NT>& h, P
             auto ends = [&](uint64_t s, uint64_t all) { return (double)s >= a.top_p * (double)all; };
             if (listed) {
                 const int n = sh.n;
-                uint64_t v[1];
-                v[0] = tid < n ? h.weight(logit_of(sp.list[tid])) : 0;
-                find_end<NT, 1>(sh, v, 0, ends);
+                const uint64_t mass = tid < n ? h.weight(logit_of(sp.list[tid])) : 0;
+                find_end<NT, 1>(sh, 0, [&](int) { return mass; }, ends);
                 if (sh.pos >= 0) cut = cut_at<NT>(sp.list, sh.pos);
             } else {
                 select<true>(h, sp, range, cut, ends);
@@ -726,145 +757,82 @@ __global__ void __launch_bounds__(NT) sample_kernel(Sample a) {
 }
 
 // ---------------------------------------------------------------- bf16 columns, counted
-// A bf16 logit with 2^-8 <= |x| < 2^8 is one of 4096: its exponent and mantissa make a code of 11 bits, the sign the twelfth.  The column is counted by code in
-// LDS, so that weights, sums and borders are those of 4096 (value, count) pairs, in their order (positive codes falling, then negative ones
-// rising), eight to a thread, and the draw looks weights up.  What has no code:
+// A bf16 logit with 2^-12 <= |x| < 2^8 is one of 5120: its exponent and mantissa make a code, the sign doubles it.  The column is counted by code in
+// LDS, so that weights, sums and borders are those of 5120 (value, count) pairs, in their order (positive codes falling, then negative ones
+// rising), ten to a thread, and the draw looks weights up.  What has no code:
 //   0 is counted by itself; smaller ones, few in logits of any spread, are kept in a list (more than it holds, or a border among them: any_column);
 //   larger negative ones, -infinity and NaN weigh nothing next to a largest logit that has a code (unless T is large: any_column);
 //   larger positive ones: any_column.
 // Two workgroups of 512 share a unit, so that one counts while the other looks for borders.
-constexpr int kCodes = 4096;
-constexpr uint32_t kFirst = 0x3b80u, kSide = 2048u;      // bits of 2^-8, codes of one sign
-constexpr int kSmall = 1024;
-constexpr float kLeastCoded = 0.00390625f, kEndCoded = 256.f;
+constexpr uint32_t kFirst = 0x3980u, kSide = 2560u;      // bits of 2^-12, codes of one sign
+constexpr int kCodes = 2 * (int)kSide;
+constexpr int kSmall = 512;
+constexpr uint32_t kNegCounts = 4096u;                   // a negative code's count lies here: a bit of its own, above a code that is none (kSide)
+constexpr float kLeastCoded = 0.000244140625f;           // 2^-12
+constexpr int kCodeThreads = 512, kPer = kCodes / kCodeThreads, kSlots = kPer + 3;
 struct Codes {
-    uint32_t count[kCodes];
+    uint32_t count[kNegCounts + kSide + 1];
     unsigned long long weight[kCodes + 1];               // the last: of what has no code
     uint32_t small[kSmall];                              // bits
 };
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ float of_bits(uint32_t b) { return __uint_as_float(b << 16); }
 // code of the bits b; without one: some number from kCodes on
 __device__ __forceinline__ uint32_t code_of(uint32_t b, bool& has) {
     const uint32_t u = (b & 0x7fffu) - kFirst;
     has = u < kSide;
-    return u + ((b >> 15) << 11);
+    return u + (b >> 15) * kSide;
 }
-__device__ __forceinline__ float of_code(uint32_t k) { return of_bits((k & (kSide - 1)) + kFirst + ((k >> 11) << 15)); }
+__device__ __forceinline__ float of_code(uint32_t k) { return k < kSide ? of_bits(k + kFirst) : of_bits(k - kSide + kFirst + 0x8000u); }
 
-__global__ void __launch_bounds__(512, 4) sample_codes_kernel(Sample a) {
-    constexpr int NT = 512, V = 8, PER = kCodes / NT, SLOTS = PER + 3;
-    __shared__ Shared<NT> sh;
-    __shared__ union {
-        Codes c;
-        Parts parts;
-    } m;
-    __shared__ uint32_t n_zero, n_small, n_large;
-    __shared__ int least_large;                           // (as an order of whole numbers: the largest of the large negative ones)
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int64_t col = a.columns ? a.columns[blockIdx.x] : (int)blockIdx.x;
-    if (col < 0 || col >= a.ncols) {
-        no_token(a);
-        return;
-    }
+// The rare way, out of line: its registers are not the counted columns'.
+template <int NT>
+__device__ __attribute__((noinline)) void far_column(const Sample a, int64_t col, Shared<NT>& sh, Parts& parts) {
     Column_<bf16_t, NT> h(a, sh, col);
-    for (int i = tid; i < kCodes / 4; i += NT) reinterpret_cast<uint4*>(m.c.count)[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (tid == 0) n_zero = n_small = n_large = 0;
-    if (tid == 0) least_large = 0;
-    __syncthreads();
-    h.all_rows<4>([&](int, const RawVec<bf16_t>& v) {
-        uint32_t odd = 0;
-#pragma unroll
-        for (int j = 0; j < V; j++) {
-            const uint32_t b = (j & 1) ? v.x[j >> 1] >> 16 : v.x[j >> 1] & 0xffffu;
-            bool has;
-            const uint32_t k = code_of(b, has);
-            if (has) atomicAdd(&m.c.count[k], 1u);
-            else odd |= 1u << j;
-        }
-        while (odd) {
-            const int j = __ffs((int)odd) - 1;
-            odd &= odd - 1;
-            uint32_t word = v.x[0];
-            if ((j >> 1) == 1) word = v.x[1];
-            if ((j >> 1) == 2) word = v.x[2];
-            if ((j >> 1) == 3) word = v.x[3];
-            const uint32_t b = (word >> (16 * (j & 1))) & 0xffffu, mag = b & 0x7fffu;
-            if (mag == 0) {
-                atomicAdd(&n_zero, 1u);
-            } else if (mag < kFirst) {
-                const uint32_t at = atomicAdd(&n_small, 1u);
-                if (at < (uint32_t)kSmall) m.c.small[at] = b;
-            } else if (mag <= 0x7f80u && b < 0x8000u) {
-                n_large = 1u;
-            } else if (mag < 0x7f80u) {
-                atomicMin(&least_large, -(int)(0x8000u - mag));        // the smallest magnitude
-            }
-        }
-    });
-    __syncthreads();
-    const uint32_t zeros = n_zero, smalls = n_small;
-    // a thread's slots, falling: its codes, and behind the smallest positive ones (thread NT / 2 - 1) the small positive ones, 0 and the small negative ones
+    any_column(a, h, parts);
+}
+
+// What is found about a column while it is counted.
+struct CodedColumn {
+    float top;
+    uint32_t zeros, smalls, small_up, small_down;          // the last two: of this thread's entries of the list
+};
+
+// Weights, border and draw.  false: the border lies among the small ones.
+__device__ __forceinline__ bool coded_column(const Sample& a, Column_<bf16_t, kCodeThreads>& h, Codes& m, const CodedColumn& k, uint32_t (&cnt)[kSlots],
+                                             const float (&x)[kPer]) {
+    constexpr int NT = kCodeThreads, V = 8, PER = kPer, SLOTS = kSlots;
+    Shared<NT>& sh = h.sh;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const bool neg = tid >= NT / 2, middle = tid == NT / 2 - 1;
-    uint32_t cnt[SLOTS];
-    float x[PER];
-    float mine = kNegInf;
-#pragma unroll
-    for (int i = PER - 1; i >= 0; i--) {
-        const uint32_t k = neg ? kSide + (uint32_t)((tid - NT / 2) * PER + i) : kSide - 1 - (uint32_t)(tid * PER + i);
-        cnt[i] = m.c.count[k];
-        x[i] = of_code(k);
-        if (cnt[i]) mine = x[i];
-    }
-    cnt[PER] = cnt[PER + 1] = cnt[PER + 2] = 0;
-    if (zeros && tid == 0) mine = fmaxf(mine, 0.f);
-    uint32_t small_up = 0, small_down = 0;                 // of this thread's entries of the list
-    bool plain = n_large == 0 && smalls <= (uint32_t)kSmall;
-    if (plain && smalls) {
-        for (uint32_t i = tid; i < smalls; i += NT) {
-            const uint32_t b = m.c.small[i];
-            mine = fmaxf(mine, of_bits(b));
-            if (b < 0x8000u) small_up++;
-            else small_down++;
-        }
-    }
-    float top = wave_max(mine);
-    if (lane == 0) sh.mx[w] = top;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < NT / 64; k++) top = fmaxf(top, sh.mx[k]);
-    // the large negative ones: at least 256 below 0, and weighing less than 2^-60 of the largest
-    if (least_large != 0) {
-        const double fall = (double)of_bits(0x8000u | (uint32_t)(0x8000 + least_large)) - (double)top;
-        plain = plain && fall * a.c < -60.0 && fall * kLog2e < -60.0;
-    }
-    if (!plain || top == kNegInf) {                        // (nothing but -infinity and NaN: said there)
-        any_column(a, h, m.parts);
-        return;
-    }
+    const float top = k.top;
+    const uint32_t zeros = k.zeros, smalls = k.smalls, small_up = k.small_up, small_down = k.small_down;
     h.set_top(top);
     // weights; sums of the small ones, which meet in the middle thread's slots
     uint64_t wt[SLOTS];
     double sum = 0.0;
+    float part = 0.f;                                      // (ten terms; the threads' sums meet in 64 bits)
 #pragma unroll
     for (int i = 0; i < PER; i++) {
         wt[i] = cnt[i] ? h.weight(x[i]) : 0;
-        if (a.logp && cnt[i]) sum += (double)cnt[i] * exp2_scaled(fmax(((double)x[i] - h.top64) * kLog2e, -1000.0), 0);
+        if (a.logp && cnt[i]) part += (float)cnt[i] * exp_of(x[i] - top);
     }
+    sum = (double)part;
     wt[PER] = wt[PER + 1] = wt[PER + 2] = 0;
     if (middle && zeros) {
         cnt[PER + 1] = zeros;
         wt[PER + 1] = h.weight(0.f);
-        if (a.logp) sum += (double)zeros * exp2_scaled(fmax(-h.top64 * kLog2e, -1000.0), 0);
+        sum += (double)zeros * exp_of(-top);
     }
     uint64_t mass_up = 0, mass_down = 0;                   // of all small ones (in the middle thread)
     if (smalls) {
         uint64_t up = 0, down = 0;
         for (uint32_t i = tid; i < smalls; i += NT) {
-            const uint32_t b = m.c.small[i];
+            const uint32_t b = m.small[i];
             const float y = of_bits(b);
             if (b < 0x8000u) up += h.weight(y);
             else down += h.weight(y);
-            if (a.logp) sum += exp2_scaled(fmax(((double)y - h.top64) * kLog2e, -1000.0), 0);
+            sum += exp_of(y - top);
         }
         up = wave_scan(up);
         down = wave_scan(down);
@@ -909,24 +877,17 @@ __global__ void __launch_bounds__(512, 4) sample_codes_kernel(Sample a) {
             cut = Cut{sh.x, (uint32_t)c, -1};
             return cut.x != 1e30f;
         };
-        uint64_t v[SLOTS];
         bool coded = true;
         if (a.top_k > 0 && a.top_k < a.X.shape[0]) {
-#pragma unroll
-            for (int i = 0; i < SLOTS; i++) v[i] = cnt[i];
-            find_end<NT, SLOTS>(sh, v, 0, [&](uint64_t s, uint64_t) { return s >= (uint64_t)a.top_k; });
+            find_end<NT, SLOTS>(sh, 0, [&](int i) -> uint64_t { return cnt[i]; }, [&](uint64_t s, uint64_t) { return s >= (uint64_t)a.top_k; });
             if (sh.pos >= 0) coded = end_at(sh.pos, (uint64_t)a.top_k - sh.before);
             __syncthreads();
         }
         if (coded && a.top_p < 1.0) {
             auto ends = [&](uint64_t s, uint64_t all) { return (double)s >= a.top_p * (double)all; };
-#pragma unroll
-            for (int i = 0; i < SLOTS; i++) v[i] = (uint64_t)cnt[i] * wt[i];
-            if (middle) {
-                v[PER] = cnt[PER] ? mass_up : 0;
-                v[PER + 2] = cnt[PER + 2] ? mass_down : 0;
-            }
-            find_end<NT, SLOTS>(sh, v, 0, ends);
+            // (the small ones' sums, not one weight of theirs)
+            auto v = [&](int i) -> uint64_t { return i == PER ? (cnt[i] ? mass_up : 0) : i == PER + 2 ? (cnt[i] ? mass_down : 0) : (uint64_t)cnt[i] * wt[i]; };
+            find_end<NT, SLOTS>(sh, 0, v, ends);
             const int pos = sh.pos;
             if (pos >= 0) {
                 const uint64_t before = sh.before, all = sh.total;
@@ -944,52 +905,172 @@ __global__ void __launch_bounds__(512, 4) sample_codes_kernel(Sample a) {
             }
             __syncthreads();
         }
-        if (!coded) {
-            any_column(a, h, m.parts);
-            return;
-        }
+        if (!coded) return false;
         cut = with_least(a, top, cut);
     }
     // the table: what lies above the border
 #pragma unroll
     for (int i = 0; i < PER; i++) {
         const uint32_t k = neg ? kSide + (uint32_t)((tid - NT / 2) * PER + i) : kSide - 1 - (uint32_t)(tid * PER + i);
-        m.c.weight[k] = x[i] > cut.x ? wt[i] : 0;
+        m.weight[k] = x[i] > cut.x ? wt[i] : 0;
     }
-    if (tid == 0) m.c.weight[kCodes] = 0;
+    if (tid == 0) m.weight[kCodes] = 0;
     __syncthreads();
     const bool tied = cut.ties != 0, small_too = cut.x < kLeastCoded && (smalls || zeros);
     bool has;
     const uint32_t border = tied ? code_of(__float_as_uint(cut.x) >> 16, has) : 0xffffffffu;
-    locate(h, tied ? h.weight(cut.x) : 0, cut.ties,
-           [&](int, const RawVec<bf16_t>& v, uint64_t (&p)[V]) {
-               uint32_t equal = 0;
-               bool odd = false;
+    const float u = a.greedy ? 0.f : random_of(a);
+    auto weigh = [&](const RawVec<bf16_t>& v, uint64_t (&p)[V]) {
+        uint32_t equal = 0;
+        bool odd = false;
 #pragma unroll
-               for (int j = 0; j < V; j++) {
-                   const uint32_t b = (j & 1) ? v.x[j >> 1] >> 16 : v.x[j >> 1] & 0xffffu;
-                   bool coded;
-                   const uint32_t k = code_of(b, coded);
-                   p[j] = m.c.weight[coded ? k : kCodes];
-                   equal |= k == border ? 1u << j : 0u;
-                   odd = odd || !coded;
-               }
-               if (small_too && __any(odd)) {
-                   equal = 0;
+        for (int j = 0; j < V; j++) {
+            const uint32_t b = (j & 1) ? v.x[j >> 1] >> 16 : v.x[j >> 1] & 0xffffu;
+            bool coded;
+            const uint32_t k = code_of(b, coded);
+            p[j] = m.weight[coded ? k : kCodes];
+            equal |= k == border ? 1u << j : 0u;
+            odd = odd || !coded;
+        }
+        if (small_too && __any(odd)) {
+            equal = 0;
+#pragma unroll
+            for (int j = 0; j < V; j++) {
+                const float y = v.at(j);
+                if (fabsf(y) < kLeastCoded) p[j] = y > cut.x ? h.weight(y) : 0;
+                equal |= tied && y == cut.x ? 1u << j : 0u;
+            }
+        }
+        return equal;
+    };
+    auto goal = [&](uint64_t all) { return share_of(u, all); };
+    const uint64_t tie = tied ? h.weight(cut.x) : 0;
+    if (cut.x >= kLeastCoded) {
+        // the border has a positive code: kept are the bits from it to the largest logit's
+        const uint32_t lowest = __float_as_uint(cut.x) >> 16, span = (__float_as_uint(top) >> 16) - lowest;
+        const unsigned long long* table = m.weight + (lowest - kFirst);
+        locate_by<4>(h, tie, cut.ties,
+               [&](const RawVec<bf16_t>& v, uint64_t& s, uint32_t& ties) {
 #pragma unroll
                    for (int j = 0; j < V; j++) {
-                       const float y = v.at(j);
-                       if (fabsf(y) < kLeastCoded) p[j] = y > cut.x ? h.weight(y) : 0;
-                       equal |= tied && y == cut.x ? 1u << j : 0u;
+                       const uint32_t t = ((j & 1) ? v.x[j >> 1] >> 16 : v.x[j >> 1] & 0xffffu) - lowest;
+                       if (t <= span) {
+                           s += table[t];
+                           ties += t == 0 && tied;
+                       }
                    }
-               }
-               return equal;
-           },
-           [&](uint64_t all) { return share_of(a.greedy ? 0.f : random_of(a), all); });
+               },
+               weigh, goal);
+    } else {
+        locate(h, tie, cut.ties, weigh, goal);
+    }
     sum = 0.0;
     if (a.logp && tid == 0)
         for (int k = 0; k < NT / 64; k++) sum += sh.sum[k];
     answer(a, sh, top, sum);
+    return true;
+}
+
+__global__ void __launch_bounds__(512, 4) sample_codes_kernel(Sample a) {
+    constexpr int NT = kCodeThreads, V = 8, PER = kPer, SLOTS = kSlots;
+    __shared__ Shared<NT> sh;
+    __shared__ union {
+        Codes c;
+        Parts parts;
+    } m;
+    __shared__ uint32_t n_zero, n_small, n_large;
+    __shared__ int least_large;                           // (as an order of whole numbers: the largest of the large negative ones)
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int64_t col = a.columns ? a.columns[blockIdx.x] : (int)blockIdx.x;
+    if (col < 0 || col >= a.ncols) {
+        no_token(a);
+        return;
+    }
+    Column_<bf16_t, NT> h(a, sh, col);
+    for (int i = tid; i < (int)kSide / 4; i += NT) {
+        reinterpret_cast<uint4*>(m.c.count)[i] = make_uint4(0u, 0u, 0u, 0u);
+        reinterpret_cast<uint4*>(m.c.count + kNegCounts)[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (tid == 0) n_zero = n_small = n_large = 0;
+    if (tid == 0) least_large = 0;
+    __syncthreads();
+    h.all_rows<4>([&](int, const RawVec<bf16_t>& v) {
+        // two logits of a word at a time: what has no code counts in a place that nobody reads
+        u16x2 most = {0, 0};
+        uint32_t magnitude[V / 2];
+#pragma unroll
+        for (int k = 0; k < V / 2; k++) {
+            const u16x2 u = __builtin_bit_cast(u16x2, v.x[k] & 0x7fff7fffu) - u16x2{(uint16_t)kFirst, (uint16_t)kFirst};
+            const u16x2 code = __builtin_elementwise_min(u, u16x2{(uint16_t)kSide, (uint16_t)kSide});
+            most = __builtin_elementwise_max(most, code);
+            magnitude[k] = __builtin_bit_cast(uint32_t, code);
+            const uint32_t at = ((v.x[k] >> 3) & 0x10001000u) | magnitude[k];
+            atomicAdd(&m.c.count[at & 0xffffu], 1u);
+            atomicAdd(&m.c.count[at >> 16], 1u);
+        }
+        if (most[0] < kSide && most[1] < kSide) return;
+        uint32_t odd = 0;
+#pragma unroll
+        for (int j = 0; j < V; j++)
+            odd |= ((j & 1) ? magnitude[j >> 1] >> 16 : magnitude[j >> 1] & 0xffffu) >= kSide ? 1u << j : 0u;
+        while (odd) {
+            const int j = __ffs((int)odd) - 1;
+            odd &= odd - 1;
+            uint32_t word = v.x[0];
+            if ((j >> 1) == 1) word = v.x[1];
+            if ((j >> 1) == 2) word = v.x[2];
+            if ((j >> 1) == 3) word = v.x[3];
+            const uint32_t b = (word >> (16 * (j & 1))) & 0xffffu, mag = b & 0x7fffu;
+            if (mag == 0) {
+                atomicAdd(&n_zero, 1u);
+            } else if (mag < kFirst) {
+                const uint32_t at = atomicAdd(&n_small, 1u);
+                if (at < (uint32_t)kSmall) m.c.small[at] = b;
+            } else if (mag <= 0x7f80u && b < 0x8000u) {
+                n_large = 1u;
+            } else if (mag < 0x7f80u) {
+                atomicMin(&least_large, -(int)(0x8000u - mag));        // the smallest magnitude
+            }
+        }
+    });
+    __syncthreads();
+    const uint32_t zeros = n_zero, smalls = n_small;
+    // a thread's slots, falling: its codes, and behind the smallest positive ones (thread NT / 2 - 1) the small positive ones, 0 and the small negative ones
+    const bool neg = tid >= NT / 2, middle = tid == NT / 2 - 1;
+    uint32_t cnt[SLOTS];
+    float x[PER];
+    float mine = kNegInf;
+#pragma unroll
+    for (int i = PER - 1; i >= 0; i--) {
+        const uint32_t k = neg ? kSide + (uint32_t)((tid - NT / 2) * PER + i) : kSide - 1 - (uint32_t)(tid * PER + i);
+        cnt[i] = m.c.count[neg ? k + (kNegCounts - kSide) : k];
+        x[i] = of_code(k);
+        if (cnt[i]) mine = x[i];
+    }
+    cnt[PER] = cnt[PER + 1] = cnt[PER + 2] = 0;
+    if (zeros && tid == 0) mine = fmaxf(mine, 0.f);
+    uint32_t small_up = 0, small_down = 0;                 // of this thread's entries of the list
+    bool plain = n_large == 0 && smalls <= (uint32_t)kSmall;
+    if (plain && smalls) {
+        for (uint32_t i = tid; i < smalls; i += NT) {
+            const uint32_t b = m.c.small[i];
+            mine = fmaxf(mine, of_bits(b));
+            if (b < 0x8000u) small_up++;
+            else small_down++;
+        }
+    }
+    float top = wave_max(mine);
+    if (lane == 0) sh.mx[w] = top;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NT / 64; k++) top = fmaxf(top, sh.mx[k]);
+    // the large negative ones: at least 256 below 0, and weighing less than 2^-60 of the largest
+    if (least_large != 0) {
+        const double fall = (double)of_bits(0x8000u | (uint32_t)(0x8000 + least_large)) - (double)top;
+        plain = plain && fall * a.c < -60.0 && fall * kLog2e < -60.0;
+    }
+    if (plain && top > kNegInf && coded_column(a, h, m.c, CodedColumn{top, zeros, smalls, small_up, small_down}, cnt, x)) return;
+    far_column<NT>(a, col, sh, m.parts);                   // (nothing but -infinity and NaN: said there)
 }
 
 int32_t launched() { return hipGetLastError() == hipSuccess ? (int32_t)NNT_OK : (int32_t)NNT_EHIP; }
