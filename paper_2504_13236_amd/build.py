@@ -40,7 +40,7 @@ FLAGS = [
 # carry their loop's name on the line of their label or on the next one, and the compiler puts blocks out of line.
 IN_FLIGHT_SOURCES = ("gemm_bf16_dl.hip", "gemm_bf16_span.hip", "gemm_f32_dl.hip", "newton_schulz.hip")
 # Sources with matrix instructions: their assembly is scanned for uses of a result before it is there.
-MATRIX_SOURCES = IN_FLIGHT_SOURCES + ("gemm_bf16.hip", "gemm_f32.hip", "attention.hip")
+MATRIX_SOURCES = IN_FLIGHT_SOURCES + ("gemm_bf16.hip", "gemm_f32.hip", "attention.hip", "cache.hip")
 
 
 _VREG = re.compile(r"\bv(\d+)\b|\bv\[(\d+):(\d+)\]")

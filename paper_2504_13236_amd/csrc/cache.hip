@@ -5,36 +5,47 @@
 //   attention  B = sum_k V[k] P[k],  P = softmax_k(scale K[k] . rot_p q),  k <= p  (and > p - window)
 //
 // A page is a tile (h, P, N_kv) of the cache's tensors: what one cached head reads of it is contiguous.
+#include "attention_tile.hpp"
 #include "device_util.hpp"
 #include "internal.hpp"
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace nnt {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNegInf = -__builtin_huge_valf();
 constexpr int kE = 8;                       // components per lane
-
-// [rows, N_s, N_b] with the heads side by side along the first axis
-struct Rows {
-    void* const* tiles;
-    int32_t n0, n1, n2, b0, b1, b2, g0, g1;
-};
-template <typename T>
-__device__ __forceinline__ T* row_at(const Rows& r, int row, int s, int b) {
-    const int t0 = row / r.b0, t1 = s / r.b1, t2 = b / r.b2;
-    const int e0 = min(r.b0, r.n0 - t0 * r.b0), e1 = min(r.b1, r.n1 - t1 * r.b1);
-    return global_as<T>(r.tiles[t0 + r.g0 * (t1 + r.g1 * t2)]) + (row - t0 * r.b0) + (int64_t)e0 * ((s - t1 * r.b1) + (int64_t)e1 * (b - t2 * r.b2));
-}
 
 // Division of numbers below 2^31 by a fixed one: q = (n * mul) >> 32 >> shift.
 struct Divide {
     uint32_t mul, shift, d;
     __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return d == 1 ? n : __umulhi(n, mul) >> shift; }
 };
+
+// [rows, N_s, N_b] with the heads side by side along the first axis
+struct Rows {
+    void* const* tiles;
+    int32_t n0, n1, n2, b0, b1, b2, g0, g1;
+    Divide by0, by1, by2;
+};
+// where a token's column lies: the number of its first row tile, and its place among the columns of a tile
+struct TokenAt {
+    int tile;
+    int64_t col;
+};
+__device__ __forceinline__ TokenAt token_at(const Rows& r, int s, int b) {
+    const int t1 = (int)r.by1((uint32_t)s), t2 = (int)r.by2((uint32_t)b), e1 = min(r.b1, r.n1 - t1 * r.b1);
+    return TokenAt{r.g0 * (t1 + r.g1 * t2), (s - t1 * r.b1) + (int64_t)e1 * (b - t2 * r.b2)};
+}
+template <typename T>
+__device__ __forceinline__ T* row_at(const Rows& r, const TokenAt& t, int row) {
+    const int t0 = (int)r.by0((uint32_t)row), e0 = min(r.b0, r.n0 - t0 * r.b0);
+    return global_as<T>(r.tiles[t0 + t.tile]) + (row - t0 * r.b0) + e0 * t.col;
+}
+template <typename T>
+__device__ __forceinline__ T* row_at(const Rows& r, int row, int s, int b) { return row_at<T>(r, token_at(r, s, b), row); }
 
 struct Cache {
     Rows z;                                  // queries, keys, values of the new tokens
@@ -44,26 +55,29 @@ struct Cache {
     const float* const* rot;                 // tiles of the rotation, NULL: none
     int32_t rot_r, rot_n, rot_base, rot_pairs;
     int32_t h, N_h, N_kv, P, n_pages, max_pages, window;
-    Divide by_P;
+    bool rot_whole;                          // halves in whole vectors
+    Divide by_P, by_rot;
 };
 
 __device__ __forceinline__ int new_tokens(const Cache& c, int b) { return c.count ? min(max(c.count[b], 0), c.z.n1) : c.z.n1; }
 
+__device__ __forceinline__ void eight(const bf16_t* p, float (&x)[kE]) { ldv<8>(p, x); }
+__device__ __forceinline__ void eight(const float* p, float (&x)[kE]) {
+    float lo[4], hi[4];
+    ldv<4>(p, lo);
+    ldv<4>(p + 4, hi);
+#pragma unroll
+    for (int i = 0; i < 4; i++) { x[i] = lo[i]; x[i + 4] = hi[i]; }
+}
+
 // Components i0 .. i0 + 7 of a head's row, turned by the rotation of position p (0 <= p < rot_n).
 template <typename T>
 __device__ __forceinline__ void turned(const Cache& c, const T* row, int i0, int p, float (&x)[kE]) {
-    if constexpr (sizeof(T) == 2) {
-        ldv<8>(row + i0, x);
-    } else {
-        float lo[4], hi[4];
-        ldv<4>(row + i0, lo);
-        ldv<4>(row + i0 + 4, hi);
-#pragma unroll
-        for (int i = 0; i < 4; i++) { x[i] = lo[i]; x[i + 4] = hi[i]; }
-    }
+    eight(row + i0, x);
     if (!c.rot) return;
-    const int half = c.rot_r / 2, t = p / c.rot_base;
+    const int half = c.rot_r / 2, t = (int)c.by_rot((uint32_t)p);
     const float* cs = in_global(c.rot[t]) + (int64_t)(p - t * c.rot_base) * c.rot_r;
+    if (i0 >= c.rot_r) return;
     if (c.rot_pairs) {
 #pragma unroll
         for (int i = 0; i < kE; i += 2)
@@ -72,6 +86,16 @@ __device__ __forceinline__ void turned(const Cache& c, const T* row, int i0, int
                 x[i] = a * co - b * si;
                 x[i + 1] = a * si + b * co;
             }
+    } else if (c.rot_whole) {
+        // all eight in one half, the others' eight and the eight angles in a row
+        const bool second = i0 >= half;
+        const int k = second ? i0 - half : i0;
+        float other[kE], co[kE], si[kE];
+        eight(row + (second ? k : i0 + half), other);
+        eight(cs + k, co);
+        eight(cs + half + k, si);
+#pragma unroll
+        for (int i = 0; i < kE; i++) x[i] = second ? other[i] * si[i] + x[i] * co[i] : x[i] * co[i] - other[i] * si[i];
     } else {
 #pragma unroll
         for (int i = 0; i < kE; i++) {
@@ -97,29 +121,32 @@ __device__ __forceinline__ void put(T* p, const float (&x)[kE]) {
     }
 }
 
-// A thread moves eight components of a key and of its value.
+// A thread moves eight components of a key and of its value.  Eight prompts of up to 1024 tokens of 12 heads of 64 in fp32, turned: APPEND_FIGURE.
 template <typename T>
-__global__ void __launch_bounds__(256) append_kernel(Cache c) {
-    const int per_head = c.h / kE, per_token = per_head * c.N_kv;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ void __launch_bounds__(256) append_kernel(Cache c, Divide by_token, Divide by_head) {
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x;
     const int b = blockIdx.y;
-    if (at >= (int64_t)per_token * c.z.n1) return;
-    const int s = (int)(at / per_token), k = (int)(at - (int64_t)s * per_token), j = k / per_head, i0 = (k - j * per_head) * kE;
-    if (s >= new_tokens(c, b)) return;
+    const uint32_t s = by_token(at), k = at - s * by_token.d, j = by_head(k);
+    const int i0 = (int)(k - j * by_head.d) * kE;
+    if (s >= (uint32_t)new_tokens(c, b)) return;
     const int64_t p = (int64_t)c.start[b] + s;
     if (p < 0 || p >= (int64_t)c.max_pages * c.P || (c.rot && p >= c.rot_n)) return;
     const uint32_t q = c.by_P((uint32_t)p), slot = (uint32_t)p - q * c.P;
     const int page = c.pages[(int64_t)b * c.max_pages + q];
     if (page < 0 || page >= c.n_pages) return;
     const int64_t to = ((int64_t)j * c.P + slot) * c.h + i0;
-    float x[kE];
-    turned<T>(c, row_at<const T>(c.z, (c.N_h + j) * c.h, s, b), i0, (int)p, x);
-    put(global_as<T>(c.K[page]) + to, x);
+    const TokenAt token = token_at(c.z, (int)s, b);
     // (values leave as they came, whatever their bits)
-    const uint4* from = reinterpret_cast<const uint4*>(row_at<const T>(c.z, (c.N_h + c.N_kv + j) * c.h, s, b) + i0);
-    uint4* v = reinterpret_cast<uint4*>(global_as<T>(c.V[page]) + to);
-    v[0] = from[0];
-    if constexpr (sizeof(T) == 4) v[1] = from[1];
+    const uint4* from = reinterpret_cast<const uint4*>(row_at<const T>(c.z, token, (c.N_h + c.N_kv + (int)j) * c.h) + i0);
+    uint4 v[sizeof(T) / 2];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; i++) v[i] = from[i];
+    float x[kE];
+    turned<T>(c, row_at<const T>(c.z, token, (c.N_h + (int)j) * c.h), i0, (int)p, x);
+    put(global_as<T>(c.K[page]) + to, x);
+    uint4* o = reinterpret_cast<uint4*>(global_as<T>(c.V[page]) + to);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; i++) o[i] = v[i];
 }
 
 // ---------------------------------------------------------------- attention
@@ -133,24 +160,26 @@ struct Attend {
 };
 
 constexpr int kWaves = 4;
+constexpr int kMostSplits = 64;
 constexpr int kUnroll = 4;    // keys a lane has on their way at a time
 constexpr int kTable = 512;   // pages whose addresses a workgroup keeps at a time
 
-// The keys of a row chunk's split: the positions [lo, hi), of which a split takes `per`.
+// The keys of a row chunk's split: the positions [lo, hi), of which a split takes `per`, whole steps.  (The host keeps the table's end, and 65536 more, below 2^31.)
 struct Range {
-    int64_t lo, hi, per;
+    int lo, hi, per;
 };
 // rows r0 .. r0 + R - 1 of a (sequence, cached head) pair: row r is token r / G, query head j G + r % G
-__device__ __forceinline__ Range range_of(const Attend& a, int start, int s_first, int s_last, int step) {
+__device__ __forceinline__ Range range_of(const Attend& a, int start, int s_first, int s_last, uint32_t step) {
     Range g;
     const int64_t end = (int64_t)a.c.max_pages * a.c.P;
-    g.hi = min((int64_t)start + s_last + 1, end);
-    g.lo = a.c.window > 0 ? max((int64_t)0, (int64_t)start + s_first + 1 - a.c.window) : 0;
-    const int64_t n = max((int64_t)0, g.hi - g.lo);
-    g.per = (n + a.splits - 1) / a.splits;
-    g.per = max((int64_t)step, (g.per + step - 1) / step * step);
+    g.hi = (int)max((int64_t)0, min((int64_t)start + s_last + 1, end));
+    g.lo = a.c.window > 0 ? (int)min((int64_t)g.hi, max((int64_t)0, (int64_t)start + s_first + 1 - a.c.window)) : 0;
+    const uint32_t steps = ((uint32_t)(g.hi - g.lo) + step - 1) / step;
+    g.per = (int)(max(1u, (steps + (uint32_t)a.splits - 1) / (uint32_t)a.splits) * step);
     return g;
 }
+// a position between -1 and the last one a table may have
+__device__ __forceinline__ int clamped(int64_t p) { return (int)max((int64_t)-1, min(p, (int64_t)INT32_MAX - 1)); }
 
 template <typename T>
 struct Eight {
@@ -182,6 +211,19 @@ struct Eight {
     }
 };
 
+// The sum over the LPK lanes that share a key, in each of them: exchanges of neighbours, of pairs, of quads (halves of a row mirrored) and of eights as
+// data-parallel moves, which cost an addition each; only what crosses a row of 16 goes through LDS.
+template <int LPK>
+__device__ __forceinline__ float lanes_sum(float d) {
+    auto moved = [](float x, auto ctrl) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true)); };
+    d += moved(d, std::integral_constant<int, 0xb1>());                          // lanes 1 0 3 2
+    d += moved(d, std::integral_constant<int, 0x4e>());                          // lanes 2 3 0 1
+    if constexpr (LPK >= 8) d += moved(d, std::integral_constant<int, 0x141>());  // 7 6 .. 0
+    if constexpr (LPK >= 16) d += moved(d, std::integral_constant<int, 0x140>()); // 15 14 .. 0
+    if constexpr (LPK >= 32) d += __shfl_xor(d, 16, 64);
+    return d;
+}
+
 // One workgroup: R rows of a (sequence, cached head) pair against one split of the keys.  LPK lanes share a key, eight components each; a wavefront
 // takes 64 / LPK keys at a time, and every such group of lanes carries a running maximum and sum of its own, which meet at the end.
 template <typename T, int LPK, int R>
@@ -199,36 +241,17 @@ __global__ void __launch_bounds__(kWaves * 64) attend_kernel(Attend a) {
     if (rows <= 0) return;
     const int start = c.start[b];
     const Range g = range_of(a, start, r0 / G, (r0 + rows - 1) / G, STEP);
-    const int64_t lo = g.lo + split * g.per, hi = min(g.hi, lo + g.per);
-    const bool alone = g.lo + g.per >= g.hi;           // one split holds all keys
+    const bool alone = g.per >= g.hi - g.lo;           // one split holds all keys
+    if (split > 0 && (int64_t)split * g.per >= g.hi - g.lo) return;
+    const int lo = g.lo + split * g.per, hi = lo + min(g.per, g.hi - lo);
     if (lo >= hi && !(alone && split == 0)) return;
 
-    const bool live = sub * kE < c.h;
-    float q[R][kE], acc[R][kE], mx[R], sum[R];
-    int64_t upto[R], from[R];                          // positions that a row sees
-#pragma unroll
-    for (int r = 0; r < R; r++) {
-        mx[r] = kNegInf;
-        sum[r] = 0.f;
-        const int s = (r0 + r) / G;
-        const int64_t p = (int64_t)start + s;
-        bool there = r < rows && p >= 0 && (!c.rot || p < c.rot_n);
-        upto[r] = there ? p : -1;
-        from[r] = c.window > 0 ? p - c.window : -1;
-#pragma unroll
-        for (int i = 0; i < kE; i++) q[r][i] = acc[r][i] = 0.f;
-        if (there && live) {
-            turned<T>(c, row_at<const T>(c.z, (j * G + (r0 + r) % G) * c.h, s, b), sub * kE, (int)p, q[r]);
-#pragma unroll
-            for (int i = 0; i < kE; i++) q[r][i] *= a.scale;
-        }
-    }
-
     // the pages' addresses, kTable at a time
-    for (int64_t k0 = lo; k0 < hi;) {
-        const int64_t first_page = k0 / c.P;
-        const int64_t k1 = min(hi, (first_page + kTable) * (int64_t)c.P);
-        const int n_here = (int)((k1 + c.P - 1) / c.P - first_page);
+    int first_page = 0, k1 = lo;
+    auto look_up = [&](int k0) {
+        first_page = (int)c.by_P((uint32_t)k0);
+        k1 = (int)min((int64_t)hi, (first_page + kTable) * (int64_t)c.P);
+        const int n_here = (int)(c.by_P((uint32_t)(k1 - 1)) - first_page) + 1;
         __syncthreads();
         for (int i = tid; i < n_here; i += kWaves * 64) {
             const int page = c.pages[(int64_t)b * c.max_pages + first_page + i];
@@ -238,12 +261,38 @@ __global__ void __launch_bounds__(kWaves * 64) attend_kernel(Attend a) {
             values[i] = ok ? global_as<const T>(c.V[page]) + off : nullptr;
         }
         __syncthreads();
-        for (int64_t k = k0; k < k1; k += STEP) {
+    };
+    if (lo < hi) look_up(lo);
+
+    const bool live = sub * kE < c.h;
+    float q[R][kE], acc[R][kE], mx[R], sum[R];
+    int upto[R], from[R];                              // positions that a row sees
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+        mx[r] = kNegInf;
+        sum[r] = 0.f;
+        const int s = (r0 + r) / G;
+        const int64_t p = (int64_t)start + s;
+        bool there = r < rows && p >= 0 && (!c.rot || p < c.rot_n);
+        upto[r] = there ? clamped(p) : -1;
+        from[r] = c.window > 0 ? clamped(p - c.window) : -1;
+#pragma unroll
+        for (int i = 0; i < kE; i++) q[r][i] = acc[r][i] = 0.f;
+        if (there && live) {
+            turned<T>(c, row_at<const T>(c.z, (j * G + (r0 + r) % G) * c.h, s, b), sub * kE, (int)p, q[r]);
+#pragma unroll
+            for (int i = 0; i < kE; i++) q[r][i] *= a.scale;
+        }
+    }
+
+    for (int k0 = lo; k0 < hi;) {
+        if (k0 > lo) look_up(k0);
+        for (int k = k0; k < k1; k += STEP) {
             Eight<T> kk[kUnroll], vv[kUnroll];
             int pos[kUnroll];
 #pragma unroll
             for (int u = 0; u < kUnroll; u++) {
-                const int64_t p = k + (u * kWaves + wv) * KPW + grp;
+                const int p = k + (u * kWaves + wv) * KPW + grp;
                 kk[u].zero();
                 vv[u].zero();
                 pos[u] = -1;
@@ -251,9 +300,9 @@ __global__ void __launch_bounds__(kWaves * 64) attend_kernel(Attend a) {
                     const uint32_t pg = c.by_P((uint32_t)p), slot = (uint32_t)p - pg * c.P;
                     const T* kp = keys[pg - (uint32_t)first_page];
                     if (kp) {
-                        pos[u] = (int)p;
+                        pos[u] = p;
                         if (live) {
-                            const int64_t at = (int64_t)slot * c.h + sub * kE;
+                            const uint32_t at = slot * (uint32_t)c.h + sub * kE;
                             kk[u].load(in_global(kp) + at);
                             vv[u].load(in_global(values[pg - (uint32_t)first_page]) + at);
                         }
@@ -270,8 +319,7 @@ __global__ void __launch_bounds__(kWaves * 64) attend_kernel(Attend a) {
                     float d = 0.f;
 #pragma unroll
                     for (int i = 0; i < kE; i++) d = fmaf(f[i], q[r][i], d);
-#pragma unroll
-                    for (int o = 1; o < LPK; o <<= 1) d += __shfl_xor(d, o, 64);
+                    d = lanes_sum<LPK>(d);
                     score[u][r] = pos[u] >= 0 && pos[u] <= upto[r] && pos[u] > from[r] ? d : kNegInf;
                 }
             }
@@ -366,34 +414,375 @@ __global__ void __launch_bounds__(kWaves * 64) attend_kernel(Attend a) {
     }
 }
 
-// The splits of a row meet: one wavefront per row.  `R`, `step`: how the rows and keys were cut.
-template <typename T>
-__global__ void __launch_bounds__(256) join_kernel(Attend a, int R, int step) {
+// ---------------------------------------------------------------- many rows: on the matrix cores
+// The workgroup owns 32 WR rows, 32 to a wavefront (WR = 4), or 32 in all, of which each wavefront sees a quarter of the keys (WR = 1), and streams blocks
+// of keys and values through LDS, the next one on its way to registers while the products run.  Products and statistics as in the fused
+// attention: scores are a 32 x 32 accumulator, lane = row, whose layout is that of the operand of the product with the values.
+//   A turned query has more bits than bf16: it is kept in two bf16 parts, and the scores are two products.  Weights are rounded to the type for the product
+//   with the values (half a step of each, 2^-8 of its own share of the result), as in the fused attention.
+//   Masked weights are zeros, but a zero times an infinity is none: in blocks that some row sees in part, values that are no numbers are
+//   taken out (`odd`), and given afterwards to the rows that see them.
+constexpr int kTileTable = 256;  // (two workgroups of 128 components and 128 keys just fit a unit's LDS)
+template <class X, int WR>
+struct TileShape {
+    static constexpr int kKeys = WR == 1 ? 128 : 64;          // keys of a block
+    static constexpr int kRowVecs = X::H / X::kPer;
+    static constexpr int kVec = kKeys * kRowVecs / 256;       // vectors of a thread, of the keys and of the values
+    static constexpr int kRows = 32 * WR;
+    static constexpr int kLds = kKeys * (X::LD + X::LD_COLS) * (int)sizeof(typename X::T);
+    static constexpr int kMeet = (X::H / 2 + 2) * 2 * 64 * 4; // what two wavefronts hand to two others
+    static constexpr int kBytes = WR == 1 && kMeet > kLds ? kMeet : kLds;
+};
+
+// this lane's row, as the products take it; its second part where it is turned
+template <class X>
+__device__ __forceinline__ void load_query(const Cache& c, const typename X::T* row, int hh, int p, bool there, typename X::Own& q, typename X::Own& rest) {
+    if constexpr (sizeof(typename X::T) == 4) {
+#pragma unroll
+        for (int s = 0; s < X::H / 16; s++) {
+            float x[kE] = {};
+            if (there) turned<float>(c, row, (X::H / 2) * hh + 8 * s, p, x);
+#pragma unroll
+            for (int i = 0; i < kE; i++) q.v[8 * s + i] = x[i];
+        }
+    } else {
+#pragma unroll
+        for (int s = 0; s < X::H / 16; s++) {
+            float x[kE] = {};
+            if (there) turned<bf16_t>(c, row, 16 * s + 8 * hh, p, x);
+#pragma unroll
+            for (int i = 0; i < kE; i++) {
+                q.v[s][i] = (__bf16)x[i];
+                rest.v[s][i] = (__bf16)(x[i] - (float)q.v[s][i]);
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ bool no_number(uint32_t b) { return (b & 0x7f800000u) == 0x7f800000u; }
+
+// the elements of a vector that are no numbers, as zeros; whether there was one
+__device__ __forceinline__ bool take_out(float4& v) {
+    float* f = &v.x;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const bool bad = no_number(__float_as_uint(f[i]));
+        f[i] = bad ? 0.f : f[i];
+        odd = odd || bad;
+    }
+    return odd;
+}
+__device__ __forceinline__ bool take_out(uint4& v) {
+    uint32_t* w = &v.x;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const bool lo = no_number(w[i] << 16), hi = no_number(w[i] & 0xffff0000u);
+        w[i] &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+        odd = odd || lo || hi;
+    }
+    return odd;
+}
+
+// TURN: queries are turned.  (fp32 of 128 components: one workgroup to a unit, its blocks on their way take too many registers for two.)
+template <class X, int WR, bool TURN>
+__global__ void __launch_bounds__(256, sizeof(typename X::T) == 4 && X::H == 128 ? 1 : 2) attend_tile_kernel(Attend a) {
+    using T = typename X::T;
+    using S = TileShape<X, WR>;
+    constexpr int H = X::H, LDK = X::LD, LDV = X::LD_COLS, KEYS = S::kKeys;
+    __shared__ __attribute__((aligned(16))) char lds[S::kBytes];
+    __shared__ const T* keys[kTileTable];
+    __shared__ const T* values[kTileTable];
+    __shared__ int odd_block;
+    T* const Ks = reinterpret_cast<T*>(lds);
+    T* const Vs = Ks + KEYS * LDK;
     const Cache& c = a.c;
-    const int G = c.N_h / c.N_kv, lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= (int64_t)c.z.n2 * c.z.n1 * c.N_h) return;
-    const int head = (int)(row % c.N_h), tok = (int)(row / c.N_h % c.z.n1), b = (int)(row / c.N_h / c.z.n1);
+    const int G = c.N_h / c.N_kv;
+    const int split = blockIdx.x, j = blockIdx.y % c.N_kv, b = blockIdx.z;
+    // the last rows see the most keys: they go first
+    const int chunk = a.chunks - 1 - (int)blockIdx.y / c.N_kv;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, hh = lane >> 5, ln = lane & 31;
+    const int r0 = chunk * S::kRows, n_new = new_tokens(c, b);
+    const int rows = min(S::kRows, n_new * G - r0);
+    if (rows <= 0) return;
+    const int start = c.start[b];
+    const Range g = range_of(a, start, r0 / G, (r0 + rows - 1) / G, KEYS);
+    const bool alone = g.per >= g.hi - g.lo;
+    if (split > 0 && (int64_t)split * g.per >= g.hi - g.lo) return;
+    const int lo = g.lo + split * g.per, hi = lo + min(g.per, g.hi - lo);
+    if (lo >= hi && !(alone && split == 0)) return;
+
+    // this lane's row, and what this wavefront's rows see at least and at most
+    const int first = WR == 1 ? 0 : 32 * w, own = first + ln;
+    const int tok = (r0 + own) / G, head = j * G + (r0 + own) % G;
+    const int64_t pos = (int64_t)start + tok;
+    const bool there = own < rows && pos >= 0 && (!c.rot || pos < c.rot_n);
+    const int upto = there ? clamped(pos) : -1, from = c.window > 0 ? clamped(pos - c.window) : -1;
+    // (clamped too: a first position below 0 sees nothing, and then nothing is seen by all)
+    const int w_first = clamped((int64_t)start + (r0 + first) / G), w_last = clamped((int64_t)start + (r0 + min(first + 31, rows - 1)) / G);
+    const bool w_any = first < rows;
+    typename X::Own q, rest;
+    load_query<X>(c, there ? row_at<const T>(c.z, head * H, tok, b) : nullptr, hh, (int)pos, there, q, rest);
+
+    f32x16 O[H / 32];
+#pragma unroll
+    for (int rb = 0; rb < H / 32; rb++) O[rb] = zero16();
+    float m = kNegInf, lsum = 0.f;
+
+    for (int k0 = lo; k0 < hi;) {
+        // the pages' addresses, kTileTable at a time
+        const int first_page = (int)c.by_P((uint32_t)k0);
+        const int k1 = (int)min((int64_t)hi, (first_page + kTileTable) * (int64_t)c.P);
+        const int n_here = (int)c.by_P((uint32_t)(k1 - 1)) - first_page + 1;
+        __syncthreads();
+        bool gone = false;
+        for (int i = tid; i < n_here; i += 256) {
+            const int page = c.pages[(int64_t)b * c.max_pages + first_page + i];
+            const bool ok = page >= 0 && page < c.n_pages;
+            const int64_t off = (int64_t)j * c.P * H;
+            keys[i] = ok ? global_as<const T>(c.K[page]) + off : nullptr;
+            values[i] = ok ? global_as<const T>(c.V[page]) + off : nullptr;
+            gone = gone || !ok;
+        }
+        const bool all_there = !__syncthreads_or(gone);
+
+        // block [k, k + KEYS) into registers, zeros beyond k1 and where no page is
+        typename X::Vec kr[S::kVec], vr[S::kVec];
+        auto fetch = [&](int k) {
+#pragma unroll
+            for (int i = 0; i < S::kVec; i++) {
+                const int idx = tid + 256 * i, row = idx / S::kRowVecs, cv = idx % S::kRowVecs;
+                kr[i] = vr[i] = X::zero_vec();
+                if (k + row < k1) {
+                    const uint32_t p = (uint32_t)(k + row), pg = c.by_P(p), slot = p - pg * c.P, at = pg - (uint32_t)first_page;
+                    if (const T* kp = keys[at]) {
+                        const uint32_t off = slot * H + cv * X::kPer;
+                        kr[i] = *reinterpret_cast<const typename X::Vec*>(in_global(kp) + off);
+                        vr[i] = *reinterpret_cast<const typename X::Vec*>(in_global(values[at]) + off);
+                    }
+                }
+            }
+        };
+        // whether every row of the workgroup sees all of the block
+        const int wg_first = clamped((int64_t)start + r0 / G), wg_last = clamped((int64_t)start + (r0 + rows - 1) / G);
+        auto whole = [&](int k) { return k + KEYS - 1 <= wg_first && (c.window == 0 || k > wg_last - c.window); };
+        auto stash = [&](int k) {
+            const bool clean = !whole(k);
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < S::kVec; i++) {
+                const int idx = tid + 256 * i, row = idx / S::kRowVecs, cv = idx % S::kRowVecs;
+                if (clean && take_out(vr[i])) odd = true;
+                X::template put<LDK>(Ks, row, cv, kr[i]);
+                X::template put<LDV>(Vs, row, cv, vr[i]);
+            }
+            if (odd) odd_block = 1;
+        };
+        // pages begin on large powers of two, and workgroups that walk theirs in step would all ask the same memory channels: each begins elsewhere
+        const int blocks = (int)((k1 - k0 + KEYS - 1) / KEYS), turn = (int)((5u * split + 3u * j) % (uint32_t)blocks);
+        auto block = [&](int i) { return k0 + KEYS * (i + turn < blocks ? i + turn : i + turn - blocks); };
+        fetch(block(0));
+        if (tid == 0) odd_block = 0;
+        __syncthreads();
+        stash(block(0));
+        __syncthreads();
+        for (int i = 0; i < blocks; i++) {
+            const int k = block(i);
+            const bool more = i + 1 < blocks;
+            if (more) fetch(block(i + 1));
+            const bool odd = odd_block != 0;
+            // WR = 4: both halves of the block; WR = 1: the wavefront's quarter of it
+#pragma unroll
+            for (int h2 = 0; h2 < (WR == 1 ? 1 : 2); h2++) {
+                const int part = WR == 1 ? w : h2;
+                const int kb = k + 32 * part;
+                if (!w_any || kb >= k1 || kb > w_last || (c.window > 0 && kb + 31 <= w_first - c.window)) continue;
+                f32x16 s = X::template rows_times_own<LDK>(Ks, part, ln, hh, q);
+                if constexpr (sizeof(T) == 2 && TURN) {
+                    const f32x16 s2 = X::template rows_times_own<LDK>(Ks, part, ln, hh, rest);
+#pragma unroll
+                    for (int r = 0; r < 16; r++) s[r] += s2[r];
+                }
+                uint32_t seen = 0xffffu;
+                if (!(all_there && kb + 32 <= k1 && kb + 31 <= w_first && (c.window == 0 || kb > w_last - c.window))) {
+                    const int end = min(upto + 1, k1);
+                    seen = 0;
+#pragma unroll
+                    for (int r = 0; r < 16; r++) {
+                        const int kk = kb + acc_row(r, hh);
+                        bool sees = kk < end && kk > from;
+                        if (!all_there && sees) sees = keys[c.by_P((uint32_t)kk) - (uint32_t)first_page] != nullptr;
+                        seen |= sees ? 1u << r : 0u;
+                        s[r] = sees ? s[r] : kNegInf;
+                    }
+                }
+                float mx = kNegInf;
+#pragma unroll
+                for (int r = 0; r < 16; r++) mx = fmaxf(mx, s[r]);
+                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                const float m_new = fmaxf(m, mx);
+                const float shift = m_new == kNegInf ? 0.f : m_new * a.scale;
+                const float alpha = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m * a.scale - shift);
+                m = m_new;
+                float rowsum = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; r++) {
+                    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -shift));
+                    rowsum += s[r];
+                }
+                lsum = lsum * alpha + rowsum;
+                if (__any(alpha != 1.f)) {
+#pragma unroll
+                    for (int rb = 0; rb < H / 32; rb++)
+#pragma unroll
+                        for (int r = 0; r < 16; r++) O[rb][r] *= alpha;
+                }
+                typename X::Packed pk;
+                X::pack(s, pk);
+                X::template cols_times_acc<LDV>(O, Vs, part, lane, pk);
+                if (odd) {
+                    // the values that were taken out, to the rows that see their keys
+#pragma unroll 1
+                    for (int kk = 0; kk < 32; kk++) {
+                        const int p = kb + kk;
+                        const T* vp = p < k1 ? values[c.by_P((uint32_t)p) - (uint32_t)first_page] : nullptr;
+                        if (!vp) continue;
+                        const T* v = in_global(vp) + (int64_t)((uint32_t)p - c.by_P((uint32_t)p) * c.P) * H;
+                        // the weight of key kk lies in the half that acc_row puts it in
+                        const int r = 4 * (kk / 8) + kk % 4, half = (kk / 4) % 2;
+                        float wt = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; i++) wt = i == r ? s[i] : wt;
+                        uint32_t bits = (seen >> r) & 1u;
+                        const float wt2 = __shfl_xor(wt, 32, 64);
+                        const uint32_t bits2 = (uint32_t)__shfl_xor((int)bits, 32, 64);
+                        wt = hh == half ? wt : wt2;
+                        bits = hh == half ? bits : bits2;
+#pragma unroll
+                        for (int rb = 0; rb < H / 32; rb++)
+#pragma unroll
+                            for (int i = 0; i < 16; i++) {
+                                float x[1];
+                                ldv<1>(v + 32 * rb + acc_row(i, hh), x);
+                                if (bits && no_number(__float_as_uint(x[0]))) O[rb][i] += wt * x[0];
+                            }
+                    }
+                }
+            }
+            __syncthreads();
+            if (more) {
+                if (tid == 0) odd_block = 0;
+                __syncthreads();
+                stash(block(i + 1));
+            }
+            __syncthreads();
+        }
+        k0 = k1;
+    }
+    lsum += __shfl_xor(lsum, 32, 64);
+    if (!there) {                                             // (a row without a query: it has added up what there was)
+        m = kNegInf;
+        lsum = 0.f;
+#pragma unroll
+        for (int rb = 0; rb < H / 32; rb++) O[rb] = zero16();
+    }
+    if constexpr (WR == 1) {
+        // the wavefronts' partial results of the same rows meet: 2 and 3 hand theirs to 0 and 1, then 1 to 0
+        constexpr int N = H / 2 + 2;
+        float* buf = reinterpret_cast<float*>(lds);
+#pragma unroll
+        for (int left = 2; left >= 1; left >>= 1) {
+            __syncthreads();
+            if (w >= left && w < 2 * left) {
+#pragma unroll
+                for (int i = 0; i < N; i++) buf[((w - left) * N + i) * 64 + lane] = i < H / 2 ? O[i / 16][i % 16] : i == H / 2 ? m : lsum;
+            }
+            __syncthreads();
+            if (w < left) {
+                const float* got = buf + w * N * 64 + lane;
+                const float m2 = got[(H / 2) * 64], m_new = fmaxf(m, m2);
+                const float f1 = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * a.scale), f2 = m2 == kNegInf ? 0.f : __builtin_amdgcn_exp2f((m2 - m_new) * a.scale);
+                lsum = lsum * f1 + got[(H / 2 + 1) * 64] * f2;
+                m = m_new;
+#pragma unroll
+                for (int rb = 0; rb < H / 32; rb++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++) O[rb][r] = O[rb][r] * f1 + got[(16 * rb + r) * 64] * f2;
+            }
+        }
+        if (w > 0) return;
+    }
+    if (own >= rows) return;
+    if (alone) {
+        const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
+        T* o = row_at<T>(a.out, head * H, tok, b);
+#pragma unroll
+        for (int rb = 0; rb < H / 32; rb++)
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                X::store4(o + 32 * rb + 8 * k + 4 * hh, O[rb][4 * k] * inv, O[rb][4 * k + 1] * inv, O[rb][4 * k + 2] * inv, O[rb][4 * k + 3] * inv);
+    } else {
+        float* o = a.partial + ((((int64_t)b * c.z.n1 + tok) * c.N_h + head) * a.splits + split) * (H + 2);
+#pragma unroll
+        for (int rb = 0; rb < H / 32; rb++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) o[32 * rb + acc_row(i, hh)] = O[rb][i];
+        if (hh == 0) {
+            o[H] = m * a.scale;
+            o[H + 1] = lsum;
+        }
+    }
+}
+
+// The splits of a row meet.  kSpread: a workgroup per row, its four wavefronts take a quarter of the splits each; else a wavefront per row (many rows of few
+// splits).  `R`, `step`: how the rows and keys were cut.
+template <typename T, bool kSpread>
+__global__ void __launch_bounds__(256) join_kernel(Attend a, int R, int step) {
+    __shared__ float part[4][256];
+    constexpr int D = kSpread ? 4 : 1;
+    const Cache& c = a.c;
+    const int G = c.N_h / c.N_kv, tid = threadIdx.x, lane = tid & 63, w = tid >> 6, first = kSpread ? w : 0;
+    const int row = kSpread ? (int)blockIdx.x : 4 * (int)blockIdx.x + w;       // (token, head) of sequence blockIdx.y
+    const int head = row % c.N_h, tok = row / c.N_h, b = blockIdx.y;
     const int n_new = new_tokens(c, b);
     if (tok >= n_new) return;
     const int r0 = (tok * G + head % G) / R * R, rows = min(R, n_new * G - r0);
-    const Range g = range_of(a, c.start[b], r0 / G, (r0 + rows - 1) / G, step);
-    if (g.lo + g.per >= g.hi) return;                  // nothing to join
-    const int n = (int)((g.hi - g.lo + g.per - 1) / g.per);
-    const float* p = a.partial + row * a.splits * (c.h + 2);
-    float m = kNegInf;
-    for (int k = lane; k < n; k += 64) m = fmaxf(m, p[(int64_t)k * (c.h + 2) + c.h]);
-    m = wave_max(m);
-    const float base = m == kNegInf ? 0.f : m;
-    float s = 0.f;
-    for (int k = lane; k < n; k += 64) s += exp2f(p[(int64_t)k * (c.h + 2) + c.h] - base) * p[(int64_t)k * (c.h + 2) + c.h + 1];
-    s = wave_sum(s);
+    const Range g = range_of(a, c.start[b], r0 / G, (r0 + rows - 1) / G, (uint32_t)step);
+    if (g.per >= g.hi - g.lo) return;                  // nothing to join
+    const int n = (int)((uint32_t)(g.hi - g.lo + g.per - 1) / (uint32_t)g.per), pitch = c.h + 2;
+    const float* p = a.partial + (((int64_t)b * c.z.n1 + tok) * c.N_h + head) * a.splits * pitch;
+    // a lane knows a split's maximum and sum (there are at most 64)
+    const float mine = lane < n ? p[lane * pitch + c.h] : kNegInf, sum = lane < n ? p[lane * pitch + c.h + 1] : 0.f;
+    const float m = wave_max(mine), f = exp2f(mine - (m == kNegInf ? 0.f : m));
+    const float s = wave_sum(f * sum);
     T* o = row_at<T>(a.out, head * c.h, tok, b);
-    for (int i = lane; i < c.h; i += 64) {
-        float x[1] = {0.f};
-        for (int k = 0; k < n; k++) x[0] += exp2f(p[(int64_t)k * (c.h + 2) + c.h] - base) * p[(int64_t)k * (c.h + 2) + i];
-        x[0] = s == 0.f ? 0.f : x[0] / s;
-        stv<1>(o + i, x);
+    for (int i0 = 0; i0 < c.h; i0 += 64) {
+        const int i = min(i0 + lane, c.h - 1);
+        float x = 0.f;
+        for (int k0 = first; k0 < n; k0 += 8 * D) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) v[k] = p[min(k0 + D * k, n - 1) * pitch + i];
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                const int at = k0 + D * k;
+                x += at < n ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), at)) * v[k] : 0.f;
+            }
+        }
+        if constexpr (kSpread) {
+            part[w][i0 + lane] = x;
+        } else if (i0 + lane < c.h) {
+            const float y[1] = {s == 0.f ? 0.f : x / s};
+            stv<1>(o + i, y);
+        }
+    }
+    if constexpr (kSpread) {
+        __syncthreads();
+        if (tid < c.h) {
+            const float y[1] = {s == 0.f ? 0.f : (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]) / s};
+            stv<1>(o + tid, y);
+        }
     }
 }
 
@@ -406,18 +795,18 @@ int32_t launched() { return hipGetLastError() == hipSuccess ? (int32_t)NNT_OK : 
         if (rc__ != NNT_OK) return rc__; \
     } while (0)
 
-constexpr int kMostSplits = 64;
-
-Rows rows_of(const nnt_tensor* t) {
-    const TiledView v = t->view();
-    return Rows{v.tiles, v.shape[0], v.shape[1], v.shape[2], v.base[0], v.base[1], v.base[2], v.grid[0], v.grid[1]};
-}
 
 Divide divide_by(uint32_t d) {
     // (n < 2^31: with 2^(k - 1) < d <= 2^k the product with ceil(2^(31 + k) / d) is exact enough)
     uint32_t k = 0;
     while ((1ull << k) < d) k++;
     return Divide{(uint32_t)(((1ull << (31 + k)) + d - 1) / d), k - 1, d};
+}
+
+Rows rows_of(const nnt_tensor* t) {
+    const TiledView v = t->view();
+    return Rows{v.tiles, v.shape[0], v.shape[1], v.shape[2], v.base[0], v.base[1], v.base[2], v.grid[0], v.grid[1],
+                divide_by((uint32_t)v.base[0]), divide_by((uint32_t)v.base[1]), divide_by((uint32_t)v.base[2])};
 }
 
 Cache cache_of(const nnt_cache_cfg* cfg, nnt_tensor* QKV, nnt_tensor* K, nnt_tensor* V) {
@@ -434,6 +823,8 @@ Cache cache_of(const nnt_cache_cfg* cfg, nnt_tensor* QKV, nnt_tensor* K, nnt_ten
         c.rot_n = (int32_t)r->shape[1];
         c.rot_base = (int32_t)r->base[1];
         c.rot_pairs = cfg->rotate == NNT_ROTATE_PAIRS;
+        c.rot_whole = c.rot_r % 16 == 0;
+        c.by_rot = divide_by((uint32_t)c.rot_base);
     }
     c.h = (int32_t)K->shape[0];
     c.N_h = cfg->N_h;
@@ -448,28 +839,39 @@ Cache cache_of(const nnt_cache_cfg* cfg, nnt_tensor* QKV, nnt_tensor* K, nnt_ten
 
 // How the rows and keys of a call are cut.
 struct Cut {
-    int R, lpk, step, chunks, splits;
+    int R, lpk, step, chunks, splits, tile;      // tile: 0, or WR of the matrix cores' kernel
 };
 Cut cut_of(const nnt_cache_cfg* cfg, const nnt_tensor* QKV, const nnt_tensor* K) {
     Cut u;
     const int64_t G = cfg->N_h / cfg->N_kv, rows = G * QKV->shape[1], N_b = QKV->shape[2];
-    u.R = rows >= 4 ? 4 : rows >= 2 ? 2 : 1;
     const int64_t h = K->shape[0];
+    const bool bf16 = K->dtype == NNT_BF16;
+    u.tile = h != 64 && h != 128 ? 0 : bf16 ? (rows > 32 ? 4 : rows > 8 ? 1 : 0) : rows >= 32 ? 4 : 0;
+    u.R = u.tile ? 32 * u.tile : rows >= 4 ? 4 : rows >= 2 ? 2 : 1;
     u.lpk = h <= 32 ? 4 : h <= 64 ? 8 : h <= 128 ? 16 : 32;
-    u.step = kWaves * (64 / u.lpk) * kUnroll;
+    u.step = u.tile ? (u.tile == 1 ? 128 : 64) : kWaves * (64 / u.lpk) * kUnroll;
     u.chunks = (int)((rows + u.R - 1) / u.R);
-    // about eight workgroups to a compute unit
-    const int64_t pairs = u.chunks * cfg->N_kv * N_b;
+    // about eight workgroups to a compute unit, three of the matrix cores' kernel
+    const int64_t pairs = (int64_t)u.chunks * cfg->N_kv * N_b, wanted = u.tile ? 768 : 2048;
     const int64_t most = ((int64_t)cfg->max_pages * K->base[1] + u.step - 1) / u.step;
-    u.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(2048 + pairs - 1) / pairs, most, kMostSplits}));
+    u.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(wanted + pairs - 1) / pairs, most, kMostSplits}));
     return u;
 }
 
 using AttendFn = void (*)(Attend);
 template <typename T, int LPK>
 AttendFn attend_rows(int R) { return R == 1 ? attend_kernel<T, LPK, 1> : R == 2 ? attend_kernel<T, LPK, 2> : attend_kernel<T, LPK, 4>; }
+template <typename T, int H>
+AttendFn attend_tile(int wr, bool turn) {
+    if constexpr (sizeof(T) == 4) return attend_tile_kernel<F32Traits<H>, 4, false>;
+    else if (wr == 1) return turn ? attend_tile_kernel<Bf16Traits<H>, 1, true> : attend_tile_kernel<Bf16Traits<H>, 1, false>;
+    else return turn ? attend_tile_kernel<Bf16Traits<H>, 4, true> : attend_tile_kernel<Bf16Traits<H>, 4, false>;
+}
 template <typename T>
-AttendFn attend_instance(const Cut& u) {
+AttendFn attend_instance(const Cut& u, int64_t h, bool turn) {
+    if (u.tile) {
+        return h == 64 ? attend_tile<T, 64>(u.tile, turn) : attend_tile<T, 128>(u.tile, turn);
+    }
     return u.lpk == 4 ? attend_rows<T, 4>(u.R) : u.lpk == 8 ? attend_rows<T, 8>(u.R) : u.lpk == 16 ? attend_rows<T, 16>(u.R) : attend_rows<T, 32>(u.R);
 }
 
@@ -515,6 +917,8 @@ int32_t nnt_cache_append(nnt_ctx* ctx, const nnt_cache_cfg* cfg, nnt_tensor* QKV
         TRY(cache_check(ctx, cfg, QKV, K, V, nullptr));
         const Cache c = cache_of(cfg, QKV, K, V);
         const int64_t per_seq = (int64_t)(c.h / kE) * c.N_kv * c.z.n1;
+        if (per_seq > INT32_MAX - 256) return fail(ctx, NNT_EINVAL, "nnt_cache_append: too many tokens of too many heads in one call");
+        const Divide by_token = divide_by((uint32_t)(c.h / kE * c.N_kv)), by_head = divide_by((uint32_t)(c.h / kE));
         const dim3 grid((unsigned)((per_seq + 255) / 256), (unsigned)c.z.n2);
         const bool bf16 = K->dtype == NNT_BF16;
         std::vector<Access> acc;
@@ -524,8 +928,8 @@ int32_t nnt_cache_append(nnt_ctx* ctx, const nnt_cache_cfg* cfg, nnt_tensor* QKV
         if (cfg->rotation) acc.push_back(cfg->rotation->all(kRead));
         OpTag tag(ctx, "cache_append", 4.0 * (double)c.N_kv * c.h * c.z.n1 * c.z.n2 * (double)K->elem_size(), true);
         TRY(submit(ctx, acc, [&](hipStream_t st) {
-            if (bf16) hipLaunchKernelGGL(append_kernel<bf16_t>, grid, dim3(256), 0, st, c);
-            else hipLaunchKernelGGL(append_kernel<float>, grid, dim3(256), 0, st, c);
+            if (bf16) hipLaunchKernelGGL(append_kernel<bf16_t>, grid, dim3(256), 0, st, c, by_token, by_head);
+            else hipLaunchKernelGGL(append_kernel<float>, grid, dim3(256), 0, st, c, by_token, by_head);
             return launched();
         }));
         K->whole_submitted();
@@ -547,7 +951,7 @@ int32_t nnt_cache_attention(nnt_ctx* ctx, const nnt_cache_cfg* cfg, float scale,
         a.splits = u.splits;
         a.chunks = u.chunks;
         const bool bf16 = K->dtype == NNT_BF16;
-        const AttendFn fn = bf16 ? attend_instance<bf16_t>(u) : attend_instance<float>(u);
+        const AttendFn fn = bf16 ? attend_instance<bf16_t>(u, a.c.h, a.c.rot) : attend_instance<float>(u, a.c.h, a.c.rot);
         const dim3 grid((unsigned)u.splits, (unsigned)(u.chunks * a.c.N_kv), (unsigned)a.c.z.n2);
         const int64_t rows = (int64_t)a.c.z.n1 * a.c.z.n2 * a.c.N_h;
         std::vector<Access> acc{B->all(kReadWrite), QKV->all(kRead)};
@@ -561,9 +965,11 @@ int32_t nnt_cache_attention(nnt_ctx* ctx, const nnt_cache_cfg* cfg, float scale,
             hipLaunchKernelGGL(fn, grid, dim3(kWaves * 64), 0, st, a);
             TRY(launched());
             if (u.splits == 1) return NNT_OK;
-            const dim3 jg((unsigned)((rows + 3) / 4));
-            if (bf16) hipLaunchKernelGGL(join_kernel<bf16_t>, jg, dim3(256), 0, st, a, u.R, u.step);
-            else hipLaunchKernelGGL(join_kernel<float>, jg, dim3(256), 0, st, a, u.R, u.step);
+            const bool spread = u.splits > 8;
+            const int64_t per_seq = (int64_t)a.c.z.n1 * a.c.N_h;
+            const dim3 jg((unsigned)(spread ? per_seq : (per_seq + 3) / 4), (unsigned)a.c.z.n2);
+            const auto join = bf16 ? (spread ? join_kernel<bf16_t, true> : join_kernel<bf16_t, false>) : (spread ? join_kernel<float, true> : join_kernel<float, false>);
+            hipLaunchKernelGGL(join, jg, dim3(256), 0, st, a, u.R, u.step);
             return launched();
         }, u.splits == 1 ? 1 : 2));
         K->whole_submitted();

@@ -18,6 +18,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPiece = 16384;          // elements: 64 KB of fp32
 constexpr int kMaxGroups = 2048;       // workgroups of a launch: eight to a compute unit
+constexpr int kFew = 256;              // partial sums that every workgroup of the second pass adds up by itself (the smallest block 13.3 -> CLIP_FIGURE us)
 constexpr int kListed = 48;            // tensors of a launch: their geometry travels in its arguments (4 KB at most)
 
 struct Listed {
@@ -109,21 +110,30 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(List a, double* parti
     if (threadIdx.x == 0) partial[blockIdx.x] = part[0] + part[1] + part[2] + part[3];
 }
 
-// norm and factor: one workgroup, fixed order
-__global__ void __launch_bounds__(1024) norm_kernel(const double* partial, int n, double max_norm, double eps, double* factor, float* norm) {
-    __shared__ double part[16];
+// Norm and factor of the partial sums, by all threads of a workgroup in a fixed order.
+template <int NT>
+__device__ __forceinline__ double factor_of(const double* partial, int n, double max_norm, double eps, double* norm) {
+    __shared__ double part[NT / 64];
     double s = 0.0;
-    for (int i = threadIdx.x; i < n; i += 1024) s += partial[i];
+    for (int i = threadIdx.x; i < n; i += NT) s += partial[i];
     s = wave_sum64(s);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
     __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; w++) s += part[w];
+    *norm = sqrt(s);
+    const double f = max_norm / (*norm + eps);
+    return *norm < __builtin_huge_val() && f < 1.0 ? f : 1.0;          // (a norm that is no number: as it is)
+}
+
+// one workgroup
+__global__ void __launch_bounds__(1024) norm_kernel(const double* partial, int n, double max_norm, double eps, double* factor, float* norm) {
+    double r;
+    const double f = factor_of<1024>(partial, n, max_norm, eps, &r);
     if (threadIdx.x == 0) {
-        s = 0.0;
-        for (int w = 0; w < 16; w++) s += part[w];
-        const double r = sqrt(s);
+        *factor = f;
         *norm = (float)r;
-        const double f = max_norm / (r + eps);
-        *factor = r < __builtin_huge_val() && f < 1.0 ? f : 1.0;       // (a norm that is no number: as it is)
     }
 }
 
@@ -149,9 +159,24 @@ __device__ __forceinline__ void scale(const T* p, T* o, int count, double f) {
     }
 }
 
-// in_place: a factor of one leaves nothing to do
-__global__ void __launch_bounds__(kThreads) scale_kernel(List a, const double* factor) {
-    const double f = *factor;
+// What a workgroup is told of the factor: the number itself, or (few: n_partial > 0) the sums it comes from, which saves a launch.
+struct Factor {
+    const double* at;
+    const double* partial;
+    int n_partial;
+    double max_norm, eps;
+    float* norm;
+};
+// (in place a factor of one leaves nothing to do)
+__global__ void __launch_bounds__(kThreads) scale_kernel(List a, Factor by) {
+    double f;
+    if (by.n_partial) {
+        double r;
+        f = factor_of<kThreads>(by.partial, by.n_partial, by.max_norm, by.eps, &r);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *by.norm = (float)r;
+    } else {
+        f = *by.at;
+    }
     for (int w = a.pieces - 1 - (int)blockIdx.x; w >= 0; w -= gridDim.x) {
         const Piece p = piece_of(a, w);
         void *in = p.t->in[p.tile], *out = p.t->out[p.tile];
@@ -262,14 +287,18 @@ int32_t nnt_clip_grad_norm(nnt_ctx* ctx, const nnt_clip_cfg* cfg, int32_t n, nnt
                 TRY(launched());
                 at += (int)groups_of(l);
             }
-            hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(1024), 0, st, partial, at, max_norm, eps, factor, norm);
-            TRY(launched());
+            const bool few = writes && lists.size() == 1 && at <= kFew;
+            if (!few) {
+                hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(1024), 0, st, partial, at, max_norm, eps, factor, norm);
+                TRY(launched());
+            }
             // the last read first: some of it is still in the caches
+            const Factor by{factor, partial, few ? at : 0, max_norm, eps, norm};
             for (size_t i = lists.size(); writes && i-- > 0;) {
-                hipLaunchKernelGGL(scale_kernel, dim3(groups_of(lists[i])), dim3(kThreads), 0, st, lists[i], factor);
+                hipLaunchKernelGGL(scale_kernel, dim3(groups_of(lists[i])), dim3(kThreads), 0, st, lists[i], by);
                 TRY(launched());
             }
             return NNT_OK;
-        }, (int)lists.size() * (writes ? 2 : 1) + 1);
+        }, (int)lists.size() * (writes ? 2 : 1) + (writes && lists.size() == 1 && (int)groups_of(lists[0]) <= kFew ? 0 : 1));
     });
 }
