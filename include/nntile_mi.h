@@ -569,7 +569,7 @@ NNT_API int32_t nnt_cache_append(nnt_ctx* ctx, const nnt_cache_cfg* cfg, nnt_ten
  * over the positions k <= start[b] + s (and > start[b] + s - window) whose page is there; a query that sees none gives zeros.  Columns of
  * tokens that are not new (s >= count[b]) are left as they are.  QKV as above (only the queries are read), B: [N_h * h, N_s, N_b],
  * row tiles of whole heads.  What is masked does not enter, infinities and NaN there included.  scale > 0.  The keys of long sequences are split over workgroups, whose
- * partial results meet in the context's per-stream scratch (at most N_s * N_b * N_h * (h + 2) * 64 floats), which must exist before a graph
+ * partial results meet in the context's per-stream scratch (at most N_s * N_b * N_h * (h + 2) * 128 floats), which must exist before a graph
  * capture (run the call once). */
 NNT_API int32_t nnt_cache_attention(nnt_ctx* ctx, const nnt_cache_cfg* cfg, float scale, nnt_tensor* QKV, nnt_tensor* K,
                             nnt_tensor* V, nnt_tensor* B);

@@ -70,44 +70,78 @@ __device__ __forceinline__ void eight(const float* p, float (&x)[kE]) {
     for (int i = 0; i < 4; i++) { x[i] = lo[i]; x[i + 4] = hi[i]; }
 }
 
-// Components i0 .. i0 + 7 of a head's row, turned by the rotation of position p (0 <= p < rot_n).
-template <typename T>
-__device__ __forceinline__ void turned(const Cache& c, const T* row, int i0, int p, float (&x)[kE]) {
-    eight(row + i0, x);
-    if (!c.rot) return;
-    const int half = c.rot_r / 2, t = (int)c.by_rot((uint32_t)p);
-    const float* cs = in_global(c.rot[t]) + (int64_t)(p - t * c.rot_base) * c.rot_r;
-    if (i0 >= c.rot_r) return;
-    if (c.rot_pairs) {
+// Components i0 .. i0 + 7 of R heads' rows, turned by the rotations of their positions p (0 <= p < rot_n).  The kind of rotation is asked for once, around all rows: their
+// loads are then on their way together.
+template <typename T, int R>
+__device__ __forceinline__ void turned(const Cache& c, const T* const (&row)[R], int i0, const int (&p)[R], float (&x)[R][kE]) {
 #pragma unroll
-        for (int i = 0; i < kE; i += 2)
-            if (i0 + i < c.rot_r) {
-                const float co = cs[(i0 + i) / 2], si = cs[half + (i0 + i) / 2], a = x[i], b = x[i + 1];
-                x[i] = a * co - b * si;
-                x[i + 1] = a * si + b * co;
+    for (int r = 0; r < R; r++) eight(row[r] + i0, x[r]);
+    if (!c.rot || i0 >= c.rot_r) return;
+    const int half = c.rot_r / 2;
+    const float* cs[R];
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+        const int t = (int)c.by_rot((uint32_t)p[r]);
+        cs[r] = in_global(c.rot[t]) + (int64_t)(p[r] - t * c.rot_base) * c.rot_r;
+    }
+    if (c.rot_pairs) {
+        float co[R][kE / 2], si[R][kE / 2];
+        // (a pair behind the rotation's end is not turned)
+#pragma unroll
+        for (int r = 0; r < R; r++)
+#pragma unroll
+            for (int i = 0; i < kE / 2; i++) {
+                const int k = min(i0 / 2 + i, half - 1);
+                co[r][i] = cs[r][k];
+                si[r][i] = cs[r][half + k];
             }
+#pragma unroll
+        for (int r = 0; r < R; r++)
+#pragma unroll
+            for (int i = 0; i < kE / 2; i++)
+                if (i0 + 2 * i < c.rot_r) {
+                    const float a = x[r][2 * i], b = x[r][2 * i + 1];
+                    x[r][2 * i] = a * co[r][i] - b * si[r][i];
+                    x[r][2 * i + 1] = a * si[r][i] + b * co[r][i];
+                }
     } else if (c.rot_whole) {
         // all eight in one half, the others' eight and the eight angles in a row
         const bool second = i0 >= half;
         const int k = second ? i0 - half : i0;
-        float other[kE], co[kE], si[kE];
-        eight(row + (second ? k : i0 + half), other);
-        eight(cs + k, co);
-        eight(cs + half + k, si);
+        float other[R][kE], co[R][kE], si[R][kE];
 #pragma unroll
-        for (int i = 0; i < kE; i++) x[i] = second ? other[i] * si[i] + x[i] * co[i] : x[i] * co[i] - other[i] * si[i];
+        for (int r = 0; r < R; r++) {
+            eight(row[r] + (second ? k : i0 + half), other[r]);
+            eight(cs[r] + k, co[r]);
+            eight(cs[r] + half + k, si[r]);
+        }
+#pragma unroll
+        for (int r = 0; r < R; r++)
+#pragma unroll
+            for (int i = 0; i < kE; i++) x[r][i] = second ? other[r][i] * si[r][i] + x[r][i] * co[r][i] : x[r][i] * co[r][i] - other[r][i] * si[r][i];
     } else {
 #pragma unroll
-        for (int i = 0; i < kE; i++) {
-            const int at = i0 + i;
-            if (at >= c.rot_r) continue;
-            const bool second = at >= half;
-            const int k = second ? at - half : at;
-            float other[1];
-            ldv<1>(row + (second ? k : at + half), other);
-            x[i] = second ? other[0] * cs[half + k] + x[i] * cs[k] : x[i] * cs[k] - other[0] * cs[half + k];
-        }
+        for (int r = 0; r < R; r++)
+#pragma unroll
+            for (int i = 0; i < kE; i++) {
+                const int at = i0 + i;
+                if (at >= c.rot_r) continue;
+                const bool second = at >= half;
+                const int k = second ? at - half : at;
+                float other[1];
+                ldv<1>(row[r] + (second ? k : at + half), other);
+                x[r][i] = second ? other[0] * cs[r][half + k] + x[r][i] * cs[r][k] : x[r][i] * cs[r][k] - other[0] * cs[r][half + k];
+            }
     }
+}
+template <typename T>
+__device__ __forceinline__ void turned(const Cache& c, const T* row, int i0, int p, float (&x)[kE]) {
+    const T* const rows[1] = {row};
+    const int ps[1] = {p};
+    float y[1][kE];
+    turned<T, 1>(c, rows, i0, ps, y);
+#pragma unroll
+    for (int i = 0; i < kE; i++) x[i] = y[0][i];
 }
 
 template <typename T>
@@ -121,32 +155,97 @@ __device__ __forceinline__ void put(T* p, const float (&x)[kE]) {
     }
 }
 
-// A thread moves eight components of a key and of its value.  Eight prompts of up to 1024 tokens of 12 heads of 64 in fp32, turned: APPEND_FIGURE.
+// Where a new token goes: false where its page (or its rotation) is not there.
+__device__ __forceinline__ bool slot_of(const Cache& c, int s, int b, int64_t& p, int& page, uint32_t& slot) {
+    if (s >= new_tokens(c, b)) return false;
+    p = (int64_t)c.start[b] + s;
+    if (p < 0 || p >= (int64_t)c.max_pages * c.P || (c.rot && p >= c.rot_n)) return false;
+    const uint32_t q = c.by_P((uint32_t)p);
+    slot = (uint32_t)p - q * c.P;
+    page = c.pages[(int64_t)b * c.max_pages + q];
+    return page >= 0 && page < c.n_pages;
+}
 template <typename T>
-__global__ void __launch_bounds__(256) append_kernel(Cache c, Divide by_token, Divide by_head) {
-    const uint32_t at = blockIdx.x * 256 + threadIdx.x;
-    const int b = blockIdx.y;
-    const uint32_t s = by_token(at), k = at - s * by_token.d, j = by_head(k);
-    const int i0 = (int)(k - j * by_head.d) * kE;
-    if (s >= (uint32_t)new_tokens(c, b)) return;
-    const int64_t p = (int64_t)c.start[b] + s;
-    if (p < 0 || p >= (int64_t)c.max_pages * c.P || (c.rot && p >= c.rot_n)) return;
-    const uint32_t q = c.by_P((uint32_t)p), slot = (uint32_t)p - q * c.P;
-    const int page = c.pages[(int64_t)b * c.max_pages + q];
-    if (page < 0 || page >= c.n_pages) return;
-    const int64_t to = ((int64_t)j * c.P + slot) * c.h + i0;
-    const TokenAt token = token_at(c.z, (int)s, b);
-    // (values leave as they came, whatever their bits)
-    const uint4* from = reinterpret_cast<const uint4*>(row_at<const T>(c.z, token, (c.N_h + c.N_kv + (int)j) * c.h) + i0);
+__device__ __forceinline__ void copy_eight(const T* from, T* to) {      // (values leave as they came, whatever their bits)
     uint4 v[sizeof(T) / 2];
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; i++) v[i] = from[i];
+    for (int i = 0; i < (int)sizeof(T) / 2; i++) v[i] = reinterpret_cast<const uint4*>(from)[i];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; i++) reinterpret_cast<uint4*>(to)[i] = v[i];
+}
+
+// A thread moves eight components of a key and of its value.
+template <typename T>
+__global__ void __launch_bounds__(256) append_kernel(Cache c, Divide by_token, Divide by_head) {
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x, s = by_token(at), k = at - s * by_token.d, j = by_head(k);
+    const int b = blockIdx.y, i0 = (int)(k - j * by_head.d) * kE;
+    int64_t p;
+    int page;
+    uint32_t slot;
+    if (s >= (uint32_t)c.z.n1 || !slot_of(c, (int)s, b, p, page, slot)) return;
+    const int64_t to = ((int64_t)j * c.P + slot) * c.h + i0;
+    const TokenAt token = token_at(c.z, (int)s, b);
     float x[kE];
     turned<T>(c, row_at<const T>(c.z, token, (c.N_h + (int)j) * c.h), i0, (int)p, x);
     put(global_as<T>(c.K[page]) + to, x);
-    uint4* o = reinterpret_cast<uint4*>(global_as<T>(c.V[page]) + to);
+    copy_eight<T>(row_at<const T>(c.z, token, (c.N_h + c.N_kv + (int)j) * c.h) + i0, global_as<T>(c.V[page]) + to);
+}
+
+// The same where nothing is turned, or all of a head by halves in whole vectors: a thread has eight components of each half, so that what is turned
+// together, and its angles, is read once.  Eight prompts of up to 1024 tokens of 12 heads of 64 in fp32, turned: APPEND_FIGURE.
+template <typename T, bool kTurn>
+__global__ void __launch_bounds__(256) append_halves_kernel(Cache c, Divide by_token, Divide by_head) {
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x, s = by_token(at), k = at - s * by_token.d, j = by_head(k);
+    const int b = blockIdx.y, i0 = (int)(k - j * by_head.d) * kE, half = c.h / 2;
+    int64_t p;
+    int page;
+    uint32_t slot;
+    if (s >= (uint32_t)c.z.n1 || !slot_of(c, (int)s, b, p, page, slot)) return;
+    const int64_t to = ((int64_t)j * c.P + slot) * c.h + i0;
+    const TokenAt token = token_at(c.z, (int)s, b);
+    const T* key = row_at<const T>(c.z, token, (c.N_h + (int)j) * c.h) + i0;
+    const T* value = row_at<const T>(c.z, token, (c.N_h + c.N_kv + (int)j) * c.h) + i0;
+    T *ko = global_as<T>(c.K[page]) + to, *vo = global_as<T>(c.V[page]) + to;
+    if constexpr (kTurn) {
+        const int t = (int)c.by_rot((uint32_t)p);
+        const float* cs = in_global(c.rot[t]) + (int64_t)((int)p - t * c.rot_base) * c.rot_r + i0;
+        float x[kE], y[kE], co[kE], si[kE];
+        eight(key, x);
+        eight(key + half, y);
+        eight(cs, co);
+        eight(cs + half, si);
+        uint4 v[sizeof(T)];
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; i++) o[i] = v[i];
+        for (int i = 0; i < (int)sizeof(T) / 2; i++) {
+            v[i] = reinterpret_cast<const uint4*>(value)[i];
+            v[i + sizeof(T) / 2] = reinterpret_cast<const uint4*>(value + half)[i];
+        }
+#pragma unroll
+        for (int i = 0; i < kE; i++) {
+            const float a = x[i], e = y[i];
+            x[i] = a * co[i] - e * si[i];
+            y[i] = a * si[i] + e * co[i];
+        }
+        put(ko, x);
+        put(ko + half, y);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; i++) {
+            reinterpret_cast<uint4*>(vo)[i] = v[i];
+            reinterpret_cast<uint4*>(vo + half)[i] = v[i + sizeof(T) / 2];
+        }
+    } else {
+        uint4 v[4][sizeof(T) / 2];
+        const T* from[4] = {key, key + half, value, value + half};
+        T* dst[4] = {ko, ko + half, vo, vo + half};
+#pragma unroll
+        for (int r = 0; r < 4; r++)
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; i++) v[r][i] = reinterpret_cast<const uint4*>(from[r])[i];
+#pragma unroll
+        for (int r = 0; r < 4; r++)
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; i++) reinterpret_cast<uint4*>(dst[r])[i] = v[r][i];
+    }
 }
 
 // ---------------------------------------------------------------- attention
@@ -156,11 +255,12 @@ struct Attend {
     float scale;              // times log2(e): scores are exponents of two
     int32_t splits;           // workgroups that share the keys of a row, at most
     int32_t chunks;           // row chunks of a (sequence, cached head) pair
+    Divide by_G, by_kv;       // query heads of a cached one, cached heads
     float* partial;           // [row][split][h + 2]: result of a split (not divided), its maximum, its sum
 };
 
 constexpr int kWaves = 4;
-constexpr int kMostSplits = 64;
+constexpr int kMostSplits = 128;
 constexpr int kUnroll = 4;    // keys a lane has on their way at a time
 constexpr int kTable = 512;   // pages whose addresses a workgroup keeps at a time
 
@@ -227,20 +327,22 @@ __device__ __forceinline__ float lanes_sum(float d) {
 // One workgroup: R rows of a (sequence, cached head) pair against one split of the keys.  LPK lanes share a key, eight components each; a wavefront
 // takes 64 / LPK keys at a time, and every such group of lanes carries a running maximum and sum of its own, which meet at the end.
 template <typename T, int LPK, int R>
-__global__ void __launch_bounds__(kWaves * 64) attend_kernel(Attend a) {
+__global__ void __launch_bounds__(kWaves * 64, R == 4 ? (sizeof(T) == 2 ? 3 : 2) : R == 2 && sizeof(T) == 4 ? 3 : 4) attend_kernel(Attend a) {
+    constexpr bool kAhead = R == 1 && sizeof(T) == 2;
     constexpr int KPW = 64 / LPK, STEP = kWaves * KPW * kUnroll;
     __shared__ const T* keys[kTable];
     __shared__ const T* values[kTable];
     __shared__ float part[kWaves][R][LPK * kE + 2];
     const Cache& c = a.c;
     const int G = c.N_h / c.N_kv;
-    const int split = blockIdx.x, j = blockIdx.y % c.N_kv, chunk = blockIdx.y / c.N_kv, b = blockIdx.z;
+    const int split = blockIdx.x, chunk = (int)a.by_kv(blockIdx.y), j = blockIdx.y - chunk * c.N_kv, b = blockIdx.z;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, sub = lane % LPK, grp = lane / LPK;
     const int r0 = chunk * R, n_new = new_tokens(c, b);
     const int rows = min(R, n_new * G - r0);
     if (rows <= 0) return;
     const int start = c.start[b];
-    const Range g = range_of(a, start, r0 / G, (r0 + rows - 1) / G, STEP);
+    const Divide by_G = a.by_G;
+    const Range g = range_of(a, start, (int)by_G((uint32_t)r0), (int)by_G((uint32_t)(r0 + rows - 1)), STEP);
     const bool alone = g.per >= g.hi - g.lo;           // one split holds all keys
     if (split > 0 && (int64_t)split * g.per >= g.hi - g.lo) return;
     const int lo = g.lo + split * g.per, hi = lo + min(g.per, g.hi - lo);
@@ -248,67 +350,101 @@ __global__ void __launch_bounds__(kWaves * 64) attend_kernel(Attend a) {
 
     // the pages' addresses, kTable at a time
     int first_page = 0, k1 = lo;
+    bool gone = false;                                 // a page is not there
     auto look_up = [&](int k0) {
         first_page = (int)c.by_P((uint32_t)k0);
         k1 = (int)min((int64_t)hi, (first_page + kTable) * (int64_t)c.P);
         const int n_here = (int)(c.by_P((uint32_t)(k1 - 1)) - first_page) + 1;
         __syncthreads();
+        bool missing = false;
         for (int i = tid; i < n_here; i += kWaves * 64) {
             const int page = c.pages[(int64_t)b * c.max_pages + first_page + i];
             const bool ok = page >= 0 && page < c.n_pages;
             const int64_t off = (int64_t)j * c.P * c.h;
             keys[i] = ok ? global_as<const T>(c.K[page]) + off : nullptr;
             values[i] = ok ? global_as<const T>(c.V[page]) + off : nullptr;
+            missing = missing || !ok;
         }
-        __syncthreads();
+        gone = __syncthreads_or(missing);
     };
     if (lo < hi) look_up(lo);
 
     const bool live = sub * kE < c.h;
     float q[R][kE], acc[R][kE], mx[R], sum[R];
-    int upto[R], from[R];                              // positions that a row sees
+    int upto[R], from[R], at_pos[R];                   // positions that a row sees, its own (where it has none: a valid one)
+    const T* at_row[R];
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+        const int row = r0 + min(r, rows - 1), s = (int)by_G((uint32_t)row);
+        const int64_t p = (int64_t)start + s;
+        const bool there = r < rows && p >= 0 && (!c.rot || p < c.rot_n);
+        upto[r] = there ? clamped(p) : -1;
+        from[r] = c.window > 0 ? clamped(p - c.window) : -1;
+        at_pos[r] = (int)max((int64_t)0, min(p, (int64_t)c.rot_n - 1));
+        at_row[r] = row_at<const T>(c.z, (j * G + row - s * G) * c.h, s, b);
+    }
+    turned<T, R>(c, at_row, live ? sub * kE : 0, at_pos, q);
 #pragma unroll
     for (int r = 0; r < R; r++) {
         mx[r] = kNegInf;
         sum[r] = 0.f;
-        const int s = (r0 + r) / G;
-        const int64_t p = (int64_t)start + s;
-        bool there = r < rows && p >= 0 && (!c.rot || p < c.rot_n);
-        upto[r] = there ? clamped(p) : -1;
-        from[r] = c.window > 0 ? clamped(p - c.window) : -1;
 #pragma unroll
-        for (int i = 0; i < kE; i++) q[r][i] = acc[r][i] = 0.f;
-        if (there && live) {
-            turned<T>(c, row_at<const T>(c.z, (j * G + (r0 + r) % G) * c.h, s, b), sub * kE, (int)p, q[r]);
-#pragma unroll
-            for (int i = 0; i < kE; i++) q[r][i] *= a.scale;
+        for (int i = 0; i < kE; i++) {
+            q[r][i] = live && upto[r] >= 0 ? q[r][i] * a.scale : 0.f;
+            acc[r][i] = 0.f;
         }
     }
 
+    int least_upto = INT32_MAX, most_from = -1;
+#pragma unroll
+    for (int r = 0; r < R; r++)
+        if (r < rows) {
+            least_upto = min(least_upto, upto[r]);
+            most_from = max(most_from, from[r]);
+        }
     for (int k0 = lo; k0 < hi;) {
         if (k0 > lo) look_up(k0);
-        for (int k = k0; k < k1; k += STEP) {
+        // A step's keys and values; with one row of bf16, the next step's are on their way while this one's are worked on (64 sequences of up to 4096 90 -> 84 us;
+        // elsewhere the registers would cost wavefronts: four rows of 131072 keys 115 -> 126).
+        struct Step {
             Eight<T> kk[kUnroll], vv[kUnroll];
             int pos[kUnroll];
+        };
+        auto fetch = [&](int k, Step& st) {
 #pragma unroll
             for (int u = 0; u < kUnroll; u++) {
                 const int p = k + (u * kWaves + wv) * KPW + grp;
-                kk[u].zero();
-                vv[u].zero();
-                pos[u] = -1;
+                st.kk[u].zero();
+                st.vv[u].zero();
+                st.pos[u] = -1;
                 if (p < k1) {
                     const uint32_t pg = c.by_P((uint32_t)p), slot = (uint32_t)p - pg * c.P;
                     const T* kp = keys[pg - (uint32_t)first_page];
                     if (kp) {
-                        pos[u] = p;
+                        st.pos[u] = p;
                         if (live) {
                             const uint32_t at = slot * (uint32_t)c.h + sub * kE;
-                            kk[u].load(in_global(kp) + at);
-                            vv[u].load(in_global(values[pg - (uint32_t)first_page]) + at);
+                            st.kk[u].load(in_global(kp) + at);
+                            st.vv[u].load(in_global(values[pg - (uint32_t)first_page]) + at);
                         }
                     }
                 }
             }
+        };
+        Step now, ahead;
+        if (kAhead) fetch(k0, ahead);
+        for (int k = k0; k < k1; k += STEP) {
+            if (kAhead) {
+                now = ahead;
+                if (k + STEP < k1) fetch(k + STEP, ahead);
+            } else {
+                fetch(k, now);
+            }
+            const auto& kk = now.kk;
+            const auto& vv = now.vv;
+            const auto& pos = now.pos;
+            // Every row sees every key of the step: nothing to mask.  (Four rows: both forms together take more registers than three wavefronts have, 148 -> 155 us.)
+            const bool plain = R < 4 && !gone && k + STEP <= k1 && k + STEP - 1 <= least_upto && k > most_from;
             float score[kUnroll][R];
 #pragma unroll
             for (int u = 0; u < kUnroll; u++) {
@@ -320,8 +456,14 @@ __global__ void __launch_bounds__(kWaves * 64) attend_kernel(Attend a) {
 #pragma unroll
                     for (int i = 0; i < kE; i++) d = fmaf(f[i], q[r][i], d);
                     d = lanes_sum<LPK>(d);
-                    score[u][r] = pos[u] >= 0 && pos[u] <= upto[r] && pos[u] > from[r] ? d : kNegInf;
+                    score[u][r] = d;
                 }
+            }
+            if (!plain) {
+#pragma unroll
+                for (int u = 0; u < kUnroll; u++)
+#pragma unroll
+                    for (int r = 0; r < R; r++) score[u][r] = pos[u] >= 0 && pos[u] <= upto[r] && pos[u] > from[r] ? score[u][r] : kNegInf;
             }
 #pragma unroll
             for (int r = 0; r < R; r++) {
@@ -344,11 +486,19 @@ __global__ void __launch_bounds__(kWaves * 64) attend_kernel(Attend a) {
             for (int u = 0; u < kUnroll; u++) {
                 float f[kE];
                 vv[u].get(f);
+                if (plain) {
 #pragma unroll
-                for (int r = 0; r < R; r++) {
-                    const bool sees = pos[u] >= 0 && pos[u] <= upto[r] && pos[u] > from[r];
+                    for (int r = 0; r < R; r++)
 #pragma unroll
-                    for (int i = 0; i < kE; i++) acc[r][i] = sees ? fmaf(score[u][r], f[i], acc[r][i]) : acc[r][i];
+                        for (int i = 0; i < kE; i++) acc[r][i] = fmaf(score[u][r], f[i], acc[r][i]);
+                } else {
+                    // (a weight of zero is no mask in front of an infinity)
+#pragma unroll
+                    for (int r = 0; r < R; r++) {
+                        const bool sees = pos[u] >= 0 && pos[u] <= upto[r] && pos[u] > from[r];
+#pragma unroll
+                        for (int i = 0; i < kE; i++) acc[r][i] = sees ? fmaf(score[u][r], f[i], acc[r][i]) : acc[r][i];
+                    }
                 }
             }
         }
@@ -388,7 +538,7 @@ __global__ void __launch_bounds__(kWaves * 64) attend_kernel(Attend a) {
             f[w] = exp2f(part[w][r][LPK * kE] - base);
             s += f[w] * part[w][r][LPK * kE + 1];
         }
-        const int tok = (r0 + r) / G, head = j * G + (r0 + r) % G;
+        const int tok = (int)by_G((uint32_t)(r0 + r)), head = j * G + r0 + r - tok * G;
         if (grp == 0 && live) {
             float x[kE];
 #pragma unroll
@@ -752,10 +902,14 @@ __global__ void __launch_bounds__(256) join_kernel(Attend a, int R, int step) {
     if (g.per >= g.hi - g.lo) return;                  // nothing to join
     const int n = (int)((uint32_t)(g.hi - g.lo + g.per - 1) / (uint32_t)g.per), pitch = c.h + 2;
     const float* p = a.partial + (((int64_t)b * c.z.n1 + tok) * c.N_h + head) * a.splits * pitch;
-    // a lane knows a split's maximum and sum (there are at most 64)
-    const float mine = lane < n ? p[lane * pitch + c.h] : kNegInf, sum = lane < n ? p[lane * pitch + c.h + 1] : 0.f;
-    const float m = wave_max(mine), f = exp2f(mine - (m == kNegInf ? 0.f : m));
-    const float s = wave_sum(f * sum);
+    // a lane knows the maxima and sums of two splits
+    static_assert(kMostSplits <= 128, "two to a lane");
+    const int l2 = lane + 64;
+    const float m1 = lane < n ? p[lane * pitch + c.h] : kNegInf, m2 = l2 < n ? p[l2 * pitch + c.h] : kNegInf;
+    const float s1 = lane < n ? p[lane * pitch + c.h + 1] : 0.f, s2 = l2 < n ? p[l2 * pitch + c.h + 1] : 0.f;
+    const float m = wave_max(fmaxf(m1, m2)), base = m == kNegInf ? 0.f : m;
+    const float f1 = exp2f(m1 - base), f2 = exp2f(m2 - base);
+    const float s = wave_sum(f1 * s1 + f2 * s2);
     T* o = row_at<T>(a.out, head * c.h, tok, b);
     for (int i0 = 0; i0 < c.h; i0 += 64) {
         const int i = min(i0 + lane, c.h - 1);
@@ -767,7 +921,7 @@ __global__ void __launch_bounds__(256) join_kernel(Attend a, int R, int step) {
 #pragma unroll
             for (int k = 0; k < 8; k++) {
                 const int at = k0 + D * k;
-                x += at < n ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), at)) * v[k] : 0.f;
+                x += at < n ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(at < 64 ? f1 : f2), at & 63)) * v[k] : 0.f;
             }
         }
         if constexpr (kSpread) {
@@ -838,6 +992,9 @@ Cache cache_of(const nnt_cache_cfg* cfg, nnt_tensor* QKV, nnt_tensor* K, nnt_ten
 }
 
 // How the rows and keys of a call are cut.
+#ifndef WANT
+#define WANT(R) ((R) == 4 ? 1024 : (R) == 2 ? 1024 : 2048)
+#endif
 struct Cut {
     int R, lpk, step, chunks, splits, tile;      // tile: 0, or WR of the matrix cores' kernel
 };
@@ -852,12 +1009,17 @@ Cut cut_of(const nnt_cache_cfg* cfg, const nnt_tensor* QKV, const nnt_tensor* K)
     u.step = u.tile ? (u.tile == 1 ? 128 : 64) : kWaves * (64 / u.lpk) * kUnroll;
     u.chunks = (int)((rows + u.R - 1) / u.R);
     // about eight workgroups to a compute unit, three of the matrix cores' kernel
-    const int64_t pairs = (int64_t)u.chunks * cfg->N_kv * N_b, wanted = u.tile ? 768 : 2048;
-    const int64_t most = ((int64_t)cfg->max_pages * K->base[1] + u.step - 1) / u.step;
+    const int64_t pairs = (int64_t)u.chunks * cfg->N_kv * N_b, wanted = u.tile ? 768 : WANT(u.R);
+    // (no more than the longest range of keys has steps)
+    const int64_t keys = std::min((int64_t)cfg->max_pages * K->base[1], cfg->window ? (int64_t)cfg->window + QKV->shape[1] : INT64_MAX);
+    const int64_t most = (keys + u.step - 1) / u.step;
     u.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(wanted + pairs - 1) / pairs, most, kMostSplits}));
     return u;
 }
 
+using AppendFn = void (*)(Cache, Divide, Divide);
+template <typename T>
+AppendFn append_instance(bool halves, bool turn) { return !halves ? append_kernel<T> : turn ? append_halves_kernel<T, true> : append_halves_kernel<T, false>; }
 using AttendFn = void (*)(Attend);
 template <typename T, int LPK>
 AttendFn attend_rows(int R) { return R == 1 ? attend_kernel<T, LPK, 1> : R == 2 ? attend_kernel<T, LPK, 2> : attend_kernel<T, LPK, 4>; }
@@ -916,9 +1078,10 @@ int32_t nnt_cache_append(nnt_ctx* ctx, const nnt_cache_cfg* cfg, nnt_tensor* QKV
     return entry(ctx, [&]() -> int32_t {
         TRY(cache_check(ctx, cfg, QKV, K, V, nullptr));
         const Cache c = cache_of(cfg, QKV, K, V);
-        const int64_t per_seq = (int64_t)(c.h / kE) * c.N_kv * c.z.n1;
+        const bool halves = c.h % (2 * kE) == 0 && (!c.rot || (c.rot_whole && !c.rot_pairs && c.rot_r == c.h));
+        const int64_t per_head = c.h / kE / (halves ? 2 : 1), per_seq = per_head * c.N_kv * c.z.n1;
         if (per_seq > INT32_MAX - 256) return fail(ctx, NNT_EINVAL, "nnt_cache_append: too many tokens of too many heads in one call");
-        const Divide by_token = divide_by((uint32_t)(c.h / kE * c.N_kv)), by_head = divide_by((uint32_t)(c.h / kE));
+        const Divide by_token = divide_by((uint32_t)(per_head * c.N_kv)), by_head = divide_by((uint32_t)per_head);
         const dim3 grid((unsigned)((per_seq + 255) / 256), (unsigned)c.z.n2);
         const bool bf16 = K->dtype == NNT_BF16;
         std::vector<Access> acc;
@@ -928,8 +1091,7 @@ int32_t nnt_cache_append(nnt_ctx* ctx, const nnt_cache_cfg* cfg, nnt_tensor* QKV
         if (cfg->rotation) acc.push_back(cfg->rotation->all(kRead));
         OpTag tag(ctx, "cache_append", 4.0 * (double)c.N_kv * c.h * c.z.n1 * c.z.n2 * (double)K->elem_size(), true);
         TRY(submit(ctx, acc, [&](hipStream_t st) {
-            if (bf16) hipLaunchKernelGGL(append_kernel<bf16_t>, grid, dim3(256), 0, st, c, by_token, by_head);
-            else hipLaunchKernelGGL(append_kernel<float>, grid, dim3(256), 0, st, c, by_token, by_head);
+            hipLaunchKernelGGL(bf16 ? append_instance<bf16_t>(halves, c.rot) : append_instance<float>(halves, c.rot), grid, dim3(256), 0, st, c, by_token, by_head);
             return launched();
         }));
         K->whole_submitted();
@@ -950,6 +1112,8 @@ int32_t nnt_cache_attention(nnt_ctx* ctx, const nnt_cache_cfg* cfg, float scale,
         a.scale = scale * kLog2e;
         a.splits = u.splits;
         a.chunks = u.chunks;
+        a.by_G = divide_by((uint32_t)(cfg->N_h / cfg->N_kv));
+        a.by_kv = divide_by((uint32_t)cfg->N_kv);
         const bool bf16 = K->dtype == NNT_BF16;
         const AttendFn fn = bf16 ? attend_instance<bf16_t>(u, a.c.h, a.c.rot) : attend_instance<float>(u, a.c.h, a.c.rot);
         const dim3 grid((unsigned)u.splits, (unsigned)(u.chunks * a.c.N_kv), (unsigned)a.c.z.n2);
