@@ -479,13 +479,17 @@ __device__ __forceinline__ void answer(const Sample& a, const Shared<NT>& sh, fl
 }
 
 // ---------------------------------------------------------------- any column
+constexpr int kMostListed = 512;              // top_k up to which the threads' largest logits are asked
 struct Parts {
     union {
         struct {
             unsigned long long mass[kBins];
             uint32_t count[kBins];
         } h;
-        unsigned long long list[kList];
+        struct {
+            unsigned long long list[kList];
+            unsigned long long weight[kMostListed];
+        };
     };
 };
 
@@ -627,20 +631,20 @@ __device__ __forceinline__ void select(const Column_<T, NT>& h, Parts& sp, float
 
 // top-k by the threads' largest logits (`mine`); the k largest are left sorted in the list.  false: more than a list of candidates.
 template <typename T, int NT>
-__device__ __forceinline__ bool list_top_k(const Column_<T, NT>& h, Parts& sp, float mine, int k, Cut& cut) {
+__device__ __forceinline__ bool list_top_k(const Column_<T, NT>& h, Parts& sp, float mine, int k) {
     constexpr int V = Column_<T, NT>::V;
     Shared<NT>& sh = h.sh;
-    // the k-th largest of NT numbers, to 20 of its key's bits (a lower one does as well)
+    // the k-th largest of NT numbers, to 16 of its key's bits (a lower one does as well)
     const uint32_t key = key_of(mine + 0.f);
     uint32_t least = 0;
-    for (int bit = 31; bit >= 12; bit--) {
+    for (int bit = 31; bit >= 16; bit--) {
         const uint32_t t = least | (1u << bit);
         if (__syncthreads_count(key >= t) >= k) least = t;
     }
     const float bound = fmaxf(of_key(max(least, key_of(kNegInf))), -3.402823466e38f);
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
-    h.template all_rows<2>([&](int f, const RawVec<T>& v) {
+    h.template all_rows<4>([&](int f, const RawVec<T>& v) {
         bool any = false;
 #pragma unroll
         for (int j = 0; j < V; j++) any = any || h.value(v, j) >= bound;
@@ -660,10 +664,38 @@ __device__ __forceinline__ bool list_top_k(const Column_<T, NT>& h, Parts& sp, f
     if (n > kList) return false;
     __syncthreads();
     sort_list<NT>(sp.list, n);
-    if (n >= k) cut = cut_at<NT>(sp.list, k - 1);
     sh.n = min(n, k);
     __syncthreads();
     return true;
+}
+
+// The draw from the first n of a sorted list (n <= kMostListed): each entry's place in the order of the numbers is the sum of the weights with numbers up to its own.
+template <typename T, int NT>
+__device__ __forceinline__ void draw_listed(const Column_<T, NT>& h, Parts& sp, int n, float u) {
+    Shared<NT>& sh = h.sh;
+    const float least = with_least(h.a, h.top, Cut{kNegInf, 0u, -1}).x;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const float x = logit_of(sp.list[i]);
+        sp.weight[i] = x > least ? h.weight(x) : 0;
+    }
+    if (threadIdx.x == 0) sh.n = -1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const uint32_t number = (uint32_t)sp.list[i];
+        uint64_t all = 0, upto = 0;
+        for (int k = 0; k < n; k++) {
+            const uint64_t w = sp.weight[k];
+            all += w;
+            upto += (uint32_t)sp.list[k] <= number ? w : 0;
+        }
+        const uint64_t to = share_of(u, all);
+        if (upto > to && upto - sp.weight[i] <= to) {
+            sh.n = (int32_t)number;
+            sh.x = logit_of(sp.list[i]);
+        }
+    }
+    __syncthreads();
 }
 
 template <typename T, int NT>
@@ -672,13 +704,24 @@ __device__ __forceinline__ void any_column(const Sample& a, Column_<T, NT>& h, P
     Shared<NT>& sh = h.sh;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     __syncthreads();                                  // the tiles' addresses
-    float mine = kNegInf, mn = kPosInf;
+    // one read for the largest and smallest logit and, each thread shifted by what it has seen so far, the sum of all exponentials
+    float mine = kNegInf, mn = kPosInf, shift = -3.402823466e38f;
+    double sum = 0.0;
     h.template all_rows<4>([&](int, const RawVec<T>& v) {
+        float y[V];
 #pragma unroll
         for (int j = 0; j < V; j++) {
-            const float y = v.at(j);
-            mine = fmaxf(mine, y);
-            if (y > kNegInf) mn = fminf(mn, y);
+            y[j] = v.at(j);
+            mine = fmaxf(mine, y[j]);
+            mn = y[j] > kNegInf ? fminf(mn, y[j]) : mn;
+        }
+        if (a.logp) {
+            float s = 0.f;
+            const float next = fmaxf(shift, mine);
+#pragma unroll
+            for (int j = 0; j < V; j++) s += exp_of(fmaxf(y[j], kNegInf) - next);           // (fmaxf: no NaN)
+            sum = fma(sum, (double)exp_of(shift - next), (double)s);
+            shift = next;
         }
     });
     float mx = wave_max(mine);
@@ -702,41 +745,44 @@ __device__ __forceinline__ void any_column(const Sample& a, Column_<T, NT>& h, P
         mn = 0.f;
         mine = mine == kPosInf ? 0.f : kNegInf;
     }
-    double sum = 0.0;
     if (a.logp) {
-        const float top = h.top;
-        h.template all_rows<2>([&](int, const RawVec<T>& v) {
-            float s = 0.f;
+        if (h.top_inf) {
+            sum = 0.0;
+            h.template all_rows<1>([&](int, const RawVec<T>& v) {
 #pragma unroll
-            for (int j = 0; j < V; j++) s += exp_of(fmaxf(h.value(v, j), -3.402823466e38f) - top);      // (no NaN, and no -infinity in two terms)
-            sum += (double)s;
-        });
+                for (int j = 0; j < V; j++) sum += h.value(v, j) == 0.f ? 1.0 : 0.0;
+            });
+        } else {
+            sum *= (double)exp_of(shift - h.top);
+        }
         sum = wave_sum64(sum);
         if (lane == 0) sh.sum[w] = sum;
     }
     Cut cut{kNegInf, 0u, -1};
+    bool drawn = false;
     if (a.greedy) {
         cut = Cut{h.top, 1u, INT32_MAX};
     } else {
         const float range = h.top - mn;
-        bool listed = false;
+        const float u = random_of(a);
+        auto ends = [&](uint64_t s, uint64_t all) { return (double)s >= a.top_p * (double)all; };
         if (a.top_k > 0 && a.top_k < a.X.shape[0]) {
-            listed = a.top_k <= NT / 2 && list_top_k(h, sp, mine, a.top_k, cut);
-            if (!listed) select<false>(h, sp, range, cut, [&](uint64_t s, uint64_t) { return s >= (uint64_t)a.top_k; });
-        }
-        if (a.top_p < 1.0) {
-            auto ends = [&](uint64_t s, uint64_t all) { return (double)s >= a.top_p * (double)all; };
-            if (listed) {
-                const int n = sh.n;
-                const uint64_t mass = tid < n ? h.weight(logit_of(sp.list[tid])) : 0;
-                find_end<NT, 1>(sh, 0, [&](int) { return mass; }, ends);
-                if (sh.pos >= 0) cut = cut_at<NT>(sp.list, sh.pos);
+            if (a.top_k <= min(kMostListed, NT / 2) && list_top_k(h, sp, mine, a.top_k)) {
+                int n = sh.n;
+                if (a.top_p < 1.0) {
+                    const uint64_t mass = tid < n ? h.weight(logit_of(sp.list[tid])) : 0;
+                    find_end<NT, 1>(sh, 0, [&](int) { return mass; }, ends);
+                    if (sh.pos >= 0) n = sh.pos + 1;
+                }
+                draw_listed(h, sp, n, u);
+                drawn = true;
             } else {
-                select<true>(h, sp, range, cut, ends);
+                select<false>(h, sp, range, cut, [&](uint64_t s, uint64_t) { return s >= (uint64_t)a.top_k; });
             }
         }
+        if (!drawn && a.top_p < 1.0) select<true>(h, sp, range, cut, ends);
     }
-    draw(h, a.greedy ? cut : with_least(a, h.top, cut), a.greedy ? 0.f : random_of(a));
+    if (!drawn) draw(h, a.greedy ? cut : with_least(a, h.top, cut), a.greedy ? 0.f : random_of(a));
     sum = 0.0;
     if (a.logp && tid == 0)
         for (int k = 0; k < NW; k++) sum += sh.sum[k];
