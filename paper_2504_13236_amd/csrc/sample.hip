@@ -823,7 +823,7 @@ struct Codes {
 };
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ float of_bits(uint32_t b) { return __uint_as_float(b << 16); }
-// code of the bits b; without one: some number from kCodes on
+// code of the bits b, if they have one
 __device__ __forceinline__ uint32_t code_of(uint32_t b, bool& has) {
     const uint32_t u = (b & 0x7fffu) - kFirst;
     has = u < kSide;
@@ -975,7 +975,7 @@ __device__ __forceinline__ bool coded_column(const Sample& a, Column_<bf16_t, kC
             bool coded;
             const uint32_t k = code_of(b, coded);
             p[j] = m.weight[coded ? k : kCodes];
-            equal |= k == border ? 1u << j : 0u;
+            equal |= coded && k == border ? 1u << j : 0u;
             odd = odd || !coded;
         }
         if (small_too && __any(odd)) {

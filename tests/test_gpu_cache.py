@@ -291,6 +291,65 @@ def test_a_long_sequence_and_many_short_ones(ctx, dtype):
     run(ctx, dtype, 2, 2, 64, 16, [int(s) for s in np.random.default_rng(5).integers(0, 200, 40)], 1, tiles=(2, 1, 7))
 
 
+# more rows than the vector units take: what the matrix cores' kernel owns, around its borders
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("h", [64, 128])
+@pytest.mark.parametrize("N_h,N_kv,N_s", [(8, 1, 1), (9, 1, 1), (4, 1, 3), (31, 1, 1), (16, 1, 2), (11, 1, 3), (8, 2, 32), (3, 1, 43)])
+def test_rows_around_the_kernels_borders(ctx, dtype, h, N_h, N_kv, N_s):
+    run(ctx, dtype, N_h, N_kv, h, 16, [70, 0, 33], N_s, count=[N_s, N_s, max(1, N_s - 1)], tiles=(2, 5, 2))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rotation", [None, ("halves", 128, 4000), ("pairs", 40, 4000)])
+@pytest.mark.parametrize("N_s,window", [(5, 0), (5, 300), (40, 0), (140, 0), (140, 100)])
+def test_split_keys_of_many_rows(ctx, dtype, rotation, N_s, window):
+    run(ctx, dtype, 4, 1, 128, 20, [2500, 3], N_s, rotation=rotation, window=window)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N_h,N_s", [(4, 3), (4, 20), (1, 150)])
+def test_no_numbers_in_the_keys_and_values_of_later_tokens_of_grouped_heads(ctx, dtype, N_h, N_s):
+    p = Problem(ctx, dtype, N_h, 1, 64, 8, [131, 60], N_s)
+    p.append()
+    p.check_append()
+    p.attention()
+    before = p.tB.download()
+    half = N_s // 2
+    Z = p.QKV.copy()
+    Z[N_h * 64:(N_h + 1) * 64, half:] = -np.inf
+    Z[(N_h + 1) * 64:, half::2] = np.inf
+    Z[(N_h + 1) * 64 + 5, half:] = np.nan
+    p.tQKV.upload(Z)
+    p.append()
+    p.attention()
+    after = p.tB.download()
+    assert np.array_equal(after[:, :half], before[:, :half])
+    p.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N_s", [1, 12, 80])
+def test_no_numbers_that_are_seen(ctx, dtype, N_s):
+    """An infinity and a NaN among the values reach the rows that see them, in their component, and no other row or component."""
+    p = Problem(ctx, dtype, 2, 2, 64, 8, [40, 20], N_s)
+    p.append()
+    p.attention()
+    want = p.tB.download().reshape(2, 64, N_s, 2)
+    V = p.tV.download()
+    last = 40 + N_s // 2
+    V[3, R.slot_of(17, 0, p.pages, 8, 99), 1] = np.inf
+    V[9, R.slot_of(last, 0, p.pages, 8, 99), 1] = np.nan
+    p.tV.upload(V)
+    p.attention()
+    got = p.tB.download().reshape(2, 64, N_s, 2)
+    assert np.array_equal(got[0], want[0]) and np.array_equal(got[..., 1], want[..., 1])
+    assert np.isposinf(got[1, 3, :, 0]).all()
+    assert np.isnan(got[1, 9, last - 40:, 0]).all() and np.array_equal(got[1, 9, :last - 40, 0], want[1, 9, :last - 40, 0])
+    others = [i for i in range(64) if i not in (3, 9)]
+    assert np.array_equal(got[1, others], want[1, others])
+    p.close()
+
+
 def test_counts_outside_the_call(ctx):
     run(ctx, "f32", 2, 2, 32, 8, [9, 0, 30], 4, count=[-5, 100, 2])
 

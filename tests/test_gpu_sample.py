@@ -234,3 +234,83 @@ def test_refusals(ctx):
     assert (tokens[:6] == 0).all() and (tokens[6:] == -5).all()
     for t in (X, flat, holes):
         t.close()
+
+
+def odd_columns(r, N_v):
+    """bf16 columns of what has no code of its own, one kind each: zeros of both signs, tiny ones, masked ones, large ones."""
+    def base(std=2.0):
+        return std * r.standard_normal(N_v)
+    cols = {}
+    x = base()
+    x[::2] = 0.0
+    x[1::4] = -0.0
+    cols["zeros"] = x
+    x = -np.abs(base()) - 0.1
+    x[::3] = 0.0
+    cols["zeros on top"] = x
+    cols["all zero"] = np.where(np.arange(N_v) % 3 == 1, -0.0, 0.0)
+    x = base()
+    x[r.integers(0, N_v, 300)] = 1e-5 * r.standard_normal(300)
+    cols["some tiny"] = x
+    cols["all tiny"] = 1e-4 * base()
+    x = -np.abs(base(0.5)) - 0.01
+    x[100:160] = 1e-6 * r.standard_normal(60)
+    cols["tiny on top"] = x
+    x = base()
+    x[500:] = -1e4
+    cols["masked by -1e4"] = x
+    x = base()
+    x[: N_v - 40] = -np.inf
+    cols["masked by -inf"] = x
+    cols["all negative"] = -np.abs(base()) - 3.0
+    cols["all below the codes"] = -300.0 - np.abs(base(20.0))
+    x = base(60.0)
+    x[7] = 300.0
+    cols["above the codes"] = x
+    x = base()
+    x[11], x[12] = 1e30, np.nan
+    cols["far above"] = x
+    cols["wide"] = base(50.0)
+    cols["narrow"] = 5.0 + 0.01 * base()
+    return cols
+
+
+@pytest.mark.parametrize("filters", [dict(), dict(temperature=0.0), dict(top_k=30), dict(top_k=6000), dict(top_p=0.9), dict(top_p=0.3, temperature=3.0), dict(min_p=0.5),
+                                     dict(top_k=5000, top_p=0.97, min_p=1e-4), dict(temperature=200.0), dict(temperature=200.0, top_p=0.8), dict(temperature=0.01, top_k=100)],
+                         ids=lambda f: "_".join("%s%g" % kv for kv in f.items()) or "none")
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_what_has_no_code(ctx, dtype, filters):
+    r = np.random.default_rng(77)
+    cols = odd_columns(r, 12345)
+    X = quant(np.stack(list(cols.values()), 1), dtype)
+    u = r.random(X.shape[1]).astype(np.float32)
+    check(X, u, draw(ctx, X, u, dtype, tile_v=5000, **filters), **filters)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_borders_of_the_lists(ctx, dtype):
+    """top-k at the ends of what is listed, and thousands of equal logits on top of it."""
+    r = np.random.default_rng(5)
+    X = quant(2.0 * r.standard_normal((20000, 6)), dtype)
+    X[:, 1] = np.where(r.random(20000) < 0.3, 4.0, X[:, 1])
+    X[:, 2] = np.where(r.random(20000) < 0.101, 50.0, X[:, 2])
+    X[:, 3] = np.round(X[:, 3])
+    u = r.random(6).astype(np.float32)
+    for k in (1, 2, 511, 512, 513, 1024, 2048, 2049, 19999, 20000, 20001):
+        for more in (dict(), dict(top_p=0.6)):
+            f = dict(top_k=k, **more)
+            check(X, u, draw(ctx, X, u, dtype, tile_v=20000, **f), **f)
+
+
+def test_many_columns_of_many_kinds(ctx):
+    """More columns than the chip takes at once, of both types, against each other's neighbours: nothing of a column reaches another."""
+    r = np.random.default_rng(6)
+    for dtype in ("bf16", "f32"):
+        X = quant((1.0 + 3.0 * r.random(1200)) * r.standard_normal((9000, 1200)), dtype)
+        X[:, ::7] = np.round(X[:, ::7])
+        u = r.random(1200).astype(np.float32)
+        f = dict(top_p=0.85, temperature=0.9)
+        tokens, logp = draw(ctx, X, u, dtype, tile_v=4096, tiles=(1, 500), **f)
+        pick = r.integers(0, 1200, 60)
+        check(X[:, pick], u[pick], (tokens[pick], logp[pick]), **f)
+        assert (tokens >= 0).all() and (tokens < 9000).all()
