@@ -20,7 +20,7 @@
  *  - The caller owns all tile memory.  On the device the library allocates only
  *    (a) descriptor tables: the tile-pointer table of every tensor, the tables of
  *    cached product plans and of grouped optimiser steps; (b) the fp32 scratch of
- *    the two-stage column sums, shared and one part per stream (grows on demand, at
+ *    the two-stage sums and of the attention over a cache, shared and one part per stream (grows on demand, at
  *    least 4 MiB each once used; a smaller one that it replaces stays as long as a
  *    graph lives that was captured with it); (c)
  *    for products whose contraction is cut into k-slices, an fp32 workspace of
@@ -568,7 +568,7 @@ NNT_API int32_t nnt_cache_append(nnt_ctx* ctx, const nnt_cache_cfg* cfg, nnt_ten
  *   B[i,s,b,j] = sum_k V[i,k] P[k],  P = softmax over k of scale * sum_i K[i,k] rot(Q)[i,s,b,j],
  * over the positions k <= start[b] + s (and > start[b] + s - window) whose page is there; a query that sees none gives zeros.  Columns of
  * tokens that are not new (s >= count[b]) are left as they are.  QKV as above (only the queries are read), B: [N_h * h, N_s, N_b],
- * row tiles of whole heads.  What is masked does not enter, infinities and NaN there included.  scale > 0.  The keys of long sequences are split over workgroups, whose
+ * row tiles of whole heads, not K or V.  What is masked does not enter, infinities and NaN there included.  scale > 0.  The keys of long sequences are split over workgroups, whose
  * partial results meet in the context's per-stream scratch (at most N_s * N_b * N_h * (h + 2) * 128 floats), which must exist before a graph
  * capture (run the call once). */
 NNT_API int32_t nnt_cache_attention(nnt_ctx* ctx, const nnt_cache_cfg* cfg, float scale, nnt_tensor* QKV, nnt_tensor* K,
@@ -786,7 +786,7 @@ NNT_API int32_t nnt_gpt2_stack_forward_cached(nnt_gpt2_stack* st, const nnt_cach
  * the model keeps pointers, not ownership.
  *   parameters (fp32 masters): W_te [N_e, N_v] (one column per vocabulary item,
  *   tiled tile_e x tile_v), W_pe [N_e, N_s] (one column per position; a tensor of more
- *   columns, with any tiling of them, is taken too, so that a model of short N_s generates with the embeddings of
+ *   columns, with any tiling of them, is taken too, with gradients, moments and copy like it, so that a model of short N_s generates with the embeddings of
  *   the trained one), gain and bias of the final layer norm [N_e]; + NNT_MDL_GRAD their gradients, +
  *   NNT_MDL_ADAM_M / _V their Adam moments; NNT_MDL_LOWP + {0, 1}: bf16 copies of
  *   W_te, W_pe (bf16 models only).

@@ -616,6 +616,11 @@ int32_t nnt_gpt2_model_create(nnt_ctx* ctx, const nnt_gpt2_block_cfg* cfg, int64
             return fail(ctx, NNT_EINVAL, "nnt_gpt2_model_create: tensor of slot " + std::to_string(i) + " has the wrong type, shape or tiling");
         }
     }
+    for (int i = NNT_MDL_WPE; i < (cfg->dtype == NNT_BF16 ? NNT_MDL_XPOS : NNT_MDL_LOWP); i += 4)
+        if (nnt_tensor* t = m->s[i]; t && !same_tiling(t, m->s[NNT_MDL_WPE])) {
+            delete m;
+            return fail(ctx, NNT_EINVAL, "nnt_gpt2_model_create: position embeddings, their gradients, moments and bf16 copy must be equally long and equally tiled");
+        }
     *out = m;
     return NNT_OK;
 }

@@ -242,6 +242,27 @@ def test_refusals():
         close(step, whole)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_position_embeddings_have_gradients_like_them(dtype):
+    from paper_2504_13236_amd import capi, tiled
+    with tiled.Context(n_streams=1) as ctx:
+        whole = make(ctx, dtype, 8, 2)
+        step = make(ctx, dtype, 1, 2, share=whole)
+        short = tiled.TiledTensor.zeros(ctx, (whole.N_e, 1), (step.slots[capi.NNT_MDL_WPE].base[0], 1))
+        others = [capi.NNT_MDL_WPE + k for k in (capi.NNT_MDL_GRAD, capi.NNT_MDL_ADAM_M, capi.NNT_MDL_ADAM_V)]
+        if dtype == "bf16":
+            others.append(capi.NNT_MDL_LOWP + capi.NNT_MDL_WPE)
+        for slot in others:
+            slots = list(step.slots)
+            slots[slot] = short if slot < capi.NNT_MDL_LOWP else tiled.TiledTensor.zeros(ctx, (whole.N_e, 1), (short.base[0], 1), "bf16")
+            h = C.c_void_p()
+            assert capi.nnt_gpt2_model_create.raw(ctx.h, C.byref(step.blocks[0].cfg), N_V, 24, step.stack.h,
+                                                  capi.ptr_array([t.h.value if t is not None else None for t in slots]), C.byref(h)) == capi.NNT_EINVAL, slot
+            if slots[slot] is not short:
+                slots[slot].close()
+        short.close()
+        close(step, whole)
+
 def test_pages_are_handed_out_and_taken_back():
     from paper_2504_13236_amd import tiled
     with tiled.Context(n_streams=1) as ctx:
