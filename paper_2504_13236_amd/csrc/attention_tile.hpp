@@ -146,9 +146,9 @@ template <int H_> struct Bf16Traits {
         return d;
     }
     template <int LDX>
-    static __device__ __forceinline__ f32x16 rows_times_own(const T* lds, int sub, int ln, int hh, const Own& o) {
+    static __device__ __forceinline__ f32x16 rows_times_own(const T* lds, int sub, int ln, int hh, const Own& o, const f32x16& more = zero16()) {
         const T* p = lds + (32 * sub + ln) * LDX + 8 * hh;
-        f32x16 acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(p), o.v[0], zero16(), 0, 0, 0);
+        f32x16 acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(p), o.v[0], more, 0, 0, 0);
 #pragma unroll
         for (int s = 1; s < H / 16; s++)
             acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(p + 16 * s), o.v[s], acc, 0, 0, 0);

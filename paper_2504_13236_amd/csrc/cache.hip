@@ -5,6 +5,10 @@
 //   attention  B = sum_k V[k] P[k],  P = softmax_k(scale K[k] . rot_p q),  k <= p  (and > p - window)
 //
 // A page is a tile (h, P, N_kv) of the cache's tensors: what one cached head reads of it is contiguous.
+//
+// The append is a copy; 58 MB take 17 us.  The attention reads what a (sequence, cached head) pair has cached once for all query rows of the pair, up to 128 of them,
+// and is bound by that read while there are few: 510 MB of 64 sequences, one row each, 84 us; 535 MB of one sequence, four rows, 109 us (a large copy's rate would
+// be 103 and 108).  Long axes are split over workgroups, whose partial results a second kernel joins; short calls (4.5 us for 100 keys) are launches.
 #include "attention_tile.hpp"
 #include "device_util.hpp"
 #include "internal.hpp"
@@ -192,7 +196,7 @@ __global__ void __launch_bounds__(256) append_kernel(Cache c, Divide by_token, D
 }
 
 // The same where nothing is turned, or all of a head by halves in whole vectors: a thread has eight components of each half, so that what is turned
-// together, and its angles, is read once.  Eight prompts of up to 1024 tokens of 12 heads of 64 in fp32, turned: APPEND_FIGURE.
+// together, and its angles, is read once.  Eight prompts of up to 1024 tokens of 12 heads of 64 in fp32 (58 MB moved), turned: 19 -> 17 us.
 template <typename T, bool kTurn>
 __global__ void __launch_bounds__(256) append_halves_kernel(Cache c, Divide by_token, Divide by_head) {
     const uint32_t at = blockIdx.x * 256 + threadIdx.x, s = by_token(at), k = at - s * by_token.d, j = by_head(k);
@@ -565,23 +569,23 @@ __global__ void __launch_bounds__(kWaves * 64, R == 4 ? (sizeof(T) == 2 ? 3 : 2)
 }
 
 // ---------------------------------------------------------------- many rows: on the matrix cores
-// The workgroup owns 32 WR rows, 32 to a wavefront (WR = 4), or 32 in all, of which each wavefront sees a quarter of the keys (WR = 1), and streams blocks
-// of keys and values through LDS, the next one on its way to registers while the products run.  Products and statistics as in the fused
-// attention: scores are a 32 x 32 accumulator, lane = row, whose layout is that of the operand of the product with the values.
+// The workgroup owns 128 rows, 32 to a wavefront, and streams blocks of 64 keys and values through LDS, the next one on its way to registers while the
+// products run.  Products and statistics as in the fused attention: scores are a 32 x 32 accumulator, lane = row, whose layout is that of the
+// operand of the product with the values.
 //   A turned query has more bits than bf16: it is kept in two bf16 parts, and the scores are two products.  Weights are rounded to the type for the product
 //   with the values (half a step of each, 2^-8 of its own share of the result), as in the fused attention.
 //   Masked weights are zeros, but a zero times an infinity is none: in blocks that some row sees in part, values that are no numbers are
 //   taken out (`odd`), and given afterwards to the rows that see them.
-constexpr int kTileTable = 256;  // (two workgroups of 128 components and 128 keys just fit a unit's LDS)
-template <class X, int WR>
+// A wavefront without rows only brings keys and values: with two rows, bound by memory like with 128, it still beats the vector units (cut_of says where).
+constexpr int kTileTable = 256;
+template <class X>
 struct TileShape {
-    static constexpr int kKeys = WR == 1 ? 128 : 64;          // keys of a block
+    static constexpr int kKeys = 64;                          // keys of a block
     static constexpr int kRowVecs = X::H / X::kPer;
     static constexpr int kVec = kKeys * kRowVecs / 256;       // vectors of a thread, of the keys and of the values
-    static constexpr int kRows = 32 * WR;
-    static constexpr int kLds = kKeys * (X::LD + X::LD_COLS) * (int)sizeof(typename X::T);
-    static constexpr int kMeet = (X::H / 2 + 2) * 2 * 64 * 4; // what two wavefronts hand to two others
-    static constexpr int kBytes = WR == 1 && kMeet > kLds ? kMeet : kLds;
+    static constexpr int kRows = 128;
+    // workgroups of a unit, by registers: what is on its way to them decides
+    static constexpr int kResident = sizeof(typename X::T) == 4 ? (X::H == 128 ? 1 : 2) : X::H == 128 ? 2 : 3;
 };
 
 // this lane's row, as the products take it; its second part where it is turned
@@ -635,13 +639,13 @@ __device__ __forceinline__ bool take_out(uint4& v) {
     return odd;
 }
 
-// TURN: queries are turned.  (fp32 of 128 components: one workgroup to a unit, its blocks on their way take too many registers for two.)
-template <class X, int WR, bool TURN>
-__global__ void __launch_bounds__(256, sizeof(typename X::T) == 4 && X::H == 128 ? 1 : 2) attend_tile_kernel(Attend a) {
+// TURN: queries are turned.
+template <class X, bool TURN>
+__global__ void __launch_bounds__(256, TileShape<X>::kResident) attend_tile_kernel(Attend a) {
     using T = typename X::T;
-    using S = TileShape<X, WR>;
+    using S = TileShape<X>;
     constexpr int H = X::H, LDK = X::LD, LDV = X::LD_COLS, KEYS = S::kKeys;
-    __shared__ __attribute__((aligned(16))) char lds[S::kBytes];
+    __shared__ __attribute__((aligned(16))) char lds[KEYS * (LDK + LDV) * sizeof(T)];
     __shared__ const T* keys[kTileTable];
     __shared__ const T* values[kTileTable];
     __shared__ int odd_block;
@@ -664,7 +668,7 @@ __global__ void __launch_bounds__(256, sizeof(typename X::T) == 4 && X::H == 128
     if (lo >= hi && !(alone && split == 0)) return;
 
     // this lane's row, and what this wavefront's rows see at least and at most
-    const int first = WR == 1 ? 0 : 32 * w, own = first + ln;
+    const int first = 32 * w, own = first + ln;
     const int tok = (r0 + own) / G, head = j * G + (r0 + own) % G;
     const int64_t pos = (int64_t)start + tok;
     const bool there = own < rows && pos >= 0 && (!c.rot || pos < c.rot_n);
@@ -742,18 +746,12 @@ __global__ void __launch_bounds__(256, sizeof(typename X::T) == 4 && X::H == 128
             const bool more = i + 1 < blocks;
             if (more) fetch(block(i + 1));
             const bool odd = odd_block != 0;
-            // WR = 4: both halves of the block; WR = 1: the wavefront's quarter of it
 #pragma unroll
-            for (int h2 = 0; h2 < (WR == 1 ? 1 : 2); h2++) {
-                const int part = WR == 1 ? w : h2;
+            for (int part = 0; part < 2; part++) {
                 const int kb = k + 32 * part;
                 if (!w_any || kb >= k1 || kb > w_last || (c.window > 0 && kb + 31 <= w_first - c.window)) continue;
                 f32x16 s = X::template rows_times_own<LDK>(Ks, part, ln, hh, q);
-                if constexpr (sizeof(T) == 2 && TURN) {
-                    const f32x16 s2 = X::template rows_times_own<LDK>(Ks, part, ln, hh, rest);
-#pragma unroll
-                    for (int r = 0; r < 16; r++) s[r] += s2[r];
-                }
+                if constexpr (sizeof(T) == 2 && TURN) s = X::template rows_times_own<LDK>(Ks, part, ln, hh, rest, s);
                 uint32_t seen = 0xffffu;
                 if (!(all_there && kb + 32 <= k1 && kb + 31 <= w_first && (c.window == 0 || kb > w_last - c.window))) {
                     const int end = min(upto + 1, k1);
@@ -836,32 +834,6 @@ __global__ void __launch_bounds__(256, sizeof(typename X::T) == 4 && X::H == 128
         lsum = 0.f;
 #pragma unroll
         for (int rb = 0; rb < H / 32; rb++) O[rb] = zero16();
-    }
-    if constexpr (WR == 1) {
-        // the wavefronts' partial results of the same rows meet: 2 and 3 hand theirs to 0 and 1, then 1 to 0
-        constexpr int N = H / 2 + 2;
-        float* buf = reinterpret_cast<float*>(lds);
-#pragma unroll
-        for (int left = 2; left >= 1; left >>= 1) {
-            __syncthreads();
-            if (w >= left && w < 2 * left) {
-#pragma unroll
-                for (int i = 0; i < N; i++) buf[((w - left) * N + i) * 64 + lane] = i < H / 2 ? O[i / 16][i % 16] : i == H / 2 ? m : lsum;
-            }
-            __syncthreads();
-            if (w < left) {
-                const float* got = buf + w * N * 64 + lane;
-                const float m2 = got[(H / 2) * 64], m_new = fmaxf(m, m2);
-                const float f1 = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * a.scale), f2 = m2 == kNegInf ? 0.f : __builtin_amdgcn_exp2f((m2 - m_new) * a.scale);
-                lsum = lsum * f1 + got[(H / 2 + 1) * 64] * f2;
-                m = m_new;
-#pragma unroll
-                for (int rb = 0; rb < H / 32; rb++)
-#pragma unroll
-                    for (int r = 0; r < 16; r++) O[rb][r] = O[rb][r] * f1 + got[(16 * rb + r) * 64] * f2;
-            }
-        }
-        if (w > 0) return;
     }
     if (own >= rows) return;
     if (alone) {
@@ -991,29 +963,35 @@ Cache cache_of(const nnt_cache_cfg* cfg, nnt_tensor* QKV, nnt_tensor* K, nnt_ten
     return c;
 }
 
-// How the rows and keys of a call are cut.
-#ifndef WANT
-#define WANT(R) ((R) == 4 ? 1024 : (R) == 2 ? 1024 : 2048)
-#endif
+// How the rows (queries that share a cached head of a sequence) and keys of a call are cut.
 struct Cut {
-    int R, lpk, step, chunks, splits, tile;      // tile: 0, or WR of the matrix cores' kernel
+    int R, lpk, step, chunks, splits;
+    bool tile;
 };
+// With heads of 64 or 128 the matrix cores take two rows or more of bf16 and 17 of fp32 (us, vector units -> matrix cores; one sequence of 131072 keys
+// of 8 cached heads of 128, 64 sequences of 2048 of 12 of 64):
+//   bf16, 1 row 106 -> 107 and 81 -> 77 (ragged lengths 84 -> 90, and a short call costs a microsecond more), 2 rows 113 -> 108 and 87 -> 78,
+//   4 rows 139 -> 108 and 108 -> 78, turned 146 -> 116 and 112 -> 79;  fp32, 16 rows 660 -> 660 and 321 -> 366, 32 rows 922 -> 660 and 567 -> 368.
 Cut cut_of(const nnt_cache_cfg* cfg, const nnt_tensor* QKV, const nnt_tensor* K) {
     Cut u;
     const int64_t G = cfg->N_h / cfg->N_kv, rows = G * QKV->shape[1], N_b = QKV->shape[2];
     const int64_t h = K->shape[0];
     const bool bf16 = K->dtype == NNT_BF16;
-    u.tile = h != 64 && h != 128 ? 0 : bf16 ? (rows > 32 ? 4 : rows > 8 ? 1 : 0) : rows >= 32 ? 4 : 0;
-    u.R = u.tile ? 32 * u.tile : rows >= 4 ? 4 : rows >= 2 ? 2 : 1;
+    u.tile = (h == 64 || h == 128) && rows >= (bf16 ? 2 : 17);
+    u.R = u.tile ? 128 : rows >= 4 ? 4 : rows >= 2 ? 2 : 1;
     u.lpk = h <= 32 ? 4 : h <= 64 ? 8 : h <= 128 ? 16 : 32;
-    u.step = u.tile ? (u.tile == 1 ? 128 : 64) : kWaves * (64 / u.lpk) * kUnroll;
+    u.step = u.tile ? 64 : kWaves * (64 / u.lpk) * kUnroll;
     u.chunks = (int)((rows + u.R - 1) / u.R);
-    // about eight workgroups to a compute unit, three of the matrix cores' kernel
-    const int64_t pairs = (int64_t)u.chunks * cfg->N_kv * N_b, wanted = u.tile ? 768 : WANT(u.R);
+    // The keys are split so that the launch fills the chip.  The matrix cores' kernel: with no more workgroups than it holds at a time (bf16, one row chunk of 131072 keys, 128 components:
+    // 512 workgroups 107 us, 768 134); the vector units': eight to a unit, or four that keep more registers (four rows: 768 174 us, 1024 155).
+    const int64_t pairs = (int64_t)u.chunks * cfg->N_kv * N_b;
+    const int64_t held = 256 * (bf16 ? (h == 128 ? TileShape<Bf16Traits<128>>::kResident : TileShape<Bf16Traits<64>>::kResident)
+                                     : (h == 128 ? TileShape<F32Traits<128>>::kResident : TileShape<F32Traits<64>>::kResident));
+    const int64_t wanted = u.tile ? held / pairs : ((u.R == 1 ? 2048 : 1024) + pairs - 1) / pairs;
     // (no more than the longest range of keys has steps)
     const int64_t keys = std::min((int64_t)cfg->max_pages * K->base[1], cfg->window ? (int64_t)cfg->window + QKV->shape[1] : INT64_MAX);
     const int64_t most = (keys + u.step - 1) / u.step;
-    u.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(wanted + pairs - 1) / pairs, most, kMostSplits}));
+    u.splits = (int)std::max<int64_t>(1, std::min<int64_t>({wanted, most, kMostSplits}));
     return u;
 }
 
@@ -1024,16 +1002,13 @@ using AttendFn = void (*)(Attend);
 template <typename T, int LPK>
 AttendFn attend_rows(int R) { return R == 1 ? attend_kernel<T, LPK, 1> : R == 2 ? attend_kernel<T, LPK, 2> : attend_kernel<T, LPK, 4>; }
 template <typename T, int H>
-AttendFn attend_tile(int wr, bool turn) {
-    if constexpr (sizeof(T) == 4) return attend_tile_kernel<F32Traits<H>, 4, false>;
-    else if (wr == 1) return turn ? attend_tile_kernel<Bf16Traits<H>, 1, true> : attend_tile_kernel<Bf16Traits<H>, 1, false>;
-    else return turn ? attend_tile_kernel<Bf16Traits<H>, 4, true> : attend_tile_kernel<Bf16Traits<H>, 4, false>;
+AttendFn attend_tile(bool turn) {
+    if constexpr (sizeof(T) == 4) return attend_tile_kernel<F32Traits<H>, false>;
+    else return turn ? attend_tile_kernel<Bf16Traits<H>, true> : attend_tile_kernel<Bf16Traits<H>, false>;
 }
 template <typename T>
 AttendFn attend_instance(const Cut& u, int64_t h, bool turn) {
-    if (u.tile) {
-        return h == 64 ? attend_tile<T, 64>(u.tile, turn) : attend_tile<T, 128>(u.tile, turn);
-    }
+    if (u.tile) return h == 64 ? attend_tile<T, 64>(turn) : attend_tile<T, 128>(turn);
     return u.lpk == 4 ? attend_rows<T, 4>(u.R) : u.lpk == 8 ? attend_rows<T, 8>(u.R) : u.lpk == 16 ? attend_rows<T, 16>(u.R) : attend_rows<T, 32>(u.R);
 }
 
@@ -1102,7 +1077,7 @@ int32_t nnt_cache_append(nnt_ctx* ctx, const nnt_cache_cfg* cfg, nnt_tensor* QKV
 
 int32_t nnt_cache_attention(nnt_ctx* ctx, const nnt_cache_cfg* cfg, float scale, nnt_tensor* QKV, nnt_tensor* K, nnt_tensor* V, nnt_tensor* B) {
     return entry(ctx, [&]() -> int32_t {
-        if (!B) return fail(ctx, NNT_EINVAL, "nnt_cache_attention: null argument");
+        if (!B || B == K || B == V) return fail(ctx, NNT_EINVAL, "nnt_cache_attention: the result must be a tensor of its own");
         TRY(cache_check(ctx, cfg, QKV, K, V, B));
         if (!(scale > 0.f && scale < 1e30f)) return fail(ctx, NNT_EINVAL, "nnt_cache_attention: scale must be positive");
         const Cut u = cut_of(cfg, QKV, K);

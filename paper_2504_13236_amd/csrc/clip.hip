@@ -18,7 +18,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPiece = 16384;          // elements: 64 KB of fp32
 constexpr int kMaxGroups = 2048;       // workgroups of a launch: eight to a compute unit
-constexpr int kFew = 256;              // partial sums that every workgroup of the second pass adds up by itself (the smallest block 13.3 -> CLIP_FIGURE us)
+constexpr int kFew = 256;              // partial sums that every workgroup of the second pass adds up by itself (the smallest block 13.3 -> 11 us)
 constexpr int kListed = 48;            // tensors of a launch: their geometry travels in its arguments (4 KB at most)
 
 struct Listed {

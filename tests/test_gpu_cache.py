@@ -288,13 +288,15 @@ def test_infinite_and_absent_scores(ctx, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_a_long_sequence_and_many_short_ones(ctx, dtype):
     run(ctx, dtype, 2, 1, 64, 64, [9000], 1)
+    run(ctx, dtype, 4, 1, 128, 64, [9000, 5], 2, rotation=("halves", 128, 9100))
     run(ctx, dtype, 2, 2, 64, 16, [int(s) for s in np.random.default_rng(5).integers(0, 200, 40)], 1, tiles=(2, 1, 7))
 
 
 # more rows than the vector units take: what the matrix cores' kernel owns, around its borders
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("h", [64, 128])
-@pytest.mark.parametrize("N_h,N_kv,N_s", [(8, 1, 1), (9, 1, 1), (4, 1, 3), (31, 1, 1), (16, 1, 2), (11, 1, 3), (8, 2, 32), (3, 1, 43)])
+@pytest.mark.parametrize("N_h,N_kv,N_s", [(1, 1, 1), (2, 1, 1), (3, 3, 2), (3, 1, 1), (8, 1, 1), (9, 1, 1), (4, 1, 3), (16, 1, 1), (17, 1, 1), (31, 1, 1), (16, 1, 2),
+                                          (11, 1, 3), (8, 2, 32), (3, 1, 43), (2, 1, 130)])
 def test_rows_around_the_kernels_borders(ctx, dtype, h, N_h, N_kv, N_s):
     run(ctx, dtype, N_h, N_kv, h, 16, [70, 0, 33], N_s, count=[N_s, N_s, max(1, N_s - 1)], tiles=(2, 5, 2))
 
@@ -459,6 +461,18 @@ def test_results_do_not_hang_on_the_run(ctx):
         assert np.array_equal(p.tB.download(), first)
     p.close()
 
+
+def test_the_result_is_no_page(ctx):
+    """With one cached head and one sequence a page's tensor has the result's shape."""
+    from paper_2504_13236_amd import capi, tiled
+    Z = tiled.TiledTensor.zeros(ctx, (3 * 8, 16, 1), (3 * 8, 16, 1))
+    K, V = (tiled.TiledTensor.zeros(ctx, (8, 16, 1), (8, 4, 1)) for _ in range(2))
+    pages, start = (torch.zeros(4, dtype=torch.int32, device="cuda") for _ in range(2))
+    cfg = capi.nnt_cache_cfg(pages.data_ptr(), start.data_ptr(), None, None, 1, 1, 4, 0, capi.NNT_ROTATE_HALVES)
+    for B in (K, V):
+        assert capi.nnt_cache_attention.raw(ctx.h, C.byref(cfg), 0.1, Z.h, K.h, V.h, B.h) == capi.NNT_EINVAL
+    for t in (V, K, Z):
+        t.close()
 
 def test_refusals(ctx):
     from paper_2504_13236_amd import capi, tiled
