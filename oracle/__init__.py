@@ -2,7 +2,7 @@
 
 Plain numpy, fp64, written from the paper's statement of the operations
 (section 3) and, where the paper is silent, from the readings listed in the
-design notes.  Two modules:
+design notes.  Three modules:
 
   definition.py  the untiled definition of every operation, the block forward,
                  its analytic adjoint, the Adam and SGD-with-momentum steps,
@@ -15,6 +15,8 @@ design notes.  Two modules:
                  softmax), and attention walked key tile by key tile with the
                  softmax subroutines' running statistics, with its recomputing
                  adjoint.  It exists to pin tiling invariance.
+  rollout.py     the paged cache and the attention over it, position by position,
+                 drawn tokens with their filters, and the norm of gradients.
 
 Only tests/, the smoke check and the benchmark's cpu_baseline leg may import
 this package.  It shares no code with the HIP library and never calls it.

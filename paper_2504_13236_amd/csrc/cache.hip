@@ -590,12 +590,12 @@ struct TileShape {
 
 // this lane's row, as the products take it; its second part where it is turned
 template <class X>
-__device__ __forceinline__ void load_query(const Cache& c, const typename X::T* row, int hh, int p, bool there, typename X::Own& q, typename X::Own& rest) {
+__device__ __forceinline__ void load_query(const Cache& c, int h, const typename X::T* row, int hh, int p, bool there, typename X::Own& q, typename X::Own& rest) {
     if constexpr (sizeof(typename X::T) == 4) {
 #pragma unroll
         for (int s = 0; s < X::H / 16; s++) {
             float x[kE] = {};
-            if (there) turned<float>(c, row, (X::H / 2) * hh + 8 * s, p, x);
+            if (there && (X::H / 2) * hh + 8 * s < h) turned<float>(c, row, (X::H / 2) * hh + 8 * s, p, x);
 #pragma unroll
             for (int i = 0; i < kE; i++) q.v[8 * s + i] = x[i];
         }
@@ -603,7 +603,7 @@ __device__ __forceinline__ void load_query(const Cache& c, const typename X::T* 
 #pragma unroll
         for (int s = 0; s < X::H / 16; s++) {
             float x[kE] = {};
-            if (there) turned<bf16_t>(c, row, 16 * s + 8 * hh, p, x);
+            if (there && 16 * s + 8 * hh < h) turned<bf16_t>(c, row, 16 * s + 8 * hh, p, x);
 #pragma unroll
             for (int i = 0; i < kE; i++) {
                 q.v[s][i] = (__bf16)x[i];
@@ -639,8 +639,8 @@ __device__ __forceinline__ bool take_out(uint4& v) {
     return odd;
 }
 
-// TURN: queries are turned.
-template <class X, bool TURN>
+// TURN: queries are turned.  FULL: heads of H components; else of fewer, zeros behind them.
+template <class X, bool TURN, bool FULL>
 __global__ void __launch_bounds__(256, TileShape<X>::kResident) attend_tile_kernel(Attend a) {
     using T = typename X::T;
     using S = TileShape<X>;
@@ -652,7 +652,7 @@ __global__ void __launch_bounds__(256, TileShape<X>::kResident) attend_tile_kern
     T* const Ks = reinterpret_cast<T*>(lds);
     T* const Vs = Ks + KEYS * LDK;
     const Cache& c = a.c;
-    const int G = c.N_h / c.N_kv;
+    const int G = c.N_h / c.N_kv, h = FULL ? H : c.h;
     const int split = blockIdx.x, j = blockIdx.y % c.N_kv, b = blockIdx.z;
     // the last rows see the most keys: they go first
     const int chunk = a.chunks - 1 - (int)blockIdx.y / c.N_kv;
@@ -677,7 +677,7 @@ __global__ void __launch_bounds__(256, TileShape<X>::kResident) attend_tile_kern
     const int w_first = clamped((int64_t)start + (r0 + first) / G), w_last = clamped((int64_t)start + (r0 + min(first + 31, rows - 1)) / G);
     const bool w_any = first < rows;
     typename X::Own q, rest;
-    load_query<X>(c, there ? row_at<const T>(c.z, head * H, tok, b) : nullptr, hh, (int)pos, there, q, rest);
+    load_query<X>(c, h, there ? row_at<const T>(c.z, head * h, tok, b) : nullptr, hh, (int)pos, there, q, rest);
 
     f32x16 O[H / 32];
 #pragma unroll
@@ -694,7 +694,7 @@ __global__ void __launch_bounds__(256, TileShape<X>::kResident) attend_tile_kern
         for (int i = tid; i < n_here; i += 256) {
             const int page = c.pages[(int64_t)b * c.max_pages + first_page + i];
             const bool ok = page >= 0 && page < c.n_pages;
-            const int64_t off = (int64_t)j * c.P * H;
+            const int64_t off = (int64_t)j * c.P * h;
             keys[i] = ok ? global_as<const T>(c.K[page]) + off : nullptr;
             values[i] = ok ? global_as<const T>(c.V[page]) + off : nullptr;
             gone = gone || !ok;
@@ -711,7 +711,7 @@ __global__ void __launch_bounds__(256, TileShape<X>::kResident) attend_tile_kern
                 if (k + row < k1) {
                     const uint32_t p = (uint32_t)(k + row), pg = c.by_P(p), slot = p - pg * c.P, at = pg - (uint32_t)first_page;
                     if (const T* kp = keys[at]) {
-                        const uint32_t off = slot * H + cv * X::kPer;
+                        const uint32_t off = slot * (uint32_t)h + (FULL ? cv * X::kPer : min(cv * X::kPer, h - X::kPer));
                         kr[i] = *reinterpret_cast<const typename X::Vec*>(in_global(kp) + off);
                         vr[i] = *reinterpret_cast<const typename X::Vec*>(in_global(values[at]) + off);
                     }
@@ -728,6 +728,7 @@ __global__ void __launch_bounds__(256, TileShape<X>::kResident) attend_tile_kern
             for (int i = 0; i < S::kVec; i++) {
                 const int idx = tid + 256 * i, row = idx / S::kRowVecs, cv = idx % S::kRowVecs;
                 if (clean && take_out(vr[i])) odd = true;
+                if (!FULL && cv * X::kPer >= h) kr[i] = X::zero_vec();
                 X::template put<LDK>(Ks, row, cv, kr[i]);
                 X::template put<LDV>(Vs, row, cv, vr[i]);
             }
@@ -796,7 +797,7 @@ __global__ void __launch_bounds__(256, TileShape<X>::kResident) attend_tile_kern
                         const int p = kb + kk;
                         const T* vp = p < k1 ? values[c.by_P((uint32_t)p) - (uint32_t)first_page] : nullptr;
                         if (!vp) continue;
-                        const T* v = in_global(vp) + (int64_t)((uint32_t)p - c.by_P((uint32_t)p) * c.P) * H;
+                        const T* v = in_global(vp) + (int64_t)((uint32_t)p - c.by_P((uint32_t)p) * c.P) * h;
                         // the weight of key kk lies in the half that acc_row puts it in
                         const int r = 4 * (kk / 8) + kk % 4, half = (kk / 4) % 2;
                         float wt = 0.f;
@@ -812,8 +813,9 @@ __global__ void __launch_bounds__(256, TileShape<X>::kResident) attend_tile_kern
 #pragma unroll
                             for (int i = 0; i < 16; i++) {
                                 float x[1];
-                                ldv<1>(v + 32 * rb + acc_row(i, hh), x);
-                                if (bits && no_number(__float_as_uint(x[0]))) O[rb][i] += wt * x[0];
+                                const bool in = FULL || 32 * rb + 8 * (i / 4) < h;   // (eights of components are there or not)
+                                ldv<1>(v + (in ? 32 * rb + 8 * (i / 4) : 0) + (4 * hh + i % 4), x);
+                                if (in && bits && no_number(__float_as_uint(x[0]))) O[rb][i] += wt * x[0];
                             }
                     }
                 }
@@ -838,21 +840,22 @@ __global__ void __launch_bounds__(256, TileShape<X>::kResident) attend_tile_kern
     if (own >= rows) return;
     if (alone) {
         const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
-        T* o = row_at<T>(a.out, head * H, tok, b);
+        T* o = row_at<T>(a.out, head * h, tok, b);
 #pragma unroll
         for (int rb = 0; rb < H / 32; rb++)
 #pragma unroll
             for (int k = 0; k < 4; k++)
-                X::store4(o + 32 * rb + 8 * k + 4 * hh, O[rb][4 * k] * inv, O[rb][4 * k + 1] * inv, O[rb][4 * k + 2] * inv, O[rb][4 * k + 3] * inv);
+                if (FULL || 32 * rb + 8 * k < h) X::store4(o + 32 * rb + 8 * k + 4 * hh, O[rb][4 * k] * inv, O[rb][4 * k + 1] * inv, O[rb][4 * k + 2] * inv, O[rb][4 * k + 3] * inv);
     } else {
-        float* o = a.partial + ((((int64_t)b * c.z.n1 + tok) * c.N_h + head) * a.splits + split) * (H + 2);
+        float* o = a.partial + ((((int64_t)b * c.z.n1 + tok) * c.N_h + head) * a.splits + split) * (h + 2);
 #pragma unroll
         for (int rb = 0; rb < H / 32; rb++)
 #pragma unroll
-            for (int i = 0; i < 16; i++) o[32 * rb + acc_row(i, hh)] = O[rb][i];
+            for (int i = 0; i < 16; i++)
+                if (FULL || 32 * rb + 8 * (i / 4) < h) o[32 * rb + acc_row(i, hh)] = O[rb][i];
         if (hh == 0) {
-            o[H] = m * a.scale;
-            o[H + 1] = lsum;
+            o[h] = m * a.scale;
+            o[h + 1] = lsum;
         }
     }
 }
@@ -968,25 +971,28 @@ struct Cut {
     int R, lpk, step, chunks, splits;
     bool tile;
 };
-// With heads of 64 or 128 the matrix cores take two rows or more of bf16 and 17 of fp32 (us, vector units -> matrix cores; one sequence of 131072 keys
-// of 8 cached heads of 128, 64 sequences of 2048 of 12 of 64):
-//   bf16, 1 row 106 -> 107 and 81 -> 77 (ragged lengths 84 -> 90, and a short call costs a microsecond more), 2 rows 113 -> 108 and 87 -> 78,
-//   4 rows 139 -> 108 and 108 -> 78, turned 146 -> 116 and 112 -> 79;  fp32, 16 rows 660 -> 660 and 321 -> 366, 32 rows 922 -> 660 and 567 -> 368.
+// Heads of up to 128 components: the matrix cores take two rows or more of bf16 and 17 of fp32, where zeros fill heads up to 64 or 128 five and 33.  In us, vector units -> matrix cores:
+//   one sequence of 131072 keys of 8 cached heads of 128 and 64 sequences of 2048 of 12 of 64:
+//   bf16, 1 row 106 -> 107 and 81 -> 77 (but ragged lengths 84 -> 90, and a short call costs a microsecond more), 2 rows 113 -> 108 and 87 -> 78,
+//   4 rows 139 -> 108 and 108 -> 78, turned 146 -> 116 and 112 -> 79;  fp32, 16 rows 660 -> 660 and 321 -> 366, 32 rows 922 -> 660 and 567 -> 368;
+//   filled up, 64 sequences, heads of 96 (1500 keys) and of 32 (2048):
+//   bf16, 4 rows 131 -> 150 and 65 -> 70, 8 rows 216 -> 151 and 93 -> 70;  fp32, 16 rows 416 -> 762 and 184 -> 384, 32 rows 779 -> 764 and 330 -> 385, 100 rows 2390 -> 838 and 926 -> 508.
 Cut cut_of(const nnt_cache_cfg* cfg, const nnt_tensor* QKV, const nnt_tensor* K) {
     Cut u;
     const int64_t G = cfg->N_h / cfg->N_kv, rows = G * QKV->shape[1], N_b = QKV->shape[2];
     const int64_t h = K->shape[0];
     const bool bf16 = K->dtype == NNT_BF16;
-    u.tile = (h == 64 || h == 128) && rows >= (bf16 ? 2 : 17);
-    u.R = u.tile ? 128 : rows >= 4 ? 4 : rows >= 2 ? 2 : 1;
+    const bool full = h == 64 || h == 128;
+    u.tile = h <= 128 && rows >= (bf16 ? (full ? 2 : 5) : full ? 17 : 33);
+    u.R = u.tile ? 128 : rows >= 3 ? 4 : rows >= 2 ? 2 : 1;       // (three rows as two and one read the keys twice: fp32 heads of 96 255 -> 180)
     u.lpk = h <= 32 ? 4 : h <= 64 ? 8 : h <= 128 ? 16 : 32;
     u.step = u.tile ? 64 : kWaves * (64 / u.lpk) * kUnroll;
     u.chunks = (int)((rows + u.R - 1) / u.R);
     // The keys are split so that the launch fills the chip.  The matrix cores' kernel: with no more workgroups than it holds at a time (bf16, one row chunk of 131072 keys, 128 components:
     // 512 workgroups 107 us, 768 134); the vector units': eight to a unit, or four that keep more registers (four rows: 768 174 us, 1024 155).
     const int64_t pairs = (int64_t)u.chunks * cfg->N_kv * N_b;
-    const int64_t held = 256 * (bf16 ? (h == 128 ? TileShape<Bf16Traits<128>>::kResident : TileShape<Bf16Traits<64>>::kResident)
-                                     : (h == 128 ? TileShape<F32Traits<128>>::kResident : TileShape<F32Traits<64>>::kResident));
+    const int64_t held = 256 * (bf16 ? (h > 64 ? TileShape<Bf16Traits<128>>::kResident : TileShape<Bf16Traits<64>>::kResident)
+                                     : (h > 64 ? TileShape<F32Traits<128>>::kResident : TileShape<F32Traits<64>>::kResident));
     const int64_t wanted = u.tile ? held / pairs : ((u.R == 1 ? 2048 : 1024) + pairs - 1) / pairs;
     // (no more than the longest range of keys has steps)
     const int64_t keys = std::min((int64_t)cfg->max_pages * K->base[1], cfg->window ? (int64_t)cfg->window + QKV->shape[1] : INT64_MAX);
@@ -1002,13 +1008,14 @@ using AttendFn = void (*)(Attend);
 template <typename T, int LPK>
 AttendFn attend_rows(int R) { return R == 1 ? attend_kernel<T, LPK, 1> : R == 2 ? attend_kernel<T, LPK, 2> : attend_kernel<T, LPK, 4>; }
 template <typename T, int H>
-AttendFn attend_tile(bool turn) {
-    if constexpr (sizeof(T) == 4) return attend_tile_kernel<F32Traits<H>, false>;
-    else return turn ? attend_tile_kernel<Bf16Traits<H>, true> : attend_tile_kernel<Bf16Traits<H>, false>;
+AttendFn attend_tile(bool turn, bool full) {
+    if constexpr (sizeof(T) == 4) return full ? attend_tile_kernel<F32Traits<H>, false, true> : attend_tile_kernel<F32Traits<H>, false, false>;
+    else if (turn) return full ? attend_tile_kernel<Bf16Traits<H>, true, true> : attend_tile_kernel<Bf16Traits<H>, true, false>;
+    else return full ? attend_tile_kernel<Bf16Traits<H>, false, true> : attend_tile_kernel<Bf16Traits<H>, false, false>;
 }
 template <typename T>
 AttendFn attend_instance(const Cut& u, int64_t h, bool turn) {
-    if (u.tile) return h == 64 ? attend_tile<T, 64>(turn) : attend_tile<T, 128>(turn);
+    if (u.tile) return h <= 64 ? attend_tile<T, 64>(turn, h == 64) : attend_tile<T, 128>(turn, h == 128);
     return u.lpk == 4 ? attend_rows<T, 4>(u.R) : u.lpk == 8 ? attend_rows<T, 8>(u.R) : u.lpk == 16 ? attend_rows<T, 16>(u.R) : attend_rows<T, 32>(u.R);
 }
 

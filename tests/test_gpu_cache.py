@@ -224,12 +224,13 @@ def test_positions_outside_the_table(ctx, start):
     p.close()
 
 
+@pytest.mark.parametrize("h", [64, 40, 96])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("what", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("N_s", [1, 3, 40])
-def test_what_is_masked_does_not_enter(ctx, dtype, what, N_s):
+def test_what_is_masked_does_not_enter(ctx, dtype, what, N_s, h):
     """Slots behind the sequences, keys before a window, pages of nobody and tokens behind a sequence's new ones hold anything."""
-    p = Problem(ctx, dtype, 4, 2, 64, 8, [41, 10], N_s, count=[N_s, (N_s + 1) // 2], window=24)
+    p = Problem(ctx, dtype, 4, 2, h, 8, [41, 10], N_s, count=[N_s, (N_s + 1) // 2], window=24)
     clean = p.expected_cache()
     K, V = np.full_like(p.K, what), np.full_like(p.V, what)
     for b in range(2):
@@ -294,8 +295,8 @@ def test_a_long_sequence_and_many_short_ones(ctx, dtype):
 
 # more rows than the vector units take: what the matrix cores' kernel owns, around its borders
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("h", [64, 128])
-@pytest.mark.parametrize("N_h,N_kv,N_s", [(1, 1, 1), (2, 1, 1), (3, 3, 2), (3, 1, 1), (8, 1, 1), (9, 1, 1), (4, 1, 3), (16, 1, 1), (17, 1, 1), (31, 1, 1), (16, 1, 2),
+@pytest.mark.parametrize("h", [8, 64, 96, 128])
+@pytest.mark.parametrize("N_h,N_kv,N_s", [(1, 1, 1), (2, 1, 1), (3, 3, 2), (3, 1, 1), (8, 1, 1), (9, 1, 1), (4, 1, 1), (5, 1, 1), (4, 1, 3), (16, 1, 1), (17, 1, 1), (31, 1, 1), (16, 1, 2), (33, 1, 1),
                                           (11, 1, 3), (8, 2, 32), (3, 1, 43), (2, 1, 130)])
 def test_rows_around_the_kernels_borders(ctx, dtype, h, N_h, N_kv, N_s):
     run(ctx, dtype, N_h, N_kv, h, 16, [70, 0, 33], N_s, count=[N_s, N_s, max(1, N_s - 1)], tiles=(2, 5, 2))
@@ -309,18 +310,28 @@ def test_split_keys_of_many_rows(ctx, dtype, rotation, N_s, window):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rotation", [None, ("halves", 80, 4000), ("pairs", 40, 4000)])
+@pytest.mark.parametrize("h", [24, 56, 80, 104])
+def test_split_keys_of_heads_that_are_filled_up(ctx, dtype, rotation, h):
+    rotation = rotation and (rotation[0], min(rotation[1], h), rotation[2])
+    run(ctx, dtype, 4, 1, h, 20, [2500, 3], 20, rotation=rotation, window=700)
+    run(ctx, dtype, 6, 2, h, 24, [100, 3, 64], 50, count=[50, 7, 49], rotation=rotation)
+
+
+@pytest.mark.parametrize("h", [64, 40, 96])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N_h,N_s", [(4, 3), (4, 20), (1, 150)])
-def test_no_numbers_in_the_keys_and_values_of_later_tokens_of_grouped_heads(ctx, dtype, N_h, N_s):
-    p = Problem(ctx, dtype, N_h, 1, 64, 8, [131, 60], N_s)
+def test_no_numbers_in_the_keys_and_values_of_later_tokens_of_grouped_heads(ctx, dtype, N_h, N_s, h):
+    p = Problem(ctx, dtype, N_h, 1, h, 8, [131, 60], N_s)
     p.append()
     p.check_append()
     p.attention()
     before = p.tB.download()
     half = N_s // 2
     Z = p.QKV.copy()
-    Z[N_h * 64:(N_h + 1) * 64, half:] = -np.inf
-    Z[(N_h + 1) * 64:, half::2] = np.inf
-    Z[(N_h + 1) * 64 + 5, half:] = np.nan
+    Z[N_h * h:(N_h + 1) * h, half:] = -np.inf
+    Z[(N_h + 1) * h:, half::2] = np.inf
+    Z[(N_h + 1) * h + 5, half:] = np.nan
     p.tQKV.upload(Z)
     p.append()
     p.attention()
@@ -329,25 +340,26 @@ def test_no_numbers_in_the_keys_and_values_of_later_tokens_of_grouped_heads(ctx,
     p.close()
 
 
+@pytest.mark.parametrize("h", [64, 40, 96])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N_s", [1, 12, 80])
-def test_no_numbers_that_are_seen(ctx, dtype, N_s):
+def test_no_numbers_that_are_seen(ctx, dtype, N_s, h):
     """An infinity and a NaN among the values reach the rows that see them, in their component, and no other row or component."""
-    p = Problem(ctx, dtype, 2, 2, 64, 8, [40, 20], N_s)
+    p = Problem(ctx, dtype, 2, 2, h, 8, [40, 20], N_s)
     p.append()
     p.attention()
-    want = p.tB.download().reshape(2, 64, N_s, 2)
+    want = p.tB.download().reshape(2, h, N_s, 2)
     V = p.tV.download()
     last = 40 + N_s // 2
     V[3, R.slot_of(17, 0, p.pages, 8, 99), 1] = np.inf
     V[9, R.slot_of(last, 0, p.pages, 8, 99), 1] = np.nan
     p.tV.upload(V)
     p.attention()
-    got = p.tB.download().reshape(2, 64, N_s, 2)
+    got = p.tB.download().reshape(2, h, N_s, 2)
     assert np.array_equal(got[0], want[0]) and np.array_equal(got[..., 1], want[..., 1])
     assert np.isposinf(got[1, 3, :, 0]).all()
     assert np.isnan(got[1, 9, last - 40:, 0]).all() and np.array_equal(got[1, 9, :last - 40, 0], want[1, 9, :last - 40, 0])
-    others = [i for i in range(64) if i not in (3, 9)]
+    others = [i for i in range(h) if i not in (3, 9)]
     assert np.array_equal(got[1, others], want[1, others])
     p.close()
 
