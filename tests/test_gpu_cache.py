@@ -200,6 +200,32 @@ def test_pages_that_are_not_there(ctx, dtype, N_s):
     p.close()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N_s", [1, 20])
+def test_sequences_that_share_their_first_pages(ctx, dtype, N_s):
+    p = Problem(ctx, dtype, 4, 2, 64, 8, [40, 90, 33], N_s)
+    p.pages[:4, 1:] = p.pages[:4, :1]
+    p.dpages.copy_(torch.from_numpy(p.pages.T.astype(np.int32)))
+    torch.cuda.synchronize()
+    p.append()
+    K, V = p.check_append()
+    p.attention()
+    p.check_attention(K, V)
+    p.close()
+
+
+# scores of some hundreds: nearly all of the mass on one key
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("h,N_s,rotation", [(64, 1, None), (64, 20, None), (128, 20, ("halves", 128, 400)), (96, 40, None)])
+def test_steep_scores(ctx, dtype, h, N_s, rotation):
+    p = Problem(ctx, dtype, 2, 1, h, 16, [300, 17], N_s, rotation=rotation, seen_std=100.0)
+    p.append()
+    K, V = p.check_append()
+    p.attention()
+    p.check_attention(K, V)
+    p.close()
+
+
 @pytest.mark.parametrize("start", [[-3, -1], [2 ** 31 - 1, 10 ** 6], [-2 ** 31, 2 ** 31 - 3]])
 def test_positions_outside_the_table(ctx, start):
     p = Problem(ctx, "f32", 2, 2, 64, 8, [40, 9], 5)
