@@ -16,7 +16,7 @@
 //   else: a histogram over 2048 equal parts of the column's range (which a monotone function of the logit picks, so a part is a run
 //     of the order); the part that holds the border is sorted in LDS, or, while it holds more than a list of 2048, divided again by the bits of its keys.
 //
-// Bound by instructions and LDS, not by memory: 1024 bf16 columns of 50304, top-p, 75 us (103 MB: 21 us at a copy's rate; vector units 65 % busy, LDS 30 to 35 %), 64 fp32
+// Bound by instructions and LDS, not by memory: 1024 bf16 columns of 50304, top-p, 67 us (103 MB: 21 us at a copy's rate; before the last step 75, vector units 65 % busy, LDS 30 to 35 %), 64 fp32
 // columns of 100003, min-p, 26 us, one of 50304, top-k, 14 us.  More columns than units are what it is made for: a column over several of them would need a second launch.
 #include "colwise.hpp"
 #include "device_util.hpp"
@@ -821,9 +821,10 @@ constexpr float kLeastCoded = 0.000244140625f;           // 2^-12
 constexpr int kCodeThreads = 512, kPer = kCodes / kCodeThreads, kSlots = kPer + 3;
 struct Codes {
     uint32_t count[kNegCounts + kSide + 1];
-    unsigned long long weight[kCodes + 1];               // the last: of what has no code
+    unsigned long long weight[kCodes + 2];               // each sign's with a 0 behind them, for what has no code
     uint32_t small[kSmall];                              // bits
 };
+constexpr unsigned long long kOneTie = 1ull << 55;       // eight weights are at most 2^54
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ float of_bits(uint32_t b) { return __uint_as_float(b << 16); }
 // code of the bits b, if they have one
@@ -957,13 +958,13 @@ __device__ __forceinline__ bool coded_column(const Sample& a, Column_<bf16_t, kC
         if (!coded) return false;
         cut = with_least(a, top, cut);
     }
-    // the table: what lies above the border
+    // the table: what lies above the border, and at it (where ties stay) a one above the weights, which counts them as sums are taken
 #pragma unroll
     for (int i = 0; i < PER; i++) {
         const uint32_t k = neg ? kSide + (uint32_t)((tid - NT / 2) * PER + i) : kSide - 1 - (uint32_t)(tid * PER + i);
-        m.weight[k] = x[i] > cut.x ? wt[i] : 0;
+        m.weight[k + (neg ? 1 : 0)] = x[i] > cut.x ? wt[i] : cut.ties && x[i] == cut.x ? kOneTie : 0;
     }
-    if (tid == 0) m.weight[kCodes] = 0;
+    if (tid < 2) m.weight[tid ? kCodes + 1 : kSide] = 0;
     __syncthreads();
     const bool tied = cut.ties != 0, small_too = cut.x < kLeastCoded && (smalls || zeros);
     bool has;
@@ -977,7 +978,7 @@ __device__ __forceinline__ bool coded_column(const Sample& a, Column_<bf16_t, kC
             const uint32_t b = (j & 1) ? v.x[j >> 1] >> 16 : v.x[j >> 1] & 0xffffu;
             bool coded;
             const uint32_t k = code_of(b, coded);
-            p[j] = m.weight[coded ? k : kCodes];
+            p[j] = m.weight[coded ? k + (b >> 15) : kSide] & (kOneTie - 1);
             equal |= coded && k == border ? 1u << j : 0u;
             odd = odd || !coded;
         }
@@ -995,23 +996,56 @@ __device__ __forceinline__ bool coded_column(const Sample& a, Column_<bf16_t, kC
     auto goal = [&](uint64_t all) { return share_of(u, all); };
     const uint64_t tie = tied ? h.weight(cut.x) : 0;
     if (cut.x >= kLeastCoded) {
-        // the border has a positive code: kept are the bits from it to the largest logit's
-        const uint32_t lowest = __float_as_uint(cut.x) >> 16, span = (__float_as_uint(top) >> 16) - lowest;
-        const unsigned long long* table = m.weight + (lowest - kFirst);
+        // The border has a positive code: kept are the bits from it to the largest logit's, all others go by the place behind those, whose weight is 0 (no logit
+        // has that code).  Two logits of a word at a time, and the look-ups of a vector are on their way together
+        // (one by one, where kept, 75 us for 1024 columns of 50304, so 67; the same below, all kept, 77 and 73).
+        const uint32_t lowest = __float_as_uint(cut.x) >> 16, behind = (__float_as_uint(top) >> 16) - lowest + 1;
+        const u16x2 low = {(uint16_t)lowest, (uint16_t)lowest}, most = {(uint16_t)behind, (uint16_t)behind};
+        const char* table = reinterpret_cast<const char*>(m.weight + (lowest - kFirst));
         locate_by<4>(h, tie, cut.ties,
                [&](const RawVec<bf16_t>& v, uint64_t& s, uint32_t& ties) {
+                   uint64_t sum8 = 0;
 #pragma unroll
-                   for (int j = 0; j < V; j++) {
-                       const uint32_t t = ((j & 1) ? v.x[j >> 1] >> 16 : v.x[j >> 1] & 0xffffu) - lowest;
-                       if (t <= span) {
-                           s += table[t];
-                           ties += t == 0 && tied;
-                       }
+                   for (int k = 0; k < V / 2; k++) {
+                       const u16x2 t = __builtin_elementwise_min((u16x2)(__builtin_bit_cast(u16x2, (uint32_t)v.x[k]) - low), most);
+                       const uint32_t at = __builtin_bit_cast(uint32_t, (u16x2)(t << (uint16_t)3));
+                       sum8 += *reinterpret_cast<const unsigned long long*>(table + (at & 0xffffu));
+                       sum8 += *reinterpret_cast<const unsigned long long*>(table + (at >> 16));
                    }
+                   s += sum8 & (kOneTie - 1);
+                   ties += (uint32_t)(sum8 / kOneTie);
                },
                weigh, goal);
     } else {
-        locate(h, tie, cut.ties, weigh, goal);
+        const u16x2 first = {(uint16_t)kFirst, (uint16_t)kFirst}, side = {(uint16_t)kSide, (uint16_t)kSide};
+        locate_by<4>(h, tie, cut.ties,
+               [&](const RawVec<bf16_t>& v, uint64_t& s, uint32_t& ties) {
+                   uint32_t at[V / 2];
+                   u16x2 largest = {0, 0};
+#pragma unroll
+                   for (int k = 0; k < V / 2; k++) {
+                       const u16x2 mag = __builtin_elementwise_min((u16x2)(__builtin_bit_cast(u16x2, (uint32_t)v.x[k] & 0x7fff7fffu) - first), side);
+                       const u16x2 sign = __builtin_bit_cast(u16x2, ((uint32_t)v.x[k] >> 15) & 0x00010001u);
+                       largest = __builtin_elementwise_max(largest, mag);
+                       at[k] = __builtin_bit_cast(uint32_t, (u16x2)((u16x2)(mag + sign * (u16x2)(side + (uint16_t)1)) << (uint16_t)3));
+                   }
+                   if (small_too && __any(largest[0] >= kSide || largest[1] >= kSide)) {
+                       uint64_t p[V];
+                       ties += __popc(weigh(v, p));
+#pragma unroll
+                       for (int j = 0; j < V; j++) s += p[j];
+                       return;
+                   }
+                   uint64_t sum8 = 0;
+#pragma unroll
+                   for (int k = 0; k < V / 2; k++) {
+                       sum8 += *reinterpret_cast<const unsigned long long*>(reinterpret_cast<const char*>(m.weight) + (at[k] & 0xffffu));
+                       sum8 += *reinterpret_cast<const unsigned long long*>(reinterpret_cast<const char*>(m.weight) + (at[k] >> 16));
+                   }
+                   s += sum8 & (kOneTie - 1);
+                   ties += (uint32_t)(sum8 / kOneTie);
+               },
+               weigh, goal);
     }
     sum = 0.0;
     if (a.logp && tid == 0)
