@@ -287,6 +287,20 @@ def test_what_has_no_code(ctx, dtype, filters):
     check(X, u, draw(ctx, X, u, dtype, tile_v=5000, **filters), **filters)
 
 
+@pytest.mark.parametrize("filters", [dict(), dict(temperature=0.0), dict(top_k=2), dict(top_p=0.5)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_infinities_in_long_columns(ctx, dtype, filters):
+    X, u = logits(10, 12345, 6, dtype)
+    X[[5, 4999, 5000, 12344], 0] = np.inf
+    X[12344, 1] = np.inf
+    X[::2, 2], X[7001, 2] = np.nan, np.inf
+    X[:, 3] = -np.inf
+    X[9999, 3] = -2.0
+    X[:, 4] = np.nan
+    check(X, u, draw(ctx, X, u, dtype, tile_v=5000, **filters), **filters)
+    check(X[:, :5], u[:5], draw(ctx, X[:, :5], u[:5], dtype, tile_v=5000, logp=False, **filters), **filters)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_borders_of_the_lists(ctx, dtype):
     """top-k at the ends of what is listed, and thousands of equal logits on top of it."""
