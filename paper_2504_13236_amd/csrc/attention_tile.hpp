@@ -161,8 +161,16 @@ template <int H_> struct Bf16Traits {
             for (int e = 0; e < 8; e++) pk.v[m][e] = (__bf16)x[8 * m + e];
     }
     static __device__ __forceinline__ void set(Packed& pk, int r, float x) { pk.v[r / 8][r % 8] = (__bf16)x; }
+    // what pack() has rounded away
+    static __device__ __forceinline__ void pack_rest(const f32x16& x, const Packed& pk, Packed& rest) {
+#pragma unroll
+        for (int m = 0; m < 2; m++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) rest.v[m][e] = (__bf16)(x[8 * m + e] - (float)pk.v[m][e]);
+    }
+    // (`rest`: a second part of p, times the same columns)
     template <int LDX>
-    static __device__ __forceinline__ void cols_times_acc(f32x16 (&out)[H / 32], const T* lds, int sub, int lane, const Packed& pk) {
+    static __device__ __forceinline__ void cols_times_acc(f32x16 (&out)[H / 32], const T* lds, int sub, int lane, const Packed& pk, const Packed* rest = nullptr) {
         // Accumulator registers 8 m + e of half hh are the rows 16 m + 8 (e / 4) + 4 hh + e % 4: two runs of
         // four consecutive rows, one transposing read each.  In such a read the 16 lanes of a group fetch
         // 8 bytes each -- lane j the columns 4 (j % 4) .. + 3 of row j / 4 of a 4 x 16 patch -- and lane j
@@ -179,6 +187,7 @@ template <int H_> struct Bf16Traits {
                 const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * LDX));
                 const s16x8 x = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
                 out[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pk.v[m], out[rb], 0, 0, 0);
+                if (rest) out[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), rest->v[m], out[rb], 0, 0, 0);
             }
     }
     static __device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {

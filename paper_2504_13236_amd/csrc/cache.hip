@@ -8,7 +8,7 @@
 //
 // The append is a copy; 58 MB take 17 us.  The attention reads what a (sequence, cached head) pair has cached once for all query rows of the pair, up to 128 of them,
 // and is bound by that read while there are few: 510 MB of 64 sequences, one row each, 84 us; 535 MB of one sequence, four rows, 109 us (a large copy's rate would
-// be 103 and 108).  Long axes are split over workgroups, whose partial results a second kernel joins; short calls (4.5 us for 100 keys) are launches.
+// be 103 and 108); 200 tokens of four sequences of up to 3200 keys, 25 heads of 64, 35 us.  Long axes are split over workgroups, whose partial results a second kernel joins; short calls (4.5 us for 100 keys) are launches.
 #include "attention_tile.hpp"
 #include "device_util.hpp"
 #include "internal.hpp"
@@ -572,11 +572,11 @@ __global__ void __launch_bounds__(kWaves * 64, R == 4 ? (sizeof(T) == 2 ? 3 : 2)
 // The workgroup owns 128 rows, 32 to a wavefront, and streams blocks of 64 keys and values through LDS, the next one on its way to registers while the
 // products run.  Products and statistics as in the fused attention: scores are a 32 x 32 accumulator, lane = row, whose layout is that of the
 // operand of the product with the values.
-//   A turned query has more bits than bf16: it is kept in two bf16 parts, and the scores are two products.  Weights are rounded to the type for the product
-//   with the values (half a step of each, 2^-8 of its own share of the result), as in the fused attention.
+//   A turned query and the weights have more bits than bf16: each is kept in two bf16 parts, and the scores (of turned queries) and the results are two products.
+//   So what a row gets is as near to fp32 weights as on the vector units, and only the result is rounded to bf16 (2^-16 of a weight is lost, half a step of bf16 is 2^-8).
 //   Masked weights are zeros, but a zero times an infinity is none: in blocks that some row sees in part, values that are no numbers are
 //   taken out (`odd`), and given afterwards to the rows that see them.
-// A wavefront without rows only brings keys and values: with two rows, bound by memory like with 128, it still beats the vector units (cut_of says where).
+// A wavefront without rows only brings keys and values: with few rows, bound by memory, it still beats the vector units (cut_of says where).
 constexpr int kTileTable = 256;
 template <class X>
 struct TileShape {
@@ -789,7 +789,13 @@ __global__ void __launch_bounds__(256, TileShape<X>::kResident) attend_tile_kern
                 }
                 typename X::Packed pk;
                 X::pack(s, pk);
-                X::template cols_times_acc<LDV>(O, Vs, part, lane, pk);
+                if constexpr (sizeof(T) == 2) {
+                    typename X::Packed low;
+                    X::pack_rest(s, pk, low);
+                    X::template cols_times_acc<LDV>(O, Vs, part, lane, pk, &low);
+                } else {
+                    X::template cols_times_acc<LDV>(O, Vs, part, lane, pk);
+                }
                 if (odd) {
                     // the values that were taken out, to the rows that see their keys
 #pragma unroll 1
@@ -971,19 +977,19 @@ struct Cut {
     int R, lpk, step, chunks, splits;
     bool tile;
 };
-// Heads of up to 128 components: the matrix cores take two rows or more of bf16 and 17 of fp32, where zeros fill heads up to 64 or 128 five and 33.  In us, vector units -> matrix cores:
+// Heads of up to 128 components: the matrix cores take three rows or more of bf16 (five where heads of more than 64 are turned, which is a second product for the scores) and 17 of fp32, where zeros fill
+// heads up to 64 or 128 five and 33.  Passes of two states one after the other, in us, vector units -> matrix cores:
 //   one sequence of 131072 keys of 8 cached heads of 128 and 64 sequences of 2048 of 12 of 64:
-//   bf16, 1 row 106 -> 107 and 81 -> 77 (but ragged lengths 84 -> 90, and a short call costs a microsecond more), 2 rows 113 -> 108 and 87 -> 78,
-//   4 rows 139 -> 108 and 108 -> 78, turned 146 -> 116 and 112 -> 79;  fp32, 16 rows 660 -> 660 and 321 -> 366, 32 rows 922 -> 660 and 567 -> 368;
-//   filled up, 64 sequences, heads of 96 (1500 keys) and of 32 (2048):
-//   bf16, 4 rows 131 -> 150 and 65 -> 70, 8 rows 216 -> 151 and 93 -> 70;  fp32, 16 rows 416 -> 762 and 184 -> 384, 32 rows 779 -> 764 and 330 -> 385, 100 rows 2390 -> 838 and 926 -> 508.
+//   bf16, 2 rows 97 -> 99 and 67 -> 69, 4 rows 105 -> 99 and 86 -> 70, turned 107 -> 117 and 88 -> 80, 5 rows turned 194 -> 117 and 138 -> 81, 16 rows 387 -> 103 and 252 -> 74;  fp32, 16 rows 660 -> 660 and 321 -> 366, 32 rows 922 -> 660 and 567 -> 368;
+//   filled up, 64 sequences, heads of 96 (4 cached ones, 1500 keys) and of 32 (8, 2048): bf16, 5 rows 63 -> 47 and 45 -> 49, 8 rows 65 -> 47 and 47 -> 49, 32 rows 234 -> 50 and 175 -> 50;
+//   12 cached ones, fp32, 16 rows 416 -> 762 and 184 -> 384, 32 rows 779 -> 764 and 330 -> 385, 100 rows 2390 -> 838 and 926 -> 508.
 Cut cut_of(const nnt_cache_cfg* cfg, const nnt_tensor* QKV, const nnt_tensor* K) {
     Cut u;
     const int64_t G = cfg->N_h / cfg->N_kv, rows = G * QKV->shape[1], N_b = QKV->shape[2];
     const int64_t h = K->shape[0];
     const bool bf16 = K->dtype == NNT_BF16;
     const bool full = h == 64 || h == 128;
-    u.tile = h <= 128 && rows >= (bf16 ? (full ? 2 : 5) : full ? 17 : 33);
+    u.tile = h <= 128 && rows >= (bf16 ? (full && !(cfg->rotation && h > 64) ? 3 : 5) : full ? 17 : 33);
     u.R = u.tile ? 128 : rows >= 3 ? 4 : rows >= 2 ? 2 : 1;       // (three rows as two and one read the keys twice: fp32 heads of 96 255 -> 180)
     u.lpk = h <= 32 ? 4 : h <= 64 ? 8 : h <= 128 ? 16 : 32;
     u.step = u.tile ? 64 : kWaves * (64 / u.lpk) * kUnroll;

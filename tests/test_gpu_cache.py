@@ -458,6 +458,26 @@ def test_two_graphs_share_the_scratch(ctx):
         p.close()
 
 
+@pytest.mark.parametrize("rotated", [False, True])
+@pytest.mark.parametrize("h", [64, 40, 128, 96])
+@pytest.mark.parametrize("N_h,N_s", [(2, 1), (5, 1), (4, 3), (1, 40), (2, 70)])
+def test_bf16_weights_are_not_rounded_to_the_type(ctx, N_h, N_s, h, rotated):
+    """However many rows share a cached head, a bf16 result is off by the rounding of the result and what fp32 weights would give.  Beside check_attention's
+    bound, without its half step of each weight: weights and turned queries in two bf16 parts lose half a step of half a step of each, 2^-16 (of a
+    weight, and of a score in both the sum above and the one below)."""
+    p = Problem(ctx, "bf16", N_h, 1, h, 16, [700, 333], N_s, rotation=("halves", h, 800) if rotated else None)
+    p.append()
+    K, V = p.check_append()
+    p.attention()
+    got = p.check_attention(K, V)
+    B, (mass, reach, _) = R.cache_attention(p.QKV, K, V, p.B, p.P, N_h, p.scale, p.pages, p.start, p.count, p.table, p.pairs, p.window)
+    n = 700 + N_s
+    weight = 2 * (h + 8) * EPS32 * reach + (4 + 2 * n) * EPS32 + 2.0 ** -16 * (1 + 2 * reach * rotated)
+    bound = HALF["bf16"] * np.abs(B) + weight * (mass + np.abs(B)) * 1.01
+    assert (np.abs(got - B) <= bound).all(), (np.abs(got - B) / bound).max()
+    p.close()
+
+
 @pytest.mark.parametrize("granularity", [0, 1])
 def test_ordinary_operations_on_a_cache_are_ordered_with_its_calls(granularity):
     """Fills and copies of the cache's tensors (tile by tile) before and after the calls that name it as a whole, on four streams."""
