@@ -166,6 +166,11 @@ NNT_API int32_t nnt_profile_read(nnt_ctx* ctx, nnt_profile_entry* out, int32_t c
 NNT_API int32_t nnt_sched_simulate(int32_t n_streams, int32_t serial, int32_t n_tiles, int32_t n_tasks,
                            const int32_t* task_first, const int32_t* acc_tile, const int32_t* acc_mode,
                            int32_t* stream_out, int64_t* seq_out, int64_t* wait_seq_out);
+/* The same where the n_tiles tiles are those of one tensor, and the number n_tiles names the tensor as a whole, as the calls on a cache
+ * name its pages with one record (modes 1, 2, 3; such a task names nothing else). */
+NNT_API int32_t nnt_sched_simulate_tensor(int32_t n_streams, int32_t serial, int32_t n_tiles, int32_t n_tasks,
+                           const int32_t* task_first, const int32_t* acc_tile, const int32_t* acc_mode,
+                           int32_t* stream_out, int64_t* seq_out, int64_t* wait_seq_out);
 
 /* Stream capture of the task flow into a HIP graph (section 2: the graph of a
  * training iteration repeats, so it can be built once and replayed).  Between

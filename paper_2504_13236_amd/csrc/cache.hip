@@ -1072,19 +1072,13 @@ int32_t nnt_cache_append(nnt_ctx* ctx, const nnt_cache_cfg* cfg, nnt_tensor* QKV
         const Divide by_token = divide_by((uint32_t)(per_head * c.N_kv)), by_head = divide_by((uint32_t)per_head);
         const dim3 grid((unsigned)((per_seq + 255) / 256), (unsigned)c.z.n2);
         const bool bf16 = K->dtype == NNT_BF16;
-        std::vector<Access> acc;
-        K->whole_access(kReadWrite, &acc);
-        V->whole_access(kReadWrite, &acc);
-        acc.push_back(QKV->all(kRead));
+        std::vector<Access> acc{K->whole_access(kReadWrite), V->whole_access(kReadWrite), QKV->all(kRead)};
         if (cfg->rotation) acc.push_back(cfg->rotation->all(kRead));
         OpTag tag(ctx, "cache_append", 4.0 * (double)c.N_kv * c.h * c.z.n1 * c.z.n2 * (double)K->elem_size(), true);
-        TRY(submit(ctx, acc, [&](hipStream_t st) {
+        return submit(ctx, acc, [&](hipStream_t st) {
             hipLaunchKernelGGL(bf16 ? append_instance<bf16_t>(halves, c.rot) : append_instance<float>(halves, c.rot), grid, dim3(256), 0, st, c, by_token, by_head);
             return launched();
-        }));
-        K->whole_submitted();
-        V->whole_submitted();
-        return NNT_OK;
+        });
     });
 }
 
@@ -1106,13 +1100,11 @@ int32_t nnt_cache_attention(nnt_ctx* ctx, const nnt_cache_cfg* cfg, float scale,
         const AttendFn fn = bf16 ? attend_instance<bf16_t>(u, a.c.h, a.c.rot) : attend_instance<float>(u, a.c.h, a.c.rot);
         const dim3 grid((unsigned)u.splits, (unsigned)(u.chunks * a.c.N_kv), (unsigned)a.c.z.n2);
         const int64_t rows = (int64_t)a.c.z.n1 * a.c.z.n2 * a.c.N_h;
-        std::vector<Access> acc{B->all(kReadWrite), QKV->all(kRead)};
-        K->whole_access(kRead, &acc);
-        V->whole_access(kRead, &acc);
+        std::vector<Access> acc{B->all(kReadWrite), QKV->all(kRead), K->whole_access(kRead), V->whole_access(kRead)};
         if (cfg->rotation) acc.push_back(cfg->rotation->all(kRead));
         // (the lengths are on the device: the work counted is that of the queries and results, and of caches that are full)
         OpTag tag(ctx, "cache_attention", (2.0 * (double)rows * a.c.h + 2.0 * (double)a.c.max_pages * a.c.P * a.c.N_kv * a.c.h * a.c.z.n2) * (double)K->elem_size(), true);
-        TRY(submit(ctx, acc, [&](hipStream_t st) -> int32_t {
+        return submit(ctx, acc, [&](hipStream_t st) -> int32_t {
             a.partial = stream_scratch_of(ctx);
             hipLaunchKernelGGL(fn, grid, dim3(kWaves * 64), 0, st, a);
             TRY(launched());
@@ -1123,9 +1115,6 @@ int32_t nnt_cache_attention(nnt_ctx* ctx, const nnt_cache_cfg* cfg, float scale,
             const auto join = bf16 ? (spread ? join_kernel<bf16_t, true> : join_kernel<bf16_t, false>) : (spread ? join_kernel<float, true> : join_kernel<float, false>);
             hipLaunchKernelGGL(join, jg, dim3(256), 0, st, a, u.R, u.step);
             return launched();
-        }, u.splits == 1 ? 1 : 2));
-        K->whole_submitted();
-        V->whole_submitted();
-        return NNT_OK;
+        }, u.splits == 1 ? 1 : 2);
     });
 }

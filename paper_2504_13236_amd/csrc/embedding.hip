@@ -205,8 +205,8 @@ int32_t nnt::embedding_after(nnt_ctx* ctx, const int32_t* tokens, nnt_tensor* W,
     const int dw = W->dtype, dy = Y->dtype;
     OpTag tag(ctx, "embedding_fwd", (double)Y->shape[0] * Y->shape[1] * Y->shape[2] * (W->elem_size() + Y->elem_size()), true);
     std::vector<Access> acc{Y->all(kWrite), W->all(kRead)};
-    if (after) after->whole_access(kRead, &acc);
-    rc = submit(ctx, acc, [=](hipStream_t st) {
+    if (after) acc.push_back(after->whole_access(kRead));
+    return submit(ctx, acc, [=](hipStream_t st) {
         const dim3 grid((unsigned)((total + 255) / 256)), block(256);
 #define NNT_EMB_FWD(TW, TY)                                                                                              \
     do {                                                                                                                 \
@@ -220,8 +220,6 @@ int32_t nnt::embedding_after(nnt_ctx* ctx, const int32_t* tokens, nnt_tensor* W,
 #undef NNT_EMB_FWD
         return hipGetLastError() == hipSuccess ? (int32_t)NNT_OK : (int32_t)NNT_EHIP;
     });
-    if (rc == NNT_OK && after) after->whole_submitted();
-    return rc;
 }
 
 int32_t nnt_embedding_bwd(nnt_ctx* ctx, const int32_t* tokens, nnt_tensor* dY, nnt_tensor* dW) {

@@ -400,16 +400,10 @@ struct nnt_graph {
     std::shared_ptr<Scratch> mem[4];     // what its tasks write partial sums and operands to: kept also where the context takes larger buffers
 };
 
-extern "C" {
-
-const char* nnt_version(void) { return "nntile_mi 0.1 (gfx950)"; }
-
-int32_t nnt_sched_simulate(int32_t n_streams, int32_t serial, int32_t n_tiles, int32_t n_tasks, const int32_t* task_first,
-                           const int32_t* acc_tile, const int32_t* acc_mode, int32_t* stream_out, int64_t* seq_out,
-                           int64_t* wait_seq_out) {
-    if (n_streams < 1 || n_streams > kMaxStreams || n_tiles < 0 || n_tasks < 0) return NNT_EINVAL;
-    if (n_tasks > 0 && (!task_first || !acc_tile || !acc_mode || !stream_out || !seq_out || !wait_seq_out)) return NNT_EINVAL;
-    std::vector<TileDep> tiles((size_t)n_tiles);
+// The replay of nnt_sched_simulate; `tensor`: the tiles are that one's, and the number behind the last names it as a whole.
+static int32_t simulate(int32_t n_streams, int32_t serial, std::vector<TileDep>* tiles, nnt_tensor* tensor, int32_t n_tasks, const int32_t* task_first,
+                        const int32_t* acc_tile, const int32_t* acc_mode, int32_t* stream_out, int64_t* seq_out, int64_t* wait_seq_out) {
+    const int32_t n_tiles = (int32_t)tiles->size();
     uint64_t tail[kMaxStreams] = {0}, synced[kMaxStreams] = {0}, waited[kMaxStreams][kMaxStreams] = {{0}};
     std::vector<uint64_t> recorded[kMaxStreams];
     std::vector<const void*> keys[kMaxStreams];
@@ -420,11 +414,17 @@ int32_t nnt_sched_simulate(int32_t n_streams, int32_t serial, int32_t n_tiles, i
         bool small = false;
         for (int i = task_first[t]; i < task_first[t + 1]; i++) {
             const int mode = acc_mode[i] & 0x7f, part = acc_mode[i] >> 8;
-            if (acc_tile[i] < 0 || acc_tile[i] >= n_tiles || acc_mode[i] < 0 || !((mode >= kRead && mode <= kReadWrite) || mode == kWritePart) ||
-                (mode != kWritePart && part != 0))
+            const bool whole = tensor && acc_tile[i] == n_tiles;
+            if (acc_tile[i] < 0 || (acc_tile[i] >= n_tiles && !whole) || acc_mode[i] < 0 || !((mode >= kRead && mode <= kReadWrite) || mode == kWritePart) ||
+                (mode != kWritePart && part != 0) || (whole && (mode == kWritePart || task_first[t + 1] - task_first[t] != 1)))
                 return NNT_EINVAL;
             small = small || (acc_mode[i] & 0x80);
-            acc.push_back(Access{&tiles[(size_t)acc_tile[i]], 1, mode, part});
+            if (whole) {
+                acc.push_back(tensor->whole_access(mode));
+            } else {
+                if (tensor) tensor->use_tiles();
+                acc.push_back(Access{&(*tiles)[(size_t)acc_tile[i]], 1, mode, part});
+            }
         }
         const TaskPlan plan = plan_task(acc, n_streams, n_streams, serial != 0, small, tail, synced, waited, &rr);
         // the waits as the executor would issue them: on the first recorded event that covers the
@@ -449,6 +449,30 @@ int32_t nnt_sched_simulate(int32_t n_streams, int32_t serial, int32_t n_tiles, i
         seq_out[t] = (int64_t)seq;
     }
     return NNT_OK;
+}
+
+extern "C" {
+
+const char* nnt_version(void) { return "nntile_mi 0.1 (gfx950)"; }
+
+int32_t nnt_sched_simulate(int32_t n_streams, int32_t serial, int32_t n_tiles, int32_t n_tasks, const int32_t* task_first,
+                           const int32_t* acc_tile, const int32_t* acc_mode, int32_t* stream_out, int64_t* seq_out,
+                           int64_t* wait_seq_out) {
+    if (n_streams < 1 || n_streams > kMaxStreams || n_tiles < 0 || n_tasks < 0) return NNT_EINVAL;
+    if (n_tasks > 0 && (!task_first || !acc_tile || !acc_mode || !stream_out || !seq_out || !wait_seq_out)) return NNT_EINVAL;
+    std::vector<TileDep> tiles((size_t)n_tiles);
+    return simulate(n_streams, serial, &tiles, nullptr, n_tasks, task_first, acc_tile, acc_mode, stream_out, seq_out, wait_seq_out);
+}
+
+int32_t nnt_sched_simulate_tensor(int32_t n_streams, int32_t serial, int32_t n_tiles, int32_t n_tasks, const int32_t* task_first,
+                           const int32_t* acc_tile, const int32_t* acc_mode, int32_t* stream_out, int64_t* seq_out,
+                           int64_t* wait_seq_out) {
+    if (n_streams < 1 || n_streams > kMaxStreams || n_tiles < 0 || n_tasks < 0) return NNT_EINVAL;
+    if (n_tasks > 0 && (!task_first || !acc_tile || !acc_mode || !stream_out || !seq_out || !wait_seq_out)) return NNT_EINVAL;
+    nnt_tensor tensor{};
+    tensor.ntiles = n_tiles;
+    tensor.deps.resize((size_t)n_tiles);
+    return simulate(n_streams, serial, &tensor.deps, &tensor, n_tasks, task_first, acc_tile, acc_mode, stream_out, seq_out, wait_seq_out);
 }
 
 int32_t nnt_ctx_create(int32_t device, int32_t n_streams, void* const* caller_streams, nnt_ctx** out) {

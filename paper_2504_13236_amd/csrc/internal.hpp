@@ -72,7 +72,7 @@ struct nnt_tensor {
     // whole tensor (whole_access) instead of one per tile.  Each side of the two kinds of users takes over what the other has left.
     nnt::TileDep whole;
     bool whole_used = false;         // `whole` is ahead of the tiles' records
-    bool tiles_used = false;         // the tiles' records are ahead of `whole`
+    bool tiles_used = false;         // the tiles' records are ahead of `whole`, which is empty then
     bool whole_tiles = false;        // every tile is there and 16-byte aligned
     uint64_t id;
 
@@ -116,14 +116,22 @@ struct nnt_tensor {
         use_tiles();
         return nnt::Access{&deps[idx], 1, mode};
     }
-    // the accesses of a task that names the tensor as a whole; whole_submitted() once it has been submitted
-    void whole_access(int mode, std::vector<nnt::Access>* acc) {
-        acc->push_back(nnt::Access{&whole, 1, mode});
-        if (tiles_used) acc->push_back(nnt::Access{deps.data(), ntiles, mode});
-    }
-    void whole_submitted() {
-        tiles_used = false;
+    // the access of a task that names the tensor as a whole
+    nnt::Access whole_access(int mode) {
+        if (tiles_used) {
+            // Every user of a tile is one of the whole: its writers as writers of parts, of which there may be one per stream and which all but
+            // writers of other parts wait for.  A reader waits for no reader, so the readers have to be known here when a writer comes after it.
+            for (const nnt::TileDep& d : deps)
+                for (int s = 0; s < nnt::kMaxStreams; s++) {
+                    const uint64_t w = d.w_stream == s && d.w_seq > d.p_seq[s] ? d.w_seq : d.p_seq[s];
+                    if (w > whole.p_seq[s]) whole.p_seq[s] = w;
+                    if (d.r_seq[s] > whole.r_seq[s]) whole.r_seq[s] = d.r_seq[s];
+                    whole.p_mixed[s] = 1;
+                }
+            tiles_used = false;
+        }
         whole_used = true;
+        return nnt::Access{&whole, 1, mode};
     }
     void use_tiles() {
         tiles_used = true;
@@ -132,7 +140,7 @@ struct nnt_tensor {
         for (nnt::TileDep& d : deps) {
             if (whole.w_stream >= 0) {
                 d = whole;           // that writer came after all that the tile's record knew of
-            } else {
+            } else {                 // readers only: the writers in `whole` are the tiles' own
                 for (int s = 0; s < nnt::kMaxStreams; s++) d.r_seq[s] = d.r_seq[s] > whole.r_seq[s] ? d.r_seq[s] : whole.r_seq[s];
             }
         }

@@ -1294,15 +1294,13 @@ int32_t sample_ordered(nnt_ctx* ctx, const nnt_sample_cfg* cfg, nnt_tensor* X, c
     int nt;
     const SampleFn fn = sample_instance(X->dtype, nvec, greedy, &nt);
     std::vector<Access> acc;
-    if (after) after->whole_access(kReadWrite, &acc);
+    if (after) acc.push_back(after->whole_access(kReadWrite));
     acc.push_back(X->all(kRead));
     OpTag tag(ctx, "sample_tokens", (double)X->shape[0] * n * X->elem_size(), true);
-    TRY(submit(ctx, acc, [=](hipStream_t st) {
+    return submit(ctx, acc, [=](hipStream_t st) {
         hipLaunchKernelGGL(fn, dim3((unsigned)n), dim3((unsigned)nt), 0, st, a);
         return launched();
-    }));
-    if (after) after->whole_submitted();
-    return NNT_OK;
+    });
 }
 
 }  // namespace nnt

@@ -346,6 +346,82 @@ def test_executor_orders_every_conflicting_pair(capi, n_streams, small):
     assert not stream.any() and not waits.any()
 
 
+class _WholeTensor:
+    """nnt_sched_simulate_tensor in the place of nnt_sched_simulate."""
+
+    def __init__(self, capi):
+        self.nnt_sched_simulate = capi.nnt_sched_simulate_tensor
+
+
+def _unordered(stream, seq, waits, conflicts):
+    """Pairs (i, j) of `conflicts` that stream order and the waits do not order."""
+    at = {(int(s), int(q)): t for t, (s, q) in enumerate(zip(stream, seq))}
+    before, last_on = [], {}
+    for t in range(len(stream)):
+        s = int(stream[t])
+        preds = ([last_on[s]] if s in last_on else []) + [at[(o, int(waits[t, o]))] for o in range(8) if waits[t, o]]
+        before.append(set(preds).union(*[before[p] for p in preds]))
+        last_on[s] = t
+    return [(i, j) for i, j in conflicts if i not in before[j]]
+
+
+def test_a_whole_reader_forgets_no_user_of_the_tiles(capi):
+    """A cache's tensor: ordinary operations name its tiles (0, 1), the calls on it the tensor as a whole (2).  A reader of the whole waits for no
+    reader of a tile, but a later writer of the whole has to; and it waits for a tile's writer, as the next reader of the whole has to."""
+    R, W, RW, all_of_it = 1, 2, 3, 2
+    flows = [
+        [[(0, R)], [(all_of_it, R)], [(all_of_it, RW)]],                                         # copy of a page, lookup or attention, append
+        [[(all_of_it, RW)], [(0, R), (1, R)], [(all_of_it, R)], [(all_of_it, RW)]],
+        [[(0, W)], [(1, W)], [(all_of_it, R)], [(all_of_it, R)], [(all_of_it, R)]],              # fill, attention, attention
+        [[(all_of_it, RW)], [(1, R)], [(all_of_it, R)], [(all_of_it, R)], [(all_of_it, R)]],     # append, copy of a page, attentions
+        [[(0, 6)], [(0, 6 + 256)], [(all_of_it, R)], [(all_of_it, R)], [(0, 6 + 256)]],          # writers of parts
+        [[(0, W)], [(all_of_it, R)], [(1, W)], [(all_of_it, R)], [(0, R)], [(all_of_it, RW)], [(1, RW)]],
+    ]
+    for flow in flows:
+        for n_streams in (2, 4, 8):
+            conflicts = []
+            for j, b in enumerate(flow):
+                for i, a in enumerate(flow[:j]):
+                    for ta, ma in a:
+                        for tb, mb in b:
+                            if (ta == tb or all_of_it in (ta, tb)) and (ma | mb) & 2 and not (ma & 0xff == 6 and mb & 0xff == 6 and ma != mb):
+                                conflicts.append((i, j))
+            out = _simulate(_WholeTensor(capi), n_streams, 0, 2, flow)
+            assert not _unordered(*out, conflicts), (flow, n_streams)
+    # readers of the whole and of tiles are not ordered among themselves: they go to different streams and wait for nothing
+    stream, seq, waits = _simulate(_WholeTensor(capi), 4, 0, 2, [[(0, R)], [(all_of_it, R)], [(1, R)], [(all_of_it, R)]])
+    assert sorted(stream.tolist()) == [0, 1, 2, 3] and not waits.any()
+
+
+@pytest.mark.parametrize("small", [False, True])
+@pytest.mark.parametrize("n_streams", [1, 2, 4, 8])
+def test_executor_orders_users_of_a_tensor_and_of_its_tiles(capi, n_streams, small):
+    """Random flows of tasks that name some tiles of a tensor or all of it as a whole: every pair with a writer among them is ordered."""
+    import numpy as np
+    r = np.random.default_rng(300 + n_streams)
+    for trial in range(40):
+        n_tiles, n_tasks, share = int(r.integers(1, 6)), int(r.integers(5, 80)), r.choice([0.2, 0.5, 0.8])
+        tasks = []
+        for _ in range(n_tasks):
+            if r.random() < share:
+                tasks.append([(n_tiles, int(r.choice([1, 1, 1, 2, 3])))])
+            else:
+                chosen = r.choice(n_tiles, size=int(r.integers(1, min(3, n_tiles) + 1)), replace=False)
+                tasks.append([(int(t), int(r.choice([1, 1, 1, 2, 3, 6, 6 + 256]))) for t in chosen])
+        told = [[(t, m | (SMALL if i == 0 and small and r.random() < 2 / 3 else 0)) for i, (t, m) in enumerate(a)] for a in tasks]
+        conflicts = {(i, j) for j in range(n_tasks) for i in range(j) for ti, mi in tasks[i] for tj, mj in tasks[j]
+                     if (ti == tj or n_tiles in (ti, tj)) and ((mi | mj) & 2) and not ((mi & 0xff) == 6 and (mj & 0xff) == 6 and mi != mj)}
+        out = _simulate(_WholeTensor(capi), n_streams, 0, n_tiles, told)
+        assert not _unordered(*out, sorted(conflicts)), trial
+    # a whole that is named beside tiles, as a part, or behind the last number, is refused
+    p = lambda *v: np.asarray(v, np.int32)
+    so, sq, wo = np.zeros(1, np.int32), np.zeros(1, np.int64), np.zeros(8, np.int64)
+    for tiles, modes in (([0, 1], [1, 1]), ([1], [6]), ([2], [1])):
+        first, t, m = p(0, len(tiles)), p(*tiles), p(*modes)
+        assert capi.nnt_sched_simulate_tensor.raw(2, 0, 1, 1, first.ctypes.data, t.ctypes.data, m.ctypes.data, so.ctypes.data, sq.ctypes.data,
+                                                  wo.ctypes.data) == capi.NNT_EINVAL
+
+
 def test_executor_keeps_small_tasks_on_a_stream_they_depend_on(capi):
     """Two chains on two streams, the second one longer; a task reads the first result of each and so is behind the tail of
     neither stream.  A long one takes the next stream in turn; a small one the stream with more behind it, where it waits
