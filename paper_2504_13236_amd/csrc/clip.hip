@@ -7,6 +7,7 @@
 // depend on which workgroup came first.  Squares are taken and added in 64 bits: gradients of 1e-23 have squares below fp32's range, and
 // 64-bit multiply-adds run at half the fp32 rate, far from what bounds this.
 // 124.5 M fp32 gradients in 148 tensors: 286 us (1.49 GB at 5.2 TB/s: the second read begins with what the first ended with).  The twelve of a block of 64: 11 us, two launches.
+#include "clip_pieces.hpp"
 #include "device_util.hpp"
 #include "internal.hpp"
 
@@ -17,61 +18,14 @@ namespace nnt {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPiece = 16384;          // elements: 64 KB of fp32
 constexpr int kMaxGroups = 2048;       // workgroups of a launch: eight to a compute unit
 constexpr int kFew = 256;              // partial sums that every workgroup of the second pass adds up by itself (the smallest block 13.3 -> 11 us)
-constexpr int kListed = 48;            // tensors of a launch: their geometry travels in its arguments (4 KB at most)
-
-struct Listed {
-    void* const* in;
-    void* const* out;
-    int32_t shape[kMaxDim], base[kMaxDim], grid[kMaxDim];
-    int32_t first;                     // number of its first piece
-    int32_t per_tile;                  // pieces of its largest tile
-    int32_t bf16;
-};
-struct List {
-    Listed t[kListed];
-    int32_t n, pieces;
-};
 static_assert(sizeof(List) + 64 <= 4096, "arguments of a launch");
 
 __device__ __forceinline__ double wave_sum64(double v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     return v;
-}
-
-// Piece number `w`: tile and elements [first, first + count) of it (count <= 0: beyond the end of a smaller tile).
-struct Piece {
-    const Listed* t;
-    int32_t tile;
-    int64_t first;
-    int32_t count;
-};
-__device__ __forceinline__ Piece piece_of(const List& a, int w) {
-    int lo = 0, hi = a.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.t[mid].first <= w) lo = mid;
-        else hi = mid - 1;
-    }
-    const Listed& t = a.t[lo];
-    const int k = w - t.first;
-    Piece p;
-    p.t = &t;
-    p.tile = k / t.per_tile;
-    p.first = (int64_t)(k - p.tile * t.per_tile) * kPiece;
-    int64_t n = 1;
-    int c = p.tile;
-#pragma unroll
-    for (int d = 0; d < kMaxDim; d++) {
-        const int at = c % t.grid[d];
-        c /= t.grid[d];
-        n *= min(t.base[d], t.shape[d] - at * t.base[d]);
-    }
-    p.count = (int)min((int64_t)kPiece, n - p.first);
-    return p;
 }
 
 template <typename T>
@@ -102,7 +56,7 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(List a, double* parti
     for (int w = blockIdx.x; w < a.pieces; w += gridDim.x) {
         const Piece p = piece_of(a, w);
         void* tile = p.t->in[p.tile];
-        if (p.count <= 0 || !tile) continue;
+        if (p.count == 0 || !tile) continue;
         s += p.t->bf16 ? squares_of<bf16_t>(global_as<const bf16_t>(tile) + p.first, p.count) : squares_of<float>(global_as<const float>(tile) + p.first, p.count);
     }
     s = wave_sum64(s);
@@ -181,7 +135,7 @@ __global__ void __launch_bounds__(kThreads) scale_kernel(List a, Factor by) {
     for (int w = a.pieces - 1 - (int)blockIdx.x; w >= 0; w -= gridDim.x) {
         const Piece p = piece_of(a, w);
         void *in = p.t->in[p.tile], *out = p.t->out[p.tile];
-        if (p.count <= 0 || !in || (f == 1.0 && in == out)) continue;
+        if (p.count == 0 || !in || (f == 1.0 && in == out)) continue;
         if (p.t->bf16) scale<bf16_t>(global_as<const bf16_t>(in) + p.first, global_as<bf16_t>(out) + p.first, p.count, f);
         else scale<float>(global_as<const float>(in) + p.first, global_as<float>(out) + p.first, p.count, f);
     }

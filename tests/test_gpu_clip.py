@@ -158,6 +158,30 @@ def test_large_tiles_and_fixed_order(ctx):
     t.close()
 
 
+def test_a_small_tile_beside_one_of_more_than_2_31_elements(ctx):
+    """Tiles of 65536 x 32770 bf16 elements and what is left, 65536 x 1: the memory behind the small one is not looked at."""
+    from paper_2504_13236_amd import capi, tiled
+    big, small = 65536 * 32770, 65536
+    buf = torch.full((big + small + 4096,), 2.0 ** -10, dtype=torch.bfloat16, device="cuda")
+    buf[big + small:] = float("inf")
+    h = C.c_void_p()
+    capi.nnt_tensor_create(ctx.h, capi.NNT_BF16, 2, capi.i64_array((65536, 32771)), capi.i64_array((65536, 32770)),
+                           capi.ptr_array([buf.data_ptr(), buf.data_ptr() + 2 * big]), C.byref(h))
+    norm = torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    cfg = capi.nnt_clip_cfg(2.0 ** -3, 0.0)
+    capi.nnt_clip_grad_norm(ctx.h, C.byref(cfg), 1, capi.ptr_array([h.value]), capi.ptr_array([h.value]), norm.data_ptr())
+    ctx.wait()
+    # 65536 * 32771 squares of 2^-10: their sum is a whole multiple of 2^-20, exact in 64 bits
+    want = (65536 * 32771) ** 0.5 * 2.0 ** -10
+    assert abs(float(norm) - want) <= EPS32 * want
+    clipped = 2.0 ** -10 * 2.0 ** -3 / want
+    for part in (buf[:1 << 20], buf[big - (1 << 20):big + small]):
+        assert float((part.double() - clipped).abs().max()) <= (HALF["bf16"] + EPS32) * clipped
+    assert torch.isinf(buf[big + small:]).all()
+    capi.nnt_tensor_destroy(h)
+
+
 def test_captured_and_replayed(ctx):
     from paper_2504_13236_amd import capi, tiled
     G = gradients(5, [(64, 64), (64,), (100, 33)], ["f32"] * 3)
