@@ -79,7 +79,7 @@ __device__ __forceinline__ double factor_of(const double* partial, int n, double
     for (int w = 0; w < NT / 64; w++) s += part[w];
     *norm = sqrt(s);
     const double f = max_norm / (*norm + eps);
-    return *norm < __builtin_huge_val() && f < 1.0 ? f : 1.0;          // (a norm that is no number: as it is)
+    return *norm < __builtin_huge_val() && f < 1.0 ? f : 1.0;          // (infinite or no number: as it is)
 }
 
 // one workgroup
@@ -92,6 +92,12 @@ __global__ void __launch_bounds__(1024) norm_kernel(const double* partial, int n
     }
 }
 
+// a 64-bit product rounded to T, once (a bf16 number is one of fp32 too)
+template <typename T>
+__device__ __forceinline__ float rounded(double v) {
+    if constexpr (sizeof(T) == 2) return (float)(__bf16)v;
+    else return (float)v;
+}
 template <typename T>
 __device__ __forceinline__ void scale(const T* p, T* o, int count, double f) {
     constexpr int V = VecOf<T>::V;
@@ -102,14 +108,14 @@ __device__ __forceinline__ void scale(const T* p, T* o, int count, double f) {
             float x[V];
             ldv<V>(p + i, x);
 #pragma unroll
-            for (int j = 0; j < V; j++) x[j] = (float)(f * (double)x[j]);
+            for (int j = 0; j < V; j++) x[j] = rounded<T>(f * (double)x[j]);
             stv<V>(o + i, x);
         }
     }
     for (int i = head + (int)threadIdx.x; i < count; i += kThreads) {
         float x[1];
         ldv<1>(p + i, x);
-        x[0] = (float)(f * (double)x[0]);
+        x[0] = rounded<T>(f * (double)x[0]);
         stv<1>(o + i, x);
     }
 }

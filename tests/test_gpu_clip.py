@@ -158,6 +158,34 @@ def test_large_tiles_and_fixed_order(ctx):
     t.close()
 
 
+def to_bf16(v):
+    """64-bit values in bf16's normal range, rounded to its 8 bits once, ties to even."""
+    m, e = np.frexp(v)
+    return np.ldexp(np.rint(m * 256.0) / 256.0, e)
+
+
+@pytest.mark.parametrize("n", [1, 100003])
+@pytest.mark.parametrize("factor", [0.5 * (1 + 3 * 2.0 ** -8) * (1 - 2.0 ** -40), 0.5 * (1 + 2.0 ** -8) * (1 + 2.0 ** -40), 0.3, 1.0 / 3.0])
+def test_bf16_results_are_rounded_once(ctx, n, factor):
+    """Products next to the middle between two bf16 numbers, nearer to it than fp32 can tell: rounded to fp32 on the way they would fall on it."""
+    from paper_2504_13236_amd import tiled
+    r = np.random.default_rng(11)
+    g = np.zeros(n) if n > 1 else np.ones(1)
+    if n > 1:
+        # one 1.0 makes up the norm, next to which the squares of the others vanish in 64 bits
+        g = to_bf16(2.0 ** -60 * (1.0 + r.random(n)) * r.choice([-1.0, 1.0], n))
+        g[n // 2], g[n // 3] = 1.0, -2.0 ** -60
+    t, o = tiled.TiledTensor.from_numpy(ctx, g, (1000,), "bf16"), tiled.TiledTensor.zeros(ctx, (n,), (1000,), "bf16")
+    norm = torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    tiled.clip_grad_norm(ctx, [t], norm, O=[o], max_norm=factor, eps=0.0)
+    got = o.download().astype(np.float64)
+    assert float(norm) == 1.0
+    assert np.array_equal(got, to_bf16(g * factor))
+    t.close()
+    o.close()
+
+
 def test_a_small_tile_beside_one_of_more_than_2_31_elements(ctx):
     """Tiles of 65536 x 32770 bf16 elements and what is left, 65536 x 1: the memory behind the small one is not looked at."""
     from paper_2504_13236_amd import capi, tiled
