@@ -605,7 +605,7 @@ NNT_API int32_t nnt_sample_tokens(nnt_ctx* ctx, const nnt_sample_cfg* cfg, nnt_t
  * G: n tensors, fp32 or bf16 each, of any shapes, each given once; tiles that are not there count as zeros.  O: n tensors with
  * the types, shapes and tilings of G, O[k] may be G[k]; or NULL: the norm alone.  norm: device float, which the caller must not reuse before nnt_wait or a later
  * operation on one of O (or G).  Sums are in 64 bits, in a fixed order; each result is rounded to its type once.  An infinite or NaN norm
- * leaves the gradients as they are.  max_norm > 0 (infinity: not clipped), eps >= 0.  One task; it uses the context's
+ * leaves the gradients as they are; one that is finite in 64 bits but beyond fp32 clips, and the caller is told infinity.  max_norm > 0 (infinity: not clipped), eps >= 0.  One task; it uses the context's
  * per-stream scratch, which must exist before a graph capture (run the call once). */
 typedef struct nnt_clip_cfg {
     double max_norm, eps;

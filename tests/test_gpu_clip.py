@@ -186,6 +186,22 @@ def test_bf16_results_are_rounded_once(ctx, n, factor):
     o.close()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_norm_beyond_fp32(ctx, dtype):
+    """Finite in 64 bits: the gradients are clipped by it, and the caller is told infinity."""
+    from paper_2504_13236_amd import tiled
+    G = [quant(np.full((40,), 3e38), dtype), quant(np.array([1e30, -2e38]), dtype)]
+    T = [tiled.TiledTensor.from_numpy(ctx, g, (16,), dtype) for g in G]
+    norm = torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    tiled.clip_grad_norm(ctx, T, norm, O=T, max_norm=1e3)
+    want, n = R.clip_grad_norm(G, 1e3, 1e-6)
+    assert 3.4028236e38 < n < np.inf and float(norm) == np.inf
+    for t, w in zip(T, want):
+        assert (np.abs(t.download() - w) <= HALF[dtype] * np.abs(w) * (1 + 1e-6)).all()
+        t.close()
+
+
 def test_a_small_tile_beside_one_of_more_than_2_31_elements(ctx):
     """Tiles of 65536 x 32770 bf16 elements and what is left, 65536 x 1: the memory behind the small one is not looked at."""
     from paper_2504_13236_amd import capi, tiled
