@@ -218,12 +218,22 @@ def muon_step(ctx, G, P, M, P_lowp=None, **hyper):
     capi.nnt_muon_step(ctx.h, C.byref(cfg), len(G), _handles(G), _handles(P), _handles(M), _handles(P_lowp) if P_lowp is not None else None)
 
 
+def _device_entries(ctx, name, t, dtype, n):
+    """The address of a device array that a call reads or writes the first n entries of."""
+    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError("%s: %d contiguous entries of %s wanted, given are %s of %s" % (name, n, dtype, tuple(t.shape), t.dtype))
+    if t.device != torch.device("cuda", ctx.device):
+        raise ValueError("%s: on %s, the context is on device %d" % (name, t.device, ctx.device))
+    return t.data_ptr()
+
+
 def clip_grad_norm(ctx, G, norm, O=None, max_norm=1.0, eps=1e-6):
     """Norm of all gradients (a list of tensors) into `norm` (device float), the clipped gradients into O (G itself: in place; None: norm only)."""
     if O is not None:
         _same_count(G, O)
     cfg = capi.nnt_clip_cfg(max_norm, eps)
-    capi.nnt_clip_grad_norm(ctx.h, C.byref(cfg), len(G), _handles(G), _handles(O) if O is not None else None, norm.data_ptr())
+    capi.nnt_clip_grad_norm(ctx.h, C.byref(cfg), len(G), _handles(G), _handles(O) if O is not None else None,
+                            _device_entries(ctx, "norm", norm, torch.float32, 1))
 
 
 def sample_cfg(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
@@ -232,11 +242,18 @@ def sample_cfg(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
 
 def sample_tokens(ctx, X, uniforms, tokens, logp=None, columns=None, **filters):
     """Draws a token from each column of the logits X that `columns` names (all of them), see sample_cfg for the filters."""
-    if len(tokens) != len(uniforms) or (logp is not None and len(logp) != len(tokens)) or (columns is not None and len(columns) != len(tokens)):
-        raise ValueError("columns, uniforms, tokens and logp must be of one length")
     cfg = sample_cfg(**filters)
-    capi.nnt_sample_tokens(ctx.h, C.byref(cfg), X.h, columns.data_ptr() if columns is not None else None, len(tokens), uniforms.data_ptr(),
-                           tokens.data_ptr(), logp.data_ptr() if logp is not None else None)
+    capi.nnt_sample_tokens(ctx.h, C.byref(cfg), X.h, *_drawn(ctx, uniforms, tokens, logp, columns))
+
+
+def _drawn(ctx, uniforms, tokens, logp, columns):
+    """Arguments of a draw: columns, n, uniforms, tokens, logp."""
+    n = len(tokens)
+    if any(t is not None and len(t) != n for t in (columns, uniforms, logp)):
+        raise ValueError("columns, uniforms, logp and what is drawn must be of one length")
+    return (_device_entries(ctx, "columns", columns, torch.int32, n) if columns is not None else None, n,
+            _device_entries(ctx, "uniforms", uniforms, torch.float32, n), _device_entries(ctx, "tokens", tokens, torch.int32, n),
+            _device_entries(ctx, "logp", logp, torch.float32, n) if logp is not None else None)
 
 
 def rotation_table(ctx, r, n_positions, base=10000.0):
@@ -280,8 +297,9 @@ class PagedCache:
 
     def cfg(self, start, count=None):
         """The calls' view of the cache: start, count are int32 device tensors of one entry per sequence (positions cached, new tokens)."""
-        return capi.nnt_cache_cfg(self.pages.data_ptr(), start.data_ptr(), count.data_ptr() if count is not None else None,
-                                  self.rotation.h.value if self.rotation is not None else None, self.N_h, self.N_kv, self.max_pages, self.window, self.rotate)
+        start, count = (_device_entries(self.ctx, name, t, torch.int32, self.N_b) if t is not None else None for name, t in (("start", start), ("count", count)))
+        return capi.nnt_cache_cfg(self.pages.data_ptr(), start, count, self.rotation.h.value if self.rotation is not None else None, self.N_h, self.N_kv,
+                                  self.max_pages, self.window, self.rotate)
 
     def append(self, QKV, start, count=None, layer=0):
         cfg = self.cfg(start, count)
@@ -377,7 +395,7 @@ class Gpt2Block:
     def clip(self, norm, max_norm=1.0, eps=1e-6):
         """The gradients clipped by their norm, which `norm` (device float) receives."""
         cfg = capi.nnt_clip_cfg(max_norm, eps)
-        capi.nnt_gpt2_block_clip(self.h, C.byref(cfg), norm.data_ptr())
+        capi.nnt_gpt2_block_clip(self.h, C.byref(cfg), _device_entries(self.ctx, "norm", norm, torch.float32, 1))
 
     def adam(self, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0):
         cfg = capi.nnt_adam_cfg(lr, beta1, beta2, eps, weight_decay)
@@ -434,7 +452,7 @@ class Gpt2Stack:
 
     def clip(self, norm, max_norm=1.0, eps=1e-6):
         cfg = capi.nnt_clip_cfg(max_norm, eps)
-        capi.nnt_gpt2_stack_clip(self.h, C.byref(cfg), norm.data_ptr())
+        capi.nnt_gpt2_stack_clip(self.h, C.byref(cfg), _device_entries(self.ctx, "norm", norm, torch.float32, 1))
 
     def adam(self, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0):
         cfg = capi.nnt_adam_cfg(lr, beta1, beta2, eps, weight_decay)
@@ -546,19 +564,18 @@ class Gpt2Model:
     def sample(self, cache, start, uniforms, next, count=None, columns=None, logp=None, positions=None, tokens=None, **filters):
         """One step of generation over a PagedCache: forward pass of the batch's tokens (or `tokens`) at `positions` (those of the last batch of
         positions), then a token drawn from each of the logits' columns that `columns` names (all of them) into `next`."""
-        if len(next) != len(uniforms) or (logp is not None and len(logp) != len(next)) or (columns is not None and len(columns) != len(next)):
-            raise ValueError("columns, uniforms, next and logp must be of one length")
         if len(cache.K) != len(self.blocks) or cache.N_b != self.N_b:
             raise ValueError("the cache is of another number of blocks or sequences")
+        tokens, positions = (_device_entries(self.ctx, name, t, torch.int32, self.N_s * self.N_b)
+                             for name, t in (("tokens", self.tokens if tokens is None else tokens), ("positions", self.pos if positions is None else positions)))
         ccfg, scfg = cache.cfg(start, count), sample_cfg(**filters)
-        capi.nnt_gpt2_model_sample(self.h, (self.tokens if tokens is None else tokens).data_ptr(), (self.pos if positions is None else positions).data_ptr(),
-                                   C.byref(ccfg), _handles(cache.K), _handles(cache.V), C.byref(scfg),
-                                   columns.data_ptr() if columns is not None else None, len(next), uniforms.data_ptr(), next.data_ptr(),
-                                   logp.data_ptr() if logp is not None else None)
+        columns, n, uniforms, next, logp = _drawn(self.ctx, uniforms, next, logp, columns)
+        capi.nnt_gpt2_model_sample(self.h, tokens, positions, C.byref(ccfg), _handles(cache.K), _handles(cache.V), C.byref(scfg), columns, n, uniforms, next,
+                                   logp)
 
     def clip(self, norm, max_norm=1.0, eps=1e-6):
         cfg = capi.nnt_clip_cfg(max_norm, eps)
-        capi.nnt_gpt2_model_clip(self.h, C.byref(cfg), norm.data_ptr())
+        capi.nnt_gpt2_model_clip(self.h, C.byref(cfg), _device_entries(self.ctx, "norm", norm, torch.float32, 1))
 
     def backward(self):
         capi.nnt_gpt2_model_backward(self.h)
