@@ -301,11 +301,17 @@ class PagedCache:
         return capi.nnt_cache_cfg(self.pages.data_ptr(), start, count, self.rotation.h.value if self.rotation is not None else None, self.N_h, self.N_kv,
                                   self.max_pages, self.window, self.rotate)
 
+    def _of(self, N_b, n_blocks=None):
+        if N_b != self.N_b or (n_blocks is not None and n_blocks != len(self.K)):
+            raise ValueError("the cache is of another number of blocks or sequences")
+
     def append(self, QKV, start, count=None, layer=0):
+        self._of(QKV.shape[2])
         cfg = self.cfg(start, count)
         capi.nnt_cache_append(self.ctx.h, C.byref(cfg), QKV.h, self.K[layer].h, self.V[layer].h)
 
     def attention(self, QKV, B, start, count=None, scale=None, layer=0):
+        self._of(QKV.shape[2])
         cfg = self.cfg(start, count)
         h = self.K[layer].shape[0]
         capi.nnt_cache_attention(self.ctx.h, C.byref(cfg), h ** -0.5 if scale is None else scale, QKV.h, self.K[layer].h, self.V[layer].h, B.h)
@@ -386,6 +392,7 @@ class Gpt2Block:
         capi.nnt_gpt2_block_forward(self.h, X.h, Out.h)
 
     def forward_cached(self, cache, X, Out, start, count=None, layer=0):
+        cache._of(self.act_shape[2])
         cfg = cache.cfg(start, count)
         capi.nnt_gpt2_block_forward_cached(self.h, C.byref(cfg), cache.K[layer].h, cache.V[layer].h, X.h, Out.h)
 
@@ -444,6 +451,7 @@ class Gpt2Stack:
         capi.nnt_gpt2_stack_forward(self.h)
 
     def forward_cached(self, cache, start, count=None):
+        cache._of(self.blocks[0].act_shape[2], len(self.blocks))
         cfg = cache.cfg(start, count)
         capi.nnt_gpt2_stack_forward_cached(self.h, C.byref(cfg), _handles(cache.K), _handles(cache.V))
 
@@ -564,8 +572,7 @@ class Gpt2Model:
     def sample(self, cache, start, uniforms, next, count=None, columns=None, logp=None, positions=None, tokens=None, **filters):
         """One step of generation over a PagedCache: forward pass of the batch's tokens (or `tokens`) at `positions` (those of the last batch of
         positions), then a token drawn from each of the logits' columns that `columns` names (all of them) into `next`."""
-        if len(cache.K) != len(self.blocks) or cache.N_b != self.N_b:
-            raise ValueError("the cache is of another number of blocks or sequences")
+        cache._of(self.N_b, len(self.blocks))
         tokens, positions = (_device_entries(self.ctx, name, t, torch.int32, self.N_s * self.N_b)
                              for name, t in (("tokens", self.tokens if tokens is None else tokens), ("positions", self.pos if positions is None else positions)))
         ccfg, scfg = cache.cfg(start, count), sample_cfg(**filters)

@@ -51,6 +51,25 @@ def test_a_count_is_looked_at_too(tiled, monkeypatch):
     assert looked == [("start", torch.int32, 3), ("count", torch.int32, 3)]
 
 
+def test_a_cache_of_other_sequences_or_blocks(tiled):
+    c, start = a_cache(tiled), i32(3)
+    with pytest.raises(ValueError, match="another number"):
+        c.append(SimpleNamespace(shape=(24, 1, 4), h=None), start)
+    with pytest.raises(ValueError, match="another number"):
+        c.attention(SimpleNamespace(shape=(24, 1, 2), h=None), None, start)
+    block = object.__new__(tiled.Gpt2Block)
+    block.ctx, block.h, block.act_shape = CTX, None, (8, 1, 4)
+    with pytest.raises(ValueError, match="another number"):
+        block.forward_cached(c, None, None, start)
+    block.act_shape = (8, 1, 3)
+    stack = object.__new__(tiled.Gpt2Stack)
+    stack.ctx, stack.h = CTX, None
+    for n in (1, 3):
+        stack.blocks = [block] * n
+        with pytest.raises(ValueError, match="another number"):
+            stack.forward_cached(c, start)
+
+
 @pytest.mark.parametrize("name,wrong", [("uniforms", torch.zeros(4, dtype=torch.float64)), ("uniforms", torch.zeros(4, dtype=torch.float16)), ("uniforms", torch.zeros(3)),
                                         ("uniforms", torch.zeros(8)[::2]), ("tokens", i32(4).long()), ("tokens", i32(8)[::2]), ("tokens", i32(5)), ("logp", torch.zeros(4).double()),
                                         ("logp", torch.zeros(5)), ("columns", i32(4).long()), ("columns", i32(3))])
