@@ -293,7 +293,7 @@ class PagedCache:
 
     def _upload(self):
         self.pages.copy_(torch.tensor([p + [-1] * (self.max_pages - len(p)) for p in self.of], dtype=torch.int32))
-        torch.cuda.synchronize()      # the context's streams do not order after torch's current stream
+        torch.cuda.synchronize(self.pages.device)      # the context's streams do not order after torch's current stream
 
     def cfg(self, start, count=None):
         """The calls' view of the cache: start, count are int32 device tensors of one entry per sequence (positions cached, new tokens)."""

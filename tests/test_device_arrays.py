@@ -100,3 +100,16 @@ def test_where_a_norm_goes(tiled, wrong):
         x.ctx, x.h = CTX, None
         with pytest.raises(ValueError, match="norm"):
             x.clip(wrong)
+
+
+def test_the_table_of_pages_is_there_when_reserve_returns(tiled, monkeypatch):
+    """The copy is waited for on the cache's device, whichever is the current one."""
+    waited = []
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda device=None: waited.append(device))
+    c = a_cache(tiled)
+    c.page, c.free, c.of = 4, [2, 1, 0], [[], [], []]
+    c.reserve([5, 0, 1])
+    assert c.pages.tolist() == [[0, 1, -1, -1], [-1] * 4, [2, -1, -1, -1]]
+    c.release(0)
+    assert c.pages.tolist()[0] == [-1] * 4
+    assert waited == [c.pages.device] * 2
