@@ -573,7 +573,7 @@ NNT_API int32_t nnt_cache_append(nnt_ctx* ctx, const nnt_cache_cfg* cfg, nnt_ten
  *   B[i,s,b,j] = sum_k V[i,k] P[k],  P = softmax over k of scale * sum_i K[i,k] rot(Q)[i,s,b,j],
  * over the positions k <= start[b] + s (and > start[b] + s - window) whose page is there; a query that sees none gives zeros.  Columns of
  * tokens that are not new (s >= count[b]) are left as they are.  QKV as above (only the queries are read), B: [N_h * h, N_s, N_b],
- * row tiles of whole heads, not K or V.  What is masked does not enter, infinities and NaN there included.  scale > 0.  The keys of long sequences are split over workgroups, whose
+ * row tiles of whole heads, not K or V.  Scores, weights and sums have fp32's bits, or two bf16 parts' (16 bits) where bf16 goes through matrix products; the result is rounded once.  What is masked does not enter, infinities and NaN there included.  scale > 0.  The keys of long sequences are split over workgroups, whose
  * partial results meet in the context's per-stream scratch (at most N_s * N_b * N_h * (h + 2) * 128 floats), which must exist before a graph
  * capture (run the call once). */
 NNT_API int32_t nnt_cache_attention(nnt_ctx* ctx, const nnt_cache_cfg* cfg, float scale, nnt_tensor* QKV, nnt_tensor* K,

@@ -7,8 +7,9 @@
 // A page is a tile (h, P, N_kv) of the cache's tensors: what one cached head reads of it is contiguous.
 //
 // The append is a copy; 58 MB take 17 us.  The attention reads what a (sequence, cached head) pair has cached once for all query rows of the pair, up to 128 of them,
-// and is bound by that read while there are few: 510 MB of 64 sequences, one row each, 84 us; 535 MB of one sequence, four rows, 109 us (a large copy's rate would
-// be 103 and 108); 200 tokens of four sequences of up to 3200 keys, 25 heads of 64, 35 us.  Long axes are split over workgroups, whose partial results a second kernel joins; short calls (4.5 us for 100 keys) are launches.
+// and is bound by that read while there are few: 510 MB of 64 sequences, one row each, 84 us; 535 MB of one sequence, four turned rows, 107 us (a large copy's rate would
+// be 103 and 108); 200 tokens of four sequences of up to 3200 keys, 25 heads of 64, 35 us.  Long axes are split over workgroups, whose partial results a second kernel joins; short calls (4.5 us for 100
+// keys) are launches.  These figures are of calls one after the other on two streams, which overlap; the launches of a call that is waited for take 22, 98 and 5, 128 and 10, 50 and 8, and 7 us.
 #include "attention_tile.hpp"
 #include "device_util.hpp"
 #include "internal.hpp"
@@ -981,6 +982,7 @@ struct Cut {
 // heads up to 64 or 128 five and 33.  Passes of two states one after the other, in us, vector units -> matrix cores:
 //   one sequence of 131072 keys of 8 cached heads of 128 and 64 sequences of 2048 of 12 of 64:
 //   bf16, 2 rows 97 -> 99 and 67 -> 69, 4 rows 105 -> 99 and 86 -> 70, turned 107 -> 117 and 88 -> 80, 5 rows turned 194 -> 117 and 138 -> 81, 16 rows 387 -> 103 and 252 -> 74;  fp32, 16 rows 660 -> 660 and 321 -> 366, 32 rows 922 -> 660 and 567 -> 368;
+//   waited for, turned, 4 rows: 131072 keys 148 -> 138, 8 sequences of 16384 of 8 heads of 128 123 -> 132;
 //   filled up, 64 sequences, heads of 96 (4 cached ones, 1500 keys) and of 32 (8, 2048): bf16, 5 rows 63 -> 47 and 45 -> 49, 8 rows 65 -> 47 and 47 -> 49, 32 rows 234 -> 50 and 175 -> 50;
 //   12 cached ones, fp32, 16 rows 416 -> 762 and 184 -> 384, 32 rows 779 -> 764 and 330 -> 385, 100 rows 2390 -> 838 and 926 -> 508.
 Cut cut_of(const nnt_cache_cfg* cfg, const nnt_tensor* QKV, const nnt_tensor* K) {
@@ -994,8 +996,8 @@ Cut cut_of(const nnt_cache_cfg* cfg, const nnt_tensor* QKV, const nnt_tensor* K)
     u.lpk = h <= 32 ? 4 : h <= 64 ? 8 : h <= 128 ? 16 : 32;
     u.step = u.tile ? 64 : kWaves * (64 / u.lpk) * kUnroll;
     u.chunks = (int)((rows + u.R - 1) / u.R);
-    // The keys are split so that the launch fills the chip.  The matrix cores' kernel: with no more workgroups than it holds at a time (bf16, one row chunk of 131072 keys, 128 components:
-    // 512 workgroups 107 us, 768 134); the vector units': eight to a unit, or four that keep more registers (four rows: 768 174 us, 1024 155).
+    // The keys are split so that the launch fills the chip.  The matrix cores' kernel: with no more workgroups than it holds at a time (bf16, four rows of 131072 keys, 128 components:
+    // 512 workgroups 100 us, 768 103, waited for 120 and 151); the vector units': eight to a unit, or four that keep more registers (four rows: 768 174 us, 1024 155).
     const int64_t pairs = (int64_t)u.chunks * cfg->N_kv * N_b;
     const int64_t held = 256 * (bf16 ? (h > 64 ? TileShape<Bf16Traits<128>>::kResident : TileShape<Bf16Traits<64>>::kResident)
                                      : (h > 64 ? TileShape<F32Traits<128>>::kResident : TileShape<F32Traits<64>>::kResident));

@@ -7,6 +7,7 @@
 // depend on which workgroup came first.  Squares are taken and added in 64 bits: gradients of 1e-23 have squares below fp32's range, and
 // 64-bit multiply-adds run at half the fp32 rate, far from what bounds this.
 // 124.5 M fp32 gradients in 148 tensors: 286 us (1.49 GB at 5.2 TB/s: the second read begins with what the first ended with).  The twelve of a block of 64: 11 us, two launches.
+// (Calls one after the other; the launches of one that is waited for add up to 326 and 10 us.)
 #include "clip_pieces.hpp"
 #include "device_util.hpp"
 #include "internal.hpp"

@@ -9,15 +9,16 @@
 //
 // One workgroup per column.  T = 0 takes the largest in one read.  Else: no column is sorted; all filters come to one border (a logit, and the last number among equal ones), and the draw is one
 // pass over the column in the order of the numbers.  Where the border lies:
-//   bf16 columns of up to 65535: the column is counted by its 16 bits in LDS.  There are few different values, so weights,
-//     sums and borders are those of some thousand (value, count) pairs.
-//   top-k of up to 512, fp32: the k-th largest of the threads' largest logits is at most the k-th largest of all, and little more than k logits
-//     are at least as large: they are sorted in LDS.
+//   bf16 columns of more than 1024 vectors of eight: the column is counted in LDS by 5120 codes, the bits of what is neither tiny nor huge.  There are few different values, so weights,
+//     sums and borders are those of some thousand (value, count) pairs.  Columns with too much that has no code go the ways below.
+//   fp32 and shorter bf16 columns, top-k of up to half the workgroup's threads (128 for columns of up to 1024 vectors, 512 for longer fp32 ones): the k-th largest of the threads' largest logits is
+//     at most the k-th largest of all, and little more than k logits are at least as large: they are sorted in LDS.
 //   else: a histogram over 2048 equal parts of the column's range (which a monotone function of the logit picks, so a part is a run
 //     of the order); the part that holds the border is sorted in LDS, or, while it holds more than a list of 2048, divided again by the bits of its keys.
 //
 // Bound by instructions and LDS, not by memory: 1024 bf16 columns of 50304, top-p, 67 us (103 MB: 21 us at a copy's rate; before the last step 75, vector units 65 % busy, LDS 30 to 35 %), 64 fp32
-// columns of 100003, min-p, 26 us, one of 50304, top-k, 14 us.  More columns than units are what it is made for: a column over several of them would need a second launch.
+// columns of 100003, min-p, 26 us, one of 50304, top-k, 14 us.  These and the other figures here are of calls one after the other on two streams, which overlap where one does not fill the chip;
+// a call that is waited for, as in a generation that draws token after token, takes 82, 53 and 29 us.  More columns than units are what it is made for: a column over several of them would need a second launch.
 #include "colwise.hpp"
 #include "device_util.hpp"
 #include "internal.hpp"
@@ -632,7 +633,7 @@ __device__ __forceinline__ void select(const Column_<T, NT>& h, Parts& sp, float
     cut = cut_at<NT>(sp.list, max(0, sh.pos));
 }
 
-// top-k by the threads' largest logits (`mine`); the k largest are left sorted in the list.  false: more than a list of candidates.
+// top-k by the threads' largest logits (`mine`), k up to half their number; the k largest are left sorted in the list.  false: more than a list of candidates.
 template <typename T, int NT>
 __device__ __forceinline__ bool list_top_k(const Column_<T, NT>& h, Parts& sp, float mine, int k) {
     constexpr int V = Column_<T, NT>::V;
@@ -802,7 +803,7 @@ __global__ void __launch_bounds__(NT) sample_kernel(Sample a) {
 
 // ---------------------------------------------------------------- the largest logit
 // One read: each thread keeps its largest logit and the first vector that holds it, beside the sum of the exponentials (shifted by what it has seen so far).
-// Bound by memory: 1024 bf16 columns of 50304 take 20 us (103 MB, 5.2 TB/s), where the draw's two reads took 61, one column 4.9 (12.5).
+// Bound by memory: 1024 bf16 columns of 50304 take 20 us (103 MB, 5.2 TB/s), where the draw's two reads took 61, one column 4.9 (12.5; one call after the other).
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT) greedy_kernel(Sample a) {
     constexpr int V = RawVec<T>::V, NW = NT / 64;
