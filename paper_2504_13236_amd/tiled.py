@@ -242,8 +242,9 @@ def sample_cfg(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
 
 def sample_tokens(ctx, X, uniforms, tokens, logp=None, columns=None, **filters):
     """Draws a token from each column of the logits X that `columns` names (all of them), see sample_cfg for the filters."""
+    drawn = _drawn(ctx, uniforms, tokens, logp, columns)
     cfg = sample_cfg(**filters)
-    capi.nnt_sample_tokens(ctx.h, C.byref(cfg), X.h, *_drawn(ctx, uniforms, tokens, logp, columns))
+    capi.nnt_sample_tokens(ctx.h, C.byref(cfg), X.h, *drawn)
 
 
 def _drawn(ctx, uniforms, tokens, logp, columns):
